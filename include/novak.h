@@ -630,6 +630,121 @@ int64_t novak_build_adapt_order(const int32_t *tensor_first, int n, int64_t lead
 /* Text of the last error on this handle ("" if none).  Owned by the handle. */
 const char *novak_last_error(const novak_opt *opt);
 
+/* ---------------------------------------------------------------------------
+ * Training operators: what makes the gradients that novak_step takes, with the
+ * activations that a backward pass needs kept in 8 bits.
+ *
+ * These calls take no handle.  Every call enqueues on `stream` (a cudaStream_t of
+ * the CURRENT device, on which the buffers live; NULL: its default stream),
+ * allocates nothing and does not synchronise.  All buffers are the caller's;
+ * nothing is kept between calls.  May be captured into a CUDA graph and called
+ * from several threads.  Results are the same bits from run to
+ * run on one kind of GPU (no floating-point atomics).  On an error nothing was
+ * enqueued (but for NOVAK_ECUDA), and novak_ops_error() has the reason.
+ *
+ * A matrix is `rows` rows of `cols` elements, each row contiguous and `stride`
+ * elements behind the one before (stride >= cols; it may be anything where
+ * rows <= 1); its base is aligned to its element.  rows = 0 is allowed and
+ * leaves weight gradients of zeros.  Bases aligned to 16 bytes with strides of a
+ * multiple of 16 bytes run on 128-bit accesses, others element by element.
+ * Statistics and sums are held in fp32; a result is rounded once, to nearest
+ * even, where it is stored as bf16. */
+enum { NOVAK_TYPE_F32 = 0, NOVAK_TYPE_BF16 = 1 };
+
+/* The 8-bit form of a matrix.  32 consecutive elements of a row (the row's last
+ * ones padded with zeros) share one exponent byte E and the scale 2^(E - 127);
+ * element = code * scale, code in [-127, 127].  E is the biased fp32 exponent of
+ * the block's largest magnitude less 6 (at least 0), so that this magnitude lies
+ * in [64, 128) scales; a code is the element divided by the scale, which is
+ * exact, rounded to nearest even and clamped to 127 at either end.  The error is
+ * at most half a scale (at most one scale for an fp32 element above 127.5
+ * scales).  A block that holds an infinity or a NaN has E = 255, codes of 0, and
+ * stands for NaNs.  What a code stands for has 7 significant bits: bf16 holds it
+ * exactly (but below 2^-126, where bf16 is subnormal too).
+ *
+ * codes: rows x novak_act8_pitch(cols) bytes, 16-byte aligned; exps: rows x
+ * novak_act8_pitch(cols) / 32 bytes; both dense.  novak_act8_pitch: cols rounded
+ * up to a multiple of 32 (0 for cols < 1). */
+int64_t novak_act8_pitch(int64_t cols);
+
+/* codes, exps <- the 8-bit form of x (type NOVAK_TYPE_*). */
+int novak_act8_pack(const void *d_x, int64_t x_stride, int type, int8_t *d_codes, uint8_t *d_exps,
+                    int64_t rows, int64_t cols, void *stream);
+
+/* out <- what codes, exps stand for, rounded to `type`. */
+int novak_act8_unpack(const int8_t *d_codes, const uint8_t *d_exps, void *d_out, int64_t out_stride,
+                      int type, int64_t rows, int64_t cols, void *stream);
+
+/* Layer norm over the columns:
+ *     mean = sum(x) / cols, rstd = 1 / sqrt(sum((x - mean)^2) / cols + eps),
+ *     xhat = (x - mean) rstd, y = xhat weight + bias.
+ * x and y of `type`, weight and bias (cols elements; bias may be NULL: 0) of
+ * param_type, d_mean and d_rstd (rows fp32 each; either may be NULL).
+ * d_codes, d_exps (both or neither): the 8-bit form of xhat, which is all that
+ * the backward pass needs beside rstd, and from which the weight gradient of a
+ * linear layer behind the norm is formed too.  y may be x (in place).
+ * eps >= 0 and finite. */
+int novak_layer_norm(const void *d_x, int64_t x_stride, void *d_y, int64_t y_stride, int type,
+                     const void *d_weight, const void *d_bias, int param_type, double eps,
+                     float *d_mean, float *d_rstd, int8_t *d_codes, uint8_t *d_exps, int64_t rows,
+                     int64_t cols, void *stream);
+
+/* Its backward pass.  With g = dy weight:
+ *     dx = rstd (g - mean(g) - xhat mean(g xhat)),
+ *     dweight = sum over rows of dy xhat, dbias = sum over rows of dy.
+ * xhat comes from d_codes, d_exps (d_x and d_mean NULL) or is formed from d_x
+ * and d_mean (d_codes and d_exps NULL).  dy, dx and x of `type`; weight of
+ * param_type; dweight and dbias (either may be NULL) of grad_type.  dx may be dy
+ * (in place).  d_work: novak_layer_norm_backward_bytes(rows, cols) bytes, 16-byte
+ * aligned; its contents need not be anything and are nothing afterwards. */
+size_t novak_layer_norm_backward_bytes(int64_t rows, int64_t cols);
+int novak_layer_norm_backward(const void *d_dy, int64_t dy_stride, const void *d_x, int64_t x_stride,
+                              int type, const float *d_mean, const float *d_rstd,
+                              const int8_t *d_codes, const uint8_t *d_exps, const void *d_weight,
+                              int param_type, void *d_dx, int64_t dx_stride, void *d_dweight,
+                              void *d_dbias, int grad_type, void *d_work, size_t work_bytes,
+                              int64_t rows, int64_t cols, void *stream);
+
+/* Activation functions.  GELU: u Phi(u), Phi the normal distribution function;
+ * GELU_TANH: u (1 + tanh(sqrt(2/pi) (u + 0.044715 u^3))) / 2; SILU: u / (1 + e^-u). */
+enum { NOVAK_ACT_GELU = 0, NOVAK_ACT_GELU_TANH = 1, NOVAK_ACT_SILU = 2 };
+
+/* a = f(u), and, where the pointers are not NULL (codes and exps together), the
+ * 8-bit forms of u (for the backward pass) and of a as rounded to `type` (for
+ * the weight gradient of the layer behind).  d_a may be NULL, or d_u (in place). */
+int novak_activation(const void *d_u, int64_t u_stride, void *d_a, int64_t a_stride, int type, int kind,
+                     int8_t *d_u_codes, uint8_t *d_u_exps, int8_t *d_a_codes, uint8_t *d_a_exps,
+                     int64_t rows, int64_t cols, void *stream);
+
+/* du = da f'(u), u from its 8-bit form (d_u NULL) or as it is (codes and exps
+ * NULL).  da, du and u of `type`; du may be da (in place). */
+int novak_activation_backward(const void *d_da, int64_t da_stride, const void *d_u, int64_t u_stride,
+                              int type, int kind, const int8_t *d_codes, const uint8_t *d_exps,
+                              void *d_du, int64_t du_stride, int64_t rows, int64_t cols, void *stream);
+
+/* Weight and bias gradient of a linear layer y = h W^T + b (W: n_out x n_in, as
+ * the framework's parameters are laid out) from the 8-bit form of its input:
+ *     dW[n, k] = sum over rows t of dy[t, n] h[t, k],  db[n] = sum of dy[t, n].
+ * h is what codes, exps (rows x n_in) stand for, or, with d_weight, d_bias
+ * (n_in elements of param_type, both or neither), h = xhat weight + bias with
+ * xhat what they stand for: the output of the layer norm that left them.
+ * dy of `type`; dW (dense) and db (may be NULL) of grad_type.  Products with a
+ * bf16 dy are exact and summed in fp32 on the tensor cores; an fp32 dy is taken
+ * as the sum of three bf16 parts, which hold its 24 bits.
+ * d_work: novak_linear_weight_grad_bytes(...) bytes, 256-byte aligned (0 bytes:
+ * may be NULL). */
+size_t novak_linear_weight_grad_bytes(const void *d_dy, int64_t dy_stride, int type, int64_t rows,
+                                      int64_t n_out, int64_t n_in);
+int novak_linear_weight_grad(const void *d_dy, int64_t dy_stride, int type, const int8_t *d_codes,
+                             const uint8_t *d_exps, const void *d_weight, const void *d_bias,
+                             int param_type, void *d_dw, void *d_db, int grad_type, void *d_work,
+                             size_t work_bytes, int64_t rows, int64_t n_out, int64_t n_in,
+                             void *stream);
+
+/* Text of the last error of a training operator on the calling thread ("" if
+ * none).  Valid until the thread's next such call. */
+const char *novak_ops_error(void);
+
 #ifdef __cplusplus
 }
 #endif

@@ -33,6 +33,8 @@ NOVAK_LOOKAHEAD_LAST, NOVAK_LOOKAHEAD_TRAJ_MEAN = 0, 1
  NOVAK_OPT_GRAPH_CAPTURABLE, NOVAK_OPT_CENTRALIZE_IN_STEP, NOVAK_OPT_LAYER_ADAPTATION_IN_STEP,
  NOVAK_OPT_LAYER_ADAPTATION_LEAD, NOVAK_OPT_LAYER_ADAPTATION_GROUP) = range(1, 28)
 NOVAK_MOMENT_F32, NOVAK_MOMENT_BF16 = 0, 1
+NOVAK_TYPE_F32, NOVAK_TYPE_BF16 = 0, 1
+NOVAK_ACT_GELU, NOVAK_ACT_GELU_TANH, NOVAK_ACT_SILU = range(3)
 NOVAK_WARN_TRUE_DOWNGRADED, NOVAK_WARN_SCALAR_PATH, NOVAK_WARN_NARROW_GRADIENT = 1, 2, 4
 
 _STATUS = {0: "NOVAK_OK", 1: "NOVAK_EINVAL", 2: "NOVAK_ESTATE", 3: "NOVAK_ECUDA", 4: "NOVAK_ENOMEM"}
@@ -80,6 +82,8 @@ class NovakError(RuntimeError):
 
 
 _lib = None
+_OPTIONAL_ELSEWHERE = ("novak_build_", "novak_act8_", "novak_layer_norm", "novak_activation",
+                       "novak_linear_weight_grad", "novak_ops_error")
 
 
 def load_library(path: str | None = None) -> ctypes.CDLL:
@@ -140,14 +144,33 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
         "novak_build_row_units": (c_int64, [i64p, i64p, c_int, POINTER(c_int32), i64p, i64p, i64p,
                                             i64p, c_int64]),
         "novak_last_error": (c_char_p, [vp]),
+        # training operators (wrapped by ops.py)
+        "novak_act8_pitch": (c_int64, [c_int64]),
+        "novak_act8_pack": (c_int, [vp, c_int64, c_int, vp, vp, c_int64, c_int64, vp]),
+        "novak_act8_unpack": (c_int, [vp, vp, vp, c_int64, c_int, c_int64, c_int64, vp]),
+        "novak_layer_norm": (c_int, [vp, c_int64, vp, c_int64, c_int, vp, vp, c_int, c_double, vp, vp,
+                                     vp, vp, c_int64, c_int64, vp]),
+        "novak_layer_norm_backward_bytes": (c_size_t, [c_int64, c_int64]),
+        "novak_layer_norm_backward": (c_int, [vp, c_int64, vp, c_int64, c_int, vp, vp, vp, vp, vp, c_int,
+                                              vp, c_int64, vp, vp, c_int, vp, c_size_t, c_int64,
+                                              c_int64, vp]),
+        "novak_activation": (c_int, [vp, c_int64, vp, c_int64, c_int, c_int, vp, vp, vp, vp, c_int64,
+                                     c_int64, vp]),
+        "novak_activation_backward": (c_int, [vp, c_int64, vp, c_int64, c_int, c_int, vp, vp, vp,
+                                              c_int64, c_int64, c_int64, vp]),
+        "novak_linear_weight_grad_bytes": (c_size_t, [vp, c_int64, c_int, c_int64, c_int64, c_int64]),
+        "novak_linear_weight_grad": (c_int, [vp, c_int64, c_int, vp, vp, vp, vp, c_int, vp, vp, c_int,
+                                             vp, c_size_t, c_int64, c_int64, c_int64, vp]),
+        "novak_ops_error": (c_char_p, []),
     }
     for name, (res, args) in sigs.items():
         try:
             fn = getattr(lib, name)
         except AttributeError:
             # an alternative build given by path (tuning, A/B against an older build) may
-            # lack the host-only table-builder hooks; the library proper must have everything
-            if path != _build.LIB and name.startswith("novak_build_"):
+            # lack the host-only table-builder hooks and the training operators; the library
+            # proper must have everything
+            if path != _build.LIB and name.startswith(_OPTIONAL_ELSEWHERE):
                 continue
             raise
         fn.restype = res

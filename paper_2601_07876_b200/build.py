@@ -21,7 +21,8 @@ LIB = os.path.join(PKG, "libnovak.so")
 PRE_MODES = tuple(range(16))
 DYN_PRE_MODES = (0, 1, 2, 4, 5, 6, 8, 9, 10, 12, 13, 14)   # no row-owning form (mode 3)
 PLAIN_SOURCES = ("novak_host.cpp", "novak_host_device.cpp", "novak_host_step.cpp", "novak_launch.cu", "novak_launch_adapt.cu",
-                 "novak_grad_stats.cu", "novak_trust_stats.cu", "novak_nesterov.cu", "novak_dyn.cu")
+                 "novak_grad_stats.cu", "novak_trust_stats.cu", "novak_nesterov.cu", "novak_dyn.cu",
+                 "novak_ops_host.cpp", "novak_act8.cu", "novak_layer_norm.cu", "novak_weight_grad.cu")
 # (source, object name, extra flags)
 UNITS = [(os.path.join(CSRC, f), f + ".o", []) for f in PLAIN_SOURCES]
 UNITS += [(os.path.join(CSRC, "novak_step_inst.cu"), f"novak_step_mode{m}.o",
@@ -36,6 +37,7 @@ HEADERS = [os.path.join(CSRC, "novak_internal.h"), os.path.join(CSRC, "novak_han
            os.path.join(CSRC, "novak_step_types.h"),
            os.path.join(CSRC, "novak_step_kernel.cuh"), os.path.join(CSRC, "novak_step_dyn.cuh"),
            os.path.join(CSRC, "novak_trust.cuh"), os.path.join(CSRC, "novak_step_adapt.cuh"),
+           os.path.join(CSRC, "novak_ops.h"), os.path.join(CSRC, "novak_ops.cuh"),
            os.path.join(ROOT, "include", "novak.h")]
 
 

@@ -662,7 +662,7 @@ enum { NOVAK_TYPE_F32 = 0, NOVAK_TYPE_BF16 = 1 };
  * stands for NaNs.  What a code stands for has 7 significant bits: bf16 holds it
  * exactly (but below 2^-126, where bf16 is subnormal too).
  *
- * codes: rows x novak_act8_pitch(cols) bytes, 16-byte aligned; exps: rows x
+ * codes: rows x novak_act8_pitch(cols) bytes, 32-byte aligned; exps: rows x
  * novak_act8_pitch(cols) / 32 bytes; both dense.  novak_act8_pitch: cols rounded
  * up to a multiple of 32 (0 for cols < 1). */
 int64_t novak_act8_pitch(int64_t cols);
@@ -731,15 +731,25 @@ int novak_activation_backward(const void *d_da, int64_t da_stride, const void *d
  * dy of `type`; dW (dense) and db (may be NULL) of grad_type.  Products with a
  * bf16 dy are exact and summed in fp32 on the tensor cores; an fp32 dy is taken
  * as the sum of three bf16 parts, which hold its 24 bits.
- * d_work: novak_linear_weight_grad_bytes(...) bytes, 256-byte aligned (0 bytes:
- * may be NULL). */
+ * d_work: novak_linear_weight_grad_bytes(...) bytes (affine: whether d_weight is
+ * given), 256-byte aligned (0 bytes: may be NULL); its contents need not be
+ * anything and are nothing afterwards.  Up to 2^31 - 1 rows, 2^22 outputs and
+ * inputs. */
 size_t novak_linear_weight_grad_bytes(const void *d_dy, int64_t dy_stride, int type, int64_t rows,
-                                      int64_t n_out, int64_t n_in);
+                                      int64_t n_out, int64_t n_in, int affine);
 int novak_linear_weight_grad(const void *d_dy, int64_t dy_stride, int type, const int8_t *d_codes,
                              const uint8_t *d_exps, const void *d_weight, const void *d_bias,
                              int param_type, void *d_dw, void *d_db, int grad_type, void *d_work,
                              size_t work_bytes, int64_t rows, int64_t n_out, int64_t n_in,
                              void *stream);
+
+/* The weight gradient's kernel has warps that wait for one another's copies and
+ * products.  Each wait is bounded (two seconds); where one runs out, which is a
+ * fault of this library or of the device, the part of dW that it was for is
+ * filled with NaNs and *count, the number of such waits on the current device
+ * since the library was loaded, goes up.  Copies 4 bytes from the device and
+ * SYNCHRONISES `stream`. */
+int novak_ops_gave_up(unsigned *count, void *stream);
 
 /* Text of the last error of a training operator on the calling thread ("" if
  * none).  Valid until the thread's next such call. */

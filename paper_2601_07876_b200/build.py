@@ -38,6 +38,7 @@ HEADERS = [os.path.join(CSRC, "novak_internal.h"), os.path.join(CSRC, "novak_han
            os.path.join(CSRC, "novak_step_kernel.cuh"), os.path.join(CSRC, "novak_step_dyn.cuh"),
            os.path.join(CSRC, "novak_trust.cuh"), os.path.join(CSRC, "novak_step_adapt.cuh"),
            os.path.join(CSRC, "novak_ops.h"), os.path.join(CSRC, "novak_ops.cuh"),
+           os.path.join(CSRC, "novak_tcgen05.cuh"),
            os.path.join(ROOT, "include", "novak.h")]
 
 

@@ -63,7 +63,7 @@ int check_codes(const char *name, const Codes &c, int64_t rows, bool needed)
     if (rows == 0) return NOVAK_OK;
     if ((c.codes == nullptr) != (c.exps == nullptr)) return refuse("%s: codes and exps come together", name);
     if (!c.codes) return needed ? refuse("%s: codes is NULL", name) : NOVAK_OK;
-    if (reinterpret_cast<uintptr_t>(c.codes) & 15u) return refuse("%s: codes are not 16-byte aligned", name);
+    if (reinterpret_cast<uintptr_t>(c.codes) & 31u) return refuse("%s: codes are not 32-byte aligned", name);
     return NOVAK_OK;
 }
 
@@ -95,6 +95,12 @@ Codes form(const int8_t *c, const uint8_t *e) { return Codes{const_cast<int8_t *
 extern "C" {
 
 const char *novak_ops_error(void) { return g_ops_error; }
+
+int novak_ops_gave_up(unsigned *count, void *stream)
+{
+    if (!count) return refuse("count is NULL");
+    return finish(weight_grad_gave_up(count, static_cast<cudaStream_t>(stream)), "novak_ops_gave_up");
+}
 
 int64_t novak_act8_pitch(int64_t cols) { return cols < 1 || cols > kMaxDim ? 0 : act_pitch(cols); }
 
@@ -221,11 +227,11 @@ int novak_activation_backward(const void *d_da, int64_t da_stride, const void *d
 }
 
 size_t novak_linear_weight_grad_bytes(const void *d_dy, int64_t dy_stride, int type, int64_t rows,
-                                      int64_t n_out, int64_t n_in)
+                                      int64_t n_out, int64_t n_in, int affine)
 {
     if (!is_type(type) || check_shape(rows, n_out) != NOVAK_OK || check_shape(rows, n_in) != NOVAK_OK ||
         check_shape(n_out, n_in) != NOVAK_OK) return 0;
-    return weight_grad_bytes(mat(d_dy, dy_stride), type, rows, n_out, n_in);
+    return weight_grad_bytes(mat(d_dy, dy_stride), type, rows, n_out, n_in, affine != 0);
 }
 
 int novak_linear_weight_grad(const void *d_dy, int64_t dy_stride, int type, const int8_t *d_codes,
@@ -250,7 +256,7 @@ int novak_linear_weight_grad(const void *d_dy, int64_t dy_stride, int type, cons
     CHECK(check_vector("dw", d_dw, grad_type));
     if (d_db) CHECK(check_vector("db", d_db, grad_type));
     const Mat dy = mat(d_dy, dy_stride);
-    const size_t need = weight_grad_bytes(dy, type, rows, n_out, n_in);
+    const size_t need = weight_grad_bytes(dy, type, rows, n_out, n_in, d_weight != nullptr);
     if (need > 0 && (!d_work || work_bytes < need || (reinterpret_cast<uintptr_t>(d_work) & 255u)))
         return refuse("work: %zu bytes, 256-byte aligned, are needed", need);
     cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -113,8 +113,8 @@ class Act8:
                              f"exps {tuple(exps.shape)}")
         if not codes.is_contiguous() or not exps.is_contiguous() or not codes.is_cuda or codes.device != exps.device:
             raise ValueError("codes and exps must be contiguous CUDA tensors of one device")
-        if codes.data_ptr() % 16 and rows:
-            raise ValueError("codes must be 16-byte aligned")
+        if codes.data_ptr() % 32 and rows:
+            raise ValueError("codes must be 32-byte aligned")
         self.codes, self.exps, self.rows, self.cols = codes, exps, rows, cols
         self.shape = (rows, cols) if shape is None else tuple(shape)
 
@@ -263,9 +263,10 @@ def activation_backward(da, saved, kind: str = "gelu"):
 
 
 @lru_cache(maxsize=1024)
-def _weight_grad_bytes(aligned: bool, stride: int, type_: int, rows: int, n_out: int, n_in: int) -> int:
+def _weight_grad_bytes(aligned: bool, stride: int, type_: int, rows: int, n_out: int, n_in: int,
+                       affine: bool) -> int:
     # only the address's alignment matters
-    return _library().novak_linear_weight_grad_bytes(256 if aligned else 2, stride, type_, rows, n_out, n_in)
+    return _library().novak_linear_weight_grad_bytes(256 if aligned else 2, stride, type_, rows, n_out, n_in, affine)
 
 
 def linear_weight_grad(dy, kept: Act8, affine=None, bias: bool = True, dtype=torch.float32):
@@ -290,7 +291,7 @@ def linear_weight_grad(dy, kept: Act8, affine=None, bias: bool = True, dtype=tor
     dw = torch.empty((n_out, n_in), dtype=dtype, device=dev)
     db = torch.empty(n_out, dtype=dtype, device=dev) if bias else None
     ptr = dy.data_ptr()
-    need = _weight_grad_bytes(ptr % 16 == 0, stride, type_, rows, n_out, n_in)
+    need = _weight_grad_bytes(ptr % 16 == 0, stride, type_, rows, n_out, n_in, affine is not None)
     work = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
     _enqueue("novak_linear_weight_grad", dev, ptr, stride, type_, kept.codes.data_ptr(), kept.exps.data_ptr(), w_ptr,
              b_ptr, param, dw.data_ptr(), db.data_ptr() if bias else None,

@@ -3,6 +3,10 @@
 //     y = xhat w + b;
 //     g = dy w, dx = rstd (g - sum(g)/C - xhat sum(g xhat)/C),
 //     dw = sum over rows of dy xhat, db = sum over rows of dy.
+// A row is read once and stays in registers: the deviations are summed after the mean
+// is known.  Three forms of each pass: rows that are 16-byte aligned and a multiple of
+// 8 elements long (8 at a time, arithmetic on pairs), other rows (one at a time,
+// neighbouring threads on neighbouring elements), and rows too long for registers.
 #include <algorithm>
 
 #include "novak_ops.cuh"
@@ -11,8 +15,9 @@ namespace novak {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kSplitRows = 128;      // rows per partial sum of a column
+constexpr int kSplitRows = 128;      // rows per partial sum of a column (long rows)
 constexpr int kColsPerCta = 32;
+constexpr int kSms = 148;
 
 __device__ __forceinline__ float param_at(const void *p, int type, int64_t i)
 {
@@ -26,6 +31,480 @@ __device__ __forceinline__ void store_param(void *p, int type, int64_t i, float 
     else static_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(v);
 }
 
+// Puts the 8-bit form of a thread's eight elements at `col` of `row` away; every thread
+// of the warp has to be here, with zeros beyond the row's elements.
+__device__ __forceinline__ void put_codes(const Codes &c, int64_t row, int64_t pitch, int64_t col, const F2 (&v)[4])
+{
+    uint32_t exp;
+    const uint2 q = quantize8(v, top_of(v), exp);
+    if (col < pitch) {
+        const int64_t at = row * pitch + col;
+        *reinterpret_cast<uint2 *>(c.codes + at) = q;
+        if ((threadIdx.x & 3) == 0) c.exps[at >> 5] = static_cast<uint8_t>(exp);
+    }
+}
+
+// Sums of N values over the G threads of a row, in every thread.  `scratch` (G > 32):
+// two halves of 32 N floats, used in turn, so that one barrier per call is enough.
+template <int G, int N>
+__device__ __forceinline__ void row_sums(float (&x)[N], float *scratch, int &turn)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = warp_sum(x[i]);
+    if constexpr (G > 32) {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        float *s = scratch + turn * 32 * N;
+        turn ^= 1;
+        if (lane == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) s[i * 32 + warp] = x[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float t = lane < G / 32 ? s[i * 32 + lane] : 0.0f;
+#pragma unroll
+            for (int d = G / 64; d > 0; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
+            x[i] = __shfl_sync(0xffffffffu, t, 0);
+        }
+    }
+}
+
+// Warps per CTA: where a row is a warp's (G = 32), what the registers of a row of NV
+// groups of V elements per lane leave room for.
+template <int G, int NV> __host__ __device__ constexpr int forward_warps() { return G == 32 ? 8 : G / 32; }
+template <int G, int NV, int V> __host__ __device__ constexpr int backward_warps()
+{
+    return G == 32 ? (NV * V <= 16 ? 16 : NV * V == 24 ? 12 : 8) : G / 32;
+}
+
+// A thread's columns of a vector that every row needs.  Where a row is a warp's, the
+// warps of a CTA share one copy in shared memory, in the order in which lanes read
+// it; elsewhere it stays in registers.
+template <int G, int NV> struct Held {
+    F2 r[NV][4];
+    __device__ __forceinline__ void load(const void *p, int type, int cols, float *)
+    {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int col = (i * G + static_cast<int>(threadIdx.x)) * 8;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                r[i][k] = p && col < cols ? F2(param_at(p, type, col + 2 * k), param_at(p, type, col + 2 * k + 1)) : F2(0.0f);
+        }
+    }
+    __device__ __forceinline__ void get(int i, F2 (&v)[4]) const
+    {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = r[i][k];
+    }
+};
+template <int NV> struct Held<32, NV> {
+    const float *s;
+    // element k of lane t's i-th group: four to a lane
+    static __device__ __forceinline__ int at(int i, int k, int t) { return ((i * 2 + k / 4) * 32 + t) * 4 + k % 4; }
+    __device__ __forceinline__ void load(const void *p, int type, int cols, float *smem)
+    {
+        for (int c = threadIdx.x; c < NV * 256; c += blockDim.x)
+            smem[at(c / 256, c % 8, c / 8 % 32)] = p && c < cols ? param_at(p, type, c) : 0.0f;
+        s = smem;
+    }
+    __device__ __forceinline__ void get(int i, F2 (&v)[4]) const
+    {
+        const int t = threadIdx.x & 31;
+        const float4 a = *reinterpret_cast<const float4 *>(s + at(i, 0, t)), b = *reinterpret_cast<const float4 *>(s + at(i, 4, t));
+        v[0] = F2(a.x, a.y);
+        v[1] = F2(a.z, a.w);
+        v[2] = F2(b.x, b.y);
+        v[3] = F2(b.z, b.w);
+    }
+};
+
+// ---- rows of aligned groups of 8 ------------------------------------------------------
+// G threads per row, NV groups of 8 each; the next row is on its way while this one is
+// worked on.
+template <int TYPE, int G, int NV>
+__global__ void __launch_bounds__(32 * forward_warps<G, NV>()) novak_layer_norm_kernel(NormArgs a)
+{
+    using T = typename Elem<TYPE>::T;
+    __shared__ float scratch[G == 32 ? 1 : 2 * 32];
+    __shared__ __align__(16) float held[G == 32 ? 2 * NV * 256 : 4];
+    int turn = 0;
+    const int t = G == 32 ? threadIdx.x & 31 : threadIdx.x, sub = G == 32 ? threadIdx.x >> 5 : 0;
+    constexpr int kSubs = G == 32 ? forward_warps<G, NV>() : 1;
+    const int cols = static_cast<int>(a.cols), pitch = (cols + 31) / 32 * 32;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * kSubs;
+    const float inv_cols = 1.0f / static_cast<float>(cols);
+    int64_t row = static_cast<int64_t>(blockIdx.x) * kSubs + sub;
+    const T *x = static_cast<const T *>(a.x.ptr) + row * a.x.stride + t * 8;
+    T *y = static_cast<T *>(a.y.ptr) + row * a.y.stride + t * 8;
+    bool in[NV];                // groups inside the row
+    Eight<TYPE> raw[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        in[i] = (i * G + t) * 8 < cols;
+        raw[i].zero();
+        if (in[i] && row < a.rows) raw[i].load(x + i * G * 8);
+    }
+    Held<G, NV> weight, bias;
+    weight.load(a.weight, a.param_type, cols, held);
+    bias.load(a.bias, a.param_type, cols, held + (G == 32 ? NV * 256 : 0));
+    if constexpr (G == 32) __syncthreads();
+    for (; row < a.rows; row += step, y += step * a.y.stride) {
+        F2 v[NV][4], sum(0.0f);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            raw[i].get(v[i]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum = sum + v[i][k];
+        }
+        x += step * a.x.stride;
+        if (row + step < a.rows)
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (in[i]) raw[i].load(x + i * G * 8);
+        float s[1] = {sum.lo() + sum.hi()};
+        row_sums<G, 1>(s, scratch, turn);
+        const float mean = s[0] * inv_cols;
+        sum = F2(0.0f);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const F2 m(in[i] ? -mean : 0.0f);           // zeros stay zeros beyond the row
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                v[i][k] = v[i][k] + m;
+                sum = fma2(v[i][k], v[i][k], sum);
+            }
+        }
+        s[0] = sum.lo() + sum.hi();
+        row_sums<G, 1>(s, scratch, turn);
+        const float rstd = rsqrtf(fmaf(s[0], inv_cols, a.eps));
+        if (t == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+        const F2 r(rstd);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            F2 o[4], w[4], b[4];
+            weight.get(i, w);
+            bias.get(i, b);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                v[i][k] = v[i][k] * r;
+                o[k] = fma2(v[i][k], w[k], b[k]);
+            }
+            Eight<TYPE> out;
+            out.set(o);
+            if (in[i]) out.store(y + i * G * 8);
+            // (a row with an infinity or NaN in it has nothing but NaNs)
+            if (a.codes.codes) put_codes(a.codes, row, pitch, (i * G + t) * 8, v[i]);
+        }
+    }
+}
+
+// The backward pass in the same manner: dy and xhat are read once, a thread's columns
+// of dw and db are added up in registers over the CTA's rows and go to
+// work[CTA][2][cols], which novak_layer_norm_finish_kernel adds up in order.
+template <int TYPE, int G, int NV, bool FROM8>
+__global__ void __launch_bounds__(32 * backward_warps<G, NV, 8>()) novak_layer_norm_back_kernel(NormBackArgs a)
+{
+    using T = typename Elem<TYPE>::T;
+    __shared__ float scratch[G == 32 ? 1 : 4 * 32];
+    extern __shared__ __align__(16) float held[];       // warps: the weight, then the warps' column sums
+    int turn = 0;
+    const int t = G == 32 ? threadIdx.x & 31 : threadIdx.x, sub = G == 32 ? threadIdx.x >> 5 : 0;
+    constexpr int kWarps = backward_warps<G, NV, 8>(), kSubs = G == 32 ? kWarps : 1;
+    asm volatile("griddepcontrol.launch_dependents;");
+    const int cols = static_cast<int>(a.cols), pitch = (cols + 31) / 32 * 32;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * kSubs;
+    const float inv_cols = 1.0f / static_cast<float>(cols);
+    int64_t row = static_cast<int64_t>(blockIdx.x) * kSubs + sub;
+    const T *dy = static_cast<const T *>(a.dy.ptr) + row * a.dy.stride + t * 8;
+    const T *x = static_cast<const T *>(a.x.ptr) + row * a.x.stride + t * 8;
+    const int8_t *codes = a.codes.codes + row * pitch + t * 8;
+    const uint8_t *exps = a.codes.exps + row * (pitch / 32) + t / 4;
+    T *dx = static_cast<T *>(a.dx.ptr) + row * a.dx.stride + t * 8;
+    bool in[NV];
+    Eight<TYPE> raw[NV], raw_x[FROM8 ? 1 : NV];
+    uint2 q[FROM8 ? NV : 1];
+    uint32_t e[FROM8 ? NV : 1];
+    float rstd = 0.0f, mean = 0.0f;
+    auto fetch = [&](int64_t at) {
+        if (at >= a.rows) return;
+        rstd = a.rstd[at];
+        if (!FROM8) mean = a.mean[at];
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (in[i]) {
+                raw[i].load(dy + i * G * 8);
+                if constexpr (FROM8) {
+                    q[i] = *reinterpret_cast<const uint2 *>(codes + i * G * 8);
+                    e[i] = exps[i * G / 4];
+                } else {
+                    raw_x[i].load(x + i * G * 8);
+                }
+            }
+    };
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        in[i] = (i * G + t) * 8 < cols;
+        raw[i].zero();
+        if constexpr (FROM8) {
+            q[i] = make_uint2(0, 0);
+            e[i] = 0;
+        } else {
+            raw_x[i].zero();
+        }
+    }
+    fetch(row);
+    Held<G, NV> weight;
+    weight.load(a.weight, a.param_type, cols, held);
+    if constexpr (G == 32) __syncthreads();
+    F2 dw[NV][4], db[NV][4];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) dw[i][k] = db[i][k] = F2(0.0f);
+    for (; row < a.rows; row += step, dx += step * a.dx.stride) {
+        // (beyond the row dy, codes or x, and the weight are zeros: xhat is finite there)
+        F2 g[NV][4], xh[NV][4], s0(0.0f), s1(0.0f);
+        const float r = rstd;
+        const F2 r2(r), m2(-mean);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            raw[i].get(g[i]);
+            if constexpr (FROM8) dequantize8(q[i], e[i], xh[i]);
+            else raw_x[i].get(xh[i]);
+            F2 w[4];
+            weight.get(i, w);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (!FROM8) xh[i][k] = (xh[i][k] + m2) * r2;
+                dw[i][k] = fma2(g[i][k], xh[i][k], dw[i][k]);
+                db[i][k] = db[i][k] + g[i][k];
+                g[i][k] = g[i][k] * w[k];
+                s0 = s0 + g[i][k];
+                s1 = fma2(g[i][k], xh[i][k], s1);
+            }
+        }
+        dy += step * a.dy.stride;
+        if constexpr (FROM8) {
+            codes += step * pitch;
+            exps += step * (pitch / 32);
+        } else {
+            x += step * a.x.stride;
+        }
+        fetch(row + step);
+        float s[2] = {s0.lo() + s0.hi(), s1.lo() + s1.hi()};
+        row_sums<G, 2>(s, scratch, turn);
+        const F2 a1(-s[1] * inv_cols * r), a0(-s[0] * inv_cols * r);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) g[i][k] = fma2(g[i][k], r2, fma2(xh[i][k], a1, a0));
+            Eight<TYPE> out;
+            out.set(g[i]);
+            if (in[i]) out.store(dx + i * G * 8);
+        }
+    }
+    if (!a.dweight && !a.dbias) return;
+    float *out = a.work + static_cast<int64_t>(blockIdx.x) * 2 * cols;
+    if constexpr (G == 32) {
+        float *part = held + NV * 256;
+        for (int which = 0; which < 2; ++which) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const F2 lo = which ? db[i][2 * k] : dw[i][2 * k], hi = which ? db[i][2 * k + 1] : dw[i][2 * k + 1];
+                    *reinterpret_cast<float4 *>(part + sub * NV * 256 + Held<G, NV>::at(i, 4 * k, t)) =
+                        make_float4(lo.lo(), lo.hi(), hi.lo(), hi.hi());
+                }
+            __syncthreads();
+            for (int c = threadIdx.x; c < cols; c += blockDim.x) {
+                const int at = Held<G, NV>::at(c / 256, c % 8, c / 8 % 32);
+                float sum = 0.0f;
+#pragma unroll
+                for (int p = 0; p < kWarps; ++p) sum += part[p * NV * 256 + at];
+                out[which * cols + c] = sum;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (in[i])
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int col = (i * G + t) * 8 + 2 * k;
+                    out[col] = dw[i][k].lo();
+                    out[col + 1] = dw[i][k].hi();
+                    out[cols + col] = db[i][k].lo();
+                    out[cols + col + 1] = db[i][k].hi();
+                }
+    }
+}
+
+// ---- other rows: one element at a time ---------------------------------------------------
+// Element (i G + t) is thread t's i-th; a warp's i-th elements are a block of 32.
+template <int TYPE, int G, int NV>
+__global__ void __launch_bounds__(32 * forward_warps<G, NV>()) novak_layer_norm_narrow_kernel(NormArgs a)
+{
+    using T = typename Elem<TYPE>::T;
+    __shared__ float scratch[G == 32 ? 1 : 2 * 32];
+    int turn = 0;
+    const int t = G == 32 ? threadIdx.x & 31 : threadIdx.x, sub = G == 32 ? threadIdx.x >> 5 : 0;
+    constexpr int kSubs = G == 32 ? forward_warps<G, NV>() : 1;
+    const int cols = static_cast<int>(a.cols), pitch = (cols + 31) / 32 * 32;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * kSubs;
+    const float inv_cols = 1.0f / static_cast<float>(cols);
+    int64_t row = static_cast<int64_t>(blockIdx.x) * kSubs + sub;
+    const T *x = static_cast<const T *>(a.x.ptr) + row * a.x.stride + t;
+    T *y = static_cast<T *>(a.y.ptr) + row * a.y.stride + t;
+    T raw[NV];
+    auto fetch = [&](int64_t at) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) raw[i] = at < a.rows && i * G + t < cols ? x[i * G] : from_float<T>(0.0f);
+    };
+    fetch(row);
+    float w[NV], b[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        w[i] = i * G + t < cols ? param_at(a.weight, a.param_type, i * G + t) : 0.0f;
+        b[i] = a.bias && i * G + t < cols ? param_at(a.bias, a.param_type, i * G + t) : 0.0f;
+    }
+    for (; row < a.rows; row += step, y += step * a.y.stride) {
+        float v[NV], s[1] = {0.0f};
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            v[i] = to_float(raw[i]);
+            s[0] += v[i];
+        }
+        x += step * a.x.stride;
+        fetch(row + step);
+        row_sums<G, 1>(s, scratch, turn);
+        const float mean = s[0] * inv_cols;
+        s[0] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            v[i] = i * G + t < cols ? v[i] - mean : 0.0f;
+            s[0] = fmaf(v[i], v[i], s[0]);
+        }
+        row_sums<G, 1>(s, scratch, turn);
+        const float rstd = rsqrtf(fmaf(s[0], inv_cols, a.eps));
+        if (t == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            v[i] *= rstd;
+            if (i * G + t < cols) y[i * G] = from_float<T>(fmaf(v[i], w[i], b[i]));
+        }
+        if (a.codes.codes)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                if (i * G + t >= pitch) break;          // (whole warps)
+                uint32_t exp;
+                const uint8_t q = quantize1(v[i], exp);
+                const int64_t at = row * pitch + i * G + t;
+                a.codes.codes[at] = static_cast<int8_t>(q);
+                if ((threadIdx.x & 31) == 0) a.codes.exps[at >> 5] = static_cast<uint8_t>(exp);
+            }
+    }
+}
+
+template <int TYPE, int G, int NV, bool FROM8>
+__global__ void __launch_bounds__(32 * backward_warps<G, NV, 1>()) novak_layer_norm_back_narrow_kernel(NormBackArgs a)
+{
+    using T = typename Elem<TYPE>::T;
+    __shared__ float scratch[G == 32 ? 1 : 4 * 32];
+    __shared__ float part[G == 32 ? backward_warps<G, NV, 1>() : 1][G == 32 ? NV * 32 : 1];
+    int turn = 0;
+    const int t = G == 32 ? threadIdx.x & 31 : threadIdx.x, sub = G == 32 ? threadIdx.x >> 5 : 0;
+    constexpr int kWarps = backward_warps<G, NV, 1>(), kSubs = G == 32 ? kWarps : 1;
+    asm volatile("griddepcontrol.launch_dependents;");
+    const int cols = static_cast<int>(a.cols), pitch = (cols + 31) / 32 * 32;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * kSubs;
+    const float inv_cols = 1.0f / static_cast<float>(cols);
+    int64_t row = static_cast<int64_t>(blockIdx.x) * kSubs + sub;
+    T raw[NV], raw_x[FROM8 ? 1 : NV];
+    int8_t q[FROM8 ? NV : 1];
+    uint8_t e[FROM8 ? NV : 1];
+    float rstd = 0.0f, mean = 0.0f, w[NV], dw[NV], db[NV];
+    auto fetch = [&](int64_t at) {
+        if (at >= a.rows) return;
+        rstd = a.rstd[at];
+        if (!FROM8) mean = a.mean[at];
+        const T *dy = static_cast<const T *>(a.dy.ptr) + at * a.dy.stride + t;
+        const T *x = static_cast<const T *>(a.x.ptr) + at * a.x.stride + t;
+        const int64_t c = at * pitch + t;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i * G + t < cols) {
+                raw[i] = dy[i * G];
+                if constexpr (FROM8) {
+                    q[i] = a.codes.codes[c + i * G];
+                    e[i] = a.codes.exps[(c + i * G) >> 5];
+                } else {
+                    raw_x[i] = x[i * G];
+                }
+            }
+    };
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        raw[i] = from_float<T>(0.0f);
+        if constexpr (FROM8) q[i] = e[i] = 0;
+        else raw_x[i] = from_float<T>(0.0f);
+        w[i] = i * G + t < cols ? param_at(a.weight, a.param_type, i * G + t) : 0.0f;
+        dw[i] = db[i] = 0.0f;
+    }
+    fetch(row);
+    for (; row < a.rows; row += step) {
+        float g[NV], xh[NV], s[2] = {0.0f, 0.0f};
+        const float r = rstd, m = mean;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            g[i] = to_float(raw[i]);
+            if constexpr (FROM8) xh[i] = static_cast<float>(q[i]) * scale_of(e[i]);
+            else xh[i] = (to_float(raw_x[i]) - m) * r;
+            dw[i] = fmaf(g[i], xh[i], dw[i]);
+            db[i] += g[i];
+            g[i] *= w[i];
+            s[0] += g[i];
+            s[1] = fmaf(g[i], xh[i], s[1]);
+        }
+        fetch(row + step);
+        row_sums<G, 2>(s, scratch, turn);
+        const float a1 = -s[1] * inv_cols * r, a0 = -s[0] * inv_cols * r;
+        T *dx = static_cast<T *>(a.dx.ptr) + row * a.dx.stride + t;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i * G + t < cols) dx[i * G] = from_float<T>(fmaf(g[i], r, fmaf(xh[i], a1, a0)));
+    }
+    if (!a.dweight && !a.dbias) return;
+    float *out = a.work + static_cast<int64_t>(blockIdx.x) * 2 * cols;
+    for (int which = 0; which < 2; ++which) {
+        if constexpr (G == 32) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < NV; ++i) part[sub][i * 32 + t] = which ? db[i] : dw[i];
+            __syncthreads();
+            for (int c = threadIdx.x; c < cols; c += blockDim.x) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int p = 0; p < kWarps; ++p) sum += part[p][c];
+                out[which * cols + c] = sum;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (i * G + t < cols) out[which * cols + i * G + t] = which ? db[i] : dw[i];
+        }
+    }
+}
+
+// ---- rows too long for registers ---------------------------------------------------------
 // One CTA per row, any length: the row is read three times (from L2 after the
 // first time).
 template <int TYPE, bool WIDE>
@@ -71,12 +550,10 @@ __global__ void __launch_bounds__(kThreads) novak_layer_norm_long_kernel(NormArg
             }
             store8<WIDE>(y, c, a.cols, o);
             if (a.codes.codes) {
-                uint32_t exp;
-                const uint2 q = quantize8(v, exp);
-                if (c < pitch) {
-                    *reinterpret_cast<uint2 *>(a.codes.codes + row * pitch + c) = q;
-                    if ((threadIdx.x & 3) == 0) a.codes.exps[(row * pitch + c) >> 5] = static_cast<uint8_t>(exp);
-                }
+                F2 p[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) p[k] = F2(v[2 * k], v[2 * k + 1]);
+                put_codes(a.codes, row, pitch, c, p);
             }
         }
     }
@@ -173,19 +650,106 @@ __global__ void __launch_bounds__(kThreads) novak_layer_norm_columns_kernel(Norm
     }
 }
 
-// dw, db from the partial sums, in order.
-__global__ void __launch_bounds__(kThreads)
+// dw, db from the partial sums: 32 columns of one of the two per CTA, each warp every
+// 32nd sum in order, then the warps in order.
+constexpr int kFinishThreads = 1024;
+__global__ void __launch_bounds__(kFinishThreads)
 novak_layer_norm_finish_kernel(const float *work, int64_t splits, int64_t cols, void *dweight, void *dbias, int type)
 {
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    if (c >= cols) return;
-    float dw = 0.0f, db = 0.0f;
-    for (int64_t s = 0; s < splits; ++s) {
-        dw += work[(2 * s) * cols + c];
-        db += work[(2 * s + 1) * cols + c];
+    __shared__ float part[32][33];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, which = blockIdx.y;
+    const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + lane;
+    void *out = which ? dbias : dweight;
+    if (!out) return;
+    float sum = 0.0f;
+    if (c < cols) {
+        const float *src = work + which * cols + c;
+#pragma unroll 8
+        for (int64_t s = warp; s < splits; s += 32) sum += src[2 * s * cols];
     }
-    if (dweight) store_param(dweight, type, c, dw);
-    if (dbias) store_param(dbias, type, c, db);
+    part[lane][warp] = sum;
+    __syncthreads();
+    sum = warp_sum(part[warp][lane]);       // column `warp` of the 32
+    const int64_t mine = static_cast<int64_t>(blockIdx.x) * 32 + warp;
+    if (lane == 0 && mine < cols) store_param(out, type, mine, sum);
+}
+
+// How a row of `cols` elements is spread over G threads, NV groups each of 8 elements
+// (v = 8: 128-bit accesses and a multiple of 8) or of one.  false: too long for
+// registers.
+struct Spread {
+    int v, g, nv;
+};
+constexpr Spread kWide[] = {{8, 32, 1}, {8, 32, 2}, {8, 32, 3}, {8, 32, 4}, {8, 256, 1}, {8, 512, 1}, {8, 512, 2}};
+constexpr Spread kNarrow[] = {{1, 32, 8}, {1, 128, 8}, {1, 512, 8}, {1, 512, 16}};
+
+bool spread_for(bool is_wide, int64_t cols, Spread &s)
+{
+    const Spread *begin = is_wide ? kWide : kNarrow, *end = begin + (is_wide ? sizeof kWide : sizeof kNarrow) / sizeof(Spread);
+    for (const Spread *c = begin; c != end; ++c)
+        if (cols <= c->v * c->g * c->nv) {
+            s = *c;
+            return true;
+        }
+    return false;
+}
+
+#define NOVAK_WIDE(F) F(32, 1) F(32, 2) F(32, 3) F(32, 4) F(256, 1) F(512, 1) F(512, 2)
+#define NOVAK_NARROW(F) F(32, 8) F(128, 8) F(512, 8) F(512, 16)
+
+// CTAs of the backward pass (each leaves one partial sum per column): one per SM
+// where its warps have a row each, two where a row is the CTA's.
+int64_t back_ctas(int64_t rows, int64_t cols)
+{
+    return std::max<int64_t>(1, std::min<int64_t>(rows, kSms * (cols <= 1024 ? 1 : 2)));
+}
+
+template <typename Kernel, typename Args>
+cudaError_t run(Kernel kernel, int64_t grid, int threads, int smem, const Args &a, cudaStream_t stream)
+{
+    if (smem > 40 * 1024) {         // (48 KB less the kernels' own)
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return e;
+    }
+    kernel<<<static_cast<unsigned>(grid), threads, smem, stream>>>(a);
+    return cudaGetLastError();
+}
+
+template <int TYPE> cudaError_t forward(const NormArgs &a, const Spread &s, cudaStream_t stream)
+{
+#define NOVAK_GRID(G, NV) \
+    std::min<int64_t>((a.rows + (G == 32 ? forward_warps<G, NV>() : 1) - 1) / (G == 32 ? forward_warps<G, NV>() : 1), \
+                      kSms * (G == 32 ? 4 : 1024 / G))
+#define NOVAK_CASE(G, NV)                   \
+    if (s.v == 8 && s.g == G && s.nv == NV) \
+        return run(novak_layer_norm_kernel<TYPE, G, NV>, NOVAK_GRID(G, NV), 32 * forward_warps<G, NV>(), 0, a, stream);
+    NOVAK_WIDE(NOVAK_CASE)
+#undef NOVAK_CASE
+#define NOVAK_CASE(G, NV)                   \
+    if (s.v == 1 && s.g == G && s.nv == NV) \
+        return run(novak_layer_norm_narrow_kernel<TYPE, G, NV>, NOVAK_GRID(G, NV), 32 * forward_warps<G, NV>(), 0, a, stream);
+    NOVAK_NARROW(NOVAK_CASE)
+#undef NOVAK_CASE
+#undef NOVAK_GRID
+    return cudaErrorInvalidValue;
+}
+
+template <int TYPE, bool FROM8>
+cudaError_t backward(const NormBackArgs &a, const Spread &s, int64_t grid, cudaStream_t stream)
+{
+#define NOVAK_CASE(G, NV)                                                                                       \
+    if (s.v == 8 && s.g == G && s.nv == NV)                                                                     \
+        return run(novak_layer_norm_back_kernel<TYPE, G, NV, FROM8>, grid, 32 * backward_warps<G, NV, 8>(),     \
+                   G == 32 ? (1 + backward_warps<G, NV, 8>()) * NV * 256 * 4 : 0, a, stream);
+    NOVAK_WIDE(NOVAK_CASE)
+#undef NOVAK_CASE
+#define NOVAK_CASE(G, NV)                   \
+    if (s.v == 1 && s.g == G && s.nv == NV) \
+        return run(novak_layer_norm_back_narrow_kernel<TYPE, G, NV, FROM8>, grid, 32 * backward_warps<G, NV, 1>(), 0, a, stream);
+    NOVAK_NARROW(NOVAK_CASE)
+#undef NOVAK_CASE
+    return cudaErrorInvalidValue;
 }
 
 }  // namespace
@@ -193,7 +757,10 @@ novak_layer_norm_finish_kernel(const float *work, int64_t splits, int64_t cols, 
 cudaError_t launch_layer_norm(const NormArgs &a, cudaStream_t stream)
 {
     const bool w = wide(a.x, a.type, a.rows) && wide(a.y, a.type, a.rows);
-    const int grid = static_cast<int>(std::min<int64_t>(a.rows, 148 * 8));
+    Spread s;
+    if (spread_for(w && a.cols % 8 == 0, a.cols, s))
+        return a.type == NOVAK_TYPE_F32 ? forward<0>(a, s, stream) : forward<1>(a, s, stream);
+    const int grid = static_cast<int>(std::min<int64_t>(a.rows, kSms * 8));
     auto kernel = a.type == NOVAK_TYPE_F32
                       ? (w ? novak_layer_norm_long_kernel<0, true> : novak_layer_norm_long_kernel<0, false>)
                       : (w ? novak_layer_norm_long_kernel<1, true> : novak_layer_norm_long_kernel<1, false>);
@@ -201,31 +768,55 @@ cudaError_t launch_layer_norm(const NormArgs &a, cudaStream_t stream)
     return cudaGetLastError();
 }
 
+// Enough for either way of the backward pass: which one it is depends on alignment.
 size_t layer_norm_backward_bytes(int64_t rows, int64_t cols)
 {
-    return static_cast<size_t>((rows + kSplitRows - 1) / kSplitRows * 2 * cols) * sizeof(float);
+    const int64_t splits = (rows + kSplitRows - 1) / kSplitRows;
+    return static_cast<size_t>(std::max(splits, back_ctas(rows, cols)) * 2 * cols) * sizeof(float);
 }
 
 cudaError_t launch_layer_norm_backward(const NormBackArgs &a, cudaStream_t stream)
 {
     const bool w = wide(a.dy, a.type, a.rows) && wide(a.dx, a.type, a.rows) &&
                    (!a.x.ptr || wide(a.x, a.type, a.rows));
-    const int64_t splits = (a.rows + kSplitRows - 1) / kSplitRows;
-    const int t = a.type == NOVAK_TYPE_F32 ? 0 : 1;
-    if (a.rows > 0 && (a.dweight || a.dbias)) {
-        auto columns = t == 0 ? (w ? novak_layer_norm_columns_kernel<0, true> : novak_layer_norm_columns_kernel<0, false>)
-                              : (w ? novak_layer_norm_columns_kernel<1, true> : novak_layer_norm_columns_kernel<1, false>);
-        const dim3 grid(static_cast<unsigned>((a.cols + kColsPerCta - 1) / kColsPerCta), static_cast<unsigned>(splits));
-        columns<<<grid, kThreads, 0, stream>>>(a);
-    }
-    if (a.rows > 0) {
+    const bool sums = a.dweight || a.dbias;
+    int64_t splits = 0;
+    Spread s;
+    if (a.rows == 0) {
+    } else if (spread_for(w && a.cols % 8 == 0, a.cols, s)) {
+        splits = back_ctas(a.rows, a.cols);
+        const bool q = a.codes.codes != nullptr;
+        const cudaError_t e = a.type == NOVAK_TYPE_F32 ? (q ? backward<0, true>(a, s, splits, stream) : backward<0, false>(a, s, splits, stream))
+                                                       : (q ? backward<1, true>(a, s, splits, stream) : backward<1, false>(a, s, splits, stream));
+        if (e != cudaSuccess) return e;
+    } else {
+        splits = (a.rows + kSplitRows - 1) / kSplitRows;
+        const int t = a.type == NOVAK_TYPE_F32 ? 0 : 1;
+        if (sums) {         // first: dx may be written over dy
+            auto columns = t == 0 ? (w ? novak_layer_norm_columns_kernel<0, true> : novak_layer_norm_columns_kernel<0, false>)
+                                  : (w ? novak_layer_norm_columns_kernel<1, true> : novak_layer_norm_columns_kernel<1, false>);
+            const dim3 grid(static_cast<unsigned>((a.cols + kColsPerCta - 1) / kColsPerCta), static_cast<unsigned>(splits));
+            columns<<<grid, kThreads, 0, stream>>>(a);
+        }
         auto kernel = t == 0 ? (w ? novak_layer_norm_back_long_kernel<0, true> : novak_layer_norm_back_long_kernel<0, false>)
                              : (w ? novak_layer_norm_back_long_kernel<1, true> : novak_layer_norm_back_long_kernel<1, false>);
-        kernel<<<static_cast<int>(std::min<int64_t>(a.rows, 148 * 8)), kThreads, 0, stream>>>(a);
+        kernel<<<static_cast<int>(std::min<int64_t>(a.rows, kSms * 8)), kThreads, 0, stream>>>(a);
     }
-    if (a.dweight || a.dbias)
-        novak_layer_norm_finish_kernel<<<static_cast<unsigned>((a.cols + kThreads - 1) / kThreads), kThreads, 0, stream>>>(
-            a.work, splits, a.cols, a.dweight, a.dbias, a.grad_type);
+    if (sums) {
+        // its CTAs may come to be while the last rows are worked on, and wait for them
+        cudaLaunchConfig_t lc = {};
+        lc.gridDim = dim3(static_cast<unsigned>((a.cols + 31) / 32), 2);
+        lc.blockDim = dim3(kFinishThreads);
+        lc.stream = stream;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        lc.attrs = attr;
+        lc.numAttrs = a.rows > 0 ? 1 : 0;
+        const cudaError_t e = cudaLaunchKernelEx(&lc, novak_layer_norm_finish_kernel, static_cast<const float *>(a.work), splits, a.cols,
+                                                 a.dweight, a.dbias, a.grad_type);
+        if (e != cudaSuccess) return e;
+    }
     return cudaGetLastError();
 }
 

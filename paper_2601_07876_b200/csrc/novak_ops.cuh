@@ -22,6 +22,43 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(f
     return __float2bfloat16_rn(x);
 }
 
+// Two fp32 numbers per instruction.
+struct F2 {
+    uint64_t v;
+    __device__ __forceinline__ F2() {}
+    __device__ __forceinline__ F2(float lo, float hi) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi)); }
+    __device__ __forceinline__ explicit F2(float x) : F2(x, x) {}
+    __device__ __forceinline__ void get(float &lo, float &hi) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+    __device__ __forceinline__ float lo() const { float a, b; get(a, b); return a; }
+    __device__ __forceinline__ float hi() const { float a, b; get(a, b); return b; }
+};
+__device__ __forceinline__ F2 operator+(F2 a, F2 b)
+{
+    asm("add.rn.f32x2 %0, %0, %1;" : "+l"(a.v) : "l"(b.v));
+    return a;
+}
+__device__ __forceinline__ F2 operator*(F2 a, F2 b)
+{
+    asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(a.v) : "l"(b.v));
+    return a;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c)
+{
+    F2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return d;
+}
+// bf16 pair -> fp32 pair, and back (to nearest even)
+__device__ __forceinline__ F2 widen(uint32_t w) { return F2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ uint32_t narrow(F2 x)
+{
+    uint32_t r;
+    float lo, hi;
+    x.get(lo, hi);
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
 // Elements [col, col + 8) of a row, zeros from `cols` on.  WIDE: the row is
 // 16-byte aligned; col is a multiple of 8.  A group that the row's end cuts is
 // read element by element either way.
@@ -88,49 +125,155 @@ __device__ __forceinline__ void store8(__nv_bfloat16 *row, int64_t col, int64_t 
     }
 }
 
-// The 8-bit form of eight elements; the four threads of a quad (lanes 4i..4i+3,
-// all of which have to be here) hold one block of 32.  Returns the block's
-// exponent byte and the eight codes.
-__device__ __forceinline__ uint2 quantize8(const float (&v)[8], uint32_t &exp)
-{
-    // Magnitudes compare as integers, infinities above all numbers and NaNs
-    // above those: one maximum finds the exponent and what cannot be held.
-    uint32_t top = 0;
+// Eight consecutive elements of a 16-byte aligned row, as they are in memory.
+template <int TYPE> struct Eight;
+template <> struct Eight<NOVAK_TYPE_BF16> {
+    uint4 w;
+    __device__ __forceinline__ void zero() { w = make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { w = *reinterpret_cast<const uint4 *>(p); }
+    __device__ __forceinline__ void get(F2 (&v)[4]) const
+    {
+        v[0] = widen(w.x);
+        v[1] = widen(w.y);
+        v[2] = widen(w.z);
+        v[3] = widen(w.w);
+    }
+    // `v` as it is stored; the bits of the largest magnitude of the eight
+    __device__ __forceinline__ void set(const F2 (&v)[4]) { w = make_uint4(narrow(v[0]), narrow(v[1]), narrow(v[2]), narrow(v[3])); }
+    __device__ __forceinline__ void store(__nv_bfloat16 *p) const { *reinterpret_cast<uint4 *>(p) = w; }
+    __device__ __forceinline__ uint32_t top() const
+    {
+        const uint32_t m = 0x7fff7fffu;
+        const uint32_t t = __vmaxu2(__vmaxu2(w.x & m, w.y & m), __vmaxu2(w.z & m, w.w & m));
+        return max(t << 16, t & 0xffff0000u);
+    }
+};
+template <> struct Eight<NOVAK_TYPE_F32> {
+    F2 x[4];
+    __device__ __forceinline__ void zero() { x[0] = x[1] = x[2] = x[3] = F2(0.0f); }
+    __device__ __forceinline__ void load(const float *p)
+    {
+        const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
+        x[0] = F2(a.x, a.y);
+        x[1] = F2(a.z, a.w);
+        x[2] = F2(b.x, b.y);
+        x[3] = F2(b.z, b.w);
+    }
+    __device__ __forceinline__ void get(F2 (&v)[4]) const
+    {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+        for (int i = 0; i < 4; ++i) v[i] = x[i];
+    }
+    __device__ __forceinline__ void set(const F2 (&v)[4])
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = v[i];
+    }
+    __device__ __forceinline__ void store(float *p) const
+    {
+        *reinterpret_cast<float4 *>(p) = make_float4(x[0].lo(), x[0].hi(), x[1].lo(), x[1].hi());
+        *reinterpret_cast<float4 *>(p + 4) = make_float4(x[2].lo(), x[2].hi(), x[3].lo(), x[3].hi());
+    }
+    __device__ __forceinline__ uint32_t top() const
+    {
+        uint32_t t = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            t = max(t, max(__float_as_uint(x[i].lo()) & 0x7fffffffu, __float_as_uint(x[i].hi()) & 0x7fffffffu));
+        return t;
+    }
+};
+
+// Exponent byte of a block whose largest magnitude has these bits (an infinity or
+// NaN: 255), and the reciprocal of its scale.
+__device__ __forceinline__ uint32_t block_exp(uint32_t top)
+{
+    const uint32_t e = top >> 23;
+    return e == 255u ? 255u : max(e, 6u) - 6u;
+}
+__device__ __forceinline__ float inverse_scale(uint32_t exp)
+{
+    return __uint_as_float((254u - (exp == 255u ? 254u : exp)) << 23);
+}
+// 128 scales is the next exponent's; what rounds to it is held at 127.  Below this
+// mantissa nothing does.
+__device__ __forceinline__ bool may_clamp(uint32_t top) { return (top & 0x7fffffu) >= 0x7f0000u; }
+
+// x * 2^k + 1.5 * 2^23 is rounded once, to nearest even, at the units' place, where
+// the sum's low byte is the code in two's complement.
+constexpr float kMagic = 12582912.0f;
+
+// The 8-bit form of eight elements; the four threads of a quad (lanes 4i..4i+3,
+// all of which have to be here) hold one block of 32.  `top`: the bits of the
+// largest magnitude of the eight.  Magnitudes compare as integers, infinities above
+// all numbers and NaNs above those.
+__device__ __forceinline__ uint2 quantize8(const F2 (&v)[4], uint32_t top, uint32_t &exp)
+{
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const uint32_t e = top >> 23;
-    if (e == 255u) {
-        exp = 255u;
-        return make_uint2(0u, 0u);
-    }
-    exp = max(e, 6u) - 6u;
-    const float inv = __uint_as_float((254u - exp) << 23);
-    // x * 2^k + 1.5 * 2^23 is rounded once, to nearest even, at the units' place,
-    // where the sum's low byte is the code in two's complement.
-    constexpr float kMagic = 12582912.0f;
-    uint32_t b[8];
+    exp = block_exp(top);
+    const F2 inv(inverse_scale(exp)), magic(kMagic);
+    float b[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        b[i] = __float_as_uint(fminf(fmaxf(fmaf(v[i], inv, kMagic), kMagic - 127.0f), kMagic + 127.0f));
-    const uint32_t lo = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
-    const uint32_t hi = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
-    return make_uint2(lo, hi);
+    for (int i = 0; i < 4; ++i) fma2(v[i], inv, magic).get(b[2 * i], b[2 * i + 1]);
+    if (may_clamp(top)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[i] = fminf(fmaxf(b[i], kMagic - 127.0f), kMagic + 127.0f);
+    }
+    uint32_t q[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        q[i] = __byte_perm(__byte_perm(__float_as_uint(b[4 * i]), __float_as_uint(b[4 * i + 1]), 0x0040),
+                           __byte_perm(__float_as_uint(b[4 * i + 2]), __float_as_uint(b[4 * i + 3]), 0x0040), 0x5410);
+    return exp == 255u ? make_uint2(0u, 0u) : make_uint2(q[0], q[1]);
+}
+
+// Bits of the largest magnitude of eight numbers that are NaNs all or none.
+__device__ __forceinline__ uint32_t top_of(const F2 (&v)[4])
+{
+    float t = 0.0f;
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i].get(x[2 * i], x[2 * i + 1]);
+    t = fmaxf(fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3]))),
+              fmaxf(fmaxf(fabsf(x[4]), fabsf(x[5])), fmaxf(fabsf(x[6]), fabsf(x[7]))));
+    return __float_as_uint(t) & 0x7fffffffu;
+}
+
+// Where a thread has one element and its warp one block.
+__device__ __forceinline__ uint8_t quantize1(float v, uint32_t &exp)
+{
+    const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7fffffffu);
+    exp = block_exp(top);
+    const float t = fminf(fmaxf(fmaf(v, inverse_scale(exp), kMagic), kMagic - 127.0f), kMagic + 127.0f);
+    return exp == 255u ? 0 : static_cast<uint8_t>(__float_as_uint(t));
+}
+
+__device__ __forceinline__ float scale_of(uint32_t exp)
+{
+    return exp ? __uint_as_float(exp << 23) : __uint_as_float(0x00400000u);
 }
 
 // What eight codes with this exponent byte stand for.  An exponent of 0 means
 // 2^-127; 255 gives an infinite scale, which makes NaNs of codes of 0.
-__device__ __forceinline__ void dequantize8(uint2 codes, uint32_t exp, float (&v)[8])
+__device__ __forceinline__ void dequantize8(uint2 codes, uint32_t exp, F2 (&v)[4])
 {
-    const float scale = exp ? __uint_as_float(exp << 23) : __uint_as_float(0x00400000u);
+    const F2 scale(scale_of(exp)), offset(-8388736.0f);
     const uint32_t w[2] = {codes.x ^ 0x80808080u, codes.y ^ 0x80808080u};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        // the float 2^23 + (code + 128), built from its bits
-        const uint32_t bits = __byte_perm(w[i / 4], 0x4b000000u, 0x7440 | (i & 3));
-        v[i] = (__uint_as_float(bits) - 8388736.0f) * scale;
+    for (int i = 0; i < 4; ++i) {
+        // the floats 2^23 + (code + 128), built from their bits
+        const uint32_t lo = __byte_perm(w[i / 2], 0x4b000000u, i & 1 ? 0x7442 : 0x7440);
+        const uint32_t hi = __byte_perm(w[i / 2], 0x4b000000u, i & 1 ? 0x7443 : 0x7441);
+        v[i] = (F2(__uint_as_float(lo), __uint_as_float(hi)) + offset) * scale;
     }
+}
+__device__ __forceinline__ void dequantize8(uint2 codes, uint32_t exp, float (&v)[8])
+{
+    F2 p[4];
+    dequantize8(codes, exp, p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i].get(v[2 * i], v[2 * i + 1]);
 }
 
 __device__ __forceinline__ float warp_sum(float x)

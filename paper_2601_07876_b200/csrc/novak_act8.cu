@@ -11,7 +11,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kIdentity = -1;
 constexpr int kUnroll = 2;          // groups of 8 per thread, all loads first
-constexpr int kNarrowUnroll = 8;    // elements per thread where rows are not aligned
 
 __device__ __forceinline__ float exp2_approx(float x)
 {
@@ -92,35 +91,34 @@ __device__ __forceinline__ F2 act_slope(F2 u)
     return F2(1.0f);
 }
 
-// Where a thread's elements are.  FLAT: rows without gaps, a multiple of 32 long, are
-// one run of elements.  Otherwise 2^log2 neighbouring threads share a row.
+// Where a thread's eight elements are.  FLAT: rows without gaps, a multiple of 32 long,
+// are one run of elements.  Otherwise 2^log2 neighbouring threads (a warp at least)
+// share a row.
 struct Place {
     int64_t rows, cols;
-    int64_t groups;         // of V elements: all of them (FLAT), or of a row's pitch
+    int64_t groups;         // of 8 elements: all of them (FLAT), or of a row's pitch
     int log2;
 };
 
 struct At {
     int64_t row, col;       // FLAT: row 0, col over the whole run
     bool in;                // inside the rows and their padding
+    int n;                  // elements of the row, 0 to 8
 };
 
-template <bool FLAT, int V, int UNROLL>
+template <bool FLAT>
 __device__ __forceinline__ At place(const Place &p, int64_t first_row, int u)
 {
     if constexpr (FLAT) {
-        const int64_t g = (static_cast<int64_t>(blockIdx.x) * UNROLL + u) * kThreads + threadIdx.x;
-        return {0, g * V, g < p.groups};
+        const int64_t g = (static_cast<int64_t>(blockIdx.x) * kUnroll + u) * kThreads + threadIdx.x;
+        const bool in = g < p.groups;
+        return {0, g * 8, in, in ? 8 : 0};
     } else {
         const int64_t g = (static_cast<int64_t>(blockIdx.x) << p.log2) + (threadIdx.x & ((1 << p.log2) - 1));
         const int64_t row = first_row + (static_cast<int64_t>(u) << (8 - p.log2)) + (threadIdx.x >> p.log2);
-        return {row, g * V, g < p.groups && row < p.rows};
+        const bool in = g < p.groups && row < p.rows;
+        return {row, g * 8, in, in ? static_cast<int>(max(min(p.cols - g * 8, int64_t(8)), int64_t(0))) : 0};
     }
-}
-
-template <bool FLAT> __device__ __forceinline__ int64_t code_at(const Place &p, const At &at, int64_t pitch)
-{
-    return FLAT ? at.col : at.row * pitch + at.col;
 }
 
 __device__ __forceinline__ void put(const Codes &c, int64_t at, bool in, const F2 (&v)[4], uint32_t top)
@@ -133,38 +131,43 @@ __device__ __forceinline__ void put(const Codes &c, int64_t at, bool in, const F
     }
 }
 
-// One thread, eight elements at a time; a quad of threads has a block.
-template <int KIND, int TYPE, bool FLAT>
+// Flat rows are aligned; others may be.
+enum Rows { kFlat, kAligned, kAny };
+
+template <int KIND, int TYPE, Rows ROWS>
 __global__ void __launch_bounds__(kThreads)
 novak_activation_kernel(const typename Elem<TYPE>::T *u, int64_t u_stride, typename Elem<TYPE>::T *a, int64_t a_stride,
                         Codes uc, Codes ac, Place p)
 {
+    constexpr bool kIsFlat = ROWS == kFlat, kIsAligned = ROWS != kAny;
     const int64_t pitch = (p.cols + 31) / 32 * 32;
-    const int64_t per_pass = FLAT ? 1 : int64_t(kUnroll) << (8 - p.log2);
-    for (int64_t row0 = blockIdx.y * per_pass; row0 < (FLAT ? 1 : p.rows); row0 += gridDim.y * per_pass) {
-        Eight<TYPE> raw[kUnroll];
+    const int64_t per_pass = kIsFlat ? 1 : int64_t(kUnroll) << (8 - p.log2);
+    const void *end = end_of(u, u_stride, p.rows, p.cols);
+    for (int64_t row0 = blockIdx.y * per_pass; row0 < (kIsFlat ? 1 : p.rows); row0 += gridDim.y * per_pass) {
+        Fetch<TYPE, kIsAligned> raw[kUnroll];
 #pragma unroll
         for (int i = 0; i < kUnroll; ++i) {
-            const At at = place<FLAT, 8, kUnroll>(p, row0, i);
+            const At at = place<kIsFlat>(p, row0, i);
             raw[i].zero();
-            if (at.in && (FLAT || at.col < p.cols)) raw[i].load(u + at.row * u_stride + at.col);
+            raw[i].load(u + at.row * u_stride + at.col, at.n, u, end);
         }
 #pragma unroll
         for (int i = 0; i < kUnroll; ++i) {
-            const At at = place<FLAT, 8, kUnroll>(p, row0, i);
-            const int64_t to = code_at<FLAT>(p, at, pitch);
+            const At at = place<kIsFlat>(p, row0, i);
+            const int64_t to = at.row * pitch + at.col;
+            const Eight<TYPE> x = raw[i].eight();
             F2 v[4];
-            raw[i].get(v);
-            if (uc.codes) put(uc, to, at.in, v, raw[i].top());
+            x.get(v);
+            if (uc.codes) put(uc, to, at.in, v, x.top());
             if constexpr (KIND != kIdentity) {
                 F2 f[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) f[k] = act<KIND>(v[k]);
                 Eight<TYPE> out;
                 out.set(f);
-                if (a && at.in && (FLAT || at.col < p.cols)) out.store(a + at.row * a_stride + at.col);
+                if (a) store_eight<kIsAligned>(a + at.row * a_stride + at.col, out, at.n);
                 if (ac.codes) {         // of what the next layer reads: the rounded values
-                    out.get(f);
+                    out.get(f);         // (beyond the row f(0) = 0)
                     put(ac, to, at.in, f, out.top());
                 }
             }
@@ -172,154 +175,84 @@ novak_activation_kernel(const typename Elem<TYPE>::T *u, int64_t u_stride, typen
     }
 }
 
-template <int KIND, int TYPE, bool FLAT, bool FROM8>
+template <int KIND, int TYPE, Rows ROWS, bool FROM8>
 __global__ void __launch_bounds__(kThreads)
 novak_activation_backward_kernel(const typename Elem<TYPE>::T *da, int64_t da_stride, const typename Elem<TYPE>::T *u,
                                  int64_t u_stride, Codes uc, typename Elem<TYPE>::T *du, int64_t du_stride, Place p)
 {
+    constexpr bool kIsFlat = ROWS == kFlat, kIsAligned = ROWS != kAny;
     const int64_t pitch = (p.cols + 31) / 32 * 32;
-    const int64_t per_pass = FLAT ? 1 : int64_t(kUnroll) << (8 - p.log2);
-    for (int64_t row0 = blockIdx.y * per_pass; row0 < (FLAT ? 1 : p.rows); row0 += gridDim.y * per_pass) {
-        Eight<TYPE> raw[kUnroll], raw_u[FROM8 ? 1 : kUnroll];
+    const int64_t per_pass = kIsFlat ? 1 : int64_t(kUnroll) << (8 - p.log2);
+    const void *da_end = end_of(da, da_stride, p.rows, p.cols), *u_end = end_of(u, u_stride, p.rows, p.cols);
+    for (int64_t row0 = blockIdx.y * per_pass; row0 < (kIsFlat ? 1 : p.rows); row0 += gridDim.y * per_pass) {
+        Fetch<TYPE, kIsAligned> raw[kUnroll], raw_u[FROM8 ? 1 : kUnroll];
         uint2 q[FROM8 ? kUnroll : 1];
         uint32_t e[FROM8 ? kUnroll : 1];
 #pragma unroll
         for (int i = 0; i < kUnroll; ++i) {
-            const At at = place<FLAT, 8, kUnroll>(p, row0, i);
-            if (!at.in || !(FLAT || at.col < p.cols)) continue;
-            if constexpr (KIND != kIdentity) raw[i].load(da + at.row * da_stride + at.col);
+            const At at = place<kIsFlat>(p, row0, i);
+            if (kIsAligned && at.n == 0) continue;
+            if constexpr (KIND != kIdentity) {
+                if (!kIsAligned) raw[i].zero();
+                raw[i].load(da + at.row * da_stride + at.col, at.n, da, da_end);
+            }
             if constexpr (FROM8) {
-                const int64_t from = code_at<FLAT>(p, at, pitch);
-                q[i] = *reinterpret_cast<const uint2 *>(uc.codes + from);
-                e[i] = uc.exps[from >> 5];
+                const int64_t from = at.row * pitch + at.col;
+                if (!kIsAligned) {
+                    q[i] = make_uint2(0, 0);
+                    e[i] = 0;
+                }
+                if (at.n > 0) {
+                    q[i] = *reinterpret_cast<const uint2 *>(uc.codes + from);
+                    e[i] = uc.exps[from >> 5];
+                }
             } else {
-                raw_u[i].load(u + at.row * u_stride + at.col);
+                if (!kIsAligned) raw_u[i].zero();
+                raw_u[i].load(u + at.row * u_stride + at.col, at.n, u, u_end);
             }
         }
 #pragma unroll
         for (int i = 0; i < kUnroll; ++i) {
-            const At at = place<FLAT, 8, kUnroll>(p, row0, i);
-            if (!at.in || !(FLAT || at.col < p.cols)) continue;
+            const At at = place<kIsFlat>(p, row0, i);
+            if (kIsAligned && at.n == 0) continue;
             F2 v[4];
             if constexpr (FROM8) dequantize8(q[i], e[i], v);
-            else raw_u[i].get(v);
+            else raw_u[i].eight().get(v);
             if constexpr (KIND != kIdentity) {
                 F2 g[4];
-                raw[i].get(g);
+                raw[i].eight().get(g);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) v[k] = g[k] * act_slope<KIND>(v[k]);
             }
             Eight<TYPE> out;
             out.set(v);
-            out.store(du + at.row * du_stride + at.col);
+            store_eight<kIsAligned>(du + at.row * du_stride + at.col, out, at.n);
         }
     }
 }
 
-// Rows that are not aligned, or not a multiple of 8 long: neighbouring threads have
-// neighbouring elements, a warp a block.
-template <int KIND, int TYPE>
-__global__ void __launch_bounds__(kThreads)
-novak_activation_narrow_kernel(const typename Elem<TYPE>::T *u, int64_t u_stride, typename Elem<TYPE>::T *a,
-                               int64_t a_stride, Codes uc, Codes ac, Place p)
+// The form that the matrices allow, and its grid.
+Rows rows_of(const Mat &x, const Mat &y, const Mat &z, int type, Place &p, dim3 &grid)
 {
-    using T = typename Elem<TYPE>::T;
-    const int64_t pitch = (p.cols + 31) / 32 * 32, per_pass = int64_t(kNarrowUnroll) << (8 - p.log2);
-    auto put1 = [&](const Codes &c, const At &at, float v) {
-        uint32_t exp;
-        const uint8_t q = quantize1(v, exp);
-        if (at.in) {
-            const int64_t to = at.row * pitch + at.col;
-            c.codes[to] = static_cast<int8_t>(q);
-            if ((threadIdx.x & 31) == 0) c.exps[to >> 5] = static_cast<uint8_t>(exp);
-        }
-    };
-    for (int64_t row0 = blockIdx.y * per_pass; row0 < p.rows; row0 += gridDim.y * per_pass) {
-        T raw[kNarrowUnroll];
-#pragma unroll
-        for (int i = 0; i < kNarrowUnroll; ++i) {
-            const At at = place<false, 1, kNarrowUnroll>(p, row0, i);
-            raw[i] = at.in && at.col < p.cols ? u[at.row * u_stride + at.col] : from_float<T>(0.0f);
-        }
-#pragma unroll
-        for (int i = 0; i < kNarrowUnroll; i += 2) {
-            const At x = place<false, 1, kNarrowUnroll>(p, row0, i), y = place<false, 1, kNarrowUnroll>(p, row0, i + 1);
-            const F2 v(to_float(raw[i]), to_float(raw[i + 1]));
-            if (uc.codes) {
-                put1(uc, x, v.lo());
-                put1(uc, y, v.hi());
-            }
-            if constexpr (KIND != kIdentity) {
-                const F2 f = act<KIND>(v);
-                const T fx = from_float<T>(f.lo()), fy = from_float<T>(f.hi());
-                if (a && x.in && x.col < p.cols) a[x.row * a_stride + x.col] = fx;
-                if (a && y.in && y.col < p.cols) a[y.row * a_stride + y.col] = fy;
-                if (ac.codes) {
-                    put1(ac, x, to_float(fx));
-                    put1(ac, y, to_float(fy));
-                }
-            }
-        }
+    const Mat *all[3] = {&x, &y, &z};
+    bool aligned = p.cols % 8 == 0, flat = p.cols % 32 == 0 && p.rows * p.cols < (int64_t(1) << 42);
+    for (const Mat *m : all) {
+        if (!m->ptr) continue;
+        aligned = aligned && wide(*m, type, p.rows);
+        flat = flat && (p.rows <= 1 || m->stride == p.cols);
     }
-}
-
-template <int KIND, int TYPE, bool FROM8>
-__global__ void __launch_bounds__(kThreads)
-novak_activation_backward_narrow_kernel(const typename Elem<TYPE>::T *da, int64_t da_stride,
-                                        const typename Elem<TYPE>::T *u, int64_t u_stride, Codes uc,
-                                        typename Elem<TYPE>::T *du, int64_t du_stride, Place p)
-{
-    using T = typename Elem<TYPE>::T;
-    const int64_t pitch = (p.cols + 31) / 32 * 32, per_pass = int64_t(kNarrowUnroll) << (8 - p.log2);
-    for (int64_t row0 = blockIdx.y * per_pass; row0 < p.rows; row0 += gridDim.y * per_pass) {
-        T raw[kNarrowUnroll], raw_u[FROM8 ? 1 : kNarrowUnroll];
-        int8_t q[FROM8 ? kNarrowUnroll : 1];
-        uint8_t e[FROM8 ? kNarrowUnroll : 1];
-#pragma unroll
-        for (int i = 0; i < kNarrowUnroll; ++i) {
-            const At at = place<false, 1, kNarrowUnroll>(p, row0, i);
-            const bool in = at.in && at.col < p.cols;
-            if constexpr (KIND != kIdentity) raw[i] = in ? da[at.row * da_stride + at.col] : from_float<T>(0.0f);
-            if constexpr (FROM8) {
-                q[i] = in ? uc.codes[at.row * pitch + at.col] : 0;
-                e[i] = in ? uc.exps[(at.row * pitch + at.col) >> 5] : 0;
-            } else {
-                raw_u[i] = in ? u[at.row * u_stride + at.col] : from_float<T>(0.0f);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < kNarrowUnroll; i += 2) {
-            const At x = place<false, 1, kNarrowUnroll>(p, row0, i), y = place<false, 1, kNarrowUnroll>(p, row0, i + 1);
-            F2 v;
-            if constexpr (FROM8)
-                v = F2(static_cast<float>(q[i]) * scale_of(e[i]), static_cast<float>(q[i + 1]) * scale_of(e[i + 1]));
-            else
-                v = F2(to_float(raw_u[i]), to_float(raw_u[i + 1]));
-            if constexpr (KIND != kIdentity) v = F2(to_float(raw[i]), to_float(raw[i + 1])) * act_slope<KIND>(v);
-            if (x.in && x.col < p.cols) du[x.row * du_stride + x.col] = from_float<T>(v.lo());
-            if (y.in && y.col < p.cols) du[y.row * du_stride + y.col] = from_float<T>(v.hi());
-        }
+    if (aligned && flat) {
+        p.groups = p.rows * p.cols / 8;
+        grid = dim3(static_cast<unsigned>((p.groups + kThreads * kUnroll - 1) / (kThreads * kUnroll)));
+        return kFlat;
     }
-}
-
-// The grid for `groups` per row of which 256 threads take 2^log2 per row.
-dim3 spread(Place &p, int64_t per_row, int unroll)
-{
-    p.groups = per_row;
+    p.groups = act_pitch(p.cols) / 8;
     p.log2 = 5;             // a warp is in one row
-    while (p.log2 < 8 && (int64_t(1) << p.log2) < per_row) ++p.log2;
-    const int64_t x = (per_row + (int64_t(1) << p.log2) - 1) >> p.log2, per_pass = int64_t(unroll) << (8 - p.log2);
-    return dim3(static_cast<unsigned>(x), static_cast<unsigned>(std::min<int64_t>((p.rows + per_pass - 1) / per_pass, 65535)));
-}
-
-// One run of elements: every matrix that is there has rows of a multiple of 32 with no
-// gaps.
-bool is_flat(const Mat &m, int64_t rows, int64_t cols) { return !m.ptr || rows <= 1 || m.stride == cols; }
-
-dim3 spread_flat(Place &p)
-{
-    p.groups = p.rows * p.cols / 8;
-    return dim3(static_cast<unsigned>((p.groups + kThreads * kUnroll - 1) / (kThreads * kUnroll)));
+    while (p.log2 < 8 && (int64_t(1) << p.log2) < p.groups) ++p.log2;
+    const int64_t per_pass = int64_t(kUnroll) << (8 - p.log2);
+    grid = dim3(static_cast<unsigned>((p.groups + (int64_t(1) << p.log2) - 1) >> p.log2),
+                static_cast<unsigned>(std::min<int64_t>((p.rows + per_pass - 1) / per_pass, 65535)));
+    return aligned ? kAligned : kAny;
 }
 
 template <int KIND, int TYPE>
@@ -327,18 +260,12 @@ cudaError_t forward(Mat u, Mat a, Codes uc, Codes ac, int64_t rows, int64_t cols
 {
     using T = typename Elem<TYPE>::T;
     Place p{rows, cols, 0, 0};
-    const T *up = static_cast<const T *>(u.ptr);
-    T *ap = static_cast<T *>(a.ptr);
-    if (cols % 8 || !wide(u, TYPE, rows) || (a.ptr && !wide(a, TYPE, rows))) {
-        const dim3 grid = spread(p, act_pitch(cols), kNarrowUnroll);
-        novak_activation_narrow_kernel<KIND, TYPE><<<grid, kThreads, 0, stream>>>(up, u.stride, ap, a.stride, uc, ac, p);
-    } else if (cols % 32 == 0 && is_flat(u, rows, cols) && is_flat(a, rows, cols) && rows * cols < (int64_t(1) << 42)) {
-        const dim3 grid = spread_flat(p);
-        novak_activation_kernel<KIND, TYPE, true><<<grid, kThreads, 0, stream>>>(up, u.stride, ap, a.stride, uc, ac, p);
-    } else {
-        const dim3 grid = spread(p, act_pitch(cols) / 8, kUnroll);
-        novak_activation_kernel<KIND, TYPE, false><<<grid, kThreads, 0, stream>>>(up, u.stride, ap, a.stride, uc, ac, p);
-    }
+    dim3 grid;
+    const Rows r = rows_of(u, a, Mat{}, TYPE, p, grid);
+    auto kernel = r == kFlat      ? novak_activation_kernel<KIND, TYPE, kFlat>
+                  : r == kAligned ? novak_activation_kernel<KIND, TYPE, kAligned>
+                                  : novak_activation_kernel<KIND, TYPE, kAny>;
+    kernel<<<grid, kThreads, 0, stream>>>(static_cast<const T *>(u.ptr), u.stride, static_cast<T *>(a.ptr), a.stride, uc, ac, p);
     return cudaGetLastError();
 }
 
@@ -347,19 +274,13 @@ cudaError_t backward(Mat da, Mat u, Codes uc, Mat du, int64_t rows, int64_t cols
 {
     using T = typename Elem<TYPE>::T;
     Place p{rows, cols, 0, 0};
-    const T *dap = static_cast<const T *>(da.ptr), *up = static_cast<const T *>(u.ptr);
-    T *dup = static_cast<T *>(du.ptr);
-    if (cols % 8 || (da.ptr && !wide(da, TYPE, rows)) || (u.ptr && !wide(u, TYPE, rows)) || !wide(du, TYPE, rows)) {
-        const dim3 grid = spread(p, act_pitch(cols), kNarrowUnroll);
-        novak_activation_backward_narrow_kernel<KIND, TYPE, FROM8><<<grid, kThreads, 0, stream>>>(dap, da.stride, up, u.stride, uc, dup, du.stride, p);
-    } else if (cols % 32 == 0 && is_flat(da, rows, cols) && is_flat(u, rows, cols) && is_flat(du, rows, cols) &&
-               rows * cols < (int64_t(1) << 42)) {
-        const dim3 grid = spread_flat(p);
-        novak_activation_backward_kernel<KIND, TYPE, true, FROM8><<<grid, kThreads, 0, stream>>>(dap, da.stride, up, u.stride, uc, dup, du.stride, p);
-    } else {
-        const dim3 grid = spread(p, act_pitch(cols) / 8, kUnroll);
-        novak_activation_backward_kernel<KIND, TYPE, false, FROM8><<<grid, kThreads, 0, stream>>>(dap, da.stride, up, u.stride, uc, dup, du.stride, p);
-    }
+    dim3 grid;
+    const Rows r = rows_of(da, u, du, TYPE, p, grid);
+    auto kernel = r == kFlat      ? novak_activation_backward_kernel<KIND, TYPE, kFlat, FROM8>
+                  : r == kAligned ? novak_activation_backward_kernel<KIND, TYPE, kAligned, FROM8>
+                                  : novak_activation_backward_kernel<KIND, TYPE, kAny, FROM8>;
+    kernel<<<grid, kThreads, 0, stream>>>(static_cast<const T *>(da.ptr), da.stride, static_cast<const T *>(u.ptr), u.stride, uc,
+                                          static_cast<T *>(du.ptr), du.stride, p);
     return cudaGetLastError();
 }
 

@@ -4,9 +4,10 @@
 //     g = dy w, dx = rstd (g - sum(g)/C - xhat sum(g xhat)/C),
 //     dw = sum over rows of dy xhat, db = sum over rows of dy.
 // A row is read once and stays in registers: the deviations are summed after the mean
-// is known.  Three forms of each pass: rows that are 16-byte aligned and a multiple of
-// 8 elements long (8 at a time, arithmetic on pairs), other rows (one at a time,
-// neighbouring threads on neighbouring elements), and rows too long for registers.
+// is known.  A thread has eight neighbouring elements at a time and computes on pairs.
+// Rows that are not 16-byte aligned, or not a multiple of 8 elements long, are read and
+// written as the aligned pieces that hold them.  Rows too long for registers have
+// kernels of their own.
 #include <algorithm>
 
 #include "novak_ops.cuh"
@@ -32,11 +33,13 @@ __device__ __forceinline__ void store_param(void *p, int type, int64_t i, float 
 }
 
 // Puts the 8-bit form of a thread's eight elements at `col` of `row` away; every thread
-// of the warp has to be here, with zeros beyond the row's elements.
+// of the warp has to be here, with zeros beyond the row's elements.  ALL: the eight are
+// NaNs together or not at all.
+template <bool ALL>
 __device__ __forceinline__ void put_codes(const Codes &c, int64_t row, int64_t pitch, int64_t col, const F2 (&v)[4])
 {
     uint32_t exp;
-    const uint2 q = quantize8(v, top_of(v), exp);
+    const uint2 q = quantize8(v, ALL ? top_of(v) : top_of_any(v), exp);
     if (col < pitch) {
         const int64_t at = row * pitch + col;
         *reinterpret_cast<uint2 *>(c.codes + at) = q;
@@ -70,11 +73,11 @@ __device__ __forceinline__ void row_sums(float (&x)[N], float *scratch, int &tur
 }
 
 // Warps per CTA: where a row is a warp's (G = 32), what the registers of a row of NV
-// groups of V elements per lane leave room for.
+// groups of 8 elements per lane leave room for.
 template <int G, int NV> __host__ __device__ constexpr int forward_warps() { return G == 32 ? 8 : G / 32; }
-template <int G, int NV, int V> __host__ __device__ constexpr int backward_warps()
+template <int G, int NV> __host__ __device__ constexpr int backward_warps()
 {
-    return G == 32 ? (NV * V <= 16 ? 16 : NV * V == 24 ? 12 : 8) : G / 32;
+    return G == 32 ? (NV <= 2 ? 16 : NV == 3 ? 12 : 8) : G / 32;
 }
 
 // A thread's columns of a vector that every row needs.  Where a row is a warp's, the
@@ -119,10 +122,10 @@ template <int NV> struct Held<32, NV> {
     }
 };
 
-// ---- rows of aligned groups of 8 ------------------------------------------------------
+// ---- rows in registers -------------------------------------------------------------------
 // G threads per row, NV groups of 8 each; the next row is on its way while this one is
 // worked on.
-template <int TYPE, int G, int NV>
+template <int TYPE, int G, int NV, bool ALIGNED>
 __global__ void __launch_bounds__(32 * forward_warps<G, NV>()) novak_layer_norm_kernel(NormArgs a)
 {
     using T = typename Elem<TYPE>::T;
@@ -137,13 +140,14 @@ __global__ void __launch_bounds__(32 * forward_warps<G, NV>()) novak_layer_norm_
     int64_t row = static_cast<int64_t>(blockIdx.x) * kSubs + sub;
     const T *x = static_cast<const T *>(a.x.ptr) + row * a.x.stride + t * 8;
     T *y = static_cast<T *>(a.y.ptr) + row * a.y.stride + t * 8;
-    bool in[NV];                // groups inside the row
-    Eight<TYPE> raw[NV];
+    const void *end = end_of(static_cast<const T *>(a.x.ptr), a.x.stride, a.rows, cols);
+    int n[NV];                  // elements of a group inside the row
+    Fetch<TYPE, ALIGNED> raw[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        in[i] = (i * G + t) * 8 < cols;
+        n[i] = max(min(cols - (i * G + t) * 8, 8), 0);
         raw[i].zero();
-        if (in[i] && row < a.rows) raw[i].load(x + i * G * 8);
+        if (row < a.rows) raw[i].load(x + i * G * 8, n[i], a.x.ptr, end);
     }
     Held<G, NV> weight, bias;
     weight.load(a.weight, a.param_type, cols, held);
@@ -153,25 +157,24 @@ __global__ void __launch_bounds__(32 * forward_warps<G, NV>()) novak_layer_norm_
         F2 v[NV][4], sum(0.0f);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            raw[i].get(v[i]);
+            raw[i].eight().get(v[i]);
 #pragma unroll
             for (int k = 0; k < 4; ++k) sum = sum + v[i][k];
         }
         x += step * a.x.stride;
         if (row + step < a.rows)
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (in[i]) raw[i].load(x + i * G * 8);
+            for (int i = 0; i < NV; ++i) raw[i].load(x + i * G * 8, n[i], a.x.ptr, end);
         float s[1] = {sum.lo() + sum.hi()};
         row_sums<G, 1>(s, scratch, turn);
         const float mean = s[0] * inv_cols;
         sum = F2(0.0f);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const F2 m(in[i] ? -mean : 0.0f);           // zeros stay zeros beyond the row
+            const F2 m(n[i] > 0 ? -mean : 0.0f);        // zeros stay zeros beyond the row
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                v[i][k] = v[i][k] + m;
+                v[i][k] = v[i][k] + (ALIGNED ? m : F2(2 * k < n[i] ? -mean : 0.0f, 2 * k + 1 < n[i] ? -mean : 0.0f));
                 sum = fma2(v[i][k], v[i][k], sum);
             }
         }
@@ -195,9 +198,9 @@ __global__ void __launch_bounds__(32 * forward_warps<G, NV>()) novak_layer_norm_
             }
             Eight<TYPE> out;
             out.set(o);
-            if (in[i]) out.store(y + i * G * 8);
-            // (a row with an infinity or NaN in it has nothing but NaNs)
-            if (a.codes.codes) put_codes(a.codes, row, pitch, (i * G + t) * 8, v[i]);
+            store_eight<ALIGNED>(y + i * G * 8, out, n[i]);
+            // (a row with an infinity or NaN in it has nothing but NaNs, and zeros beyond it)
+            if (a.codes.codes) put_codes<ALIGNED>(a.codes, row, pitch, (i * G + t) * 8, v[i]);
         }
     }
 }
@@ -205,15 +208,16 @@ __global__ void __launch_bounds__(32 * forward_warps<G, NV>()) novak_layer_norm_
 // The backward pass in the same manner: dy and xhat are read once, a thread's columns
 // of dw and db are added up in registers over the CTA's rows and go to
 // work[CTA][2][cols], which novak_layer_norm_finish_kernel adds up in order.
-template <int TYPE, int G, int NV, bool FROM8>
-__global__ void __launch_bounds__(32 * backward_warps<G, NV, 8>()) novak_layer_norm_back_kernel(NormBackArgs a)
+template <int TYPE, int G, int NV, bool ALIGNED, bool FROM8>
+__global__ void __launch_bounds__(32 * backward_warps<G, NV>(), G == 512 && NV == 1 && ALIGNED ? 2 : 1)
+novak_layer_norm_back_kernel(NormBackArgs a)
 {
     using T = typename Elem<TYPE>::T;
     __shared__ float scratch[G == 32 ? 1 : 4 * 32];
     extern __shared__ __align__(16) float held[];       // warps: the weight, then the warps' column sums
     int turn = 0;
     const int t = G == 32 ? threadIdx.x & 31 : threadIdx.x, sub = G == 32 ? threadIdx.x >> 5 : 0;
-    constexpr int kWarps = backward_warps<G, NV, 8>(), kSubs = G == 32 ? kWarps : 1;
+    constexpr int kWarps = backward_warps<G, NV>(), kSubs = G == 32 ? kWarps : 1;
     asm volatile("griddepcontrol.launch_dependents;");
     const int cols = static_cast<int>(a.cols), pitch = (cols + 31) / 32 * 32;
     const int64_t step = static_cast<int64_t>(gridDim.x) * kSubs;
@@ -224,8 +228,10 @@ __global__ void __launch_bounds__(32 * backward_warps<G, NV, 8>()) novak_layer_n
     const int8_t *codes = a.codes.codes + row * pitch + t * 8;
     const uint8_t *exps = a.codes.exps + row * (pitch / 32) + t / 4;
     T *dx = static_cast<T *>(a.dx.ptr) + row * a.dx.stride + t * 8;
-    bool in[NV];
-    Eight<TYPE> raw[NV], raw_x[FROM8 ? 1 : NV];
+    const void *dy_end = end_of(static_cast<const T *>(a.dy.ptr), a.dy.stride, a.rows, cols);
+    const void *x_end = end_of(static_cast<const T *>(a.x.ptr), a.x.stride, a.rows, cols);
+    int n[NV];
+    Fetch<TYPE, ALIGNED> raw[NV], raw_x[FROM8 ? 1 : NV];
     uint2 q[FROM8 ? NV : 1];
     uint32_t e[FROM8 ? NV : 1];
     float rstd = 0.0f, mean = 0.0f;
@@ -234,20 +240,21 @@ __global__ void __launch_bounds__(32 * backward_warps<G, NV, 8>()) novak_layer_n
         rstd = a.rstd[at];
         if (!FROM8) mean = a.mean[at];
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (in[i]) {
-                raw[i].load(dy + i * G * 8);
-                if constexpr (FROM8) {
+        for (int i = 0; i < NV; ++i) {
+            raw[i].load(dy + i * G * 8, n[i], a.dy.ptr, dy_end);
+            if constexpr (FROM8) {
+                if (n[i] > 0) {
                     q[i] = *reinterpret_cast<const uint2 *>(codes + i * G * 8);
                     e[i] = exps[i * G / 4];
-                } else {
-                    raw_x[i].load(x + i * G * 8);
                 }
+            } else {
+                raw_x[i].load(x + i * G * 8, n[i], a.x.ptr, x_end);
             }
+        }
     };
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        in[i] = (i * G + t) * 8 < cols;
+        n[i] = max(min(cols - (i * G + t) * 8, 8), 0);
         raw[i].zero();
         if constexpr (FROM8) {
             q[i] = make_uint2(0, 0);
@@ -272,9 +279,9 @@ __global__ void __launch_bounds__(32 * backward_warps<G, NV, 8>()) novak_layer_n
         const F2 r2(r), m2(-mean);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            raw[i].get(g[i]);
+            raw[i].eight().get(g[i]);
             if constexpr (FROM8) dequantize8(q[i], e[i], xh[i]);
-            else raw_x[i].get(xh[i]);
+            else raw_x[i].eight().get(xh[i]);
             F2 w[4];
             weight.get(i, w);
 #pragma unroll
@@ -304,7 +311,7 @@ __global__ void __launch_bounds__(32 * backward_warps<G, NV, 8>()) novak_layer_n
             for (int k = 0; k < 4; ++k) g[i][k] = fma2(g[i][k], r2, fma2(xh[i][k], a1, a0));
             Eight<TYPE> out;
             out.set(g[i]);
-            if (in[i]) out.store(dx + i * G * 8);
+            store_eight<ALIGNED>(dx + i * G * 8, out, n[i]);
         }
     }
     if (!a.dweight && !a.dbias) return;
@@ -333,174 +340,18 @@ __global__ void __launch_bounds__(32 * backward_warps<G, NV, 8>()) novak_layer_n
     } else {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            if (in[i])
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int col = (i * G + t) * 8 + 2 * k;
+            for (int k = 0; k < 4; ++k) {
+                const int col = (i * G + t) * 8 + 2 * k;
+                if (2 * k < n[i]) {
                     out[col] = dw[i][k].lo();
-                    out[col + 1] = dw[i][k].hi();
                     out[cols + col] = db[i][k].lo();
+                }
+                if (2 * k + 1 < n[i]) {
+                    out[col + 1] = dw[i][k].hi();
                     out[cols + col + 1] = db[i][k].hi();
                 }
-    }
-}
-
-// ---- other rows: one element at a time ---------------------------------------------------
-// Element (i G + t) is thread t's i-th; a warp's i-th elements are a block of 32.
-template <int TYPE, int G, int NV>
-__global__ void __launch_bounds__(32 * forward_warps<G, NV>()) novak_layer_norm_narrow_kernel(NormArgs a)
-{
-    using T = typename Elem<TYPE>::T;
-    __shared__ float scratch[G == 32 ? 1 : 2 * 32];
-    int turn = 0;
-    const int t = G == 32 ? threadIdx.x & 31 : threadIdx.x, sub = G == 32 ? threadIdx.x >> 5 : 0;
-    constexpr int kSubs = G == 32 ? forward_warps<G, NV>() : 1;
-    const int cols = static_cast<int>(a.cols), pitch = (cols + 31) / 32 * 32;
-    const int64_t step = static_cast<int64_t>(gridDim.x) * kSubs;
-    const float inv_cols = 1.0f / static_cast<float>(cols);
-    int64_t row = static_cast<int64_t>(blockIdx.x) * kSubs + sub;
-    const T *x = static_cast<const T *>(a.x.ptr) + row * a.x.stride + t;
-    T *y = static_cast<T *>(a.y.ptr) + row * a.y.stride + t;
-    T raw[NV];
-    auto fetch = [&](int64_t at) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) raw[i] = at < a.rows && i * G + t < cols ? x[i * G] : from_float<T>(0.0f);
-    };
-    fetch(row);
-    float w[NV], b[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        w[i] = i * G + t < cols ? param_at(a.weight, a.param_type, i * G + t) : 0.0f;
-        b[i] = a.bias && i * G + t < cols ? param_at(a.bias, a.param_type, i * G + t) : 0.0f;
-    }
-    for (; row < a.rows; row += step, y += step * a.y.stride) {
-        float v[NV], s[1] = {0.0f};
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            v[i] = to_float(raw[i]);
-            s[0] += v[i];
-        }
-        x += step * a.x.stride;
-        fetch(row + step);
-        row_sums<G, 1>(s, scratch, turn);
-        const float mean = s[0] * inv_cols;
-        s[0] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            v[i] = i * G + t < cols ? v[i] - mean : 0.0f;
-            s[0] = fmaf(v[i], v[i], s[0]);
-        }
-        row_sums<G, 1>(s, scratch, turn);
-        const float rstd = rsqrtf(fmaf(s[0], inv_cols, a.eps));
-        if (t == 0) {
-            if (a.mean) a.mean[row] = mean;
-            if (a.rstd) a.rstd[row] = rstd;
-        }
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            v[i] *= rstd;
-            if (i * G + t < cols) y[i * G] = from_float<T>(fmaf(v[i], w[i], b[i]));
-        }
-        if (a.codes.codes)
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                if (i * G + t >= pitch) break;          // (whole warps)
-                uint32_t exp;
-                const uint8_t q = quantize1(v[i], exp);
-                const int64_t at = row * pitch + i * G + t;
-                a.codes.codes[at] = static_cast<int8_t>(q);
-                if ((threadIdx.x & 31) == 0) a.codes.exps[at >> 5] = static_cast<uint8_t>(exp);
             }
-    }
-}
-
-template <int TYPE, int G, int NV, bool FROM8>
-__global__ void __launch_bounds__(32 * backward_warps<G, NV, 1>()) novak_layer_norm_back_narrow_kernel(NormBackArgs a)
-{
-    using T = typename Elem<TYPE>::T;
-    __shared__ float scratch[G == 32 ? 1 : 4 * 32];
-    __shared__ float part[G == 32 ? backward_warps<G, NV, 1>() : 1][G == 32 ? NV * 32 : 1];
-    int turn = 0;
-    const int t = G == 32 ? threadIdx.x & 31 : threadIdx.x, sub = G == 32 ? threadIdx.x >> 5 : 0;
-    constexpr int kWarps = backward_warps<G, NV, 1>(), kSubs = G == 32 ? kWarps : 1;
-    asm volatile("griddepcontrol.launch_dependents;");
-    const int cols = static_cast<int>(a.cols), pitch = (cols + 31) / 32 * 32;
-    const int64_t step = static_cast<int64_t>(gridDim.x) * kSubs;
-    const float inv_cols = 1.0f / static_cast<float>(cols);
-    int64_t row = static_cast<int64_t>(blockIdx.x) * kSubs + sub;
-    T raw[NV], raw_x[FROM8 ? 1 : NV];
-    int8_t q[FROM8 ? NV : 1];
-    uint8_t e[FROM8 ? NV : 1];
-    float rstd = 0.0f, mean = 0.0f, w[NV], dw[NV], db[NV];
-    auto fetch = [&](int64_t at) {
-        if (at >= a.rows) return;
-        rstd = a.rstd[at];
-        if (!FROM8) mean = a.mean[at];
-        const T *dy = static_cast<const T *>(a.dy.ptr) + at * a.dy.stride + t;
-        const T *x = static_cast<const T *>(a.x.ptr) + at * a.x.stride + t;
-        const int64_t c = at * pitch + t;
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (i * G + t < cols) {
-                raw[i] = dy[i * G];
-                if constexpr (FROM8) {
-                    q[i] = a.codes.codes[c + i * G];
-                    e[i] = a.codes.exps[(c + i * G) >> 5];
-                } else {
-                    raw_x[i] = x[i * G];
-                }
-            }
-    };
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        raw[i] = from_float<T>(0.0f);
-        if constexpr (FROM8) q[i] = e[i] = 0;
-        else raw_x[i] = from_float<T>(0.0f);
-        w[i] = i * G + t < cols ? param_at(a.weight, a.param_type, i * G + t) : 0.0f;
-        dw[i] = db[i] = 0.0f;
-    }
-    fetch(row);
-    for (; row < a.rows; row += step) {
-        float g[NV], xh[NV], s[2] = {0.0f, 0.0f};
-        const float r = rstd, m = mean;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            g[i] = to_float(raw[i]);
-            if constexpr (FROM8) xh[i] = static_cast<float>(q[i]) * scale_of(e[i]);
-            else xh[i] = (to_float(raw_x[i]) - m) * r;
-            dw[i] = fmaf(g[i], xh[i], dw[i]);
-            db[i] += g[i];
-            g[i] *= w[i];
-            s[0] += g[i];
-            s[1] = fmaf(g[i], xh[i], s[1]);
-        }
-        fetch(row + step);
-        row_sums<G, 2>(s, scratch, turn);
-        const float a1 = -s[1] * inv_cols * r, a0 = -s[0] * inv_cols * r;
-        T *dx = static_cast<T *>(a.dx.ptr) + row * a.dx.stride + t;
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (i * G + t < cols) dx[i * G] = from_float<T>(fmaf(g[i], r, fmaf(xh[i], a1, a0)));
-    }
-    if (!a.dweight && !a.dbias) return;
-    float *out = a.work + static_cast<int64_t>(blockIdx.x) * 2 * cols;
-    for (int which = 0; which < 2; ++which) {
-        if constexpr (G == 32) {
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < NV; ++i) part[sub][i * 32 + t] = which ? db[i] : dw[i];
-            __syncthreads();
-            for (int c = threadIdx.x; c < cols; c += blockDim.x) {
-                float sum = 0.0f;
-#pragma unroll
-                for (int p = 0; p < kWarps; ++p) sum += part[p][c];
-                out[which * cols + c] = sum;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (i * G + t < cols) out[which * cols + i * G + t] = which ? db[i] : dw[i];
-        }
     }
 }
 
@@ -553,7 +404,7 @@ __global__ void __launch_bounds__(kThreads) novak_layer_norm_long_kernel(NormArg
                 F2 p[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) p[k] = F2(v[2 * k], v[2 * k + 1]);
-                put_codes(a.codes, row, pitch, c, p);
+                put_codes<false>(a.codes, row, pitch, c, p);
             }
         }
     }
@@ -675,34 +526,36 @@ novak_layer_norm_finish_kernel(const float *work, int64_t splits, int64_t cols, 
     if (lane == 0 && mine < cols) store_param(out, type, mine, sum);
 }
 
-// How a row of `cols` elements is spread over G threads, NV groups each of 8 elements
-// (v = 8: 128-bit accesses and a multiple of 8) or of one.  false: too long for
-// registers.
+// How a row of `cols` elements is spread: G threads, NV groups of 8 each.  false: too
+// long for registers.  Rows that are not aligned need more registers per group.
 struct Spread {
-    int v, g, nv;
+    int g, nv;
 };
-constexpr Spread kWide[] = {{8, 32, 1}, {8, 32, 2}, {8, 32, 3}, {8, 32, 4}, {8, 256, 1}, {8, 512, 1}, {8, 512, 2}};
-constexpr Spread kNarrow[] = {{1, 32, 8}, {1, 128, 8}, {1, 512, 8}, {1, 512, 16}};
+constexpr Spread kAlignedRows[] = {{32, 1}, {32, 2}, {32, 3}, {32, 4}, {256, 1}, {512, 1}, {512, 2}};
+constexpr Spread kAnyRows[] = {{32, 1}, {128, 1}, {512, 1}, {512, 2}};
 
-bool spread_for(bool is_wide, int64_t cols, Spread &s)
+bool spread_for(bool aligned, int64_t cols, Spread &s)
 {
-    const Spread *begin = is_wide ? kWide : kNarrow, *end = begin + (is_wide ? sizeof kWide : sizeof kNarrow) / sizeof(Spread);
+    const Spread *begin = aligned ? kAlignedRows : kAnyRows;
+    const Spread *end = begin + (aligned ? sizeof kAlignedRows : sizeof kAnyRows) / sizeof(Spread);
     for (const Spread *c = begin; c != end; ++c)
-        if (cols <= c->v * c->g * c->nv) {
+        if (cols <= 8 * c->g * c->nv) {
             s = *c;
             return true;
         }
     return false;
 }
 
-#define NOVAK_WIDE(F) F(32, 1) F(32, 2) F(32, 3) F(32, 4) F(256, 1) F(512, 1) F(512, 2)
-#define NOVAK_NARROW(F) F(32, 8) F(128, 8) F(512, 8) F(512, 16)
+#define NOVAK_SPREADS(F)                                                                                          \
+    F(32, 1, true) F(32, 2, true) F(32, 3, true) F(32, 4, true) F(256, 1, true) F(512, 1, true) F(512, 2, true) \
+    F(32, 1, false) F(128, 1, false) F(512, 1, false) F(512, 2, false)
 
 // CTAs of the backward pass (each leaves one partial sum per column): one per SM
-// where its warps have a row each, two where a row is the CTA's.
-int64_t back_ctas(int64_t rows, int64_t cols)
+// where its warps have a row each, else as many as registers let an SM hold.
+int64_t back_ctas(const Spread &s, int64_t rows)
 {
-    return std::max<int64_t>(1, std::min<int64_t>(rows, kSms * (cols <= 1024 ? 1 : 2)));
+    const int per_sm = s.g == 32 ? 1 : s.g == 512 ? (s.nv == 1 ? 2 : 1) : s.g == 128 ? 4 : 2;
+    return std::min<int64_t>(rows, kSms * per_sm);
 }
 
 template <typename Kernel, typename Args>
@@ -716,38 +569,29 @@ cudaError_t run(Kernel kernel, int64_t grid, int threads, int smem, const Args &
     return cudaGetLastError();
 }
 
-template <int TYPE> cudaError_t forward(const NormArgs &a, const Spread &s, cudaStream_t stream)
+template <int TYPE> cudaError_t forward(const NormArgs &a, const Spread &s, bool aligned, cudaStream_t stream)
 {
-#define NOVAK_GRID(G, NV) \
-    std::min<int64_t>((a.rows + (G == 32 ? forward_warps<G, NV>() : 1) - 1) / (G == 32 ? forward_warps<G, NV>() : 1), \
-                      kSms * (G == 32 ? 4 : 1024 / G))
-#define NOVAK_CASE(G, NV)                   \
-    if (s.v == 8 && s.g == G && s.nv == NV) \
-        return run(novak_layer_norm_kernel<TYPE, G, NV>, NOVAK_GRID(G, NV), 32 * forward_warps<G, NV>(), 0, a, stream);
-    NOVAK_WIDE(NOVAK_CASE)
+#define NOVAK_CASE(G, NV, ALIGNED)                                                                                    \
+    if (s.g == G && s.nv == NV && aligned == ALIGNED) {                                                               \
+        constexpr int warps = forward_warps<G, NV>(), rows = G == 32 ? warps : 1;                                     \
+        const int64_t grid = std::min<int64_t>((a.rows + rows - 1) / rows, kSms * (G == 32 ? 4 : 1024 / G));          \
+        return run(novak_layer_norm_kernel<TYPE, G, NV, ALIGNED>, grid, 32 * warps, 0, a, stream);                    \
+    }
+    NOVAK_SPREADS(NOVAK_CASE)
 #undef NOVAK_CASE
-#define NOVAK_CASE(G, NV)                   \
-    if (s.v == 1 && s.g == G && s.nv == NV) \
-        return run(novak_layer_norm_narrow_kernel<TYPE, G, NV>, NOVAK_GRID(G, NV), 32 * forward_warps<G, NV>(), 0, a, stream);
-    NOVAK_NARROW(NOVAK_CASE)
-#undef NOVAK_CASE
-#undef NOVAK_GRID
     return cudaErrorInvalidValue;
 }
 
 template <int TYPE, bool FROM8>
-cudaError_t backward(const NormBackArgs &a, const Spread &s, int64_t grid, cudaStream_t stream)
+cudaError_t backward(const NormBackArgs &a, const Spread &s, bool aligned, int64_t grid, cudaStream_t stream)
 {
-#define NOVAK_CASE(G, NV)                                                                                       \
-    if (s.v == 8 && s.g == G && s.nv == NV)                                                                     \
-        return run(novak_layer_norm_back_kernel<TYPE, G, NV, FROM8>, grid, 32 * backward_warps<G, NV, 8>(),     \
-                   G == 32 ? (1 + backward_warps<G, NV, 8>()) * NV * 256 * 4 : 0, a, stream);
-    NOVAK_WIDE(NOVAK_CASE)
-#undef NOVAK_CASE
-#define NOVAK_CASE(G, NV)                   \
-    if (s.v == 1 && s.g == G && s.nv == NV) \
-        return run(novak_layer_norm_back_narrow_kernel<TYPE, G, NV, FROM8>, grid, 32 * backward_warps<G, NV, 1>(), 0, a, stream);
-    NOVAK_NARROW(NOVAK_CASE)
+#define NOVAK_CASE(G, NV, ALIGNED)                                                                                    \
+    if (s.g == G && s.nv == NV && aligned == ALIGNED) {                                                               \
+        constexpr int warps = backward_warps<G, NV>();                                                                \
+        return run(novak_layer_norm_back_kernel<TYPE, G, NV, ALIGNED, FROM8>, grid, 32 * warps,                       \
+                   G == 32 ? (1 + warps) * NV * 256 * 4 : 0, a, stream);                                              \
+    }
+    NOVAK_SPREADS(NOVAK_CASE)
 #undef NOVAK_CASE
     return cudaErrorInvalidValue;
 }
@@ -757,9 +601,10 @@ cudaError_t backward(const NormBackArgs &a, const Spread &s, int64_t grid, cudaS
 cudaError_t launch_layer_norm(const NormArgs &a, cudaStream_t stream)
 {
     const bool w = wide(a.x, a.type, a.rows) && wide(a.y, a.type, a.rows);
+    const bool aligned = w && a.cols % 8 == 0;
     Spread s;
-    if (spread_for(w && a.cols % 8 == 0, a.cols, s))
-        return a.type == NOVAK_TYPE_F32 ? forward<0>(a, s, stream) : forward<1>(a, s, stream);
+    if (spread_for(aligned, a.cols, s))
+        return a.type == NOVAK_TYPE_F32 ? forward<0>(a, s, aligned, stream) : forward<1>(a, s, aligned, stream);
     const int grid = static_cast<int>(std::min<int64_t>(a.rows, kSms * 8));
     auto kernel = a.type == NOVAK_TYPE_F32
                       ? (w ? novak_layer_norm_long_kernel<0, true> : novak_layer_norm_long_kernel<0, false>)
@@ -771,23 +616,26 @@ cudaError_t launch_layer_norm(const NormArgs &a, cudaStream_t stream)
 // Enough for either way of the backward pass: which one it is depends on alignment.
 size_t layer_norm_backward_bytes(int64_t rows, int64_t cols)
 {
-    const int64_t splits = (rows + kSplitRows - 1) / kSplitRows;
-    return static_cast<size_t>(std::max(splits, back_ctas(rows, cols)) * 2 * cols) * sizeof(float);
+    int64_t splits = (rows + kSplitRows - 1) / kSplitRows;
+    Spread s;
+    for (const bool aligned : {false, true})
+        if (spread_for(aligned, cols, s)) splits = std::max(splits, back_ctas(s, rows));
+    return static_cast<size_t>(splits * 2 * cols) * sizeof(float);
 }
 
 cudaError_t launch_layer_norm_backward(const NormBackArgs &a, cudaStream_t stream)
 {
     const bool w = wide(a.dy, a.type, a.rows) && wide(a.dx, a.type, a.rows) &&
                    (!a.x.ptr || wide(a.x, a.type, a.rows));
-    const bool sums = a.dweight || a.dbias;
+    const bool sums = a.dweight || a.dbias, aligned = w && a.cols % 8 == 0;
     int64_t splits = 0;
     Spread s;
     if (a.rows == 0) {
-    } else if (spread_for(w && a.cols % 8 == 0, a.cols, s)) {
-        splits = back_ctas(a.rows, a.cols);
+    } else if (spread_for(aligned, a.cols, s)) {
+        splits = back_ctas(s, a.rows);
         const bool q = a.codes.codes != nullptr;
-        const cudaError_t e = a.type == NOVAK_TYPE_F32 ? (q ? backward<0, true>(a, s, splits, stream) : backward<0, false>(a, s, splits, stream))
-                                                       : (q ? backward<1, true>(a, s, splits, stream) : backward<1, false>(a, s, splits, stream));
+        const cudaError_t e = a.type == NOVAK_TYPE_F32 ? (q ? backward<0, true>(a, s, aligned, splits, stream) : backward<0, false>(a, s, aligned, splits, stream))
+                                                       : (q ? backward<1, true>(a, s, aligned, splits, stream) : backward<1, false>(a, s, aligned, splits, stream));
         if (e != cudaSuccess) return e;
     } else {
         splits = (a.rows + kSplitRows - 1) / kSplitRows;

@@ -184,6 +184,189 @@ template <> struct Eight<NOVAK_TYPE_F32> {
     }
 };
 
+// Eight consecutive elements of any row, fetched as the aligned 16-byte pieces that hold
+// them: `words` as they are in memory, the first element `skip` bytes in.  Only the
+// first n elements count (0 to 8), the others read as zeros.  A piece that reaches
+// beyond the matrix (of bytes begin to end) is fetched element by element.
+template <int TYPE> struct AnyEight {
+    using T = typename Elem<TYPE>::T;
+    static constexpr int kSize = static_cast<int>(sizeof(T)), kPieces = kSize / 2 + 1;
+    uint32_t words[4 * kPieces];
+    int skip, n;
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < 4 * kPieces; ++i) words[i] = 0;
+        skip = n = 0;
+    }
+    __device__ __forceinline__ void load(const T *p, int count, const void *begin, const void *end)
+    {
+        n = count;
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+        skip = static_cast<int>(at & 15u);
+        const char *piece = reinterpret_cast<const char *>(at - skip);
+        const int bytes = skip + n * kSize;
+        if (n > 0 && (piece < begin || piece + (bytes + 15) / 16 * 16 > end)) {
+            skip = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if constexpr (kSize == 4) {
+                    words[i] = i < n ? __float_as_uint(p[i]) : 0u;
+                } else {
+                    const uint32_t x = i < n ? reinterpret_cast<const uint16_t *>(p)[i] : 0u;
+                    words[i / 2] = i & 1 ? words[i / 2] | x << 16 : x;
+                }
+            }
+            return;
+        }
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) {
+            uint4 w = make_uint4(0, 0, 0, 0);
+            if (n > 0 && 16 * k < bytes) w = *reinterpret_cast<const uint4 *>(piece + 16 * k);
+            words[4 * k] = w.x;
+            words[4 * k + 1] = w.y;
+            words[4 * k + 2] = w.z;
+            words[4 * k + 3] = w.w;
+        }
+    }
+    __device__ __forceinline__ Eight<TYPE> eight() const
+    {
+        constexpr int kWords = 2 * kSize;           // of eight elements
+        uint32_t w[kWords + 4];
+#pragma unroll
+        for (int i = 0; i < kWords + 4; ++i) w[i] = words[i];
+        if (skip & 8)
+#pragma unroll
+            for (int i = 0; i < kWords + 2; ++i) w[i] = w[i + 2];
+        if (skip & 4)
+#pragma unroll
+            for (int i = 0; i < kWords + 1; ++i) w[i] = w[i + 1];
+        Eight<TYPE> r;
+        if constexpr (kSize == 2) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (skip & 2) * 8);
+            if (n < 8)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (2 * i >= n) w[i] = 0;
+                    else if (2 * i + 1 >= n) w[i] &= 0xffffu;
+                }
+            r.w = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+            if (n < 8)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i >= n) w[i] = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r.x[i] = F2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+        }
+        return r;
+    }
+};
+
+// Stores the first n of eight elements of any row (p aligned to its element).  The
+// warp's lanes have consecutive groups of one row and are all here; those with elements
+// come first, and only the last of them may have fewer than eight.  What an aligned
+// 16-byte piece holds of two neighbouring lanes goes out in one store; the pieces at
+// the warp's ends, whose other elements are not here, go element by element.
+__device__ __forceinline__ void store_any(__nv_bfloat16 *p, const Eight<NOVAK_TYPE_BF16> &v, int n)
+{
+    const int lane = threadIdx.x & 31, skip = static_cast<int>(reinterpret_cast<uintptr_t>(p) & 15u), head = (16 - skip) / 2;
+    // words 0-3 of the lane before, 4-7 own; the piece starts skip bytes before word 4
+    uint32_t w[8] = {0, 0, 0, 0, v.w.x, v.w.y, v.w.z, v.w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __shfl_up_sync(0xffffffffu, w[4 + i], 1);
+    // a piece that starts skip bytes before w[4]: word 4 - skip / 4 rounded up, then a half
+    const int back = (skip + 3) / 4;                        // words
+    uint32_t t[5];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) {
+        const uint32_t a = i < 4 ? (back & 1 ? w[3 + i] : w[4 + i]) : (back & 1 ? w[7] : 0u);
+        const uint32_t b = back & 1 ? w[1 + i] : w[2 + i];
+        t[i] = back & 2 ? b : a;
+    }
+    if (back == 4) {
+#pragma unroll
+        for (int i = 0; i < 5; ++i) t[i] = w[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = __funnelshift_r(t[i], t[i + 1], (skip & 2) * 8);
+    const bool full = n >= head && (skip == 0 || lane > 0);
+    const int next_full = __shfl_down_sync(0xffffffffu, static_cast<int>(full), 1);
+    if (full) *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(p) - skip) = make_uint4(t[0], t[1], t[2], t[3]);
+    const int from = full ? head : 0, to = lane < 31 && next_full ? min(n, head) : n;
+    if (from < to) {
+        const uint32_t own[4] = {v.w.x, v.w.y, v.w.z, v.w.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i >= from && i < to)
+                reinterpret_cast<uint16_t *>(p)[i] = static_cast<uint16_t>(i & 1 ? own[i / 2] >> 16 : own[i / 2]);
+    }
+}
+
+__device__ __forceinline__ void store_any(float *p, const Eight<NOVAK_TYPE_F32> &v, int n)
+{
+    const int lane = threadIdx.x & 31, back = static_cast<int>(reinterpret_cast<uintptr_t>(p) & 15u) / 4, head = 4 - back;
+    // elements 0-3: the last of the lane before; 4-11: own
+    float w[12];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v.x[i].get(w[4 + 2 * i], w[5 + 2 * i]);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) w[i] = __shfl_up_sync(0xffffffffu, w[8 + i], 1);
+    float t[8];         // two pieces, from `back` elements before the first
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float a = back & 1 ? w[3 + i] : w[4 + i], b = back & 1 ? w[1 + i] : w[2 + i];
+        t[i] = back & 2 ? b : a;
+    }
+    const bool first = n >= head && (back == 0 || lane > 0), second = n >= head + 4;
+    const int next_first = __shfl_down_sync(0xffffffffu, static_cast<int>(first), 1);
+    if (first) *reinterpret_cast<float4 *>(p - back) = make_float4(t[0], t[1], t[2], t[3]);
+    if (second) *reinterpret_cast<float4 *>(p - back + 4) = make_float4(t[4], t[5], t[6], t[7]);
+    const bool next = lane < 31 && next_first && n == 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const bool done = i < head ? first : i < head + 4 ? second : next;
+        if (i < n && !done) p[i] = w[4 + i];
+    }
+}
+
+// The two behind one face.  ALIGNED: n is 0 or 8 (rows are 16-byte aligned and a
+// multiple of 8 elements long).
+template <int TYPE, bool ALIGNED> struct Fetch;
+template <int TYPE> struct Fetch<TYPE, true> {
+    using T = typename Elem<TYPE>::T;
+    Eight<TYPE> x;
+    __device__ __forceinline__ void zero() { x.zero(); }
+    __device__ __forceinline__ void load(const T *p, int n, const void *, const void *)
+    {
+        if (n > 0) x.load(p);
+    }
+    __device__ __forceinline__ const Eight<TYPE> &eight() const { return x; }
+};
+template <int TYPE> struct Fetch<TYPE, false> {
+    using T = typename Elem<TYPE>::T;
+    AnyEight<TYPE> x;
+    __device__ __forceinline__ void zero() { x.zero(); }
+    __device__ __forceinline__ void load(const T *p, int n, const void *begin, const void *end) { x.load(p, n, begin, end); }
+    __device__ __forceinline__ Eight<TYPE> eight() const { return x.eight(); }
+};
+template <bool ALIGNED, int TYPE>
+__device__ __forceinline__ void store_eight(typename Elem<TYPE>::T *p, const Eight<TYPE> &v, int n)
+{
+    if constexpr (ALIGNED) {
+        if (n > 0) v.store(p);
+    } else {
+        store_any(p, v, n);
+    }
+}
+
+// Address behind a matrix's last element.
+template <typename T> __device__ __forceinline__ const void *end_of(const T *p, int64_t stride, int64_t rows, int64_t cols)
+{
+    return p + (rows - 1) * stride + cols;
+}
+
 // Exponent byte of a block whose largest magnitude has these bits (an infinity or
 // NaN: 255), and the reciprocal of its scale.
 __device__ __forceinline__ uint32_t block_exp(uint32_t top)
@@ -228,7 +411,17 @@ __device__ __forceinline__ uint2 quantize8(const F2 (&v)[4], uint32_t top, uint3
     return exp == 255u ? make_uint2(0u, 0u) : make_uint2(q[0], q[1]);
 }
 
-// Bits of the largest magnitude of eight numbers that are NaNs all or none.
+// Bits of the largest magnitude of eight numbers.
+__device__ __forceinline__ uint32_t top_of_any(const F2 (&v)[4])
+{
+    uint32_t t = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        t = max(t, max(__float_as_uint(v[i].lo()) & 0x7fffffffu, __float_as_uint(v[i].hi()) & 0x7fffffffu));
+    return t;
+}
+
+// The same of numbers that are NaNs all or none.
 __device__ __forceinline__ uint32_t top_of(const F2 (&v)[4])
 {
     float t = 0.0f;
@@ -238,15 +431,6 @@ __device__ __forceinline__ uint32_t top_of(const F2 (&v)[4])
     t = fmaxf(fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3]))),
               fmaxf(fmaxf(fabsf(x[4]), fabsf(x[5])), fmaxf(fabsf(x[6]), fabsf(x[7]))));
     return __float_as_uint(t) & 0x7fffffffu;
-}
-
-// Where a thread has one element and its warp one block.
-__device__ __forceinline__ uint8_t quantize1(float v, uint32_t &exp)
-{
-    const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7fffffffu);
-    exp = block_exp(top);
-    const float t = fminf(fmaxf(fmaf(v, inverse_scale(exp), kMagic), kMagic - 127.0f), kMagic + 127.0f);
-    return exp == 255u ? 0 : static_cast<uint8_t>(__float_as_uint(t));
 }
 
 __device__ __forceinline__ float scale_of(uint32_t exp)

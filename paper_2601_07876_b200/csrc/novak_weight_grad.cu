@@ -253,14 +253,20 @@ __device__ __forceinline__ void tile_slots(const Cut &c, int tile, int &slot, in
 constexpr int kStages = 5;
 constexpr int kStageBytes = 2 * 128 * kRows * 2;        // dy and x: 128 columns each, bf16
 constexpr int kHalf = 64 * kRows * 2;                   // 64 columns of an operand
-constexpr int kRaws = 5;
+constexpr int kRaws = 4;        // steps of codes on their way
 constexpr int kRawBytes = 128 * kRows;                  // codes of 128 columns
 constexpr int kRun = 16;        // steps that the tensor cores add up by themselves: their sums round toward
                                 // zero, so that a chain's error grows with its length
-constexpr int kOutWarps = 8, kFillWarps = 8, kLoadWarps = 4, kSumWarps = 2;
+constexpr int kOutWarps = 8, kFillWarps = 8, kFillGroups = 2, kLoadWarps = 4, kSumWarps = 2;
+constexpr int kGroupWarps = kFillWarps / kFillGroups;   // that fill a step's x; the groups take turns
 constexpr int kLoadWarp = kOutWarps + kFillWarps, kCopyWarp = kLoadWarp + kLoadWarps, kMmaWarp = kCopyWarp + 1,
               kSumWarp = kCopyWarp + 2;
 constexpr int kThreads = 32 * (kSumWarp + kSumWarps);
+// A barrier's parity tells one phase from the next, not from the one after that: whoever
+// waits for a slot's use number k has to know that use k - 1 is over.  The two groups do
+// not finish steps in order among each other, so a slot of codes belongs to one group for
+// good; the products free the stages in order.
+static_assert(kRaws % kFillGroups == 0 && kRaws % kLoadWarps == 0, "slots of codes change hands");
 constexpr int kPad = 17;
 // Registers per thread: 80 at launch, 768 x 80 = 61440 = 256 x 160 + 512 x 40.
 constexpr int kOutRegs = 160, kOtherRegs = 40;
@@ -279,7 +285,7 @@ struct KernelArgs {
     Codes codes;
     int64_t pitch;
     void *dw;
-    int grad_type;
+    int grad_type, vector;
     int64_t rows, n_out, n_in;
     float *partial;                 // [slot][64][256 rows][4 columns] per tile
     float *sums;                    // [slot][256]; NULL: not asked for
@@ -356,48 +362,56 @@ __device__ __forceinline__ void load_codes(const KernelArgs &a, const CUtensorMa
     }
 }
 
-// Warps kOutWarps ..: x, 64 rows x 128 columns per step, a thread one block of one
-// row.  The eight threads of a shared-memory access have eight consecutive rows,
-// which the 128-byte swizzle spreads over all banks, of the codes and of x.
+// Warps kOutWarps ..: x, 64 rows x 128 columns per step, a thread one block of each of
+// two rows.  The eight threads of a shared-memory access have eight consecutive rows,
+// which the 128-byte swizzle spreads over all banks, of the codes and of x.  Two groups
+// of four warps have every other step each: a step's waits, its proxy fence and its
+// arrival take longer than its arithmetic.
 __device__ __forceinline__ void fill_x(const KernelArgs &a, Shared &sh, uint32_t stages, uint32_t raws, uint32_t rank,
                                        int pair)
 {
-    const int warp = threadIdx.x / 32 - kOutWarps, lane = threadIdx.x % 32;
-    const int half = warp & 1, r = (warp >> 1) * 16 + (lane & 15), b = lane >> 4;
+    const int group = (threadIdx.x / 32 - kOutWarps) / kGroupWarps, warp = (threadIdx.x / 32 - kOutWarps) % kGroupWarps;
+    const int lane = threadIdx.x % 32, half = warp & 1, r = (warp >> 1) * 32 + (lane & 15), b = lane >> 4;
     const uint32_t dst0 = stages + 2 * kHalf + half * kHalf + r * 128 + ((4 * b ^ (r & 7)) << 4);
     const uint32_t src0 = raws + r * 128 + (((half * 4 + b * 2) ^ (r & 7)) << 4);
     const uint32_t exp0 = smem_addr(&sh.exps[0][0]) + r * 4 + half * 2 + b;
-    int left = 0;
+    int steps = 0;
     {
         Walk count(a.cut, pair);
         Piece piece;
-        while (count.next(piece)) left += piece.count;
+        while (count.next(piece)) steps += piece.count;
     }
-    uint32_t stage = 0, phase = 0, raw = 0, raw_phase = 0;
+    uint32_t stage = group, phase = 0, raw = group, raw_phase = 0;
     const uint32_t empty = smem_addr(&sh.empty[0]), dy_full = smem_addr(&sh.dy_full[0]);
     const uint32_t raw_full = smem_addr(&sh.raw_full[0]), raw_empty = smem_addr(&sh.raw_empty[0]);
     const uint32_t lead_full = at_rank(smem_addr(&sh.full[0]), 0);
     const bool passes_on = rank == 1 && warp == 0;
-    for (; left > 0; --left) {
+    for (int step = group; step < steps; step += kFillGroups) {
         if (!mbar_wait_warp(raw_full + raw * 8, raw_phase)) return;
-        uint32_t q[2][4], e;
+        uint32_t q[4][4], e[2];
         const uint32_t src = src0 + raw * kRawBytes;
-        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(e) : "r"(exp0 + raw * (kRows * 4)));
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q[h][0]), "=r"(q[h][1]), "=r"(q[h][2]), "=r"(q[h][3])
-                         : "r"(src ^ h << 4));
+        for (int k = 0; k < 2; ++k) {
+            asm volatile("ld.shared.u8 %0, [%1];" : "=r"(e[k]) : "r"(exp0 + raw * (kRows * 4) + k * 64));
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q[2 * k + h][0]), "=r"(q[2 * k + h][1]),
+                             "=r"(q[2 * k + h][2]), "=r"(q[2 * k + h][3]) : "r"((src ^ h << 4) + k * 2048));
+        }
         if (!mbar_wait_warp(empty + stage * 8, phase ^ 1)) return;
-        const uint32_t s = e ? e << 7 : 0x40u;          // 2^(e - 127) in bf16 (255: infinity)
         const uint32_t dst = dst0 + stage * kStageBytes;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            uint32_t v[8];
-            codes_to_bf16(q[h], s | s << 16, v);
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst ^ (2 * h) << 4), "r"(v[0]), "r"(v[1]),
-                         "r"(v[2]), "r"(v[3]) : "memory");
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst ^ (2 * h + 1) << 4), "r"(v[4]), "r"(v[5]),
-                         "r"(v[6]), "r"(v[7]) : "memory");
+        for (int k = 0; k < 2; ++k) {
+            const uint32_t s = e[k] ? e[k] << 7 : 0x40u;        // 2^(e - 127) in bf16 (255: infinity)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t v[8];
+                codes_to_bf16(q[2 * k + h], s | s << 16, v);
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"((dst ^ (2 * h) << 4) + k * 2048), "r"(v[0]),
+                             "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"((dst ^ (2 * h + 1) << 4) + k * 2048), "r"(v[4]),
+                             "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+            }
         }
         fence_async_shared();
         // the leading CTA's products read this CTA's dy too: its arrival is passed on
@@ -407,8 +421,27 @@ __device__ __forceinline__ void fill_x(const KernelArgs &a, Shared &sh, uint32_t
             mbar_arrive_cluster(lead_full + stage * 8);
             mbar_arrive(raw_empty + raw * 8);
         }
-        if (++stage == kStages) { stage = 0; phase ^= 1; }
-        if (++raw == kRaws) { raw = 0; raw_phase ^= 1; }
+        stage += kFillGroups;
+        if (stage >= kStages) { stage -= kStages; phase ^= 1; }
+        raw += kFillGroups;
+        if (raw >= kRaws) { raw -= kRaws; raw_phase ^= 1; }
+    }
+}
+
+// Four neighbouring elements of dW's row, column k on.
+template <typename Args>
+__device__ __forceinline__ void store_four(const Args &a, int64_t at, int64_t k, float x0, float x1, float x2, float x3)
+{
+    if (a.vector && k < a.n_in) {           // n_in is a multiple of 4 and dw aligned to four elements
+        if (a.grad_type == NOVAK_TYPE_F32)
+            *reinterpret_cast<float4 *>(static_cast<float *>(a.dw) + at) = make_float4(x0, x1, x2, x3);
+        else
+            *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(a.dw) + at) = make_uint2(bf16_pair(x0, x1), bf16_pair(x2, x3));
+    } else {
+        const float x[4] = {x0, x1, x2, x3};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (k + i < a.n_in) store_param(a.dw, a.grad_type, at + i, x[i]);
     }
 }
 
@@ -460,16 +493,20 @@ __device__ __forceinline__ void take_out(const KernelArgs &a, Shared &sh, uint32
             for (int i = 0; i < 32; ++i)
                 dst[i * 256] = make_float4(total[4 * i], total[4 * i + 1], total[4 * i + 2], total[4 * i + 3]);
         } else {
+            // through shared memory: four neighbouring columns of eight rows per store
             float *turn = sh.turn[warp];
-            const int64_t row0 = n0 + quarter * 32 + lane / 16, k0 = static_cast<int64_t>(tk) * kTileK + side * 128 + lane % 16;
+            const int row = lane / 4, col = lane % 4 * 4;
+            const int64_t row0 = n0 + quarter * 32 + row, k0 = static_cast<int64_t>(tk) * kTileK + side * 128 + col;
 #pragma unroll
             for (int c = 0; c < 128; c += 16) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) turn[lane * kPad + i] = total[c + i];
                 __syncwarp();
-                if (k0 + c < a.n_in)
-                    for (int i = 0; i < 32 && row0 + i < a.n_out; i += 2)
-                        store_param(a.dw, a.grad_type, (row0 + i) * a.n_in + k0 + c, turn[(lane / 16 + i) * kPad + lane % 16]);
+#pragma unroll
+                for (int i = 0; i < 32; i += 8) {
+                    const float *src = turn + (row + i) * kPad + col;
+                    if (row0 + i < a.n_out) store_four(a, (row0 + i) * a.n_in + k0 + c, k0 + c, src[0], src[1], src[2], src[3]);
+                }
                 __syncwarp();
             }
         }
@@ -547,12 +584,12 @@ novak_weight_grad_kernel(const __grid_constant__ KernelArgs a, const __grid_cons
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
             mbar_init(smem_addr(&sh.dy_full[s]), 1);
-            mbar_init(smem_addr(&sh.full[s]), 2 * kFillWarps);
+            mbar_init(smem_addr(&sh.full[s]), 2 * kGroupWarps);
             mbar_init(smem_addr(&sh.empty[s]), a.sums ? 1 + kSumWarps : 1);
         }
         for (int r = 0; r < kRaws; ++r) {
             mbar_init(smem_addr(&sh.raw_full[r]), 2);
-            mbar_init(smem_addr(&sh.raw_empty[r]), kFillWarps);
+            mbar_init(smem_addr(&sh.raw_empty[r]), kGroupWarps);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(smem_addr(&sh.out_full[b]), 1);
@@ -568,20 +605,19 @@ novak_weight_grad_kernel(const __grid_constant__ KernelArgs a, const __grid_cons
     tcgen05_after_sync();
     const uint32_t tmem = sh.tmem;
 
+    // (every warp of a warpgroup executes the same one of the two)
+    if (warp < kOutWarps) registers_up<kOutRegs>();
+    else registers_down<kOtherRegs>();
+
     if (warp < kOutWarps) {
-        registers_up<kOutRegs>();
         take_out(a, sh, tmem, rank, pair);
     } else if (warp < kLoadWarp) {
-        registers_down<kOtherRegs>();
         fill_x(a, sh, stages, raws, rank, pair);
     } else if (warp < kCopyWarp) {
-        registers_down<kOtherRegs>();
         load_codes(a, &codes_map, sh, raws, rank, pair);
     } else if (warp >= kSumWarp) {
-        registers_down<kOtherRegs>();
         if (a.sums) sum_dy(a, sh, stages, rank, pair);
     } else {
-        registers_down<kOtherRegs>();
         Walk walk(cut, pair);
         Piece piece;
         bool ok = true;
@@ -662,35 +698,37 @@ struct FinishArgs {
     const void *weight, *bias;
     int param_type;
     void *dw, *db;
-    int grad_type;
+    int grad_type, vector;
     int64_t n_out, n_in;
-    int first_tile, n_tiles;        // to be added up; then tiles_n blocks x 8 for db
+    int first_tile, n_tiles;        // to be added up; then tiles_n for db
 };
 
-// 32 rows of a tile per CTA.
+// kFinishRows rows of a tile per CTA, two groups of four columns of one per thread.
+constexpr int kFinishRows = 8, kFinishCtas = kTileN / kFinishRows;
 __global__ void __launch_bounds__(256) novak_weight_grad_finish_kernel(const __grid_constant__ FinishArgs a)
 {
-    __shared__ float turn[32][257], part[8][33], total[32];
+    __shared__ float part[32][kFinishRows + 1], total[kFinishRows];
+    __shared__ float turn[kFinishRows][kTileK + 4];
     const Cut &cut = a.cut;
-    const int group = blockIdx.x % 8, item = blockIdx.x / 8;
+    const int group = blockIdx.x % kFinishCtas, item = blockIdx.x / kFinishCtas;
     const bool for_db = item >= a.n_tiles;
     int tn, tk = 0, slot, n;
     if (for_db) tn = item - a.n_tiles;
     else tile_at(cut, a.first_tile + item, tn, tk);
-    const int row = threadIdx.x % 32, lane8 = threadIdx.x / 32;
-    const int64_t n0 = static_cast<int64_t>(tn) * kTileN + group * 32;
+    const int row = threadIdx.x % kFinishRows, lane = threadIdx.x / kFinishRows;
+    const int64_t n0 = static_cast<int64_t>(tn) * kTileN + group * kFinishRows;
     if (n0 >= a.n_out) return;
     if (for_db || a.weight) {
         float s = 0.0f;
-        for (int k = lane8; k < cut.tiles_k; k += 8) {
+        for (int k = lane; k < cut.tiles_k; k += 32) {
             tile_slots(cut, tile_index(cut, tn, k), slot, n);
-            for (int i = 0; i < n; ++i) s += a.sums[static_cast<int64_t>(slot + i) * 256 + group * 32 + row];
+            for (int i = 0; i < n; ++i) s += a.sums[static_cast<int64_t>(slot + i) * 256 + group * kFinishRows + row];
         }
-        part[lane8][row] = s;
+        part[lane][row] = s;
         __syncthreads();
-        if (threadIdx.x < 32) {
+        if (threadIdx.x < kFinishRows) {
             s = 0.0f;
-            for (int i = 0; i < 8; ++i) s += part[i][row];
+            for (int i = 0; i < 32; ++i) s += part[i][row];
             total[row] = s;
             if (for_db && n0 + row < a.n_out) store_param(a.db, a.grad_type, n0 + row, s);
         }
@@ -698,27 +736,34 @@ __global__ void __launch_bounds__(256) novak_weight_grad_finish_kernel(const __g
     }
     tile_slots(cut, a.first_tile + item, slot, n);
     if (n == 1 && !cut.all_partial) return;         // stored as it was
-    for (int c = lane8; c < 64; c += 8) {
-        const float4 *src = reinterpret_cast<const float4 *>(a.partial) + (static_cast<int64_t>(slot) * 64 + c) * 256 + group * 32 + row;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int c = lane + 32 * j;
+        const float4 *src = reinterpret_cast<const float4 *>(a.partial) + (static_cast<int64_t>(slot) * 64 + c) * 256 +
+                            group * kFinishRows + row;
         float4 v = make_float4(0, 0, 0, 0);
+#pragma unroll 4
         for (int i = 0; i < n; ++i) {
             const float4 p = src[static_cast<int64_t>(i) * 64 * 256];
             v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
         }
-        turn[row][4 * c] = v.x;
-        turn[row][4 * c + 1] = v.y;
-        turn[row][4 * c + 2] = v.z;
-        turn[row][4 * c + 3] = v.w;
+        *reinterpret_cast<float4 *>(&turn[row][4 * c]) = v;
     }
     __syncthreads();
-    const int64_t k = static_cast<int64_t>(tk) * kTileK + threadIdx.x;
-    if (k >= a.n_in) return;
-    const float w = a.weight ? param_at(a.weight, a.param_type, k) : 1.0f;
-    const float b = a.weight ? param_at(a.bias, a.param_type, k) : 0.0f;
-    for (int i = 0; i < 32 && n0 + i < a.n_out; ++i) {
-        float v = turn[i][threadIdx.x];
-        if (a.weight) v = fmaf(v, w, b * total[i]);
-        store_param(a.dw, a.grad_type, (n0 + i) * a.n_in + k, v);
+    const int64_t k0 = static_cast<int64_t>(tk) * kTileK;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int r = threadIdx.x / 64 + 4 * j, c = threadIdx.x % 64 * 4;
+        const int64_t k = k0 + c;
+        if (n0 + r >= a.n_out || k >= a.n_in) continue;
+        float x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = turn[r][c + i];
+            if (a.weight && k + i < a.n_in)
+                x[i] = fmaf(x[i], param_at(a.weight, a.param_type, k + i), param_at(a.bias, a.param_type, k + i) * total[r]);
+        }
+        store_four(a, (n0 + r) * a.n_in + k, k, x[0], x[1], x[2], x[3]);
     }
 }
 
@@ -845,19 +890,21 @@ cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t stream)
     if (e != cudaSuccess) return e;
 
     const bool sums = a.db || a.weight;
-    KernelArgs k{l.cut, a.codes, act_pitch(a.n_in), a.dw, a.grad_type, a.rows, a.n_out, a.n_in,
+    const int vector = a.n_in % 4 == 0 && reinterpret_cast<uintptr_t>(a.dw) % (a.grad_type == NOVAK_TYPE_F32 ? 16 : 8) == 0;
+    KernelArgs k{l.cut, a.codes, act_pitch(a.n_in), a.dw, a.grad_type, vector, a.rows, a.n_out, a.n_in,
                  reinterpret_cast<float *>(work + l.planes_bytes), nullptr};
     float *sums_at = reinterpret_cast<float *>(work + l.planes_bytes + l.partial_bytes);
     if (sums) k.sums = sums_at;
     const int pairs = l.cut.waves > 0 ? l.cut.pairs : l.cut.rest_pairs;
     novak_weight_grad_kernel<<<2 * pairs, kThreads, kSmemBytes, stream>>>(k, map, codes_map);
 
-    FinishArgs f{l.cut, k.partial, sums_at, a.weight, a.bias, a.param_type, a.dw, a.db, a.grad_type, a.n_out, a.n_in, 0, 0};
+    FinishArgs f{l.cut, k.partial, sums_at, a.weight, a.bias, a.param_type, a.dw, a.db, a.grad_type, vector,
+                 a.n_out, a.n_in, 0, 0};
     const int tiles = l.cut.tiles_n * l.cut.tiles_k, whole = l.cut.waves * l.cut.pairs;
     f.first_tile = l.cut.all_partial ? 0 : whole;
     f.n_tiles = tiles - f.first_tile;
-    const int blocks = 8 * (f.n_tiles + (a.db ? l.cut.tiles_n : 0));
-    if (blocks > 0) novak_weight_grad_finish_kernel<<<blocks, 256, 0, stream>>>(f);
+    const int64_t blocks = static_cast<int64_t>(kFinishCtas) * (f.n_tiles + (a.db ? l.cut.tiles_n : 0));
+    if (blocks > 0) novak_weight_grad_finish_kernel<<<static_cast<unsigned>(blocks), 256, 0, stream>>>(f);
     return cudaGetLastError();
 }
 

@@ -23,6 +23,14 @@ __device__ __forceinline__ uint32_t at_rank(uint32_t addr, uint32_t rank)
     return r;
 }
 
+// One lane of a converged warp.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(p));
+    return p != 0;
+}
+
 __device__ __forceinline__ uint32_t cluster_rank()
 {
     uint32_t r;
@@ -79,13 +87,16 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
     return done != 0;
 }
 
+// (The clock is slow to read: only a wait that has gone wrong looks at it.)
 __device__ __forceinline__ bool mbar_wait_long(uint32_t bar, uint32_t parity)
 {
-    const uint64_t t0 = global_ns();
+    uint64_t t0 = 0;
     for (;;) {
-        for (int i = 0; i < 64; ++i)
+        for (int i = 0; i < 2048; ++i)
             if (mbar_try(bar, parity)) return true;
-        if (global_ns() - t0 > kWaitNs) return false;
+        const uint64_t t = global_ns();
+        if (t0 == 0) t0 = t;
+        else if (t - t0 > kWaitNs) return false;
     }
 }
 
@@ -163,6 +174,19 @@ __device__ __forceinline__ void tmem_load16(uint32_t tmem, float (&v)[16])
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
+
+// The other way.
+__device__ __forceinline__ void tmem_store16(uint32_t tmem, const float *v)
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(tmem), "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])), "r"(__float_as_uint(v[3])),
+          "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])), "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7])),
+          "r"(__float_as_uint(v[8])), "r"(__float_as_uint(v[9])), "r"(__float_as_uint(v[10])), "r"(__float_as_uint(v[11])),
+          "r"(__float_as_uint(v[12])), "r"(__float_as_uint(v[13])), "r"(__float_as_uint(v[14])), "r"(__float_as_uint(v[15])) : "memory");
+}
+__device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Moves registers between the CTA's warpgroups; every warp of one executes it.
 template <int N> __device__ __forceinline__ void registers_up()

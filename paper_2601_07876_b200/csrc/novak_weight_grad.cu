@@ -468,8 +468,6 @@ __device__ __forceinline__ void take_out(const KernelArgs &a, Shared &sh, uint32
             ok = mbar_wait_warp(smem_addr(&sh.out_full[buf]), (n >> 1) & 1);
             if (!ok) {
                 if (lane == 0) atomicAdd(&g_gave_up, 1u);
-#pragma unroll
-                for (int i = 0; i < 128; ++i) total[i] = __uint_as_float(0x7fffffffu);     // nobody takes it for a result
                 break;
             }
             tcgen05_after_sync();
@@ -481,26 +479,39 @@ __device__ __forceinline__ void take_out(const KernelArgs &a, Shared &sh, uint32
 #pragma unroll
                 for (int i = 0; i < 16; ++i) total[c + i] += v[i];
             }
+            if (left <= kRun) break;            // the last run's columns stay this warp's for a while
             tcgen05_before_sync();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(at_rank(smem_addr(&sh.out_empty[buf]), 0));
             ++n;
         }
-        if (!piece.whole || cut.all_partial) {
-            float4 *dst = reinterpret_cast<float4 *>(a.partial) + (static_cast<int64_t>(piece.slot) * 64 + side * 32) * 256 +
-                          rank * 128 + quarter * 32 + lane;
+        // The tile goes out in a loop, not unrolled over the registers it is in: code that runs
+        // once per tile comes from far away.  So it goes through tensor memory once more.
+        const uint32_t at = tmem + (n & 1) * 256 + side * 128 + (static_cast<uint32_t>(quarter) * 32 << 16);
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-                dst[i * 256] = make_float4(total[4 * i], total[4 * i + 1], total[4 * i + 2], total[4 * i + 3]);
-        } else {
-            // through shared memory: four neighbouring columns of eight rows per store
-            float *turn = sh.turn[warp];
-            const int row = lane / 4, col = lane % 4 * 4;
-            const int64_t row0 = n0 + quarter * 32 + row, k0 = static_cast<int64_t>(tk) * kTileK + side * 128 + col;
+        for (int c = 0; c < 128; c += 16) tmem_store16(at + c, total + c);
+        tmem_store_wait();
+        const bool partial = !piece.whole || cut.all_partial;
+        float4 *dst = reinterpret_cast<float4 *>(a.partial) + (static_cast<int64_t>(piece.slot) * 64 + side * 32) * 256 +
+                      rank * 128 + quarter * 32 + lane;
+        float *turn = sh.turn[warp];
+        const int row = lane / 4, col = lane % 4 * 4;
+        const int64_t row0 = n0 + quarter * 32 + row, k0 = static_cast<int64_t>(tk) * kTileK + side * 128 + col;
+#pragma unroll 1
+        for (int c = 0; c < 128; c += 16) {
+            float v[16];
+            tmem_load16(at + c, v);
+            if (!ok)        // nobody takes this for a result
 #pragma unroll
-            for (int c = 0; c < 128; c += 16) {
+                for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(0x7fffffffu);
+            if (partial) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) turn[lane * kPad + i] = total[c + i];
+                for (int i = 0; i < 4; ++i)
+                    dst[(c / 4 + i) * 256] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            } else {
+                // through shared memory: four neighbouring columns of eight rows per store
+#pragma unroll
+                for (int i = 0; i < 16; ++i) turn[lane * kPad + i] = v[i];
                 __syncwarp();
 #pragma unroll
                 for (int i = 0; i < 32; i += 8) {
@@ -510,6 +521,11 @@ __device__ __forceinline__ void take_out(const KernelArgs &a, Shared &sh, uint32
                 __syncwarp();
             }
         }
+        if (!ok) break;
+        tcgen05_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(at_rank(smem_addr(&sh.out_empty[n & 1]), 0));
+        ++n;
     }
 }
 
@@ -651,35 +667,41 @@ novak_weight_grad_kernel(const __grid_constant__ KernelArgs a, const __grid_cons
             if (!ok)
                 for (int64_t i = max(issued - kStages, int64_t(0)); i < issued; ++i)
                     mbar_wait(smem_addr(&sh.dy_full[i % kStages]), (i / kStages) & 1);
-        } else if (warp == kMmaWarp && lane == 0 && rank == 0) {
-            // ---- the products
+        } else if (warp == kMmaWarp && rank == 0) {
+            // ---- the products.  The warp stays together and one lane issues, so that the
+            // descriptors are the warp's: formed by a lane on its own they cost more time
+            // than the products take.
             uint32_t n = 0;
             constexpr uint32_t idesc = instr_desc(256, 256);
+            const uint64_t dy0 = operand_desc(stages, kHalf, 1024), x0 = operand_desc(stages + 2 * kHalf, kHalf, 1024);
             while (ok && walk.next(piece)) {
                 for (int left = piece.count; ok && left > 0; ++n) {
                     const int run = min(left, kRun);
                     left -= run;
-                    const uint32_t buf = n & 1;
-                    ok = mbar_wait(smem_addr(&sh.out_empty[buf]), ((n >> 1) & 1) ^ 1);
+                    const uint32_t buf = n & 1, d = tmem + buf * 256;
+                    ok = mbar_wait_warp(smem_addr(&sh.out_empty[buf]), ((n >> 1) & 1) ^ 1);
                     tcgen05_after_sync();
                     for (int i = 0; ok && i < run; ++i) {
-                        ok = mbar_wait(smem_addr(&sh.full[stage]), phase) && mbar_wait(smem_addr(&sh.dy_full[stage]), phase);
+                        ok = mbar_wait_warp(smem_addr(&sh.full[stage]), phase) && mbar_wait_warp(smem_addr(&sh.dy_full[stage]), phase);
                         if (!ok) break;
                         tcgen05_after_sync();
-                        const uint32_t base = stages + stage * kStageBytes;
+                        const uint64_t at = static_cast<uint64_t>(stage) * (kStageBytes >> 4);
+                        if (elect_one()) {
 #pragma unroll
-                        for (int k = 0; k < kRows / 16; ++k)
-                            mma_pair_bf16(tmem + buf * 256, operand_desc(base + k * 2048, kHalf, 1024),
-                                          operand_desc(base + 2 * kHalf + k * 2048, kHalf, 1024), idesc, i > 0 || k > 0);
-                        mma_commit_pair(smem_addr(&sh.empty[stage]));
+                            for (int k = 0; k < kRows / 16; ++k)
+                                mma_pair_bf16(d, dy0 + at + k * (2048 >> 4), x0 + at + k * (2048 >> 4), idesc, i > 0 || k > 0);
+                            mma_commit_pair(smem_addr(&sh.empty[stage]));
+                            if (i == run - 1) mma_commit_pair(smem_addr(&sh.out_full[buf]));
+                        }
+                        __syncwarp();
                         if (++stage == kStages) { stage = 0; phase ^= 1; }
                     }
-                    if (ok) mma_commit_pair(smem_addr(&sh.out_full[buf]));
                 }
             }
             if (!ok) {      // products in flight end before their operands and sums go
-                mma_commit_pair(smem_addr(&sh.drained));
-                mbar_wait(smem_addr(&sh.drained), 0);
+                if (elect_one()) mma_commit_pair(smem_addr(&sh.drained));
+                __syncwarp();
+                mbar_wait_warp(smem_addr(&sh.drained), 0);
             }
         }
     }

@@ -16,9 +16,7 @@
 //   warp 20      dy by tensor copies,
 //   warp 21      the products (of the pair: in the leading CTA),
 //   warps 22-23  sums of dy's columns.
-// (The warps that hand x to the tensor cores load nothing from global memory: the
-// proxy fence that each step needs waits for a thread's loads in flight, which
-// made every step as long as a load, 3200 cycles instead of the products' 512.)
+//
 // dy and x both have the summed dimension (rows) outermost, so both operands are
 // "M-major" and neither is transposed.
 //
@@ -250,10 +248,9 @@ __device__ __forceinline__ void tile_slots(const Cut &c, int tile, int &slot, in
 }
 
 // ---- the kernel ----------------------------------------------------------------------
-constexpr int kStages = 5;
-constexpr int kStageBytes = 2 * 128 * kRows * 2;        // dy and x: 128 columns each, bf16
-constexpr int kHalf = 64 * kRows * 2;                   // 64 columns of an operand
-constexpr int kRaws = 4;        // steps of codes on their way
+constexpr int kDySlots = 6, kXSlots = 3, kRawSlots = 8;         // steps of dy, of x, of codes
+constexpr int kHalf = 64 * kRows * 2;                   // 64 columns of an operand, bf16
+constexpr int kSlotBytes = 2 * kHalf;                   // 128 columns
 constexpr int kRawBytes = 128 * kRows;                  // codes of 128 columns
 constexpr int kRun = 16;        // steps that the tensor cores add up by themselves: their sums round toward
                                 // zero, so that a chain's error grows with its length
@@ -265,20 +262,37 @@ constexpr int kThreads = 32 * (kSumWarp + kSumWarps);
 // A barrier's parity tells one phase from the next, not from the one after that: whoever
 // waits for a slot's use number k has to know that use k - 1 is over.  The two groups do
 // not finish steps in order among each other, so a slot of codes belongs to one group for
-// good; the products free the stages in order.
-static_assert(kRaws % kFillGroups == 0 && kRaws % kLoadWarps == 0, "slots of codes change hands");
-constexpr int kPad = 17;
+// good; the products free the slots of dy and x in order.
+static_assert(kRawSlots % kFillGroups == 0 && kRawSlots % kLoadWarps == 0, "slots of codes change hands");
+static_assert(kXSlots <= kDySlots, "a step's end is kept for as long as dy's slots last");
+constexpr int kPad = 9;
 // Registers per thread: 80 at launch, 768 x 80 = 61440 = 256 x 160 + 512 x 40.
 constexpr int kOutRegs = 160, kOtherRegs = 40;
 
 struct Shared {
-    alignas(8) uint64_t dy_full[kStages], full[kStages], empty[kStages], raw_full[kRaws], raw_empty[kRaws], out_full[2],
-        out_empty[2], drained;
+    alignas(8) uint64_t dy_full[kDySlots], full[kXSlots], filled[kXSlots], raw_full[kRawSlots], raw_empty[kRawSlots], out_full[2], out_empty[2],
+        drained;
+    uint64_t done[kDySlots];            // a step's products are over: step i's is done[i % kDySlots]
     uint32_t tmem;
-    uint32_t exps[kRaws][kRows];        // of four blocks
+    uint32_t exps[kRawSlots][kRows];    // of four blocks
     float turn[kOutWarps][32 * kPad];
 };
-constexpr int kSmemBytes = kStages * kStageBytes + kRaws * kRawBytes + 1024 + static_cast<int>(sizeof(Shared));
+constexpr int kSmemBytes = (kDySlots + kXSlots) * kSlotBytes + kRawSlots * kRawBytes + 1024 + static_cast<int>(sizeof(Shared));
+static_assert(kSmemBytes <= 227 * 1024, "shared memory");
+
+// A position in a ring of N slots, and the parity of its use.
+template <int N> struct Ring {
+    uint32_t slot, phase = 0;
+    __device__ explicit Ring(uint32_t first = 0) : slot(first) {}
+    __device__ __forceinline__ void advance(int n = 1)
+    {
+        slot += n;
+        if (slot >= N) {
+            slot -= N;
+            phase ^= 1;
+        }
+    }
+};
 
 struct KernelArgs {
     Cut cut;
@@ -318,8 +332,9 @@ __device__ __forceinline__ void load_codes(const KernelArgs &a, const CUtensorMa
     const bool words = (blocks & 3) == 0 && (reinterpret_cast<uintptr_t>(a.codes.exps) & 3) == 0;
     Walk walk(a.cut, pair);
     Piece piece;
-    uint32_t raw = 0, phase = 0, step = 0, last_phase = 0;
-    int last = -1;
+    Ring<kRawSlots> raw, last;
+    uint32_t step = 0;
+    bool any = false;
     while (walk.next(piece)) {
         int tn, tk;
         tile_at(a.cut, piece.tile, tn, tk);
@@ -327,16 +342,16 @@ __device__ __forceinline__ void load_codes(const KernelArgs &a, const CUtensorMa
         const int64_t block0 = static_cast<int64_t>(tk) * (kTileK / 32) + rank * 4;
         for (int i = 0; i < piece.count; ++i, ++step, at.advance(a.cut)) {
             if (step % kLoadWarps == mine) {
-                if (!mbar_wait_warp(smem_addr(&sh.raw_empty[raw]), phase ^ 1)) {
-                    if (last >= 0) mbar_wait_warp(smem_addr(&sh.raw_full[last]), last_phase);     // its copy in flight
+                if (!mbar_wait_warp(smem_addr(&sh.raw_empty[raw.slot]), raw.phase ^ 1)) {
+                    if (any) mbar_wait_warp(smem_addr(&sh.raw_full[last.slot]), last.phase);      // its copy in flight
                     return;
                 }
-                last = static_cast<int>(raw);
-                last_phase = phase;
-                const uint32_t bar = smem_addr(&sh.raw_full[raw]);
+                last = raw;
+                any = true;
+                const uint32_t bar = smem_addr(&sh.raw_full[raw.slot]);
                 if (lane == 0) {
                     mbar_expect(bar, kRawBytes);
-                    tma_load_2d(raws + raw * kRawBytes, map, static_cast<int>(block0) * 32, at.chunk * kRows, bar);
+                    tma_load_2d(raws + raw.slot * kRawBytes, map, static_cast<int>(block0) * 32, at.chunk * kRows, bar);
                 }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -352,12 +367,12 @@ __device__ __forceinline__ void load_codes(const KernelArgs &a, const CUtensorMa
                                 if (block0 + k < blocks) e |= static_cast<uint32_t>(__ldg(src + k)) << (8 * k);
                         }
                     }
-                    sh.exps[raw][lane + 32 * h] = e;
+                    sh.exps[raw.slot][lane + 32 * h] = e;
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar);
             }
-            if (++raw == kRaws) { raw = 0; phase ^= 1; }
+            raw.advance();
         }
     }
 }
@@ -367,12 +382,11 @@ __device__ __forceinline__ void load_codes(const KernelArgs &a, const CUtensorMa
 // which the 128-byte swizzle spreads over all banks, of the codes and of x.  Two groups
 // of four warps have every other step each: a step's waits, its proxy fence and its
 // arrival take longer than its arithmetic.
-__device__ __forceinline__ void fill_x(const KernelArgs &a, Shared &sh, uint32_t stages, uint32_t raws, uint32_t rank,
-                                       int pair)
+__device__ __forceinline__ void fill_x(const KernelArgs &a, Shared &sh, uint32_t xs, uint32_t raws, uint32_t rank, int pair)
 {
     const int group = (threadIdx.x / 32 - kOutWarps) / kGroupWarps, warp = (threadIdx.x / 32 - kOutWarps) % kGroupWarps;
     const int lane = threadIdx.x % 32, half = warp & 1, r = (warp >> 1) * 32 + (lane & 15), b = lane >> 4;
-    const uint32_t dst0 = stages + 2 * kHalf + half * kHalf + r * 128 + ((4 * b ^ (r & 7)) << 4);
+    const uint32_t dst0 = xs + half * kHalf + r * 128 + ((4 * b ^ (r & 7)) << 4);
     const uint32_t src0 = raws + r * 128 + (((half * 4 + b * 2) ^ (r & 7)) << 4);
     const uint32_t exp0 = smem_addr(&sh.exps[0][0]) + r * 4 + half * 2 + b;
     int steps = 0;
@@ -381,25 +395,26 @@ __device__ __forceinline__ void fill_x(const KernelArgs &a, Shared &sh, uint32_t
         Piece piece;
         while (count.next(piece)) steps += piece.count;
     }
-    uint32_t stage = group, phase = 0, raw = group, raw_phase = 0;
-    const uint32_t empty = smem_addr(&sh.empty[0]), dy_full = smem_addr(&sh.dy_full[0]);
+    Ring<kXSlots> x(group);
+    Ring<kRawSlots> raw(group);
+    Ring<kDySlots> before(kDySlots + group - kXSlots);      // the step that had x's slot before
+    before.phase = 1;
+    const uint32_t done = smem_addr(&sh.done[0]), filled = smem_addr(rank == 0 ? &sh.full[0] : &sh.filled[0]);
     const uint32_t raw_full = smem_addr(&sh.raw_full[0]), raw_empty = smem_addr(&sh.raw_empty[0]);
-    const uint32_t lead_full = at_rank(smem_addr(&sh.full[0]), 0);
-    const bool passes_on = rank == 1 && warp == 0;
     for (int step = group; step < steps; step += kFillGroups) {
-        if (!mbar_wait_warp(raw_full + raw * 8, raw_phase)) return;
+        if (!mbar_wait_warp(raw_full + raw.slot * 8, raw.phase)) return;
         uint32_t q[4][4], e[2];
-        const uint32_t src = src0 + raw * kRawBytes;
+        const uint32_t src = src0 + raw.slot * kRawBytes;
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            asm volatile("ld.shared.u8 %0, [%1];" : "=r"(e[k]) : "r"(exp0 + raw * (kRows * 4) + k * 64));
+            asm volatile("ld.shared.u8 %0, [%1];" : "=r"(e[k]) : "r"(exp0 + raw.slot * (kRows * 4) + k * 64));
 #pragma unroll
             for (int h = 0; h < 2; ++h)
                 asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q[2 * k + h][0]), "=r"(q[2 * k + h][1]),
                              "=r"(q[2 * k + h][2]), "=r"(q[2 * k + h][3]) : "r"((src ^ h << 4) + k * 2048));
         }
-        if (!mbar_wait_warp(empty + stage * 8, phase ^ 1)) return;
-        const uint32_t dst = dst0 + stage * kStageBytes;
+        if (!mbar_wait_warp(done + before.slot * 8, before.phase)) return;
+        const uint32_t dst = dst0 + x.slot * kSlotBytes;
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             const uint32_t s = e[k] ? e[k] << 7 : 0x40u;        // 2^(e - 127) in bf16 (255: infinity)
@@ -414,17 +429,14 @@ __device__ __forceinline__ void fill_x(const KernelArgs &a, Shared &sh, uint32_t
             }
         }
         fence_async_shared();
-        // the leading CTA's products read this CTA's dy too: its arrival is passed on
-        if (passes_on && !mbar_wait_warp(dy_full + stage * 8, phase)) return;
         __syncwarp();
         if (lane == 0) {
-            mbar_arrive_cluster(lead_full + stage * 8);
-            mbar_arrive(raw_empty + raw * 8);
+            mbar_arrive(filled + x.slot * 8);
+            mbar_arrive(raw_empty + raw.slot * 8);
         }
-        stage += kFillGroups;
-        if (stage >= kStages) { stage -= kStages; phase ^= 1; }
-        raw += kFillGroups;
-        if (raw >= kRaws) { raw -= kRaws; raw_phase ^= 1; }
+        x.advance(kFillGroups);
+        raw.advance(kFillGroups);
+        before.advance(kFillGroups);
     }
 }
 
@@ -495,7 +507,7 @@ __device__ __forceinline__ void take_out(const KernelArgs &a, Shared &sh, uint32
         float4 *dst = reinterpret_cast<float4 *>(a.partial) + (static_cast<int64_t>(piece.slot) * 64 + side * 32) * 256 +
                       rank * 128 + quarter * 32 + lane;
         float *turn = sh.turn[warp];
-        const int row = lane / 4, col = lane % 4 * 4;
+        const int row = lane / 2, col = lane % 2 * 4;
         const int64_t row0 = n0 + quarter * 32 + row, k0 = static_cast<int64_t>(tk) * kTileK + side * 128 + col;
 #pragma unroll 1
         for (int c = 0; c < 128; c += 16) {
@@ -509,16 +521,20 @@ __device__ __forceinline__ void take_out(const KernelArgs &a, Shared &sh, uint32
                 for (int i = 0; i < 4; ++i)
                     dst[(c / 4 + i) * 256] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
             } else {
-                // through shared memory: four neighbouring columns of eight rows per store
+                // through shared memory: four neighbouring columns of sixteen rows per store
 #pragma unroll
-                for (int i = 0; i < 16; ++i) turn[lane * kPad + i] = v[i];
-                __syncwarp();
+                for (int h = 0; h < 16; h += 8) {
 #pragma unroll
-                for (int i = 0; i < 32; i += 8) {
-                    const float *src = turn + (row + i) * kPad + col;
-                    if (row0 + i < a.n_out) store_four(a, (row0 + i) * a.n_in + k0 + c, k0 + c, src[0], src[1], src[2], src[3]);
+                    for (int i = 0; i < 8; ++i) turn[lane * kPad + i] = v[h + i];
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 32; i += 16) {
+                        const float *src = turn + (row + i) * kPad + col;
+                        const int64_t k = k0 + c + h;
+                        if (row0 + i < a.n_out) store_four(a, (row0 + i) * a.n_in + k, k, src[0], src[1], src[2], src[3]);
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
             }
         }
         if (!ok) break;
@@ -531,23 +547,23 @@ __device__ __forceinline__ void take_out(const KernelArgs &a, Shared &sh, uint32
 
 // Warps kSumWarp, + 1: sums over dy's columns, 64 columns of a warp, from shared
 // memory.  The tiles of a tile row share the chunks of rows among them.
-__device__ __forceinline__ void sum_dy(const KernelArgs &a, Shared &sh, uint32_t stages, uint32_t rank, int pair)
+__device__ __forceinline__ void sum_dy(const KernelArgs &a, Shared &sh, uint32_t dys, uint32_t rank, int pair)
 {
     const Cut &cut = a.cut;
     const int half = threadIdx.x / 32 - kSumWarp, lane = threadIdx.x % 32;
     const int chunk = lane % 8, row0 = lane / 8;        // 8 columns of every fourth row
     Walk walk(cut, pair);
     Piece piece;
-    uint32_t stage = 0, phase = 0;
+    Ring<kDySlots> dy;
     while (walk.next(piece)) {
         int tn, tk;
         tile_at(cut, piece.tile, tn, tk);
         StepPos at(cut, piece.first);
         float s[8] = {}, total[8] = {};
         for (int i = 0; i < piece.count; ++i, at.advance(cut)) {
-            if (!mbar_wait_warp(smem_addr(&sh.dy_full[stage]), phase)) return;
+            if (!mbar_wait_warp(smem_addr(&sh.dy_full[dy.slot]), dy.phase)) return;
             if (at.chunk % cut.tiles_k == tk) {
-                const uint32_t src = stages + stage * kStageBytes + half * kHalf;
+                const uint32_t src = dys + dy.slot * kSlotBytes + half * kHalf;
 #pragma unroll 4
                 for (int t = row0; t < kRows; t += 4) {
                     uint32_t w[4];
@@ -561,8 +577,8 @@ __device__ __forceinline__ void sum_dy(const KernelArgs &a, Shared &sh, uint32_t
                 }
             }
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_addr(&sh.empty[stage]));
-            if (++stage == kStages) { stage = 0; phase ^= 1; }
+            if (lane == 0) mbar_arrive(smem_addr(&sh.done[dy.slot]));
+            dy.advance();
             if (i % kRun == kRun - 1 || i == piece.count - 1) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
@@ -589,23 +605,25 @@ novak_weight_grad_kernel(const __grid_constant__ KernelArgs a, const __grid_cons
                          const __grid_constant__ CUtensorMap codes_map)
 {
     extern __shared__ uint8_t raw[];
-    const uint32_t stages = (smem_addr(raw) + 1023) & ~1023u;
-    const uint32_t raws = stages + kStages * kStageBytes;
-    Shared &sh = *reinterpret_cast<Shared *>(raw + (raws - smem_addr(raw)) + kRaws * kRawBytes);
+    const uint32_t dys = (smem_addr(raw) + 1023) & ~1023u, xs = dys + kDySlots * kSlotBytes, raws = xs + kXSlots * kSlotBytes;
+    Shared &sh = *reinterpret_cast<Shared *>(raw + (raws - smem_addr(raw)) + kRawSlots * kRawBytes);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = cluster_rank();
     const int pair = blockIdx.x / 2;
     const Cut &cut = a.cut;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) {
-            mbar_init(smem_addr(&sh.dy_full[s]), 1);
-            mbar_init(smem_addr(&sh.full[s]), 2 * kGroupWarps);
-            mbar_init(smem_addr(&sh.empty[s]), a.sums ? 1 + kSumWarps : 1);
+        for (int i = 0; i < kDySlots; ++i) {
+            mbar_init(smem_addr(&sh.dy_full[i]), 1);
+            mbar_init(smem_addr(&sh.done[i]), a.sums ? 1 + kSumWarps : 1);
         }
-        for (int r = 0; r < kRaws; ++r) {
-            mbar_init(smem_addr(&sh.raw_full[r]), 2);
-            mbar_init(smem_addr(&sh.raw_empty[r]), kGroupWarps);
+        for (int i = 0; i < kXSlots; ++i) {
+            mbar_init(smem_addr(&sh.full[i]), kGroupWarps + 1);         // the leading CTA's warps and the other CTA
+            mbar_init(smem_addr(&sh.filled[i]), kGroupWarps);
+        }
+        for (int i = 0; i < kRawSlots; ++i) {
+            mbar_init(smem_addr(&sh.raw_full[i]), 2);
+            mbar_init(smem_addr(&sh.raw_empty[i]), kGroupWarps);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(smem_addr(&sh.out_full[b]), 1);
@@ -628,18 +646,19 @@ novak_weight_grad_kernel(const __grid_constant__ KernelArgs a, const __grid_cons
     if (warp < kOutWarps) {
         take_out(a, sh, tmem, rank, pair);
     } else if (warp < kLoadWarp) {
-        fill_x(a, sh, stages, raws, rank, pair);
+        fill_x(a, sh, xs, raws, rank, pair);
     } else if (warp < kCopyWarp) {
         load_codes(a, &codes_map, sh, raws, rank, pair);
     } else if (warp >= kSumWarp) {
-        if (a.sums) sum_dy(a, sh, stages, rank, pair);
+        if (a.sums) sum_dy(a, sh, dys, rank, pair);
     } else {
         Walk walk(cut, pair);
         Piece piece;
         bool ok = true;
-        uint32_t stage = 0, phase = 0;
+        Ring<kDySlots> dy;
         if (warp == kCopyWarp && lane == 0) {
             // ---- dy: 64 rows x 128 columns per step, by tensor copies
+            Ring<kDySlots> first_open;          // the oldest step whose copy may not have been waited for by anyone
             int64_t issued = 0;
             while (ok && walk.next(piece)) {
                 int tn, tk;
@@ -647,33 +666,47 @@ novak_weight_grad_kernel(const __grid_constant__ KernelArgs a, const __grid_cons
                 const int x = tn * kTileN + static_cast<int>(rank) * 128;
                 StepPos at(cut, piece.first);
                 for (int i = 0; i < piece.count; ++i) {
-                    ok = mbar_wait(smem_addr(&sh.empty[stage]), phase ^ 1);
+                    ok = mbar_wait(smem_addr(&sh.done[dy.slot]), dy.phase ^ 1);
                     if (!ok) break;
-                    const uint32_t bar = smem_addr(&sh.dy_full[stage]), dst = stages + stage * kStageBytes;
+                    const uint32_t bar = smem_addr(&sh.dy_full[dy.slot]), dst = dys + dy.slot * kSlotBytes;
                     mbar_expect(bar, 2 * kHalf);
                     tma_load_3d(dst, &map, x, at.chunk * kRows, at.plane, bar);
                     tma_load_3d(dst + kHalf, &map, x + 64, at.chunk * kRows, at.plane, bar);
                     at.advance(cut);
-                    ++issued;
-                    if (++stage == kStages) { stage = 0; phase ^= 1; }
+                    dy.advance();
+                    if (++issued > kDySlots) first_open.advance();
                 }
             }
             // Every commit of the leading CTA has arrived here before this CTA leaves ...
-            for (int i = 0; ok && i < kStages; ++i) {
-                ok = mbar_wait(smem_addr(&sh.empty[stage]), phase ^ 1);
-                if (++stage == kStages) { stage = 0; phase ^= 1; }
+            for (int i = 0; ok && i < kDySlots; ++i) {
+                ok = mbar_wait(smem_addr(&sh.done[dy.slot]), dy.phase ^ 1);
+                dy.advance();
             }
             // ... and so has every copy, where a wait gave up and nobody took them
             if (!ok)
-                for (int64_t i = max(issued - kStages, int64_t(0)); i < issued; ++i)
-                    mbar_wait(smem_addr(&sh.dy_full[i % kStages]), (i / kStages) & 1);
-        } else if (warp == kMmaWarp && rank == 0) {
+                for (int64_t i = 0; i < min(issued, static_cast<int64_t>(kDySlots)); ++i, first_open.advance())
+                    mbar_wait(smem_addr(&sh.dy_full[first_open.slot]), first_open.phase);
+        } else if (warp == kMmaWarp && rank == 1) {
+            // ---- the leading CTA's products read this CTA's dy and x too: one arrival there
+            // tells of both (an arrival at another CTA takes long: no warp that fills makes one)
+            Ring<kXSlots> x;
+            const uint32_t lead_full = at_rank(smem_addr(&sh.full[0]), 0);
+            while (ok && walk.next(piece))
+                for (int i = 0; ok && i < piece.count; ++i) {
+                    ok = mbar_wait_warp(smem_addr(&sh.dy_full[dy.slot]), dy.phase) && mbar_wait_warp(smem_addr(&sh.filled[x.slot]), x.phase);
+                    if (ok && lane == 0) mbar_arrive_cluster(lead_full + x.slot * 8);
+                    __syncwarp();
+                    dy.advance();
+                    x.advance();
+                }
+        } else if (warp == kMmaWarp) {
             // ---- the products.  The warp stays together and one lane issues, so that the
             // descriptors are the warp's: formed by a lane on its own they cost more time
             // than the products take.
             uint32_t n = 0;
             constexpr uint32_t idesc = instr_desc(256, 256);
-            const uint64_t dy0 = operand_desc(stages, kHalf, 1024), x0 = operand_desc(stages + 2 * kHalf, kHalf, 1024);
+            const uint64_t dy0 = operand_desc(dys, kHalf, 1024), x0 = operand_desc(xs, kHalf, 1024);
+            Ring<kXSlots> x;
             while (ok && walk.next(piece)) {
                 for (int left = piece.count; ok && left > 0; ++n) {
                     const int run = min(left, kRun);
@@ -682,19 +715,20 @@ novak_weight_grad_kernel(const __grid_constant__ KernelArgs a, const __grid_cons
                     ok = mbar_wait_warp(smem_addr(&sh.out_empty[buf]), ((n >> 1) & 1) ^ 1);
                     tcgen05_after_sync();
                     for (int i = 0; ok && i < run; ++i) {
-                        ok = mbar_wait_warp(smem_addr(&sh.full[stage]), phase) && mbar_wait_warp(smem_addr(&sh.dy_full[stage]), phase);
+                        ok = mbar_wait_warp(smem_addr(&sh.dy_full[dy.slot]), dy.phase) && mbar_wait_warp(smem_addr(&sh.full[x.slot]), x.phase);
                         if (!ok) break;
                         tcgen05_after_sync();
-                        const uint64_t at = static_cast<uint64_t>(stage) * (kStageBytes >> 4);
+                        const uint64_t dy_at = dy0 + dy.slot * (kSlotBytes >> 4), x_at = x0 + x.slot * (kSlotBytes >> 4);
                         if (elect_one()) {
 #pragma unroll
                             for (int k = 0; k < kRows / 16; ++k)
-                                mma_pair_bf16(d, dy0 + at + k * (2048 >> 4), x0 + at + k * (2048 >> 4), idesc, i > 0 || k > 0);
-                            mma_commit_pair(smem_addr(&sh.empty[stage]));
+                                mma_pair_bf16(d, dy_at + k * (2048 >> 4), x_at + k * (2048 >> 4), idesc, i > 0 || k > 0);
+                            mma_commit_pair(smem_addr(&sh.done[dy.slot]));
                             if (i == run - 1) mma_commit_pair(smem_addr(&sh.out_full[buf]));
                         }
                         __syncwarp();
-                        if (++stage == kStages) { stage = 0; phase ^= 1; }
+                        dy.advance();
+                        x.advance();
                     }
                 }
             }

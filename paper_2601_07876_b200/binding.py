@@ -158,7 +158,7 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
                                      c_int64, vp]),
         "novak_activation_backward": (c_int, [vp, c_int64, vp, c_int64, c_int, c_int, vp, vp, vp,
                                               c_int64, c_int64, c_int64, vp]),
-        "novak_linear_weight_grad_bytes": (c_size_t, [vp, c_int64, c_int, c_int64, c_int64, c_int64, c_int]),
+        "novak_linear_weight_grad_bytes": (c_size_t, [vp, c_int64, c_int, c_int64, c_int64, c_int64]),
         "novak_linear_weight_grad": (c_int, [vp, c_int64, c_int, vp, vp, vp, vp, c_int, vp, vp, c_int,
                                              vp, c_size_t, c_int64, c_int64, c_int64, vp]),
         "novak_ops_gave_up": (c_int, [POINTER(c_uint32), vp]),

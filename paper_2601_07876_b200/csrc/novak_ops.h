@@ -80,7 +80,7 @@ struct WeightGradArgs {
     void *work;
     int64_t rows, n_out, n_in;     // rows may be 0
 };
-size_t weight_grad_bytes(const Mat &dy, int type, int64_t rows, int64_t n_out, int64_t n_in, bool affine);
+size_t weight_grad_bytes(const Mat &dy, int type, int64_t rows, int64_t n_out, int64_t n_in);
 cudaError_t weight_grad_gave_up(unsigned *count, cudaStream_t stream);
 cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t stream);
 

@@ -227,11 +227,11 @@ int novak_activation_backward(const void *d_da, int64_t da_stride, const void *d
 }
 
 size_t novak_linear_weight_grad_bytes(const void *d_dy, int64_t dy_stride, int type, int64_t rows,
-                                      int64_t n_out, int64_t n_in, int affine)
+                                      int64_t n_out, int64_t n_in)
 {
     if (!is_type(type) || check_shape(rows, n_out) != NOVAK_OK || check_shape(rows, n_in) != NOVAK_OK ||
         check_shape(n_out, n_in) != NOVAK_OK) return 0;
-    return weight_grad_bytes(mat(d_dy, dy_stride), type, rows, n_out, n_in, affine != 0);
+    return weight_grad_bytes(mat(d_dy, dy_stride), type, rows, n_out, n_in);
 }
 
 int novak_linear_weight_grad(const void *d_dy, int64_t dy_stride, int type, const int8_t *d_codes,
@@ -256,7 +256,7 @@ int novak_linear_weight_grad(const void *d_dy, int64_t dy_stride, int type, cons
     CHECK(check_vector("dw", d_dw, grad_type));
     if (d_db) CHECK(check_vector("db", d_db, grad_type));
     const Mat dy = mat(d_dy, dy_stride);
-    const size_t need = weight_grad_bytes(dy, type, rows, n_out, n_in, d_weight != nullptr);
+    const size_t need = weight_grad_bytes(dy, type, rows, n_out, n_in);
     if (need > 0 && (!d_work || work_bytes < need || (reinterpret_cast<uintptr_t>(d_work) & 255u)))
         return refuse("work: %zu bytes, 256-byte aligned, are needed", need);
     cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -77,13 +77,14 @@ __device__ __forceinline__ uint64_t global_ns()
 
 constexpr uint64_t kWaitNs = 2000000000ull;     // a wait gives up after two seconds
 
+// Sleeps until the phase of this parity is complete, a millisecond at most.
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
 {
     uint32_t done;
     asm volatile("{\n.reg .pred p;\n"
-                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
                  "selp.u32 %0, 1, 0, p;\n}"
-                 : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+                 : "=r"(done) : "r"(bar), "r"(parity), "r"(1000000) : "memory");
     return done != 0;
 }
 
@@ -92,7 +93,7 @@ __device__ __forceinline__ bool mbar_wait_long(uint32_t bar, uint32_t parity)
 {
     uint64_t t0 = 0;
     for (;;) {
-        for (int i = 0; i < 2048; ++i)
+        for (int i = 0; i < 64; ++i)
             if (mbar_try(bar, parity)) return true;
         const uint64_t t = global_ns();
         if (t0 == 0) t0 = t;
@@ -159,6 +160,31 @@ __device__ __forceinline__ void mma_commit_pair(uint32_t bar)
 
 __device__ __forceinline__ void tcgen05_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tcgen05_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+
+__device__ __forceinline__ void prefetch_map(const CUtensorMap *map)
+{
+    asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+
+// Programmatic dependent launch: what follows sees everything that the kernels before
+// have written; nothing before it may touch memory that they use.
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_launch_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// ---- one warp's own tensor instructions (for sums over few columns) ----------------
+// Four 8 x 8 bf16 matrices, transposed: lane i has the address of row i % 8 of matrix i / 8.
+__device__ __forceinline__ void load_transposed(uint32_t addr, uint32_t (&r)[4])
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+// d (16 x 8) += a (16 x 16) times ones: each of d's columns gets a's row sums.
+__device__ __forceinline__ void add_row_sums(float (&d)[4], const uint32_t (&a)[4])
+{
+    const uint32_t ones = 0x3f803f80u;
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %8}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(ones));
+}
 
 // 16 consecutive columns of this warp's 32 lanes: thread i gets lane i's.
 __device__ __forceinline__ void tmem_load16(uint32_t tmem, float (&v)[16])

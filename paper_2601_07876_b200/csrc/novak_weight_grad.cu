@@ -14,8 +14,7 @@
 //   warps 8-15   codes -> bf16, from and to swizzled shared memory,
 //   warps 16-19  codes by tensor copies, and exponent bytes,
 //   warp 20      dy by tensor copies,
-//   warp 21      the products (of the pair: in the leading CTA),
-//   warps 22-23  sums of dy's columns.
+//   warp 21      the products (of the pair: in the leading CTA).
 //
 // dy and x both have the summed dimension (rows) outermost, so both operands are
 // "M-major" and neither is transposed.
@@ -114,6 +113,8 @@ novak_weight_grad_planes_kernel(const typename Elem<TYPE>::T *dy, int64_t stride
                                 int64_t rows, int64_t cols)
 {
     const int64_t groups = ld / 8, n = rows * groups, plane = rows * ld;
+    grid_wait();
+    grid_launch_next();
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256) {
         const int64_t row = i / groups, col = (i - row * groups) * 8;
         float v[8];
@@ -150,24 +151,35 @@ struct Cut {
     int pairs;              // that run whole tiles
     int waves;              // whole tiles per pair
     int rest;               // tiles left over, after the first waves * pairs
-    int rest_pairs;         // pairs among which their steps are cut
-    int all_partial;        // every tile goes through the workspace
+    int rest_pairs;         // pairs among which their steps are cut:
+    int64_t share;          // so many each,
+    int extra;              // and one more for the first of them
 };
 
 struct Piece {
     int tile;
     int first, count;       // steps
-    int slot;               // of partial sums in the workspace
+    int slot;               // in the workspace, of a piece that is not the whole tile
     bool whole;
 };
 
-// Steps [i] of the tiles left over that pair p starts with.
-__host__ __device__ __forceinline__ int64_t rest_start(const Cut &c, int p)
-{
-    return static_cast<int64_t>(c.steps) * c.rest * p / c.rest_pairs;
-}
+// The step of the tiles left over that pair p starts with.
+__device__ __forceinline__ int64_t rest_start(const Cut &c, int p) { return c.share * p + min(p, c.extra); }
 
-__host__ __device__ __forceinline__ int slots(const Cut &c) { return c.rest_pairs + c.rest + c.tiles_n * c.tiles_k; }
+// The pair that has step i of them, and the tile that it is in.
+__device__ __forceinline__ int divide(int64_t a, int64_t b)
+{
+    if (a <= 0x7fffffff && b <= 0x7fffffff) return static_cast<int>(a) / static_cast<int>(b);
+    return static_cast<int>(a / b);
+}
+__device__ __forceinline__ int rest_pair(const Cut &c, int64_t i)
+{
+    const int64_t longer = (c.share + 1) * c.extra;
+    return i < longer ? divide(i, c.share + 1) : c.extra + divide(i - longer, c.share);
+}
+__device__ __forceinline__ int rest_tile(const Cut &c, int64_t i) { return divide(i, c.steps); }
+
+__host__ __device__ __forceinline__ int slots(const Cut &c) { return c.rest_pairs + c.rest; }
 
 struct Walk {
     const Cut &c;
@@ -180,6 +192,8 @@ struct Walk {
             end = rest_start(c, p + 1);
         }
     }
+    // all steps of the walk, at its start
+    __device__ int steps() const { return static_cast<int>(static_cast<int64_t>(c.waves) * c.steps + end - pos); }
     __device__ bool next(Piece &p)
     {
         if (wave < c.waves) {
@@ -188,7 +202,7 @@ struct Walk {
             p.count = c.steps;
             ++wave;
         } else if (pos < end) {
-            const int r = static_cast<int>(pos / c.steps);
+            const int r = rest_tile(c, pos);
             p.tile = c.waves * c.pairs + r;
             p.first = static_cast<int>(pos - static_cast<int64_t>(r) * c.steps);
             p.count = static_cast<int>(min(static_cast<int64_t>(c.steps - p.first), end - pos));
@@ -198,7 +212,6 @@ struct Walk {
             return false;
         }
         p.whole = p.count == c.steps;
-        if (p.whole) p.slot = c.rest_pairs + c.rest + p.tile;
         return true;
     }
 };
@@ -225,57 +238,101 @@ __device__ __forceinline__ void tile_at(const Cut &c, int tile, int &tn, int &tk
     tn = g * kGroupN + in - tk * rows;
 }
 
-__device__ __forceinline__ int tile_index(const Cut &c, int tn, int tk)
+// First slot and number of slots (consecutive) of tile r of those left over; one: the
+// tile is whole, and not in the workspace.
+__device__ __forceinline__ void tile_slots(const Cut &c, int r, int &slot, int &n)
 {
-    const int g = tn / kGroupN, rows = min(kGroupN, c.tiles_n - g * kGroupN);
-    return g * kGroupN * c.tiles_k + tk * rows + tn - g * kGroupN;
-}
-
-// First slot and number of slots of a tile's partial sums (consecutive).
-__device__ __forceinline__ void tile_slots(const Cut &c, int tile, int &slot, int &n)
-{
-    const int r = tile - c.waves * c.pairs;
-    slot = c.rest_pairs + c.rest + tile;
-    n = 1;
-    if (r < 0) return;
-    const int64_t steps = c.steps, total = steps * c.rest;
-    // the pair that has step i: the last p with total p / rest_pairs <= i
-    const int lo = static_cast<int>((static_cast<int64_t>(c.rest_pairs) * (r * steps + 1) - 1) / total);
-    const int hi = static_cast<int>((static_cast<int64_t>(c.rest_pairs) * ((r + 1) * steps) - 1) / total);
-    if (lo == hi) return;
+    const int64_t first = static_cast<int64_t>(r) * c.steps;
+    const int lo = rest_pair(c, first), hi = rest_pair(c, first + c.steps - 1);
     slot = lo + r;
     n = hi - lo + 1;
 }
 
+// ---- db, and what a layer norm's offset is multiplied with ------------------------------
+// Sums of dy's columns over a part of the rows: sums[part][ld], 256 columns per CTA, 8 per
+// lane, the warps on rows in turn.
+constexpr int kSumRows = 64;            // rows that a CTA is worth
+constexpr int kMostParts = 64;
+
+template <int TYPE, bool ALIGNED>
+__global__ void __launch_bounds__(256)
+novak_weight_grad_sums_kernel(const typename Elem<TYPE>::T *dy, int64_t stride, float *sums, int64_t ld, int64_t rows,
+                              int64_t cols, int64_t rows_per_part)
+{
+    __shared__ float part[8][256];
+    grid_wait();
+    grid_launch_next();
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int64_t col = (static_cast<int64_t>(blockIdx.x) * 32 + lane) * 8;
+    const int64_t row0 = blockIdx.y * rows_per_part, row1 = min(row0 + rows_per_part, rows);
+    const int n = static_cast<int>(max(min(cols - col, int64_t(8)), int64_t(0)));
+    const void *end = end_of(dy, stride, rows, cols);
+    F2 s[4] = {F2(0.0f), F2(0.0f), F2(0.0f), F2(0.0f)};
+    constexpr int kAhead = 4;
+    for (int64_t row = row0 + warp; row < row1; row += 8 * kAhead) {
+        Fetch<TYPE, ALIGNED> raw[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            raw[i].zero();
+            if (row + 8 * i < row1) raw[i].load(dy + (row + 8 * i) * stride + col, n, dy, end);
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            F2 v[4];
+            raw[i].eight().get(v);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s[k] = s[k] + v[k];
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        part[warp][lane * 8 + 2 * k] = s[k].lo();
+        part[warp][lane * 8 + 2 * k + 1] = s[k].hi();
+    }
+    __syncthreads();
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += part[i][threadIdx.x];
+    const int64_t out = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (out < cols) sums[blockIdx.y * ld + out] = sum;
+}
+
+// The parts added up, in order.
+__device__ __forceinline__ float column_sum(const float *sums, int parts, int64_t ld, int64_t n)
+{
+    float s = 0.0f;
+#pragma unroll 8
+    for (int i = 0; i < parts; ++i) s += sums[i * ld + n];
+    return s;
+}
+
 // ---- the kernel ----------------------------------------------------------------------
-constexpr int kDySlots = 6, kXSlots = 3, kRawSlots = 8;         // steps of dy, of x, of codes
+constexpr int kDySlots = 6, kXSlots = 4, kRawSlots = 4;         // steps of dy, of x, of codes
 constexpr int kHalf = 64 * kRows * 2;                   // 64 columns of an operand, bf16
 constexpr int kSlotBytes = 2 * kHalf;                   // 128 columns
 constexpr int kRawBytes = 128 * kRows;                  // codes of 128 columns
 constexpr int kRun = 16;        // steps that the tensor cores add up by themselves: their sums round toward
                                 // zero, so that a chain's error grows with its length
-constexpr int kOutWarps = 8, kFillWarps = 8, kFillGroups = 2, kLoadWarps = 4, kSumWarps = 2;
+constexpr int kOutWarps = 8, kFillWarps = 8, kFillGroups = 2, kLoadWarps = 4;
 constexpr int kGroupWarps = kFillWarps / kFillGroups;   // that fill a step's x; the groups take turns
-constexpr int kLoadWarp = kOutWarps + kFillWarps, kCopyWarp = kLoadWarp + kLoadWarps, kMmaWarp = kCopyWarp + 1,
-              kSumWarp = kCopyWarp + 2;
-constexpr int kThreads = 32 * (kSumWarp + kSumWarps);
+constexpr int kLoadWarp = kOutWarps + kFillWarps, kCopyWarp = kLoadWarp + kLoadWarps, kMmaWarp = kCopyWarp + 1;
+constexpr int kThreads = 32 * (kCopyWarp + 4);          // (a warpgroup has four)
 // A barrier's parity tells one phase from the next, not from the one after that: whoever
 // waits for a slot's use number k has to know that use k - 1 is over.  The two groups do
 // not finish steps in order among each other, so a slot of codes belongs to one group for
-// good; the products free the slots of dy and x in order.
+// good, and one of x too.
 static_assert(kRawSlots % kFillGroups == 0 && kRawSlots % kLoadWarps == 0, "slots of codes change hands");
-static_assert(kXSlots <= kDySlots, "a step's end is kept for as long as dy's slots last");
-constexpr int kPad = 9;
+static_assert(kXSlots % kFillGroups == 0, "slots of x change hands");
 // Registers per thread: 80 at launch, 768 x 80 = 61440 = 256 x 160 + 512 x 40.
 constexpr int kOutRegs = 160, kOtherRegs = 40;
 
 struct Shared {
-    alignas(8) uint64_t dy_full[kDySlots], full[kXSlots], filled[kXSlots], raw_full[kRawSlots], raw_empty[kRawSlots], out_full[2], out_empty[2],
+    alignas(8) uint64_t dy_full[kDySlots], full[kXSlots], filled[kXSlots], x_done[kXSlots], raw_full[kRawSlots], raw_empty[kRawSlots], out_full[2], out_empty[2],
         drained;
-    uint64_t done[kDySlots];            // a step's products are over: step i's is done[i % kDySlots]
+    uint64_t done[kDySlots];
     uint32_t tmem;
     uint32_t exps[kRawSlots][kRows];    // of four blocks
-    float turn[kOutWarps][32 * kPad];
+    alignas(16) float4 turn[kOutWarps][32 * 8];     // 32 rows x 32 columns
 };
 constexpr int kSmemBytes = (kDySlots + kXSlots) * kSlotBytes + kRawSlots * kRawBytes + 1024 + static_cast<int>(sizeof(Shared));
 static_assert(kSmemBytes <= 227 * 1024, "shared memory");
@@ -302,7 +359,11 @@ struct KernelArgs {
     int grad_type, vector;
     int64_t rows, n_out, n_in;
     float *partial;                 // [slot][64][256 rows][4 columns] per tile
-    float *sums;                    // [slot][256]; NULL: not asked for
+    const float *sums;              // [parts][sums_ld], where a layer norm's weight and bias are given
+    int parts;
+    int64_t sums_ld;
+    const void *weight, *bias;
+    int param_type;
 };
 
 __device__ unsigned g_gave_up;       // warps whose wait for a tile ran out, since the library was loaded
@@ -389,17 +450,10 @@ __device__ __forceinline__ void fill_x(const KernelArgs &a, Shared &sh, uint32_t
     const uint32_t dst0 = xs + half * kHalf + r * 128 + ((4 * b ^ (r & 7)) << 4);
     const uint32_t src0 = raws + r * 128 + (((half * 4 + b * 2) ^ (r & 7)) << 4);
     const uint32_t exp0 = smem_addr(&sh.exps[0][0]) + r * 4 + half * 2 + b;
-    int steps = 0;
-    {
-        Walk count(a.cut, pair);
-        Piece piece;
-        while (count.next(piece)) steps += piece.count;
-    }
+    const int steps = Walk(a.cut, pair).steps();
     Ring<kXSlots> x(group);
     Ring<kRawSlots> raw(group);
-    Ring<kDySlots> before(kDySlots + group - kXSlots);      // the step that had x's slot before
-    before.phase = 1;
-    const uint32_t done = smem_addr(&sh.done[0]), filled = smem_addr(rank == 0 ? &sh.full[0] : &sh.filled[0]);
+    const uint32_t done = smem_addr(&sh.x_done[0]), filled = smem_addr(rank == 0 ? &sh.full[0] : &sh.filled[0]);
     const uint32_t raw_full = smem_addr(&sh.raw_full[0]), raw_empty = smem_addr(&sh.raw_empty[0]);
     for (int step = group; step < steps; step += kFillGroups) {
         if (!mbar_wait_warp(raw_full + raw.slot * 8, raw.phase)) return;
@@ -413,7 +467,7 @@ __device__ __forceinline__ void fill_x(const KernelArgs &a, Shared &sh, uint32_t
                 asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q[2 * k + h][0]), "=r"(q[2 * k + h][1]),
                              "=r"(q[2 * k + h][2]), "=r"(q[2 * k + h][3]) : "r"((src ^ h << 4) + k * 2048));
         }
-        if (!mbar_wait_warp(done + before.slot * 8, before.phase)) return;
+        if (!mbar_wait_warp(done + x.slot * 8, x.phase ^ 1)) return;
         const uint32_t dst = dst0 + x.slot * kSlotBytes;
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
@@ -436,8 +490,10 @@ __device__ __forceinline__ void fill_x(const KernelArgs &a, Shared &sh, uint32_t
         }
         x.advance(kFillGroups);
         raw.advance(kFillGroups);
-        before.advance(kFillGroups);
     }
+    // every commit of the leading CTA has arrived here before this CTA leaves
+    for (int i = 0; i < kXSlots; i += kFillGroups, x.advance(kFillGroups))
+        if (!mbar_wait_warp(done + x.slot * 8, x.phase ^ 1)) return;
 }
 
 // Four neighbouring elements of dW's row, column k on.
@@ -454,6 +510,17 @@ __device__ __forceinline__ void store_four(const Args &a, int64_t at, int64_t k,
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (k + i < a.n_in) store_param(a.dw, a.grad_type, at + i, x[i]);
+    }
+}
+
+// A layer norm's weight and bias for four columns, k on.
+template <typename Args>
+__device__ __forceinline__ void load_affine(const Args &a, int64_t k, float (&w)[4], float (&b)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        w[i] = k + i < a.n_in ? param_at(a.weight, a.param_type, k + i) : 0.0f;
+        b[i] = k + i < a.n_in ? param_at(a.bias, a.param_type, k + i) : 0.0f;
     }
 }
 
@@ -503,38 +570,50 @@ __device__ __forceinline__ void take_out(const KernelArgs &a, Shared &sh, uint32
 #pragma unroll
         for (int c = 0; c < 128; c += 16) tmem_store16(at + c, total + c);
         tmem_store_wait();
-        const bool partial = !piece.whole || cut.all_partial;
+        const bool partial = !piece.whole;
         float4 *dst = reinterpret_cast<float4 *>(a.partial) + (static_cast<int64_t>(piece.slot) * 64 + side * 32) * 256 +
                       rank * 128 + quarter * 32 + lane;
-        float *turn = sh.turn[warp];
-        const int row = lane / 2, col = lane % 2 * 4;
-        const int64_t row0 = n0 + quarter * 32 + row, k0 = static_cast<int64_t>(tk) * kTileK + side * 128 + col;
+        const uint32_t turn = smem_addr(sh.turn[warp]);
+        const int row = lane / 8, col = lane % 8;               // four rows, eight groups of four columns
+        const int64_t row0 = n0 + quarter * 32 + row, k0 = static_cast<int64_t>(tk) * kTileK + side * 128 + 4 * col;
+        float mine = 0.0f;              // lane i: the column sum of dy for row i
+        if (a.weight && !partial && n0 + quarter * 32 + lane < a.n_out)
+            mine = column_sum(a.sums, a.parts, a.sums_ld, n0 + quarter * 32 + lane);
 #pragma unroll 1
-        for (int c = 0; c < 128; c += 16) {
-            float v[16];
-            tmem_load16(at + c, v);
+        for (int c = 0; c < 128; c += 32) {
+            float v[32];
+            tmem_load16(at + c, reinterpret_cast<float (&)[16]>(v[0]));
+            tmem_load16(at + c + 16, reinterpret_cast<float (&)[16]>(v[16]));
             if (!ok)        // nobody takes this for a result
 #pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(0x7fffffffu);
+                for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(0x7fffffffu);
             if (partial) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < 8; ++i)
                     dst[(c / 4 + i) * 256] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
             } else {
-                // through shared memory: four neighbouring columns of sixteen rows per store
+                // through shared memory, so that a store has whole lines of 32 columns; a row's
+                // groups of four change places by the row's number, which spreads them over all banks
 #pragma unroll
-                for (int h = 0; h < 16; h += 8) {
+                for (int i = 0; i < 8; ++i)
+                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(turn + (lane * 8 + (i ^ (lane & 7))) * 16),
+                                 "f"(v[4 * i]), "f"(v[4 * i + 1]), "f"(v[4 * i + 2]), "f"(v[4 * i + 3]) : "memory");
+                __syncwarp();
+                float w[4], b[4];
+                if (a.weight) load_affine(a, k0 + c, w, b);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) turn[lane * kPad + i] = v[h + i];
-                    __syncwarp();
+                for (int i = 0; i < 32; i += 4) {
+                    float x[4];
+                    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3])
+                                 : "r"(turn + ((row + i) * 8 + (col ^ ((row + i) & 7))) * 16) : "memory");
+                    if (a.weight) {
+                        const float s = __shfl_sync(0xffffffffu, mine, row + i);
 #pragma unroll
-                    for (int i = 0; i < 32; i += 16) {
-                        const float *src = turn + (row + i) * kPad + col;
-                        const int64_t k = k0 + c + h;
-                        if (row0 + i < a.n_out) store_four(a, (row0 + i) * a.n_in + k, k, src[0], src[1], src[2], src[3]);
+                        for (int j = 0; j < 4; ++j) x[j] = fmaf(x[j], w[j], b[j] * s);
                     }
-                    __syncwarp();
+                    if (row0 + i < a.n_out) store_four(a, (row0 + i) * a.n_in + k0 + c, k0 + c, x[0], x[1], x[2], x[3]);
                 }
+                __syncwarp();
             }
         }
         if (!ok) break;
@@ -542,61 +621,6 @@ __device__ __forceinline__ void take_out(const KernelArgs &a, Shared &sh, uint32
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(at_rank(smem_addr(&sh.out_empty[n & 1]), 0));
         ++n;
-    }
-}
-
-// Warps kSumWarp, + 1: sums over dy's columns, 64 columns of a warp, from shared
-// memory.  The tiles of a tile row share the chunks of rows among them.
-__device__ __forceinline__ void sum_dy(const KernelArgs &a, Shared &sh, uint32_t dys, uint32_t rank, int pair)
-{
-    const Cut &cut = a.cut;
-    const int half = threadIdx.x / 32 - kSumWarp, lane = threadIdx.x % 32;
-    const int chunk = lane % 8, row0 = lane / 8;        // 8 columns of every fourth row
-    Walk walk(cut, pair);
-    Piece piece;
-    Ring<kDySlots> dy;
-    while (walk.next(piece)) {
-        int tn, tk;
-        tile_at(cut, piece.tile, tn, tk);
-        StepPos at(cut, piece.first);
-        float s[8] = {}, total[8] = {};
-        for (int i = 0; i < piece.count; ++i, at.advance(cut)) {
-            if (!mbar_wait_warp(smem_addr(&sh.dy_full[dy.slot]), dy.phase)) return;
-            if (at.chunk % cut.tiles_k == tk) {
-                const uint32_t src = dys + dy.slot * kSlotBytes + half * kHalf;
-#pragma unroll 4
-                for (int t = row0; t < kRows; t += 4) {
-                    uint32_t w[4];
-                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-                                 : "r"(src + t * 128 + ((chunk ^ (t & 7)) << 4)));
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        s[2 * k] += __uint_as_float(w[k] << 16);
-                        s[2 * k + 1] += __uint_as_float(w[k] & 0xffff0000u);
-                    }
-                }
-            }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_addr(&sh.done[dy.slot]));
-            dy.advance();
-            if (i % kRun == kRun - 1 || i == piece.count - 1) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    total[k] += s[k];
-                    s[k] = 0.0f;
-                }
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            total[k] += __shfl_xor_sync(0xffffffffu, total[k], 8);
-            total[k] += __shfl_xor_sync(0xffffffffu, total[k], 16);
-        }
-        if (lane < 8) {
-            float4 *dst = reinterpret_cast<float4 *>(a.sums + static_cast<int64_t>(piece.slot) * 256 + rank * 128 + half * 64 + chunk * 8);
-            dst[0] = make_float4(total[0], total[1], total[2], total[3]);
-            dst[1] = make_float4(total[4], total[5], total[6], total[7]);
-        }
     }
 }
 
@@ -615,11 +639,12 @@ novak_weight_grad_kernel(const __grid_constant__ KernelArgs a, const __grid_cons
     if (threadIdx.x == 0) {
         for (int i = 0; i < kDySlots; ++i) {
             mbar_init(smem_addr(&sh.dy_full[i]), 1);
-            mbar_init(smem_addr(&sh.done[i]), a.sums ? 1 + kSumWarps : 1);
+            mbar_init(smem_addr(&sh.done[i]), 1);
         }
         for (int i = 0; i < kXSlots; ++i) {
             mbar_init(smem_addr(&sh.full[i]), kGroupWarps + 1);         // the leading CTA's warps and the other CTA
             mbar_init(smem_addr(&sh.filled[i]), kGroupWarps);
+            mbar_init(smem_addr(&sh.x_done[i]), 1);
         }
         for (int i = 0; i < kRawSlots; ++i) {
             mbar_init(smem_addr(&sh.raw_full[i]), 2);
@@ -633,11 +658,17 @@ novak_weight_grad_kernel(const __grid_constant__ KernelArgs a, const __grid_cons
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0) tmem_alloc_pair(smem_addr(&sh.tmem), 512);
+    if (threadIdx.x == 32 * kCopyWarp) {
+        prefetch_map(&map);
+        prefetch_map(&codes_map);
+    }
     tcgen05_before_sync();
     __syncthreads();
     cluster_sync();
     tcgen05_after_sync();
     const uint32_t tmem = sh.tmem;
+    grid_launch_next();
+    grid_wait();
 
     // (every warp of a warpgroup executes the same one of the two)
     if (warp < kOutWarps) registers_up<kOutRegs>();
@@ -649,8 +680,6 @@ novak_weight_grad_kernel(const __grid_constant__ KernelArgs a, const __grid_cons
         fill_x(a, sh, xs, raws, rank, pair);
     } else if (warp < kCopyWarp) {
         load_codes(a, &codes_map, sh, raws, rank, pair);
-    } else if (warp >= kSumWarp) {
-        if (a.sums) sum_dy(a, sh, dys, rank, pair);
     } else {
         Walk walk(cut, pair);
         Piece piece;
@@ -723,6 +752,7 @@ novak_weight_grad_kernel(const __grid_constant__ KernelArgs a, const __grid_cons
 #pragma unroll
                             for (int k = 0; k < kRows / 16; ++k)
                                 mma_pair_bf16(d, dy_at + k * (2048 >> 4), x_at + k * (2048 >> 4), idesc, i > 0 || k > 0);
+                            mma_commit_pair(smem_addr(&sh.x_done[x.slot]));
                             mma_commit_pair(smem_addr(&sh.done[dy.slot]));
                             if (i == run - 1) mma_commit_pair(smem_addr(&sh.out_full[buf]));
                         }
@@ -747,51 +777,45 @@ novak_weight_grad_kernel(const __grid_constant__ KernelArgs a, const __grid_cons
     if (warp == 0) tmem_free_pair(tmem, 512);
 }
 
-// ---- partial tiles and column sums --------------------------------------------------
+// ---- partial tiles, db -------------------------------------------------------------------
 struct FinishArgs {
     Cut cut;
     const float *partial, *sums;
+    int parts;
+    int64_t sums_ld;
     const void *weight, *bias;
     int param_type;
     void *dw, *db;
     int grad_type, vector;
     int64_t n_out, n_in;
-    int first_tile, n_tiles;        // to be added up; then tiles_n for db
 };
 
-// kFinishRows rows of a tile per CTA, two groups of four columns of one per thread.
+// kFinishRows rows of a tile left over per CTA, two groups of four columns of one per
+// thread; then a CTA for each 256 elements of db.
 constexpr int kFinishRows = 8, kFinishCtas = kTileN / kFinishRows;
 __global__ void __launch_bounds__(256) novak_weight_grad_finish_kernel(const __grid_constant__ FinishArgs a)
 {
-    __shared__ float part[32][kFinishRows + 1], total[kFinishRows];
+    __shared__ float total[kFinishRows], part[32][kFinishRows + 1];
     __shared__ float turn[kFinishRows][kTileK + 4];
     const Cut &cut = a.cut;
+    grid_wait();
     const int group = blockIdx.x % kFinishCtas, item = blockIdx.x / kFinishCtas;
-    const bool for_db = item >= a.n_tiles;
-    int tn, tk = 0, slot, n;
-    if (for_db) tn = item - a.n_tiles;
-    else tile_at(cut, a.first_tile + item, tn, tk);
-    const int row = threadIdx.x % kFinishRows, lane = threadIdx.x / kFinishRows;
-    const int64_t n0 = static_cast<int64_t>(tn) * kTileN + group * kFinishRows;
-    if (n0 >= a.n_out) return;
-    if (for_db || a.weight) {
-        float s = 0.0f;
-        for (int k = lane; k < cut.tiles_k; k += 32) {
-            tile_slots(cut, tile_index(cut, tn, k), slot, n);
-            for (int i = 0; i < n; ++i) s += a.sums[static_cast<int64_t>(slot + i) * 256 + group * kFinishRows + row];
-        }
-        part[lane][row] = s;
-        __syncthreads();
-        if (threadIdx.x < kFinishRows) {
-            s = 0.0f;
-            for (int i = 0; i < 32; ++i) s += part[i][row];
-            total[row] = s;
-            if (for_db && n0 + row < a.n_out) store_param(a.db, a.grad_type, n0 + row, s);
-        }
-        if (for_db) return;
+    if (item >= cut.rest) {
+        const int64_t n = static_cast<int64_t>(blockIdx.x - cut.rest * kFinishCtas) * 256 + threadIdx.x;
+        if (n < a.n_out) store_param(a.db, a.grad_type, n, column_sum(a.sums, a.parts, a.sums_ld, n));
+        return;
     }
-    tile_slots(cut, a.first_tile + item, slot, n);
-    if (n == 1 && !cut.all_partial) return;         // stored as it was
+    int tn, tk, slot, n;
+    tile_at(cut, cut.waves * cut.pairs + item, tn, tk);
+    tile_slots(cut, item, slot, n);
+    const int64_t n0 = static_cast<int64_t>(tn) * kTileN + group * kFinishRows;
+    if (n == 1 || n0 >= a.n_out) return;
+    const int row = threadIdx.x % kFinishRows, lane = threadIdx.x / kFinishRows;
+    if (a.weight) {
+        float s = 0.0f;
+        for (int i = lane; i < a.parts; i += 32) s += a.sums[i * a.sums_ld + n0 + row];        // (padded to whole tiles)
+        part[lane][row] = s;
+    }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const int c = lane + 32 * j;
@@ -806,18 +830,28 @@ __global__ void __launch_bounds__(256) novak_weight_grad_finish_kernel(const __g
         *reinterpret_cast<float4 *>(&turn[row][4 * c]) = v;
     }
     __syncthreads();
-    const int64_t k0 = static_cast<int64_t>(tk) * kTileK;
+    if (a.weight) {
+        if (threadIdx.x < kFinishRows) {
+            float s = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) s += part[i][threadIdx.x];
+            total[threadIdx.x] = s;
+        }
+        __syncthreads();
+    }
+    const int c = threadIdx.x % 64 * 4;
+    const int64_t k = static_cast<int64_t>(tk) * kTileK + c;
+    float w[4], b[4];
+    if (a.weight) load_affine(a, k, w, b);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const int r = threadIdx.x / 64 + 4 * j, c = threadIdx.x % 64 * 4;
-        const int64_t k = k0 + c;
+        const int r = threadIdx.x / 64 + 4 * j;
         if (n0 + r >= a.n_out || k >= a.n_in) continue;
         float x[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             x[i] = turn[r][c + i];
-            if (a.weight && k + i < a.n_in)
-                x[i] = fmaf(x[i], param_at(a.weight, a.param_type, k + i), param_at(a.bias, a.param_type, k + i) * total[r]);
+            if (a.weight) x[i] = fmaf(x[i], w[i], b[i] * total[r]);
         }
         store_four(a, (n0 + r) * a.n_in + k, k, x[0], x[1], x[2], x[3]);
     }
@@ -829,13 +863,15 @@ struct Layout {
     bool copied;            // dy goes through the workspace
     int64_t ld;             // elements between rows as the tensor copies see them
     Cut cut;
+    int parts;              // of the rows, in sums of dy's columns
+    int64_t rows_per_part, sums_ld;
     size_t planes_bytes, partial_bytes, sums_bytes;
 };
 
 constexpr size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
 
-// The workspace holds for a call with or without sums and a layer norm's scale.
-Layout layout_for(const Mat &dy, int type, int64_t rows, int64_t n_out, int64_t n_in, bool affine)
+// (The workspace is the same with and without db and a layer norm's weight and bias.)
+Layout layout_for(const Mat &dy, int type, int64_t rows, int64_t n_out, int64_t n_in)
 {
     Layout l{};
     l.planes = type == NOVAK_TYPE_F32 ? 3 : 1;
@@ -853,11 +889,17 @@ Layout layout_for(const Mat &dy, int type, int64_t rows, int64_t n_out, int64_t 
     c.waves = tiles / kPairs;
     c.rest = tiles % kPairs;
     c.rest_pairs = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kPairs, static_cast<int64_t>(c.rest) * c.steps / kMinSteps)));
-    c.all_partial = affine;
-    // (whole tiles take slots behind the pieces' only where they go through the workspace)
-    const size_t n_slots = static_cast<size_t>(c.rest_pairs) + c.rest + (affine ? tiles : 0);
-    l.partial_bytes = n_slots * kTileN * kTileK * sizeof(float);
-    l.sums_bytes = round_up(static_cast<size_t>(slots(c)) * 256 * sizeof(float));
+    const int64_t left = static_cast<int64_t>(c.rest) * c.steps;
+    c.share = left / c.rest_pairs;
+    c.extra = static_cast<int>(left % c.rest_pairs);
+    l.partial_bytes = static_cast<size_t>(slots(c)) * kTileN * kTileK * sizeof(float);
+    // sums of columns: about four CTAs per SM
+    const int64_t column_ctas = (n_out + 255) / 256;
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(kMostParts, 148 * 4 / column_ctas), rows / kSumRows));
+    l.rows_per_part = (rows + want - 1) / want;
+    l.parts = static_cast<int>((rows + l.rows_per_part - 1) / l.rows_per_part);
+    l.sums_ld = column_ctas * 256;
+    l.sums_bytes = round_up(static_cast<size_t>(l.parts) * l.sums_ld * sizeof(float));
     return l;
 }
 
@@ -877,12 +919,39 @@ EncodeTiled encoder()
     return fn;
 }
 
+// Launches with programmatic stream serialization: the kernel's CTAs may come to be, and
+// set up what is theirs alone, while the one before still runs.
+template <typename... Params, typename... Args>
+cudaError_t launch(void (*kernel)(Params...), dim3 grid, int threads, int smem, cudaStream_t stream, Args... args)
+{
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = grid;
+    lc.blockDim = dim3(static_cast<unsigned>(threads));
+    lc.dynamicSmemBytes = static_cast<size_t>(smem);
+    lc.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = attr;
+    lc.numAttrs = 1;
+    return cudaLaunchKernelEx(&lc, kernel, static_cast<Params>(args)...);
+}
+
+template <int TYPE> cudaError_t launch_sums(const WeightGradArgs &a, const Layout &l, float *sums, cudaStream_t stream)
+{
+    using T = typename Elem<TYPE>::T;
+    auto kernel = wide(a.dy, TYPE, a.rows) && a.n_out % 8 == 0 ? novak_weight_grad_sums_kernel<TYPE, true>
+                                                               : novak_weight_grad_sums_kernel<TYPE, false>;
+    return launch(kernel, dim3(static_cast<unsigned>(l.sums_ld / 256), static_cast<unsigned>(l.parts)), 256, 0, stream,
+                  static_cast<const T *>(a.dy.ptr), a.dy.stride, sums, l.sums_ld, a.rows, a.n_out, l.rows_per_part);
+}
+
 }  // namespace
 
-size_t weight_grad_bytes(const Mat &dy, int type, int64_t rows, int64_t n_out, int64_t n_in, bool affine)
+size_t weight_grad_bytes(const Mat &dy, int type, int64_t rows, int64_t n_out, int64_t n_in)
 {
     if (rows <= kFewRows) return 0;
-    const Layout l = layout_for(dy, type, rows, n_out, n_in, affine);
+    const Layout l = layout_for(dy, type, rows, n_out, n_in);
     return l.planes_bytes + l.partial_bytes + l.sums_bytes;
 }
 
@@ -901,17 +970,22 @@ cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t stream)
         else novak_weight_grad_few_kernel<1><<<grid, kPlainThreads, 0, stream>>>(a);
         return cudaGetLastError();
     }
-    const Layout l = layout_for(a.dy, a.type, a.rows, a.n_out, a.n_in, a.weight != nullptr);
+    const Layout l = layout_for(a.dy, a.type, a.rows, a.n_out, a.n_in);
     uint8_t *work = static_cast<uint8_t *>(a.work);
+    float *sums = reinterpret_cast<float *>(work + l.planes_bytes + l.partial_bytes);
+    if (a.db || a.weight) {
+        const cudaError_t e = a.type == NOVAK_TYPE_F32 ? launch_sums<0>(a, l, sums, stream) : launch_sums<1>(a, l, sums, stream);
+        if (e != cudaSuccess) return e;
+    }
     const __nv_bfloat16 *dy = static_cast<const __nv_bfloat16 *>(a.dy.ptr);
     if (l.copied) {
         __nv_bfloat16 *out = reinterpret_cast<__nv_bfloat16 *>(work);
         const int grid = static_cast<int>(std::min<int64_t>((a.rows * (l.ld / 8) + 255) / 256, 148 * 32));
-        if (a.type == NOVAK_TYPE_F32)
-            novak_weight_grad_planes_kernel<0><<<grid, 256, 0, stream>>>(static_cast<const float *>(a.dy.ptr), a.dy.stride,
-                                                                         out, l.ld, a.rows, a.n_out);
-        else
-            novak_weight_grad_planes_kernel<1><<<grid, 256, 0, stream>>>(dy, a.dy.stride, out, l.ld, a.rows, a.n_out);
+        const cudaError_t e = a.type == NOVAK_TYPE_F32
+                                  ? launch(novak_weight_grad_planes_kernel<0>, grid, 256, 0, stream, static_cast<const float *>(a.dy.ptr),
+                                           a.dy.stride, out, l.ld, a.rows, a.n_out)
+                                  : launch(novak_weight_grad_planes_kernel<1>, grid, 256, 0, stream, dy, a.dy.stride, out, l.ld, a.rows, a.n_out);
+        if (e != cudaSuccess) return e;
         dy = out;
     }
     const EncodeTiled encode = encoder();
@@ -945,23 +1019,18 @@ cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t stream)
     }
     if (e != cudaSuccess) return e;
 
-    const bool sums = a.db || a.weight;
     const int vector = a.n_in % 4 == 0 && reinterpret_cast<uintptr_t>(a.dw) % (a.grad_type == NOVAK_TYPE_F32 ? 16 : 8) == 0;
-    KernelArgs k{l.cut, a.codes, act_pitch(a.n_in), a.dw, a.grad_type, vector, a.rows, a.n_out, a.n_in,
-                 reinterpret_cast<float *>(work + l.planes_bytes), nullptr};
-    float *sums_at = reinterpret_cast<float *>(work + l.planes_bytes + l.partial_bytes);
-    if (sums) k.sums = sums_at;
+    float *partial = reinterpret_cast<float *>(work + l.planes_bytes);
+    const KernelArgs k{l.cut, a.codes, act_pitch(a.n_in), a.dw, a.grad_type, vector, a.rows, a.n_out, a.n_in, partial,
+                       sums, l.parts, l.sums_ld, a.weight, a.bias, a.param_type};
     const int pairs = l.cut.waves > 0 ? l.cut.pairs : l.cut.rest_pairs;
-    novak_weight_grad_kernel<<<2 * pairs, kThreads, kSmemBytes, stream>>>(k, map, codes_map);
+    e = launch(novak_weight_grad_kernel, 2 * pairs, kThreads, kSmemBytes, stream, k, map, codes_map);
+    if (e != cudaSuccess) return e;
 
-    FinishArgs f{l.cut, k.partial, sums_at, a.weight, a.bias, a.param_type, a.dw, a.db, a.grad_type, vector,
-                 a.n_out, a.n_in, 0, 0};
-    const int tiles = l.cut.tiles_n * l.cut.tiles_k, whole = l.cut.waves * l.cut.pairs;
-    f.first_tile = l.cut.all_partial ? 0 : whole;
-    f.n_tiles = tiles - f.first_tile;
-    const int64_t blocks = static_cast<int64_t>(kFinishCtas) * (f.n_tiles + (a.db ? l.cut.tiles_n : 0));
-    if (blocks > 0) novak_weight_grad_finish_kernel<<<static_cast<unsigned>(blocks), 256, 0, stream>>>(f);
-    return cudaGetLastError();
+    const FinishArgs f{l.cut, partial, sums, l.parts, l.sums_ld, a.weight, a.bias, a.param_type, a.dw, a.db, a.grad_type,
+                       vector, a.n_out, a.n_in};
+    const int64_t blocks = static_cast<int64_t>(kFinishCtas) * l.cut.rest + (a.db ? (a.n_out + 255) / 256 : 0);
+    return blocks > 0 ? launch(novak_weight_grad_finish_kernel, dim3(static_cast<unsigned>(blocks)), 256, 0, stream, f) : cudaSuccess;
 }
 
 }  // namespace novak

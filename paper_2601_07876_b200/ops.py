@@ -19,6 +19,7 @@ BLOCK = 32          # elements that share an exponent byte
 _TYPE = {torch.float32: B.NOVAK_TYPE_F32, torch.bfloat16: B.NOVAK_TYPE_BF16}
 _KIND = {"gelu": B.NOVAK_ACT_GELU, "gelu_tanh": B.NOVAK_ACT_GELU_TANH, "silu": B.NOVAK_ACT_SILU}
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _lib = None
 
 
@@ -30,13 +31,12 @@ def _library():
     return _lib
 
 
-def _enqueue(name: str, device, *args):
-    """Calls the C entry point on torch's current stream of `device`, with that device current
-    (the raw stream lookup where torch has it: the Stream object costs 2 us per call)."""
+def _enqueue(name: str, index: int, *args):
+    """Calls the C entry point on torch's current stream of device `index`, with that device
+    current (the raw lookups where torch has them: the objects cost 2 us per call)."""
     lib = _lib or _library()
-    index = device.index
-    stream = _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
-    if torch.cuda.current_device() == index:
+    stream = _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(index).cuda_stream
+    if _current_device() == index:
         status = getattr(lib, name)(*args, stream)
     else:
         with torch.cuda.device(index):
@@ -58,12 +58,11 @@ def _rows(t, name: str):
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
     shape = t.shape
-    n = len(shape)
-    if n == 0 or shape[-1] == 0:
+    if not shape or shape[-1] == 0:
         raise ValueError(f"{name} needs a last dimension of at least one element")
     cols = shape[-1]
     if t.is_contiguous():
-        return t.numel() // cols, cols, cols
+        return (shape[0] if len(shape) == 2 else t.numel() // cols), cols, cols
     st = t.stride()
     if st[-1] != 1 and cols > 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
@@ -81,17 +80,17 @@ def _rows(t, name: str):
     return rows, cols, stride
 
 
-def _same(t, name: str, like, shape, dtype=None):
-    if t.device != like.device:
-        raise ValueError(f"{name} is on {t.device}, not on {like.device}")
-    if tuple(t.shape) != tuple(shape):
+def _same(t, name: str, index: int, shape, dtype=None):
+    if t.get_device() != index:
+        raise ValueError(f"{name} is on {t.device}, not on cuda:{index}")
+    if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
 
 
-def _vector(t, name: str, like, n: int):
-    _same(t, name, like, (n,))
+def _vector(t, name: str, index: int, n: int):
+    _same(t, name, index, (n,))
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return _type(t, name)
@@ -102,60 +101,86 @@ class Act8:
     (uint8, rows x padded columns / 32), see include/novak.h.  ``shape`` is that of the
     tensor it was made from."""
 
-    __slots__ = ("codes", "exps", "rows", "cols", "shape")
+    __slots__ = ("_codes", "_exps", "_both", "rows", "cols", "shape", "codes_ptr", "exps_ptr", "index")
 
     def __init__(self, codes, exps, cols: int, shape=None):
         rows, pitch = codes.shape
         if codes.dtype != torch.int8 or exps.dtype != torch.uint8:
             raise TypeError("codes must be int8 and exps uint8")
-        if cols < 1 or pitch != (cols + BLOCK - 1) // BLOCK * BLOCK or tuple(exps.shape) != (rows, pitch // BLOCK):
+        if cols < 1 or pitch != (cols + BLOCK - 1) // BLOCK * BLOCK or exps.shape != (rows, pitch // BLOCK):
             raise ValueError(f"no 8-bit form of rows of {cols} elements: codes {tuple(codes.shape)}, "
                              f"exps {tuple(exps.shape)}")
-        if not codes.is_contiguous() or not exps.is_contiguous() or not codes.is_cuda or codes.device != exps.device:
+        index = codes.get_device()
+        if not codes.is_contiguous() or not exps.is_contiguous() or index < 0 or exps.get_device() != index:
             raise ValueError("codes and exps must be contiguous CUDA tensors of one device")
-        if codes.data_ptr() % 32 and rows:
+        self.codes_ptr, self.exps_ptr = codes.data_ptr(), exps.data_ptr()
+        if self.codes_ptr % 32 and rows:
             raise ValueError("codes must be 32-byte aligned")
-        self.codes, self.exps, self.rows, self.cols = codes, exps, rows, cols
+        self._codes, self._exps, self._both, self.rows, self.cols, self.index = codes, exps, None, rows, cols, index
         self.shape = (rows, cols) if shape is None else tuple(shape)
 
     @classmethod
     def empty(cls, rows: int, cols: int, device, shape=None):
-        """Uninitialised codes and exponents for rows x cols elements."""
+        """Uninitialised codes and exponents for rows x cols elements, in one buffer."""
         self = object.__new__(cls)
         blocks = (cols + BLOCK - 1) // BLOCK
-        self.codes = torch.empty((rows, blocks * BLOCK), dtype=torch.int8, device=device)
-        self.exps = torch.empty((rows, blocks), dtype=torch.uint8, device=device)
-        self.rows, self.cols = rows, cols
-        self.shape = (rows, cols) if shape is None else tuple(shape)
+        both = torch.empty(rows * blocks * (BLOCK + 1), dtype=torch.uint8, device=device)
+        self._codes = self._exps = None
+        self._both, self.rows, self.cols, self.index = both, rows, cols, both.get_device()
+        self.codes_ptr = both.data_ptr()
+        self.exps_ptr = self.codes_ptr + rows * blocks * BLOCK
+        self.shape = (rows, cols) if shape is None else shape
         return self
+
+    def _split(self):
+        blocks = (self.cols + BLOCK - 1) // BLOCK
+        n = self.rows * blocks * BLOCK
+        self._codes = self._both[:n].view(torch.int8).view(self.rows, blocks * BLOCK)
+        self._exps = self._both[n:].view(self.rows, blocks)
+
+    @property
+    def codes(self):
+        if self._codes is None:
+            self._split()
+        return self._codes
+
+    @property
+    def exps(self):
+        if self._exps is None:
+            self._split()
+        return self._exps
 
     @property
     def device(self):
-        return self.codes.device
+        return (self._codes if self._both is None else self._both).device
 
     @property
     def nbytes(self) -> int:
-        return self.codes.numel() + self.exps.numel()
+        return self.rows * ((self.cols + BLOCK - 1) // BLOCK) * (BLOCK + 1)
 
     def __repr__(self):
-        return f"Act8(shape={self.shape}, {self.nbytes} bytes on {self.device})"
+        return f"Act8(shape={tuple(self.shape)}, {self.nbytes} bytes on {self.device})"
+
+
+def _belongs(kept: Act8, rows: int, cols: int, index: int, name: str):
+    if kept.rows != rows or kept.cols != cols or kept.index != index:
+        raise ValueError(f"the 8-bit form of {kept.rows} x {kept.cols} elements on cuda:{kept.index} does not belong "
+                         f"to {name} of {rows} x {cols} on cuda:{index}")
 
 
 def act8_pack(x) -> Act8:
     """The 8-bit form of x (float32 or bfloat16)."""
     rows, cols, stride = _rows(x, "x")
-    dev = x.device
-    kept = Act8.empty(rows, cols, dev, x.shape)
-    _enqueue("novak_act8_pack", dev, x.data_ptr(), stride, _type(x, "x"), kept.codes.data_ptr(), kept.exps.data_ptr(),
+    kept = Act8.empty(rows, cols, x.device, x.shape)
+    _enqueue("novak_act8_pack", kept.index, x.data_ptr(), stride, _type(x, "x"), kept.codes_ptr, kept.exps_ptr,
              rows, cols)
     return kept
 
 
 def act8_unpack(kept: Act8, dtype=torch.bfloat16):
     """A tensor of what an 8-bit form stands for (bfloat16 holds it exactly)."""
-    dev = kept.codes.device
-    out = torch.empty(kept.shape, dtype=dtype, device=dev)
-    _enqueue("novak_act8_unpack", dev, kept.codes.data_ptr(), kept.exps.data_ptr(), out.data_ptr(), kept.cols,
+    out = torch.empty(kept.shape, dtype=dtype, device=kept.device)
+    _enqueue("novak_act8_unpack", kept.index, kept.codes_ptr, kept.exps_ptr, out.data_ptr(), kept.cols,
              _type(out, "dtype"), kept.rows, kept.cols)
     return out
 
@@ -166,52 +191,56 @@ def layer_norm(x, weight, bias=None, eps: float = 1e-5, checkpoint: bool = False
     xhat = (x - mean) rstd (else None), from which ``layer_norm_backward`` and the next
     layer's ``linear_weight_grad`` work."""
     rows, cols, stride = _rows(x, "x")
-    dev, shape = x.device, x.shape
-    param = _vector(weight, "weight", x, cols)
-    if bias is not None and _vector(bias, "bias", x, cols) != param:
+    index, shape, dev = x.get_device(), x.shape, x.device
+    param = _vector(weight, "weight", index, cols)
+    if bias is not None and _vector(bias, "bias", index, cols) != param:
         raise TypeError("weight and bias must have one dtype")
     y = torch.empty(shape, dtype=x.dtype, device=dev)
-    stats = torch.empty((2,) + tuple(shape[:-1]), dtype=torch.float32, device=dev)
-    mean, rstd = stats.unbind(0)
-    kept = Act8.empty(rows, cols, dev, shape) if checkpoint else None
-    _enqueue("novak_layer_norm", dev, x.data_ptr(), stride, y.data_ptr(), cols, _type(x, "x"), weight.data_ptr(),
-             bias.data_ptr() if bias is not None else None, param, eps, mean.data_ptr(),
-             rstd.data_ptr(), kept.codes.data_ptr() if checkpoint else None,
-             kept.exps.data_ptr() if checkpoint else None, rows, cols)
+    mean, rstd = torch.empty((2,) + shape[:-1], dtype=torch.float32, device=dev).unbind(0)
+    kept = None
+    codes = exps = None
+    if checkpoint:
+        kept = Act8.empty(rows, cols, dev, shape)
+        codes, exps = kept.codes_ptr, kept.exps_ptr
+    _enqueue("novak_layer_norm", index, x.data_ptr(), stride, y.data_ptr(), cols, _type(x, "x"), weight.data_ptr(),
+             None if bias is None else bias.data_ptr(), param, eps, mean.data_ptr(), rstd.data_ptr(), codes, exps,
+             rows, cols)
     return y, mean, rstd, kept
+
+
+@lru_cache(maxsize=1024)
+def _norm_backward_bytes(rows: int, cols: int) -> int:
+    return _library().novak_layer_norm_backward_bytes(rows, cols)
 
 
 def layer_norm_backward(dy, saved, rstd, weight, mean=None, grad_dtype=torch.float32):
     """(dx, dweight, dbias) of ``layer_norm``.  ``saved`` is the 8-bit form of xhat that the
     forward pass left, or its input x (then ``mean`` is needed too)."""
     rows, cols, stride = _rows(dy, "dy")
-    dev, type_ = dy.device, _type(dy, "dy")
-    param = _vector(weight, "weight", dy, cols)
-    _same(rstd, "rstd", dy, dy.shape[:-1], torch.float32)
-    x_ptr = x_stride = codes = exps = mean_ptr = None
+    index, shape, dev, type_ = dy.get_device(), dy.shape, dy.device, _type(dy, "dy")
+    param = _vector(weight, "weight", index, cols)
+    _same(rstd, "rstd", index, shape[:-1], torch.float32)
+    rstd = rstd.contiguous()
+    x_ptr = codes = exps = mean_ptr = None
+    x_stride = 0
     if isinstance(saved, Act8):
-        if saved.rows != rows or saved.cols != cols or saved.codes.device != dev:
-            raise ValueError(f"the 8-bit form of {saved.rows} x {saved.cols} elements on {saved.device} does not "
-                             f"belong to dy of {rows} x {cols} on {dev}")
-        codes, exps, x_stride = saved.codes.data_ptr(), saved.exps.data_ptr(), 0
+        _belongs(saved, rows, cols, index, "dy")
+        codes, exps = saved.codes_ptr, saved.exps_ptr
     else:
-        _same(saved, "x", dy, dy.shape, dy.dtype)
+        _same(saved, "x", index, shape, dy.dtype)
         if mean is None:
             raise ValueError("mean is needed beside x")
-        _same(mean, "mean", dy, dy.shape[:-1], torch.float32)
+        _same(mean, "mean", index, shape[:-1], torch.float32)
         mean = mean.contiguous()
         _, _, x_stride = _rows(saved, "x")
         x_ptr, mean_ptr = saved.data_ptr(), mean.data_ptr()
-    rstd = rstd.contiguous()
-    dx = torch.empty(dy.shape, dtype=dy.dtype, device=dev)
-    grads = torch.empty((2, cols), dtype=grad_dtype, device=dev)
-    dw, db = grads.unbind(0)
-    need = _library().novak_layer_norm_backward_bytes(rows, cols)
+    dx = torch.empty(shape, dtype=dy.dtype, device=dev)
+    dw, db = torch.empty((2, cols), dtype=grad_dtype, device=dev).unbind(0)
+    need = _norm_backward_bytes(rows, cols)
     work = torch.empty(need, dtype=torch.uint8, device=dev)
-    _enqueue("novak_layer_norm_backward", dev, dy.data_ptr(), stride, x_ptr, x_stride, type_, mean_ptr, rstd.data_ptr(),
-             codes, exps, weight.data_ptr(), param, dx.data_ptr(), cols, dw.data_ptr(),
-             db.data_ptr(), _type(grads, "grad_dtype"), work.data_ptr(), need, rows,
-             cols)
+    _enqueue("novak_layer_norm_backward", index, dy.data_ptr(), stride, x_ptr, x_stride, type_, mean_ptr,
+             rstd.data_ptr(), codes, exps, weight.data_ptr(), param, dx.data_ptr(), cols, dw.data_ptr(), db.data_ptr(),
+             _type(dw, "grad_dtype"), work.data_ptr(), need, rows, cols)
     return dx, dw, db
 
 
@@ -230,13 +259,16 @@ def activation(u, kind: str = "gelu", save_input: bool = True, save_output: bool
     rows, cols, stride = _rows(u, "u")
     dev, shape = u.device, u.shape
     a = torch.empty(shape, dtype=u.dtype, device=dev)
-    kept_u = Act8.empty(rows, cols, dev, shape) if save_input else None
-    kept_a = Act8.empty(rows, cols, dev, shape) if save_output else None
-    _enqueue("novak_activation", dev, u.data_ptr(), stride, a.data_ptr(), cols, _type(u, "u"), k,
-             kept_u.codes.data_ptr() if save_input else None,
-             kept_u.exps.data_ptr() if save_input else None,
-             kept_a.codes.data_ptr() if save_output else None,
-             kept_a.exps.data_ptr() if save_output else None, rows, cols)
+    kept_u = kept_a = None
+    u_codes = u_exps = a_codes = a_exps = None
+    if save_input:
+        kept_u = Act8.empty(rows, cols, dev, shape)
+        u_codes, u_exps = kept_u.codes_ptr, kept_u.exps_ptr
+    if save_output:
+        kept_a = Act8.empty(rows, cols, dev, shape)
+        a_codes, a_exps = kept_a.codes_ptr, kept_a.exps_ptr
+    _enqueue("novak_activation", u.get_device(), u.data_ptr(), stride, a.data_ptr(), cols, _type(u, "u"), k, u_codes,
+             u_exps, a_codes, a_exps, rows, cols)
     return a, kept_u, kept_a
 
 
@@ -244,29 +276,26 @@ def activation_backward(da, saved, kind: str = "gelu"):
     """du = da f'(u); ``saved`` is the 8-bit form of u, or u itself."""
     k = _kind(kind)
     rows, cols, stride = _rows(da, "da")
-    dev = da.device
+    index = da.get_device()
     u_ptr = codes = exps = None
     u_stride = 0
     if isinstance(saved, Act8):
-        if saved.rows != rows or saved.cols != cols or saved.codes.device != dev:
-            raise ValueError(f"the 8-bit form of {saved.rows} x {saved.cols} elements on {saved.device} does not "
-                             f"belong to da of {rows} x {cols} on {dev}")
-        codes, exps = saved.codes.data_ptr(), saved.exps.data_ptr()
+        _belongs(saved, rows, cols, index, "da")
+        codes, exps = saved.codes_ptr, saved.exps_ptr
     else:
-        _same(saved, "u", da, da.shape, da.dtype)
+        _same(saved, "u", index, da.shape, da.dtype)
         _, _, u_stride = _rows(saved, "u")
         u_ptr = saved.data_ptr()
-    du = torch.empty(da.shape, dtype=da.dtype, device=dev)
-    _enqueue("novak_activation_backward", dev, da.data_ptr(), stride, u_ptr, u_stride, _type(da, "da"), k, codes, exps,
-             du.data_ptr(), cols, rows, cols)
+    du = torch.empty(da.shape, dtype=da.dtype, device=da.device)
+    _enqueue("novak_activation_backward", index, da.data_ptr(), stride, u_ptr, u_stride, _type(da, "da"), k, codes,
+             exps, du.data_ptr(), cols, rows, cols)
     return du
 
 
 @lru_cache(maxsize=1024)
-def _weight_grad_bytes(aligned: bool, stride: int, type_: int, rows: int, n_out: int, n_in: int,
-                       affine: bool) -> int:
+def _weight_grad_bytes(aligned: bool, stride: int, type_: int, rows: int, n_out: int, n_in: int) -> int:
     # only the address's alignment matters
-    return _library().novak_linear_weight_grad_bytes(256 if aligned else 2, stride, type_, rows, n_out, n_in, affine)
+    return _library().novak_linear_weight_grad_bytes(256 if aligned else 2, stride, type_, rows, n_out, n_in)
 
 
 def linear_weight_grad(dy, kept: Act8, affine=None, bias: bool = True, dtype=torch.float32):
@@ -276,25 +305,31 @@ def linear_weight_grad(dy, kept: Act8, affine=None, bias: bool = True, dtype=tor
     = (weight, bias) of a layer norm, ``kept`` is that norm's xhat and
     h = xhat weight + bias, the layer norm's output."""
     rows, n_out, stride = _rows(dy, "dy")
-    dev, type_ = dy.device, _type(dy, "dy")
-    n_in = kept.cols
-    if kept.rows != rows or kept.codes.device != dev:
-        raise ValueError(f"the 8-bit form has {kept.rows} rows on {kept.device}, dy {rows} on {dev}")
+    index, dev, type_, n_in = dy.get_device(), dy.device, _type(dy, "dy"), kept.cols
+    _belongs(kept, rows, n_in, index, "dy")
     w_ptr = b_ptr = None
     param = 0
     if affine is not None:
         weight, beta = affine
-        param = _vector(weight, "weight", dy, n_in)
-        if _vector(beta, "bias", dy, n_in) != param:
+        param = _vector(weight, "weight", index, n_in)
+        if _vector(beta, "bias", index, n_in) != param:
             raise TypeError("weight and bias must have one dtype")
         w_ptr, b_ptr = weight.data_ptr(), beta.data_ptr()
     dw = torch.empty((n_out, n_in), dtype=dtype, device=dev)
     db = torch.empty(n_out, dtype=dtype, device=dev) if bias else None
     ptr = dy.data_ptr()
-    need = _weight_grad_bytes(ptr % 16 == 0, stride, type_, rows, n_out, n_in, affine is not None)
+    need = _weight_grad_bytes(ptr % 16 == 0, stride, type_, rows, n_out, n_in)
     work = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    _enqueue("novak_linear_weight_grad", dev, ptr, stride, type_, kept.codes.data_ptr(), kept.exps.data_ptr(), w_ptr,
-             b_ptr, param, dw.data_ptr(), db.data_ptr() if bias else None,
-             _type(dw, "dtype"), work.data_ptr() if need else None, need, rows, n_out,
-             n_in)
+    _enqueue("novak_linear_weight_grad", index, ptr, stride, type_, kept.codes_ptr, kept.exps_ptr, w_ptr, b_ptr, param,
+             dw.data_ptr(), None if db is None else db.data_ptr(), _type(dw, "dtype"),
+             None if work is None else work.data_ptr(), need, rows, n_out, n_in)
     return dw, db
+
+
+def wait_failures() -> int:
+    """How many bounded waits inside the weight gradient's kernel ran out on the current
+    device since the library was loaded (0, or something is broken; see include/novak.h).
+    Synchronises torch's current stream."""
+    count = B.c_uint32()
+    _enqueue("novak_ops_gave_up", torch.cuda.current_device(), B.byref(count))
+    return count.value

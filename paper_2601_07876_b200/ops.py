@@ -195,7 +195,7 @@ def layer_norm(x, weight, bias=None, eps: float = 1e-5, checkpoint: bool = False
     param = _vector(weight, "weight", index, cols)
     if bias is not None and _vector(bias, "bias", index, cols) != param:
         raise TypeError("weight and bias must have one dtype")
-    y = torch.empty(shape, dtype=x.dtype, device=dev)
+    y = torch.empty_like(x) if stride == cols else torch.empty(shape, dtype=x.dtype, device=dev)
     mean, rstd = torch.empty((2,) + shape[:-1], dtype=torch.float32, device=dev).unbind(0)
     kept = None
     codes = exps = None
@@ -234,7 +234,7 @@ def layer_norm_backward(dy, saved, rstd, weight, mean=None, grad_dtype=torch.flo
         mean = mean.contiguous()
         _, _, x_stride = _rows(saved, "x")
         x_ptr, mean_ptr = saved.data_ptr(), mean.data_ptr()
-    dx = torch.empty(shape, dtype=dy.dtype, device=dev)
+    dx = torch.empty_like(dy) if stride == cols else torch.empty(shape, dtype=dy.dtype, device=dev)
     dw, db = torch.empty((2, cols), dtype=grad_dtype, device=dev).unbind(0)
     need = _norm_backward_bytes(rows, cols)
     work = torch.empty(need, dtype=torch.uint8, device=dev)
@@ -258,7 +258,7 @@ def activation(u, kind: str = "gelu", save_input: bool = True, save_output: bool
     k = _kind(kind)
     rows, cols, stride = _rows(u, "u")
     dev, shape = u.device, u.shape
-    a = torch.empty(shape, dtype=u.dtype, device=dev)
+    a = torch.empty_like(u) if stride == cols else torch.empty(shape, dtype=u.dtype, device=dev)
     kept_u = kept_a = None
     u_codes = u_exps = a_codes = a_exps = None
     if save_input:
@@ -286,7 +286,7 @@ def activation_backward(da, saved, kind: str = "gelu"):
         _same(saved, "u", index, da.shape, da.dtype)
         _, _, u_stride = _rows(saved, "u")
         u_ptr = saved.data_ptr()
-    du = torch.empty(da.shape, dtype=da.dtype, device=da.device)
+    du = torch.empty_like(da) if stride == cols else torch.empty(da.shape, dtype=da.dtype, device=da.device)
     _enqueue("novak_activation_backward", index, da.data_ptr(), stride, u_ptr, u_stride, _type(da, "da"), k, codes,
              exps, du.data_ptr(), cols, rows, cols)
     return du

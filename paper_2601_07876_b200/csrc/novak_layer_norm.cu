@@ -209,7 +209,7 @@ __global__ void __launch_bounds__(32 * forward_warps<G, NV>()) novak_layer_norm_
 // of dw and db are added up in registers over the CTA's rows and go to
 // work[CTA][2][cols], which novak_layer_norm_finish_kernel adds up in order.
 template <int TYPE, int G, int NV, bool ALIGNED, bool FROM8>
-__global__ void __launch_bounds__(32 * backward_warps<G, NV>(), G == 512 && NV == 1 && ALIGNED ? 2 : 1)
+__global__ void __launch_bounds__(32 * backward_warps<G, NV>(), G == 256 ? 2 : 1)
 novak_layer_norm_back_kernel(NormBackArgs a)
 {
     using T = typename Elem<TYPE>::T;
@@ -531,31 +531,38 @@ novak_layer_norm_finish_kernel(const float *work, int64_t splits, int64_t cols, 
 struct Spread {
     int g, nv;
 };
-constexpr Spread kAlignedRows[] = {{32, 1}, {32, 2}, {32, 3}, {32, 4}, {256, 1}, {512, 1}, {512, 2}};
+constexpr Spread kAlignedRows[] = {{32, 1}, {32, 2}, {32, 3}, {32, 4}, {256, 1}, {256, 2}, {512, 2}};
 constexpr Spread kAnyRows[] = {{32, 1}, {128, 1}, {512, 1}, {512, 2}};
 
-bool spread_for(bool aligned, int64_t cols, Spread &s)
+template <int N> bool spread_for(const Spread (&from)[N], int64_t cols, Spread &s)
 {
-    const Spread *begin = aligned ? kAlignedRows : kAnyRows;
-    const Spread *end = begin + (aligned ? sizeof kAlignedRows : sizeof kAnyRows) / sizeof(Spread);
-    for (const Spread *c = begin; c != end; ++c)
-        if (cols <= 8 * c->g * c->nv) {
-            s = *c;
+    for (const Spread &c : from)
+        if (cols <= 8 * c.g * c.nv) {
+            s = c;
             return true;
         }
     return false;
 }
 
 #define NOVAK_SPREADS(F)                                                                                          \
-    F(32, 1, true) F(32, 2, true) F(32, 3, true) F(32, 4, true) F(256, 1, true) F(512, 1, true) F(512, 2, true) \
+    F(32, 1, true) F(32, 2, true) F(32, 3, true) F(32, 4, true) F(256, 1, true) F(256, 2, true) F(512, 2, true) \
     F(32, 1, false) F(128, 1, false) F(512, 1, false) F(512, 2, false)
 
-// CTAs of the backward pass (each leaves one partial sum per column): one per SM
-// where its warps have a row each, else as many as registers let an SM hold.
+// CTAs of the backward pass, each of which leaves one partial sum per column: one per SM
+// where its warps have a row each, else what hides a row's latency (12608 x 2048 bf16:
+// one of 256 threads per SM 65 us, two 44, three 56, whose partial sums cost more than
+// they hide; 8000 x 4096 bf16: one of 512 threads 54, two of 256 51).
 int64_t back_ctas(const Spread &s, int64_t rows)
 {
-    const int per_sm = s.g == 32 ? 1 : s.g == 512 ? (s.nv == 1 ? 2 : 1) : s.g == 128 ? 4 : 2;
+    const int per_sm = s.g == 32 || s.g == 512 ? 1 : s.g == 128 ? 4 : 2;
     return std::min<int64_t>(rows, kSms * per_sm);
+}
+
+// CTAs per SM of the forward pass: what registers leave room for (4096 columns: bf16
+// 33 us with three of 256 threads, 39 with two of 512; fp32 29 and 30).
+constexpr int forward_ctas(int type, int g, int nv)
+{
+    return g == 32 ? 4 : g == 256 ? (nv == 1 ? 4 : type == NOVAK_TYPE_F32 ? 2 : 3) : 1024 / g / nv;
 }
 
 template <typename Kernel, typename Args>
@@ -574,7 +581,7 @@ template <int TYPE> cudaError_t forward(const NormArgs &a, const Spread &s, bool
 #define NOVAK_CASE(G, NV, ALIGNED)                                                                                    \
     if (s.g == G && s.nv == NV && aligned == ALIGNED) {                                                               \
         constexpr int warps = forward_warps<G, NV>(), rows = G == 32 ? warps : 1;                                     \
-        const int64_t grid = std::min<int64_t>((a.rows + rows - 1) / rows, kSms * (G == 32 ? 4 : 1024 / G));          \
+        const int64_t grid = std::min<int64_t>((a.rows + rows - 1) / rows, kSms * forward_ctas(TYPE, G, NV));         \
         return run(novak_layer_norm_kernel<TYPE, G, NV, ALIGNED>, grid, 32 * warps, 0, a, stream);                    \
     }
     NOVAK_SPREADS(NOVAK_CASE)
@@ -603,7 +610,7 @@ cudaError_t launch_layer_norm(const NormArgs &a, cudaStream_t stream)
     const bool w = wide(a.x, a.type, a.rows) && wide(a.y, a.type, a.rows);
     const bool aligned = w && a.cols % 8 == 0;
     Spread s;
-    if (spread_for(aligned, a.cols, s))
+    if (aligned ? spread_for(kAlignedRows, a.cols, s) : spread_for(kAnyRows, a.cols, s))
         return a.type == NOVAK_TYPE_F32 ? forward<0>(a, s, aligned, stream) : forward<1>(a, s, aligned, stream);
     const int grid = static_cast<int>(std::min<int64_t>(a.rows, kSms * 8));
     auto kernel = a.type == NOVAK_TYPE_F32
@@ -618,8 +625,8 @@ size_t layer_norm_backward_bytes(int64_t rows, int64_t cols)
 {
     int64_t splits = (rows + kSplitRows - 1) / kSplitRows;
     Spread s;
-    for (const bool aligned : {false, true})
-        if (spread_for(aligned, cols, s)) splits = std::max(splits, back_ctas(s, rows));
+    if (spread_for(kAnyRows, cols, s)) splits = std::max(splits, back_ctas(s, rows));
+    if (spread_for(kAlignedRows, cols, s)) splits = std::max(splits, back_ctas(s, rows));
     return static_cast<size_t>(splits * 2 * cols) * sizeof(float);
 }
 
@@ -631,7 +638,7 @@ cudaError_t launch_layer_norm_backward(const NormBackArgs &a, cudaStream_t strea
     int64_t splits = 0;
     Spread s;
     if (a.rows == 0) {
-    } else if (spread_for(aligned, a.cols, s)) {
+    } else if (aligned ? spread_for(kAlignedRows, a.cols, s) : spread_for(kAnyRows, a.cols, s)) {
         splits = back_ctas(s, a.rows);
         const bool q = a.codes.codes != nullptr;
         const cudaError_t e = a.type == NOVAK_TYPE_F32 ? (q ? backward<0, true>(a, s, aligned, splits, stream) : backward<0, false>(a, s, aligned, splits, stream))

@@ -149,37 +149,37 @@ template <> struct Eight<NOVAK_TYPE_BF16> {
     }
 };
 template <> struct Eight<NOVAK_TYPE_F32> {
-    F2 x[4];
-    __device__ __forceinline__ void zero() { x[0] = x[1] = x[2] = x[3] = F2(0.0f); }
+    // as they were loaded: forming pairs here would wait for the load
+    float4 a, b;
+    __device__ __forceinline__ void zero() { a = b = make_float4(0, 0, 0, 0); }
     __device__ __forceinline__ void load(const float *p)
     {
-        const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
-        x[0] = F2(a.x, a.y);
-        x[1] = F2(a.z, a.w);
-        x[2] = F2(b.x, b.y);
-        x[3] = F2(b.z, b.w);
+        a = *reinterpret_cast<const float4 *>(p);
+        b = *reinterpret_cast<const float4 *>(p + 4);
     }
     __device__ __forceinline__ void get(F2 (&v)[4]) const
     {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = x[i];
+        v[0] = F2(a.x, a.y);
+        v[1] = F2(a.z, a.w);
+        v[2] = F2(b.x, b.y);
+        v[3] = F2(b.z, b.w);
     }
     __device__ __forceinline__ void set(const F2 (&v)[4])
     {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = v[i];
+        a = make_float4(v[0].lo(), v[0].hi(), v[1].lo(), v[1].hi());
+        b = make_float4(v[2].lo(), v[2].hi(), v[3].lo(), v[3].hi());
     }
     __device__ __forceinline__ void store(float *p) const
     {
-        *reinterpret_cast<float4 *>(p) = make_float4(x[0].lo(), x[0].hi(), x[1].lo(), x[1].hi());
-        *reinterpret_cast<float4 *>(p + 4) = make_float4(x[2].lo(), x[2].hi(), x[3].lo(), x[3].hi());
+        *reinterpret_cast<float4 *>(p) = a;
+        *reinterpret_cast<float4 *>(p + 4) = b;
     }
     __device__ __forceinline__ uint32_t top() const
     {
+        const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
         uint32_t t = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            t = max(t, max(__float_as_uint(x[i].lo()) & 0x7fffffffu, __float_as_uint(x[i].hi()) & 0x7fffffffu));
+        for (int i = 0; i < 8; ++i) t = max(t, __float_as_uint(x[i]) & 0x7fffffffu);
         return t;
     }
 };
@@ -257,8 +257,8 @@ template <int TYPE> struct AnyEight {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     if (i >= n) w[i] = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) r.x[i] = F2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+            r.a = make_float4(__uint_as_float(w[0]), __uint_as_float(w[1]), __uint_as_float(w[2]), __uint_as_float(w[3]));
+            r.b = make_float4(__uint_as_float(w[4]), __uint_as_float(w[5]), __uint_as_float(w[6]), __uint_as_float(w[7]));
         }
         return r;
     }
@@ -308,9 +308,7 @@ __device__ __forceinline__ void store_any(float *p, const Eight<NOVAK_TYPE_F32> 
 {
     const int lane = threadIdx.x & 31, back = static_cast<int>(reinterpret_cast<uintptr_t>(p) & 15u) / 4, head = 4 - back;
     // elements 0-3: the last of the lane before; 4-11: own
-    float w[12];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v.x[i].get(w[4 + 2 * i], w[5 + 2 * i]);
+    float w[12] = {0, 0, 0, 0, v.a.x, v.a.y, v.a.z, v.a.w, v.b.x, v.b.y, v.b.z, v.b.w};
 #pragma unroll
     for (int i = 1; i < 4; ++i) w[i] = __shfl_up_sync(0xffffffffu, w[8 + i], 1);
     float t[8];         // two pieces, from `back` elements before the first

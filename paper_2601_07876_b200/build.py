@@ -1,12 +1,15 @@
 """Builds ``libnovak.so`` (the C-ABI library) in-tree with nvcc for sm_100a.
 
-Every source is compiled to an object on its own, in parallel, then linked."""
+Every source is compiled to an object on its own, in parallel, then linked.  Beside it
+stands a small host extension, ``_novak_torch``: the training operators' calls from torch
+tensors, compiled by the host compiler against torch's headers."""
 from __future__ import annotations
 
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 import tempfile
 import zlib
 from concurrent.futures import ThreadPoolExecutor
@@ -135,5 +138,43 @@ def build(force: bool = False, verbose: bool = False, extra: list[str] | None = 
     return out
 
 
+TORCH_SOURCE = os.path.join(CSRC, "novak_torch.cpp")
+
+
+def torch_extension() -> str:
+    """Where the host extension stands: one file per interpreter and torch version, since it
+    holds for those alone."""
+    import torch
+    return os.path.join(PKG, f"_novak_torch.{sys.implementation.cache_tag}.torch-{torch.__version__}.so")
+
+
+def build_torch(force: bool = False) -> str:
+    """Compiles the host extension if its source is newer than the built file."""
+    import torch
+    out = torch_extension()
+    reads = (TORCH_SOURCE, os.path.join(ROOT, "include", "novak.h"))
+    if not force and os.path.exists(out) and all(os.path.getmtime(f) <= os.path.getmtime(out) for f in reads):
+        return out
+    home = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(nvcc_path()))
+    tmp = f"{out}.{os.getpid()}.tmp"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Wextra",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include")]
+    for path in (os.path.join(home, "include"), os.path.join(home, "include", "torch", "csrc", "api", "include"),
+                 os.path.join(cuda, "include"), sysconfig.get_paths()["include"]):
+        cmd += ["-isystem", path]
+    cmd += [TORCH_SOURCE, "-o", tmp, "-L" + os.path.join(home, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu",
+            "-lc10", "-lc10_cuda"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        sys.stderr.write(res.stdout + res.stderr)
+        if os.path.exists(tmp):
+            os.remove(tmp)
+        raise RuntimeError("the host compiler failed building the torch extension")
+    os.replace(tmp, out)
+    return out
+
+
 if __name__ == "__main__":
+    print(build_torch(force="-f" in sys.argv))
     print(build(force="-f" in sys.argv, verbose="-v" in sys.argv))

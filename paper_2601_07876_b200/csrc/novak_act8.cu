@@ -247,8 +247,9 @@ Rows rows_of(const Mat &x, const Mat &y, const Mat &z, int type, Place &p, dim3 
         return kFlat;
     }
     p.groups = act_pitch(p.cols) / 8;
-    p.log2 = 5;             // a warp is in one row
-    while (p.log2 < 8 && (int64_t(1) << p.log2) < p.groups) ++p.log2;
+    p.log2 = 5;             // a warp is in one row; the most threads that leave the fewest over
+    for (int i = 6; i <= 8; ++i)
+        if ((-p.groups & ((int64_t(1) << i) - 1)) <= (-p.groups & 31)) p.log2 = i;
     const int64_t per_pass = int64_t(kUnroll) << (8 - p.log2);
     grid = dim3(static_cast<unsigned>((p.groups + (int64_t(1) << p.log2) - 1) >> p.log2),
                 static_cast<unsigned>(std::min<int64_t>((p.rows + per_pass - 1) / per_pass, 65535)));

@@ -102,47 +102,11 @@ __global__ void __launch_bounds__(kPlainThreads) novak_weight_grad_few_kernel(We
     }
 }
 
-// ---- dy as the tensor copies need it ---------------------------------------------
-// [planes][rows][ld] bf16, ld a multiple of 8: a copy of a bf16 matrix whose rows
-// are not 16-byte aligned, or the three parts of an fp32 one.  Each part is what
-// is left cut to 8 bits toward zero (so that none rounds up to an infinity); an
-// infinity or NaN is in the first part alone.
-template <int TYPE>
-__global__ void __launch_bounds__(256)
-novak_weight_grad_planes_kernel(const typename Elem<TYPE>::T *dy, int64_t stride, __nv_bfloat16 *out, int64_t ld,
-                                int64_t rows, int64_t cols)
-{
-    const int64_t groups = ld / 8, n = rows * groups, plane = rows * ld;
-    grid_wait();
-    grid_launch_next();
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256) {
-        const int64_t row = i / groups, col = (i - row * groups) * 8;
-        float v[8];
-        load8<false>(dy + row * stride, col, cols, v);
-        __nv_bfloat16 *dst = out + row * ld + col;
-        if constexpr (TYPE == NOVAK_TYPE_BF16) {
-            store8<true>(dst, 0, 8, v);
-        } else {
-#pragma unroll
-            for (int p = 0; p < 3; ++p) {
-                float part[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const bool finite = (__float_as_uint(v[k]) & 0x7f800000u) != 0x7f800000u;
-                    part[k] = finite ? __uint_as_float(__float_as_uint(v[k]) & 0xffff0000u) : v[k];
-                    v[k] = finite ? v[k] - part[k] : 0.0f;
-                }
-                store8<true>(dst + p * plane, 0, 8, part);
-            }
-        }
-    }
-}
-
 // ---- the work, cut up --------------------------------------------------------------
 constexpr int kTileN = 256, kTileK = 256;       // dW rows and columns of a pair
 constexpr int kRows = 64;                       // rows of dy and x per step
 constexpr int kGroupN = 8;                      // tiles whose x is shared by neighbours in time
-constexpr int kMinSteps = 4;                    // steps that are worth a pair's while
+constexpr int kMinSteps = 4;                    // steps of a cut tile that are worth a pair's while
 
 struct Cut {
     int tiles_n, tiles_k;
@@ -248,16 +212,21 @@ __device__ __forceinline__ void tile_slots(const Cut &c, int r, int &slot, int &
     n = hi - lo + 1;
 }
 
-// ---- db, and what a layer norm's offset is multiplied with ------------------------------
-// Sums of dy's columns over a part of the rows: sums[part][ld], 256 columns per CTA, 8 per
+// ---- one pass over dy before the products ----------------------------------------------
+// Sums of dy's columns over a part of the rows, for db and for what a layer norm's offset
+// is multiplied with: sums[part][ld] (null: not asked for).  256 columns per CTA, 8 per
 // lane, the warps on rows in turn.
-constexpr int kSumRows = 64;            // rows that a CTA is worth
+// COPY: dy as the tensor copies need it too, out[planes][rows][out_ld] in bf16, out_ld a
+// multiple of 8: a copy of a bf16 matrix whose rows are not 16-byte aligned, or the three
+// parts of an fp32 one.  Each part is what is left cut to 8 bits toward zero (so that none
+// rounds up to an infinity); an infinity or NaN is in the first part alone.
+constexpr int kSumRows = 16;            // rows that a CTA is worth
 constexpr int kMostParts = 64;
 
-template <int TYPE, bool ALIGNED>
+template <int TYPE, bool ALIGNED, bool COPY>
 __global__ void __launch_bounds__(256)
 novak_weight_grad_sums_kernel(const typename Elem<TYPE>::T *dy, int64_t stride, float *sums, int64_t ld, int64_t rows,
-                              int64_t cols, int64_t rows_per_part)
+                              int64_t cols, int64_t rows_per_part, __nv_bfloat16 *out, int64_t out_ld)
 {
     __shared__ float part[8][256];
     grid_wait();
@@ -282,8 +251,38 @@ novak_weight_grad_sums_kernel(const typename Elem<TYPE>::T *dy, int64_t stride, 
             raw[i].eight().get(v);
 #pragma unroll
             for (int k = 0; k < 4; ++k) s[k] = s[k] + v[k];
+            if (COPY && n > 0 && row + 8 * i < row1) {
+                __nv_bfloat16 *dst = out + (row + 8 * i) * out_ld + col;
+                Eight<NOVAK_TYPE_BF16> e;
+                if constexpr (TYPE == NOVAK_TYPE_BF16) {
+                    e.set(v);
+                    e.store(dst);
+                } else {
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) {
+                        F2 cut[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            float c[2] = {v[k].lo(), v[k].hi()}, left[2];
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const uint32_t bits = __float_as_uint(c[h]);
+                                const bool finite = (bits & 0x7f800000u) != 0x7f800000u;
+                                const float whole = c[h];
+                                if (finite) c[h] = __uint_as_float(bits & 0xffff0000u);
+                                left[h] = finite ? whole - c[h] : 0.0f;
+                            }
+                            cut[k] = F2(c[0], c[1]);
+                            v[k] = F2(left[0], left[1]);
+                        }
+                        e.set(cut);
+                        e.store(dst + p * rows * out_ld);
+                    }
+                }
+            }
         }
     }
+    if (!sums) return;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         part[warp][lane * 8 + 2 * k] = s[k].lo();
@@ -293,15 +292,15 @@ novak_weight_grad_sums_kernel(const typename Elem<TYPE>::T *dy, int64_t stride, 
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum += part[i][threadIdx.x];
-    const int64_t out = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (out < cols) sums[blockIdx.y * ld + out] = sum;
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (at < cols) sums[blockIdx.y * ld + at] = sum;
 }
 
 // The parts added up, in order.
 __device__ __forceinline__ float column_sum(const float *sums, int parts, int64_t ld, int64_t n)
 {
     float s = 0.0f;
-#pragma unroll 8
+#pragma unroll 16
     for (int i = 0; i < parts; ++i) s += sums[i * ld + n];
     return s;
 }
@@ -354,12 +353,11 @@ template <int N> struct Ring {
 struct KernelArgs {
     Cut cut;
     Codes codes;
-    int64_t pitch;
-    void *dw;
+    void *dw, *db;
     int grad_type, vector;
     int64_t rows, n_out, n_in;
     float *partial;                 // [slot][64][256 rows][4 columns] per tile
-    const float *sums;              // [parts][sums_ld], where a layer norm's weight and bias are given
+    const float *sums;              // [parts][sums_ld], with db or a layer norm's weight and bias
     int parts;
     int64_t sums_ld;
     const void *weight, *bias;
@@ -389,7 +387,7 @@ __device__ __forceinline__ void load_codes(const KernelArgs &a, const CUtensorMa
                                            uint32_t rank, int pair)
 {
     const int mine = threadIdx.x / 32 - kLoadWarp, lane = threadIdx.x % 32;
-    const int64_t blocks = a.pitch / 32;
+    const int64_t blocks = (a.n_in + 31) / 32;
     const bool words = (blocks & 3) == 0 && (reinterpret_cast<uintptr_t>(a.codes.exps) & 3) == 0;
     Walk walk(a.cut, pair);
     Piece piece;
@@ -577,8 +575,11 @@ __device__ __forceinline__ void take_out(const KernelArgs &a, Shared &sh, uint32
         const int row = lane / 8, col = lane % 8;               // four rows, eight groups of four columns
         const int64_t row0 = n0 + quarter * 32 + row, k0 = static_cast<int64_t>(tk) * kTileK + side * 128 + 4 * col;
         float mine = 0.0f;              // lane i: the column sum of dy for row i
-        if (a.weight && !partial && n0 + quarter * 32 + lane < a.n_out)
+        const bool bias = a.db && tk == 0 && side == 0;
+        if ((a.weight || bias) && !partial && n0 + quarter * 32 + lane < a.n_out) {
             mine = column_sum(a.sums, a.parts, a.sums_ld, n0 + quarter * 32 + lane);
+            if (bias) store_param(a.db, a.grad_type, n0 + quarter * 32 + lane, mine);
+        }
 #pragma unroll 1
         for (int c = 0; c < 128; c += 32) {
             float v[32];
@@ -790,8 +791,8 @@ struct FinishArgs {
     int64_t n_out, n_in;
 };
 
-// kFinishRows rows of a tile left over per CTA, two groups of four columns of one per
-// thread; then a CTA for each 256 elements of db.
+// kFinishRows rows of a tile that was cut per CTA, two groups of four columns of one per
+// thread.
 constexpr int kFinishRows = 8, kFinishCtas = kTileN / kFinishRows;
 __global__ void __launch_bounds__(256) novak_weight_grad_finish_kernel(const __grid_constant__ FinishArgs a)
 {
@@ -800,18 +801,14 @@ __global__ void __launch_bounds__(256) novak_weight_grad_finish_kernel(const __g
     const Cut &cut = a.cut;
     grid_wait();
     const int group = blockIdx.x % kFinishCtas, item = blockIdx.x / kFinishCtas;
-    if (item >= cut.rest) {
-        const int64_t n = static_cast<int64_t>(blockIdx.x - cut.rest * kFinishCtas) * 256 + threadIdx.x;
-        if (n < a.n_out) store_param(a.db, a.grad_type, n, column_sum(a.sums, a.parts, a.sums_ld, n));
-        return;
-    }
     int tn, tk, slot, n;
     tile_at(cut, cut.waves * cut.pairs + item, tn, tk);
     tile_slots(cut, item, slot, n);
     const int64_t n0 = static_cast<int64_t>(tn) * kTileN + group * kFinishRows;
     if (n == 1 || n0 >= a.n_out) return;
     const int row = threadIdx.x % kFinishRows, lane = threadIdx.x / kFinishRows;
-    if (a.weight) {
+    const bool bias = a.db && tk == 0;
+    if (a.weight || bias) {
         float s = 0.0f;
         for (int i = lane; i < a.parts; i += 32) s += a.sums[i * a.sums_ld + n0 + row];        // (padded to whole tiles)
         part[lane][row] = s;
@@ -830,12 +827,13 @@ __global__ void __launch_bounds__(256) novak_weight_grad_finish_kernel(const __g
         *reinterpret_cast<float4 *>(&turn[row][4 * c]) = v;
     }
     __syncthreads();
-    if (a.weight) {
+    if (a.weight || bias) {
         if (threadIdx.x < kFinishRows) {
             float s = 0.0f;
 #pragma unroll
             for (int i = 0; i < 32; ++i) s += part[i][threadIdx.x];
             total[threadIdx.x] = s;
+            if (bias && n0 + row < a.n_out) store_param(a.db, a.grad_type, n0 + row, s);
         }
         __syncthreads();
     }
@@ -861,6 +859,7 @@ __global__ void __launch_bounds__(256) novak_weight_grad_finish_kernel(const __g
 struct Layout {
     int planes;
     bool copied;            // dy goes through the workspace
+    bool cut_up;            // some tiles do
     int64_t ld;             // elements between rows as the tensor copies see them
     Cut cut;
     int parts;              // of the rows, in sums of dy's columns
@@ -888,12 +887,19 @@ Layout layout_for(const Mat &dy, int type, int64_t rows, int64_t n_out, int64_t 
     c.pairs = kPairs;
     c.waves = tiles / kPairs;
     c.rest = tiles % kPairs;
-    c.rest_pairs = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kPairs, static_cast<int64_t>(c.rest) * c.steps / kMinSteps)));
+    // The tiles left over: each whole on a pair of its own, or their steps cut evenly over all pairs, which
+    // costs one more kernel and the way of the partial tiles through memory, 256 KB each: as much as about
+    // four steps, and one for every eight of them (1024 x 256 -> 256: cut 14 us, whole 19; 1024 x 768 -> 768:
+    // 15 and 20; 1024 x 2048 -> 1024: 22 and 19).
     const int64_t left = static_cast<int64_t>(c.rest) * c.steps;
+    const int cut_pairs = static_cast<int>(std::min<int64_t>(kPairs, left / kMinSteps));
+    c.rest_pairs = std::max(c.rest, 1);
+    if (cut_pairs > c.rest && c.steps - left / cut_pairs >= 4 + (cut_pairs + c.rest) / 8) c.rest_pairs = cut_pairs;
     c.share = left / c.rest_pairs;
     c.extra = static_cast<int>(left % c.rest_pairs);
-    l.partial_bytes = static_cast<size_t>(slots(c)) * kTileN * kTileK * sizeof(float);
-    // sums of columns: about four CTAs per SM
+    l.cut_up = c.rest_pairs > c.rest && c.rest > 0;
+    l.partial_bytes = l.cut_up ? static_cast<size_t>(slots(c)) * kTileN * kTileK * sizeof(float) : 0;
+    // the pass over dy: about four CTAs per SM
     const int64_t column_ctas = (n_out + 255) / 256;
     const int64_t want = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(kMostParts, 148 * 4 / column_ctas), rows / kSumRows));
     l.rows_per_part = (rows + want - 1) / want;
@@ -937,13 +943,14 @@ cudaError_t launch(void (*kernel)(Params...), dim3 grid, int threads, int smem, 
     return cudaLaunchKernelEx(&lc, kernel, static_cast<Params>(args)...);
 }
 
-template <int TYPE> cudaError_t launch_sums(const WeightGradArgs &a, const Layout &l, float *sums, cudaStream_t stream)
+template <int TYPE, bool ALIGNED>
+cudaError_t launch_sums(const WeightGradArgs &a, const Layout &l, float *sums, __nv_bfloat16 *out, cudaStream_t stream)
 {
-    using T = typename Elem<TYPE>::T;
-    auto kernel = wide(a.dy, TYPE, a.rows) && a.n_out % 8 == 0 ? novak_weight_grad_sums_kernel<TYPE, true>
-                                                               : novak_weight_grad_sums_kernel<TYPE, false>;
+    constexpr bool kAlways = TYPE == NOVAK_TYPE_F32;
+    const auto kernel = out ? novak_weight_grad_sums_kernel<TYPE, ALIGNED, true> : novak_weight_grad_sums_kernel<TYPE, ALIGNED, kAlways>;
     return launch(kernel, dim3(static_cast<unsigned>(l.sums_ld / 256), static_cast<unsigned>(l.parts)), 256, 0, stream,
-                  static_cast<const T *>(a.dy.ptr), a.dy.stride, sums, l.sums_ld, a.rows, a.n_out, l.rows_per_part);
+                  static_cast<const typename Elem<TYPE>::T *>(a.dy.ptr), a.dy.stride, sums, l.sums_ld, a.rows, a.n_out,
+                  l.rows_per_part, out, l.ld);
 }
 
 }  // namespace
@@ -973,20 +980,16 @@ cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t stream)
     const Layout l = layout_for(a.dy, a.type, a.rows, a.n_out, a.n_in);
     uint8_t *work = static_cast<uint8_t *>(a.work);
     float *sums = reinterpret_cast<float *>(work + l.planes_bytes + l.partial_bytes);
-    if (a.db || a.weight) {
-        const cudaError_t e = a.type == NOVAK_TYPE_F32 ? launch_sums<0>(a, l, sums, stream) : launch_sums<1>(a, l, sums, stream);
-        if (e != cudaSuccess) return e;
-    }
     const __nv_bfloat16 *dy = static_cast<const __nv_bfloat16 *>(a.dy.ptr);
-    if (l.copied) {
-        __nv_bfloat16 *out = reinterpret_cast<__nv_bfloat16 *>(work);
-        const int grid = static_cast<int>(std::min<int64_t>((a.rows * (l.ld / 8) + 255) / 256, 148 * 32));
-        const cudaError_t e = a.type == NOVAK_TYPE_F32
-                                  ? launch(novak_weight_grad_planes_kernel<0>, grid, 256, 0, stream, static_cast<const float *>(a.dy.ptr),
-                                           a.dy.stride, out, l.ld, a.rows, a.n_out)
-                                  : launch(novak_weight_grad_planes_kernel<1>, grid, 256, 0, stream, dy, a.dy.stride, out, l.ld, a.rows, a.n_out);
+    if (l.copied || a.db || a.weight) {
+        __nv_bfloat16 *copy = l.copied ? reinterpret_cast<__nv_bfloat16 *>(work) : nullptr;
+        if (!a.db && !a.weight) sums = nullptr;
+        const bool aligned = wide(a.dy, a.type, a.rows) && a.n_out % 8 == 0;
+        const auto pass = a.type == NOVAK_TYPE_F32 ? (aligned ? launch_sums<0, true> : launch_sums<0, false>)
+                                                   : (aligned ? launch_sums<1, true> : launch_sums<1, false>);
+        const cudaError_t e = pass(a, l, sums, copy, stream);
         if (e != cudaSuccess) return e;
-        dy = out;
+        if (copy) dy = copy;
     }
     const EncodeTiled encode = encoder();
     if (!encode) return cudaErrorNotSupported;
@@ -1021,16 +1024,16 @@ cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t stream)
 
     const int vector = a.n_in % 4 == 0 && reinterpret_cast<uintptr_t>(a.dw) % (a.grad_type == NOVAK_TYPE_F32 ? 16 : 8) == 0;
     float *partial = reinterpret_cast<float *>(work + l.planes_bytes);
-    const KernelArgs k{l.cut, a.codes, act_pitch(a.n_in), a.dw, a.grad_type, vector, a.rows, a.n_out, a.n_in, partial,
+    const KernelArgs k{l.cut, a.codes, a.dw, a.db, a.grad_type, vector, a.rows, a.n_out, a.n_in, partial,
                        sums, l.parts, l.sums_ld, a.weight, a.bias, a.param_type};
     const int pairs = l.cut.waves > 0 ? l.cut.pairs : l.cut.rest_pairs;
     e = launch(novak_weight_grad_kernel, 2 * pairs, kThreads, kSmemBytes, stream, k, map, codes_map);
     if (e != cudaSuccess) return e;
 
+    if (!l.cut_up) return cudaSuccess;
     const FinishArgs f{l.cut, partial, sums, l.parts, l.sums_ld, a.weight, a.bias, a.param_type, a.dw, a.db, a.grad_type,
                        vector, a.n_out, a.n_in};
-    const int64_t blocks = static_cast<int64_t>(kFinishCtas) * l.cut.rest + (a.db ? (a.n_out + 255) / 256 : 0);
-    return blocks > 0 ? launch(novak_weight_grad_finish_kernel, dim3(static_cast<unsigned>(blocks)), 256, 0, stream, f) : cudaSuccess;
+    return launch(novak_weight_grad_finish_kernel, dim3(static_cast<unsigned>(kFinishCtas * l.cut.rest)), 256, 0, stream, f);
 }
 
 }  // namespace novak

@@ -43,62 +43,114 @@ __device__ __forceinline__ void store_param(void *p, int type, int64_t i, float 
     else static_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(v);
 }
 
-// ---- few rows: the outer products, in fp32 on the ordinary cores ----------------
-constexpr int kFewRows = 16;
-constexpr int kTile = 64, kDepth = 16, kPlainThreads = 256;
-
-// A 64 x 64 tile per CTA, 4 x 4 products per thread.
-template <int TYPE>
-__global__ void __launch_bounds__(kPlainThreads) novak_weight_grad_few_kernel(WeightGradArgs a)
+// Four neighbouring elements of dW's row, column k on.
+template <typename Args>
+__device__ __forceinline__ void store_four(const Args &a, int64_t at, int64_t k, float x0, float x1, float x2, float x3)
 {
-    using T = typename Elem<TYPE>::T;
-    __shared__ float sdy[kDepth][kTile], sx[kDepth][kTile];
-    const int64_t pitch = (a.n_in + 31) / 32 * 32;
-    const int64_t n0 = static_cast<int64_t>(blockIdx.y) * kTile, k0 = static_cast<int64_t>(blockIdx.x) * kTile;
-    const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
-    float acc[4][4] = {}, sum[4] = {};
-    for (int i = threadIdx.x; i < kDepth * kTile; i += kPlainThreads) {
-        const int64_t t = i / kTile, n = n0 + i % kTile;
-        sdy[i / kTile][i % kTile] = t < a.rows && n < a.n_out
-                                        ? to_float(static_cast<const T *>(a.dy.ptr)[t * a.dy.stride + n]) : 0.0f;
-    }
-    if (threadIdx.x < kDepth * kTile / 8) {
-        const int64_t t = threadIdx.x / 8, k = k0 + threadIdx.x % 8 * 8;
-        float v[8] = {};
-        if (t < a.rows && k < pitch)
-            dequantize8(*reinterpret_cast<const uint2 *>(a.codes.codes + t * pitch + k),
-                        a.codes.exps[(t * pitch + k) >> 5], v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sx[threadIdx.x / 8][threadIdx.x % 8 * 8 + i] = v[i];
-    }
-    __syncthreads();
-    for (int d = 0; d < static_cast<int>(a.rows); ++d) {
-        float x[4], y[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            y[i] = sdy[d][ty * 4 + i];
-            x[i] = sx[d][tx + 16 * i];
-            sum[i] += y[i];
-        }
+    if (a.vector && k < a.n_in) {           // n_in is a multiple of 4 and dw aligned to four elements
+        if (a.grad_type == NOVAK_TYPE_F32)
+            *reinterpret_cast<float4 *>(static_cast<float *>(a.dw) + at) = make_float4(x0, x1, x2, x3);
+        else
+            *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(a.dw) + at) = make_uint2(bf16_pair(x0, x1), bf16_pair(x2, x3));
+    } else {
+        const float x[4] = {x0, x1, x2, x3};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(y[i], x[j], acc[i][j]);
+            if (k + i < a.n_in) store_param(a.dw, a.grad_type, at + i, x[i]);
     }
+}
+
+// A layer norm's weight and bias for four columns, k on.
+template <typename Args>
+__device__ __forceinline__ void load_affine(const Args &a, int64_t k, float (&w)[4], float (&b)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        w[i] = k + i < a.n_in ? param_at(a.weight, a.param_type, k + i) : 0.0f;
+        b[i] = k + i < a.n_in ? param_at(a.bias, a.param_type, k + i) : 0.0f;
+    }
+}
+
+// ---- little work: the products in fp32 on the ordinary cores ---------------------
+constexpr int kTile = 64, kDepth = 32, kPlainThreads = 256;
+
+struct FewArgs : WeightGradArgs {
+    int vector;
+};
+
+// A 64 x 64 tile per CTA, 4 x 4 products per thread; 32 rows at a time, the next ones
+// on their way while these are worked on.
+template <int TYPE>
+__global__ void __launch_bounds__(kPlainThreads) novak_weight_grad_few_kernel(FewArgs a)
+{
+    using T = typename Elem<TYPE>::T;
+    __shared__ __align__(16) float sdy[2][kDepth][kTile], sx[2][kDepth][kTile];
+    constexpr int kEach = kDepth * kTile / kPlainThreads, kStep = kPlainThreads / kTile;
+    const int64_t pitch = (a.n_in + 31) / 32 * 32;
+    const int64_t n0 = static_cast<int64_t>(blockIdx.y) * kTile, k0 = static_cast<int64_t>(blockIdx.x) * kTile;
+    const int ty = threadIdx.x / 16, tx = threadIdx.x % 16, rows = static_cast<int>(a.rows);
+    // what a thread brings: dy's column n0 + cn of every fourth row; 8 codes of a row
+    static_assert(kDepth * kTile / 8 == kPlainThreads, "eight codes each");
+    const int cn = threadIdx.x % kTile, rn = threadIdx.x / kTile, rk = threadIdx.x / 8, ck = threadIdx.x % 8 * 8;
+    const bool has_n = n0 + cn < a.n_out, has_k = k0 + ck < pitch;
+    T y_next[kEach];
+    uint2 q_next;
+    uint32_t e_next;
+    const auto fetch = [&](int t0) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int t = t0 + rn + kStep * i;
+            y_next[i] = T(0.0f);
+            if (has_n && t < rows) y_next[i] = static_cast<const T *>(a.dy.ptr)[t * a.dy.stride + n0 + cn];
+        }
+        q_next = make_uint2(0, 0);
+        e_next = 0;
+        if (has_k && t0 + rk < rows) {
+            const int64_t at = (t0 + rk) * pitch + k0 + ck;
+            q_next = *reinterpret_cast<const uint2 *>(a.codes.codes + at);
+            e_next = a.codes.exps[at >> 5];
+        }
+    };
+    float acc[4][4] = {}, sum[4] = {};
+    fetch(0);
+    for (int t0 = 0, buf = 0; t0 < rows; t0 += kDepth, buf ^= 1) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) sdy[buf][rn + kStep * i][cn] = to_float(y_next[i]);
+        float v[8];
+        dequantize8(q_next, e_next, v);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            *reinterpret_cast<float4 *>(&sx[buf][rk][ck + 4 * i]) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        __syncthreads();        // (and nobody is in the other buffers any more when they are next written)
+        if (t0 + kDepth < rows) fetch(t0 + kDepth);
+        const int depth = min(kDepth, rows - t0);
+#pragma unroll 4
+        for (int d = 0; d < depth; ++d) {
+            const float4 y4 = *reinterpret_cast<const float4 *>(&sdy[buf][d][ty * 4]);
+            const float4 x4 = *reinterpret_cast<const float4 *>(&sx[buf][d][tx * 4]);
+            const float y[4] = {y4.x, y4.y, y4.z, y4.w}, x[4] = {x4.x, x4.y, x4.z, x4.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                sum[i] += y[i];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(y[i], x[j], acc[i][j]);
+            }
+        }
+    }
+    const int64_t k = k0 + tx * 4;
+    float w[4], b[4];
+    if (a.weight) load_affine(a, k, w, b);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int64_t n = n0 + ty * 4 + i;
         if (n >= a.n_out) continue;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t k = k0 + tx + 16 * j;
-            if (k >= a.n_in) continue;
-            float v = acc[i][j];
-            if (a.weight)
-                v = fmaf(v, param_at(a.weight, a.param_type, k), param_at(a.bias, a.param_type, k) * sum[i]);
-            store_param(a.dw, a.grad_type, n * a.n_in + k, v);
-        }
         if (a.db && blockIdx.x == 0 && tx == 0) store_param(a.db, a.grad_type, n, sum[i]);
+        if (k >= a.n_in) continue;
+        float *x = acc[i];
+        if (a.weight)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = fmaf(x[j], w[j], b[j] * sum[i]);
+        store_four(a, n * a.n_in + k, k, x[0], x[1], x[2], x[3]);
     }
 }
 
@@ -494,34 +546,6 @@ __device__ __forceinline__ void fill_x(const KernelArgs &a, Shared &sh, uint32_t
         if (!mbar_wait_warp(done + x.slot * 8, x.phase ^ 1)) return;
 }
 
-// Four neighbouring elements of dW's row, column k on.
-template <typename Args>
-__device__ __forceinline__ void store_four(const Args &a, int64_t at, int64_t k, float x0, float x1, float x2, float x3)
-{
-    if (a.vector && k < a.n_in) {           // n_in is a multiple of 4 and dw aligned to four elements
-        if (a.grad_type == NOVAK_TYPE_F32)
-            *reinterpret_cast<float4 *>(static_cast<float *>(a.dw) + at) = make_float4(x0, x1, x2, x3);
-        else
-            *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(a.dw) + at) = make_uint2(bf16_pair(x0, x1), bf16_pair(x2, x3));
-    } else {
-        const float x[4] = {x0, x1, x2, x3};
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (k + i < a.n_in) store_param(a.dw, a.grad_type, at + i, x[i]);
-    }
-}
-
-// A layer norm's weight and bias for four columns, k on.
-template <typename Args>
-__device__ __forceinline__ void load_affine(const Args &a, int64_t k, float (&w)[4], float (&b)[4])
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        w[i] = k + i < a.n_in ? param_at(a.weight, a.param_type, k + i) : 0.0f;
-        b[i] = k + i < a.n_in ? param_at(a.bias, a.param_type, k + i) : 0.0f;
-    }
-}
-
 // Warps 0 ..: the tile.  A warp has 32 rows (its quarter of the lanes) x 128 columns
 // of it in registers and adds to them what the tensor cores have summed of a run.
 __device__ __forceinline__ void take_out(const KernelArgs &a, Shared &sh, uint32_t tmem, uint32_t rank, int pair)
@@ -869,6 +893,15 @@ struct Layout {
 
 constexpr size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
 
+// Whether the ordinary cores are done before the tensor cores' kernels are under way
+// (us here and there: 64 x 256 -> 256 4.9 and 11.1, 192 x 256 -> 256 10.7 and 12.2, 256 x
+// 256 -> 256 13.4 and 12.1; 64 x 1024 -> 1024 7.4 and 11.5, 128 x 1024 -> 1024 12.5 and
+// 12.2, 40 x 2048 -> 2048 15.1 and 12.2).  Up to 16 rows it is writing dW that takes time.
+bool little(int64_t rows, int64_t n_out, int64_t n_in)
+{
+    return rows <= 16 || (rows <= 192 && static_cast<double>(rows) * n_out * n_in <= 1e8);
+}
+
 // (The workspace is the same with and without db and a layer norm's weight and bias.)
 Layout layout_for(const Mat &dy, int type, int64_t rows, int64_t n_out, int64_t n_in)
 {
@@ -957,7 +990,7 @@ cudaError_t launch_sums(const WeightGradArgs &a, const Layout &l, float *sums, _
 
 size_t weight_grad_bytes(const Mat &dy, int type, int64_t rows, int64_t n_out, int64_t n_in)
 {
-    if (rows <= kFewRows) return 0;
+    if (little(rows, n_out, n_in)) return 0;
     const Layout l = layout_for(dy, type, rows, n_out, n_in);
     return l.planes_bytes + l.partial_bytes + l.sums_bytes;
 }
@@ -970,11 +1003,13 @@ cudaError_t weight_grad_gave_up(unsigned *count, cudaStream_t stream)
 
 cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t stream)
 {
-    if (a.rows <= kFewRows) {
+    const int vector = a.n_in % 4 == 0 && reinterpret_cast<uintptr_t>(a.dw) % (a.grad_type == NOVAK_TYPE_F32 ? 16 : 8) == 0;
+    if (little(a.rows, a.n_out, a.n_in)) {
         const dim3 grid(static_cast<unsigned>((a.n_in + kTile - 1) / kTile),
                         static_cast<unsigned>((a.n_out + kTile - 1) / kTile));
-        if (a.type == NOVAK_TYPE_F32) novak_weight_grad_few_kernel<0><<<grid, kPlainThreads, 0, stream>>>(a);
-        else novak_weight_grad_few_kernel<1><<<grid, kPlainThreads, 0, stream>>>(a);
+        const FewArgs f{a, vector};
+        if (a.type == NOVAK_TYPE_F32) novak_weight_grad_few_kernel<0><<<grid, kPlainThreads, 0, stream>>>(f);
+        else novak_weight_grad_few_kernel<1><<<grid, kPlainThreads, 0, stream>>>(f);
         return cudaGetLastError();
     }
     const Layout l = layout_for(a.dy, a.type, a.rows, a.n_out, a.n_in);
@@ -1022,7 +1057,6 @@ cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t stream)
     }
     if (e != cudaSuccess) return e;
 
-    const int vector = a.n_in % 4 == 0 && reinterpret_cast<uintptr_t>(a.dw) % (a.grad_type == NOVAK_TYPE_F32 ? 16 : 8) == 0;
     float *partial = reinterpret_cast<float *>(work + l.planes_bytes);
     const KernelArgs k{l.cut, a.codes, a.dw, a.db, a.grad_type, vector, a.rows, a.n_out, a.n_in, partial,
                        sums, l.parts, l.sums_ld, a.weight, a.bias, a.param_type};

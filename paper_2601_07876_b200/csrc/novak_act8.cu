@@ -1,6 +1,17 @@
 // The 8-bit form of activations (packing, unpacking) and the activation functions
-// that leave it and take it up.  One element costs one read and one write of
-// everything it has: HBM-bound.
+// that leave it and take it up:
+//     E = max(exponent(max |x| of 32) - 6, 0), s = 2^(E - 127), q = clamp(rint(x / s));
+//     a = f(u), du = da f'(s q).
+// One element costs one read and one write of everything it has.  A thread has eight
+// neighbouring elements, a quad of lanes a block of 32, so that loads and stores are of
+// 16 bytes and a block's maximum is two shuffles; two such groups per thread, both loaded
+// first.  Bound by HBM where rows are 16-byte aligned: 8192 x 4096 bf16 packed in 15.8 us
+// (6.42 TB/s) and unpacked in 14.8 (6.86, some of it out of L2); 12608 x 3072 bf16 through
+// GELU with both forms left in 38.8 us (6.05 TB/s), back in 31.3 (6.23).  Rows that are
+// not aligned are bound by the shifting of what they load and store, 410 instructions
+// per warp and group of 8 at 77 % of the issue slots: 12608 x 3071 bf16 72 and 65 us,
+// 8192 x 4095 packed in 26.8, unpacked in 29.8.  A small matrix is a launch: 197 x 1000
+// fp32 2.1 and 2.4 us.
 #include <algorithm>
 
 #include "novak_ops.cuh"

@@ -6,8 +6,20 @@
 // A row is read once and stays in registers: the deviations are summed after the mean
 // is known.  A thread has eight neighbouring elements at a time and computes on pairs.
 // Rows that are not 16-byte aligned, or not a multiple of 8 elements long, are read and
-// written as the aligned pieces that hold them.  Rows too long for registers have
-// kernels of their own.
+// written as the aligned pieces that hold them.  Rows too long for registers (more than
+// 8192 elements) have kernels of their own.
+//
+// Up to 1024 elements a row is a warp's and needs no barrier; wider ones are 256 or 512
+// threads'.  What bounds them is not bytes but what a row has to wait for, its load, two
+// sums over its threads one after the other, at the occupancy that its registers leave:
+//   forward with the 8-bit form left: 12608 x 768 bf16 12.1 us (4.0 TB/s; without it 10.0),
+//   8000 x 4096 bf16 32.8 (5.0), 4099 x 4096 fp32 29.0 (5.2);
+//   backward: 12608 x 768 bf16 14.6 us (3.3 TB/s; 17.1 when nothing is in L2), 8000 x 4096
+//   bf16 48 (3.4), 4099 x 4096 fp32 from x 43 (4.7), 5 to 6 us of each for the last sums of
+//   dw and db.  (4096 columns: 282 instructions per warp and row at 40 % of the issue
+//   slots; stalls on loads, shuffles, barriers and the load queue in like parts.)
+//   Not aligned: 12608 x 771 bf16 26.8 and 28.2 us.  Long: 2000 x 20000 bf16 123 and 181.
+//   One row of 768: 3.6 us.
 #include <algorithm>
 
 #include "novak_ops.cuh"

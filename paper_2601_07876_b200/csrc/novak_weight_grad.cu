@@ -22,6 +22,14 @@
 // Work: whole tiles as long as every pair gets one; the rows of the tiles that
 // are left over are cut evenly over all pairs, partial tiles going to a
 // workspace that novak_weight_grad_finish_kernel adds up in a fixed order.
+//
+// What bounds it: 16384 x 4096 -> 4096 bf16 takes 469 us (1173 TFLOP/s; 530 where the power
+// limit holds the clock down), the products with every wait but without filling x about
+// 360: a step's 64 rows are 16 KB of dy and 24 KB of codes and x through each SM's shared
+// memory besides the 48 KB that the products read, close to what it can deliver.
+// 12608 x 768 -> 2304 bf16: 46 us (970 TFLOP/s), of which the partial tiles' way through
+// memory takes 5; with db or a layer norm 60, since dy is read once more (sums inside
+// this kernel were 75: they take the shared memory's time too).
 #include <algorithm>
 #include <atomic>
 
@@ -79,7 +87,8 @@ struct FewArgs : WeightGradArgs {
 };
 
 // A 64 x 64 tile per CTA, 4 x 4 products per thread; 32 rows at a time, the next ones
-// on their way while these are worked on.
+// on their way while these are worked on.  One launch and no workspace: bound by latency,
+// 2.9 us for one row of 1024 -> 1024; 32 x 256 -> 256 3.5 and 1.4 more for every 32 rows.
 template <int TYPE>
 __global__ void __launch_bounds__(kPlainThreads) novak_weight_grad_few_kernel(FewArgs a)
 {
@@ -164,6 +173,7 @@ struct Cut {
     int tiles_n, tiles_k;
     int planes;
     int steps;              // of a tile: planes x ceil(rows / 64)
+    int run;                // steps that the tensor cores add up by themselves
     int pairs;              // that run whole tiles
     int waves;              // whole tiles per pair
     int rest;               // tiles left over, after the first waves * pairs
@@ -267,7 +277,8 @@ __device__ __forceinline__ void tile_slots(const Cut &c, int r, int &slot, int &
 // ---- one pass over dy before the products ----------------------------------------------
 // Sums of dy's columns over a part of the rows, for db and for what a layer norm's offset
 // is multiplied with: sums[part][ld] (null: not asked for).  256 columns per CTA, 8 per
-// lane, the warps on rows in turn.
+// lane, the warps on rows in turn.  Bound by HBM: 50432 x 3072 bf16 55 us (5.6 TB/s);
+// 12608 x 2304 13.4 (4.3 TB/s: the start and the end count).
 // COPY: dy as the tensor copies need it too, out[planes][rows][out_ld] in bf16, out_ld a
 // multiple of 8: a copy of a bf16 matrix whose rows are not 16-byte aligned, or the three
 // parts of an fp32 one.  Each part is what is left cut to 8 bits toward zero (so that none
@@ -362,8 +373,6 @@ constexpr int kDySlots = 6, kXSlots = 4, kRawSlots = 4;         // steps of dy, 
 constexpr int kHalf = 64 * kRows * 2;                   // 64 columns of an operand, bf16
 constexpr int kSlotBytes = 2 * kHalf;                   // 128 columns
 constexpr int kRawBytes = 128 * kRows;                  // codes of 128 columns
-constexpr int kRun = 16;        // steps that the tensor cores add up by themselves: their sums round toward
-                                // zero, so that a chain's error grows with its length
 constexpr int kOutWarps = 8, kFillWarps = 8, kFillGroups = 2, kLoadWarps = 4;
 constexpr int kGroupWarps = kFillWarps / kFillGroups;   // that fill a step's x; the groups take turns
 constexpr int kLoadWarp = kOutWarps + kFillWarps, kCopyWarp = kLoadWarp + kLoadWarps, kMmaWarp = kCopyWarp + 1;
@@ -564,7 +573,7 @@ __device__ __forceinline__ void take_out(const KernelArgs &a, Shared &sh, uint32
         float total[128];
 #pragma unroll
         for (int i = 0; i < 128; ++i) total[i] = 0.0f;
-        for (int left = piece.count; left > 0; left -= kRun) {
+        for (int left = piece.count; left > 0; left -= cut.run) {
             const uint32_t buf = n & 1;
             ok = mbar_wait_warp(smem_addr(&sh.out_full[buf]), (n >> 1) & 1);
             if (!ok) {
@@ -580,7 +589,7 @@ __device__ __forceinline__ void take_out(const KernelArgs &a, Shared &sh, uint32
 #pragma unroll
                 for (int i = 0; i < 16; ++i) total[c + i] += v[i];
             }
-            if (left <= kRun) break;            // the last run's columns stay this warp's for a while
+            if (left <= cut.run) break;            // the last run's columns stay this warp's for a while
             tcgen05_before_sync();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(at_rank(smem_addr(&sh.out_empty[buf]), 0));
@@ -763,7 +772,7 @@ novak_weight_grad_kernel(const __grid_constant__ KernelArgs a, const __grid_cons
             Ring<kXSlots> x;
             while (ok && walk.next(piece)) {
                 for (int left = piece.count; ok && left > 0; ++n) {
-                    const int run = min(left, kRun);
+                    const int run = min(left, cut.run);
                     left -= run;
                     const uint32_t buf = n & 1, d = tmem + buf * 256;
                     ok = mbar_wait_warp(smem_addr(&sh.out_empty[buf]), ((n >> 1) & 1) ^ 1);
@@ -816,7 +825,7 @@ struct FinishArgs {
 };
 
 // kFinishRows rows of a tile that was cut per CTA, two groups of four columns of one per
-// thread.
+// thread.  The parts are mostly in L2: 27 tiles from 101 parts (26 MB) take 5 us.
 constexpr int kFinishRows = 8, kFinishCtas = kTileN / kFinishRows;
 __global__ void __launch_bounds__(256) novak_weight_grad_finish_kernel(const __grid_constant__ FinishArgs a)
 {
@@ -915,6 +924,10 @@ Layout layout_for(const Mat &dy, int type, int64_t rows, int64_t n_out, int64_t 
     c.tiles_k = static_cast<int>((n_in + kTileK - 1) / kTileK);
     c.planes = l.planes;
     c.steps = static_cast<int>(l.planes * ((rows + kRows - 1) / kRows));
+    // The tensor cores' sums round toward zero, so that a chain's error grows with its length: it is cut
+    // every 1024 rows, and every 256 products of an fp32 dy, from which more is expected (250 rows in one
+    // chain: 9.6e-7 off, cut 3.1e-7, an fp32 sum 2.8e-7; no slower)
+    c.run = l.planes > 1 ? 4 : 16;
     constexpr int kPairs = 74;          // pairs of SMs
     const int tiles = c.tiles_n * c.tiles_k;
     c.pairs = kPairs;

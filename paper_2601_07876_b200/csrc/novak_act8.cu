@@ -154,6 +154,7 @@ novak_activation_kernel(const typename Elem<TYPE>::T *u, int64_t u_stride, typen
     const int64_t pitch = (p.cols + 31) / 32 * 32;
     const int64_t per_pass = kIsFlat ? 1 : int64_t(kUnroll) << (8 - p.log2);
     const void *end = end_of(u, u_stride, p.rows, p.cols);
+    start();
     for (int64_t row0 = blockIdx.y * per_pass; row0 < (kIsFlat ? 1 : p.rows); row0 += gridDim.y * per_pass) {
         Fetch<TYPE, kIsAligned> raw[kUnroll];
 #pragma unroll
@@ -195,6 +196,7 @@ novak_activation_backward_kernel(const typename Elem<TYPE>::T *da, int64_t da_st
     const int64_t pitch = (p.cols + 31) / 32 * 32;
     const int64_t per_pass = kIsFlat ? 1 : int64_t(kUnroll) << (8 - p.log2);
     const void *da_end = end_of(da, da_stride, p.rows, p.cols), *u_end = end_of(u, u_stride, p.rows, p.cols);
+    start();
     for (int64_t row0 = blockIdx.y * per_pass; row0 < (kIsFlat ? 1 : p.rows); row0 += gridDim.y * per_pass) {
         Fetch<TYPE, kIsAligned> raw[kUnroll], raw_u[FROM8 ? 1 : kUnroll];
         uint2 q[FROM8 ? kUnroll : 1];
@@ -277,8 +279,7 @@ cudaError_t forward(Mat u, Mat a, Codes uc, Codes ac, int64_t rows, int64_t cols
     auto kernel = r == kFlat      ? novak_activation_kernel<KIND, TYPE, kFlat>
                   : r == kAligned ? novak_activation_kernel<KIND, TYPE, kAligned>
                                   : novak_activation_kernel<KIND, TYPE, kAny>;
-    kernel<<<grid, kThreads, 0, stream>>>(static_cast<const T *>(u.ptr), u.stride, static_cast<T *>(a.ptr), a.stride, uc, ac, p);
-    return cudaGetLastError();
+    return launch(kernel, grid, kThreads, 0, stream, static_cast<const T *>(u.ptr), u.stride, static_cast<T *>(a.ptr), a.stride, uc, ac, p);
 }
 
 template <int KIND, int TYPE, bool FROM8>
@@ -291,9 +292,8 @@ cudaError_t backward(Mat da, Mat u, Codes uc, Mat du, int64_t rows, int64_t cols
     auto kernel = r == kFlat      ? novak_activation_backward_kernel<KIND, TYPE, kFlat, FROM8>
                   : r == kAligned ? novak_activation_backward_kernel<KIND, TYPE, kAligned, FROM8>
                                   : novak_activation_backward_kernel<KIND, TYPE, kAny, FROM8>;
-    kernel<<<grid, kThreads, 0, stream>>>(static_cast<const T *>(da.ptr), da.stride, static_cast<const T *>(u.ptr), u.stride, uc,
-                                          static_cast<T *>(du.ptr), du.stride, p);
-    return cudaGetLastError();
+    return launch(kernel, grid, kThreads, 0, stream, static_cast<const T *>(da.ptr), da.stride, static_cast<const T *>(u.ptr),
+                  u.stride, uc, static_cast<T *>(du.ptr), du.stride, p);
 }
 
 template <int KIND>

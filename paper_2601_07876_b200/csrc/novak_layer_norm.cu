@@ -155,6 +155,7 @@ __global__ void __launch_bounds__(32 * forward_warps<G, NV>()) novak_layer_norm_
     const void *end = end_of(static_cast<const T *>(a.x.ptr), a.x.stride, a.rows, cols);
     int n[NV];                  // elements of a group inside the row
     Fetch<TYPE, ALIGNED> raw[NV];
+    start();
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         n[i] = max(min(cols - (i * G + t) * 8, 8), 0);
@@ -230,7 +231,6 @@ novak_layer_norm_back_kernel(NormBackArgs a)
     int turn = 0;
     const int t = G == 32 ? threadIdx.x & 31 : threadIdx.x, sub = G == 32 ? threadIdx.x >> 5 : 0;
     constexpr int kWarps = backward_warps<G, NV>(), kSubs = G == 32 ? kWarps : 1;
-    asm volatile("griddepcontrol.launch_dependents;");
     const int cols = static_cast<int>(a.cols), pitch = (cols + 31) / 32 * 32;
     const int64_t step = static_cast<int64_t>(gridDim.x) * kSubs;
     const float inv_cols = 1.0f / static_cast<float>(cols);
@@ -275,6 +275,7 @@ novak_layer_norm_back_kernel(NormBackArgs a)
             raw_x[i].zero();
         }
     }
+    start();
     fetch(row);
     Held<G, NV> weight;
     weight.load(a.weight, a.param_type, cols, held);
@@ -375,6 +376,7 @@ __global__ void __launch_bounds__(kThreads) novak_layer_norm_long_kernel(NormArg
 {
     using T = typename Elem<TYPE>::T;
     __shared__ float scratch[33];
+    start();
     const int64_t pitch = (a.cols + 31) / 32 * 32;
     const float inv_cols = 1.0f / static_cast<float>(a.cols);
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
@@ -443,6 +445,7 @@ __global__ void __launch_bounds__(kThreads) novak_layer_norm_back_long_kernel(No
 {
     using T = typename Elem<TYPE>::T;
     __shared__ float scratch[33];
+    start();
     const int64_t pitch = (a.cols + 31) / 32 * 32;
     const float inv_cols = 1.0f / static_cast<float>(a.cols);
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
@@ -482,6 +485,7 @@ __global__ void __launch_bounds__(kThreads) novak_layer_norm_columns_kernel(Norm
 {
     using T = typename Elem<TYPE>::T;
     __shared__ float part[2][kThreads / 4][kColsPerCta + 1];
+    start();
     const int64_t pitch = (a.cols + 31) / 32 * 32;
     const int quad = threadIdx.x & 3, lane = threadIdx.x >> 2;
     const int64_t c = static_cast<int64_t>(blockIdx.x) * kColsPerCta + quad * 8;
@@ -520,7 +524,7 @@ __global__ void __launch_bounds__(kFinishThreads)
 novak_layer_norm_finish_kernel(const float *work, int64_t splits, int64_t cols, void *dweight, void *dbias, int type)
 {
     __shared__ float part[32][33];
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    start();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, which = blockIdx.y;
     const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + lane;
     void *out = which ? dbias : dweight;
@@ -584,8 +588,7 @@ cudaError_t run(Kernel kernel, int64_t grid, int threads, int smem, const Args &
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         if (e != cudaSuccess) return e;
     }
-    kernel<<<static_cast<unsigned>(grid), threads, smem, stream>>>(a);
-    return cudaGetLastError();
+    return launch(kernel, dim3(static_cast<unsigned>(grid)), threads, smem, stream, a);
 }
 
 template <int TYPE> cudaError_t forward(const NormArgs &a, const Spread &s, bool aligned, cudaStream_t stream)
@@ -628,8 +631,7 @@ cudaError_t launch_layer_norm(const NormArgs &a, cudaStream_t stream)
     auto kernel = a.type == NOVAK_TYPE_F32
                       ? (w ? novak_layer_norm_long_kernel<0, true> : novak_layer_norm_long_kernel<0, false>)
                       : (w ? novak_layer_norm_long_kernel<1, true> : novak_layer_norm_long_kernel<1, false>);
-    kernel<<<grid, kThreads, 0, stream>>>(a);
-    return cudaGetLastError();
+    return launch(kernel, dim3(static_cast<unsigned>(grid)), kThreads, 0, stream, a);
 }
 
 // Enough for either way of the backward pass: which one it is depends on alignment.
@@ -663,28 +665,17 @@ cudaError_t launch_layer_norm_backward(const NormBackArgs &a, cudaStream_t strea
             auto columns = t == 0 ? (w ? novak_layer_norm_columns_kernel<0, true> : novak_layer_norm_columns_kernel<0, false>)
                                   : (w ? novak_layer_norm_columns_kernel<1, true> : novak_layer_norm_columns_kernel<1, false>);
             const dim3 grid(static_cast<unsigned>((a.cols + kColsPerCta - 1) / kColsPerCta), static_cast<unsigned>(splits));
-            columns<<<grid, kThreads, 0, stream>>>(a);
+            const cudaError_t e = launch(columns, grid, kThreads, 0, stream, a);
+            if (e != cudaSuccess) return e;
         }
         auto kernel = t == 0 ? (w ? novak_layer_norm_back_long_kernel<0, true> : novak_layer_norm_back_long_kernel<0, false>)
                              : (w ? novak_layer_norm_back_long_kernel<1, true> : novak_layer_norm_back_long_kernel<1, false>);
-        kernel<<<static_cast<int>(std::min<int64_t>(a.rows, kSms * 8)), kThreads, 0, stream>>>(a);
-    }
-    if (sums) {
-        // its CTAs may come to be while the last rows are worked on, and wait for them
-        cudaLaunchConfig_t lc = {};
-        lc.gridDim = dim3(static_cast<unsigned>((a.cols + 31) / 32), 2);
-        lc.blockDim = dim3(kFinishThreads);
-        lc.stream = stream;
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[0].val.programmaticStreamSerializationAllowed = 1;
-        lc.attrs = attr;
-        lc.numAttrs = a.rows > 0 ? 1 : 0;
-        const cudaError_t e = cudaLaunchKernelEx(&lc, novak_layer_norm_finish_kernel, static_cast<const float *>(a.work), splits, a.cols,
-                                                 a.dweight, a.dbias, a.grad_type);
+        const cudaError_t e = launch(kernel, dim3(static_cast<unsigned>(std::min<int64_t>(a.rows, kSms * 8))), kThreads, 0, stream, a);
         if (e != cudaSuccess) return e;
     }
-    return cudaGetLastError();
+    if (!sums) return cudaSuccess;
+    return launch(novak_layer_norm_finish_kernel, dim3(static_cast<unsigned>((a.cols + 31) / 32), 2), kFinishThreads, 0, stream,
+                  static_cast<const float *>(a.work), splits, a.cols, a.dweight, a.dbias, a.grad_type);
 }
 
 }  // namespace novak

@@ -9,6 +9,34 @@
 
 namespace novak {
 
+// The operators' kernels are launched with programmatic stream serialization: a kernel's
+// CTAs come to be, and set up what is theirs alone, while the kernel before drains (packing
+// and unpacking 8192 x 4096 bf16 in a row: 32.3 us, 34.8 with plain launches; layer norm of
+// 12608 x 768 and unpacking its form: 19.3 and 22.5).  Each of them starts with this: it
+// waits for the kernel before, and only then lets the next one come.  The other way round
+// the one after the next could start while what came before this one is still at work.
+__device__ __forceinline__ void start()
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+template <typename... Params, typename... Args>
+cudaError_t launch(void (*kernel)(Params...), dim3 grid, int threads, int smem, cudaStream_t stream, Args... args)
+{
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = grid;
+    lc.blockDim = dim3(static_cast<unsigned>(threads));
+    lc.dynamicSmemBytes = static_cast<size_t>(smem);
+    lc.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = attr;
+    lc.numAttrs = 1;
+    return cudaLaunchKernelEx(&lc, kernel, static_cast<Params>(args)...);
+}
+
 template <int TYPE> struct Elem;
 template <> struct Elem<NOVAK_TYPE_F32> { using T = float; };
 template <> struct Elem<NOVAK_TYPE_BF16> { using T = __nv_bfloat16; };

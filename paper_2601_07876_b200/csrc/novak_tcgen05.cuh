@@ -166,11 +166,6 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap *map)
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
 
-// Programmatic dependent launch: what follows sees everything that the kernels before
-// have written; nothing before it may touch memory that they use.
-__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void grid_launch_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-
 // ---- one warp's own tensor instructions (for sums over few columns) ----------------
 // Four 8 x 8 bf16 matrices, transposed: lane i has the address of row i % 8 of matrix i / 8.
 __device__ __forceinline__ void load_transposed(uint32_t addr, uint32_t (&r)[4])

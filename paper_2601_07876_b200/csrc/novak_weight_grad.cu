@@ -121,6 +121,7 @@ __global__ void __launch_bounds__(kPlainThreads) novak_weight_grad_few_kernel(Fe
         }
     };
     float acc[4][4] = {}, sum[4] = {};
+    start();
     fetch(0);
     for (int t0 = 0, buf = 0; t0 < rows; t0 += kDepth, buf ^= 1) {
 #pragma unroll
@@ -292,8 +293,7 @@ novak_weight_grad_sums_kernel(const typename Elem<TYPE>::T *dy, int64_t stride, 
                               int64_t cols, int64_t rows_per_part, __nv_bfloat16 *out, int64_t out_ld)
 {
     __shared__ float part[8][256];
-    grid_wait();
-    grid_launch_next();
+    start();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int64_t col = (static_cast<int64_t>(blockIdx.x) * 32 + lane) * 8;
     const int64_t row0 = blockIdx.y * rows_per_part, row1 = min(row0 + rows_per_part, rows);
@@ -701,8 +701,7 @@ novak_weight_grad_kernel(const __grid_constant__ KernelArgs a, const __grid_cons
     cluster_sync();
     tcgen05_after_sync();
     const uint32_t tmem = sh.tmem;
-    grid_launch_next();
-    grid_wait();
+    start();
 
     // (every warp of a warpgroup executes the same one of the two)
     if (warp < kOutWarps) registers_up<kOutRegs>();
@@ -832,7 +831,7 @@ __global__ void __launch_bounds__(256) novak_weight_grad_finish_kernel(const __g
     __shared__ float total[kFinishRows], part[32][kFinishRows + 1];
     __shared__ float turn[kFinishRows][kTileK + 4];
     const Cut &cut = a.cut;
-    grid_wait();
+    start();
     const int group = blockIdx.x % kFinishCtas, item = blockIdx.x / kFinishCtas;
     int tn, tk, slot, n;
     tile_at(cut, cut.waves * cut.pairs + item, tn, tk);
@@ -971,24 +970,6 @@ EncodeTiled encoder()
     return fn;
 }
 
-// Launches with programmatic stream serialization: the kernel's CTAs may come to be, and
-// set up what is theirs alone, while the one before still runs.
-template <typename... Params, typename... Args>
-cudaError_t launch(void (*kernel)(Params...), dim3 grid, int threads, int smem, cudaStream_t stream, Args... args)
-{
-    cudaLaunchConfig_t lc = {};
-    lc.gridDim = grid;
-    lc.blockDim = dim3(static_cast<unsigned>(threads));
-    lc.dynamicSmemBytes = static_cast<size_t>(smem);
-    lc.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    lc.attrs = attr;
-    lc.numAttrs = 1;
-    return cudaLaunchKernelEx(&lc, kernel, static_cast<Params>(args)...);
-}
-
 template <int TYPE, bool ALIGNED>
 cudaError_t launch_sums(const WeightGradArgs &a, const Layout &l, float *sums, __nv_bfloat16 *out, cudaStream_t stream)
 {
@@ -1021,9 +1002,8 @@ cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t stream)
         const dim3 grid(static_cast<unsigned>((a.n_in + kTile - 1) / kTile),
                         static_cast<unsigned>((a.n_out + kTile - 1) / kTile));
         const FewArgs f{a, vector};
-        if (a.type == NOVAK_TYPE_F32) novak_weight_grad_few_kernel<0><<<grid, kPlainThreads, 0, stream>>>(f);
-        else novak_weight_grad_few_kernel<1><<<grid, kPlainThreads, 0, stream>>>(f);
-        return cudaGetLastError();
+        return launch(a.type == NOVAK_TYPE_F32 ? novak_weight_grad_few_kernel<0> : novak_weight_grad_few_kernel<1>, grid,
+                      kPlainThreads, 0, stream, f);
     }
     const Layout l = layout_for(a.dy, a.type, a.rows, a.n_out, a.n_in);
     uint8_t *work = static_cast<uint8_t *>(a.work);

@@ -14,7 +14,7 @@
 // sums over its threads one after the other, at the occupancy that its registers leave:
 //   forward with the 8-bit form left: 12608 x 768 bf16 12.1 us (4.0 TB/s; without it 10.0),
 //   8000 x 4096 bf16 32.8 (5.0), 4099 x 4096 fp32 29.0 (5.2);
-//   backward: 12608 x 768 bf16 14.6 us (3.3 TB/s; 17.1 when nothing is in L2), 8000 x 4096
+//   backward: 12608 x 768 bf16 13.0 us (3.7 TB/s; 16.9 when nothing is in L2), 8000 x 4096
 //   bf16 48 (3.4), 4099 x 4096 fp32 from x 43 (4.7), 5 to 6 us of each for the last sums of
 //   dw and db.  (4096 columns: 282 instructions per warp and row at 40 % of the issue
 //   slots; stalls on loads, shuffles, barriers and the load queue in like parts.)
@@ -85,11 +85,13 @@ __device__ __forceinline__ void row_sums(float (&x)[N], float *scratch, int &tur
 }
 
 // Warps per CTA: where a row is a warp's (G = 32), what the registers of a row of NV
-// groups of 8 elements per lane leave room for.
+// groups of 8 elements per lane leave room for (backward of 12608 x 768: 12 warps, which
+// spill, 14.4 us in bf16 and 22.6 in fp32; 8 warps 13.0 and 17.3; two rows ahead of 8
+// warps 12.6 and 17.3, of 12 warps 20 and 36).
 template <int G, int NV> __host__ __device__ constexpr int forward_warps() { return G == 32 ? 8 : G / 32; }
 template <int G, int NV> __host__ __device__ constexpr int backward_warps()
 {
-    return G == 32 ? (NV <= 2 ? 16 : NV == 3 ? 12 : 8) : G / 32;
+    return G == 32 ? (NV <= 2 ? 16 : 8) : G / 32;
 }
 
 // A thread's columns of a vector that every row needs.  Where a row is a warp's, the

@@ -32,18 +32,6 @@ constexpr int kSplitRows = 128;      // rows per partial sum of a column (long r
 constexpr int kColsPerCta = 32;
 constexpr int kSms = 148;
 
-__device__ __forceinline__ float param_at(const void *p, int type, int64_t i)
-{
-    return type == NOVAK_TYPE_F32 ? static_cast<const float *>(p)[i]
-                                  : to_float(static_cast<const __nv_bfloat16 *>(p)[i]);
-}
-
-__device__ __forceinline__ void store_param(void *p, int type, int64_t i, float v)
-{
-    if (type == NOVAK_TYPE_F32) static_cast<float *>(p)[i] = v;
-    else static_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(v);
-}
-
 // Puts the 8-bit form of a thread's eight elements at `col` of `row` away; every thread
 // of the warp has to be here, with zeros beyond the row's elements.  ALL: the eight are
 // NaNs together or not at all.

@@ -43,11 +43,16 @@ template <> struct Elem<NOVAK_TYPE_BF16> { using T = __nv_bfloat16; };
 
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
-template <typename T> __device__ __forceinline__ T from_float(float x);
-template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
-template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x)
+// Element i of a vector of either type.
+__device__ __forceinline__ float param_at(const void *p, int type, int64_t i)
 {
-    return __float2bfloat16_rn(x);
+    return type == NOVAK_TYPE_F32 ? static_cast<const float *>(p)[i]
+                                  : to_float(static_cast<const __nv_bfloat16 *>(p)[i]);
+}
+__device__ __forceinline__ void store_param(void *p, int type, int64_t i, float v)
+{
+    if (type == NOVAK_TYPE_F32) static_cast<float *>(p)[i] = v;
+    else static_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(v);
 }
 
 // Two fp32 numbers per instruction.

@@ -166,21 +166,6 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap *map)
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
 
-// ---- one warp's own tensor instructions (for sums over few columns) ----------------
-// Four 8 x 8 bf16 matrices, transposed: lane i has the address of row i % 8 of matrix i / 8.
-__device__ __forceinline__ void load_transposed(uint32_t addr, uint32_t (&r)[4])
-{
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-}
-// d (16 x 8) += a (16 x 16) times ones: each of d's columns gets a's row sums.
-__device__ __forceinline__ void add_row_sums(float (&d)[4], const uint32_t (&a)[4])
-{
-    const uint32_t ones = 0x3f803f80u;
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %8}, {%0, %1, %2, %3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(ones));
-}
-
 // 16 consecutive columns of this warp's 32 lanes: thread i gets lane i's.
 __device__ __forceinline__ void tmem_load16(uint32_t tmem, float (&v)[16])
 {

@@ -39,18 +39,6 @@
 namespace novak {
 namespace {
 
-__device__ __forceinline__ float param_at(const void *p, int type, int64_t i)
-{
-    return type == NOVAK_TYPE_F32 ? static_cast<const float *>(p)[i]
-                                  : to_float(static_cast<const __nv_bfloat16 *>(p)[i]);
-}
-
-__device__ __forceinline__ void store_param(void *p, int type, int64_t i, float v)
-{
-    if (type == NOVAK_TYPE_F32) static_cast<float *>(p)[i] = v;
-    else static_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(v);
-}
-
 // Four neighbouring elements of dW's row, column k on.
 template <typename Args>
 __device__ __forceinline__ void store_four(const Args &a, int64_t at, int64_t k, float x0, float x1, float x2, float x3)

@@ -72,6 +72,7 @@ constexpr int kTile = 64, kDepth = 32, kPlainThreads = 256;
 
 struct FewArgs : WeightGradArgs {
     int vector;
+    unsigned tiles_k;       // (the grid's second dimension would not hold all of n_out's)
 };
 
 // A 64 x 64 tile per CTA, 4 x 4 products per thread; 32 rows at a time, the next ones
@@ -84,7 +85,8 @@ __global__ void __launch_bounds__(kPlainThreads) novak_weight_grad_few_kernel(Fe
     __shared__ __align__(16) float sdy[2][kDepth][kTile], sx[2][kDepth][kTile];
     constexpr int kEach = kDepth * kTile / kPlainThreads, kStep = kPlainThreads / kTile;
     const int64_t pitch = (a.n_in + 31) / 32 * 32;
-    const int64_t n0 = static_cast<int64_t>(blockIdx.y) * kTile, k0 = static_cast<int64_t>(blockIdx.x) * kTile;
+    const unsigned tile_n = blockIdx.x / a.tiles_k, tile_k = blockIdx.x - tile_n * a.tiles_k;
+    const int64_t n0 = static_cast<int64_t>(tile_n) * kTile, k0 = static_cast<int64_t>(tile_k) * kTile;
     const int ty = threadIdx.x / 16, tx = threadIdx.x % 16, rows = static_cast<int>(a.rows);
     // what a thread brings: dy's column n0 + cn of every fourth row; 8 codes of a row
     static_assert(kDepth * kTile / 8 == kPlainThreads, "eight codes each");
@@ -142,7 +144,7 @@ __global__ void __launch_bounds__(kPlainThreads) novak_weight_grad_few_kernel(Fe
     for (int i = 0; i < 4; ++i) {
         const int64_t n = n0 + ty * 4 + i;
         if (n >= a.n_out) continue;
-        if (a.db && blockIdx.x == 0 && tx == 0) store_param(a.db, a.grad_type, n, sum[i]);
+        if (a.db && tile_k == 0 && tx == 0) store_param(a.db, a.grad_type, n, sum[i]);
         if (k >= a.n_in) continue;
         float *x = acc[i];
         if (a.weight)
@@ -987,9 +989,9 @@ cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t stream)
 {
     const int vector = a.n_in % 4 == 0 && reinterpret_cast<uintptr_t>(a.dw) % (a.grad_type == NOVAK_TYPE_F32 ? 16 : 8) == 0;
     if (little(a.rows, a.n_out, a.n_in)) {
-        const dim3 grid(static_cast<unsigned>((a.n_in + kTile - 1) / kTile),
-                        static_cast<unsigned>((a.n_out + kTile - 1) / kTile));
-        const FewArgs f{a, vector};
+        const int64_t tiles_k = (a.n_in + kTile - 1) / kTile, tiles = tiles_k * ((a.n_out + kTile - 1) / kTile);
+        const dim3 grid(static_cast<unsigned>(tiles));      // (below 2^31: dW has 4096 elements for each)
+        const FewArgs f{a, vector, static_cast<unsigned>(tiles_k)};
         return launch(a.type == NOVAK_TYPE_F32 ? novak_weight_grad_few_kernel<0> : novak_weight_grad_few_kernel<1>, grid,
                       kPlainThreads, 0, stream, f);
     }

@@ -99,3 +99,10 @@ def test_bad_values_keep_to_their_columns_in_the_tensor_cores(ops):
     assert torch.isnan(dw[:, 32:64]).all() and torch.equal(db, sums)
     keep = [i for i in range(n_in) if not 32 <= i < 64]
     assert torch.equal(dw[:, keep], clean[:, keep])
+
+
+@pytest.mark.parametrize("rows,n_in,n_out", [(3, 8, 1 << 22), (200, 8, 1 << 22), (3, 1 << 22, 8), (200, 1 << 22, 8)])
+def test_the_widest_matrices(ops, rows, n_in, n_out):
+    dy, x = whole(rows, n_in, n_out, 4)
+    dw, db = ops.linear_weight_grad(dy.to(BF16), ops.act8_pack(x))
+    assert torch.equal(dw, dy.t() @ x) and torch.equal(db, dy.sum(0))        # (whole numbers: exact in fp32 too)

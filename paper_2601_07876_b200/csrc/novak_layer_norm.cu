@@ -93,8 +93,9 @@ template <int G, int NV> struct Held {
         for (int i = 0; i < NV; ++i) {
             const int col = (i * G + static_cast<int>(threadIdx.x)) * 8;
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                r[i][k] = p && col < cols ? F2(param_at(p, type, col + 2 * k), param_at(p, type, col + 2 * k + 1)) : F2(0.0f);
+            for (int k = 0; k < 4; ++k)         // (the row's end may cut a group: nothing is read beyond it)
+                r[i][k] = F2(p && col + 2 * k < cols ? param_at(p, type, col + 2 * k) : 0.0f,
+                             p && col + 2 * k + 1 < cols ? param_at(p, type, col + 2 * k + 1) : 0.0f);
         }
     }
     __device__ __forceinline__ void get(int i, F2 (&v)[4]) const

@@ -1,0 +1,45 @@
+"""The training operators where memory ends and numbers do: what stands behind their vectors, infinities, sums that
+overflow."""
+import math
+
+import pytest
+import torch
+
+import ops_reference as R
+from test_gpu_ops import BF16, F32, TYPES, check_layer_norm, gen, matrix
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ops():
+    from paper_2601_07876_b200 import ops
+    return ops
+
+
+# ---- what stands behind a vector --------------------------------------------------
+def slice_of_nans(n, dtype, offset, values):
+    """A vector of these values, NaNs before and behind it."""
+    buf = torch.full((offset + n + 64,), math.nan, dtype=dtype, device="cuda")
+    buf[offset:offset + n] = values.to(dtype)
+    return buf[offset:offset + n]
+
+
+@pytest.mark.parametrize("param", TYPES)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [7, 96, 257, 771, 1001, 1031, 2048, 4099, 8190, 20001])
+def test_nothing_behind_weight_and_bias_is_read(ops, cols, dtype, param):
+    rows, g = 9, gen(cols)
+    x, dy = matrix(rows, cols, dtype, cols), matrix(rows, cols, dtype, cols + 1, scale=1e-3)
+    values, shift = 1 + 0.2 * torch.randn(cols, generator=g), torch.randn(cols, generator=g)
+    for offset in (0, 1):
+        w, b = slice_of_nans(cols, param, offset, values), slice_of_nans(cols, param, offset, shift)
+        y, mean, rstd, kept = ops.layer_norm(x, w, b, checkpoint=True)
+        check_layer_norm(ops, x, w, b, 1e-5, y, mean, rstd, kept)
+        from_x = (x.cpu().double() - mean.cpu().double()[:, None]) * rstd.cpu().double()[:, None]
+        for saved, ref, err in ((kept, R.act8_values(kept.codes, kept.exps, cols), 0.0), (x, from_x, 3 * R.U)):
+            got = ops.layer_norm_backward(dy, saved, rstd, w, mean=mean)
+            want = R.layer_norm_backward(dy, ref, rstd, w)
+            bounds = R.layer_norm_backward_bounds(dy, ref, rstd, w, dtype, F32, err)
+            for a, c, bound, what in zip(got, want, bounds, ("dx", "dw", "db")):
+                R.assert_within(a, c, bound, what)

@@ -218,6 +218,8 @@ PyObject *unpack(PyObject *const *args)
     const Tensor &out = tensor(args[1], "out");
     const int64_t cols = attribute(args[0], names.cols), rows = attribute(args[0], names.rows);
     const Form f = form_of(args[0], rows, cols, out, "out");
+    if (cols < 1 || !out.is_contiguous() || out.numel() / cols != rows || out.numel() % cols != 0)
+        value_error("%s must be contiguous and hold the 8-bit form's elements", "out");
     ENQUEUE(novak_act8_unpack, out, f.codes, f.exps, out.data_ptr(), cols, type_of(out, "dtype"), rows, cols);
     Py_RETURN_NONE;
 }

@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes
 import importlib.machinery
 import importlib.util
+import math
 
 import torch
 
@@ -65,6 +66,9 @@ class Act8:
         if cols < 1 or pitch != (cols + BLOCK - 1) // BLOCK * BLOCK or exps.shape != (rows, pitch // BLOCK):
             raise ValueError(f"no 8-bit form of rows of {cols} elements: codes {tuple(codes.shape)}, "
                              f"exps {tuple(exps.shape)}")
+        shape = (rows, cols) if shape is None else tuple(shape)
+        if not shape or shape[-1] != cols or math.prod(shape[:-1]) != rows:
+            raise ValueError(f"shape {shape} does not fold into {rows} rows of {cols} elements")
         index = codes.get_device()
         if not codes.is_contiguous() or not exps.is_contiguous() or index < 0 or exps.get_device() != index:
             raise ValueError("codes and exps must be contiguous CUDA tensors of one device")
@@ -72,7 +76,7 @@ class Act8:
         if self.codes_ptr % 32 and rows:
             raise ValueError("codes must be 32-byte aligned")
         self._codes, self._exps, self._both, self.rows, self.cols, self.index = codes, exps, None, rows, cols, index
-        self.shape = (rows, cols) if shape is None else tuple(shape)
+        self.shape = shape
 
     @classmethod
     def _of(cls, both, cols: int, shape):

@@ -43,3 +43,14 @@ def test_nothing_behind_weight_and_bias_is_read(ops, cols, dtype, param):
             bounds = R.layer_norm_backward_bounds(dy, ref, rstd, w, dtype, F32, err)
             for a, c, bound, what in zip(got, want, bounds, ("dx", "dw", "db")):
                 R.assert_within(a, c, bound, what)
+
+
+# ---- a form's shape ---------------------------------------------------------------
+def test_unpacking_writes_nothing_but_the_forms_elements(ops):
+    kept = ops.act8_pack(matrix(300, 64, F32, 1))
+    again = ops.Act8(kept.codes, kept.exps, 64, shape=(3, 100, 64))
+    assert torch.equal(ops.act8_unpack(again).view(300, 64), ops.act8_unpack(kept))
+    for out in (torch.zeros(1, 64, device="cuda"), torch.zeros(64, 300, device="cuda").t(), torch.zeros(301, 64, device="cuda")):
+        with pytest.raises(ValueError, match="elements"):
+            ops._calls.unpack(kept, out)
+        assert not out.any()

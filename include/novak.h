@@ -744,11 +744,23 @@ int novak_linear_weight_grad(const void *d_dy, int64_t dy_stride, int type, cons
 
 /* The weight gradient's kernel has warps that wait for one another's copies and
  * products.  Each wait is bounded (two seconds); where one runs out, which is a
- * fault of this library or of the device, the part of dW that it was for is
- * filled with NaNs and *count, the number of such waits on the current device
- * since the library was loaded, goes up.  Copies 4 bytes from the device and
- * SYNCHRONISES `stream`. */
+ * fault of this library or of the device, all of dW that the two SMs at work
+ * there had not yet finished is filled with NaNs (db is formed elsewhere and
+ * stays right) and *count, the number of warps whose wait for a part of dW ran
+ * out on the current device since the library was loaded, goes up.  Copies 4
+ * bytes from the device and SYNCHRONISES `stream`. */
 int novak_ops_gave_up(unsigned *count, void *stream);
+
+/* Test hook for those waits: novak_linear_weight_grad with a limit of wait_ns on
+ * each (0: the usual one; the clock is looked at every 64 ms or so), and with the word
+ * left out that tells the warps which store dW that the first sum of pair `pair`
+ * of SMs is complete (their wait runs out, and so do those that depend on it).
+ * NOVAK_EINVAL where fewer pairs are at work; with few rows none are. */
+int novak_selftest_weight_grad_wait(const void *d_dy, int64_t dy_stride, int type, const int8_t *d_codes,
+                                    const uint8_t *d_exps, const void *d_weight, const void *d_bias,
+                                    int param_type, void *d_dw, void *d_db, int grad_type, void *d_work,
+                                    size_t work_bytes, int64_t rows, int64_t n_out, int64_t n_in, int pair,
+                                    uint64_t wait_ns, void *stream);
 
 /* Text of the last error of a training operator on the calling thread ("" if
  * none).  Valid until the thread's next such call. */

@@ -83,7 +83,7 @@ class NovakError(RuntimeError):
 
 _lib = None
 _OPTIONAL_ELSEWHERE = ("novak_build_", "novak_act8_", "novak_layer_norm", "novak_activation",
-                       "novak_linear_weight_grad", "novak_ops_")
+                       "novak_linear_weight_grad", "novak_ops_", "novak_selftest_weight_grad")
 
 
 def load_library(path: str | None = None) -> ctypes.CDLL:
@@ -161,6 +161,8 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
         "novak_linear_weight_grad_bytes": (c_size_t, [vp, c_int64, c_int, c_int64, c_int64, c_int64]),
         "novak_linear_weight_grad": (c_int, [vp, c_int64, c_int, vp, vp, vp, vp, c_int, vp, vp, c_int,
                                              vp, c_size_t, c_int64, c_int64, c_int64, vp]),
+        "novak_selftest_weight_grad_wait": (c_int, [vp, c_int64, c_int, vp, vp, vp, vp, c_int, vp, vp, c_int,
+                                                    vp, c_size_t, c_int64, c_int64, c_int64, c_int, c_uint64, vp]),
         "novak_ops_gave_up": (c_int, [POINTER(c_uint32), vp]),
         "novak_ops_error": (c_char_p, []),
     }

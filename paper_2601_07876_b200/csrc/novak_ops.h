@@ -79,7 +79,11 @@ struct WeightGradArgs {
     int grad_type;
     void *work;
     int64_t rows, n_out, n_in;     // rows may be 0
+    uint64_t wait_ns = 0;          // a wait's limit; 0: the usual one
+    int withheld = -1;             // pair of SMs whose first sum is not announced (a test of the limit)
 };
+// Pairs of SMs that work on it; 0: the ordinary cores do, and wait for nothing.
+int weight_grad_pairs(const Mat &dy, int type, int64_t rows, int64_t n_out, int64_t n_in);
 size_t weight_grad_bytes(const Mat &dy, int type, int64_t rows, int64_t n_out, int64_t n_in);
 cudaError_t weight_grad_gave_up(unsigned *count, cudaStream_t stream);
 cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t stream);

@@ -84,13 +84,36 @@ int check_floats(const char *name, const float *p)
 Mat mat(const void *p, int64_t stride) { return Mat{const_cast<void *>(p), stride}; }
 Codes form(const int8_t *c, const uint8_t *e) { return Codes{const_cast<int8_t *>(c), const_cast<uint8_t *>(e)}; }
 
-}  // namespace
-
 #define CHECK(call)                         \
     do {                                    \
         const int check_rc = (call);        \
         if (check_rc != NOVAK_OK) return check_rc; \
     } while (0)
+
+int check_weight_grad(const WeightGradArgs &a, size_t work_bytes)
+{
+    if (!is_type(a.type)) return refuse("bad type");
+    CHECK(check_shape(a.rows, a.n_out));
+    CHECK(check_shape(a.rows, a.n_in));
+    CHECK(check_shape(a.n_out, a.n_in));
+    if (a.rows > INT32_MAX || a.n_out > (1 << 22) || a.n_in > (1 << 22) || a.n_out < 1)
+        return refuse("sizes of up to 2^31 - 1 rows and 2^22 inputs and outputs are taken");
+    CHECK(check_mat("dy", a.dy, a.type, a.rows, a.n_out));
+    CHECK(check_codes("x", a.codes, a.rows, true));
+    if ((a.weight != nullptr) != (a.bias != nullptr)) return refuse("the norm's weight and bias come together");
+    if (a.weight) {
+        CHECK(check_vector("weight", a.weight, a.param_type));
+        CHECK(check_vector("bias", a.bias, a.param_type));
+    }
+    CHECK(check_vector("dw", a.dw, a.grad_type));
+    if (a.db) CHECK(check_vector("db", a.db, a.grad_type));
+    const size_t need = weight_grad_bytes(a.dy, a.type, a.rows, a.n_out, a.n_in);
+    if (need > 0 && (!a.work || work_bytes < need || (reinterpret_cast<uintptr_t>(a.work) & 255u)))
+        return refuse("work: %zu bytes, 256-byte aligned, are needed", need);
+    return NOVAK_OK;
+}
+
+}  // namespace
 
 extern "C" {
 
@@ -240,29 +263,24 @@ int novak_linear_weight_grad(const void *d_dy, int64_t dy_stride, int type, cons
                              size_t work_bytes, int64_t rows, int64_t n_out, int64_t n_in,
                              void *stream)
 {
-    if (!is_type(type)) return refuse("bad type");
-    CHECK(check_shape(rows, n_out));
-    CHECK(check_shape(rows, n_in));
-    CHECK(check_shape(n_out, n_in));
-    if (rows > INT32_MAX || n_out > (1 << 22) || n_in > (1 << 22) || n_out < 1)
-        return refuse("sizes of up to 2^31 - 1 rows and 2^22 inputs and outputs are taken");
-    CHECK(check_mat("dy", mat(d_dy, dy_stride), type, rows, n_out));
-    CHECK(check_codes("x", form(d_codes, d_exps), rows, true));
-    if ((d_weight != nullptr) != (d_bias != nullptr)) return refuse("the norm's weight and bias come together");
-    if (d_weight) {
-        CHECK(check_vector("weight", d_weight, param_type));
-        CHECK(check_vector("bias", d_bias, param_type));
-    }
-    CHECK(check_vector("dw", d_dw, grad_type));
-    if (d_db) CHECK(check_vector("db", d_db, grad_type));
-    const Mat dy = mat(d_dy, dy_stride);
-    const size_t need = weight_grad_bytes(dy, type, rows, n_out, n_in);
-    if (need > 0 && (!d_work || work_bytes < need || (reinterpret_cast<uintptr_t>(d_work) & 255u)))
-        return refuse("work: %zu bytes, 256-byte aligned, are needed", need);
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const WeightGradArgs a{dy, type, form(d_codes, d_exps), d_weight, d_bias, param_type, d_dw, d_db, grad_type,
-                           d_work, rows, n_out, n_in};
-    return finish(launch_weight_grad(a, s), "novak_linear_weight_grad");
+    const WeightGradArgs a{mat(d_dy, dy_stride), type, form(d_codes, d_exps), d_weight, d_bias, param_type, d_dw, d_db,
+                           grad_type, d_work, rows, n_out, n_in};
+    CHECK(check_weight_grad(a, work_bytes));
+    return finish(launch_weight_grad(a, static_cast<cudaStream_t>(stream)), "novak_linear_weight_grad");
+}
+
+int novak_selftest_weight_grad_wait(const void *d_dy, int64_t dy_stride, int type, const int8_t *d_codes,
+                                    const uint8_t *d_exps, const void *d_weight, const void *d_bias,
+                                    int param_type, void *d_dw, void *d_db, int grad_type, void *d_work,
+                                    size_t work_bytes, int64_t rows, int64_t n_out, int64_t n_in, int pair,
+                                    uint64_t wait_ns, void *stream)
+{
+    const WeightGradArgs a{mat(d_dy, dy_stride), type, form(d_codes, d_exps), d_weight, d_bias, param_type, d_dw, d_db,
+                           grad_type, d_work, rows, n_out, n_in, wait_ns, pair};
+    CHECK(check_weight_grad(a, work_bytes));
+    const int pairs = weight_grad_pairs(a.dy, type, rows, n_out, n_in);
+    if (pair < 0 || pair >= pairs) return refuse("pair %d of %d", pair, pairs);
+    return finish(launch_weight_grad(a, static_cast<cudaStream_t>(stream)), "novak_selftest_weight_grad_wait");
 }
 
 }  // extern "C"

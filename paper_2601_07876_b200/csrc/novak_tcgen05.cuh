@@ -75,7 +75,7 @@ __device__ __forceinline__ uint64_t global_ns()
     return t;
 }
 
-constexpr uint64_t kWaitNs = 2000000000ull;     // a wait gives up after two seconds
+constexpr uint64_t kWaitNs = 2000000000ull;     // a wait gives up after two seconds unless told otherwise
 
 // Sleeps until the phase of this parity is complete, a millisecond at most.
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
@@ -89,7 +89,7 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
 }
 
 // (The clock is slow to read: only a wait that has gone wrong looks at it.)
-__device__ __forceinline__ bool mbar_wait_long(uint32_t bar, uint32_t parity)
+__device__ __forceinline__ bool mbar_wait_long(uint32_t bar, uint32_t parity, uint64_t limit)
 {
     uint64_t t0 = 0;
     for (;;) {
@@ -97,21 +97,21 @@ __device__ __forceinline__ bool mbar_wait_long(uint32_t bar, uint32_t parity)
             if (mbar_try(bar, parity)) return true;
         const uint64_t t = global_ns();
         if (t0 == 0) t0 = t;
-        else if (t - t0 > kWaitNs) return false;
+        else if (t - t0 > limit) return false;
     }
 }
 
 // Waits for the phase of this parity to complete; false when it gave up.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity)
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint64_t limit = kWaitNs)
 {
-    return mbar_try(bar, parity) || mbar_wait_long(bar, parity);
+    return mbar_try(bar, parity) || mbar_wait_long(bar, parity, limit);
 }
 
 // The same by a whole warp, which agrees on the answer.
-__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity)
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, uint64_t limit = kWaitNs)
 {
     const bool done = mbar_try(bar, parity);
-    return __all_sync(0xffffffffu, done) || __all_sync(0xffffffffu, mbar_wait_long(bar, parity));
+    return __all_sync(0xffffffffu, done) || __all_sync(0xffffffffu, mbar_wait_long(bar, parity, limit));
 }
 
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)

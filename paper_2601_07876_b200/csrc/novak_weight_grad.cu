@@ -413,6 +413,8 @@ struct KernelArgs {
     int64_t sums_ld;
     const void *weight, *bias;
     int param_type;
+    uint64_t wait_ns;               // after which a wait gives up (waits for copies and products in flight: kWaitNs)
+    int withheld;                   // a pair that is never told of its first sum, for a test of that; or -1
 };
 
 __device__ unsigned g_gave_up;       // warps whose wait for a tile ran out, since the library was loaded
@@ -452,7 +454,7 @@ __device__ __forceinline__ void load_codes(const KernelArgs &a, const CUtensorMa
         const int64_t block0 = static_cast<int64_t>(tk) * (kTileK / 32) + rank * 4;
         for (int i = 0; i < piece.count; ++i, ++step, at.advance(a.cut)) {
             if (step % kLoadWarps == mine) {
-                if (!mbar_wait_warp(smem_addr(&sh.raw_empty[raw.slot]), raw.phase ^ 1)) {
+                if (!mbar_wait_warp(smem_addr(&sh.raw_empty[raw.slot]), raw.phase ^ 1, a.wait_ns)) {
                     if (any) mbar_wait_warp(smem_addr(&sh.raw_full[last.slot]), last.phase);      // its copy in flight
                     return;
                 }
@@ -485,6 +487,7 @@ __device__ __forceinline__ void load_codes(const KernelArgs &a, const CUtensorMa
             raw.advance();
         }
     }
+    if (any) mbar_wait_warp(smem_addr(&sh.raw_full[last.slot]), last.phase);      // (whoever fills may have given up)
 }
 
 // Warps kOutWarps ..: x, 64 rows x 128 columns per step, a thread one block of each of
@@ -505,7 +508,7 @@ __device__ __forceinline__ void fill_x(const KernelArgs &a, Shared &sh, uint32_t
     const uint32_t done = smem_addr(&sh.x_done[0]), filled = smem_addr(rank == 0 ? &sh.full[0] : &sh.filled[0]);
     const uint32_t raw_full = smem_addr(&sh.raw_full[0]), raw_empty = smem_addr(&sh.raw_empty[0]);
     for (int step = group; step < steps; step += kFillGroups) {
-        if (!mbar_wait_warp(raw_full + raw.slot * 8, raw.phase)) return;
+        if (!mbar_wait_warp(raw_full + raw.slot * 8, raw.phase, a.wait_ns)) return;
         uint32_t q[4][4], e[2];
         const uint32_t src = src0 + raw.slot * kRawBytes;
 #pragma unroll
@@ -516,7 +519,7 @@ __device__ __forceinline__ void fill_x(const KernelArgs &a, Shared &sh, uint32_t
                 asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q[2 * k + h][0]), "=r"(q[2 * k + h][1]),
                              "=r"(q[2 * k + h][2]), "=r"(q[2 * k + h][3]) : "r"((src ^ h << 4) + k * 2048));
         }
-        if (!mbar_wait_warp(done + x.slot * 8, x.phase ^ 1)) return;
+        if (!mbar_wait_warp(done + x.slot * 8, x.phase ^ 1, a.wait_ns)) return;
         const uint32_t dst = dst0 + x.slot * kSlotBytes;
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
@@ -542,11 +545,12 @@ __device__ __forceinline__ void fill_x(const KernelArgs &a, Shared &sh, uint32_t
     }
     // every commit of the leading CTA has arrived here before this CTA leaves
     for (int i = 0; i < kXSlots; i += kFillGroups, x.advance(kFillGroups))
-        if (!mbar_wait_warp(done + x.slot * 8, x.phase ^ 1)) return;
+        if (!mbar_wait_warp(done + x.slot * 8, x.phase ^ 1, a.wait_ns)) return;
 }
 
 // Warps 0 ..: the tile.  A warp has 32 rows (its quarter of the lanes) x 128 columns
 // of it in registers and adds to them what the tensor cores have summed of a run.
+// Where a wait gave up, NaNs go out in place of this piece and of all that follow it.
 __device__ __forceinline__ void take_out(const KernelArgs &a, Shared &sh, uint32_t tmem, uint32_t rank, int pair)
 {
     const Cut &cut = a.cut;
@@ -556,16 +560,16 @@ __device__ __forceinline__ void take_out(const KernelArgs &a, Shared &sh, uint32
     Piece piece;
     uint32_t n = 0;
     bool ok = true;
-    while (ok && walk.next(piece)) {
+    while (walk.next(piece)) {
         int tn, tk;
         tile_at(cut, piece.tile, tn, tk);
         const int64_t n0 = static_cast<int64_t>(tn) * kTileN + rank * 128;
         float total[128];
 #pragma unroll
         for (int i = 0; i < 128; ++i) total[i] = 0.0f;
-        for (int left = piece.count; left > 0; left -= cut.run) {
+        for (int left = piece.count; ok && left > 0; left -= cut.run) {
             const uint32_t buf = n & 1;
-            ok = mbar_wait_warp(smem_addr(&sh.out_full[buf]), (n >> 1) & 1);
+            ok = mbar_wait_warp(smem_addr(&sh.out_full[buf]), (n >> 1) & 1, a.wait_ns);
             if (!ok) {
                 if (lane == 0) atomicAdd(&g_gave_up, 1u);
                 break;
@@ -589,7 +593,8 @@ __device__ __forceinline__ void take_out(const KernelArgs &a, Shared &sh, uint32
         // once per tile comes from far away.  So it goes through tensor memory once more.
         const uint32_t at = tmem + (n & 1) * 256 + side * 128 + (static_cast<uint32_t>(quarter) * 32 << 16);
 #pragma unroll
-        for (int c = 0; c < 128; c += 16) tmem_store16(at + c, total + c);
+        for (int c = 0; c < 128; c += 16)
+            if (ok) tmem_store16(at + c, total + c);
         tmem_store_wait();
         const bool partial = !piece.whole;
         float4 *dst = reinterpret_cast<float4 *>(a.partial) + (static_cast<int64_t>(piece.slot) * 64 + side * 32) * 256 +
@@ -606,11 +611,13 @@ __device__ __forceinline__ void take_out(const KernelArgs &a, Shared &sh, uint32
 #pragma unroll 1
         for (int c = 0; c < 128; c += 32) {
             float v[32];
-            tmem_load16(at + c, reinterpret_cast<float (&)[16]>(v[0]));
-            tmem_load16(at + c + 16, reinterpret_cast<float (&)[16]>(v[16]));
-            if (!ok)        // nobody takes this for a result
+            if (ok) {
+                tmem_load16(at + c, reinterpret_cast<float (&)[16]>(v[0]));
+                tmem_load16(at + c + 16, reinterpret_cast<float (&)[16]>(v[16]));
+            } else {        // nobody takes this for a result
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(0x7fffffffu);
+            }
             if (partial) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
@@ -640,7 +647,7 @@ __device__ __forceinline__ void take_out(const KernelArgs &a, Shared &sh, uint32
                 __syncwarp();
             }
         }
-        if (!ok) break;
+        if (!ok) continue;
         tcgen05_before_sync();
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(at_rank(smem_addr(&sh.out_empty[n & 1]), 0));
@@ -718,7 +725,7 @@ novak_weight_grad_kernel(const __grid_constant__ KernelArgs a, const __grid_cons
                 const int x = tn * kTileN + static_cast<int>(rank) * 128;
                 StepPos at(cut, piece.first);
                 for (int i = 0; i < piece.count; ++i) {
-                    ok = mbar_wait(smem_addr(&sh.done[dy.slot]), dy.phase ^ 1);
+                    ok = mbar_wait(smem_addr(&sh.done[dy.slot]), dy.phase ^ 1, a.wait_ns);
                     if (!ok) break;
                     const uint32_t bar = smem_addr(&sh.dy_full[dy.slot]), dst = dys + dy.slot * kSlotBytes;
                     mbar_expect(bar, 2 * kHalf);
@@ -731,7 +738,7 @@ novak_weight_grad_kernel(const __grid_constant__ KernelArgs a, const __grid_cons
             }
             // Every commit of the leading CTA has arrived here before this CTA leaves ...
             for (int i = 0; ok && i < kDySlots; ++i) {
-                ok = mbar_wait(smem_addr(&sh.done[dy.slot]), dy.phase ^ 1);
+                ok = mbar_wait(smem_addr(&sh.done[dy.slot]), dy.phase ^ 1, a.wait_ns);
                 dy.advance();
             }
             // ... and so has every copy, where a wait gave up and nobody took them
@@ -745,12 +752,14 @@ novak_weight_grad_kernel(const __grid_constant__ KernelArgs a, const __grid_cons
             const uint32_t lead_full = at_rank(smem_addr(&sh.full[0]), 0);
             while (ok && walk.next(piece))
                 for (int i = 0; ok && i < piece.count; ++i) {
-                    ok = mbar_wait_warp(smem_addr(&sh.dy_full[dy.slot]), dy.phase) && mbar_wait_warp(smem_addr(&sh.filled[x.slot]), x.phase);
+                    ok = mbar_wait_warp(smem_addr(&sh.dy_full[dy.slot]), dy.phase, a.wait_ns) &&
+                         mbar_wait_warp(smem_addr(&sh.filled[x.slot]), x.phase, a.wait_ns);
                     if (ok && lane == 0) mbar_arrive_cluster(lead_full + x.slot * 8);
                     __syncwarp();
                     dy.advance();
                     x.advance();
                 }
+            mbar_wait_warp(smem_addr(&sh.drained), 0);
         } else if (warp == kMmaWarp) {
             // ---- the products.  The warp stays together and one lane issues, so that the
             // descriptors are the warp's: formed by a lane on its own they cost more time
@@ -764,10 +773,11 @@ novak_weight_grad_kernel(const __grid_constant__ KernelArgs a, const __grid_cons
                     const int run = min(left, cut.run);
                     left -= run;
                     const uint32_t buf = n & 1, d = tmem + buf * 256;
-                    ok = mbar_wait_warp(smem_addr(&sh.out_empty[buf]), ((n >> 1) & 1) ^ 1);
+                    ok = mbar_wait_warp(smem_addr(&sh.out_empty[buf]), ((n >> 1) & 1) ^ 1, a.wait_ns);
                     tcgen05_after_sync();
                     for (int i = 0; ok && i < run; ++i) {
-                        ok = mbar_wait_warp(smem_addr(&sh.dy_full[dy.slot]), dy.phase) && mbar_wait_warp(smem_addr(&sh.full[x.slot]), x.phase);
+                        ok = mbar_wait_warp(smem_addr(&sh.dy_full[dy.slot]), dy.phase, a.wait_ns) &&
+                             mbar_wait_warp(smem_addr(&sh.full[x.slot]), x.phase, a.wait_ns);
                         if (!ok) break;
                         tcgen05_after_sync();
                         const uint64_t dy_at = dy0 + dy.slot * (kSlotBytes >> 4), x_at = x0 + x.slot * (kSlotBytes >> 4);
@@ -777,7 +787,7 @@ novak_weight_grad_kernel(const __grid_constant__ KernelArgs a, const __grid_cons
                                 mma_pair_bf16(d, dy_at + k * (2048 >> 4), x_at + k * (2048 >> 4), idesc, i > 0 || k > 0);
                             mma_commit_pair(smem_addr(&sh.x_done[x.slot]));
                             mma_commit_pair(smem_addr(&sh.done[dy.slot]));
-                            if (i == run - 1) mma_commit_pair(smem_addr(&sh.out_full[buf]));
+                            if (i == run - 1 && (n > 0 || pair != a.withheld)) mma_commit_pair(smem_addr(&sh.out_full[buf]));
                         }
                         __syncwarp();
                         dy.advance();
@@ -785,11 +795,11 @@ novak_weight_grad_kernel(const __grid_constant__ KernelArgs a, const __grid_cons
                     }
                 }
             }
-            if (!ok) {      // products in flight end before their operands and sums go
-                if (elect_one()) mma_commit_pair(smem_addr(&sh.drained));
-                __syncwarp();
-                mbar_wait_warp(smem_addr(&sh.drained), 0);
-            }
+            // products in flight end, and every commit arrives in both CTAs, before operands, sums and
+            // barriers go (whoever would have waited for them may have given up)
+            if (elect_one()) mma_commit_pair(smem_addr(&sh.drained));
+            __syncwarp();
+            mbar_wait_warp(smem_addr(&sh.drained), 0);
         }
     }
     __syncwarp();
@@ -972,6 +982,13 @@ cudaError_t launch_sums(const WeightGradArgs &a, const Layout &l, float *sums, _
 
 }  // namespace
 
+int weight_grad_pairs(const Mat &dy, int type, int64_t rows, int64_t n_out, int64_t n_in)
+{
+    if (little(rows, n_out, n_in)) return 0;
+    const Cut c = layout_for(dy, type, rows, n_out, n_in).cut;
+    return c.waves > 0 ? c.pairs : c.rest_pairs;
+}
+
 size_t weight_grad_bytes(const Mat &dy, int type, int64_t rows, int64_t n_out, int64_t n_in)
 {
     if (little(rows, n_out, n_in)) return 0;
@@ -1042,7 +1059,7 @@ cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t stream)
 
     float *partial = reinterpret_cast<float *>(work + l.planes_bytes);
     const KernelArgs k{l.cut, a.codes, a.dw, a.db, a.grad_type, vector, a.rows, a.n_out, a.n_in, partial,
-                       sums, l.parts, l.sums_ld, a.weight, a.bias, a.param_type};
+                       sums, l.parts, l.sums_ld, a.weight, a.bias, a.param_type, a.wait_ns ? a.wait_ns : kWaitNs, a.withheld};
     const int pairs = l.cut.waves > 0 ? l.cut.pairs : l.cut.rest_pairs;
     e = launch(novak_weight_grad_kernel, 2 * pairs, kThreads, kSmemBytes, stream, k, map, codes_map);
     if (e != cudaSuccess) return e;

@@ -706,7 +706,9 @@ int novak_layer_norm_backward(const void *d_dy, int64_t dy_stride, const void *d
                               int64_t rows, int64_t cols, void *stream);
 
 /* Activation functions.  GELU: u Phi(u), Phi the normal distribution function;
- * GELU_TANH: u (1 + tanh(sqrt(2/pi) (u + 0.044715 u^3))) / 2; SILU: u / (1 + e^-u). */
+ * GELU_TANH: u (1 + tanh(sqrt(2/pi) (u + 0.044715 u^3))) / 2; SILU: u / (1 + e^-u).
+ * Of plus infinity all are plus infinity, of minus infinity (times 0) and of a NaN
+ * NaNs; the slopes at the infinities are NaNs or the limits, 1 and 0. */
 enum { NOVAK_ACT_GELU = 0, NOVAK_ACT_GELU_TANH = 1, NOVAK_ACT_SILU = 2 };
 
 /* a = f(u), and, where the pointers are not NULL (codes and exps together), the

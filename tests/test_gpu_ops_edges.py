@@ -54,3 +54,33 @@ def test_unpacking_writes_nothing_but_the_forms_elements(ops):
         with pytest.raises(ValueError, match="elements"):
             ops._calls.unpack(kept, out)
         assert not out.any()
+
+
+# ---- infinities through the activation functions -------------------------------------
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("kind", ["gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("cols", [96, 33])
+def test_infinities_and_nans_through_the_activations(ops, cols, kind, dtype):
+    """f(inf) = inf.  f(-inf) is -inf times 0 by each of the formulas, a NaN; the slopes at the infinities are NaNs too
+    or their limits, 1 and 0.  Neighbours see nothing of it."""
+    u = matrix(5, cols, dtype, 1)
+    clean, _, _ = ops.activation(u, kind, save_input=False)
+    slope = ops.activation_backward(torch.ones_like(u), u, kind)
+    at = {(0, 3): math.inf, (1, 8): -math.inf, (2, cols - 1): math.nan, (4, 0): math.inf}
+    for place, value in at.items():
+        u[place] = value
+    a, _, kept_a = ops.activation(u, kind, save_output=True)
+    du = ops.activation_backward(torch.ones_like(u), u, kind)
+    for place, value in at.items():
+        if value == math.inf:
+            assert a[place] == math.inf
+        else:
+            assert torch.isnan(a[place])
+        limit = 1.0 if value == math.inf else 0.0
+        assert torch.isnan(du[place]) or (du[place] == limit and not math.isnan(value))
+    others = torch.ones(5, cols, dtype=torch.bool, device="cuda")
+    for place in at:
+        others[place] = False
+    assert torch.equal(a[others], clean[others]) and torch.equal(du[others], slope[others])
+    blocks = torch.nn.functional.pad(~torch.isfinite(a), (0, -cols % 32)).view(5, -1, 32).any(2)
+    assert torch.equal(kept_a.exps == 255, blocks)

@@ -12,13 +12,15 @@ passes:
 ``MlpBlock8`` is the pre-norm residual block of both: 9.3 bytes per token and unit of
 width instead of 20 in bf16 (with a hidden width of four times the width).  Parameters
 are float32, as ``optim.Novak`` takes them; products run in the input's type (bfloat16
-under ``x.to(torch.bfloat16)``), and the gradients arrive in float32.
+under ``x.to(torch.bfloat16)``), and the gradients arrive in float32.  The backward
+passes have none of their own: asking for second derivatives raises.
 """
 from __future__ import annotations
 
 import math
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import ops
 
@@ -45,6 +47,7 @@ class _NormLinear(torch.autograd.Function):
         return torch.nn.functional.linear(h, weight.to(h.dtype), None if bias is None else bias.to(h.dtype))
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         rstd, gamma, beta, weight = ctx.saved_tensors
         dy = _dense(dy)
@@ -65,6 +68,7 @@ class _ActLinear(torch.autograd.Function):
         return torch.nn.functional.linear(a, weight.to(a.dtype), None if bias is None else bias.to(a.dtype))
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         (weight,) = ctx.saved_tensors
         da, dw, db = _linear_backward(ctx, _dense(dy), ctx.kept_a, weight, ctx.needs_input_grad[:3])

@@ -33,13 +33,11 @@ constexpr int kColsPerCta = 32;
 constexpr int kSms = 148;
 
 // Puts the 8-bit form of a thread's eight elements at `col` of `row` away; every thread
-// of the warp has to be here, with zeros beyond the row's elements.  ALL: the eight are
-// NaNs together or not at all.
-template <bool ALL>
+// of the warp has to be here, with zeros beyond the row's elements.
 __device__ __forceinline__ void put_codes(const Codes &c, int64_t row, int64_t pitch, int64_t col, const F2 (&v)[4])
 {
     uint32_t exp;
-    const uint2 q = quantize8(v, ALL ? top_of(v) : top_of_any(v), exp);
+    const uint2 q = quantize8(v, top_of(v), exp);
     if (col < pitch) {
         const int64_t at = row * pitch + col;
         *reinterpret_cast<uint2 *>(c.codes + at) = q;
@@ -203,8 +201,7 @@ __global__ void __launch_bounds__(32 * forward_warps<G, NV>()) novak_layer_norm_
             Eight<TYPE> out;
             out.set(o);
             store_eight<ALIGNED>(y + i * G * 8, out, n[i]);
-            // (a row with an infinity or NaN in it has nothing but NaNs, and zeros beyond it)
-            if (a.codes.codes) put_codes<ALIGNED>(a.codes, row, pitch, (i * G + t) * 8, v[i]);
+            if (a.codes.codes) put_codes(a.codes, row, pitch, (i * G + t) * 8, v[i]);
         }
     }
 }
@@ -409,7 +406,7 @@ __global__ void __launch_bounds__(kThreads) novak_layer_norm_long_kernel(NormArg
                 F2 p[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) p[k] = F2(v[2 * k], v[2 * k + 1]);
-                put_codes<false>(a.codes, row, pitch, c, p);
+                put_codes(a.codes, row, pitch, c, p);
             }
         }
     }

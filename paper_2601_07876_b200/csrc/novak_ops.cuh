@@ -442,26 +442,19 @@ __device__ __forceinline__ uint2 quantize8(const F2 (&v)[4], uint32_t top, uint3
     return exp == 255u ? make_uint2(0u, 0u) : make_uint2(q[0], q[1]);
 }
 
-// Bits of the largest magnitude of eight numbers.
-__device__ __forceinline__ uint32_t top_of_any(const F2 (&v)[4])
+// Bits of the largest magnitude of eight numbers, a NaN's if one is among them.
+__device__ __forceinline__ float larger(float a, float b)
 {
-    uint32_t t = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        t = max(t, max(__float_as_uint(v[i].lo()) & 0x7fffffffu, __float_as_uint(v[i].hi()) & 0x7fffffffu));
-    return t;
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)));
+    return r;
 }
-
-// The same of numbers that are NaNs all or none.
 __device__ __forceinline__ uint32_t top_of(const F2 (&v)[4])
 {
-    float t = 0.0f;
     float x[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i].get(x[2 * i], x[2 * i + 1]);
-    t = fmaxf(fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3]))),
-              fmaxf(fmaxf(fabsf(x[4]), fabsf(x[5])), fmaxf(fabsf(x[6]), fabsf(x[7]))));
-    return __float_as_uint(t) & 0x7fffffffu;
+    return __float_as_uint(larger(larger(larger(x[0], x[1]), larger(x[2], x[3])), larger(larger(x[4], x[5]), larger(x[6], x[7]))));
 }
 
 __device__ __forceinline__ float scale_of(uint32_t exp)

@@ -84,3 +84,23 @@ def test_infinities_and_nans_through_the_activations(ops, cols, kind, dtype):
     assert torch.equal(a[others], clean[others]) and torch.equal(du[others], slope[others])
     blocks = torch.nn.functional.pad(~torch.isfinite(a), (0, -cols % 32)).view(5, -1, 32).any(2)
     assert torch.equal(kept_a.exps == 255, blocks)
+
+
+# ---- sums that overflow ----------------------------------------------------------------
+@pytest.mark.parametrize("cols,offset", [(8, 0), (40, 0), (40, 1), (1024, 0), (4096, 0), (9000, 0)])
+def test_a_deviation_that_overflows_is_the_same_nan_in_both_results(ops, cols, offset):
+    """fp32's largest numbers: the first element's deviation from the mean is an infinity, the root's reciprocal 0, and
+    xhat a NaN there and 0 in the others.  Its block of the 8-bit form stands for NaNs."""
+    buf = torch.zeros(offset + 2 * cols, device="cuda")
+    x = buf[offset:].view(2, cols)
+    top = 3.4028234e38
+    x[0, 0], x[0, 1:] = top, -1.01 * top / (cols - 1)       # (no part of their sum overflows; the mean is below 0)
+    x[1] = torch.linspace(-1, 1, cols, device="cuda")
+    w = torch.ones(cols, device="cuda")
+    y, _, _, kept = ops.layer_norm(x, w, checkpoint=True)
+    value = ops.act8_unpack(kept, dtype=F32)
+    bad = torch.isnan(y)
+    assert bad[0, 0] and not bad[0, 1:].any() and not bad[1].any()
+    blocks = torch.nn.functional.pad(bad, (0, -cols % 32)).view(2, -1, 32).any(2)
+    assert torch.equal(kept.exps == 255, blocks)
+    assert torch.equal(torch.isnan(value), blocks.repeat_interleave(32, 1)[:, :cols])

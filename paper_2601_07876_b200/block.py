@@ -13,7 +13,8 @@ passes:
 width instead of 20 in bf16 (with a hidden width of four times the width).  Parameters
 are float32, as ``optim.Novak`` takes them; products run in the input's type (bfloat16
 under ``x.to(torch.bfloat16)``), and the gradients arrive in float32.  The backward
-passes have none of their own: asking for second derivatives raises.
+passes have none of their own: asking for second derivatives raises.  What is kept are saved
+tensors: the backward pass lets go of them, and saved-tensor hooks see them.
 """
 from __future__ import annotations
 
@@ -42,20 +43,21 @@ class _NormLinear(torch.autograd.Function):
     def forward(ctx, x, gamma, beta, weight, bias, eps):
         x = _dense(x)
         h, _, rstd, kept = ops.layer_norm(x, gamma, beta, eps, checkpoint=True)
-        ctx.save_for_backward(rstd, gamma, beta, weight)
-        ctx.kept = kept
+        ctx.save_for_backward(kept.buffer, rstd, gamma, beta, weight)
+        ctx.width = x.shape[-1]
         return torch.nn.functional.linear(h, weight.to(h.dtype), None if bias is None else bias.to(h.dtype))
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
-        rstd, gamma, beta, weight = ctx.saved_tensors
+        buffer, rstd, gamma, beta, weight = ctx.saved_tensors
+        kept = ops.Act8.from_buffer(buffer, ctx.width)
         dy = _dense(dy)
         norm = ctx.needs_input_grad[0] or ctx.needs_input_grad[1] or ctx.needs_input_grad[2]
-        dh, dw, db = _linear_backward(ctx, dy, ctx.kept, weight, (norm, *ctx.needs_input_grad[3:5]), (gamma, beta))
+        dh, dw, db = _linear_backward(ctx, dy, kept, weight, (norm, *ctx.needs_input_grad[3:5]), (gamma, beta))
         dx = dgamma = dbeta = None
         if norm:
-            dx, dgamma, dbeta = ops.layer_norm_backward(dh, ctx.kept, rstd, gamma, grad_dtype=gamma.dtype)
+            dx, dgamma, dbeta = ops.layer_norm_backward(dh, kept, rstd, gamma, grad_dtype=gamma.dtype)
         return dx, dgamma, dbeta, dw, db, None
 
 
@@ -63,16 +65,16 @@ class _ActLinear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, u, weight, bias, kind):
         a, kept_u, kept_a = ops.activation(_dense(u), kind, save_input=True, save_output=True)
-        ctx.save_for_backward(weight)
-        ctx.kept_u, ctx.kept_a, ctx.kind = kept_u, kept_a, kind
+        ctx.save_for_backward(kept_u.buffer, kept_a.buffer, weight)
+        ctx.width, ctx.kind = u.shape[-1], kind
         return torch.nn.functional.linear(a, weight.to(a.dtype), None if bias is None else bias.to(a.dtype))
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
-        (weight,) = ctx.saved_tensors
-        da, dw, db = _linear_backward(ctx, _dense(dy), ctx.kept_a, weight, ctx.needs_input_grad[:3])
-        du = ops.activation_backward(da, ctx.kept_u, ctx.kind) if ctx.needs_input_grad[0] else None
+        of_u, of_a, weight = ctx.saved_tensors
+        da, dw, db = _linear_backward(ctx, _dense(dy), ops.Act8.from_buffer(of_a, ctx.width), weight, ctx.needs_input_grad[:3])
+        du = ops.activation_backward(da, ops.Act8.from_buffer(of_u, ctx.width), ctx.kind) if ctx.needs_input_grad[0] else None
         return du, dw, db, None
 
 

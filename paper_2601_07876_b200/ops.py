@@ -52,6 +52,13 @@ def _type(dtype, name: str) -> int:
         raise TypeError(f"{name} must be float32 or bfloat16, got {dtype}") from None
 
 
+def _folded(shape, rows: int, cols: int):
+    shape = (rows, cols) if shape is None else tuple(shape)
+    if not shape or shape[-1] != cols or math.prod(shape[:-1]) != rows:
+        raise ValueError(f"shape {shape} does not fold into {rows} rows of {cols} elements")
+    return shape
+
+
 class Act8:
     """The 8-bit form of a matrix: ``codes`` (int8, rows x padded columns) and ``exps``
     (uint8, rows x padded columns / 32), see include/novak.h.  ``shape`` is that of the
@@ -66,9 +73,7 @@ class Act8:
         if cols < 1 or pitch != (cols + BLOCK - 1) // BLOCK * BLOCK or exps.shape != (rows, pitch // BLOCK):
             raise ValueError(f"no 8-bit form of rows of {cols} elements: codes {tuple(codes.shape)}, "
                              f"exps {tuple(exps.shape)}")
-        shape = (rows, cols) if shape is None else tuple(shape)
-        if not shape or shape[-1] != cols or math.prod(shape[:-1]) != rows:
-            raise ValueError(f"shape {shape} does not fold into {rows} rows of {cols} elements")
+        shape = _folded(shape, rows, cols)
         index = codes.get_device()
         if not codes.is_contiguous() or not exps.is_contiguous() or index < 0 or exps.get_device() != index:
             raise ValueError("codes and exps must be contiguous CUDA tensors of one device")
@@ -77,6 +82,17 @@ class Act8:
             raise ValueError("codes must be 32-byte aligned")
         self._codes, self._exps, self._both, self.rows, self.cols, self.index = codes, exps, None, rows, cols, index
         self.shape = shape
+
+    @classmethod
+    def from_buffer(cls, buffer, cols: int, shape=None):
+        """The form whose ``buffer`` this is (or a copy of it), of rows of ``cols`` elements."""
+        if buffer.dtype != torch.uint8 or buffer.dim() != 1 or not buffer.is_contiguous():
+            raise TypeError("a form's buffer is one contiguous dimension of uint8")
+        size = (cols + BLOCK - 1) // BLOCK * (BLOCK + 1)
+        if cols < 1 or buffer.shape[0] % size or buffer.get_device() < 0 or buffer.data_ptr() % 32:
+            raise ValueError(f"no buffer of the 8-bit form of rows of {cols} elements: {buffer.shape[0]} bytes on "
+                             f"{buffer.device}")
+        return cls._of(buffer, cols, _folded(shape, buffer.shape[0] // size, cols))
 
     @classmethod
     def _of(cls, both, cols: int, shape):
@@ -107,6 +123,13 @@ class Act8:
         if self._exps is None:
             self._split()
         return self._exps
+
+    @property
+    def buffer(self):
+        """Codes and exponents as one tensor, codes first: what to keep, move or save of a form."""
+        if self._both is None:
+            return torch.cat([self._codes.view(torch.uint8).view(-1), self._exps.view(-1)])
+        return self._both
 
     @property
     def device(self):

@@ -104,3 +104,17 @@ def test_a_deviation_that_overflows_is_the_same_nan_in_both_results(ops, cols, o
     blocks = torch.nn.functional.pad(bad, (0, -cols % 32)).view(2, -1, 32).any(2)
     assert torch.equal(kept.exps == 255, blocks)
     assert torch.equal(torch.isnan(value), blocks.repeat_interleave(32, 1)[:, :cols])
+
+
+# ---- a form's buffer -------------------------------------------------------------------
+def test_a_form_from_its_buffer_is_the_form(ops):
+    x = matrix(30, 70, F32, 1)
+    kept = ops.act8_pack(x.view(3, 10, 70) if x.is_contiguous() else x)
+    by_parts = ops.Act8(kept.codes.clone(), kept.exps.clone(), 70)
+    for form in (kept, by_parts):
+        copy = ops.Act8.from_buffer(form.buffer.clone(), 70, shape=(3, 10, 70))
+        assert copy.rows == 30 and torch.equal(copy.codes, kept.codes) and torch.equal(copy.exps, kept.exps)
+        assert torch.equal(ops.act8_unpack(copy).view(30, 70), ops.act8_unpack(kept).view(30, 70))
+    for cols, shape in ((64, None), (70, (3, 11, 70)), (70, (30, 64))):
+        with pytest.raises(ValueError):
+            ops.Act8.from_buffer(kept.buffer[:-1] if shape is None else kept.buffer, cols, shape)

@@ -10,3 +10,13 @@ def test_a_form_is_refused_a_shape_that_is_not_its_own(shape):
     codes, exps = torch.zeros(300, 64, dtype=torch.int8), torch.zeros(300, 2, dtype=torch.uint8)
     with pytest.raises(ValueError, match="fold"):
         ops.Act8(codes, exps, 64, shape=shape)
+
+
+@pytest.mark.parametrize("cols", [0, -5, -100, 64])
+def test_a_form_is_refused_a_buffer_that_is_not_its_own(cols):
+    from paper_2601_07876_b200 import ops
+    with pytest.raises(ValueError, match="buffer"):
+        ops.Act8.from_buffer(torch.zeros(66 * 4 + 1, dtype=torch.uint8), cols)
+    for wrong in (torch.zeros(66), torch.zeros(4, 66, dtype=torch.uint8), torch.zeros(132, dtype=torch.uint8)[::2]):
+        with pytest.raises(TypeError):
+            ops.Act8.from_buffer(wrong, cols)

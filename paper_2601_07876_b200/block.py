@@ -14,7 +14,8 @@ width instead of 20 in bf16 (with a hidden width of four times the width).  Para
 are float32, as ``optim.Novak`` takes them; products run in the input's type (bfloat16
 under ``x.to(torch.bfloat16)``), and the gradients arrive in float32.  The backward
 passes have none of their own: asking for second derivatives raises.  What is kept are saved
-tensors: the backward pass lets go of them, and saved-tensor hooks see them.
+tensors: the backward pass lets go of them, and saved-tensor hooks see them.  Forms that
+no gradient needs (under ``no_grad``, of frozen parameters) are not made.
 """
 from __future__ import annotations
 
@@ -30,11 +31,17 @@ def _dense(t):
     return t if t.is_contiguous() else t.contiguous()
 
 
-def _linear_backward(ctx, dy, kept, weight, needs, affine=None):
+def _linear(x, weight, bias):
+    return torch.nn.functional.linear(x, weight.to(x.dtype), None if bias is None else bias.to(x.dtype))
+
+
+def _linear_backward(dy, kept, weight, needs, affine=None):
     """(dx, dW, db) of a linear layer whose input was kept in 8 bits."""
     dw = db = None
-    if needs[1] or needs[2]:
+    if needs[1]:
         dw, db = ops.linear_weight_grad(dy, kept, affine=affine, bias=needs[2], dtype=weight.dtype)
+    elif needs[2]:
+        db = dy.reshape(-1, dy.shape[-1]).sum(0, dtype=torch.float32).to(weight.dtype)
     return (torch.matmul(dy, weight.to(dy.dtype)) if needs[0] else None), dw, db
 
 
@@ -42,19 +49,20 @@ class _NormLinear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, gamma, beta, weight, bias, eps):
         x = _dense(x)
-        h, _, rstd, kept = ops.layer_norm(x, gamma, beta, eps, checkpoint=True)
-        ctx.save_for_backward(kept.buffer, rstd, gamma, beta, weight)
+        keep = any(ctx.needs_input_grad[:4])            # (the bias's gradient needs nothing of it)
+        h, _, rstd, kept = ops.layer_norm(x, gamma, beta, eps, checkpoint=keep)
+        ctx.save_for_backward(kept.buffer if keep else None, rstd, gamma, beta, weight)
         ctx.width = x.shape[-1]
-        return torch.nn.functional.linear(h, weight.to(h.dtype), None if bias is None else bias.to(h.dtype))
+        return _linear(h, weight, bias)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
         buffer, rstd, gamma, beta, weight = ctx.saved_tensors
-        kept = ops.Act8.from_buffer(buffer, ctx.width)
+        kept = None if buffer is None else ops.Act8.from_buffer(buffer, ctx.width)
         dy = _dense(dy)
         norm = ctx.needs_input_grad[0] or ctx.needs_input_grad[1] or ctx.needs_input_grad[2]
-        dh, dw, db = _linear_backward(ctx, dy, kept, weight, (norm, *ctx.needs_input_grad[3:5]), (gamma, beta))
+        dh, dw, db = _linear_backward(dy, kept, weight, (norm, *ctx.needs_input_grad[3:5]), (gamma, beta))
         dx = dgamma = dbeta = None
         if norm:
             dx, dgamma, dbeta = ops.layer_norm_backward(dh, kept, rstd, gamma, grad_dtype=gamma.dtype)
@@ -64,27 +72,37 @@ class _NormLinear(torch.autograd.Function):
 class _ActLinear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, u, weight, bias, kind):
-        a, kept_u, kept_a = ops.activation(_dense(u), kind, save_input=True, save_output=True)
-        ctx.save_for_backward(kept_u.buffer, kept_a.buffer, weight)
+        a, kept_u, kept_a = ops.activation(_dense(u), kind, *ctx.needs_input_grad[:2])
+        ctx.save_for_backward(*(None if kept is None else kept.buffer for kept in (kept_u, kept_a)), weight)
         ctx.width, ctx.kind = u.shape[-1], kind
-        return torch.nn.functional.linear(a, weight.to(a.dtype), None if bias is None else bias.to(a.dtype))
+        return _linear(a, weight, bias)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
         of_u, of_a, weight = ctx.saved_tensors
-        da, dw, db = _linear_backward(ctx, _dense(dy), ops.Act8.from_buffer(of_a, ctx.width), weight, ctx.needs_input_grad[:3])
-        du = ops.activation_backward(da, ops.Act8.from_buffer(of_u, ctx.width), ctx.kind) if ctx.needs_input_grad[0] else None
+        kept_u, kept_a = (None if t is None else ops.Act8.from_buffer(t, ctx.width) for t in (of_u, of_a))
+        da, dw, db = _linear_backward(_dense(dy), kept_a, weight, ctx.needs_input_grad[:3])
+        du = ops.activation_backward(da, kept_u, ctx.kind) if ctx.needs_input_grad[0] else None
         return du, dw, db, None
 
 
+def _recorded(*inputs):
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs)
+
+
 def norm_linear(x, gamma, beta, weight, bias=None, eps: float = 1e-5):
-    """linear(layer_norm(x, gamma, beta), weight, bias), kept in 8 bits for the backward pass."""
+    """linear(layer_norm(x, gamma, beta), weight, bias), kept in 8 bits for the backward pass
+    (where there is one to come)."""
+    if not _recorded(x, gamma, beta, weight, bias):
+        return _linear(ops.layer_norm(_dense(x), gamma, beta, eps)[0], weight, bias)
     return _NormLinear.apply(x, gamma, beta, weight, bias, eps)
 
 
 def act_linear(u, weight, bias=None, kind: str = "gelu"):
-    """linear(f(u), weight, bias), kept in 8 bits for the backward pass."""
+    """linear(f(u), weight, bias), kept in 8 bits for the backward pass (where there is one to come)."""
+    if not _recorded(u, weight, bias):
+        return _linear(ops.activation(_dense(u), kind, save_input=False)[0], weight, bias)
     return _ActLinear.apply(u, weight, bias, kind)
 
 

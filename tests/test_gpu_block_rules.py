@@ -85,3 +85,75 @@ def test_backward_twice(block):
         assert all(torch.equal(a, b) for a, b in zip(first, second))
         with pytest.raises(RuntimeError, match="second time"):
             torch.autograd.grad(y, wrt, torch.ones_like(y))
+
+
+# ---- what no gradient needs ---------------------------------------------------------
+@pytest.fixture
+def calls(block, monkeypatch):
+    """(operator, forms asked for) of each call that leaves forms, and the others' names."""
+    made = []
+    inner = {name: getattr(block.ops, name) for name in ("layer_norm", "activation", "linear_weight_grad")}
+
+    def layer_norm(x, w, b, eps=1e-5, checkpoint=False):
+        made.append(("layer_norm", checkpoint))
+        return inner["layer_norm"](x, w, b, eps, checkpoint)
+
+    def activation(u, kind="gelu", save_input=True, save_output=False):
+        made.append(("activation", save_input, save_output))
+        return inner["activation"](u, kind, save_input, save_output)
+
+    def linear_weight_grad(*args, **kw):
+        made.append(("linear_weight_grad",))
+        return inner["linear_weight_grad"](*args, **kw)
+    for f in (layer_norm, activation, linear_weight_grad):
+        monkeypatch.setattr(block.ops, f.__name__, f)
+    return made
+
+
+def test_evaluation_keeps_nothing(block, calls):
+    b = block.MlpBlock8(64, 96)
+    x = torch.randn(20, 64, device="cuda")
+    want = b(x).detach()
+    assert calls == [("layer_norm", True), ("activation", True, True)]
+    nothing = [("layer_norm", False), ("activation", False, False)]
+    for context in (torch.no_grad(), torch.inference_mode()):
+        calls.clear()
+        with context:
+            y = b(x)
+        assert calls == nothing and torch.equal(y, want) and not y.requires_grad
+    for p in b.parameters():
+        p.requires_grad_(False)
+    calls.clear()
+    assert torch.equal(b(x), want) and calls == nothing
+
+
+def test_frozen_parameters_keep_what_the_others_need(block, calls):
+    b = block.MlpBlock8(64, 96)
+    x, dy = torch.randn(20, 64, device="cuda", requires_grad=True), torch.randn(20, 64, device="cuda")
+    parameters = dict(b.named_parameters(), x=x)
+    want = dict(zip(parameters, torch.autograd.grad(b(x), list(parameters.values()), dy)))
+    # trained alone: the forms of the norm and of the activation's input and output, whole weight gradients formed
+    for names, norm, act, grads in ((["down.bias"], False, (False, False), 0), (["down.weight"], False, (False, True), 1),
+                                    (["up.bias"], False, (True, False), 0), (["up.weight"], True, (True, False), 1),
+                                    (["x"], True, (True, False), 0), (["up.gamma", "up.beta"], True, (True, False), 0),
+                                    (["up.weight", "down.weight"], True, (True, True), 2)):
+        for n, p in parameters.items():
+            p.requires_grad_(n in names)
+        calls.clear()
+        got = torch.autograd.grad(b(x), [parameters[n] for n in names], dy)
+        assert [c for c in calls if c[0] == "layer_norm"] == [("layer_norm", norm)], names
+        assert [c for c in calls if c[0] == "activation"] == [("activation", *act)], names
+        assert sum(c[0] == "linear_weight_grad" for c in calls) == grads, names
+        for n, g in zip(names, got):
+            # (a bias's gradient alone is the same sum in another order)
+            bound = 20 * 2.0 ** -24 * dy.abs().sum() if n.endswith("bias") else 0.0
+            assert (g - want[n]).abs().max() <= bound, n
+
+
+def test_a_bias_alone_of_one_row_and_of_none(block, calls):
+    layer = block.ActLinear8(64, 96)
+    layer.weight.requires_grad_(False)
+    one, = torch.autograd.grad(layer(torch.randn(64, device="cuda")), [layer.bias], torch.arange(96.0, device="cuda"))
+    assert torch.equal(one, torch.arange(96.0, device="cuda"))
+    none, = torch.autograd.grad(layer(torch.empty(0, 64, device="cuda")), [layer.bias], torch.empty(0, 96, device="cuda"))
+    assert torch.equal(none, torch.zeros(96, device="cuda"))

@@ -708,7 +708,9 @@ int novak_layer_norm_backward(const void *d_dy, int64_t dy_stride, const void *d
 /* Activation functions.  GELU: u Phi(u), Phi the normal distribution function;
  * GELU_TANH: u (1 + tanh(sqrt(2/pi) (u + 0.044715 u^3))) / 2; SILU: u / (1 + e^-u).
  * Of plus infinity all are plus infinity, of minus infinity (times 0) and of a NaN
- * NaNs; the slopes at the infinities are NaNs or the limits, 1 and 0. */
+ * NaNs; the slopes at the infinities are NaNs or the limits, 1 and 0.  Computed in
+ * fp32: GELU as near as u (1 + erf) / 2 in fp32 operations or nearer (erf to
+ * 1.5e-7 where the type is bf16), the others to a few roundings. */
 enum { NOVAK_ACT_GELU = 0, NOVAK_ACT_GELU_TANH = 1, NOVAK_ACT_SILU = 2 };
 
 /* a = f(u), and, where the pointers are not NULL (codes and exps together), the

@@ -38,7 +38,7 @@ __device__ __forceinline__ float rcp_approx(float x)
 __device__ __forceinline__ F2 exp2_approx(F2 x) { return F2(exp2_approx(x.lo()), exp2_approx(x.hi())); }
 __device__ __forceinline__ F2 rcp_approx(F2 x) { return F2(rcp_approx(x.lo()), rcp_approx(x.hi())); }
 
-// Phi(-|u|) and exp(-u^2/2), Phi the normal distribution function, by formula
+// Phi(-|u|) and exp(-u^2/2), Phi the normal distribution function, for bf16: by formula
 // 7.1.26 of Abramowitz and Stegun (erf to 1.5e-7) for x = |u| / sqrt(2).
 __device__ __forceinline__ void normal_tail(F2 u, F2 &mag, F2 &tail, F2 &e)
 {
@@ -50,6 +50,38 @@ __device__ __forceinline__ void normal_tail(F2 u, F2 &mag, F2 &tail, F2 &e)
     p = fma2(p, t, F2(0.5f * -0.284496736f));
     p = fma2(p, t, F2(0.5f * 0.254829592f));
     tail = p * t * e;
+}
+
+// The same and Phi(u) for fp32, which that formula leaves twice as far off as erf in fp32
+// does.  Below |u| = 1, Phi = 1/2 + u q(u^2); above, Phi(-|u|) = t p(t) exp(-u^2/2) with t = 1 /
+// (1 + 0.3 |u|), as there, one degree more.  q and p are least-maximum fits by reweighted
+// least squares, with the coefficients rounded one after the other: Phi is off by at most 9e-9
+// and 3e-9 (and 4e-6 of the tail) beside the arithmetic.  12608 x 3072 fp32 stays bound by
+// HBM (59 us, back 52); on rows that are not aligned it takes 7 us of 84 more than the formula
+// above, erff 15 and erfcf 37.
+__device__ __forceinline__ F2 below_one(F2 u, F2 small, F2 large)
+{
+    return F2(fabsf(u.lo()) < 1.0f ? small.lo() : large.lo(), fabsf(u.hi()) < 1.0f ? small.hi() : large.hi());
+}
+__device__ __forceinline__ void normal_f32(F2 u, F2 &minus_mag, F2 &tail, F2 &cdf, F2 &e)
+{
+    const F2 mag(fabsf(u.lo()), fabsf(u.hi())), sq = u * u;
+    minus_mag = mag * F2(-1.0f);
+    const F2 t = rcp_approx(fma2(mag, F2(0.3f), F2(1.0f)));
+    e = exp2_approx(sq * F2(-0.5f * 1.44269504f));
+    F2 p = fma2(t, F2(-0.08579722f), F2(0.24261388f));
+    p = fma2(p, t, F2(-0.04816293f));
+    p = fma2(p, t, F2(0.16174269f));
+    p = fma2(p, t, F2(0.109038524f));
+    p = fma2(p, t, F2(0.120554216f));
+    const F2 far = p * t * e, rest = fma2(far, F2(-1.0f), F2(1.0f));
+    F2 q = fma2(sq, F2(9.2202055e-05f), F2(-0.001164883f));
+    q = fma2(q, sq, F2(0.009963931f));
+    q = fma2(q, sq, F2(-0.066488706f));
+    q = fma2(q, sq, F2(0.3989422f));
+    tail = below_one(u, fma2(minus_mag, q, F2(0.5f)), far);
+    cdf = below_one(u, fma2(u, q, F2(0.5f)),
+                    F2(u.lo() > 0.0f ? rest.lo() : far.lo(), u.hi() > 0.0f ? rest.hi() : far.hi()));
 }
 
 // (1 + tanh z) / 2 is the logistic function of 2 z: tanh-GELU is u times it.
@@ -64,14 +96,19 @@ __device__ __forceinline__ F2 tanh_argument(F2 u)
     return u * fma2(u * u, F2(-kLog2e * kTanh * kCubic), F2(-kLog2e * kTanh));
 }
 
-template <int KIND>
+template <int KIND, int TYPE>
 __device__ __forceinline__ F2 act(F2 u)
 {
     if constexpr (KIND == NOVAK_ACT_GELU) {
-        F2 mag, tail, e;
-        normal_tail(u, mag, tail, e);
+        F2 minus_mag, tail, cdf, e;
+        if constexpr (TYPE == NOVAK_TYPE_F32) {
+            normal_f32(u, minus_mag, tail, cdf, e);
+        } else {
+            normal_tail(u, minus_mag, tail, e);
+            minus_mag = minus_mag * F2(-1.0f);
+        }
         // u (1 - tail) above zero, u tail below
-        return fma2(mag * F2(-1.0f), tail, F2(fmaxf(u.lo(), 0.0f), fmaxf(u.hi(), 0.0f)));
+        return fma2(minus_mag, tail, F2(fmaxf(u.lo(), 0.0f), fmaxf(u.hi(), 0.0f)));
     }
     if constexpr (KIND == NOVAK_ACT_GELU_TANH) return u * logistic(tanh_argument(u));
     if constexpr (KIND == NOVAK_ACT_SILU) return u * logistic(u * F2(-kLog2e));
@@ -90,15 +127,19 @@ __device__ __forceinline__ void put_infinities(const F2 (&u)[4], F2 (&f)[4])
         f[k] = F2(u[k].lo() == inf ? inf : f[k].lo(), u[k].hi() == inf ? inf : f[k].hi());
 }
 
-template <int KIND>
+template <int KIND, int TYPE>
 __device__ __forceinline__ F2 act_slope(F2 u)
 {
     if constexpr (KIND == NOVAK_ACT_GELU) {
-        F2 mag, tail, e;
-        normal_tail(u, mag, tail, e);
-        const F2 h = fma2(tail, F2(-1.0f), F2(0.5f));       // Phi(u) = 1/2 +- h
-        const F2 phi = F2(copysignf(h.lo(), u.lo()), copysignf(h.hi(), u.hi())) + F2(0.5f);
-        return fma2(u * F2(0.39894228f), e, phi);
+        F2 mag, tail, e, cdf;
+        if constexpr (TYPE == NOVAK_TYPE_F32) {
+            normal_f32(u, mag, tail, cdf, e);
+        } else {
+            normal_tail(u, mag, tail, e);
+            const F2 h = fma2(tail, F2(-1.0f), F2(0.5f));   // Phi(u) = 1/2 +- h
+            cdf = F2(copysignf(h.lo(), u.lo()), copysignf(h.hi(), u.hi())) + F2(0.5f);
+        }
+        return fma2(u * F2(0.39894228f), e, cdf);
     }
     if constexpr (KIND == NOVAK_ACT_GELU_TANH) {
         const F2 p = logistic(tanh_argument(u));
@@ -189,7 +230,7 @@ novak_activation_kernel(const typename Elem<TYPE>::T *u, int64_t u_stride, typen
             if constexpr (KIND != kIdentity) {
                 F2 f[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) f[k] = act<KIND>(v[k]);
+                for (int k = 0; k < 4; ++k) f[k] = act<KIND, TYPE>(v[k]);
                 if (KIND == NOVAK_ACT_GELU && top >= kInfinityBits) put_infinities(v, f);
                 Eight<TYPE> out;
                 out.set(f);
@@ -203,8 +244,11 @@ novak_activation_kernel(const typename Elem<TYPE>::T *u, int64_t u_stride, typen
     }
 }
 
+// fp32 from the 8-bit form on rows that are not aligned is held to 64 registers, four CTAs per
+// SM: 12608 x 3071 GELU 91 us, 97 with the 66 that it would take; SiLU 76.6 and 80.7.  From u,
+// SiLU is slower for it (98.7 and 92.8).
 template <int KIND, int TYPE, Rows ROWS, bool FROM8>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, FROM8 && TYPE == NOVAK_TYPE_F32 && ROWS == kAny ? 4 : 0)
 novak_activation_backward_kernel(const typename Elem<TYPE>::T *da, int64_t da_stride, const typename Elem<TYPE>::T *u,
                                  int64_t u_stride, Codes uc, typename Elem<TYPE>::T *du, int64_t du_stride, Place p)
 {
@@ -251,7 +295,7 @@ novak_activation_backward_kernel(const typename Elem<TYPE>::T *da, int64_t da_st
                 F2 g[4];
                 raw[i].eight().get(g);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[k] = g[k] * act_slope<KIND>(v[k]);
+                for (int k = 0; k < 4; ++k) v[k] = g[k] * act_slope<KIND, TYPE>(v[k]);
             }
             Eight<TYPE> out;
             out.set(v);

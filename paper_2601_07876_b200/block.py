@@ -35,13 +35,22 @@ def _linear(x, weight, bias):
     return torch.nn.functional.linear(x, weight.to(x.dtype), None if bias is None else bias.to(x.dtype))
 
 
+def _recorded_linear(x, weight, bias, weight_trained):
+    """The same where a backward pass is to come, which has to be able to take up its types."""
+    if weight_trained:
+        ops._type(weight.dtype, "weight")
+    y = _linear(x, weight, bias)
+    ops._type(y.dtype, "the output (under autocast)")
+    return y
+
+
 def _linear_backward(dy, kept, weight, needs, affine=None):
     """(dx, dW, db) of a linear layer whose input was kept in 8 bits."""
     dw = db = None
     if needs[1]:
         dw, db = ops.linear_weight_grad(dy, kept, affine=affine, bias=needs[2], dtype=weight.dtype)
     elif needs[2]:
-        db = dy.reshape(-1, dy.shape[-1]).sum(0, dtype=torch.float32).to(weight.dtype)
+        db = dy.reshape(-1, dy.shape[-1]).sum(0, dtype=torch.float32)
     return (torch.matmul(dy, weight.to(dy.dtype)) if needs[0] else None), dw, db
 
 
@@ -53,7 +62,7 @@ class _NormLinear(torch.autograd.Function):
         h, _, rstd, kept = ops.layer_norm(x, gamma, beta, eps, checkpoint=keep)
         ctx.save_for_backward(kept.buffer if keep else None, rstd, gamma, beta, weight)
         ctx.width = x.shape[-1]
-        return _linear(h, weight, bias)
+        return _recorded_linear(h, weight, bias, ctx.needs_input_grad[3])
 
     @staticmethod
     @once_differentiable
@@ -66,7 +75,7 @@ class _NormLinear(torch.autograd.Function):
         dx = dgamma = dbeta = None
         if norm:
             dx, dgamma, dbeta = ops.layer_norm_backward(dh, kept, rstd, gamma, grad_dtype=gamma.dtype)
-        return dx, dgamma, dbeta, dw, db, None
+        return dx, dgamma, None if beta is None else dbeta, dw, db, None
 
 
 class _ActLinear(torch.autograd.Function):
@@ -75,7 +84,7 @@ class _ActLinear(torch.autograd.Function):
         a, kept_u, kept_a = ops.activation(_dense(u), kind, *ctx.needs_input_grad[:2])
         ctx.save_for_backward(*(None if kept is None else kept.buffer for kept in (kept_u, kept_a)), weight)
         ctx.width, ctx.kind = u.shape[-1], kind
-        return _linear(a, weight, bias)
+        return _recorded_linear(a, weight, bias, ctx.needs_input_grad[1])
 
     @staticmethod
     @once_differentiable
@@ -93,7 +102,7 @@ def _recorded(*inputs):
 
 def norm_linear(x, gamma, beta, weight, bias=None, eps: float = 1e-5):
     """linear(layer_norm(x, gamma, beta), weight, bias), kept in 8 bits for the backward pass
-    (where there is one to come)."""
+    (where there is one to come).  beta and bias may be None."""
     if not _recorded(x, gamma, beta, weight, bias):
         return _linear(ops.layer_norm(_dense(x), gamma, beta, eps)[0], weight, bias)
     return _NormLinear.apply(x, gamma, beta, weight, bias, eps)

@@ -205,8 +205,10 @@ def linear_weight_grad(dy, kept: Act8, affine=None, bias: bool = True, dtype=tor
     n_out) and the 8-bit form of its input (rows x n_in): dW (n_out x n_in) = dy^T h,
     db = the sum of dy's rows (None without ``bias``), both of ``dtype``.  With ``affine``
     = (weight, bias) of a layer norm, ``kept`` is that norm's xhat and
-    h = xhat weight + bias, the layer norm's output."""
+    h = xhat weight + bias, the layer norm's output; its bias may be None."""
     weight, beta = (None, None) if affine is None else affine
+    if weight is not None and beta is None:
+        beta = torch.zeros_like(weight)
     return _calls.linear_weight_grad(dy, kept, weight, beta, bias, _type(dtype, "dtype"))
 
 

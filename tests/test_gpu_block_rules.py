@@ -157,3 +157,46 @@ def test_a_bias_alone_of_one_row_and_of_none(block, calls):
     assert torch.equal(one, torch.arange(96.0, device="cuda"))
     none, = torch.autograd.grad(layer(torch.empty(0, 64, device="cuda")), [layer.bias], torch.empty(0, 96, device="cuda"))
     assert torch.equal(none, torch.zeros(96, device="cuda"))
+
+
+# ---- what the backward pass could not take up ------------------------------------------
+def test_a_norm_without_bias(block):
+    """As one whose bias is zeros, to the bit."""
+    x = torch.randn(300, 64, device="cuda", requires_grad=True)
+    gamma = torch.randn(64, device="cuda", requires_grad=True)
+    weight = torch.randn(96, 64, device="cuda", requires_grad=True)
+    results = []
+    for beta in (None, torch.zeros(64, device="cuda")):
+        y = block.norm_linear(x, gamma, beta, weight)
+        results.append((y, *torch.autograd.grad(y, [x, gamma, weight], torch.ones_like(y))))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    kept = block.ops.act8_pack(x.detach())
+    dy, w = torch.randn(300, 96, device="cuda"), gamma.detach()
+    without = block.ops.linear_weight_grad(dy, kept, affine=(w, None))
+    assert all(torch.equal(a, b) for a, b in zip(without, block.ops.linear_weight_grad(dy, kept, affine=(w, 0 * w))))
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float64])
+def test_types_that_the_backward_pass_does_not_take_are_refused_before_it(block, dtype):
+    for layer, width in layers(block):
+        if hasattr(layer, "weight"):
+            layer.weight.data = layer.weight.data.to(dtype)
+        else:
+            layer.down.weight.data = layer.down.weight.data.to(dtype)
+        x = torch.randn(20, width, device="cuda")
+        with pytest.raises(TypeError, match="weight"):
+            layer(x)
+        with torch.no_grad():
+            assert layer(x).dtype == torch.float32
+
+
+def test_autocast(block):
+    """bf16: taken; fp16: refused, and not only by the backward pass."""
+    for layer, width in layers(block):
+        x = torch.randn(20, width, device="cuda", requires_grad=True)
+        with torch.autocast("cuda", torch.float16), pytest.raises(TypeError, match="autocast"):
+            layer(x)
+        with torch.autocast("cuda", torch.bfloat16):
+            y = layer(x)
+        y.float().sum().backward()
+        assert x.grad.dtype == torch.float32 and torch.isfinite(x.grad).all()

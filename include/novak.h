@@ -735,9 +735,9 @@ int novak_activation_backward(const void *d_da, int64_t da_stride, const void *d
  * dy of `type`; dW (dense) and db (may be NULL) of grad_type.  Products with a
  * bf16 dy are exact and summed in fp32 on the tensor cores; an fp32 dy is taken
  * as the sum of three bf16 parts, which hold its 24 bits.
- * d_work: novak_linear_weight_grad_bytes(...) bytes, 256-byte aligned (0 bytes: may be NULL); its contents need not be
- * anything and are nothing afterwards.  Up to 2^31 - 1 rows, 2^22 outputs and
- * inputs. */
+ * d_work: novak_linear_weight_grad_bytes(...) bytes, 256-byte aligned (0 bytes:
+ * may be NULL); its contents need not be anything and are nothing afterwards.  Up
+ * to 2^31 - 1 rows, 2^22 outputs and inputs (beyond: 0 bytes, and a refusal). */
 size_t novak_linear_weight_grad_bytes(const void *d_dy, int64_t dy_stride, int type, int64_t rows,
                                       int64_t n_out, int64_t n_in);
 int novak_linear_weight_grad(const void *d_dy, int64_t dy_stride, int type, const int8_t *d_codes,

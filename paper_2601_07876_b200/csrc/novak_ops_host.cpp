@@ -90,14 +90,19 @@ Codes form(const int8_t *c, const uint8_t *e) { return Codes{const_cast<int8_t *
         if (check_rc != NOVAK_OK) return check_rc; \
     } while (0)
 
+int check_weight_grad_sizes(int64_t rows, int64_t n_out, int64_t n_in)
+{
+    CHECK(check_shape(rows, n_out));
+    CHECK(check_shape(rows, n_in));
+    if (rows > INT32_MAX || n_out > (1 << 22) || n_in > (1 << 22))
+        return refuse("sizes of up to 2^31 - 1 rows and 2^22 inputs and outputs are taken");
+    return NOVAK_OK;
+}
+
 int check_weight_grad(const WeightGradArgs &a, size_t work_bytes)
 {
     if (!is_type(a.type)) return refuse("bad type");
-    CHECK(check_shape(a.rows, a.n_out));
-    CHECK(check_shape(a.rows, a.n_in));
-    CHECK(check_shape(a.n_out, a.n_in));
-    if (a.rows > INT32_MAX || a.n_out > (1 << 22) || a.n_in > (1 << 22) || a.n_out < 1)
-        return refuse("sizes of up to 2^31 - 1 rows and 2^22 inputs and outputs are taken");
+    CHECK(check_weight_grad_sizes(a.rows, a.n_out, a.n_in));
     CHECK(check_mat("dy", a.dy, a.type, a.rows, a.n_out));
     CHECK(check_codes("x", a.codes, a.rows, true));
     if ((a.weight != nullptr) != (a.bias != nullptr)) return refuse("the norm's weight and bias come together");
@@ -252,8 +257,7 @@ int novak_activation_backward(const void *d_da, int64_t da_stride, const void *d
 size_t novak_linear_weight_grad_bytes(const void *d_dy, int64_t dy_stride, int type, int64_t rows,
                                       int64_t n_out, int64_t n_in)
 {
-    if (!is_type(type) || check_shape(rows, n_out) != NOVAK_OK || check_shape(rows, n_in) != NOVAK_OK ||
-        check_shape(n_out, n_in) != NOVAK_OK) return 0;
+    if (!is_type(type) || check_weight_grad_sizes(rows, n_out, n_in) != NOVAK_OK) return 0;
     return weight_grad_bytes(mat(d_dy, dy_stride), type, rows, n_out, n_in);
 }
 

@@ -182,6 +182,8 @@ __global__ void __launch_bounds__(32 * forward_warps<G, NV>()) novak_layer_norm_
         }
         s[0] = sum.lo() + sum.hi();
         row_sums<G, 1>(s, scratch, turn);
+        // (to 2 ulp.  A root and a division, as for long rows, cost 0.4 us of 12 and leave as many of
+        // xhat's codes on the other side of halfway: of 58 million 72, this 73, torch's operations 80)
         const float rstd = rsqrtf(fmaf(s[0], inv_cols, a.eps));
         if (t == 0) {
             if (a.mean) a.mean[row] = mean;
@@ -531,7 +533,10 @@ novak_layer_norm_finish_kernel(const float *work, int64_t splits, int64_t cols, 
 }
 
 // How a row of `cols` elements is spread: G threads, NV groups of 8 each.  false: too
-// long for registers.  Rows that are not aligned need more registers per group.
+// long for registers.  Rows that are not aligned need more registers per group, and threads
+// without elements cost what the others do (bf16, forward with the 8-bit form left and back:
+// 12608 x 771 with 128 threads 25.5 and 27.1 us, with 512 112 and 84; 8000 x 2051 with 512 of one
+// group 75 and 60, of two 100 and 105).
 struct Spread {
     int g, nv;
 };
@@ -555,7 +560,8 @@ template <int N> bool spread_for(const Spread (&from)[N], int64_t cols, Spread &
 // CTAs of the backward pass, each of which leaves one partial sum per column: one per SM
 // where its warps have a row each, else what hides a row's latency (12608 x 2048 bf16:
 // one of 256 threads per SM 65 us, two 44, three 56, whose partial sums cost more than
-// they hide; 8000 x 4096 bf16: one of 512 threads 54, two of 256 51).
+// they hide; 8000 x 4096 bf16: one of 512 threads 54, two of 256 51; 12608 x 771 bf16, 128
+// threads: two 36.7, four 27.1, eight 31.9).
 int64_t back_ctas(const Spread &s, int64_t rows)
 {
     const int per_sm = s.g == 32 || s.g == 512 ? 1 : s.g == 128 ? 4 : 2;
@@ -563,20 +569,13 @@ int64_t back_ctas(const Spread &s, int64_t rows)
 }
 
 // CTAs per SM of the forward pass: what registers leave room for (4096 columns: bf16
-// 33 us with three of 256 threads, 39 with two of 512; fp32 29 and 30).
+// 33 us with three of 256 threads, 39 with two of 512; fp32 29 and 30).  Rows that are not
+// aligned: 12608 x 771 with four of 128 threads 27.6 us (fp32 42.6), with eight 25.5 (30.6), with
+// twelve 25.5 (28.9); 8000 x 2051 with one of 512 73.9, two 74.9, three 75.9; 4000 x 7001, two
+// groups per thread, with one 63.1, two 64.1.
 constexpr int forward_ctas(int type, int g, int nv)
 {
     return g == 32 ? 4 : g == 256 ? (nv == 1 ? 4 : type == NOVAK_TYPE_F32 ? 2 : 3) : 1024 / g / nv;
-}
-
-template <typename Kernel, typename Args>
-cudaError_t run(Kernel kernel, int64_t grid, int threads, int smem, const Args &a, cudaStream_t stream)
-{
-    if (smem > 40 * 1024) {         // (48 KB less the kernels' own)
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-        if (e != cudaSuccess) return e;
-    }
-    return launch(kernel, dim3(static_cast<unsigned>(grid)), threads, smem, stream, a);
 }
 
 template <int TYPE> cudaError_t forward(const NormArgs &a, const Spread &s, bool aligned, cudaStream_t stream)
@@ -585,7 +584,8 @@ template <int TYPE> cudaError_t forward(const NormArgs &a, const Spread &s, bool
     if (s.g == G && s.nv == NV && aligned == ALIGNED) {                                                               \
         constexpr int warps = forward_warps<G, NV>(), rows = G == 32 ? warps : 1;                                     \
         const int64_t grid = std::min<int64_t>((a.rows + rows - 1) / rows, kSms * forward_ctas(TYPE, G, NV));         \
-        return run(novak_layer_norm_kernel<TYPE, G, NV, ALIGNED>, grid, 32 * warps, 0, a, stream);                    \
+        return launch(novak_layer_norm_kernel<TYPE, G, NV, ALIGNED>, dim3(static_cast<unsigned>(grid)), 32 * warps,   \
+                      0, stream, a);                                                                                  \
     }
     NOVAK_SPREADS(NOVAK_CASE)
 #undef NOVAK_CASE
@@ -597,9 +597,10 @@ cudaError_t backward(const NormBackArgs &a, const Spread &s, bool aligned, int64
 {
 #define NOVAK_CASE(G, NV, ALIGNED)                                                                                    \
     if (s.g == G && s.nv == NV && aligned == ALIGNED) {                                                               \
-        constexpr int warps = backward_warps<G, NV>();                                                                \
-        return run(novak_layer_norm_back_kernel<TYPE, G, NV, ALIGNED, FROM8>, grid, 32 * warps,                       \
-                   G == 32 ? (1 + warps) * NV * 256 * 4 : 0, a, stream);                                              \
+        constexpr int warps = backward_warps<G, NV>(), smem = G == 32 ? (1 + warps) * NV * 256 * 4 : 0;               \
+        static_assert(smem <= 40 * 1024, "48 KB without asking, less the kernel's own");                              \
+        return launch(novak_layer_norm_back_kernel<TYPE, G, NV, ALIGNED, FROM8>, dim3(static_cast<unsigned>(grid)),   \
+                      32 * warps, smem, stream, a);                                                                   \
     }
     NOVAK_SPREADS(NOVAK_CASE)
 #undef NOVAK_CASE

@@ -176,7 +176,7 @@ struct Cut {
 struct Piece {
     int tile;
     int first, count;       // steps
-    int slot;               // in the workspace, of a piece that is not the whole tile
+    int slot;               // in the workspace, of a tile left over (used where the piece is not all of it)
     bool whole;
 };
 
@@ -217,6 +217,7 @@ struct Walk {
             p.tile = wave * c.pairs + pair;
             p.first = 0;
             p.count = c.steps;
+            p.slot = 0;
             ++wave;
         } else if (pos < end) {
             const int r = rest_tile(c, pos);

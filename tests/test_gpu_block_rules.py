@@ -55,6 +55,20 @@ def test_what_is_kept_goes_with_the_backward_pass(block):
         assert kept > rows * width and after < kept / 20, (kept, after)
 
 
+def test_nothing_is_kept_but_the_8_bit_forms(block):
+    """The allocator counts at most 1 MiB more for each of the four tensors that are kept; the norm's output or the
+    hidden layer, kept in bf16 as well, would be 25 or 75 MB."""
+    rows, width, hidden = 16384, 768, 2304
+    b = block.MlpBlock8(width, hidden)
+    x = torch.randn(rows, width, device="cuda").to(torch.bfloat16).requires_grad_()
+    b(x)
+    before = allocated()
+    y = b(x)
+    kept = allocated() - before - y.numel() * 2
+    forms = rows * (width + 2 * hidden) * 33 // 32
+    assert forms <= kept <= forms + 8 * rows + 5 * 2 ** 20, (kept, forms)
+
+
 def test_saved_tensor_hooks_see_what_is_kept(block):
     """Kept on the host between the passes: the same gradients, and next to nothing on the device meanwhile."""
     torch.manual_seed(0)

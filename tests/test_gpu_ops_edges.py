@@ -136,3 +136,21 @@ def test_gelu_in_fp32_is_as_good_as_the_formula_in_fp32(ops, lo, hi):
     want = R.act_slope("gelu", u)
     plain = cdf + u * torch.exp(-0.5 * u * u) * (1 / math.sqrt(2 * math.pi))
     assert off(ops.activation_backward(torch.ones_like(u), u, "gelu"), want) <= 1.1 * off(plain, want)
+
+
+# ---- more rows than a grid's second dimension holds --------------------------------------
+@pytest.mark.parametrize("cols", [33, 40])
+def test_more_rows_than_the_grid_has_places_for(ops, cols):
+    """1.1 million rows, 16 to a CTA: the CTAs go on with further rows.  Rows know nothing of one another, so that the
+    last ones on their own give the same bits."""
+    rows, part = 1_100_000, slice(1_000_000, None)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    u = torch.empty(rows, cols, device="cuda").normal_(generator=g).to(BF16)
+    da = torch.empty(rows, cols, device="cuda").normal_(generator=g).to(BF16)
+    a, kept_u, kept_a = ops.activation(u, "gelu", save_output=True)
+    du, back = ops.activation_backward(da, kept_u, "gelu"), ops.act8_unpack(kept_a)
+    few, few_u, few_a = ops.activation(u[part].contiguous(), "gelu", save_output=True)
+    assert torch.equal(a[part], few) and torch.equal(kept_u.codes[part], few_u.codes)
+    assert torch.equal(kept_a.exps[part], few_a.exps) and torch.equal(back[part], ops.act8_unpack(few_a))
+    assert torch.equal(du[part], ops.activation_backward(da[part].contiguous(), few_u, "gelu"))
+    assert torch.equal(ops.act8_pack(u).codes, kept_u.codes)

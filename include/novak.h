@@ -646,7 +646,9 @@ const char *novak_last_error(const novak_opt *opt);
  * elements behind the one before (stride >= cols; it may be anything where
  * rows <= 1); its base is aligned to its element.  rows = 0 is allowed and
  * leaves weight gradients of zeros.  Bases aligned to 16 bytes with strides of a
- * multiple of 16 bytes run on 128-bit accesses, others element by element.
+ * multiple of 16 bytes (and, but for the weight gradient, rows of a multiple of 8
+ * elements) run fastest: others are read and written as the aligned pieces that
+ * hold them and shifted, layer norm's rows of more than 8192 elements one by one.
  * Statistics and sums are held in fp32; a result is rounded once, to nearest
  * even, where it is stored as bf16. */
 enum { NOVAK_TYPE_F32 = 0, NOVAK_TYPE_BF16 = 1 };

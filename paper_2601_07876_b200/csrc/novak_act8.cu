@@ -7,7 +7,7 @@
 // 16 bytes and a block's maximum is two shuffles; two such groups per thread, both loaded
 // first.  Bound by HBM where rows are 16-byte aligned: 8192 x 4096 bf16 packed in 15.8 us
 // (6.42 TB/s) and unpacked in 14.8 (6.86, some of it out of L2); 12608 x 3072 bf16 through
-// GELU with both forms left in 39.5 us (5.95 TB/s), back in 31.3 (6.23).  Rows that are
+// GELU with both forms left in 39.5 us (5.95 TB/s), back in 30.2 (6.46).  Rows that are
 // not aligned are bound by the shifting of what they load and store, 410 instructions
 // per warp and group of 8 at 77 % of the issue slots: 12608 x 3071 bf16 72 and 65 us,
 // 8192 x 4095 packed in 26.8, unpacked in 29.8.  A small matrix is a launch: 197 x 1000
@@ -199,7 +199,7 @@ __device__ __forceinline__ void put(const Codes &c, int64_t at, bool in, const F
 enum Rows { kFlat, kAligned, kAny };
 
 // bf16 in one run is held to 32 registers, with which every thread that an SM has room for
-// is there: GELU of 12608 x 3072 39.5 us, 40.2 with the 36 that it would take.  (0: no bound.)
+// is there: GELU of 12608 x 3072 39.5 us, 40.2 with those that it would take.  (0: no bound.)
 template <int KIND, int TYPE, Rows ROWS>
 __global__ void __launch_bounds__(kThreads, TYPE == NOVAK_TYPE_BF16 && ROWS == kFlat ? 2048 / kThreads : 0)
 novak_activation_kernel(const typename Elem<TYPE>::T *u, int64_t u_stride, typename Elem<TYPE>::T *a, int64_t a_stride,

@@ -12,13 +12,13 @@
 // Up to 1024 elements a row is a warp's and needs no barrier; wider ones are 256 or 512
 // threads'.  What bounds them is not bytes but what a row has to wait for, its load, two
 // sums over its threads one after the other, at the occupancy that its registers leave:
-//   forward with the 8-bit form left: 12608 x 768 bf16 12.1 us (4.0 TB/s; without it 10.0),
-//   8000 x 4096 bf16 32.8 (5.0), 4099 x 4096 fp32 29.0 (5.2);
-//   backward: 12608 x 768 bf16 13.0 us (3.7 TB/s; 16.9 when nothing is in L2), 8000 x 4096
-//   bf16 48 (3.4), 4099 x 4096 fp32 from x 43 (4.7), 5 to 6 us of each for the last sums of
-//   dw and db.  (4096 columns: 282 instructions per warp and row at 40 % of the issue
+//   forward with the 8-bit form left: 12608 x 768 bf16 12.6 us (3.9 TB/s), 8000 x 4096 bf16 32.2
+//   (5.1), 4099 x 4096 fp32 28.5 (5.3);
+//   backward: 12608 x 768 bf16 11.8 us (4.1 TB/s; 18.4 with other inputs each time), 8000 x 4096
+//   bf16 50 (3.2), 4099 x 4096 fp32 from x 41.4 (4.9), 5 to 6 us of each for the last sums of
+//   dw and db (single calls, one after the other on the same inputs).  (4096 columns: 282 instructions per warp and row at 40 % of the issue
 //   slots; stalls on loads, shuffles, barriers and the load queue in like parts.)
-//   Not aligned: 12608 x 771 bf16 26.8 and 28.2 us.  Long: 2000 x 20000 bf16 123 and 181.
+//   Not aligned: 12608 x 771 bf16 25.4 and 27.1 us.  Long: 2000 x 20000 bf16 122 and 186.
 //   One row of 768: 3.6 us.
 #include <algorithm>
 

@@ -23,9 +23,10 @@
 // are left over are cut evenly over all pairs, partial tiles going to a
 // workspace that novak_weight_grad_finish_kernel adds up in a fixed order.
 //
-// What bounds it: 16384 x 4096 -> 4096 bf16 takes 469 us (1173 TFLOP/s; 530 where the power
-// limit holds the clock down), the products with every wait but without filling x about
-// 360: a step's 64 rows are 16 KB of dy and 24 KB of codes and x through each SM's shared
+// What bounds it (single calls, the same inputs again and again, clocks high; with other
+// inputs each time and one call behind the other 16384 x 4096 -> 4096 is 545 us and 12608 x 768 ->
+// 2304 with db and a norm 70): 16384 x 4096 -> 4096 bf16 takes 469 us (1173 TFLOP/s), the
+// products with every wait but without filling x about 360: a step's 64 rows are 16 KB of dy and 24 KB of codes and x through each SM's shared
 // memory besides the 48 KB that the products read, close to what it can deliver.
 // 12608 x 768 -> 2304 bf16: 46 us (970 TFLOP/s), of which the partial tiles' way through
 // memory takes 5; with db or a layer norm 60, since dy is read once more (sums inside

@@ -768,6 +768,116 @@ int novak_selftest_weight_grad_wait(const void *d_dy, int64_t dy_stride, int typ
                                     size_t work_bytes, int64_t rows, int64_t n_out, int64_t n_in, int pair,
                                     uint64_t wait_ns, void *stream);
 
+/* Root-mean-square norm over the columns, with the residual's addition in front:
+ *     h = x + residual (rounded to `type`; d_residual NULL: h = x),
+ *     rstd = 1 / sqrt(sum(h^2) / cols + eps), xhat = h rstd, y = xhat weight.
+ * x, residual, h and y of `type`; weight (cols elements) of param_type; d_rstd
+ * (rows fp32) may be NULL.  d_h comes with d_residual (both or neither).  d_codes,
+ * d_exps (both or neither): the 8-bit form of xhat, from which the backward pass
+ * and the weight gradient of a linear layer behind the norm (its d_weight with a
+ * d_bias of zeros) are formed.  h may be x or residual, y may be x (in place); y
+ * and h may not be one.  eps >= 0 and finite. */
+int novak_rms_norm(const void *d_x, int64_t x_stride, const void *d_residual, int64_t residual_stride,
+                   void *d_h, int64_t h_stride, void *d_y, int64_t y_stride, int type,
+                   const void *d_weight, int param_type, double eps, float *d_rstd, int8_t *d_codes,
+                   uint8_t *d_exps, int64_t rows, int64_t cols, void *stream);
+
+/* Its backward pass.  With g = dy weight and dh (d_dh; NULL: 0) the gradient that
+ * reaches h by other ways than the norm:
+ *     dx = dh + rstd (g - xhat mean(g xhat)),  dweight = sum over rows of dy xhat;
+ * dx is the gradient of x and of the residual.  xhat comes from d_codes, d_exps
+ * (d_h NULL) or is h rstd (d_codes and d_exps NULL).  dy, dh, h and dx of `type`;
+ * weight of param_type; dweight (may be NULL) of grad_type.  dx may be dy or dh (in
+ * place).  d_work: novak_rms_norm_backward_bytes(rows, cols) bytes, 16-byte aligned;
+ * its contents need not be anything and are nothing afterwards. */
+size_t novak_rms_norm_backward_bytes(int64_t rows, int64_t cols);
+int novak_rms_norm_backward(const void *d_dy, int64_t dy_stride, const void *d_dh, int64_t dh_stride,
+                            const void *d_h, int64_t h_stride, int type, const float *d_rstd,
+                            const int8_t *d_codes, const uint8_t *d_exps, const void *d_weight,
+                            int param_type, void *d_dx, int64_t dx_stride, void *d_dweight,
+                            int grad_type, void *d_work, size_t work_bytes, int64_t rows,
+                            int64_t cols, void *stream);
+
+/* Token embedding: out[t] = scale table[ids[t]], t < tokens.  ids (dense) of
+ * id_type; an id outside [0, vocab) stands for no token: its row of out is zeros,
+ * and it takes no part in the gradient.  table: vocab rows of cols elements of
+ * table_type; out of out_type; the product is rounded once.  scale: finite, taken
+ * in fp32.  Up to 2^31 - 1 tokens and 2^31 - 1 rows of the table. */
+enum { NOVAK_ID_I32 = 0, NOVAK_ID_I64 = 1 };
+int novak_embedding(const void *d_ids, int id_type, const void *d_table, int64_t table_stride,
+                    int table_type, double scale, void *d_out, int64_t out_stride, int out_type,
+                    int64_t tokens, int64_t vocab, int64_t cols, void *stream);
+
+/* Its gradient: dtable[v] = scale sum of dout[t] over the t with ids[t] = v, rows
+ * that no id names being zeros; with `add` not 0 that sum is added to what dtable
+ * holds (in fp32, rounded once), and rows that no id names stay as they are.  dout
+ * of `type`, dtable of grad_type.  Tokens of one id are summed in fp32 in an order that
+ * goes by their places alone.  d_work: novak_embedding_grad_bytes(tokens, vocab,
+ * cols) bytes, 256-byte aligned; its contents need not be anything and are nothing
+ * afterwards. */
+size_t novak_embedding_grad_bytes(int64_t tokens, int64_t vocab, int64_t cols);
+int novak_embedding_grad(const void *d_dout, int64_t dout_stride, int type, const void *d_ids,
+                         int id_type, double scale, void *d_dtable, int64_t dtable_stride,
+                         int grad_type, int add, void *d_work, size_t work_bytes, int64_t tokens,
+                         int64_t vocab, int64_t cols, void *stream);
+
+/* Orthogonalised updates of n matrices by Newton-Schulz products.  For each matrix G
+ * (rows[i] x cols[i], of `type`, row stride g_stride[i]):
+ *     X = G / max(|G|, eps), |G| the Frobenius norm (G = 0: X = 0), and then, for
+ *     each of the `steps` triples (a, b, c) of `coefficients`,
+ *     A = X X^T, X <- a X + (b A + c A^2) X   (A = X^T X and X <- a X + X (b A + c A^2)
+ *     where G has more rows than columns, which is the same),
+ * and X goes out as bf16 (row stride out_stride[i]).  A matrix that holds an
+ * infinity or a NaN gives NaNs, and touches no other.  The polynomials have to keep
+ * singular values in [0, 4] and their b t + c t^2 in [-15, 15] (t a squared singular
+ * value), starting from [0, 1], or the call is refused; 1 to 32 steps.
+ *
+ * Products run on the tensor cores on operands rounded to fp16 (11 bits; scaled by
+ * powers of two, so that nothing is lost to its range that matters), summed in fp32.
+ * X itself is held in 22 bits beside that, and the diagonals of A and of b A + c A^2
+ * in fp32, so that small singular values, which the steps make large, are not drowned
+ * in what the large ones were rounded by: with (3.4445, -4.7750, 2.0315) five times,
+ * X is within about 2e-3 of its norm of the exact one before it is rounded to bf16,
+ * whatever G's singular values are.
+ *
+ * d_g, g_stride, d_out, out_stride, rows, cols, coefficients: HOST arrays, read before
+ * the call returns.  Matrices without rows or columns are passed over.  Up to 2^16
+ * rows and columns and 2^14 matrices.  d_work: novak_orthogonalize_bytes(rows, cols, n)
+ * bytes, 256-byte aligned (0 where that is too much); its contents need not be
+ * anything and are nothing afterwards.  out may not overlap any G. */
+size_t novak_orthogonalize_bytes(const int64_t *rows, const int64_t *cols, int n);
+int novak_orthogonalize(const void *const *d_g, const int64_t *g_stride, int type, void *const *d_out,
+                        const int64_t *out_stride, const int64_t *rows, const int64_t *cols, int n,
+                        const double *coefficients, int steps, double eps, void *d_work,
+                        size_t work_bytes, void *stream);
+
+/* One step of momentum with orthogonalised updates for n matrices, in place:
+ *     m <- momentum m + g,  G = g + momentum m (nesterov not 0) or m,
+ *     theta <- decay theta - step[i] X,
+ * X that of novak_orthogonalize for G (not rounded to bf16).  theta and m: dense fp32,
+ * g: dense, of grad_type.  step: HOST array (learning rate times the matrix's scale);
+ * momentum in [0, 1), decay and step finite.  The other arguments and d_work as in
+ * novak_orthogonalize. */
+int novak_orthogonal_step(float *const *d_theta, const void *const *d_g, int grad_type,
+                          float *const *d_m, const int64_t *rows, const int64_t *cols, int n,
+                          double momentum, int nesterov, const double *step, double decay,
+                          const double *coefficients, int steps, double eps, void *d_work,
+                          size_t work_bytes, void *stream);
+
+/* The kernel of the two calls above has warps that wait for one another's copies,
+ * products and tiles.  Each wait is bounded (two seconds); where one runs out, which
+ * is a fault of this library or of the device, every output of the call (X, or theta)
+ * is filled with NaNs, and the count of novak_ops_gave_up goes up.  Test hook for
+ * that: novak_orthogonalize with a limit of wait_ns on each wait (0: the usual one)
+ * and with the end of tile number `withheld` never announced (of tiles counted from 0
+ * in the order in which they are begun; -1: none). */
+int novak_selftest_orthogonalize_wait(const void *const *d_g, const int64_t *g_stride, int type,
+                                      void *const *d_out, const int64_t *out_stride,
+                                      const int64_t *rows, const int64_t *cols, int n,
+                                      const double *coefficients, int steps, double eps, void *d_work,
+                                      size_t work_bytes, int64_t withheld, uint64_t wait_ns,
+                                      void *stream);
+
 /* Text of the last error of a training operator on the calling thread ("" if
  * none).  Valid until the thread's next such call. */
 const char *novak_ops_error(void);

@@ -35,6 +35,7 @@ NOVAK_LOOKAHEAD_LAST, NOVAK_LOOKAHEAD_TRAJ_MEAN = 0, 1
 NOVAK_MOMENT_F32, NOVAK_MOMENT_BF16 = 0, 1
 NOVAK_TYPE_F32, NOVAK_TYPE_BF16 = 0, 1
 NOVAK_ACT_GELU, NOVAK_ACT_GELU_TANH, NOVAK_ACT_SILU = range(3)
+NOVAK_ID_I32, NOVAK_ID_I64 = 0, 1
 NOVAK_WARN_TRUE_DOWNGRADED, NOVAK_WARN_SCALAR_PATH, NOVAK_WARN_NARROW_GRADIENT = 1, 2, 4
 
 _STATUS = {0: "NOVAK_OK", 1: "NOVAK_EINVAL", 2: "NOVAK_ESTATE", 3: "NOVAK_ECUDA", 4: "NOVAK_ENOMEM"}
@@ -83,7 +84,8 @@ class NovakError(RuntimeError):
 
 _lib = None
 _OPTIONAL_ELSEWHERE = ("novak_build_", "novak_act8_", "novak_layer_norm", "novak_activation",
-                       "novak_linear_weight_grad", "novak_ops_", "novak_selftest_weight_grad")
+                       "novak_linear_weight_grad", "novak_ops_", "novak_selftest_weight_grad",
+                       "novak_rms_norm", "novak_embedding", "novak_orthogonal", "novak_selftest_orthogonalize")
 
 
 def load_library(path: str | None = None) -> ctypes.CDLL:
@@ -163,6 +165,23 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
                                              vp, c_size_t, c_int64, c_int64, c_int64, vp]),
         "novak_selftest_weight_grad_wait": (c_int, [vp, c_int64, c_int, vp, vp, vp, vp, c_int, vp, vp, c_int,
                                                     vp, c_size_t, c_int64, c_int64, c_int64, c_int, c_uint64, vp]),
+        "novak_rms_norm": (c_int, [vp, c_int64, vp, c_int64, vp, c_int64, vp, c_int64, c_int, vp, c_int,
+                                   c_double, vp, vp, vp, c_int64, c_int64, vp]),
+        "novak_rms_norm_backward_bytes": (c_size_t, [c_int64, c_int64]),
+        "novak_rms_norm_backward": (c_int, [vp, c_int64, vp, c_int64, vp, c_int64, c_int, vp, vp, vp, vp,
+                                            c_int, vp, c_int64, vp, c_int, vp, c_size_t, c_int64, c_int64, vp]),
+        "novak_embedding": (c_int, [vp, c_int, vp, c_int64, c_int, c_double, vp, c_int64, c_int, c_int64,
+                                    c_int64, c_int64, vp]),
+        "novak_embedding_grad_bytes": (c_size_t, [c_int64, c_int64, c_int64]),
+        "novak_embedding_grad": (c_int, [vp, c_int64, c_int, vp, c_int, c_double, vp, c_int64, c_int, c_int,
+                                         vp, c_size_t, c_int64, c_int64, c_int64, vp]),
+        "novak_orthogonalize_bytes": (c_size_t, [vp, vp, c_int]),
+        "novak_orthogonalize": (c_int, [vp, vp, c_int, vp, vp, vp, vp, c_int, vp, c_int, c_double, vp,
+                                        c_size_t, vp]),
+        "novak_orthogonal_step": (c_int, [vp, vp, c_int, vp, vp, vp, c_int, c_double, c_int, vp, c_double,
+                                          vp, c_int, c_double, vp, c_size_t, vp]),
+        "novak_selftest_orthogonalize_wait": (c_int, [vp, vp, c_int, vp, vp, vp, vp, c_int, vp, c_int,
+                                                      c_double, vp, c_size_t, c_int64, c_uint64, vp]),
         "novak_ops_gave_up": (c_int, [POINTER(c_uint32), vp]),
         "novak_ops_error": (c_char_p, []),
     }

@@ -68,6 +68,89 @@ struct NormBackArgs {
 size_t layer_norm_backward_bytes(int64_t rows, int64_t cols);
 cudaError_t launch_layer_norm_backward(const NormBackArgs &a, cudaStream_t stream);
 
+// novak_rms_norm.cu
+struct RmsArgs {
+    Mat x, residual, h, y;      // residual and h: both or neither
+    int type;
+    const void *weight;
+    int param_type;
+    float eps;
+    float *rstd;
+    Codes codes;
+    int64_t rows, cols;
+};
+cudaError_t launch_rms_norm(const RmsArgs &a, cudaStream_t stream);
+
+struct RmsBackArgs {
+    Mat dy, dh, h;              // dh may be NULL; h or codes
+    int type;
+    const float *rstd;
+    Codes codes;
+    const void *weight;
+    int param_type;
+    Mat dx;
+    void *dweight;
+    int grad_type;
+    float *work;
+    int64_t rows, cols;         // rows may be 0
+};
+size_t rms_norm_backward_bytes(int64_t rows, int64_t cols);
+cudaError_t launch_rms_norm_backward(const RmsBackArgs &a, cudaStream_t stream);
+
+// novak_embedding.cu
+struct EmbedArgs {
+    const void *ids;
+    int id_type;
+    Mat table;
+    int table_type;
+    float scale;
+    Mat out;
+    int out_type;
+    int64_t tokens, vocab, cols;
+};
+cudaError_t launch_embedding(const EmbedArgs &a, cudaStream_t stream);
+
+struct EmbedGradArgs {
+    Mat dout;
+    int type;
+    const void *ids;
+    int id_type;
+    float scale;
+    Mat dtable;
+    int grad_type, add;
+    void *work;
+    int64_t tokens, vocab, cols;    // tokens may be 0
+};
+size_t embedding_grad_bytes(int64_t tokens, int64_t vocab, int64_t cols);
+cudaError_t launch_embedding_grad(const EmbedGradArgs &a, cudaStream_t stream);
+
+// novak_orthogonalize.cu
+constexpr int kMostSteps = 32;
+struct OrthArgs {               // arrays of n on the host
+    const void *const *g;
+    const int64_t *g_stride;    // NULL: dense
+    int type;
+    void *const *out;           // bf16; or NULL, and theta is stepped
+    const int64_t *out_stride;
+    const int64_t *rows, *cols;
+    int n;
+    float coefficients[kMostSteps][3];
+    int steps;
+    double eps;
+    float *const *theta, *const *m;
+    float momentum;
+    bool nesterov;
+    const double *step;
+    float decay;
+    void *work;
+    int64_t withheld = -1;      // a tile whose end is not announced (a test of the waits' limit)
+    uint64_t wait_ns = 0;       // a wait's limit; 0: the usual one
+};
+// 0: the matrices are too large or too many to be addressed.
+size_t orthogonalize_bytes(const int64_t *rows, const int64_t *cols, int n);
+cudaError_t orthogonalize_gave_up(unsigned *count, cudaStream_t stream);
+cudaError_t launch_orthogonalize(const OrthArgs &a, cudaStream_t stream);
+
 // novak_weight_grad.cu
 struct WeightGradArgs {
     Mat dy;

@@ -7,6 +7,8 @@
 // the functions are those of the library that binding.py has loaded.
 #include <Python.h>
 
+#include <vector>
+
 #include <ATen/ATen.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -145,7 +147,9 @@ Tensor new_like(const Tensor &t) { return at::empty(t.sizes(), t.options()); }
 #define NOVAK_ENTRIES(X)                                                                                               \
     X(novak_act8_pack) X(novak_act8_unpack) X(novak_layer_norm) X(novak_layer_norm_backward_bytes)                     \
     X(novak_layer_norm_backward) X(novak_activation) X(novak_activation_backward) X(novak_linear_weight_grad_bytes)    \
-    X(novak_linear_weight_grad) X(novak_ops_error)
+    X(novak_linear_weight_grad) X(novak_rms_norm) X(novak_rms_norm_backward_bytes) X(novak_rms_norm_backward)          \
+    X(novak_embedding) X(novak_embedding_grad_bytes) X(novak_embedding_grad) X(novak_orthogonalize_bytes)              \
+    X(novak_orthogonalize) X(novak_orthogonal_step) X(novak_ops_error)
 struct Api {
 #define X(f) decltype(&::f) f = nullptr;
     NOVAK_ENTRIES(X)
@@ -380,6 +384,265 @@ PyObject *linear_weight_grad(PyObject *const *args)
     return Py_BuildValue("(NN)", wrap(dw), none_or(db));
 }
 
+// A tensor of the other one's type and shape, or none.
+const Tensor *beside(PyObject *o, const char *name, const Tensor &like)
+{
+    if (is_none(o)) return nullptr;
+    const Tensor &t = tensor(o, name);
+    same(t, name, like, like.sizes());
+    if (t.scalar_type() != like.scalar_type()) {
+        PyErr_Format(PyExc_TypeError, "%s must be of the same dtype as the other arguments", name);
+        throw Refused{};
+    }
+    return &t;
+}
+
+double number(PyObject *o)
+{
+    const double x = PyFloat_AsDouble(o);
+    if (x == -1.0 && PyErr_Occurred()) throw Refused{};
+    return x;
+}
+
+// rms_norm(x, weight, residual or None, eps, checkpoint) -> (y, h, rstd, buffer or None)
+PyObject *rms_norm(PyObject *const *args)
+{
+    const Tensor &x = tensor(args[0], "x"), &weight = tensor(args[1], "weight");
+    const Rows r = rows_of(x, "x");
+    const int type = type_of(x, "x"), param = vector_type(weight, "weight", x, r.cols);
+    const Tensor *residual = beside(args[2], "residual", x);
+    const double eps = number(args[3]);
+    const int64_t residual_stride = residual ? rows_of(*residual, "residual").stride : 0;
+    const Tensor y = at::empty(x.sizes(), x.options()), h = residual ? at::empty(x.sizes(), x.options()) : x;
+    const Tensor rstd = at::empty(x.sizes().slice(0, x.dim() - 1), x.options().dtype(at::kFloat));
+    Form f;
+    Tensor both;
+    if (truth(args[4])) {
+        const NewForm n(r.rows, r.cols, x);
+        f = n.form;
+        both = n.both;
+    }
+    ENQUEUE(novak_rms_norm, x, x.data_ptr(), r.stride, residual ? residual->data_ptr() : nullptr, residual_stride,
+            residual ? h.data_ptr() : nullptr, r.cols, y.data_ptr(), r.cols, type, weight.data_ptr(), param, eps,
+            static_cast<float *>(rstd.data_ptr()), f.codes, f.exps, r.rows, r.cols);
+    return Py_BuildValue("(NNNN)", wrap(y), wrap(h), wrap(rstd), none_or(both));
+}
+
+// rms_norm_backward(dy, kept or None, h or None, rstd, weight, dh or None, gradient's type) -> (dx, dw)
+PyObject *rms_norm_backward(PyObject *const *args)
+{
+    const Tensor &dy = tensor(args[0], "dy"), &weight = tensor(args[4], "weight");
+    const Rows r = rows_of(dy, "dy");
+    const int type = type_of(dy, "dy"), param = vector_type(weight, "weight", dy, r.cols);
+    const int grad = static_cast<int>(integer(args[6]));
+    const Tensor rstd = floats(tensor(args[3], "rstd"), "rstd", dy, dy.sizes().slice(0, dy.dim() - 1));
+    const Tensor *h = beside(args[2], "h", dy), *dh = beside(args[5], "dh", dy);
+    Form f;
+    if (!h) f = form_of(args[1], r.rows, r.cols, dy, "dy");
+    const int64_t h_stride = h ? rows_of(*h, "h").stride : 0, dh_stride = dh ? rows_of(*dh, "dh").stride : 0;
+    const Tensor dx = at::empty(dy.sizes(), dy.options());
+    const Tensor dw = at::empty({r.cols}, dy.options().dtype(grad == NOVAK_TYPE_BF16 ? at::kBFloat16 : at::kFloat));
+    const size_t need = api.novak_rms_norm_backward_bytes(r.rows, r.cols);
+    const Tensor work = at::empty({static_cast<int64_t>(need)}, dy.options().dtype(at::kByte));
+    ENQUEUE(novak_rms_norm_backward, dy, dy.data_ptr(), r.stride, dh ? dh->data_ptr() : nullptr, dh_stride,
+            h ? h->data_ptr() : nullptr, h_stride, type, static_cast<const float *>(rstd.data_ptr()), f.codes, f.exps,
+            weight.data_ptr(), param, dx.data_ptr(), r.cols, dw.data_ptr(), grad, work.data_ptr(), need, r.rows, r.cols);
+    return Py_BuildValue("(NN)", wrap(dx), wrap(dw));
+}
+
+// Token ids as a dense tensor, and their type.
+Tensor ids_of(const Tensor &t, const Tensor &like, int &type)
+{
+    if (t.device() != like.device()) value_error("%s is on another device", "ids");
+    if (t.scalar_type() != at::kLong && t.scalar_type() != at::kInt) {
+        PyErr_Format(PyExc_TypeError, "ids must be int64 or int32, got %s", c10::toString(t.scalar_type()));
+        throw Refused{};
+    }
+    type = t.scalar_type() == at::kLong ? NOVAK_ID_I64 : NOVAK_ID_I32;
+    return t.contiguous();
+}
+
+// A matrix as it stands: rows of any stride.
+Rows table_of(const Tensor &t, const char *name)
+{
+    if (t.dim() != 2) value_error("%s must be a matrix", name);
+    if (t.size(0) > 0) return rows_of(t, name);
+    if (!t.is_cuda()) value_error("%s must be a CUDA tensor", name);
+    if (t.size(1) == 0) value_error("%s needs a last dimension of at least one element", name);
+    return {0, t.size(1), t.size(1)};
+}
+
+at::ScalarType scalar_of(int type) { return type == NOVAK_TYPE_BF16 ? at::kBFloat16 : at::kFloat; }
+
+// embedding(ids, table, scale, type) -> out
+PyObject *embedding(PyObject *const *args)
+{
+    const Tensor &table = tensor(args[1], "table");
+    const Rows r = table_of(table, "table");
+    const int type = type_of(table, "table"), out_type = static_cast<int>(integer(args[3]));
+    int id_type;
+    const Tensor ids = ids_of(tensor(args[0], "ids"), table, id_type);
+    const double scale = number(args[2]);
+    c10::DimVector shape(ids.sizes().begin(), ids.sizes().end());
+    shape.push_back(r.cols);
+    const Tensor out = at::empty(shape, table.options().dtype(scalar_of(out_type)));
+    ENQUEUE(novak_embedding, table, ids.data_ptr(), id_type, table.data_ptr(), r.stride, type, scale, out.data_ptr(),
+            r.cols, out_type, ids.numel(), r.rows, r.cols);
+    return wrap(out);
+}
+
+// embedding_grad(dout, ids, vocab, scale, type, out or None) -> dtable
+PyObject *embedding_grad(PyObject *const *args)
+{
+    const Tensor &dout = tensor(args[0], "dout");
+    const Rows r = rows_of(dout, "dout");
+    const int type = type_of(dout, "dout");
+    int id_type;
+    const Tensor ids = ids_of(tensor(args[1], "ids"), dout, id_type);
+    if (ids.sizes() != dout.sizes().slice(0, dout.dim() - 1)) value_error("%s has another shape than dout's leading dimensions", "ids");
+    const int64_t vocab = integer(args[2]);
+    if (vocab < 0) value_error("%s must be >= 0", "vocab");
+    const double scale = number(args[3]);
+    const bool add = !is_none(args[5]);
+    const Tensor out = add ? tensor(args[5], "out") : at::empty({vocab, r.cols}, dout.options().dtype(scalar_of(static_cast<int>(integer(args[4])))));
+    same(out, "out", dout, {vocab, r.cols});
+    const Rows o = table_of(out, "out");
+    const int64_t tokens = ids.numel();
+    const size_t need = api.novak_embedding_grad_bytes(tokens, vocab, r.cols);
+    const Tensor work = at::empty({static_cast<int64_t>(need)}, dout.options().dtype(at::kByte));
+    ENQUEUE(novak_embedding_grad, dout, dout.data_ptr(), r.stride, type, ids.data_ptr(), id_type, scale, out.data_ptr(),
+            o.stride, type_of(out, "out"), static_cast<int>(add), work.data_ptr(), need, tokens, vocab, r.cols);
+    return wrap(out);
+}
+
+// Numbers of a sequence, flattened by the caller.
+std::vector<double> numbers(PyObject *o, const char *name)
+{
+    THPObjectPtr fast(PySequence_Fast(o, name));
+    if (!fast) throw Refused{};
+    std::vector<double> v(PySequence_Fast_GET_SIZE(fast.get()));
+    for (size_t i = 0; i < v.size(); ++i) v[i] = number(PySequence_Fast_GET_ITEM(fast.get(), i));
+    return v;
+}
+
+struct Tensors {
+    THPObjectPtr fast;
+    Tensors(PyObject *o, const char *name) : fast(PySequence_Fast(o, name))
+    {
+        if (!fast) throw Refused{};
+    }
+    int64_t size() const { return PySequence_Fast_GET_SIZE(fast.get()); }
+    const Tensor &at(int64_t i, const char *name) const { return tensor(PySequence_Fast_GET_ITEM(fast.get(), i), name); }
+};
+
+// The matrices in a list of tensors: a tensor of more than two dimensions is a batch of them.
+struct Matrices {
+    std::vector<void *> ptr;
+    std::vector<int64_t> rows, cols, stride;
+    void add(const Tensor &t, const char *name)
+    {
+        if (!t.is_cuda()) value_error("%s must be CUDA tensors", name);
+        if (t.dim() < 2) value_error("%s must have two dimensions or more", name);
+        const int64_t r = t.size(-2), c = t.size(-1), bytes = t.element_size();
+        if (t.numel() == 0) return;
+        if (c > 1 && t.stride(-1) != 1) value_error("%s: the last dimension must be contiguous", name);
+        if (r > 1 && t.stride(-2) < c) value_error("%s: rows overlap", name);
+        const int64_t batch = t.numel() / (r * c);
+        for (int64_t b = 0; b < batch; ++b) {
+            int64_t left = b, at = 0;
+            for (int64_t d = t.dim() - 3; d >= 0; --d) {
+                at += left % t.size(d) * t.stride(d);
+                left /= t.size(d);
+            }
+            ptr.push_back(static_cast<char *>(t.data_ptr()) + at * bytes);
+            rows.push_back(r);
+            cols.push_back(c);
+            stride.push_back(r > 1 ? t.stride(-2) : c);
+        }
+    }
+    int count() const
+    {
+        if (ptr.size() > (1u << 14)) value_error("%s: 2^14 of them at most", "matrices");
+        return static_cast<int>(ptr.size());
+    }
+};
+
+// orthogonalize(list, coefficients, eps) -> list
+PyObject *orthogonalize(PyObject *const *args)
+{
+    const Tensors list(args[0], "a list of tensors is needed");
+    const std::vector<double> abc = numbers(args[1], "coefficients must be numbers");
+    const double eps = number(args[2]);
+    THPObjectPtr result(PyList_New(list.size()));
+    if (!result) throw Refused{};
+    Matrices g, out;
+    int type = NOVAK_TYPE_F32;
+    std::vector<Tensor> outs;
+    for (int64_t i = 0; i < list.size(); ++i) {
+        const Tensor &t = list.at(i, "a matrix"), &first = list.at(0, "a matrix");
+        const int its = type_of(t, "a matrix");
+        if (i == 0) type = its;
+        if (its != type || t.device() != first.device()) value_error("%s must be of one dtype and on one device", "matrices");
+        g.add(t, "matrices");
+        outs.push_back(at::empty(t.sizes(), t.options().dtype(at::kBFloat16)));
+        out.add(outs.back(), "matrices");
+        PyList_SET_ITEM(result.get(), i, wrap(outs.back()));
+    }
+    const int n = g.count();
+    if (n > 0) {
+        const Tensor &on = list.at(0, "a matrix");
+        const size_t need = api.novak_orthogonalize_bytes(g.rows.data(), g.cols.data(), n);
+        const Tensor work = at::empty({static_cast<int64_t>(need)}, on.options().dtype(at::kByte));
+        ENQUEUE(novak_orthogonalize, on, g.ptr.data(), g.stride.data(), type, out.ptr.data(), out.stride.data(), g.rows.data(),
+                g.cols.data(), n, abc.data(), static_cast<int>(abc.size() / 3), eps, work.data_ptr(), need);
+    }
+    return result.release();
+}
+
+// orthogonal_step(parameters, gradients, momenta, momentum, nesterov, steps, decay, coefficients, eps)
+PyObject *orthogonal_step(PyObject *const *args)
+{
+    const Tensors params(args[0], "a list of parameters is needed"), grads(args[1], "a list of gradients is needed"),
+        momenta(args[2], "a list of momenta is needed");
+    const std::vector<double> each = numbers(args[5], "steps must be numbers"), abc = numbers(args[7], "coefficients must be numbers");
+    const double momentum = number(args[3]), decay = number(args[6]), eps = number(args[8]);
+    const int64_t count = params.size();
+    if (grads.size() != count || momenta.size() != count || static_cast<int64_t>(each.size()) != count)
+        value_error("%s must be as many as the parameters", "gradients, momenta and steps");
+    Matrices theta, g, m;
+    std::vector<double> step;
+    int type = NOVAK_TYPE_F32;
+    for (int64_t i = 0; i < count; ++i) {
+        const Tensor &p = params.at(i, "a parameter"), &gr = grads.at(i, "a gradient"), &mo = momenta.at(i, "a momentum");
+        if (i == 0) type = type_of(gr, "a gradient");
+        if (type_of(gr, "a gradient") != type) value_error("%s must be of one dtype", "gradients");
+        same(gr, "a gradient", params.at(0, "a parameter"), p.sizes());
+        same(mo, "a momentum", params.at(0, "a parameter"), p.sizes());
+        same(p, "a parameter", params.at(0, "a parameter"), p.sizes());
+        if (p.scalar_type() != at::kFloat || mo.scalar_type() != at::kFloat) {
+            PyErr_SetString(PyExc_TypeError, "parameters and momenta must be float32");
+            throw Refused{};
+        }
+        if (!p.is_contiguous() || !gr.is_contiguous() || !mo.is_contiguous())
+            value_error("%s must be contiguous", "parameters, gradients and momenta");
+        theta.add(p, "parameters");
+        g.add(gr, "gradients");
+        m.add(mo, "momenta");
+        step.resize(theta.ptr.size(), each[i]);
+    }
+    const int n = theta.count();
+    if (n > 0) {
+        const Tensor &on = params.at(0, "a parameter");
+        const size_t need = api.novak_orthogonalize_bytes(theta.rows.data(), theta.cols.data(), n);
+        const Tensor work = at::empty({static_cast<int64_t>(need)}, on.options().dtype(at::kByte));
+        ENQUEUE(novak_orthogonal_step, on, reinterpret_cast<float *const *>(theta.ptr.data()), g.ptr.data(), type,
+                reinterpret_cast<float *const *>(m.ptr.data()), theta.rows.data(), theta.cols.data(), n, momentum,
+                static_cast<int>(truth(args[4])), step.data(), decay, abc.data(), static_cast<int>(abc.size() / 3), eps,
+                work.data_ptr(), need);
+    }
+    Py_RETURN_NONE;
+}
+
 // bind(error class, address of each of NOVAK_ENTRIES in that order)
 PyObject *bind(PyObject *const *args)
 {
@@ -400,7 +663,7 @@ template <PyObject *(*F)(PyObject *const *), int N> PyMethodDef def(const char *
 }
 
 PyMethodDef methods[] = {
-    def<bind, 11>("bind"),
+    def<bind, 20>("bind"),
     def<pack, 1>("pack"),
     def<unpack, 2>("unpack"),
     def<layer_norm, 5>("layer_norm"),
@@ -408,6 +671,12 @@ PyMethodDef methods[] = {
     def<activation, 4>("activation"),
     def<activation_backward, 4>("activation_backward"),
     def<linear_weight_grad, 6>("linear_weight_grad"),
+    def<rms_norm, 5>("rms_norm"),
+    def<rms_norm_backward, 7>("rms_norm_backward"),
+    def<embedding, 4>("embedding"),
+    def<embedding_grad, 6>("embedding_grad"),
+    def<orthogonalize, 3>("orthogonalize"),
+    def<orthogonal_step, 9>("orthogonal_step"),
     {nullptr, nullptr, 0, nullptr},
 };
 

@@ -1,6 +1,7 @@
 """Training operators of the library (include/novak.h, "Training operators"):
-8-bit forms of activations, layer norm, activation functions and the weight
-gradient of a linear layer, on torch tensors.
+8-bit forms of activations, layer norm, root-mean-square norm with the residual's
+addition, activation functions, the weight gradient of a linear layer, token embedding
+and its gradient, and orthogonalised updates of matrices, on torch tensors.
 
 A tensor is seen as rows of its last dimension, its address goes to the C entry
 point of the same name, and the work is enqueued on torch's current stream of the
@@ -24,7 +25,14 @@ _TYPE = {torch.float32: B.NOVAK_TYPE_F32, torch.bfloat16: B.NOVAK_TYPE_BF16}
 _KIND = {"gelu": B.NOVAK_ACT_GELU, "gelu_tanh": B.NOVAK_ACT_GELU_TANH, "silu": B.NOVAK_ACT_SILU}
 _ENTRIES = ("novak_act8_pack", "novak_act8_unpack", "novak_layer_norm", "novak_layer_norm_backward_bytes",
             "novak_layer_norm_backward", "novak_activation", "novak_activation_backward",
-            "novak_linear_weight_grad_bytes", "novak_linear_weight_grad", "novak_ops_error")
+            "novak_linear_weight_grad_bytes", "novak_linear_weight_grad", "novak_rms_norm",
+            "novak_rms_norm_backward_bytes", "novak_rms_norm_backward", "novak_embedding", "novak_embedding_grad_bytes",
+            "novak_embedding_grad", "novak_orthogonalize_bytes", "novak_orthogonalize", "novak_orthogonal_step",
+            "novak_ops_error")
+
+# The triples (a, b, c) of five Newton-Schulz steps that bring singular values above 1e-3 of the
+# largest to between 0.7 and 1.2 (those of the Muon optimiser).
+NEWTON_SCHULZ = ((3.4445, -4.7750, 2.0315),) * 5
 
 
 class _Calls:
@@ -175,6 +183,66 @@ def layer_norm_backward(dy, saved, rstd, weight, mean=None, grad_dtype=torch.flo
     if mean is None:
         raise ValueError("mean is needed beside x")
     return _calls.layer_norm_backward(dy, None, saved, mean, rstd, weight, grad)
+
+
+def rms_norm(x, weight, residual=None, eps: float = 1e-6, checkpoint: bool = False):
+    """Root-mean-square norm over the last dimension, of h = x + residual (``residual`` None:
+    of x).  Returns (y, h, rstd, kept): y = h rstd weight and h like x (h is x itself without
+    a residual), rstd fp32 with x's leading dimensions, and with ``checkpoint`` the 8-bit form
+    of xhat = h rstd (else None), from which ``rms_norm_backward`` and the next layer's
+    ``linear_weight_grad`` (affine = (weight, None)) work."""
+    y, h, rstd, both = _calls.rms_norm(x, weight, residual, eps, checkpoint)
+    return y, h, rstd, Act8._of(both, x.shape[-1], x.shape) if checkpoint else None
+
+
+def rms_norm_backward(dy, saved, rstd, weight, dh=None, grad_dtype=torch.float32):
+    """(dx, dweight) of ``rms_norm``: dx is the gradient of x and of the residual alike.
+    ``saved`` is the 8-bit form of xhat that the forward pass left, or its h; ``dh`` the
+    gradient that reaches h from elsewhere (the stream's), added to dx."""
+    grad = _type(grad_dtype, "grad_dtype")
+    if isinstance(saved, Act8):
+        return _calls.rms_norm_backward(dy, saved, None, rstd, weight, dh, grad)
+    return _calls.rms_norm_backward(dy, None, saved, rstd, weight, dh, grad)
+
+
+def embedding(ids, table, scale: float = 1.0, dtype=None):
+    """out[...] = scale table[ids[...]], of ``dtype`` (None: the table's); ids int64 or int32 of any
+    shape.  An id outside [0, rows of the table) stands for no token and gives zeros."""
+    return _calls.embedding(ids, table, scale, _type(table.dtype if dtype is None else dtype, "dtype"))
+
+
+def embedding_grad(dout, ids, vocab: int, scale: float = 1.0, dtype=torch.float32, out=None):
+    """The gradient of ``embedding``'s table (vocab x the last dimension of dout) of ``dtype``:
+    scale times the sum of dout over the tokens of each id.  With ``out``, that sum is added to
+    it, in place, and rows that no token names are not touched."""
+    return _calls.embedding_grad(dout, ids, vocab, scale, _type(dtype, "dtype"), out)
+
+
+def _flat(coefficients):
+    flat = []
+    for triple in coefficients:
+        a, b, c = triple
+        flat += (a, b, c)
+    return flat
+
+
+def orthogonalize(matrices, coefficients=NEWTON_SCHULZ, eps: float = 1e-7):
+    """Matrices brought close to orthogonal (their singular values close to 1) by Newton-Schulz
+    products, as new bfloat16 tensors: X = G / max(|G|, eps), then X <- a X + (b A + c A^2) X
+    with A = X X^T for each (a, b, c) of ``coefficients``.  ``matrices`` is a tensor or a list of
+    tensors of one dtype (float32 or bfloat16), which are worked on together; one of more than two
+    dimensions is a batch of matrices.  See include/novak.h for what is held in how many bits."""
+    if isinstance(matrices, torch.Tensor):
+        return _calls.orthogonalize((matrices,), _flat(coefficients), eps)[0]
+    return _calls.orthogonalize(matrices, _flat(coefficients), eps)
+
+
+def orthogonal_step(params, grads, momenta, steps, momentum: float = 0.95, nesterov: bool = True, decay: float = 1.0,
+                    coefficients=NEWTON_SCHULZ, eps: float = 1e-7):
+    """In place, for each matrix: m <- momentum m + g, G = g + momentum m (``nesterov``) or m,
+    theta <- decay theta - step X, X the orthogonalised G.  ``params`` and ``momenta`` are
+    contiguous float32 tensors, ``grads`` of one dtype, ``steps`` one number each."""
+    _calls.orthogonal_step(params, grads, momenta, momentum, nesterov, steps, decay, _flat(coefficients), eps)
 
 
 def _kind(kind) -> int:

@@ -3,6 +3,7 @@
 // cores' allocation, product, commit and load.
 #pragma once
 
+#include <atomic>
 #include <cstdint>
 
 #include <cuda.h>
@@ -213,10 +214,53 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t addr, uint32_t lead, u
            static_cast<uint64_t>(stride >> 4) << 32 | 1ull << 46 | 2ull << 61;
 }
 
+// A position in a ring of N slots, and the parity of its use.
+template <int N> struct Ring {
+    uint32_t slot, phase = 0;
+    __device__ explicit Ring(uint32_t first = 0) : slot(first) {}
+    __device__ __forceinline__ void advance(int n = 1)
+    {
+        slot += n;
+        if (slot >= N) {
+            slot -= N;
+            phase ^= 1;
+        }
+    }
+};
+
 // bf16 x bf16 -> fp32, both operands with contiguous M / N.
 __host__ __device__ constexpr uint32_t instr_desc(uint32_t m, uint32_t n)
 {
     return 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | (n >> 3) << 17 | (m >> 4) << 24;
+}
+
+// ---- host ---------------------------------------------------------------------------
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                 const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+inline EncodeTiled tensor_map_encoder()
+{
+    static EncodeTiled fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) != cudaSuccess ||
+            r != cudaDriverEntryPointSuccess) p = nullptr;
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return fn;
+}
+
+// Shared memory beyond 48 KB has to be asked for once on each device.
+template <typename Kernel> cudaError_t ask_shared_memory(Kernel kernel, int bytes, std::atomic<uint64_t> &asked)
+{
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e == cudaSuccess && (device >= 64 || !(asked.load() >> device & 1))) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e == cudaSuccess && device < 64) asked.fetch_or(uint64_t(1) << device);
+    }
+    return e;
 }
 
 }  // namespace novak

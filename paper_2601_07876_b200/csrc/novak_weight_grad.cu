@@ -32,7 +32,6 @@
 // memory takes 5; with db or a layer norm 60, since dy is read once more (sums inside
 // this kernel were 75: they take the shared memory's time too).
 #include <algorithm>
-#include <atomic>
 
 #include "novak_ops.cuh"
 #include "novak_tcgen05.cuh"
@@ -388,20 +387,6 @@ struct Shared {
 };
 constexpr int kSmemBytes = (kDySlots + kXSlots) * kSlotBytes + kRawSlots * kRawBytes + 1024 + static_cast<int>(sizeof(Shared));
 static_assert(kSmemBytes <= 227 * 1024, "shared memory");
-
-// A position in a ring of N slots, and the parity of its use.
-template <int N> struct Ring {
-    uint32_t slot, phase = 0;
-    __device__ explicit Ring(uint32_t first = 0) : slot(first) {}
-    __device__ __forceinline__ void advance(int n = 1)
-    {
-        slot += n;
-        if (slot >= N) {
-            slot -= N;
-            phase ^= 1;
-        }
-    }
-};
 
 struct KernelArgs {
     Cut cut;
@@ -956,22 +941,6 @@ Layout layout_for(const Mat &dy, int type, int64_t rows, int64_t n_out, int64_t 
     return l;
 }
 
-using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                 const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiled encoder()
-{
-    static EncodeTiled fn = [] {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult r;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) != cudaSuccess ||
-            r != cudaDriverEntryPointSuccess) p = nullptr;
-        return reinterpret_cast<EncodeTiled>(p);
-    }();
-    return fn;
-}
-
 template <int TYPE, bool ALIGNED>
 cudaError_t launch_sums(const WeightGradArgs &a, const Layout &l, float *sums, __nv_bfloat16 *out, cudaStream_t stream)
 {
@@ -1028,7 +997,7 @@ cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t stream)
         if (e != cudaSuccess) return e;
         if (copy) dy = copy;
     }
-    const EncodeTiled encode = encoder();
+    const EncodeTiled encode = tensor_map_encoder();
     if (!encode) return cudaErrorNotSupported;
     CUtensorMap map;
     const int64_t plane = a.rows * l.ld;
@@ -1049,14 +1018,8 @@ cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t stream)
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return cudaErrorInvalidValue;
 
-    // shared memory beyond 48 KB has to be asked for once on each device
     static std::atomic<uint64_t> asked{0};
-    int device = 0;
-    cudaError_t e = cudaGetDevice(&device);
-    if (e == cudaSuccess && (device >= 64 || !(asked.load() >> device & 1))) {
-        e = cudaFuncSetAttribute(novak_weight_grad_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
-        if (e == cudaSuccess && device < 64) asked.fetch_or(uint64_t(1) << device);
-    }
+    cudaError_t e = ask_shared_memory(novak_weight_grad_kernel, kSmemBytes, asked);
     if (e != cudaSuccess) return e;
 
     float *partial = reinterpret_cast<float *>(work + l.planes_bytes);

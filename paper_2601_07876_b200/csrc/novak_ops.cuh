@@ -2,6 +2,8 @@
 // at a time, and the 8-bit form of activations.
 #pragma once
 
+#include <atomic>
+
 #include <cuda_bf16.h>
 
 #include "novak.h"
@@ -35,6 +37,18 @@ cudaError_t launch(void (*kernel)(Params...), dim3 grid, int threads, int smem, 
     lc.attrs = attr;
     lc.numAttrs = 1;
     return cudaLaunchKernelEx(&lc, kernel, static_cast<Params>(args)...);
+}
+
+// Shared memory beyond 48 KB has to be asked for once on each device.
+template <typename Kernel> cudaError_t ask_shared_memory(Kernel kernel, int bytes, std::atomic<uint64_t> &asked)
+{
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e == cudaSuccess && (device >= 64 || !(asked.load() >> device & 1))) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e == cudaSuccess && device < 64) asked.fetch_or(uint64_t(1) << device);
+    }
+    return e;
 }
 
 template <int TYPE> struct Elem;

@@ -3,7 +3,6 @@
 // cores' allocation, product, commit and load.
 #pragma once
 
-#include <atomic>
 #include <cstdint>
 
 #include <cuda.h>
@@ -249,18 +248,6 @@ inline EncodeTiled tensor_map_encoder()
         return reinterpret_cast<EncodeTiled>(p);
     }();
     return fn;
-}
-
-// Shared memory beyond 48 KB has to be asked for once on each device.
-template <typename Kernel> cudaError_t ask_shared_memory(Kernel kernel, int bytes, std::atomic<uint64_t> &asked)
-{
-    int device = 0;
-    cudaError_t e = cudaGetDevice(&device);
-    if (e == cudaSuccess && (device >= 64 || !(asked.load() >> device & 1))) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-        if (e == cudaSuccess && device < 64) asked.fetch_or(uint64_t(1) << device);
-    }
-    return e;
 }
 
 }  // namespace novak

@@ -5,21 +5,23 @@
 // that long rows are cut among warps.
 //
 // The gradient of a whole table is mostly zeros to be written; the rest is to bring each id's
-// tokens together in an order that goes by their places alone.  No sort of all ids by digits:
-// ids are dealt out by their low bits to some hundred CTAs (words of like frequency have like
-// numbers; so they go to different ones), and each CTA looks through all ids, which L2
-// holds, for its own.  It counts its rows' tokens and those of the CTAs before it, which says where
-// its tokens lie in the order of all, and
-//   writes zeros for rows without tokens (or leaves them, where the sum is added),
-//   sums rows of up to 64 tokens by itself, a warp 256 columns,
-//   leaves the tokens of longer ones, in order, to the second kernel, which cuts the order of
-//   all tokens into pieces of 64 and gives each a CTA; the last one of a row's pieces to be done
-//   adds their sums up in order.
-// So it is one pass over dout and one over the table, however unevenly words occur.
+// tokens together in an order that goes by their places alone.  Two kernels.
+// The first one orders the tokens.  No sort of all ids by digits: ids are dealt out by their low bits
+// to some hundred CTAs (words of like frequency have like numbers; so they go to different ones),
+// and each cluster of eight looks through all ids, an eighth each, and passes on to each other
+// what is whose.  A CTA counts its rows' tokens and those of the CTAs before it, which says where its
+// tokens lie in the order of all, and puts them there, row by row.
+// The second one is one pass over dout and one over the table.  Warps have a few rows of 256 columns:
+// zeros where there are no tokens, the sum of up to 16.  The order of all tokens is cut into pieces of 16
+// besides, and those of longer rows have a CTA each; the last one of a row's pieces to be done adds
+// their sums up in order.  So no word is too frequent.
+// (Zeros and sums in the first kernel, once it knows its rows: 58 to 77 us for 16384 tokens of 50000 x 768,
+// since its shared memory leaves room for too few warps to hide what loads wait for.)
 #include <algorithm>
 #include <climits>
 
 #include "novak_ops.cuh"
+#include "novak_tcgen05.cuh"
 
 namespace novak {
 namespace {
@@ -69,29 +71,32 @@ __global__ void __launch_bounds__(kLookThreads) novak_embedding_kernel(LookArgs 
         for (int k = 0; k < 4; ++k) v[k] = there ? v[k] * scale : F2(0.0f);
         Eight<OUT> e;
         e.set(v);
-        store_eight<ALIGNED>(out + i * a.lanes * 8, e, n[i]);
+        put_eight<ALIGNED>(out + i * a.lanes * 8, e, n[i]);
     }
 }
 
 // ---- the gradient --------------------------------------------------------------------
 constexpr int kOwnThreads = 512, kOwnRows = 4096;       // rows of the table per CTA at most
-constexpr int kList = 2048, kBitWords = 2048;           // tokens that a CTA keeps in shared memory; words of its bit map
-constexpr int kPiece = 64;                              // tokens in a piece of the second kernel
-constexpr int kSlice = 1024, kSumThreads = 256;         // columns of a CTA there
-constexpr int kFewTokens = 256;                         // up to which there is no second kernel
+constexpr int kCluster = 8;                             // CTAs that look through the ids together (each all of them: 33 MB out of L2, 8 us)
+constexpr int kList = 4096, kBitWords = 4 * kOwnThreads;        // tokens that a CTA keeps in shared memory; words of its bit map
+constexpr int kPiece = 16;                              // tokens in a piece; rows of more go by pieces
+constexpr int kSlice = 1024, kSumThreads = 256, kSumWarps = kSumThreads / 32;   // columns of a piece's CTA
+constexpr int kMostRows = 16;                           // rows of a group of lanes in the second kernel
 
-struct Segment {            // of a token in the order of all, if it is its row's second kernel's
+struct Place {              // of a token in the order of all; row < 0: its row is not summed by pieces
     int row, start, count, token;
 };
 
 struct GradArgs : EmbedGradArgs {
-    int shift;              // CTA p has the ids whose low `shift` bits are p
-    int longest;            // tokens of a row that are summed at once
-    int lanes;              // of a row (ALIGNED), of 8 columns each
-    int slices;             // of the columns, in the second kernel
-    int group;              // its threads per token
+    int shift, fold;        // CTA p has the ids whose `shift` bits above the low `fold` ones are p
+    int lanes;              // of a row, of 8 columns each
+    int64_t steps;          // of that many columns
+    int each;               // rows of a group of them, a power of two, up to kMostRows and `lanes`
+    int slices, group;      // of kSlice columns; threads per token there
+    int64_t pieces;         // CTAs of the second kernel that sum them
     int *list;              // tokens, for CTAs that have more than kList
-    Segment *order;
+    Place *order;
+    int2 *rows;             // of the table: how many tokens a row has, and where they are in that order; a single one itself
     int *counts;            // [piece][slice]: sums that are done, where a row begins in that piece
     int *valid;             // tokens in all
     float *partial;         // [piece][2][cols]: of a row that began before, of one that begins here
@@ -112,6 +117,7 @@ __device__ __forceinline__ int scan(int x, int *scratch, int &all)
     __syncthreads();
     int before = 0;
     all = 0;
+#pragma unroll
     for (int w = 0; w < kOwnThreads / 32; ++w) {
         const int y = scratch[w];
         if (w < warp) before += y;
@@ -120,48 +126,239 @@ __device__ __forceinline__ int scan(int x, int *scratch, int &all)
     return before + s - x;
 }
 
-// Adds the lanes that are `mine` to counters[row], lanes of one row together (an id may be on
-// every lane); the place of each among what the counter had and the lanes before it.
+// Adds the lanes that are `mine` to counters[row]; the place of each.  Lanes of the first one's
+// row go together (a word may be on all of them), the others by themselves.
 __device__ __forceinline__ int count_rows(bool mine, int row, int *counters)
 {
-    unsigned left = __ballot_sync(0xffffffffu, mine);
-    const int lane = threadIdx.x & 31;
+    const unsigned there = __ballot_sync(0xffffffffu, mine);
+    if (there == 0) return 0;
+    const int lane = threadIdx.x & 31, leader = __ffs(static_cast<int>(there)) - 1, of = __shfl_sync(0xffffffffu, row, leader);
+    const bool together = mine && row == of;
+    const unsigned same = __ballot_sync(0xffffffffu, together);
     int place = 0;
-    while (left) {
-        const int leader = __ffs(static_cast<int>(left)) - 1, of = __shfl_sync(0xffffffffu, row, leader);
-        const unsigned same = __ballot_sync(0xffffffffu, mine && row == of);
-        int base = 0;
-        if (lane == leader) base = atomicAdd(counters + of, __popc(same));
-        base = __shfl_sync(0xffffffffu, base, leader);
-        if (mine && row == of) place = base + __popc(same & ((1u << lane) - 1));
-        left &= ~same;
+    if (lane == leader || (mine && !together)) place = atomicAdd(counters + row, together ? __popc(same) : 1);
+    const int base = __shfl_sync(0xffffffffu, place, leader);
+    return together ? base + __popc(same & ((1u << lane) - 1)) : place;
+}
+
+// In another CTA's shared memory (addresses from at_rank).
+__device__ __forceinline__ uint32_t atomic_add_at(uint32_t addr, uint32_t x)
+{
+    uint32_t r;
+    asm volatile("atom.relaxed.cluster.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(r) : "r"(addr), "r"(x) : "memory");
+    return r;
+}
+__device__ __forceinline__ void store_at(uint32_t addr, int x) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(x) : "memory"); }
+__device__ __forceinline__ void store_at(uint32_t addr, uint16_t x) { asm volatile("st.shared::cluster.u16 [%0], %1;" ::"r"(addr), "h"(x) : "memory"); }
+
+struct OwnShared {
+    int counts[kOwnRows], starts[kOwnRows];
+    int found[kList], list[kList];              // tokens as they were found, row by row
+    uint16_t found_row[kList];
+    uint32_t bits[kBitWords];
+    uint16_t few[kOwnRows], many[kOwnRows];     // rows of 1 to 16 tokens, and of more
+    int passed[kCluster];                       // tokens that this CTA found, by whose they are
+    int before[kCluster], valid[kCluster];      // of each CTA's share of the ids: those of CTAs before this one; all
+    int sums[2][kOwnThreads / 32], scratch[kOwnThreads / 32];
+    int n, n_few, n_many;
+};
+
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kOwnThreads, 2) novak_embedding_order_kernel(GradArgs a)
+{
+    extern __shared__ uint8_t raw_shared[];
+    OwnShared &sh = *reinterpret_cast<OwnShared *>(raw_shared);
+    const int64_t own = blockIdx.x, low = (int64_t(1) << a.shift) - 1;
+    const int fold = a.fold, above = fold + a.shift, inside = (1 << fold) - 1;
+    // blocks of 2^fold rows: own, own + 2^shift, ...; some of the last one's may be beyond the table
+    const int rows = static_cast<int>(max((((a.vocab + inside) >> fold) - own + low) >> a.shift, static_cast<int64_t>(0)) << fold);
+    const auto row_of = [&](int64_t id) { return static_cast<int>(id >> above << fold | (id & inside)); };
+    const auto id_of = [&](int row) { return static_cast<int64_t>(row >> fold) << above | own << fold | (row & inside); };
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int i = threadIdx.x; i < rows; i += kOwnThreads) sh.counts[i] = 0;
+    if (threadIdx.x < kCluster) sh.passed[threadIdx.x] = 0;
+    if (threadIdx.x == 0) sh.n = sh.n_few = sh.n_many = 0;
+    cluster_sync();
+    start();
+
+    // ---- this CTA's share of the ids: whose they are, and how many belong to CTAs before this cluster
+    constexpr int kAhead = 4, kAgain = 8;
+    const auto fetch = [&](int64_t t0, auto &id) {          // (what is none: the largest number)
+#pragma unroll
+        for (int k = 0; k < static_cast<int>(sizeof id / sizeof id[0]); ++k) {
+            const int64_t t = t0 + k * kOwnThreads + threadIdx.x, x = t < a.tokens ? id_at(a.ids, a.id_type, t) : -1;
+            id[k] = x >= 0 && x < a.vocab ? static_cast<uint32_t>(x) : ~0u;
+        }
+    };
+    const auto owner = [&](uint32_t id) { return id >> fold & static_cast<uint32_t>(low); };
+    const uint32_t rank = cluster_rank(), cluster0 = static_cast<uint32_t>(own) - rank;
+    {
+        int before = 0, valid = 0;
+        for (int64_t t0 = rank * kAhead * kOwnThreads; t0 < a.tokens; t0 += kCluster * kAhead * kOwnThreads) {
+            uint32_t id[kAhead];
+            fetch(t0, id);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const uint32_t whose = owner(id[k]) - cluster0;
+                if (id[k] == ~0u) continue;
+                ++valid;
+                before += owner(id[k]) < cluster0;
+                if (whose >= kCluster) continue;
+                atomicAdd(&sh.passed[whose], 1);
+                const uint32_t at = atomic_add_at(at_rank(smem_addr(&sh.n), whose), 1);
+                if (at < kList) {
+                    store_at(at_rank(smem_addr(&sh.found[at]), whose), static_cast<int>(t0 + k * kOwnThreads + threadIdx.x));
+                    store_at(at_rank(smem_addr(&sh.found_row[at]), whose), static_cast<uint16_t>(row_of(id[k])));
+                }
+            }
+        }
+        before = __reduce_add_sync(0xffffffffu, before);
+        valid = __reduce_add_sync(0xffffffffu, valid);
+        if (lane == 0) {
+            sh.sums[0][warp] = before;
+            sh.sums[1][warp] = valid;
+        }
+        __syncthreads();
+        if (threadIdx.x < kCluster) {
+            before = valid = 0;
+            for (int w = 0; w < kOwnThreads / 32; ++w) {
+                before += sh.sums[0][w];
+                valid += sh.sums[1][w];
+            }
+            for (int r = 0; r < static_cast<int>(threadIdx.x); ++r) before += sh.passed[r];
+            store_at(at_rank(smem_addr(&sh.before[rank]), threadIdx.x), before);
+            store_at(at_rank(smem_addr(&sh.valid[rank]), threadIdx.x), valid);
+        }
     }
-    return place;
+    cluster_sync();             // (from here on nobody looks into another CTA)
+    int before = 0;
+    for (int r = 0; r < kCluster; ++r) before += sh.before[r];
+    if (own == 0 && threadIdx.x == 0) {
+        int valid = 0;
+        for (int r = 0; r < kCluster; ++r) valid += sh.valid[r];
+        *a.valid = valid;
+    }
+    const int n = sh.n;
+    int *list = n <= kList ? sh.list : a.list + before;
+    if (n <= kList) {
+        for (int i = warp * 32; i < n; i += kOwnThreads) count_rows(i + lane < n, i + lane < n ? sh.found_row[i + lane] : 0, sh.counts);
+    } else {
+        for (int64_t t0 = 0; t0 < a.tokens; t0 += kAgain * kOwnThreads) {
+            uint32_t id[kAgain];
+            fetch(t0, id);
+#pragma unroll
+            for (int k = 0; k < kAgain; ++k) count_rows(id[k] != ~0u && owner(id[k]) == own, row_of(id[k]), sh.counts);
+        }
+    }
+    __syncthreads();
+
+    // ---- where each row's tokens begin
+    {
+        constexpr int kEach = kOwnRows / kOwnThreads;
+        const int first = threadIdx.x * kEach;
+        int sum = 0, all;
+        if (first < rows)
+            for (int i = first; i < min(first + kEach, rows); ++i) sum += sh.counts[i];
+        int at = scan(sum, sh.scratch, all);
+        if (first < rows)
+            for (int i = first; i < min(first + kEach, rows); ++i) {
+                const int count = sh.counts[i];
+                sh.starts[i] = at;
+                if (count > 0 && count <= kPiece) sh.few[atomicAdd(&sh.n_few, 1)] = static_cast<uint16_t>(i);
+                if (count > kPiece) sh.many[atomicAdd(&sh.n_many, 1)] = static_cast<uint16_t>(i);
+                at += count;
+            }
+    }
+    __syncthreads();
+    for (int row = threadIdx.x; row < rows; row += kOwnThreads)
+        if (id_of(row) < a.vocab && sh.counts[row] != 1) a.rows[id_of(row)] = make_int2(before + sh.starts[row], sh.counts[row]);
+    __syncthreads();
+
+    // ---- the tokens, row by row: put there in any order (starts go up to the ends) ...
+    const auto put = [&](bool mine, int row, int t) {
+        if (__any_sync(0xffffffffu, mine)) {
+            const int place = count_rows(mine, row, sh.starts);
+            if (mine) list[place] = t;
+        }
+    };
+    if (n <= kList) {
+        for (int i = warp * 32; i < n; i += kOwnThreads) {
+            const bool in = i + lane < n;
+            put(in, in ? sh.found_row[i + lane] : 0, in ? sh.found[i + lane] : 0);
+        }
+    } else {
+        for (int64_t t0 = 0; t0 < a.tokens; t0 += kAgain * kOwnThreads) {
+            uint32_t id[kAgain];
+            fetch(t0, id);
+#pragma unroll
+            for (int k = 0; k < kAgain; ++k)
+                put(id[k] != ~0u && owner(id[k]) == own, row_of(id[k]), static_cast<int>(t0 + k * kOwnThreads + threadIdx.x));
+        }
+    }
+    __syncthreads();
+
+    // ---- ... and then in order.  Of few tokens a lane has one each: its place is the number of tokens before it.
+    const int n_few = sh.n_few;
+    for (int i = warp; i < n_few; i += kOwnThreads / 32) {
+        const int row = sh.few[i], count = sh.counts[row], first = sh.starts[row] - count;
+        if (count == 1 && lane == 0) a.rows[id_of(row)] = make_int2(list[first], 1);
+        const int x = lane < count ? list[first + lane] : INT_MAX;
+        int place = 0;
+        for (int j = 0; j < count; ++j) place += __shfl_sync(0xffffffffu, x, j) < x;
+        if (lane < count) a.order[before + first + place] = Place{-1, 0, 0, x};
+    }
+    // Many: the tokens as bits of a map, 65536 of them at a time.
+    for (int k = 0; k < sh.n_many; ++k) {
+        const int row = sh.many[k], count = sh.counts[row], first = sh.starts[row] - count;
+        int done = 0;
+        for (int64_t t0 = 0; t0 < a.tokens && done < count; t0 += 32 * kBitWords) {
+            __syncthreads();
+            for (int i = threadIdx.x; i < kBitWords; i += kOwnThreads) sh.bits[i] = 0;
+            __syncthreads();
+            for (int i = threadIdx.x; i < count; i += kOwnThreads) {
+                const int64_t t = list[first + i] - t0;
+                if (t >= 0 && t < 32 * kBitWords) atomicOr(&sh.bits[t >> 5], 1u << (t & 31));
+            }
+            __syncthreads();
+            constexpr int kEach = kBitWords / kOwnThreads;
+            int bits = 0, all;
+            for (int i = 0; i < kEach; ++i) bits += __popc(sh.bits[threadIdx.x * kEach + i]);
+            int at = done + scan(bits, sh.scratch, all);
+            done += all;
+            for (int i = 0; i < kEach; ++i)
+                for (uint32_t m = sh.bits[threadIdx.x * kEach + i]; m; m &= m - 1, ++at) {
+                    const int t = static_cast<int>(t0) + (threadIdx.x * kEach + i) * 32 + __ffs(static_cast<int>(m)) - 1;
+                    a.order[before + first + at] = Place{static_cast<int>(id_of(row)), before + first, count, t};
+                }
+        }
+        for (int i = threadIdx.x; i < a.slices; i += kOwnThreads) a.counts[static_cast<int64_t>((before + first) / kPiece) * a.slices + i] = 0;
+    }
 }
 
 // Eight columns of the sum over `count` tokens.
-template <int TYPE, bool ALIGNED>
-__device__ __forceinline__ void sum_tokens(const EmbedGradArgs &a, const int *tokens, int count, int64_t col, int n, const void *begin,
+template <int TYPE, bool ALIGNED, typename Token>
+__device__ __forceinline__ void sum_tokens(const EmbedGradArgs &a, const Token &token, int count, int64_t col, int n, const void *begin,
                                            const void *end, F2 (&sum)[4])
 {
     using T = typename Elem<TYPE>::T;
-    constexpr int kAhead = !ALIGNED ? 2 : TYPE == NOVAK_TYPE_F32 ? 4 : 8;
+    constexpr int kAhead = TYPE == NOVAK_TYPE_BF16 && ALIGNED ? 8 : 4;
     const T *base = static_cast<const T *>(a.dout.ptr) + col;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] = F2(0.0f);
     for (int j = 0; j < count; j += kAhead) {
         Fetch<TYPE, ALIGNED> raw[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             raw[k].zero();
-            if (j + k < count) raw[k].load(base + tokens[j + k] * a.dout.stride, n, begin, end);
+            if (j + k < count) raw[k].load(base + token(j + k) * a.dout.stride, n, begin, end);
         }
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            F2 v[4];
-            raw[k].eight().get(v);
-            if (j + k < count)
+        for (int k = 0; k < kAhead; ++k)
+            if (j + k < count) {
+                F2 v[4];
+                raw[k].eight().get(v);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) sum[i] = sum[i] + v[i];
-        }
+            }
     }
 }
 
@@ -184,210 +381,36 @@ __device__ __forceinline__ void put_sum(const EmbedGradArgs &a, typename Elem<GR
     }
     Eight<GRAD> e;
     e.set(v);
-    store_eight<ALIGNED>(p, e, n);
+    put_eight<ALIGNED>(p, e, n);
 }
 
-struct OwnShared {
-    int counts[kOwnRows], starts[kOwnRows];
-    int2 found[kList];          // row, token
-    int list[kList];
-    uint32_t bits[kBitWords];
-    int scratch[kOwnThreads / 32];
-    int n;
-};
-
-template <int TYPE, int GRAD, bool ALIGNED>
-__global__ void __launch_bounds__(kOwnThreads, 2) novak_embedding_grad_kernel(GradArgs a)
-{
-    using G = typename Elem<GRAD>::T;
-    extern __shared__ uint8_t raw_shared[];
-    OwnShared &sh = *reinterpret_cast<OwnShared *>(raw_shared);
-    const int64_t own = blockIdx.x, low = (int64_t(1) << a.shift) - 1;
-    const int rows = static_cast<int>((a.vocab - own + low) >> a.shift);        // ids own, own + 2^shift, ...
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (int i = threadIdx.x; i < rows; i += kOwnThreads) sh.counts[i] = 0;
-    if (threadIdx.x == 0) sh.n = 0;
-    __syncthreads();
-    start();
-
-    // ---- all ids: how many are this CTA's, by row, and how many belong to CTAs before it
-    int before = 0, valid = 0;
-    const auto look = [&](auto &&take) {
-        constexpr int kAhead = 8;
-        for (int64_t t0 = 0; t0 < a.tokens; t0 += kAhead * kOwnThreads) {
-            int64_t id[kAhead];
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-                const int64_t t = t0 + k * kOwnThreads + threadIdx.x;
-                id[k] = t < a.tokens ? id_at(a.ids, a.id_type, t) : -1;
-            }
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) take(id[k], static_cast<int>(t0 + k * kOwnThreads + threadIdx.x));
-        }
-    };
-    look([&](int64_t id, int t) {
-        const bool there = id >= 0 && id < a.vocab;
-        valid += there;
-        before += there && (id & low) < own;
-        const bool mine = there && (id & low) == own;
-        const unsigned m = __ballot_sync(0xffffffffu, mine);
-        if (m == 0) return;
-        const int row = static_cast<int>(id >> a.shift);
-        count_rows(mine, row, sh.counts);
-        int at = 0;
-        if (lane == 0) at = atomicAdd(&sh.n, __popc(m));
-        at = __shfl_sync(0xffffffffu, at, 0) + __popc(m & ((1u << lane) - 1));
-        if (mine && at < kList) sh.found[at] = make_int2(row, t);
-    });
-    int all;
-    scan(before, sh.scratch, all);
-    before = all;
-    if (own == 0) {
-        scan(valid, sh.scratch, all);
-        if (threadIdx.x == 0) *a.valid = all;
-    }
-    __syncthreads();
-    const int n = sh.n;
-    int *list = n <= kList ? sh.list : a.list + before;
-
-    // ---- where each row's tokens begin
-    {
-        constexpr int kEach = kOwnRows / kOwnThreads;
-        const int first = threadIdx.x * kEach;
-        int sum = 0;
-        if (first < rows)
-            for (int i = first; i < min(first + kEach, rows); ++i) sum += sh.counts[i];
-        int at = scan(sum, sh.scratch, all);
-        if (first < rows)
-            for (int i = first; i < min(first + kEach, rows); ++i) {
-                sh.starts[i] = at;
-                at += sh.counts[i];
-            }
-    }
-    __syncthreads();
-
-    // ---- the tokens, row by row: put there in any order (counts go down to 0, starts up to the ends) ...
-    const auto put = [&](bool mine, int row, int t) {
-        if (__any_sync(0xffffffffu, mine)) {
-            const int place = count_rows(mine, row, sh.starts);
-            if (mine) list[place] = t;
-        }
-    };
-    if (n <= kList) {
-        for (int i = warp * 32; i < n; i += kOwnThreads) {
-            const int2 f = i + lane < n ? sh.found[i + lane] : make_int2(0, 0);
-            put(i + lane < n, f.x, f.y);
-        }
-    } else {
-        look([&](int64_t id, int t) { put(id >= 0 && id < a.vocab && (id & low) == own, static_cast<int>(id >> a.shift), t); });
-    }
-    __syncthreads();
-
-    // ---- ... and then in order.  A warp has short rows, a lane up to two tokens: its place is the
-    // number of tokens before it.
-    for (int row = warp; row < rows; row += kOwnThreads / 32) {
-        const int count = sh.counts[row];
-        if (count < 2 || count > 64) continue;
-        int *mine = list + sh.starts[row] - count;
-        const int x = lane < count ? mine[lane] : INT_MAX, y = lane + 32 < count ? mine[lane + 32] : INT_MAX;
-        int px = 0, py = 0;
-        for (int j = 0; j < min(count, 32); ++j) {
-            const int u = __shfl_sync(0xffffffffu, x, j), v = __shfl_sync(0xffffffffu, y, j);
-            px += (u < x) + (v < x);
-            py += (u < y) + (v < y);
-        }
-        __syncwarp();
-        if (lane < count) mine[px] = x;
-        if (lane + 32 < count) mine[py] = y;
-    }
-    // Long ones: the tokens as bits of a map, 65536 of them at a time.
-    for (int row = 0; row < rows; ++row) {
-        const int count = sh.counts[row];
-        if (count <= 64) continue;                  // (the same for all threads)
-        const int first = sh.starts[row] - count;
-        const bool later = count > a.longest;       // the second kernel's
-        int done = 0;
-        for (int64_t t0 = 0; t0 < a.tokens && done < count; t0 += 32 * kBitWords) {
-            __syncthreads();
-            for (int i = threadIdx.x; i < kBitWords; i += kOwnThreads) sh.bits[i] = 0;
-            __syncthreads();
-            for (int i = threadIdx.x; i < count; i += kOwnThreads) {
-                const int64_t t = list[first + i] - t0;
-                if (t >= 0 && t < 32 * kBitWords) atomicOr(&sh.bits[t >> 5], 1u << (t & 31));
-            }
-            __syncthreads();
-            constexpr int kEach = kBitWords / kOwnThreads;
-            int bits = 0;
-            for (int i = 0; i < kEach; ++i) bits += __popc(sh.bits[threadIdx.x * kEach + i]);
-            int at = done + scan(bits, sh.scratch, all);
-            done += all;
-            for (int i = 0; i < kEach; ++i)
-                for (uint32_t m = sh.bits[threadIdx.x * kEach + i]; m; m &= m - 1, ++at) {
-                    const int t = static_cast<int>(t0) + (threadIdx.x * kEach + i) * 32 + __ffs(static_cast<int>(m)) - 1;
-                    if (later) a.order[before + first + at] = Segment{static_cast<int>(own + (static_cast<int64_t>(row) << a.shift)), before + first, count, t};
-                    else list[first + at] = t;      // (one map holds all tokens: nothing of the list is needed any more)
-                }
-        }
-        if (later)
-            for (int i = threadIdx.x; i < a.slices; i += kOwnThreads) a.counts[static_cast<int64_t>((before + first) / kPiece) * a.slices + i] = 0;
-    }
-    __syncthreads();
-
-    // ---- the table's rows: groups of lanes, a piece of a row's columns each
-    if (a.longest < INT_MAX)                // what the second kernel passes over
-        for (int row = warp; row < rows; row += kOwnThreads / 32) {
-            const int count = sh.counts[row];
-            if (count <= a.longest)
-                for (int i = lane; i < count; i += 32) a.order[before + sh.starts[row] - count + i].row = -1;
-        }
-    const int lanes = ALIGNED ? a.lanes : 32, groups = kOwnThreads / lanes, mine = threadIdx.x / lanes;
-    const int64_t steps = (a.cols + 8 * lanes - 1) / (8 * lanes), units = steps * rows;
-    using T = typename Elem<TYPE>::T;
-    const void *begin = a.dout.ptr, *end = end_of(static_cast<const T *>(a.dout.ptr), a.dout.stride, a.tokens, a.cols);
-    const void *out_begin = a.dtable.ptr, *out_end = end_of(static_cast<const G *>(a.dtable.ptr), a.dtable.stride, a.vocab, a.cols);
-    for (int64_t u = mine; u < units; u += groups) {
-        const int row = units <= INT_MAX ? static_cast<int>(static_cast<unsigned>(u) / static_cast<unsigned>(steps)) : static_cast<int>(u / steps);
-        const int count = sh.counts[row];
-        if (count > a.longest || (a.add && count == 0)) continue;
-        const int64_t col = (u - row * steps) * 8 * lanes + threadIdx.x % lanes * 8;
-        const int here = static_cast<int>(max(min(a.cols - col, static_cast<int64_t>(8)), static_cast<int64_t>(0)));
-        F2 sum[4] = {F2(0.0f), F2(0.0f), F2(0.0f), F2(0.0f)};
-        if (!ALIGNED || here > 0) {
-            sum_tokens<TYPE, ALIGNED>(a, list + sh.starts[row] - count, count, col, here, begin, end, sum);
-            put_sum<GRAD, ALIGNED>(a, static_cast<G *>(a.dtable.ptr) + (own + (static_cast<int64_t>(row) << a.shift)) * a.dtable.stride + col, here,
-                                   sum, out_begin, out_end);
-        }
-    }
-}
-
-// A piece of the order of all tokens, 1024 columns: of at most two rows, since each row here has more tokens than a
+// A piece of the order of all tokens, kSlice columns: of at most two rows, since each row here has more tokens than a
 // piece has: one that began before, and one that begins here.
-template <int TYPE, int GRAD, bool ALIGNED>
-__global__ void __launch_bounds__(kSumThreads) novak_embedding_pieces_kernel(GradArgs a)
+template <int TYPE, int GRAD, bool ALIGNED> __device__ __forceinline__ void sum_piece(const GradArgs &a, int piece, int slice)
 {
     using G = typename Elem<GRAD>::T;
     using T = typename Elem<TYPE>::T;
-    __shared__ int tokens[kPiece];
     __shared__ __align__(16) float part[kSumThreads * 8];
-    __shared__ Segment first;
+    __shared__ Place first, second;
     __shared__ int begins;
     __shared__ bool last;
-    start();
-    const int piece = blockIdx.x, slice = blockIdx.y, from = piece * kPiece;
-    const int here = min(*a.valid - from, kPiece);
-    if (here <= 0) return;
-    if (threadIdx.x == 0) begins = kPiece;
-    Segment s{-1, 0, 0, 0};
-    __syncthreads();
-    if (threadIdx.x < kPiece) {
-        if (static_cast<int>(threadIdx.x) < here) s = a.order[from + threadIdx.x];
-        tokens[threadIdx.x] = s.token;
-        if (threadIdx.x == 0) first = s;
-        if (s.row >= 0 && s.start == from + static_cast<int>(threadIdx.x)) begins = threadIdx.x;
+    __shared__ int tokens[kPiece];
+    const int from = piece * kPiece;
+    if (threadIdx.x < 32) {
+        Place s{-1, 0, 0, 0};
+        const int valid = *a.valid, at_most = static_cast<int>(min(a.tokens - from, static_cast<int64_t>(kPiece))), lane = threadIdx.x;
+        if (lane < at_most) s = a.order[from + lane];           // (nothing there behind the valid ones)
+        if (from + lane >= valid) s.row = -1;
+        if (lane < kPiece) tokens[lane] = s.token;
+        const unsigned m = __ballot_sync(0xffffffffu, s.row >= 0 && s.start == from + static_cast<int>(threadIdx.x));
+        const int at = m ? __ffs(static_cast<int>(m)) - 1 : kPiece;
+        if (threadIdx.x == 0) {
+            begins = at;
+            first = s;
+        }
+        if (static_cast<int>(threadIdx.x) == at) second = s;
     }
-    __syncthreads();
-    __shared__ Segment second;
-    if (static_cast<int>(threadIdx.x) == begins) second = s;
+    static_assert(kPiece <= 32, "a warp looks at a piece");
     __syncthreads();
     const int group = a.group, subs = kSumThreads / group, sub = threadIdx.x / group, t = threadIdx.x % group;
     const int64_t col = static_cast<int64_t>(slice) * kSlice + t * 8;
@@ -396,22 +419,21 @@ __global__ void __launch_bounds__(kSumThreads) novak_embedding_pieces_kernel(Gra
     for (int kind = 0; kind < 2; ++kind) {
         const int at = kind ? begins : 0;
         if (kind ? begins == kPiece : first.row < 0 || begins == 0) continue;
-        const Segment seg = kind ? second : first;
+        const Place seg = kind ? second : first;
         const int count = min(seg.start + seg.count - from, kPiece) - at;
         // this piece: every group of threads its share of the tokens, then the groups in order
-        F2 sum[4] = {F2(0.0f), F2(0.0f), F2(0.0f), F2(0.0f)};
+        F2 sum[4];
         const int share = (count + subs - 1) / subs, begin_at = min(sub * share, count);
-        sum_tokens<TYPE, ALIGNED>(a, tokens + at + begin_at, min(share, count - begin_at), col, n, begin, end, sum);
+        sum_tokens<TYPE, ALIGNED>(a, [&](int k) { return tokens[at + begin_at + k]; }, min(share, count - begin_at), col, n, begin, end, sum);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 4; ++i) *reinterpret_cast<float2 *>(part + threadIdx.x * 8 + 2 * i) = make_float2(sum[i].lo(), sum[i].hi());
         __syncthreads();
-        const int64_t pitch = a.cols;
         for (int c = threadIdx.x; c < group * 8; c += kSumThreads) {
             float x = 0.0f;
             for (int i = 0; i < subs; ++i) x += part[i * group * 8 + c];
             const int64_t out = static_cast<int64_t>(slice) * kSlice + c;
-            if (out < a.cols) a.partial[(2 * static_cast<int64_t>(piece) + kind) * pitch + out] = x;
+            if (out < a.cols) a.partial[(2 * static_cast<int64_t>(piece) + kind) * a.cols + out] = x;
         }
         // the last of the row's pieces to be done adds all of them up
         const int head = seg.start / kPiece, pieces = (seg.start + seg.count - 1) / kPiece - head + 1;
@@ -424,14 +446,14 @@ __global__ void __launch_bounds__(kSumThreads) novak_embedding_pieces_kernel(Gra
         for (int c = threadIdx.x; c < group * 8; c += kSumThreads) {
             const int64_t out = static_cast<int64_t>(slice) * kSlice + c;
             if (out >= a.cols) continue;
-            const float *p = a.partial + (2 * static_cast<int64_t>(head) + 1) * pitch + out;
+            const float *p = a.partial + (2 * static_cast<int64_t>(head) + 1) * a.cols + out;
             float x = __ldcg(p);
 #pragma unroll 16
-            for (int i = 1; i < pieces; ++i) x += __ldcg(p + (2 * static_cast<int64_t>(i) - 1) * pitch);     // (of a row that began before)
+            for (int i = 1; i < pieces; ++i) x += __ldcg(p + (2 * static_cast<int64_t>(i) - 1) * a.cols);    // (of a row that began before)
             part[c] = x;
         }
         __syncthreads();
-        if (threadIdx.x < group) {
+        if (static_cast<int>(threadIdx.x) < group) {
             F2 v[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = F2(part[threadIdx.x * 8 + 2 * i], part[threadIdx.x * 8 + 2 * i + 1]);
@@ -439,6 +461,83 @@ __global__ void __launch_bounds__(kSumThreads) novak_embedding_pieces_kernel(Gra
             put_sum<GRAD, ALIGNED>(a, p, n, v, a.dtable.ptr, end_of(static_cast<const G *>(a.dtable.ptr), a.dtable.stride, a.vocab, a.cols));
         }
         __syncthreads();
+    }
+}
+
+template <int TYPE, int GRAD, bool ALIGNED>
+__global__ void __launch_bounds__(kSumThreads, ALIGNED ? 4 : 3) novak_embedding_grad_kernel(GradArgs a)
+{
+    using G = typename Elem<GRAD>::T;
+    using T = typename Elem<TYPE>::T;
+    start();
+    // Pieces first, since they take long, but by turns with the others: they wait more than they move.
+    const int64_t pieces = a.pieces * a.slices, rest = gridDim.x - pieces, both = 2 * min(pieces, rest), b = blockIdx.x;
+    const bool is_piece = b < both ? b % 2 == 0 : pieces > rest;
+    const int64_t index = b < both ? b / 2 : b - both / 2;
+    if (is_piece) {
+        const int piece = static_cast<int>(index / a.slices);
+        sum_piece<TYPE, GRAD, ALIGNED>(a, piece, static_cast<int>(index - static_cast<int64_t>(piece) * a.slices));
+        return;
+    }
+    const int lanes = ALIGNED ? a.lanes : 32, lane = threadIdx.x % lanes;
+    const int64_t item = index * kSumWarps + threadIdx.x / 32;
+    const int64_t block = item <= INT_MAX && a.steps <= INT_MAX ? static_cast<unsigned>(item) / static_cast<unsigned>(a.steps) : item / a.steps;
+    const int64_t col = ((item - block * a.steps) * lanes + lane) * 8;
+    const int n = static_cast<int>(max(min(a.cols - col, static_cast<int64_t>(8)), static_cast<int64_t>(0)));
+    const int64_t row0 = (block * (32 / lanes) + threadIdx.x % 32 / lanes) * a.each;
+    const void *begin = a.dout.ptr, *end = end_of(static_cast<const T *>(a.dout.ptr), a.dout.stride, a.tokens, a.cols);
+    const void *out_begin = a.dtable.ptr, *out_end = end_of(static_cast<const G *>(a.dtable.ptr), a.dtable.stride, a.vocab, a.cols);
+    // a lane knows of a row; rows beyond the table are nobody's
+    int2 mine = make_int2(0, INT_MAX);
+    if (lane < a.each && row0 + lane < a.vocab) mine = a.rows[row0 + lane];
+    const unsigned group = lanes == 32 ? ~0u : ((1u << lanes) - 1) << (threadIdx.x % 32 / lanes * lanes);
+    const int shift = threadIdx.x % 32 / lanes * lanes;
+    G *p = static_cast<G *>(a.dtable.ptr) + row0 * a.dtable.stride + col;
+    unsigned none = (__ballot_sync(0xffffffffu, mine.y == 0 && lane < a.each) & group) >> shift;
+    unsigned one = (__ballot_sync(0xffffffffu, mine.y == 1) & group) >> shift;
+    unsigned some = (__ballot_sync(0xffffffffu, mine.y > 1 && mine.y <= kPiece) & group) >> shift;
+    if (!a.add)
+        for (; none; none &= none - 1) {
+            G *row = p + (__ffs(static_cast<int>(none)) - 1) * a.dtable.stride;
+            if constexpr (ALIGNED && GRAD == NOVAK_TYPE_F32) {
+                // (neighbouring lanes neighbouring pieces: with 32 bytes each, in two stores, 40 us instead of 24)
+                float4 *piece = reinterpret_cast<float4 *>(row - lane * 8) + lane;
+                const int64_t left = (a.cols - (col - lane * 8)) / 4 - lane;
+                if (left > 0) piece[0] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (left > lanes) piece[lanes] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            } else {
+                Eight<GRAD> e;
+                e.zero();
+                store_eight<ALIGNED>(row, e, n);
+            }
+        }
+    // rows of one token (most): several on their way
+    constexpr int kRows = TYPE == NOVAK_TYPE_BF16 && ALIGNED ? 4 : 2;
+    while (__any_sync(0xffffffffu, one != 0)) {
+        Fetch<TYPE, ALIGNED> raw[kRows];
+        int at[kRows];
+#pragma unroll
+        for (int k = 0; k < kRows; ++k, one &= one - 1) {
+            at[k] = __ffs(static_cast<int>(one)) - 1;           // -1: none
+            const int token = __shfl_sync(0xffffffffu, mine.x, max(at[k], 0), lanes);
+            raw[k].zero();
+            if (at[k] >= 0) raw[k].load(static_cast<const T *>(a.dout.ptr) + token * a.dout.stride + col, n, begin, end);
+        }
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) {
+            if (at[k] < 0 || (ALIGNED && n == 0)) continue;
+            F2 sum[4];
+            raw[k].eight().get(sum);
+            put_sum<GRAD, ALIGNED>(a, p + at[k] * a.dtable.stride, n, sum, out_begin, out_end);
+        }
+    }
+    for (; __any_sync(0xffffffffu, some != 0); some &= some - 1) {
+        const int i = some ? __ffs(static_cast<int>(some)) - 1 : 0;
+        const int first = __shfl_sync(0xffffffffu, mine.x, i, lanes), count = __shfl_sync(0xffffffffu, mine.y, i, lanes);
+        if (some == 0 || (ALIGNED && n == 0)) continue;
+        F2 sum[4];
+        sum_tokens<TYPE, ALIGNED>(a, [&](int k) { return a.order[first + k].token; }, count, col, n, begin, end, sum);
+        put_sum<GRAD, ALIGNED>(a, p + i * a.dtable.stride, n, sum, out_begin, out_end);
     }
 }
 
@@ -456,35 +555,29 @@ int power(int64_t n, int most)
 struct GradLayout {
     int64_t pieces;
     int slices;
-    size_t list, order, counts, valid, partial, bytes;
+    size_t list, order, rows, counts, valid, partial, bytes;
 };
 
-GradLayout layout_of(int64_t tokens, int64_t cols)
+GradLayout layout_of(int64_t tokens, int64_t vocab, int64_t cols)
 {
     GradLayout l{};
-    const bool second = tokens > kFewTokens;
-    l.pieces = second ? (tokens + kPiece - 1) / kPiece : 0;
+    l.pieces = tokens > kPiece ? (tokens + kPiece - 1) / kPiece : 0;        // (fewer tokens are no long row's)
     l.slices = static_cast<int>((cols + kSlice - 1) / kSlice);
     l.list = 0;
     l.order = l.list + round_up((tokens > kList ? tokens : 0) * sizeof(int));
-    l.counts = l.order + round_up((second ? tokens : 0) * sizeof(Segment));
+    l.rows = l.order + round_up(tokens * sizeof(Place));
+    l.counts = l.rows + round_up(vocab * sizeof(int2));
     l.valid = l.counts + round_up(l.pieces * l.slices * sizeof(int));
     l.partial = l.valid + round_up(sizeof(int));
     l.bytes = l.partial + round_up(2 * l.pieces * cols * sizeof(float));
     return l;
 }
 
-template <int TYPE, int GRAD, bool ALIGNED> cudaError_t launch_grad(const GradArgs &g, int64_t pieces, cudaStream_t stream)
+template <int TYPE, int GRAD, bool ALIGNED> cudaError_t launch_grad(const GradArgs &g, cudaStream_t stream)
 {
-    const auto kernel = novak_embedding_grad_kernel<TYPE, GRAD, ALIGNED>;
-    static std::atomic<uint64_t> asked{0};
-    cudaError_t e = ask_shared_memory(kernel, sizeof(OwnShared), asked);
-    if (e != cudaSuccess) return e;
-    const int64_t ctas = std::min<int64_t>(int64_t(1) << g.shift, g.vocab);
-    e = launch(kernel, dim3(static_cast<unsigned>(ctas)), kOwnThreads, sizeof(OwnShared), stream, g);
-    if (e != cudaSuccess || pieces == 0) return e;
-    return launch(novak_embedding_pieces_kernel<TYPE, GRAD, ALIGNED>, dim3(static_cast<unsigned>(pieces), static_cast<unsigned>(g.slices)),
-                  kSumThreads, 0, stream, g);
+    const int lanes = ALIGNED ? g.lanes : 32, rows = g.each * (32 / lanes);
+    const int64_t items = (g.vocab + rows - 1) / rows * g.steps, ctas = g.pieces * g.slices + (items + kSumWarps - 1) / kSumWarps;
+    return launch(novak_embedding_grad_kernel<TYPE, GRAD, ALIGNED>, dim3(static_cast<unsigned>(ctas)), kSumThreads, 0, stream, g);
 }
 
 }  // namespace
@@ -508,27 +601,42 @@ cudaError_t launch_embedding(const EmbedArgs &a, cudaStream_t stream)
     return launch(kernel, dim3(static_cast<unsigned>(ctas)), kLookThreads, 0, stream, l);
 }
 
-size_t embedding_grad_bytes(int64_t tokens, int64_t, int64_t cols) { return layout_of(tokens, cols).bytes; }
+size_t embedding_grad_bytes(int64_t tokens, int64_t vocab, int64_t cols) { return layout_of(tokens, vocab, cols).bytes; }
 
 cudaError_t launch_embedding_grad(const EmbedGradArgs &a, cudaStream_t stream)
 {
-    const GradLayout l = layout_of(a.tokens, a.cols);
+    const GradLayout l = layout_of(a.tokens, a.vocab, a.cols);
     uint8_t *base = static_cast<uint8_t *>(a.work);
-    GradArgs g{a, 8, l.pieces ? kPiece : INT_MAX, 0, l.slices, 0, reinterpret_cast<int *>(base + l.list), reinterpret_cast<Segment *>(base + l.order),
-               reinterpret_cast<int *>(base + l.counts), reinterpret_cast<int *>(base + l.valid), reinterpret_cast<float *>(base + l.partial)};
-    while ((a.vocab >> g.shift) >= kOwnRows) ++g.shift;
-    g.lanes = power((a.cols + 7) / 8, 32);
-    g.group = std::max(power((std::min<int64_t>(a.cols, kSlice) + 7) / 8, kSlice / 8), 32);
+    GradArgs g{a, 8, 0, 0, 0, 1, l.slices, 0, l.pieces, reinterpret_cast<int *>(base + l.list), reinterpret_cast<Place *>(base + l.order),
+               reinterpret_cast<int2 *>(base + l.rows), reinterpret_cast<int *>(base + l.counts), reinterpret_cast<int *>(base + l.valid),
+               reinterpret_cast<float *>(base + l.partial)};
+    // Neighbouring rows that are short together go to one CTA, as long as there are blocks for all CTAs.
+    while ((a.cols << g.fold) < 256 && (a.vocab >> (g.fold + g.shift)) >= 2) ++g.fold;
+    while (((((a.vocab + (1 << g.fold) - 1) >> g.fold) + (int64_t(1) << g.shift) - 1) >> g.shift << g.fold) > kOwnRows) ++g.shift;
+    const int64_t ctas = std::min<int64_t>(int64_t(1) << g.shift, (a.vocab + (int64_t(1) << g.fold) - 1) >> g.fold);
+    static std::atomic<uint64_t> asked{0};
+    cudaError_t e = ask_shared_memory(novak_embedding_order_kernel, sizeof(OwnShared), asked);
+    if (e == cudaSuccess)
+        e = launch(novak_embedding_order_kernel, dim3(static_cast<unsigned>((ctas + kCluster - 1) / kCluster * kCluster)), kOwnThreads, sizeof(OwnShared), stream, g);
+    if (e != cudaSuccess) return e;
+
     const bool aligned = (a.tokens == 0 || wide(a.dout, a.type, a.tokens)) && wide(a.dtable, a.grad_type, a.vocab) && a.cols % 8 == 0;
+    g.lanes = power((a.cols + 7) / 8, 32);
+    const int lanes = aligned ? g.lanes : 32;
+    g.steps = (a.cols + 8 * lanes - 1) / (8 * lanes);
+    // as many rows as leave two rounds of warps (148 SMs with 32 each) something to do
+    g.each = 1;
+    while (g.each < std::min(kMostRows, lanes) && a.vocab * g.steps / (2 * g.each * (32 / lanes)) >= 148 * 32 * 2) g.each *= 2;
+    g.group = std::max(power((std::min<int64_t>(a.cols, kSlice) + 7) / 8, kSlice / 8), 32);
     const int which = a.type * 4 + a.grad_type * 2 + aligned;
-    return which == 0   ? launch_grad<0, 0, false>(g, l.pieces, stream)
-           : which == 1 ? launch_grad<0, 0, true>(g, l.pieces, stream)
-           : which == 2 ? launch_grad<0, 1, false>(g, l.pieces, stream)
-           : which == 3 ? launch_grad<0, 1, true>(g, l.pieces, stream)
-           : which == 4 ? launch_grad<1, 0, false>(g, l.pieces, stream)
-           : which == 5 ? launch_grad<1, 0, true>(g, l.pieces, stream)
-           : which == 6 ? launch_grad<1, 1, false>(g, l.pieces, stream)
-                        : launch_grad<1, 1, true>(g, l.pieces, stream);
+    return which == 0   ? launch_grad<0, 0, false>(g, stream)
+           : which == 1 ? launch_grad<0, 0, true>(g, stream)
+           : which == 2 ? launch_grad<0, 1, false>(g, stream)
+           : which == 3 ? launch_grad<0, 1, true>(g, stream)
+           : which == 4 ? launch_grad<1, 0, false>(g, stream)
+           : which == 5 ? launch_grad<1, 0, true>(g, stream)
+           : which == 6 ? launch_grad<1, 1, false>(g, stream)
+                        : launch_grad<1, 1, true>(g, stream);
 }
 
 }  // namespace novak

@@ -35,6 +35,7 @@ namespace {
 constexpr float kScaleX = 4096.0f, kScaleA = 2048.0f, kScaleB = 4096.0f, kScaleLow = 2048.0f;   // (the low part: on top of X's)
 constexpr int kPanel = 64, kBlock = 128, kThreads = 256;
 constexpr int kUnitRows = 128;              // a unit of the first two kernels: so many rows of a panel
+constexpr int kMostChunks = kThreads;       // of a matrix
 
 // A matrix as the kernels see it.  Panels' places are in rows of 128 bytes from the workspace's start.
 struct Item {
@@ -46,7 +47,8 @@ struct Item {
     int x[2], low, gram, poly;  // X's first part (taken in turns), second part, A, B
     int x_pitch, s_pitch;       // rows of a panel
     int diag;                   // floats from the diagonals' start: A's, then B's (s_pitch each)
-    int unit, units;            // first unit, how many
+    int unit, units;            // of 128 rows of a panel: first one, how many
+    int chunk, chunks;          // of units, whose squares are summed together: first one, how many
     int tile[3], tiles[3];      // of each product: the first one (from the product's first), how many
     float step;
 };
@@ -55,9 +57,7 @@ struct Work {
     __half *panels;
     float *diags;
     Item *items;
-    double *partial;            // per unit
-    float2 *scale;              // per matrix: G is multiplied by one, then by the other
-    unsigned *arrived;          // per matrix: units, of the first kernel
+    double *partial;            // per chunk
     unsigned *done;             // per matrix: parts of its tiles that are stored
 };
 
@@ -66,8 +66,8 @@ struct Control {
 };
 
 struct Layout {
-    int64_t panel_rows = 0, diag_floats = 0, units = 0;
-    size_t diags, items, partial, scale, arrived, done, control, bytes;
+    int64_t panel_rows = 0, diag_floats = 0, units = 0, chunks = 0;
+    size_t diags, items, partial, done, control, bytes;
 };
 
 constexpr size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
@@ -99,6 +99,9 @@ bool place(Layout &l, int64_t rows, int64_t cols, Item &it)
     it.unit = static_cast<int>(l.units);
     it.units = static_cast<int>(x / kUnitRows);
     l.units += it.units;
+    it.chunk = static_cast<int>(l.chunks);
+    it.chunks = std::min(it.units, kMostChunks);
+    l.chunks += it.chunks;
     return true;
 }
 
@@ -107,134 +110,175 @@ bool finish_layout(Layout &l, int n)
     l.diags = static_cast<size_t>(l.panel_rows) * 128;
     l.items = l.diags + round_up(l.diag_floats * sizeof(float));
     l.partial = l.items + round_up(n * sizeof(Item));
-    l.scale = l.partial + round_up(l.units * sizeof(double));
-    l.arrived = l.scale + round_up(n * sizeof(float2));
-    l.done = l.arrived + round_up(n * sizeof(unsigned));
+    l.done = l.partial + round_up(l.chunks * sizeof(double));
     l.control = l.done + round_up(n * sizeof(unsigned));
     l.bytes = l.control + round_up(sizeof(Control));
     return true;
 }
 
 // ---- device: what the kernels share -------------------------------------------------
-// The matrix that `unit` belongs to, by the whole warp: of the items' first units the last one
-// that is not above it.
-__device__ __forceinline__ int item_of(const Item *items, int n, int unit)
+__device__ __forceinline__ uint32_t pack_half(float a, float b)
+{
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ float2 unpack_half(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
+
+// Of n items the last one whose first(item) is not above `at`, by the whole warp.
+template <typename First> __device__ __forceinline__ int item_of(int n, int at, const First &first)
 {
     int lo = 0, count = n;          // the answer is in [lo, lo + count)
     while (count > 1) {
-        const int stride = (count + 31) / 32, at = lo + static_cast<int>(threadIdx.x % 32) * stride;
-        const unsigned below = __ballot_sync(0xffffffffu, at < lo + count && items[at].unit <= unit);
-        const int k = 31 - __clz(static_cast<int>(below));      // (the first always is)
-        const int end = lo + count;
-        lo += k * stride;
+        const int stride = (count + 31) / 32, mine = lo + static_cast<int>(threadIdx.x % 32) * stride, end = lo + count;
+        const unsigned below = __ballot_sync(0xffffffffu, mine < end && first(mine) <= at);
+        lo += (31 - __clz(static_cast<int>(below))) * stride;       // (the first always is)
         count = min(stride, end - lo);
     }
     return lo;
 }
 
+// ---- |G|, and X to begin with
 struct HostItems {
-    static constexpr int kMost = 200;        // (a launch takes 32764 bytes)
+    static constexpr int kMost = 200;       // (a launch takes 32764 bytes)
     Item item[kMost];
 };
-
-__global__ void novak_orthogonalize_items_kernel(const __grid_constant__ HostItems from, int first, int count, Work w, Control *control)
-{
-    start();
-    for (int i = threadIdx.x; i < count; i += blockDim.x) {
-        w.items[first + i] = from.item[i];
-        w.arrived[first + i] = w.done[first + i] = 0;
-    }
-    if (threadIdx.x == 0) *control = Control{0, 0, 0};
-}
+static_assert(sizeof(HostItems) + 256 <= 32764, "a launch's parameters");
 
 struct Momentum {
     int on, nesterov;
     float momentum;
 };
 
-// An element of G: of g, or of the momentum that g is part of.
-template <int TYPE>
-__device__ __forceinline__ float update_of(const Item &it, const Momentum &mo, int64_t row, int64_t col, bool advance)
+// A unit of G, four neighbouring elements of 8 rows per thread: f(row, column of the panel, elements), zeros beyond
+// the matrix.  G is g, or what momentum makes of it (`advance`: and m goes on).
+template <int TYPE, typename F>
+__device__ __forceinline__ void for_unit(const Item &it, const Momentum &mo, int unit, bool advance, const F &f)
 {
-    const float g = param_at(it.g, TYPE, row * it.g_stride + col);
-    if (!mo.on) return g;
-    float *p = it.m + row * it.cols + col;
-    float m = *p;
-    if (advance) *p = m = fmaf(mo.momentum, m, g);
-    return mo.nesterov ? fmaf(mo.momentum, m, g) : m;
-}
-
-// |G|^2 in 64 bits (a square in fp32 would be lost below 1e-19), a sum per unit; the CTA whose
-// unit is its matrix's last to arrive adds them up in order.
-template <int TYPE>
-__global__ void __launch_bounds__(kThreads) novak_orthogonalize_norm_kernel(Work w, int n, Momentum mo, float eps)
-{
-    __shared__ double sums[kThreads / 32];
-    __shared__ bool last;
-    start();
-    const int which = item_of(w.items, n, blockIdx.x);
-    const Item &it = w.items[which];
-    const int unit = static_cast<int>(blockIdx.x) - it.unit, blocks = it.x_pitch / kUnitRows;
-    const int row0 = unit % blocks * kUnitRows, col0 = unit / blocks * kPanel;
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    double sum = 0.0;
-    for (int i = warp; i < kUnitRows; i += kThreads / 32)
-        for (int k = 0; k < 2; ++k) {
-            const int row = row0 + i, col = col0 + 32 * k + lane;
-            if (row < it.rows && col < it.cols) {
-                const double x = update_of<TYPE>(it, mo, row, col, true);
-                sum = fma(x, x, sum);
+    using T = typename Elem<TYPE>::T;
+    const int panels = (it.cols + kPanel - 1) / kPanel, row0 = unit / panels * kUnitRows + threadIdx.x / 16, c = threadIdx.x % 16 * 4;
+    const int col = unit % panels * kPanel + c;
+    const T *g = static_cast<const T *>(it.g) + col;
+    const bool vector = (reinterpret_cast<uintptr_t>(it.g) & (4 * sizeof(T) - 1)) == 0 && it.g_stride % 4 == 0 && it.cols % 4 == 0 &&
+                        (reinterpret_cast<uintptr_t>(it.m) & 15u) == 0;
+    constexpr int kRows = kUnitRows / (kThreads / 16);
+    float v[kRows][4] = {}, m[kRows][4];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const int row = row0 + i * (kThreads / 16);
+        if (row >= it.rows || col >= it.cols) continue;
+        if (vector) {
+            if constexpr (TYPE == NOVAK_TYPE_F32) {
+                const float4 x = *reinterpret_cast<const float4 *>(g + row * it.g_stride);
+                v[i][0] = x.x; v[i][1] = x.y; v[i][2] = x.z; v[i][3] = x.w;
+            } else {
+                const uint2 x = *reinterpret_cast<const uint2 *>(g + row * it.g_stride);
+                widen(x.x).get(v[i][0], v[i][1]);
+                widen(x.y).get(v[i][2], v[i][3]);
             }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (col + k < it.cols) v[i][k] = to_float(g[row * it.g_stride + k]);
         }
-    const auto reduce = [&](double x) {
-        for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-        __syncthreads();
-        if (lane == 0) sums[warp] = x;
-        __syncthreads();
-        x = 0.0;
-        for (int i = 0; i < kThreads / 32; ++i) x += sums[i];
-        return x;
-    };
-    sum = reduce(sum);
-    if (threadIdx.x == 0) {
-        w.partial[blockIdx.x] = sum;
-        __threadfence();
-        last = atomicAdd(w.arrived + which, 1u) + 1 == static_cast<unsigned>(it.units);
     }
+    if (mo.on) {
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            const int row = row0 + i * (kThreads / 16);
+            if (row >= it.rows || col >= it.cols) continue;
+            float *p = it.m + static_cast<int64_t>(row) * it.cols + col;
+            if (vector) {
+                const float4 x = *reinterpret_cast<const float4 *>(p);
+                m[i][0] = x.x; m[i][1] = x.y; m[i][2] = x.z; m[i][3] = x.w;
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) m[i][k] = col + k < it.cols ? p[k] : 0.0f;
+            }
+            if (advance) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) m[i][k] = fmaf(mo.momentum, m[i][k], v[i][k]);
+                if (vector) {
+                    *reinterpret_cast<float4 *>(p) = make_float4(m[i][0], m[i][1], m[i][2], m[i][3]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (col + k < it.cols) p[k] = m[i][k];
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[i][k] = mo.nesterov ? fmaf(mo.momentum, m[i][k], v[i][k]) : m[i][k];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) f(row0 + i * (kThreads / 16), c, v[i]);
+}
+
+__device__ __forceinline__ double sum_of_all(double x, double *scratch)
+{
+    for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+    if (threadIdx.x % 32 == 0) scratch[threadIdx.x / 32] = x;
     __syncthreads();
-    if (!last) return;
-    __threadfence();
-    sum = 0.0;
-    for (int i = threadIdx.x; i < it.units; i += kThreads) sum += __ldcg(w.partial + it.unit + i);
-    sum = sqrt(reduce(sum));
-    // (a norm that is not finite makes everything of the matrix NaN)
-    const double scale = !(sum < INFINITY) ? NAN : sum > 0.0 ? kScaleX / fmax(sum, static_cast<double>(eps)) : 0.0;
-    const float tiny = scale > 1e36 ? 0x1p100f : 1.0f;          // (its reciprocal is beyond fp32)
-    if (threadIdx.x == 0) w.scale[which] = make_float2(tiny, static_cast<float>(scale / tiny));
+    x = 0.0;
+    for (int i = 0; i < kThreads / 32; ++i) x += scratch[i];
+    return x;
 }
 
-// X's two parts in units of 2^-12: v is close to hi + lo / 2^11.
-__device__ __forceinline__ void split(float v, __half &hi, __half &lo)
-{
-    hi = __float2half_rn(v);
-    lo = __float2half_rn((v - __half2float(hi)) * kScaleLow);
-}
-
+// The sum of a chunk's squares, in 64 bits (a square in fp32 would be lost below 1e-19).  The items come with the
+// launch, from number `first` on, and are put down for the kernels behind.
 template <int TYPE>
-__global__ void __launch_bounds__(kThreads) novak_orthogonalize_start_kernel(Work w, int n, Momentum mo)
+__global__ void __launch_bounds__(kThreads) novak_orthogonalize_norm_kernel(const __grid_constant__ HostItems from, int first, int count, Work w,
+                                                                             Control *control, Momentum mo)
 {
+    __shared__ double scratch[kThreads / 32];
     start();
-    const int which = item_of(w.items, n, blockIdx.x);
-    const Item &it = w.items[which];
-    const int unit = static_cast<int>(blockIdx.x) - it.unit, blocks = it.x_pitch / kUnitRows;
-    const int row0 = unit % blocks * kUnitRows, panel = unit / blocks;
-    const float2 scale = w.scale[which];
-    for (int e = threadIdx.x; e < kUnitRows * kPanel; e += kThreads) {
-        const int row = row0 + e / kPanel, col = panel * kPanel + e % kPanel;
-        const float v = row < it.rows && col < it.cols ? update_of<TYPE>(it, mo, row, col, false) * scale.x * scale.y : 0.0f;
-        const int64_t at = (static_cast<int64_t>(panel) * it.x_pitch + row) * kPanel + e % kPanel;
-        split(v, w.panels[static_cast<int64_t>(it.x[0]) * kPanel + at], w.panels[static_cast<int64_t>(it.low) * kPanel + at]);
+    if (blockIdx.x == 0) {
+        for (int i = threadIdx.x; i < count; i += kThreads) {
+            w.items[first + i] = from.item[i];
+            w.done[first + i] = 0;
+        }
+        if (threadIdx.x == 0) *control = Control{0, 0, 0};
     }
+    const int chunk = from.item[0].chunk + static_cast<int>(blockIdx.x);
+    const Item &it = from.item[item_of(count, chunk, [&](int i) { return from.item[i].chunk; })];
+    const int64_t mine = chunk - it.chunk;
+    double sum = 0.0;
+    for (int64_t u = mine * it.units / it.chunks; u < (mine + 1) * it.units / it.chunks; ++u)
+        for_unit<TYPE>(it, mo, static_cast<int>(u), true, [&](int, int, const float (&v)[4]) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum = fma(static_cast<double>(v[k]), static_cast<double>(v[k]), sum);
+        });
+    sum = sum_of_all(sum, scratch);
+    if (threadIdx.x == 0) w.partial[chunk] = sum;
+}
+
+// X's two parts in units of 2^-12.
+template <int TYPE>
+__global__ void __launch_bounds__(kThreads) novak_orthogonalize_start_kernel(Work w, int n, Momentum mo, float eps)
+{
+    __shared__ double scratch[kThreads / 32];
+    start();
+    const int unit = blockIdx.x;
+    const Item &it = w.items[item_of(n, unit, [&](int i) { return w.items[i].unit; })];
+    const double norm = sqrt(sum_of_all(static_cast<int>(threadIdx.x) < it.chunks ? w.partial[it.chunk + threadIdx.x] : 0.0, scratch));
+    // (a norm that is not finite makes everything of the matrix NaN)
+    const double scale = !(norm < INFINITY) ? NAN : norm > 0.0 ? kScaleX / fmax(norm, static_cast<double>(eps)) : 0.0;
+    const float tiny = scale > 1e36 ? 0x1p100f : 1.0f, rest = static_cast<float>(scale / tiny);     // (its reciprocal is beyond fp32)
+    const int panels = (it.cols + kPanel - 1) / kPanel, panel = (unit - it.unit) % panels;
+    for_unit<TYPE>(it, mo, unit - it.unit, false, [&](int row, int c, const float (&v)[4]) {
+        float x[4];
+        uint32_t hi[2], lo[2];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = v[k] * tiny * rest;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            hi[k] = pack_half(x[2 * k], x[2 * k + 1]);
+            const float2 h = unpack_half(hi[k]);
+            lo[k] = pack_half((x[2 * k] - h.x) * kScaleLow, (x[2 * k + 1] - h.y) * kScaleLow);
+        }
+        const int64_t at = (static_cast<int64_t>(panel) * it.x_pitch + row) * kPanel + c;
+        *reinterpret_cast<uint2 *>(w.panels + static_cast<int64_t>(it.x[0]) * kPanel + at) = make_uint2(hi[0], hi[1]);
+        *reinterpret_cast<uint2 *>(w.panels + static_cast<int64_t>(it.low) * kPanel + at) = make_uint2(lo[0], lo[1]);
+    });
 }
 
 // ---- the products on the tensor cores --------------------------------------------------
@@ -255,8 +299,8 @@ __global__ void __launch_bounds__(kThreads) novak_orthogonalize_start_kernel(Wor
 // In each CTA: warps 0-7 take tiles out (a warp a quarter of the lanes, warps 0-3 the left half of
 // the columns), warp 8 brings operands, warp 9 issues the products (of the pair: in the
 // leading CTA), warp 10 of the leading CTA hands tiles out.
-constexpr int kPairs = 74, kStages = 6, kRing = 2;
-constexpr int kBoxBytes = kPanel * 128, kStageBytes = 4 * kBoxBytes, kSideBytes = 2 * kBoxBytes;
+constexpr int kPairs = 74, kStages = 7, kRing = 2;
+constexpr int kBoxBytes = kPanel * 128, kStageBytes = 4 * kBoxBytes;
 constexpr int kOutWarps = 8, kLoadWarp = 8, kMmaWarp = 9, kTileWarp = 10, kTcThreads = 384;
 
 // What is to be done for a tile, as the leading CTA's warp 10 writes it into both CTAs.
@@ -281,7 +325,7 @@ struct Shared {
     Tile tiles[kRing];
     alignas(16) float columns[2][128];      // a half's columns of a diagonal
 };
-constexpr int kSmemBytes = kStages * kStageBytes + 2 * kSideBytes + 1024 + static_cast<int>(sizeof(Shared));
+constexpr int kSmemBytes = kStages * kStageBytes + 1024 + static_cast<int>(sizeof(Shared));
 static_assert(kSmemBytes <= 227 * 1024, "shared memory");
 
 struct ProductArgs {
@@ -361,15 +405,6 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap *map, i
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];"
                  ::"r"(dst), "l"(map), "r"(0), "r"(y), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void store_box(const CUtensorMap *map, int y, uint32_t src)
-{
-    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
-                 ::"l"(map), "r"(0), "r"(y), "r"(src) : "memory");
-}
-__device__ __forceinline__ void stores_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
-__device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
-
 // The four warps of one half of the columns; whether all of them agree.
 __device__ __forceinline__ void half_sync(int side)
 {
@@ -390,10 +425,19 @@ __device__ constexpr uint32_t fp16_descriptor(int columns, bool a_across, bool b
     return 1u << 4 | (a_across ? 1u << 15 : 0u) | (b_across ? 1u << 16 : 0u) | static_cast<uint32_t>(columns >> 3) << 17 | (256u >> 4) << 24;
 }
 
-__device__ __forceinline__ void tmem_load32(uint32_t tmem, float (&v)[32])
+// 32 consecutive columns of this warp's 32 lanes; done at tmem_load_wait.
+__device__ __forceinline__ void tmem_load32(uint32_t tmem, uint32_t (&r)[32])
 {
-    tmem_load16(tmem, reinterpret_cast<float (&)[16]>(v[0]));
-    tmem_load16(tmem + 16, reinterpret_cast<float (&)[16]>(v[16]));
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
+          "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]),
+          "=r"(r[30]), "=r"(r[31])
+        : "r"(tmem) : "memory");
 }
 
 // Tile number t, by the whole warp.
@@ -405,14 +449,7 @@ __device__ __forceinline__ Tile tile_at(const ProductArgs &a, int64_t t)
     int rest = static_cast<int>(t % per_step);
     r.what = rest >= a.first[2] ? 2 : rest >= a.first[1] ? 1 : 0;
     rest -= a.first[r.what];
-    // the matrix: the last one whose tiles begin at `rest` or before
-    int lo = 0, count = a.n;
-    while (count > 1) {
-        const int stride = (count + 31) / 32, at = lo + static_cast<int>(threadIdx.x % 32) * stride, end = lo + count;
-        const unsigned below = __ballot_sync(0xffffffffu, at < end && a.w.items[at].tile[r.what] <= rest);
-        lo += (31 - __clz(static_cast<int>(below))) * stride;
-        count = min(stride, end - lo);
-    }
+    const int lo = item_of(a.n, rest, [&](int i) { return a.w.items[i].tile[r.what]; });
     r.which = lo;
     const Item &it = a.w.items[lo];
     rest -= it.tile[r.what];
@@ -475,243 +512,205 @@ __device__ __forceinline__ Tile tile_at(const ProductArgs &a, int64_t t)
 }
 
 // ---- taking a tile out
-// Packed fp16 (or bf16) pairs of 64 columns of a thread's row: into a half's place in shared
-// memory, as the boxes of a panel's rows lie there (128 bytes a row, 16-byte pieces
-// changing places by the row's number).
-__device__ __forceinline__ void put_row(uint32_t place, int r, const uint32_t (&h)[32])
+// A thread has a row (a lane of tensor memory) and 32 columns at a time, 64 bytes of a panel's
+// row, which go straight to memory and come from there by 32 bytes: whole sectors of L2, which
+// a way through shared memory would not make better (with tensor copies out of shared memory, which the
+// next part waited for, a tile took longer than 768 products of it).
+// 32 columns of a panel's row (other SMs wrote it: not from the first-level cache).
+__device__ __forceinline__ void get_part(const __half *p, uint32_t (&h)[16])
 {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(place + r * 128 + ((j ^ (r & 7)) << 4)), "r"(h[4 * j]), "r"(h[4 * j + 1]),
-                     "r"(h[4 * j + 2]), "r"(h[4 * j + 3]) : "memory");
+    for (int j = 0; j < 2; ++j)
+        asm volatile("ld.relaxed.gpu.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(h[8 * j]), "=r"(h[8 * j + 1]), "=r"(h[8 * j + 2]), "=r"(h[8 * j + 3]), "=r"(h[8 * j + 4]), "=r"(h[8 * j + 5]),
+                       "=r"(h[8 * j + 6]), "=r"(h[8 * j + 7]) : "l"(p + 16 * j) : "memory");
 }
-// The same transposed: the columns become rows, the 128 rows two boxes' columns.
-__device__ __forceinline__ void put_column(uint32_t place, int r, const uint32_t (&h)[32])
+__device__ __forceinline__ void put_part(__half *p, const uint32_t (&h)[16])
 {
-    const uint32_t at = place + (r >> 6) * kBoxBytes + (r & 7) * 2;
-    const int piece = (r & 63) >> 3;
 #pragma unroll
-    for (int c = 0; c < 64; ++c)
-        asm volatile("st.shared.u16 [%0], %1;" ::"r"(at + c * 128 + ((piece ^ (c & 7)) << 4)),
-                     "h"(static_cast<uint16_t>(c & 1 ? h[c / 2] >> 16 : h[c / 2])) : "memory");
+    for (int j = 0; j < 2; ++j)
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p + 16 * j), "r"(h[8 * j]), "r"(h[8 * j + 1]), "r"(h[8 * j + 2]),
+                     "r"(h[8 * j + 3]), "r"(h[8 * j + 4]), "r"(h[8 * j + 5]), "r"(h[8 * j + 6]), "r"(h[8 * j + 7]) : "memory");
 }
-
-// Two boxes of a half's place on their way to rows y0 and y1 (-1: not stored).
-__device__ __forceinline__ void send(const CUtensorMap *map, uint32_t place, int side, bool issuer, int y0, int y1)
+// The same transposed: 32 rows of a warp's 32 lanes.  `p`: the first of them, at the lane's column but
+// for its lowest bit; neighbouring lanes exchange halves, so that each has two columns of every other row.
+__device__ __forceinline__ void put_across(__half *p, const uint32_t (&h)[16])
 {
-    fence_async_shared();
-    half_sync(side);
-    if (issuer) {
-        if (y0 >= 0) store_box(map, y0, place);
-        if (y1 >= 0) store_box(map, y1, place + kBoxBytes);
-        stores_commit();
-    }
-}
-// The half's place is free again.
-__device__ __forceinline__ void reclaim(int side, bool issuer)
-{
-    if (issuer) stores_read();
-    half_sync(side);
-}
-
-__device__ __forceinline__ uint32_t pack_half(float a, float b)
-{
-    const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t *>(&h);
-}
-__device__ __forceinline__ float2 unpack_half(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
-
-// 32 columns of a row of a panel, 64 bytes, past the first-level cache (other SMs wrote it).
-__device__ __forceinline__ void get_row(const __half *panels, int64_t row, int half, uint32_t (&h)[16])
-{
-    const uint4 *p = reinterpret_cast<const uint4 *>(panels + row * kPanel + 32 * half);
+    const bool odd = threadIdx.x & 1;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const uint4 v = __ldcg(p + j);
-        h[4 * j] = v.x;
-        h[4 * j + 1] = v.y;
-        h[4 * j + 2] = v.z;
-        h[4 * j + 3] = v.w;
+    for (int i = 0; i < 16; ++i) {
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, h[i], 1);
+        const uint32_t w = odd ? __byte_perm(other, h[i], 0x7632) : __byte_perm(h[i], other, 0x5410);
+        *reinterpret_cast<uint32_t *>(p + (2 * i + odd) * kPanel) = w;
     }
 }
 
-// A half's 64 columns (bf16: two to a word; theta's step: fp32, 32 columns at a time) to the caller's
-// rows, from shared memory, so that a row's pieces go out together.
-template <bool THETA>
-__device__ __forceinline__ void write_out(const ProductArgs &a, const Item &it, uint32_t place, int t, int row0, int col0)
+// 32 columns of X (bf16: two to a word), or of theta's step, to a caller's row.
+__device__ __forceinline__ void write_out(const Item &it, int64_t row, int col, const float (&v)[32])
 {
-    constexpr int kEach = THETA ? 4 : 8;            // elements of a piece
-    const bool vector = THETA ? it.cols % 4 == 0 && (reinterpret_cast<uintptr_t>(it.out) & 15u) == 0
-                              : it.out_stride % 8 == 0 && (reinterpret_cast<uintptr_t>(it.out) & 15u) == 0;
-#pragma unroll 2
-    for (int i = 0; i < 8; ++i) {
-        const int r = i * 16 + t / 8, j = t % 8, row = row0 + r, col = col0 + j * kEach;
-        uint32_t v[4];
-        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
-                     : "r"(place + r * 128 + ((j ^ (r & 7)) << 4)) : "memory");
-        if (row >= it.rows || col >= it.cols) continue;
-        if constexpr (THETA) {
-            float *p = static_cast<float *>(it.out) + static_cast<int64_t>(row) * it.out_stride + col;
-            if (vector) {
-                float4 x = *reinterpret_cast<const float4 *>(p);
-                x.x = fmaf(-it.step, __uint_as_float(v[0]), a.decay * x.x);
-                x.y = fmaf(-it.step, __uint_as_float(v[1]), a.decay * x.y);
-                x.z = fmaf(-it.step, __uint_as_float(v[2]), a.decay * x.z);
-                x.w = fmaf(-it.step, __uint_as_float(v[3]), a.decay * x.w);
-                *reinterpret_cast<float4 *>(p) = x;
-            } else {
+    uint16_t *p = static_cast<uint16_t *>(it.out) + row * it.out_stride + col;
+    if ((reinterpret_cast<uintptr_t>(p) & 15u) == 0 && col + 32 <= it.cols) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (col + k < it.cols) p[k] = fmaf(-it.step, __uint_as_float(v[k]), a.decay * p[k]);
-            }
-        } else {
-            uint16_t *p = static_cast<uint16_t *>(it.out) + static_cast<int64_t>(row) * it.out_stride + col;
-            if (vector && col + 8 <= it.cols) {
-                *reinterpret_cast<uint4 *>(p) = make_uint4(v[0], v[1], v[2], v[3]);
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (col + k < it.cols) p[k] = static_cast<uint16_t>(k & 1 ? v[k / 2] >> 16 : v[k / 2]);
-            }
-        }
-    }
-}
-
-// A panel's width of a thread's row (lane of tensor memory), from column `col` on.
-__device__ __forceinline__ void take_panel(const ProductArgs &a, const CUtensorMap *map, const Item &it, const Tile &tile, uint32_t src,
-                                           uint32_t place, int side, int r, int row0, int col, float *columns)
-{
-    const bool issuer = r == 0;
-    const int row = row0 + r, panel = col / kPanel;
-    float *da = a.w.diags + it.diag, *db = da + it.s_pitch;
-    if (tile.what < 2) {
-        // block row and column of 128
-        const int bi = row0 / kBlock, bj = col / kBlock;
-        if (bj < bi) return;                // (the same for all of the half)
-        const bool mirror = bj > bi;
-        const int base = tile.what == 0 ? it.gram : it.poly;
-        const float b = a.coefficients[tile.step][1], c = a.coefficients[tile.step][2];
-        uint32_t h[32];
-        float d_row = 0.0f;
-        if (tile.what == 1) {
-            if (r < 64) columns[r] = __ldcg(da + col + r);
-            d_row = __ldcg(da + row);
-        }
-        reclaim(side, issuer);
-#pragma unroll
-        for (int part = 0; part < 2; ++part) {
-            uint32_t old[16];
-            if (tile.what == 1) get_row(a.w.panels, static_cast<int64_t>(it.gram) + static_cast<int64_t>(panel) * it.s_pitch + row, part, old);
-            float v[32];
-            tmem_load32(src + 32 * part, v);
-            const int on = row - col - 32 * part;           // this row's diagonal element is here if in [0, 32)
-            if (tile.what == 0) {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    if (i == on) {
-                        da[row] = v[i] * (1.0f / (kScaleX * kScaleX));
-                        v[i] = 0.0f;
-                    }
-                    v[i] *= kScaleA / (kScaleX * kScaleX);
-                }
-            } else {
-                constexpr float kSquare = 1.0f / (kScaleA * kScaleA);
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    const float2 pair = unpack_half(old[i / 2]);
-                    const float off = (i & 1 ? pair.y : pair.x) * (1.0f / kScaleA), d = d_row + columns[32 * part + i];
-                    if (i == on) {
-                        db[row] = fmaf(c, fmaf(v[i], kSquare, d_row * d_row), b * d_row);
-                        v[i] = 0.0f;
-                    } else {
-                        v[i] = kScaleB * fmaf(c, fmaf(v[i], kSquare, d * off), b * off);
-                    }
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) h[16 * part + i] = pack_half(v[2 * i], v[2 * i + 1]);
-        }
-        put_row(place, r, h);
-        const int y = base + panel * it.s_pitch + row0;
-        send(map, place, side, issuer, y, y + 64);
-        if (mirror) {
-            reclaim(side, issuer);
-            put_column(place, r, h);
-            const int z = base + row0 / kPanel * it.s_pitch + col;
-            send(map, place, side, issuer, z, row0 + 64 < it.side ? z + it.s_pitch : -1);
-        }
-        return;
-    }
-    const bool last = tile.step + 1 == a.steps, full = tile.step + 2 >= a.steps;
-    const int turn = tile.step & 1;
-    const float ca = a.coefficients[tile.step][0];
-    float d_row = 0.0f;
-    if (it.tall) {
-        if (r < 64) columns[r] = __ldcg(db + col + r);
+        for (int j = 0; j < 4; ++j)
+            *reinterpret_cast<uint4 *>(p + 8 * j) = make_uint4(bf16_pair(v[8 * j], v[8 * j + 1]), bf16_pair(v[8 * j + 2], v[8 * j + 3]),
+                                                               bf16_pair(v[8 * j + 4], v[8 * j + 5]), bf16_pair(v[8 * j + 6], v[8 * j + 7]));
     } else {
-        d_row = __ldcg(db + row);
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (col + j < it.cols) reinterpret_cast<__nv_bfloat16 *>(p)[j] = __float2bfloat16_rn(v[j]);
     }
-    reclaim(side, issuer);
-    const int64_t at = static_cast<int64_t>(panel) * it.x_pitch + row;
-    uint32_t hi[32], lo[32];
+}
+__device__ __forceinline__ void step_theta(const Item &it, float decay, int64_t row, int col, const float (&v)[32])
+{
+    float *p = static_cast<float *>(it.out) + row * it.out_stride + col;
+    if ((reinterpret_cast<uintptr_t>(p) & 15u) == 0 && col + 32 <= it.cols) {
 #pragma unroll
-    for (int part = 0; part < 2; ++part) {
-        uint32_t x_hi[16], x_lo[16];
-        get_row(a.w.panels, it.x[turn] + at, part, x_hi);
-        get_row(a.w.panels, it.low + at, part, x_lo);
-        float v[32];
-        tmem_load32(src + 32 * part, v);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float2 p = unpack_half(x_hi[i]), q = unpack_half(x_lo[i]);
-            const float x0 = fmaf(q.x, 1.0f / kScaleLow, p.x), x1 = fmaf(q.y, 1.0f / kScaleLow, p.y);
-            const float d0 = it.tall ? columns[32 * part + 2 * i] : d_row, d1 = it.tall ? columns[32 * part + 2 * i + 1] : d_row;
-            v[2 * i] = fmaf(v[2 * i], 1.0f / kScaleB, fmaf(d0, full ? x0 : p.x, ca * x0));
-            v[2 * i + 1] = fmaf(v[2 * i + 1], 1.0f / kScaleB, fmaf(d1, full ? x1 : p.y, ca * x1));
+        for (int j = 0; j < 8; ++j) {
+            float4 x = *reinterpret_cast<const float4 *>(p + 4 * j);
+            x.x = fmaf(-it.step, v[4 * j], decay * x.x);
+            x.y = fmaf(-it.step, v[4 * j + 1], decay * x.y);
+            x.z = fmaf(-it.step, v[4 * j + 2], decay * x.z);
+            x.w = fmaf(-it.step, v[4 * j + 3], decay * x.w);
+            *reinterpret_cast<float4 *>(p + 4 * j) = x;
         }
-        if (last) {
-            if (a.theta) {
+    } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(place + r * 128 + ((j ^ (r & 7)) << 4)),
-                                 "f"(v[4 * j] * (1.0f / kScaleX)), "f"(v[4 * j + 1] * (1.0f / kScaleX)), "f"(v[4 * j + 2] * (1.0f / kScaleX)),
-                                 "f"(v[4 * j + 3] * (1.0f / kScaleX)) : "memory");
-                half_sync(side);
-                write_out<true>(a, it, place, r, row0, col + 32 * part);
-                half_sync(side);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) hi[16 * part + i] = bf16_pair(v[2 * i] * (1.0f / kScaleX), v[2 * i + 1] * (1.0f / kScaleX));
-            }
+        for (int j = 0; j < 32; ++j)
+            if (col + j < it.cols) p[j] = fmaf(-it.step, v[j], decay * p[j]);
+    }
+}
+
+// A half's columns of a tile: `parts` times 32 of a thread's row, from column `col` on.  What the tile
+// needs beside its products is on its way before they are awaited, and a part's while the one before
+// is worked on.
+struct Taking {
+    const ProductArgs &a;
+    const Item &it;
+    const Tile &tile;
+    int row0, r, col, parts;        // the CTA's first row, this thread's among its 128
+    float *columns;
+    uint32_t x[16], low[16];        // the next part's
+
+    __device__ __forceinline__ __half *at(int base, int pitch, int part, int64_t row) const
+    {
+        const int c = col + 32 * part;
+        return a.w.panels + ((static_cast<int64_t>(base) + static_cast<int64_t>(c / kPanel) * pitch + row) * kPanel + c % kPanel);
+    }
+    // Panels are stored to their ends, which are summed over as zeros; blocks of A and B below the
+    // diagonal are not stored from here.  (The same for all of a half.)
+    __device__ __forceinline__ bool here(int part) const
+    {
+        const int c = col + 32 * part, panel = c / kPanel * kPanel;
+        return part < parts && (tile.what == 2 ? panel < it.cols : panel < it.side && c / kBlock >= row0 / kBlock);
+    }
+    __device__ __forceinline__ void fetch(int part)
+    {
+        if (!here(part) || tile.what == 0) return;
+        if (tile.what == 1) {
+            get_part(at(it.gram, it.s_pitch, part, row0 + r), x);
         } else {
+            get_part(at(it.x[tile.step & 1], it.x_pitch, part, row0 + r), x);
+            get_part(at(it.low, it.x_pitch, part, row0 + r), low);
+        }
+    }
+    __device__ __forceinline__ void take(uint32_t src)
+    {
+        const int row = row0 + r;
+        float *da = a.w.diags + it.diag, *db = da + it.s_pitch;
+        const float ca = a.coefficients[tile.step][0], cb = a.coefficients[tile.step][1], cc = a.coefficients[tile.step][2];
+        const bool last = tile.step + 1 == a.steps, full = tile.step + 2 >= a.steps;
+        float d_row = 0.0f;
+        if (tile.what == 1) d_row = __ldcg(da + row);
+        if (tile.what == 2 && !it.tall) d_row = __ldcg(db + row);
+#pragma unroll 1
+        for (int part = 0; part < parts; ++part) {
+            if (!here(part)) {
+                fetch(part + 1);
+                continue;
+            }
+            uint32_t raw[32], h[16], own[16], own_low[16];
+            tmem_load32(src + 32 * part, raw);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                hi[16 * part + i] = pack_half(v[2 * i], v[2 * i + 1]);
-                const float2 p = unpack_half(hi[16 * part + i]);
-                lo[16 * part + i] = pack_half((v[2 * i] - p.x) * kScaleLow, (v[2 * i + 1] - p.y) * kScaleLow);
+                own[i] = x[i];
+                own_low[i] = low[i];
             }
+            fetch(part + 1);
+            const float *d_cols = columns + 32 * part;
+            const int c0 = col + 32 * part;
+            float v[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(raw[i]);
+            if (tile.what < 2) {
+                const int on = row - c0;                        // this row's diagonal element is here if in [0, 32)
+                if (tile.what == 0) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        if (i == on) {
+                            da[row] = v[i] * (1.0f / (kScaleX * kScaleX));
+                            v[i] = 0.0f;
+                        }
+                        v[i] *= kScaleA / (kScaleX * kScaleX);
+                    }
+                } else {
+                    constexpr float kSquare = 1.0f / (kScaleA * kScaleA);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const float2 pair = unpack_half(own[i / 2]);
+                        const float off = (i & 1 ? pair.y : pair.x) * (1.0f / kScaleA), d = d_row + d_cols[i];
+                        if (i == on) {
+                            db[row] = fmaf(cc, fmaf(v[i], kSquare, d_row * d_row), cb * d_row);
+                            v[i] = 0.0f;
+                        } else {
+                            v[i] = kScaleB * fmaf(cc, fmaf(v[i], kSquare, d * off), cb * off);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) h[i] = pack_half(v[2 * i], v[2 * i + 1]);
+                const int base = tile.what == 0 ? it.gram : it.poly;
+                put_part(at(base, it.s_pitch, part, row), h);
+                // above the diagonal: the transposed block too
+                if (c0 / kBlock > row0 / kBlock)
+                    put_across(a.w.panels + (static_cast<int64_t>(base) + static_cast<int64_t>(row / kPanel) * it.s_pitch + c0) * kPanel + (row % kPanel & ~1), h);
+                continue;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float2 p = unpack_half(own[i]), q = unpack_half(own_low[i]);
+                const float x0 = fmaf(q.x, 1.0f / kScaleLow, p.x), x1 = fmaf(q.y, 1.0f / kScaleLow, p.y);
+                const float d0 = it.tall ? d_cols[2 * i] : d_row, d1 = it.tall ? d_cols[2 * i + 1] : d_row;
+                v[2 * i] = fmaf(v[2 * i], 1.0f / kScaleB, fmaf(d0, full ? x0 : p.x, ca * x0));
+                v[2 * i + 1] = fmaf(v[2 * i + 1], 1.0f / kScaleB, fmaf(d1, full ? x1 : p.y, ca * x1));
+            }
+            if (last) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] *= 1.0f / kScaleX;
+                if (row < it.rows) {
+                    if (a.theta) step_theta(it, a.decay, row, c0, v);
+                    else write_out(it, row, c0, v);
+                }
+                __syncwarp();
+                continue;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                h[i] = pack_half(v[2 * i], v[2 * i + 1]);
+                const float2 p = unpack_half(h[i]);
+                own_low[i] = pack_half((v[2 * i] - p.x) * kScaleLow, (v[2 * i + 1] - p.y) * kScaleLow);
+            }
+            put_part(at(it.x[1 - (tile.step & 1)], it.x_pitch, part, row), h);
+            put_part(at(it.low, it.x_pitch, part, row), own_low);
         }
     }
-    if (!last) {
-        const int y = panel * it.x_pitch + row0;
-        put_row(place, r, hi);
-        send(map, place, side, issuer, it.x[1 - turn] + y, it.x[1 - turn] + y + 64);
-        reclaim(side, issuer);
-        put_row(place, r, lo);
-        send(map, place, side, issuer, it.low + y, it.low + y + 64);
-    } else if (!a.theta) {
-        put_row(place, r, hi);
-        half_sync(side);
-        write_out<false>(a, it, place, r, row0, col);
-    }
-}
+};
 
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
 novak_orthogonalize_products_kernel(const __grid_constant__ ProductArgs a, const __grid_constant__ CUtensorMap map)
 {
     extern __shared__ uint8_t raw[];
-    const uint32_t stages = (smem_addr(raw) + 1023) & ~1023u, places = stages + kStages * kStageBytes;
-    Shared &sh = *reinterpret_cast<Shared *>(raw + (places - smem_addr(raw)) + 2 * kSideBytes);
+    const uint32_t stages = (smem_addr(raw) + 1023) & ~1023u;
+    Shared &sh = *reinterpret_cast<Shared *>(raw + (stages - smem_addr(raw)) + kStages * kStageBytes);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = cluster_rank();
 
@@ -760,43 +759,42 @@ novak_orthogonalize_products_kernel(const __grid_constant__ ProductArgs a, const
     Tile tile;
     if (warp < kOutWarps) {
         const int side = warp / 4, r = threadIdx.x % 128;
-        const uint32_t place = places + side * kSideBytes, row_of = static_cast<uint32_t>(warp % 4) * 32 << 16;
-        float *columns = sh.columns[side];
+        const uint32_t row_of = static_cast<uint32_t>(warp % 4) * 32 << 16;
         uint32_t count = 0;
         for (;;) {
             const uint32_t buf = count & 1;
-            bool more = next(tile);
-            if (more && !mbar_wait_warp(smem_addr(&sh.out_full[buf]), (count >> 1) & 1, a.wait_ns)) {
-                if (lane == 0) gave_up(a);
-                ok = false;
+            const bool more = next(tile);
+            const Item &it = a.w.items[more ? tile.which : 0];
+            const int row0 = tile.row + static_cast<int>(rank) * kBlock, half = tile.columns / 2;
+            const int height = tile.what == 2 ? it.x_pitch : it.s_pitch;
+            Taking taking{a, it, tile, row0, r, tile.col + side * half, row0 < height ? half / 32 : 0, sh.columns[side], {}, {}};
+            if (more) {
+                if (lane == 0) ok = wait_parts(a, a.w.done + tile.which, tile.need);
+                ok = __shfl_sync(0xffffffffu, ok, 0);
+                if (ok) {
+                    const float *d = a.w.diags + it.diag;
+                    const int width = tile.what == 1 ? it.s_pitch : tile.what == 2 && it.tall ? it.s_pitch : 0, c = taking.col + r;
+                    if (r < half && c < width) taking.columns[r] = __ldcg(d + (tile.what == 1 ? 0 : it.s_pitch) + c);
+                    taking.fetch(0);
+                    ok = mbar_wait_warp(smem_addr(&sh.out_full[buf]), (count >> 1) & 1, a.wait_ns);
+                }
+                if (!ok && lane == 0) gave_up(a);
             }
             // (where one's wait gave up the others do not go on to barriers that it will not come to)
             ok = half_agree(side, ok);
             if (!ok || !more) break;
             tcgen05_after_sync();
-            const Item &it = a.w.items[tile.which];
-            const int row0 = tile.row + static_cast<int>(rank) * kBlock, half = tile.columns / 2;
-            const int height = tile.what == 2 ? it.x_pitch : it.s_pitch, width = tile.what == 2 ? it.cols : it.side;
-            if (row0 < height)
-                for (int c = 0; c < half; c += kPanel)
-                    if (tile.col + side * half + c < width)
-                        take_panel(a, &map, it, tile, tmem + buf * 256 + side * half + c + row_of, place, side, r, row0,
-                                   tile.col + side * half + c, columns);
+            taking.take(tmem + buf * 256 + side * half + row_of);
             tcgen05_before_sync();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(at_rank(smem_addr(&sh.out_empty[buf]), 0));
             ++count;
-            // everything of this half is in memory before that is told
+            // everything of this half is in memory, for tensor copies too, before that is told
             __threadfence();
+            asm volatile("fence.proxy.async;" ::: "memory");
             half_sync(side);
-            if (r == 0 && tile.announced) {
-                stores_done();
-                asm volatile("fence.proxy.async;" ::: "memory");
-                __threadfence();
-                asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(a.w.done + tile.which), "r"(1u) : "memory");
-            }
+            if (r == 0 && tile.announced) asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(a.w.done + tile.which), "r"(1u) : "memory");
         }
-        if (r == 0) stores_done();
     } else if (warp == kLoadWarp) {
         Ring<kStages> at;
         int64_t issued = 0;
@@ -976,8 +974,7 @@ cudaError_t launch_orthogonalize(const OrthArgs &a, cudaStream_t stream)
     finish_layout(l, n);
     uint8_t *base = static_cast<uint8_t *>(a.work);
     const Work w{reinterpret_cast<__half *>(base), reinterpret_cast<float *>(base + l.diags), reinterpret_cast<Item *>(base + l.items),
-                 reinterpret_cast<double *>(base + l.partial), reinterpret_cast<float2 *>(base + l.scale),
-                 reinterpret_cast<unsigned *>(base + l.arrived), reinterpret_cast<unsigned *>(base + l.done)};
+                 reinterpret_cast<double *>(base + l.partial), reinterpret_cast<unsigned *>(base + l.done)};
     ProductArgs p{};
     p.w = w;
     p.control = reinterpret_cast<Control *>(base + l.control);
@@ -991,11 +988,15 @@ cudaError_t launch_orthogonalize(const OrthArgs &a, cudaStream_t stream)
         p.first[what + 1] = p.first[what] + static_cast<int>(tiles[what][narrow]);
         most = std::max(most, tiles[what][narrow]);
     }
+    const Momentum mo{a.m != nullptr, a.nesterov, a.momentum};
+    const bool f32 = a.type == NOVAK_TYPE_F32;
     Layout again;
-    HostItems items;
+    HostItems items{};
     int first = 0, count = 0;
     const auto send = [&] {
-        const cudaError_t e = launch(novak_orthogonalize_items_kernel, dim3(1), kThreads, 0, stream, items, first, count, w, p.control);
+        const int64_t chunks = again.chunks - items.item[0].chunk;
+        const cudaError_t e = launch(f32 ? novak_orthogonalize_norm_kernel<0> : novak_orthogonalize_norm_kernel<1>, dim3(static_cast<unsigned>(chunks)),
+                                     kThreads, 0, stream, items, first, count, w, p.control, mo);
         first += count;
         count = 0;
         return e;
@@ -1019,14 +1020,9 @@ cudaError_t launch_orthogonalize(const OrthArgs &a, cudaStream_t stream)
         if (count == HostItems::kMost) e = send();
     }
     if (e == cudaSuccess && count > 0) e = send();
-    if (e != cudaSuccess) return e;
-    const Momentum mo{a.m != nullptr, a.nesterov, a.momentum};
-    const dim3 units(static_cast<unsigned>(l.units));
-    const bool f32 = a.type == NOVAK_TYPE_F32;
-    e = launch(f32 ? novak_orthogonalize_norm_kernel<0> : novak_orthogonalize_norm_kernel<1>, units, kThreads, 0, stream, w, n, mo,
-               static_cast<float>(a.eps));
     if (e == cudaSuccess)
-        e = launch(f32 ? novak_orthogonalize_start_kernel<0> : novak_orthogonalize_start_kernel<1>, units, kThreads, 0, stream, w, n, mo);
+        e = launch(f32 ? novak_orthogonalize_start_kernel<0> : novak_orthogonalize_start_kernel<1>, dim3(static_cast<unsigned>(l.units)), kThreads, 0,
+                   stream, w, n, mo, static_cast<float>(a.eps));
     if (e != cudaSuccess) return e;
 
     for (int k = 0; k < a.steps; ++k)

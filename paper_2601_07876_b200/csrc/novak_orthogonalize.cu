@@ -297,10 +297,12 @@ __global__ void __launch_bounds__(kThreads) novak_orthogonalize_start_kernel(Wor
 // or the summed dimension (X^T X, the X of B X) with the operand's other one contiguous.
 //
 // In each CTA: warps 0-7 take tiles out (a warp a quarter of the lanes, warps 0-3 the left half of
-// the columns), warp 8 brings operands, warp 9 issues the products (of the pair: in the
+// the columns, each on its own), warp 8 brings operands, warp 9 issues the products (of the pair: in the
 // leading CTA), warp 10 of the leading CTA hands tiles out.
-constexpr int kPairs = 74, kStages = 7, kRing = 2;
+constexpr int kPairs = 74, kStages = 5, kRing = 2;
 constexpr int kBoxBytes = kPanel * 128, kStageBytes = 4 * kBoxBytes;
+constexpr int kPartBytes = 32 * 64, kPlaceBytes = 2 * kPartBytes;       // 32 x 32 elements in fp16; two of those
+constexpr int kTold = 16;       // parts of a tile that are told of when they are stored: each warp's that takes it out
 constexpr int kOutWarps = 8, kLoadWarp = 8, kMmaWarp = 9, kTileWarp = 10, kTcThreads = 384;
 
 // What is to be done for a tile, as the leading CTA's warp 10 writes it into both CTAs.
@@ -321,11 +323,12 @@ static_assert(kTileWords <= 32, "a lane each");
 
 struct Shared {
     alignas(8) uint64_t full[kStages], empty[kStages], out_full[2], out_empty[2], tile_full[kRing], tile_empty[kRing], want, drained;
+    uint64_t part_full[kOutWarps][2];
     uint32_t tmem;
     Tile tiles[kRing];
-    alignas(16) float columns[2][128];      // a half's columns of a diagonal
+    alignas(16) float columns[kOutWarps][32];       // of a diagonal, for the part that is worked on
 };
-constexpr int kSmemBytes = kStages * kStageBytes + 1024 + static_cast<int>(sizeof(Shared));
+constexpr int kSmemBytes = kStages * kStageBytes + 2 * kOutWarps * kPlaceBytes + 1024 + static_cast<int>(sizeof(Shared));
 static_assert(kSmemBytes <= 227 * 1024, "shared memory");
 
 struct ProductArgs {
@@ -405,19 +408,17 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap *map, i
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];"
                  ::"r"(dst), "l"(map), "r"(0), "r"(y), "r"(bar) : "memory");
 }
-// The four warps of one half of the columns; whether all of them agree.
-__device__ __forceinline__ void half_sync(int side)
+// 32 rows of 32 columns of a panel, in shared memory as 32 rows of 64 bytes whose 16-byte pieces change places by the
+// row's number; loads are told to a barrier of this CTA.
+__device__ __forceinline__ void load_part(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) { tma_load_2d(dst, map, x, y, bar); }
+__device__ __forceinline__ void store_part(const CUtensorMap *map, int x, int y, uint32_t src)
 {
-    asm volatile("bar.sync %0, 128;" ::"r"(1 + side) : "memory");
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
+                 ::"l"(map), "r"(x), "r"(y), "r"(src) : "memory");
 }
-__device__ __forceinline__ bool half_agree(int side, bool yes)
-{
-    uint32_t all;
-    asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %1, 0;\n"
-                 "barrier.cta.red.and.aligned.pred q, %2, 128, p;\n"
-                 "selp.u32 %0, 1, 0, q;\n}" : "=r"(all) : "r"(static_cast<uint32_t>(yes)), "r"(1 + side) : "memory");
-    return all != 0;
-}
+__device__ __forceinline__ void stores_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 // fp16 x fp16 -> fp32; `a_across`, `b_across`: the operand's own dimension is the contiguous one.
 __device__ constexpr uint32_t fp16_descriptor(int columns, bool a_across, bool b_across)
@@ -506,190 +507,251 @@ __device__ __forceinline__ Tile tile_at(const ProductArgs &a, int64_t t)
     r.descriptor = fp16_descriptor(n, a_across, b_across);
     const unsigned s = it.tiles[0], x = it.tiles[2];        // (as many of B as of A unless their tiles differ)
     const unsigned before = r.what == 0 ? 0 : r.what == 1 ? s : s + it.tiles[1];
-    r.need = 4u * (static_cast<unsigned>(r.step) * (s + it.tiles[1] + x) + before);
+    r.need = static_cast<unsigned>(kTold) * (static_cast<unsigned>(r.step) * (s + it.tiles[1] + x) + before);
     r.announced = t != a.withheld;
     return r;
 }
 
 // ---- taking a tile out
-// A thread has a row (a lane of tensor memory) and 32 columns at a time, 64 bytes of a panel's
-// row, which go straight to memory and come from there by 32 bytes: whole sectors of L2, which
-// a way through shared memory would not make better (with tensor copies out of shared memory, which the
-// next part waited for, a tile took longer than 768 products of it).
-// 32 columns of a panel's row (other SMs wrote it: not from the first-level cache).
-__device__ __forceinline__ void get_part(const __half *p, uint32_t (&h)[16])
+// A warp has 32 rows (a thread a lane of tensor memory) and 32 columns at a time.  What it needs of
+// X or A comes into shared memory by tensor copies, the results take its place and go from there by
+// tensor copies: rows straight from and to memory are 32 lines at a time, of each of which the
+// first-level cache moves a sector (15000 cycles a tile of X).  Two places by turns: the next part
+// is on its way while one is worked on.
+__device__ __forceinline__ uint32_t piece_at(uint32_t place, int row, int piece) { return place + row * 64 + ((piece ^ (row >> 1 & 3)) << 4); }
+__device__ __forceinline__ void get_row(uint32_t place, int row, uint32_t (&h)[16])
 {
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-        asm volatile("ld.relaxed.gpu.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                     : "=r"(h[8 * j]), "=r"(h[8 * j + 1]), "=r"(h[8 * j + 2]), "=r"(h[8 * j + 3]), "=r"(h[8 * j + 4]), "=r"(h[8 * j + 5]),
-                       "=r"(h[8 * j + 6]), "=r"(h[8 * j + 7]) : "l"(p + 16 * j) : "memory");
+    for (int j = 0; j < 4; ++j)
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(h[4 * j]), "=r"(h[4 * j + 1]), "=r"(h[4 * j + 2]), "=r"(h[4 * j + 3])
+                     : "r"(piece_at(place, row, j)) : "memory");
 }
-__device__ __forceinline__ void put_part(__half *p, const uint32_t (&h)[16])
+__device__ __forceinline__ void put_row(uint32_t place, int row, const uint32_t (&h)[16])
 {
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p + 16 * j), "r"(h[8 * j]), "r"(h[8 * j + 1]), "r"(h[8 * j + 2]),
-                     "r"(h[8 * j + 3]), "r"(h[8 * j + 4]), "r"(h[8 * j + 5]), "r"(h[8 * j + 6]), "r"(h[8 * j + 7]) : "memory");
+    for (int j = 0; j < 4; ++j)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(piece_at(place, row, j)), "r"(h[4 * j]), "r"(h[4 * j + 1]), "r"(h[4 * j + 2]),
+                     "r"(h[4 * j + 3]) : "memory");
 }
-// The same transposed: 32 rows of a warp's 32 lanes.  `p`: the first of them, at the lane's column but
-// for its lowest bit; neighbouring lanes exchange halves, so that each has two columns of every other row.
-__device__ __forceinline__ void put_across(__half *p, const uint32_t (&h)[16])
+// The same transposed.  Neighbouring lanes exchange halves, so that each has two columns of every other row.
+__device__ __forceinline__ void put_across(uint32_t place, const uint32_t (&h)[16])
 {
-    const bool odd = threadIdx.x & 1;
+    const int lane = threadIdx.x & 31, odd = lane & 1;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         const uint32_t other = __shfl_xor_sync(0xffffffffu, h[i], 1);
         const uint32_t w = odd ? __byte_perm(other, h[i], 0x7632) : __byte_perm(h[i], other, 0x5410);
-        *reinterpret_cast<uint32_t *>(p + (2 * i + odd) * kPanel) = w;
+        const int row = 2 * i + odd;
+        asm volatile("st.shared.b32 [%0], %1;" ::"r"(piece_at(place, row, lane >> 3) + (lane & 6) * 2), "r"(w) : "memory");
     }
 }
 
-// 32 columns of X (bf16: two to a word), or of theta's step, to a caller's row.
-__device__ __forceinline__ void write_out(const Item &it, int64_t row, int col, const float (&v)[32])
+// The warp's 32 x 32 elements of X to the caller's rows, by way of shared memory, so that rows go out together.
+__device__ __forceinline__ void write_out(const Item &it, uint32_t place, int row0, int col, const float (&v)[32])
 {
-    uint16_t *p = static_cast<uint16_t *>(it.out) + row * it.out_stride + col;
-    if ((reinterpret_cast<uintptr_t>(p) & 15u) == 0 && col + 32 <= it.cols) {
+    const int lane = threadIdx.x & 31;
+    uint32_t h[16];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            *reinterpret_cast<uint4 *>(p + 8 * j) = make_uint4(bf16_pair(v[8 * j], v[8 * j + 1]), bf16_pair(v[8 * j + 2], v[8 * j + 3]),
-                                                               bf16_pair(v[8 * j + 4], v[8 * j + 5]), bf16_pair(v[8 * j + 6], v[8 * j + 7]));
-    } else {
+    for (int i = 0; i < 16; ++i) h[i] = bf16_pair(v[2 * i], v[2 * i + 1]);
+    put_row(place, lane, h);
+    __syncwarp();
+    uint16_t *out = static_cast<uint16_t *>(it.out) + row0 * it.out_stride + col;
+    if ((reinterpret_cast<uintptr_t>(out) & 15u) == 0 && it.out_stride % 8 == 0 && col + 32 <= it.cols) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-            if (col + j < it.cols) reinterpret_cast<__nv_bfloat16 *>(p)[j] = __float2bfloat16_rn(v[j]);
-    }
-}
-__device__ __forceinline__ void step_theta(const Item &it, float decay, int64_t row, int col, const float (&v)[32])
-{
-    float *p = static_cast<float *>(it.out) + row * it.out_stride + col;
-    if ((reinterpret_cast<uintptr_t>(p) & 15u) == 0 && col + 32 <= it.cols) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float4 x = *reinterpret_cast<const float4 *>(p + 4 * j);
-            x.x = fmaf(-it.step, v[4 * j], decay * x.x);
-            x.y = fmaf(-it.step, v[4 * j + 1], decay * x.y);
-            x.z = fmaf(-it.step, v[4 * j + 2], decay * x.z);
-            x.w = fmaf(-it.step, v[4 * j + 3], decay * x.w);
-            *reinterpret_cast<float4 *>(p + 4 * j) = x;
+        for (int i = 0; i < 4; ++i) {
+            const int row = i * 8 + lane / 4, piece = lane % 4;
+            uint4 x;
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(piece_at(place, row, piece)) : "memory");
+            if (row0 + row < it.rows) *reinterpret_cast<uint4 *>(out + row * it.out_stride + piece * 8) = x;
         }
     } else {
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-            if (col + j < it.cols) p[j] = fmaf(-it.step, v[j], decay * p[j]);
+#pragma unroll 4
+        for (int row = 0; row < 32; ++row) {
+            uint16_t x;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(piece_at(place, row, lane / 8) + lane % 8 * 2) : "memory");
+            if (row0 + row < it.rows && col + lane < it.cols) out[row * it.out_stride + lane] = x;
+        }
     }
+    __syncwarp();
+}
+// The same for theta's step: fp32, rows of 128 bytes in both of a place's parts.
+__device__ __forceinline__ void step_theta(const Item &it, float decay, uint32_t place, int row0, int col, const float (&v)[32])
+{
+    const int lane = threadIdx.x & 31;
+    const auto at = [&](int row, int piece) { return place + row * 128 + ((piece ^ (row & 7)) << 4); };
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at(lane, j)), "f"(v[4 * j]), "f"(v[4 * j + 1]), "f"(v[4 * j + 2]), "f"(v[4 * j + 3]) : "memory");
+    __syncwarp();
+    float *out = static_cast<float *>(it.out) + row0 * it.out_stride + col;
+    if ((reinterpret_cast<uintptr_t>(out) & 15u) == 0 && it.out_stride % 4 == 0 && col + 32 <= it.cols) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int row = i * 4 + lane / 8, piece = lane % 8;
+            float4 x;
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(at(row, piece)) : "memory");
+            if (row0 + row >= it.rows) continue;
+            float4 *p = reinterpret_cast<float4 *>(out + row * it.out_stride + piece * 4);
+            const float4 t = *p;
+            *p = make_float4(fmaf(-it.step, x.x, decay * t.x), fmaf(-it.step, x.y, decay * t.y), fmaf(-it.step, x.z, decay * t.z), fmaf(-it.step, x.w, decay * t.w));
+        }
+    } else {
+#pragma unroll 4
+        for (int row = 0; row < 32; ++row) {
+            float x;
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(at(row, lane / 4) + lane % 4 * 4) : "memory");
+            if (row0 + row >= it.rows || col + lane >= it.cols) continue;
+            float *p = out + row * it.out_stride + lane;
+            *p = fmaf(-it.step, x, decay * *p);
+        }
+    }
+    __syncwarp();
 }
 
-// A half's columns of a tile: `parts` times 32 of a thread's row, from column `col` on.  What the tile
-// needs beside its products is on its way before they are awaited, and a part's while the one before
-// is worked on.
+// A warp that takes tiles out: its places in shared memory, their barriers and uses.
 struct Taking {
     const ProductArgs &a;
-    const Item &it;
-    const Tile &tile;
-    int row0, r, col, parts;        // the CTA's first row, this thread's among its 128
+    const CUtensorMap *map;
+    uint32_t places, bars;          // two places of two parts; two barriers
     float *columns;
-    uint32_t x[16], low[16];        // the next part's
+    float next_column;              // this lane's, for the next part
+    uint32_t phases;                // of the barriers, a bit each
+    // of a tile:
+    int row0, col, parts;           // the warp's first row and column; times 32 columns
 
-    __device__ __forceinline__ __half *at(int base, int pitch, int part, int64_t row) const
-    {
-        const int c = col + 32 * part;
-        return a.w.panels + ((static_cast<int64_t>(base) + static_cast<int64_t>(c / kPanel) * pitch + row) * kPanel + c % kPanel);
-    }
     // Panels are stored to their ends, which are summed over as zeros; blocks of A and B below the
-    // diagonal are not stored from here.  (The same for all of a half.)
-    __device__ __forceinline__ bool here(int part) const
+    // diagonal are not stored from here.  (The same for all of a warp.)
+    __device__ __forceinline__ bool here(const Item &it, const Tile &tile, int part) const
     {
         const int c = col + 32 * part, panel = c / kPanel * kPanel;
         return part < parts && (tile.what == 2 ? panel < it.cols : panel < it.side && c / kBlock >= row0 / kBlock);
     }
-    __device__ __forceinline__ void fetch(int part)
+    // What a part needs on its way into place part % 2, once what was there is out.
+    __device__ __forceinline__ void fetch(const Item &it, const Tile &tile, int part)
     {
-        if (!here(part) || tile.what == 0) return;
-        if (tile.what == 1) {
-            get_part(at(it.gram, it.s_pitch, part, row0 + r), x);
-        } else {
-            get_part(at(it.x[tile.step & 1], it.x_pitch, part, row0 + r), x);
-            get_part(at(it.low, it.x_pitch, part, row0 + r), low);
+        if (!here(it, tile, part)) return;
+        const int lane = threadIdx.x & 31, set = part & 1, c = col + 32 * part;
+        if (tile.what == 1 || (tile.what == 2 && it.tall)) next_column = __ldcg(a.w.diags + it.diag + (tile.what == 1 ? 0 : it.s_pitch) + c + lane);
+        if (lane == 0) {
+            stores_read();
+            if (tile.what > 0) {
+                const uint32_t place = places + set * kPlaceBytes, bar = bars + set * 8;
+                const int turn = tile.step & 1, pitch = tile.what == 1 ? it.s_pitch : it.x_pitch, y = c / kPanel * pitch + row0;
+                mbar_expect(bar, tile.what == 1 ? kPartBytes : 2 * kPartBytes);
+                load_part(place, map, c % kPanel, (tile.what == 1 ? it.gram : it.x[turn]) + y, bar);
+                if (tile.what == 2) load_part(place + kPartBytes, map, c % kPanel, it.low + y, bar);
+            }
         }
+        __syncwarp();
     }
-    __device__ __forceinline__ void take(uint32_t src)
+    // false: a wait gave up.
+    __device__ __forceinline__ bool take(const Item &it, const Tile &tile, uint32_t src)
     {
-        const int row = row0 + r;
+        const int lane = threadIdx.x & 31, row = row0 + lane;
         float *da = a.w.diags + it.diag, *db = da + it.s_pitch;
         const float ca = a.coefficients[tile.step][0], cb = a.coefficients[tile.step][1], cc = a.coefficients[tile.step][2];
         const bool last = tile.step + 1 == a.steps, full = tile.step + 2 >= a.steps;
         float d_row = 0.0f;
-        if (tile.what == 1) d_row = __ldcg(da + row);
-        if (tile.what == 2 && !it.tall) d_row = __ldcg(db + row);
+        if (parts > 0 && tile.what == 1) d_row = __ldcg(da + row);
+        if (parts > 0 && tile.what == 2 && !it.tall) d_row = __ldcg(db + row);
 #pragma unroll 1
         for (int part = 0; part < parts; ++part) {
-            if (!here(part)) {
-                fetch(part + 1);
-                continue;
+            columns[lane] = next_column;
+            __syncwarp();
+            fetch(it, tile, part + 1);
+            if (!here(it, tile, part)) continue;
+            const int set = part & 1, c0 = col + 32 * part;
+            const uint32_t place = places + set * kPlaceBytes;
+            uint32_t raw[32], h[16];
+            if (tile.what > 0) {
+                if (!mbar_wait_warp(bars + set * 8, phases >> set & 1, a.wait_ns)) return false;
+                phases ^= 1u << set;
             }
-            uint32_t raw[32], h[16], own[16], own_low[16];
             tmem_load32(src + 32 * part, raw);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                own[i] = x[i];
-                own_low[i] = low[i];
-            }
-            fetch(part + 1);
-            const float *d_cols = columns + 32 * part;
-            const int c0 = col + 32 * part;
             float v[32];
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(raw[i]);
+            const float4 *d_cols = reinterpret_cast<const float4 *>(columns);
             if (tile.what < 2) {
                 const int on = row - c0;                        // this row's diagonal element is here if in [0, 32)
                 if (tile.what == 0) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        if (i == on) {
-                            da[row] = v[i] * (1.0f / (kScaleX * kScaleX));
-                            v[i] = 0.0f;
-                        }
-                        v[i] *= kScaleA / (kScaleX * kScaleX);
+                    for (int i = 0; i < 32; ++i) v[i] *= kScaleA / (kScaleX * kScaleX);
+                    if (c0 == row0) {                           // (the warp's block is on the diagonal as a whole, or off)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (i == on) {
+                                da[row] = v[i] * (1.0f / kScaleA);
+                                v[i] = 0.0f;
+                            }
                     }
                 } else {
                     constexpr float kSquare = 1.0f / (kScaleA * kScaleA);
+                    get_row(place, lane, h);
+                    float mine = 0.0f;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        const float2 pair = unpack_half(own[i / 2]);
-                        const float off = (i & 1 ? pair.y : pair.x) * (1.0f / kScaleA), d = d_row + d_cols[i];
-                        if (i == on) {
-                            db[row] = fmaf(cc, fmaf(v[i], kSquare, d_row * d_row), cb * d_row);
-                            v[i] = 0.0f;
-                        } else {
-                            v[i] = kScaleB * fmaf(cc, fmaf(v[i], kSquare, d * off), cb * off);
+                    for (int i = 0; i < 32; i += 4) {
+                        const float4 d4 = d_cols[i / 4];
+                        const float d[4] = {d4.x, d4.y, d4.z, d4.w};
+                        const float2 lo = unpack_half(h[i / 2]), hi = unpack_half(h[i / 2 + 1]);
+                        const float off[4] = {lo.x, lo.y, hi.x, hi.y};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            if (i + k == on) mine = v[i + k];
+                            const float o = off[k] * (1.0f / kScaleA);
+                            v[i + k] = kScaleB * fmaf(cc, fmaf(v[i + k], kSquare, (d_row + d[k]) * o), cb * o);
                         }
+                    }
+                    if (c0 == row0) {
+                        db[row] = fmaf(cc, fmaf(mine, kSquare, d_row * d_row), cb * d_row);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (i == on) v[i] = 0.0f;
                     }
                 }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) h[i] = pack_half(v[2 * i], v[2 * i + 1]);
-                const int base = tile.what == 0 ? it.gram : it.poly;
-                put_part(at(base, it.s_pitch, part, row), h);
-                // above the diagonal: the transposed block too
-                if (c0 / kBlock > row0 / kBlock)
-                    put_across(a.w.panels + (static_cast<int64_t>(base) + static_cast<int64_t>(row / kPanel) * it.s_pitch + c0) * kPanel + (row % kPanel & ~1), h);
+                // above the diagonal's blocks: the transposed part too
+                const bool mirror = c0 / kBlock > row0 / kBlock;
+                put_row(place, lane, h);
+                if (mirror) put_across(place + kPartBytes, h);
+                fence_async_shared();
+                __syncwarp();
+                if (lane == 0) {
+                    const int base = tile.what == 0 ? it.gram : it.poly;
+                    store_part(map, c0 % kPanel, base + c0 / kPanel * it.s_pitch + row0, place);
+                    if (mirror) store_part(map, row0 % kPanel, base + row0 / kPanel * it.s_pitch + c0, place + kPartBytes);
+                    stores_commit();
+                }
+                __syncwarp();
                 continue;
             }
+            uint32_t low[16];
+            get_row(place, lane, h);
+            get_row(place + kPartBytes, lane, low);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float2 p = unpack_half(own[i]), q = unpack_half(own_low[i]);
-                const float x0 = fmaf(q.x, 1.0f / kScaleLow, p.x), x1 = fmaf(q.y, 1.0f / kScaleLow, p.y);
-                const float d0 = it.tall ? d_cols[2 * i] : d_row, d1 = it.tall ? d_cols[2 * i + 1] : d_row;
-                v[2 * i] = fmaf(v[2 * i], 1.0f / kScaleB, fmaf(d0, full ? x0 : p.x, ca * x0));
-                v[2 * i + 1] = fmaf(v[2 * i + 1], 1.0f / kScaleB, fmaf(d1, full ? x1 : p.y, ca * x1));
+            for (int i = 0; i < 32; i += 4) {
+                float d[4] = {d_row, d_row, d_row, d_row};
+                if (it.tall) {
+                    const float4 d4 = d_cols[i / 4];
+                    d[0] = d4.x; d[1] = d4.y; d[2] = d4.z; d[3] = d4.w;
+                }
+                const float2 p0 = unpack_half(h[i / 2]), p1 = unpack_half(h[i / 2 + 1]), q0 = unpack_half(low[i / 2]), q1 = unpack_half(low[i / 2 + 1]);
+                const float p[4] = {p0.x, p0.y, p1.x, p1.y}, q[4] = {q0.x, q0.y, q1.x, q1.y};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float x = fmaf(q[k], 1.0f / kScaleLow, p[k]);
+                    v[i + k] = fmaf(v[i + k], 1.0f / kScaleB, fmaf(d[k], full ? x : p[k], ca * x));
+                }
             }
             if (last) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[i] *= 1.0f / kScaleX;
-                if (row < it.rows) {
-                    if (a.theta) step_theta(it, a.decay, row, c0, v);
-                    else write_out(it, row, c0, v);
-                }
+                __syncwarp();
+                if (a.theta) step_theta(it, a.decay, place, row0, c0, v);
+                else write_out(it, place, row0, c0, v);
+                // (the next load into this place comes behind what was read there)
+                fence_async_shared();
                 __syncwarp();
                 continue;
             }
@@ -697,20 +759,31 @@ struct Taking {
             for (int i = 0; i < 16; ++i) {
                 h[i] = pack_half(v[2 * i], v[2 * i + 1]);
                 const float2 p = unpack_half(h[i]);
-                own_low[i] = pack_half((v[2 * i] - p.x) * kScaleLow, (v[2 * i + 1] - p.y) * kScaleLow);
+                low[i] = pack_half((v[2 * i] - p.x) * kScaleLow, (v[2 * i + 1] - p.y) * kScaleLow);
             }
-            put_part(at(it.x[1 - (tile.step & 1)], it.x_pitch, part, row), h);
-            put_part(at(it.low, it.x_pitch, part, row), own_low);
+            put_row(place, lane, h);
+            put_row(place + kPartBytes, lane, low);
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) {
+                const int y = c0 / kPanel * it.x_pitch + row0;
+                store_part(map, c0 % kPanel, it.x[1 - (tile.step & 1)] + y, place);
+                store_part(map, c0 % kPanel, it.low + y, place + kPartBytes);
+                stores_commit();
+            }
+            __syncwarp();
         }
+        return true;
     }
 };
 
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
-novak_orthogonalize_products_kernel(const __grid_constant__ ProductArgs a, const __grid_constant__ CUtensorMap map)
+novak_orthogonalize_products_kernel(const __grid_constant__ ProductArgs a, const __grid_constant__ CUtensorMap map,
+                                    const __grid_constant__ CUtensorMap part_map)
 {
     extern __shared__ uint8_t raw[];
-    const uint32_t stages = (smem_addr(raw) + 1023) & ~1023u;
-    Shared &sh = *reinterpret_cast<Shared *>(raw + (stages - smem_addr(raw)) + kStages * kStageBytes);
+    const uint32_t stages = (smem_addr(raw) + 1023) & ~1023u, places = stages + kStages * kStageBytes;
+    Shared &sh = *reinterpret_cast<Shared *>(raw + (places - smem_addr(raw)) + 2 * kOutWarps * kPlaceBytes);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = cluster_rank();
 
@@ -727,12 +800,16 @@ novak_orthogonalize_products_kernel(const __grid_constant__ ProductArgs a, const
             mbar_init(smem_addr(&sh.tile_full[i]), 1);
             mbar_init(smem_addr(&sh.tile_empty[i]), 2 * kOutWarps + 3);      // who takes, who brings, and who issues
         }
+        for (int i = 0; i < 2 * kOutWarps; ++i) mbar_init(smem_addr(&sh.part_full[0][0]) + 8 * i, 1);
         mbar_init(smem_addr(&sh.want), 1);
         mbar_init(smem_addr(&sh.drained), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0) tmem_alloc_pair(smem_addr(&sh.tmem), 512);
-    if (threadIdx.x == 32 * kLoadWarp) prefetch_map(&map);
+    if (threadIdx.x == 32 * kLoadWarp) {
+        prefetch_map(&map);
+        prefetch_map(&part_map);
+    }
     tcgen05_before_sync();
     __syncthreads();
     cluster_sync();
@@ -758,43 +835,47 @@ novak_orthogonalize_products_kernel(const __grid_constant__ ProductArgs a, const
     };
     Tile tile;
     if (warp < kOutWarps) {
-        const int side = warp / 4, r = threadIdx.x % 128;
-        const uint32_t row_of = static_cast<uint32_t>(warp % 4) * 32 << 16;
-        uint32_t count = 0;
-        for (;;) {
+        const int side = warp / 4, quarter = warp % 4;
+        Taking taking{a, &part_map, places + 2 * warp * kPlaceBytes, smem_addr(sh.part_full[warp]), sh.columns[warp], 0.0f, 0, 0, 0, 0};
+        for (uint32_t count = 0; next(tile); ++count) {
             const uint32_t buf = count & 1;
-            const bool more = next(tile);
-            const Item &it = a.w.items[more ? tile.which : 0];
-            const int row0 = tile.row + static_cast<int>(rank) * kBlock, half = tile.columns / 2;
-            const int height = tile.what == 2 ? it.x_pitch : it.s_pitch;
-            Taking taking{a, it, tile, row0, r, tile.col + side * half, row0 < height ? half / 32 : 0, sh.columns[side], {}, {}};
-            if (more) {
-                if (lane == 0) ok = wait_parts(a, a.w.done + tile.which, tile.need);
-                ok = __shfl_sync(0xffffffffu, ok, 0);
-                if (ok) {
-                    const float *d = a.w.diags + it.diag;
-                    const int width = tile.what == 1 ? it.s_pitch : tile.what == 2 && it.tall ? it.s_pitch : 0, c = taking.col + r;
-                    if (r < half && c < width) taking.columns[r] = __ldcg(d + (tile.what == 1 ? 0 : it.s_pitch) + c);
-                    taking.fetch(0);
-                    ok = mbar_wait_warp(smem_addr(&sh.out_full[buf]), (count >> 1) & 1, a.wait_ns);
-                }
-                if (!ok && lane == 0) gave_up(a);
+            const Item &it = a.w.items[tile.which];
+            const int half = tile.columns / 2, height = tile.what == 2 ? it.x_pitch : it.s_pitch;
+            taking.row0 = tile.row + static_cast<int>(rank) * kBlock + quarter * 32;
+            taking.col = tile.col + side * half;
+            taking.parts = taking.row0 < height ? half / 32 : 0;
+            // what the tile needs beside its products, on its way before they are awaited
+            if (lane == 0) ok = wait_parts(a, a.w.done + tile.which, tile.need);
+            ok = __shfl_sync(0xffffffffu, ok, 0);
+            if (ok) {
+                asm volatile("fence.proxy.async;" ::: "memory");
+                taking.fetch(it, tile, 0);
+                ok = mbar_wait_warp(smem_addr(&sh.out_full[buf]), (count >> 1) & 1, a.wait_ns);
             }
-            // (where one's wait gave up the others do not go on to barriers that it will not come to)
-            ok = half_agree(side, ok);
-            if (!ok || !more) break;
-            tcgen05_after_sync();
-            taking.take(tmem + buf * 256 + side * half + row_of);
+            if (ok) {
+                tcgen05_after_sync();
+                ok = taking.take(it, tile, tmem + buf * 256 + side * half + (static_cast<uint32_t>(quarter) * 32 << 16));
+            }
+            if (!ok) {
+                if (lane == 0) gave_up(a);
+                break;
+            }
             tcgen05_before_sync();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(at_rank(smem_addr(&sh.out_empty[buf]), 0));
-            ++count;
-            // everything of this half is in memory, for tensor copies too, before that is told
+            // everything of this warp's is in memory, for tensor copies too, before that is told
             __threadfence();
-            asm volatile("fence.proxy.async;" ::: "memory");
-            half_sync(side);
-            if (r == 0 && tile.announced) asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(a.w.done + tile.which), "r"(1u) : "memory");
+            __syncwarp();
+            if (lane == 0 && tile.announced) {
+                stores_done();
+                asm volatile("fence.proxy.async;" ::: "memory");
+                __threadfence();
+                asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(a.w.done + tile.which), "r"(1u) : "memory");
+            }
+            __syncwarp();
         }
+        if (lane == 0) stores_done();
+        __syncwarp();
     } else if (warp == kLoadWarp) {
         Ring<kStages> at;
         int64_t issued = 0;
@@ -1040,11 +1121,16 @@ cudaError_t launch_orthogonalize(const OrthArgs &a, cudaStream_t stream)
     if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return cudaErrorInvalidValue;
+    CUtensorMap part_map;
+    const cuuint32_t part_box[2] = {32, 32};
+    if (encode(&part_map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, dims, strides, part_box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return cudaErrorInvalidValue;
     static std::atomic<uint64_t> asked{0};
     e = ask_shared_memory(novak_orthogonalize_products_kernel, kSmemBytes, asked);
     if (e != cudaSuccess) return e;
     return launch(novak_orthogonalize_products_kernel, dim3(static_cast<unsigned>(2 * std::min<int64_t>(kPairs, most))), kTcThreads, kSmemBytes,
-                  stream, p, map);
+                  stream, p, map, part_map);
 }
 
 }  // namespace novak

@@ -296,16 +296,18 @@ __global__ void __launch_bounds__(kThreads) novak_orthogonalize_start_kernel(Wor
 // boxes: a panel's rows are an operand's rows with the summed dimension contiguous (X X^T, A, B),
 // or the summed dimension (X^T X, the X of B X) with the operand's other one contiguous.
 //
-// In each CTA: warps 0-7 take tiles out (a warp a quarter of the lanes, warps 0-3 the left half of
-// the columns, each on its own), warp 8 brings operands, warp 9 issues the products (of the pair: in the
-// leading CTA), warp 10 of the leading CTA hands tiles out.
-constexpr int kPairs = 74, kStages = 5, kRing = 2;
+// In each CTA: warps 0-15 take tiles out (a warp a quarter of the lanes and of the columns, each on
+// its own), warp 16 brings operands, warp 17 issues the products (of the pair: in the leading
+// CTA), warp 18 of the leading CTA hands tiles out.
+constexpr int kPairs = 74, kStages = 5, kRing = 4;
 constexpr int kBoxBytes = kPanel * 128, kStageBytes = 4 * kBoxBytes;
 constexpr int kPartBytes = 32 * 64, kPlaceBytes = 2 * kPartBytes;       // 32 x 32 elements in fp16; two of those
-constexpr int kTold = 16;       // parts of a tile that are told of when they are stored: each warp's that takes it out
-constexpr int kOutWarps = 8, kLoadWarp = 8, kMmaWarp = 9, kTileWarp = 10, kTcThreads = 384;
+constexpr int kTold = 32;       // parts of a tile that are told of when they are stored: each warp's that takes it out
+constexpr int kOutWarps = 16, kLoadWarp = kOutWarps, kMmaWarp = kLoadWarp + 1, kTileWarp = kMmaWarp + 1, kTcThreads = 32 * (kTileWarp + 1);
 
-// What is to be done for a tile, as the leading CTA's warp 10 writes it into both CTAs.
+// What is to be done for a tile, as the leading CTA's warp 18 sends it to both CTAs: all that they need to know (what
+// the matrices' records say comes from L2 each time, since every wait for other SMs' tiles empties the
+// first-level cache).
 struct Tile {
     int what;               // 0: A; 1: B; 2: X; -1: no more
     int which, step, columns;
@@ -317,18 +319,24 @@ struct Tile {
     uint32_t descriptor;    // of the instruction
     unsigned need;          // parts of this matrix that have to be stored before
     int announced;          // 0: a test's tile whose end nobody is told
+    // of what takes it out, in rows of 128 bytes as above:
+    int height, width;      // rows and columns that are stored
+    int pitch;              // rows of a panel
+    int in, low, out;       // what the tile needs beside its products, X's second part, where it goes
+    int diag;               // floats to the diagonal that is needed, or that A's and B's own diagonals are put to
+    int tall;
 };
 constexpr int kTileWords = sizeof(Tile) / 4;
+__device__ __forceinline__ uint32_t tile_word(const Tile &t, int i) { return reinterpret_cast<const uint32_t *>(&t)[i]; }
 static_assert(kTileWords <= 32, "a lane each");
 
 struct Shared {
-    alignas(8) uint64_t full[kStages], empty[kStages], out_full[2], out_empty[2], tile_full[kRing], tile_empty[kRing], want, drained;
-    uint64_t part_full[kOutWarps][2];
+    alignas(8) uint64_t full[kStages], empty[kStages], out_full[2], out_empty[2], tile_full[kRing], tile_empty[kRing], ready[kRing], want, drained;
+    uint64_t part_full[kOutWarps];
     uint32_t tmem;
     Tile tiles[kRing];
-    alignas(16) float columns[kOutWarps][32];       // of a diagonal, for the part that is worked on
 };
-constexpr int kSmemBytes = kStages * kStageBytes + 2 * kOutWarps * kPlaceBytes + 1024 + static_cast<int>(sizeof(Shared));
+constexpr int kSmemBytes = kStages * kStageBytes + kOutWarps * kPlaceBytes + 1024 + static_cast<int>(sizeof(Shared));
 static_assert(kSmemBytes <= 227 * 1024, "shared memory");
 
 struct ProductArgs {
@@ -376,30 +384,29 @@ __device__ __forceinline__ bool wait_parts(const ProductArgs &a, const unsigned 
     }
 }
 
-// Waits for a barrier that the other CTA of the pair completes, with what it wrote before.
-__device__ __forceinline__ bool mbar_try_cluster(uint32_t bar, uint32_t parity)
+// Words of a tile into a CTA of the pair, whose barrier there is told of them as of a copy: who waits for
+// it needs no fence beyond its CTA (a wait with one of the cluster's took 2000 cycles).
+__device__ __forceinline__ void mbar_expect_at(uint32_t bar, uint32_t bytes)
 {
-    uint32_t ok;
-    asm volatile("{\n.reg .pred p;\n"
-                 "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n"
-                 "selp.u32 %0, 1, 0, p;\n}"
-                 : "=r"(ok) : "r"(bar), "r"(parity), "r"(1000000) : "memory");
-    return ok != 0;
+    asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, uint64_t limit)
+__device__ __forceinline__ void send_word(uint32_t dst, uint32_t word, uint32_t bar)
 {
-    uint64_t t0 = 0;
-    for (;;) {
-        for (int i = 0; i < 64; ++i)
-            if (mbar_try_cluster(bar, parity)) return true;
-        const uint64_t t = global_ns();
-        if (t0 == 0) t0 = t;
-        else if (t - t0 > limit) return false;
-    }
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(dst), "r"(word), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void mbar_arrive_release(uint32_t bar)
+// (A tile's words have been used when its place is given back; a release at the cluster's scope would wait for
+// all stores on their way, 9000 cycles.)
+__device__ __forceinline__ void mbar_arrive_relaxed(uint32_t bar)
 {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+// Whether a phase is complete, without waiting.
+__device__ __forceinline__ bool mbar_try_now(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done != 0;
 }
 
 // A 64 x 64 box, whose arrival is told to a barrier of the leading CTA.
@@ -424,21 +431,6 @@ __device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait
 __device__ constexpr uint32_t fp16_descriptor(int columns, bool a_across, bool b_across)
 {
     return 1u << 4 | (a_across ? 1u << 15 : 0u) | (b_across ? 1u << 16 : 0u) | static_cast<uint32_t>(columns >> 3) << 17 | (256u >> 4) << 24;
-}
-
-// 32 consecutive columns of this warp's 32 lanes; done at tmem_load_wait.
-__device__ __forceinline__ void tmem_load32(uint32_t tmem, uint32_t (&r)[32])
-{
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
-          "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]),
-          "=r"(r[30]), "=r"(r[31])
-        : "r"(tmem) : "memory");
 }
 
 // Tile number t, by the whole warp.
@@ -509,6 +501,14 @@ __device__ __forceinline__ Tile tile_at(const ProductArgs &a, int64_t t)
     const unsigned before = r.what == 0 ? 0 : r.what == 1 ? s : s + it.tiles[1];
     r.need = static_cast<unsigned>(kTold) * (static_cast<unsigned>(r.step) * (s + it.tiles[1] + x) + before);
     r.announced = t != a.withheld;
+    r.height = r.what == 2 ? it.x_pitch : it.s_pitch;
+    r.width = r.what == 2 ? it.cols : it.side;
+    r.pitch = r.height;
+    r.in = r.what == 2 ? it.x[turn] : it.gram;
+    r.low = it.low;
+    r.out = r.what == 0 ? it.gram : r.what == 1 ? it.poly : it.x[1 - turn];
+    r.diag = it.diag + (r.what == 2 ? it.s_pitch : 0);
+    r.tall = it.tall;
     return r;
 }
 
@@ -608,172 +608,204 @@ __device__ __forceinline__ void step_theta(const Item &it, float decay, uint32_t
     __syncwarp();
 }
 
-// A warp that takes tiles out: its places in shared memory, their barriers and uses.
+__device__ __forceinline__ F2 halves(uint32_t w)
+{
+    const float2 p = unpack_half(w);
+    return F2(p.x, p.y);
+}
+__device__ __forceinline__ uint32_t pack_half(F2 x) { return pack_half(x.lo(), x.hi()); }
+
+// A warp that takes tiles out: its place in shared memory and the barrier of what comes there.
 struct Taking {
     const ProductArgs &a;
     const CUtensorMap *map;
-    uint32_t places, bars;          // two places of two parts; two barriers
-    float *columns;
-    float next_column;              // this lane's, for the next part
-    uint32_t phases;                // of the barriers, a bit each
+    uint32_t place, bar;
+    uint32_t phase;                 // of the barrier
+    bool untold;                    // stores are on their way that nobody has been told of
+    int told_which, told;           // whose; whether they are to be
+    bool own_stores;                // and not by tensor copies alone
     // of a tile:
     int row0, col, parts;           // the warp's first row and column; times 32 columns
+    float column, next_column;      // of a diagonal, this lane's, for the part that is worked on and for the next
 
     // Panels are stored to their ends, which are summed over as zeros; blocks of A and B below the
     // diagonal are not stored from here.  (The same for all of a warp.)
-    __device__ __forceinline__ bool here(const Item &it, const Tile &tile, int part) const
+    __device__ __forceinline__ bool here(const Tile &tile, int part) const
     {
         const int c = col + 32 * part, panel = c / kPanel * kPanel;
-        return part < parts && (tile.what == 2 ? panel < it.cols : panel < it.side && c / kBlock >= row0 / kBlock);
+        return part < parts && panel < tile.width && (tile.what == 2 || c / kBlock >= row0 / kBlock);
     }
-    // What a part needs on its way into place part % 2, once what was there is out.
-    __device__ __forceinline__ void fetch(const Item &it, const Tile &tile, int part)
+    // What a part needs on its way, once what was in its place is out.
+    __device__ __forceinline__ void fetch(const Tile &tile, int part)
     {
-        if (!here(it, tile, part)) return;
-        const int lane = threadIdx.x & 31, set = part & 1, c = col + 32 * part;
-        if (tile.what == 1 || (tile.what == 2 && it.tall)) next_column = __ldcg(a.w.diags + it.diag + (tile.what == 1 ? 0 : it.s_pitch) + c + lane);
+        if (!here(tile, part)) return;
+        const int lane = threadIdx.x & 31, c = col + 32 * part;
+        if (tile.what == 1 || (tile.what == 2 && tile.tall)) next_column = __ldcg(a.w.diags + tile.diag + c + lane);
         if (lane == 0) {
             stores_read();
             if (tile.what > 0) {
-                const uint32_t place = places + set * kPlaceBytes, bar = bars + set * 8;
-                const int turn = tile.step & 1, pitch = tile.what == 1 ? it.s_pitch : it.x_pitch, y = c / kPanel * pitch + row0;
+                const int y = c / kPanel * tile.pitch + row0;
                 mbar_expect(bar, tile.what == 1 ? kPartBytes : 2 * kPartBytes);
-                load_part(place, map, c % kPanel, (tile.what == 1 ? it.gram : it.x[turn]) + y, bar);
-                if (tile.what == 2) load_part(place + kPartBytes, map, c % kPanel, it.low + y, bar);
+                load_part(place, map, c % kPanel, tile.in + y, bar);
+                if (tile.what == 2) load_part(place + kPartBytes, map, c % kPanel, tile.low + y, bar);
             }
         }
         __syncwarp();
     }
+    // Everything of the tile before is in memory, for tensor copies too: told.
+    __device__ __forceinline__ void tell()
+    {
+        if (!untold) return;
+        untold = false;
+        if (own_stores) __threadfence();
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) {
+            stores_done();
+            if (told) asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(a.w.done + told_which), "r"(1u) : "memory");
+        }
+        __syncwarp();
+    }
+    // The diagonal's elements of columns i and i + 1 of a part.
+    __device__ __forceinline__ F2 columns(int i) const { return F2(__shfl_sync(0xffffffffu, column, i), __shfl_sync(0xffffffffu, column, i + 1)); }
+    // Sixteen columns of A or B, from the sums in tensor memory (and of what A has there).
+    __device__ __forceinline__ void square16(const Tile &tile, int row, bool diagonal, float d_row, const float (&raw)[16],
+                                             uint32_t *h, int first) const
+    {
+        const int on = (threadIdx.x & 31) - first;              // this row's diagonal element
+        if (tile.what == 0) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[i] = pack_half(F2(raw[2 * i], raw[2 * i + 1]) * F2(kScaleA / (kScaleX * kScaleX)));
+            if (diagonal && on >= 0 && on < 16) {
+                float mine = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (i == on) mine = raw[i];
+                a.w.diags[tile.diag + row] = mine * (1.0f / (kScaleX * kScaleX));
+            }
+        } else {
+            const float cb = a.coefficients[tile.step][1], cc = a.coefficients[tile.step][2];
+            constexpr float kSquare = 1.0f / (kScaleA * kScaleA);
+            // B' scale = scale (c (square + d a) + b a), a the element of A': (c d + b) a scale + square c scale
+            const F2 rest(kScaleB * cc * kSquare), cd(cc * (kScaleB / kScaleA)), bd(fmaf(cc, d_row, cb) * (kScaleB / kScaleA));
+            if (diagonal && on >= 0 && on < 16) {
+                float mine = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (i == on) mine = raw[i];
+                a.w.diags[tile.diag + tile.pitch + row] = fmaf(cc, fmaf(mine, kSquare, d_row * d_row), cb * d_row);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const F2 d = columns(first + 2 * i);
+                h[i] = pack_half(fma2(F2(raw[2 * i], raw[2 * i + 1]), rest, fma2(d, cd, bd) * halves(h[i])));
+            }
+        }
+        if (diagonal) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (2 * i == on) h[i] &= 0xffff0000u;
+                if (2 * i + 1 == on) h[i] &= 0xffffu;
+            }
+        }
+    }
     // false: a wait gave up.
-    __device__ __forceinline__ bool take(const Item &it, const Tile &tile, uint32_t src)
+    __device__ __forceinline__ bool take(const Tile &tile, uint32_t src)
     {
         const int lane = threadIdx.x & 31, row = row0 + lane;
-        float *da = a.w.diags + it.diag, *db = da + it.s_pitch;
-        const float ca = a.coefficients[tile.step][0], cb = a.coefficients[tile.step][1], cc = a.coefficients[tile.step][2];
+        const float ca = a.coefficients[tile.step][0];
         const bool last = tile.step + 1 == a.steps, full = tile.step + 2 >= a.steps;
         float d_row = 0.0f;
-        if (parts > 0 && tile.what == 1) d_row = __ldcg(da + row);
-        if (parts > 0 && tile.what == 2 && !it.tall) d_row = __ldcg(db + row);
+        if (parts > 0 && (tile.what == 1 || (tile.what == 2 && !tile.tall))) d_row = __ldcg(a.w.diags + tile.diag + row);
 #pragma unroll 1
         for (int part = 0; part < parts; ++part) {
-            columns[lane] = next_column;
-            __syncwarp();
-            fetch(it, tile, part + 1);
-            if (!here(it, tile, part)) continue;
-            const int set = part & 1, c0 = col + 32 * part;
-            const uint32_t place = places + set * kPlaceBytes;
-            uint32_t raw[32], h[16];
-            if (tile.what > 0) {
-                if (!mbar_wait_warp(bars + set * 8, phases >> set & 1, a.wait_ns)) return false;
-                phases ^= 1u << set;
-            }
-            tmem_load32(src + 32 * part, raw);
-            float v[32];
+            if (here(tile, part)) {
+                const int c0 = col + 32 * part;
+                column = next_column;
+                if (tile.what > 0) {
+                    if (!mbar_wait_warp(bar, phase, a.wait_ns)) return false;
+                    phase ^= 1;
+                }
+                __syncwarp();
+                uint32_t h[16];
+                if (tile.what < 2) {
+                    if (tile.what == 1) get_row(place, lane, h);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(raw[i]);
-            const float4 *d_cols = reinterpret_cast<const float4 *>(columns);
-            if (tile.what < 2) {
-                const int on = row - c0;                        // this row's diagonal element is here if in [0, 32)
-                if (tile.what == 0) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] *= kScaleA / (kScaleX * kScaleX);
-                    if (c0 == row0) {                           // (the warp's block is on the diagonal as a whole, or off)
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (i == on) {
-                                da[row] = v[i] * (1.0f / kScaleA);
-                                v[i] = 0.0f;
-                            }
+                    for (int k = 0; k < 2; ++k) {
+                        float raw[16];
+                        tmem_load16(src + 32 * part + 16 * k, raw);
+                        // (a warp's 32 x 32 are on the diagonal as a whole, or off)
+                        square16(tile, row, c0 == row0, d_row, raw, h + 8 * k, 16 * k);
                     }
-                } else {
-                    constexpr float kSquare = 1.0f / (kScaleA * kScaleA);
+                    // above the diagonal's blocks: the transposed part too
+                    const bool mirror = c0 / kBlock > row0 / kBlock;
+                    put_row(place, lane, h);
+                    if (mirror) put_across(place + kPartBytes, h);
+                    fence_async_shared();
+                    __syncwarp();
+                    if (lane == 0) {
+                        store_part(map, c0 % kPanel, tile.out + c0 / kPanel * tile.pitch + row0, place);
+                        if (mirror) store_part(map, row0 % kPanel, tile.out + row0 / kPanel * tile.pitch + c0, place + kPartBytes);
+                        stores_commit();
+                    }
+                } else if (!last) {
+                    uint32_t low[16];
                     get_row(place, lane, h);
-                    float mine = 0.0f;
+                    get_row(place + kPartBytes, lane, low);
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
-                        const float4 d4 = d_cols[i / 4];
-                        const float d[4] = {d4.x, d4.y, d4.z, d4.w};
-                        const float2 lo = unpack_half(h[i / 2]), hi = unpack_half(h[i / 2 + 1]);
-                        const float off[4] = {lo.x, lo.y, hi.x, hi.y};
+                    for (int k = 0; k < 2; ++k) {
+                        float raw[16];
+                        tmem_load16(src + 32 * part + 16 * k, raw);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            if (i + k == on) mine = v[i + k];
-                            const float o = off[k] * (1.0f / kScaleA);
-                            v[i + k] = kScaleB * fmaf(cc, fmaf(v[i + k], kSquare, (d_row + d[k]) * o), cb * o);
+                        for (int i = 0; i < 8; ++i) {
+                            const F2 v = next_x(tile, 16 * k + 2 * i, F2(raw[2 * i], raw[2 * i + 1]), h[8 * k + i], low[8 * k + i], d_row, ca, full);
+                            h[8 * k + i] = pack_half(v);
+                            low[8 * k + i] = pack_half(fma2(halves(h[8 * k + i]), F2(-1.0f), v) * F2(kScaleLow));
                         }
                     }
-                    if (c0 == row0) {
-                        db[row] = fmaf(cc, fmaf(mine, kSquare, d_row * d_row), cb * d_row);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (i == on) v[i] = 0.0f;
+                    put_row(place, lane, h);
+                    put_row(place + kPartBytes, lane, low);
+                    fence_async_shared();
+                    __syncwarp();
+                    if (lane == 0) {
+                        const int y = c0 / kPanel * tile.pitch + row0;
+                        store_part(map, c0 % kPanel, tile.out + y, place);
+                        store_part(map, c0 % kPanel, tile.low + y, place + kPartBytes);
+                        stores_commit();
                     }
+                } else {
+                    uint32_t low[16];
+                    get_row(place, lane, h);
+                    get_row(place + kPartBytes, lane, low);
+                    float v[32];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        float raw[16];
+                        tmem_load16(src + 32 * part + 16 * k, raw);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            (next_x(tile, 16 * k + 2 * i, F2(raw[2 * i], raw[2 * i + 1]), h[8 * k + i], low[8 * k + i], d_row, ca, full) * F2(1.0f / kScaleX))
+                                .get(v[16 * k + 2 * i], v[16 * k + 2 * i + 1]);
+                    }
+                    __syncwarp();
+                    const Item &it = a.w.items[tile.which];
+                    if (a.theta) step_theta(it, a.decay, place, row0, c0, v);
+                    else write_out(it, place, row0, c0, v);
+                    // (the next load into this place comes behind what was read there)
+                    fence_async_shared();
                 }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) h[i] = pack_half(v[2 * i], v[2 * i + 1]);
-                // above the diagonal's blocks: the transposed part too
-                const bool mirror = c0 / kBlock > row0 / kBlock;
-                put_row(place, lane, h);
-                if (mirror) put_across(place + kPartBytes, h);
-                fence_async_shared();
                 __syncwarp();
-                if (lane == 0) {
-                    const int base = tile.what == 0 ? it.gram : it.poly;
-                    store_part(map, c0 % kPanel, base + c0 / kPanel * it.s_pitch + row0, place);
-                    if (mirror) store_part(map, row0 % kPanel, base + row0 / kPanel * it.s_pitch + c0, place + kPartBytes);
-                    stores_commit();
-                }
-                __syncwarp();
-                continue;
             }
-            uint32_t low[16];
-            get_row(place, lane, h);
-            get_row(place + kPartBytes, lane, low);
-#pragma unroll
-            for (int i = 0; i < 32; i += 4) {
-                float d[4] = {d_row, d_row, d_row, d_row};
-                if (it.tall) {
-                    const float4 d4 = d_cols[i / 4];
-                    d[0] = d4.x; d[1] = d4.y; d[2] = d4.z; d[3] = d4.w;
-                }
-                const float2 p0 = unpack_half(h[i / 2]), p1 = unpack_half(h[i / 2 + 1]), q0 = unpack_half(low[i / 2]), q1 = unpack_half(low[i / 2 + 1]);
-                const float p[4] = {p0.x, p0.y, p1.x, p1.y}, q[4] = {q0.x, q0.y, q1.x, q1.y};
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float x = fmaf(q[k], 1.0f / kScaleLow, p[k]);
-                    v[i + k] = fmaf(v[i + k], 1.0f / kScaleB, fmaf(d[k], full ? x : p[k], ca * x));
-                }
-            }
-            if (last) {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] *= 1.0f / kScaleX;
-                __syncwarp();
-                if (a.theta) step_theta(it, a.decay, place, row0, c0, v);
-                else write_out(it, place, row0, c0, v);
-                // (the next load into this place comes behind what was read there)
-                fence_async_shared();
-                __syncwarp();
-                continue;
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                h[i] = pack_half(v[2 * i], v[2 * i + 1]);
-                const float2 p = unpack_half(h[i]);
-                low[i] = pack_half((v[2 * i] - p.x) * kScaleLow, (v[2 * i + 1] - p.y) * kScaleLow);
-            }
-            put_row(place, lane, h);
-            put_row(place + kPartBytes, lane, low);
-            fence_async_shared();
-            __syncwarp();
-            if (lane == 0) {
-                const int y = c0 / kPanel * it.x_pitch + row0;
-                store_part(map, c0 % kPanel, it.x[1 - (tile.step & 1)] + y, place);
-                store_part(map, c0 % kPanel, it.low + y, place + kPartBytes);
-                stores_commit();
-            }
-            __syncwarp();
+            fetch(tile, part + 1);
         }
         return true;
+    }
+    // Two elements of the next X: a x + d x + (the product's sum), x by its two parts.
+    __device__ __forceinline__ F2 next_x(const Tile &tile, int i, F2 sum, uint32_t hi, uint32_t low, float d_row, float ca, bool full) const
+    {
+        const F2 p = halves(hi), x = fma2(halves(low), F2(1.0f / kScaleLow), p);
+        F2 d(d_row);
+        if (tile.tall) d = columns(i);
+        return fma2(sum, F2(1.0f / kScaleB), fma2(d, full ? x : p, x * F2(ca)));
     }
 };
 
@@ -783,7 +815,7 @@ novak_orthogonalize_products_kernel(const __grid_constant__ ProductArgs a, const
 {
     extern __shared__ uint8_t raw[];
     const uint32_t stages = (smem_addr(raw) + 1023) & ~1023u, places = stages + kStages * kStageBytes;
-    Shared &sh = *reinterpret_cast<Shared *>(raw + (places - smem_addr(raw)) + 2 * kOutWarps * kPlaceBytes);
+    Shared &sh = *reinterpret_cast<Shared *>(raw + (places - smem_addr(raw)) + kOutWarps * kPlaceBytes);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = cluster_rank();
 
@@ -798,9 +830,10 @@ novak_orthogonalize_products_kernel(const __grid_constant__ ProductArgs a, const
         }
         for (int i = 0; i < kRing; ++i) {
             mbar_init(smem_addr(&sh.tile_full[i]), 1);
+            mbar_init(smem_addr(&sh.ready[i]), 1);
             mbar_init(smem_addr(&sh.tile_empty[i]), 2 * kOutWarps + 3);      // who takes, who brings, and who issues
         }
-        for (int i = 0; i < 2 * kOutWarps; ++i) mbar_init(smem_addr(&sh.part_full[0][0]) + 8 * i, 1);
+        for (int i = 0; i < kOutWarps; ++i) mbar_init(smem_addr(&sh.part_full[i]), 1);
         mbar_init(smem_addr(&sh.want), 1);
         mbar_init(smem_addr(&sh.drained), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -819,42 +852,47 @@ novak_orthogonalize_products_kernel(const __grid_constant__ ProductArgs a, const
 
     bool ok = true;
     Ring<kRing> ring;
-    // The next tile; its words are this warp's after that, and the place in the ring is given back.
-    const auto next = [&](Tile &tile) {
-        ok = mbar_wait_cluster(smem_addr(&sh.tile_full[ring.slot]), ring.phase, a.wait_ns);
-        ok = __all_sync(0xffffffffu, ok);
+    // The next tile is in its place in the ring; to be given back when it is done with.
+    const auto next = [&] {
+        ok = mbar_wait_warp(smem_addr(&sh.tile_full[ring.slot]), ring.phase, a.wait_ns);
         if (!ok) {
             if (lane == 0) gave_up(a);
             return false;
         }
-        tile = sh.tiles[ring.slot];
-        __syncwarp();
-        if (lane == 0) mbar_arrive_release(at_rank(smem_addr(&sh.tile_empty[ring.slot]), 0));
-        ring.advance();
-        return tile.what >= 0;
+        return sh.tiles[ring.slot].what >= 0;
     };
-    Tile tile;
+    const auto release = [&] {
+        __syncwarp();
+        if (lane == 0) mbar_arrive_relaxed(at_rank(smem_addr(&sh.tile_empty[ring.slot]), 0));
+        ring.advance();
+    };
     if (warp < kOutWarps) {
-        const int side = warp / 4, quarter = warp % 4;
-        Taking taking{a, &part_map, places + 2 * warp * kPlaceBytes, smem_addr(sh.part_full[warp]), sh.columns[warp], 0.0f, 0, 0, 0, 0};
-        for (uint32_t count = 0; next(tile); ++count) {
-            const uint32_t buf = count & 1;
-            const Item &it = a.w.items[tile.which];
-            const int half = tile.columns / 2, height = tile.what == 2 ? it.x_pitch : it.s_pitch;
+        const int group = warp / 4, quarter = warp % 4;
+        Taking taking{a, &part_map, places + warp * kPlaceBytes, smem_addr(&sh.part_full[warp]), 0, false, 0, 0, false, 0, 0, 0, 0.0f, 0.0f};
+        for (uint32_t count = 0;; ++count) {
+            const uint32_t buf = count & 1, ready = smem_addr(&sh.ready[ring.slot]);
+            // (nobody waits longer than need be for what is stored)
+            if (!__all_sync(0xffffffffu, mbar_try_now(smem_addr(&sh.tile_full[ring.slot]), ring.phase))) taking.tell();
+            if (!next()) break;
+            const Tile &tile = sh.tiles[ring.slot];
+            const int quarter_columns = tile.columns / 4;
             taking.row0 = tile.row + static_cast<int>(rank) * kBlock + quarter * 32;
-            taking.col = tile.col + side * half;
-            taking.parts = taking.row0 < height ? half / 32 : 0;
-            // what the tile needs beside its products, on its way before they are awaited
-            if (lane == 0) ok = wait_parts(a, a.w.done + tile.which, tile.need);
-            ok = __shfl_sync(0xffffffffu, ok, 0);
+            taking.col = tile.col + group * quarter_columns;
+            taking.parts = taking.row0 < tile.height ? quarter_columns / 32 : 0;
+            // What the tile needs beside its products, on its way before they are awaited, and before the tile before has
+            // arrived in memory, unless this one waits for that.
+            if (!__all_sync(0xffffffffu, mbar_try_now(ready, ring.phase))) {
+                taking.tell();
+                ok = mbar_wait_warp(ready, ring.phase, a.wait_ns);
+            }
             if (ok) {
-                asm volatile("fence.proxy.async;" ::: "memory");
-                taking.fetch(it, tile, 0);
+                taking.fetch(tile, 0);
+                taking.tell();
                 ok = mbar_wait_warp(smem_addr(&sh.out_full[buf]), (count >> 1) & 1, a.wait_ns);
             }
             if (ok) {
                 tcgen05_after_sync();
-                ok = taking.take(it, tile, tmem + buf * 256 + side * half + (static_cast<uint32_t>(quarter) * 32 << 16));
+                ok = taking.take(tile, tmem + buf * 256 + group * quarter_columns + (static_cast<uint32_t>(quarter) * 32 << 16));
             }
             if (!ok) {
                 if (lane == 0) gave_up(a);
@@ -863,27 +901,27 @@ novak_orthogonalize_products_kernel(const __grid_constant__ ProductArgs a, const
             tcgen05_before_sync();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(at_rank(smem_addr(&sh.out_empty[buf]), 0));
-            // everything of this warp's is in memory, for tensor copies too, before that is told
-            __threadfence();
-            __syncwarp();
-            if (lane == 0 && tile.announced) {
-                stores_done();
-                asm volatile("fence.proxy.async;" ::: "memory");
-                __threadfence();
-                asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(a.w.done + tile.which), "r"(1u) : "memory");
-            }
-            __syncwarp();
+            taking.untold = true;
+            taking.told_which = tile.which;
+            taking.told = tile.announced;
+            taking.own_stores = tile.what < 2 || tile.step + 1 == a.steps;
+            release();
         }
-        if (lane == 0) stores_done();
-        __syncwarp();
+        taking.tell();
     } else if (warp == kLoadWarp) {
         Ring<kStages> at;
         int64_t issued = 0;
         const uint32_t full0 = at_rank(smem_addr(&sh.full[0]), 0);
-        while (ok && next(tile)) {
+        for (;;) {
+            const uint32_t ready = smem_addr(&sh.ready[ring.slot]);
+            if (!ok || !next()) break;
+            const Tile tile = sh.tiles[ring.slot];
+            release();
             if (lane == 0) {
                 ok = wait_parts(a, a.w.done + tile.which, tile.need);
+                // (what other SMs have stored is there for tensor copies, this warp's and those of the warps that wait for `ready`)
                 asm volatile("fence.proxy.async;" ::: "memory");
+                if (ok) mbar_arrive(ready);
                 const int boxes = tile.columns / 128;
                 int ya = tile.a + static_cast<int>(rank) * tile.a_rank, yb = tile.b + static_cast<int>(rank) * tile.b_rank;
                 for (int i = 0; ok && i < tile.steps; ++i, ya += tile.a_step, yb += tile.b_step) {
@@ -897,7 +935,7 @@ novak_orthogonalize_products_kernel(const __grid_constant__ ProductArgs a, const
                     if (boxes == 2) load_box(dst + 3 * kBoxBytes, &map, yb + tile.b_half, bar);
                     at.advance();
                     ++issued;
-                    if (rank == 0 && i == max(tile.steps - 3, 0)) mbar_arrive(smem_addr(&sh.want));
+                    if (rank == 0 && i == max(tile.steps - 12, 0)) mbar_arrive(smem_addr(&sh.want));
                 }
                 if (!ok) gave_up(a);
             }
@@ -915,7 +953,9 @@ novak_orthogonalize_products_kernel(const __grid_constant__ ProductArgs a, const
     } else if (warp == kMmaWarp && rank == 0) {
         Ring<kStages> at;
         uint32_t count = 0;
-        while (ok && next(tile)) {
+        while (ok && next()) {
+            const Tile tile = sh.tiles[ring.slot];
+            release();
             const uint32_t buf = count & 1, d = tmem + buf * 256;
             const bool a_across = tile.descriptor >> 15 & 1, b_across = tile.descriptor >> 16 & 1;
             const uint32_t a_next = a_across ? 2048 >> 4 : 32 >> 4, b_next = b_across ? 2048 >> 4 : 32 >> 4;
@@ -944,10 +984,9 @@ novak_orthogonalize_products_kernel(const __grid_constant__ ProductArgs a, const
         mbar_wait_warp(smem_addr(&sh.drained), 0);
     } else if (warp == kTileWarp && rank == 0) {
         const int64_t all = static_cast<int64_t>(a.first[3]) * a.steps;
-        const uint32_t other = at_rank(smem_addr(&sh.tiles[0]), 1), other_full = at_rank(smem_addr(&sh.tile_full[0]), 1);
         bool more = true;
-        // The next tile is taken when this one's last operands are on their way, not before: with fewer
-        // tiles than pairs everybody is to have one.
+        // The next tile is taken some 6000 cycles before this one's last operands are on their way, which finding
+        // out what it is takes, and not before: with fewer tiles than pairs everybody is to have one.
         for (uint32_t taken = 0; more && ok; ++taken) {
             int64_t t = 0;
             if (taken > 0 && !mbar_wait_warp(smem_addr(&sh.want), (taken - 1) & 1, a.wait_ns)) {
@@ -957,23 +996,24 @@ novak_orthogonalize_products_kernel(const __grid_constant__ ProductArgs a, const
             if (lane == 0) t = !ok || load_acquire(&a.control->failed) ? all : atomicAdd(&a.control->ticket, 1u);
             t = __shfl_sync(0xffffffffu, t, 0);
             more = t < all;
+            Tile tile{};
             if (more) tile = tile_at(a, t);
             else tile.what = -1;
-            if (!__all_sync(0xffffffffu, mbar_wait_cluster(smem_addr(&sh.tile_empty[ring.slot]), ring.phase ^ 1, a.wait_ns))) {
+            if (!mbar_wait_warp(smem_addr(&sh.tile_empty[ring.slot]), ring.phase ^ 1, a.wait_ns)) {
                 ok = false;
                 if (lane == 0) gave_up(a);
                 break;
             }
-            if (lane == 0) sh.tiles[ring.slot] = tile;
-            __syncwarp();
-            if (lane < kTileWords) {
-                const uint32_t word = reinterpret_cast<const uint32_t *>(&sh.tiles[ring.slot])[lane];
-                asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(other + ring.slot * static_cast<uint32_t>(sizeof(Tile)) + 4 * lane), "r"(word) : "memory");
-            }
-            __syncwarp();
-            if (lane == 0) {
-                mbar_arrive_release(at_rank(smem_addr(&sh.tile_full[ring.slot]), 0));
-                mbar_arrive_release(other_full + ring.slot * 8);
+            // (every lane has all of its words: lane i sends word i to both CTAs)
+            uint32_t word = 0;
+#pragma unroll
+            for (int i = 0; i < kTileWords; ++i)
+                if (lane == i) word = tile_word(tile, i);
+            for (uint32_t r = 0; r < 2; ++r) {
+                const uint32_t bar = at_rank(smem_addr(&sh.tile_full[ring.slot]), r);
+                if (lane == 0) mbar_expect_at(bar, sizeof(Tile));
+                __syncwarp();
+                if (lane < kTileWords) send_word(at_rank(smem_addr(&sh.tiles[ring.slot]), r) + 4 * lane, word, bar);
             }
             ring.advance();
         }

@@ -23,6 +23,7 @@
 #include <algorithm>
 #include <atomic>
 #include <climits>
+#include <type_traits>
 
 #include <cuda_fp16.h>
 
@@ -35,7 +36,7 @@ namespace {
 constexpr float kScaleX = 4096.0f, kScaleA = 2048.0f, kScaleB = 4096.0f, kScaleLow = 2048.0f;   // (the low part: on top of X's)
 constexpr int kPanel = 64, kBlock = 128, kThreads = 256;
 constexpr int kUnitRows = 128;              // a unit of the first two kernels: so many rows of a panel
-constexpr int kMostChunks = kThreads;       // of a matrix
+constexpr int kMostChunks = 4 * kThreads;   // of a matrix
 
 // A matrix as the kernels see it.  Panels' places are in rows of 128 bytes from the workspace's start.
 struct Item {
@@ -138,11 +139,11 @@ template <typename First> __device__ __forceinline__ int item_of(int n, int at, 
 }
 
 // ---- |G|, and X to begin with
-struct HostItems {
-    static constexpr int kMost = 200;       // (a launch takes 32764 bytes)
-    Item item[kMost];
+constexpr int kMostItems = 200;             // with one launch, which takes 32764 bytes
+template <int N> struct HostItems {         // (a launch of 200 takes 10 us, one of 8 three)
+    Item item[N];
 };
-static_assert(sizeof(HostItems) + 256 <= 32764, "a launch's parameters");
+static_assert(sizeof(HostItems<kMostItems>) + 256 <= 32764, "a launch's parameters");
 
 struct Momentum {
     int on, nesterov;
@@ -162,24 +163,38 @@ __device__ __forceinline__ void for_unit(const Item &it, const Momentum &mo, int
                         (reinterpret_cast<uintptr_t>(it.m) & 15u) == 0;
     constexpr int kRows = kUnitRows / (kThreads / 16);
     float v[kRows][4] = {}, m[kRows][4];
+    if (vector) {               // (all of them on their way before the first is looked at)
+        using Raw = typename std::conditional<TYPE == NOVAK_TYPE_F32, float4, uint2>::type;
+        Raw x[kRows];
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-        const int row = row0 + i * (kThreads / 16);
-        if (row >= it.rows || col >= it.cols) continue;
-        if (vector) {
-            if constexpr (TYPE == NOVAK_TYPE_F32) {
-                const float4 x = *reinterpret_cast<const float4 *>(g + row * it.g_stride);
-                v[i][0] = x.x; v[i][1] = x.y; v[i][2] = x.z; v[i][3] = x.w;
-            } else {
-                const uint2 x = *reinterpret_cast<const uint2 *>(g + row * it.g_stride);
-                widen(x.x).get(v[i][0], v[i][1]);
-                widen(x.y).get(v[i][2], v[i][3]);
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (col + k < it.cols) v[i][k] = to_float(g[row * it.g_stride + k]);
+        for (int i = 0; i < kRows; ++i) {
+            const int row = row0 + i * (kThreads / 16);
+            x[i] = Raw{};
+            if (row < it.rows && col < it.cols) x[i] = *reinterpret_cast<const Raw *>(g + row * it.g_stride);
         }
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            if constexpr (TYPE == NOVAK_TYPE_F32) {
+                v[i][0] = x[i].x; v[i][1] = x[i].y; v[i][2] = x[i].z; v[i][3] = x[i].w;
+            } else {
+                widen(x[i].x).get(v[i][0], v[i][1]);
+                widen(x[i].y).get(v[i][2], v[i][3]);
+            }
+        }
+    } else {
+        T x[kRows][4];
+#pragma unroll
+        for (int i = 0; i < kRows; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int row = row0 + i * (kThreads / 16);
+                x[i][k] = T(0.0f);
+                if (row < it.rows && col + k < it.cols) x[i][k] = g[row * it.g_stride + k];
+            }
+#pragma unroll
+        for (int i = 0; i < kRows; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[i][k] = to_float(x[i][k]);
     }
     if (mo.on) {
 #pragma unroll
@@ -223,10 +238,11 @@ __device__ __forceinline__ double sum_of_all(double x, double *scratch)
     return x;
 }
 
-// The sum of a chunk's squares, in 64 bits (a square in fp32 would be lost below 1e-19).  The items come with the
-// launch, from number `first` on, and are put down for the kernels behind.
-template <int TYPE>
-__global__ void __launch_bounds__(kThreads) novak_orthogonalize_norm_kernel(const __grid_constant__ HostItems from, int first, int count, Work w,
+// The sum of a chunk's squares, in 64 bits (a square in fp32 would be lost below 1e-19): a thread's 32 in fp32,
+// scaled by a power of two to where they lie.  The items come with the launch, from number `first` on,
+// and are put down for the kernels behind.
+template <int TYPE, int N>
+__global__ void __launch_bounds__(kThreads) novak_orthogonalize_norm_kernel(const __grid_constant__ HostItems<N> from, int first, int count, Work w,
                                                                              Control *control, Momentum mo)
 {
     __shared__ double scratch[kThreads / 32];
@@ -242,43 +258,70 @@ __global__ void __launch_bounds__(kThreads) novak_orthogonalize_norm_kernel(cons
     const Item &it = from.item[item_of(count, chunk, [&](int i) { return from.item[i].chunk; })];
     const int64_t mine = chunk - it.chunk;
     double sum = 0.0;
-    for (int64_t u = mine * it.units / it.chunks; u < (mine + 1) * it.units / it.chunks; ++u)
+    for (int64_t u = mine * it.units / it.chunks; u < (mine + 1) * it.units / it.chunks; ++u) {
+        float x[kUnitRows / (kThreads / 16)][4], top = 0.0f;
+        int n = 0;
         for_unit<TYPE>(it, mo, static_cast<int>(u), true, [&](int, int, const float (&v)[4]) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) sum = fma(static_cast<double>(v[k]), static_cast<double>(v[k]), sum);
+            for (int k = 0; k < 4; ++k) top = fmaxf(top, fabsf(x[n][k] = v[k]));
+            ++n;
         });
+        // 2^-e of top = m 2^e, m in [1, 2) (of an infinity, and of what is below the normal numbers, near enough)
+        const int e = max(min(static_cast<int>(__float_as_uint(top) >> 23) - 127, 126), -126);
+        const float scale = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+        F2 s(0.0f);
+#pragma unroll
+        for (int i = 0; i < kUnitRows / (kThreads / 16); ++i)
+#pragma unroll
+            for (int k = 0; k < 4; k += 2) {
+                const F2 y = F2(x[i][k], x[i][k + 1]) * F2(scale);
+                s = fma2(y, y, s);
+            }
+        sum += scalbn(static_cast<double>(s.lo() + s.hi()), 2 * e);
+    }
     sum = sum_of_all(sum, scratch);
     if (threadIdx.x == 0) w.partial[chunk] = sum;
 }
 
 // X's two parts in units of 2^-12.
 template <int TYPE>
-__global__ void __launch_bounds__(kThreads) novak_orthogonalize_start_kernel(Work w, int n, Momentum mo, float eps)
+__global__ void __launch_bounds__(kThreads) novak_orthogonalize_start_kernel(Work w, int n, int64_t units, Momentum mo, float eps)
 {
     __shared__ double scratch[kThreads / 32];
     start();
-    const int unit = blockIdx.x;
-    const Item &it = w.items[item_of(n, unit, [&](int i) { return w.items[i].unit; })];
-    const double norm = sqrt(sum_of_all(static_cast<int>(threadIdx.x) < it.chunks ? w.partial[it.chunk + threadIdx.x] : 0.0, scratch));
-    // (a norm that is not finite makes everything of the matrix NaN)
-    const double scale = !(norm < INFINITY) ? NAN : norm > 0.0 ? kScaleX / fmax(norm, static_cast<double>(eps)) : 0.0;
-    const float tiny = scale > 1e36 ? 0x1p100f : 1.0f, rest = static_cast<float>(scale / tiny);     // (its reciprocal is beyond fp32)
-    const int panels = (it.cols + kPanel - 1) / kPanel, panel = (unit - it.unit) % panels;
-    for_unit<TYPE>(it, mo, unit - it.unit, false, [&](int row, int c, const float (&v)[4]) {
-        float x[4];
-        uint32_t hi[2], lo[2];
+    // this CTA's share of all units, matrix by matrix
+    int unit = static_cast<int>(blockIdx.x * units / gridDim.x);
+    const int end = static_cast<int>((blockIdx.x + 1) * units / gridDim.x);
+    if (unit >= end) return;
+    for (int which = item_of(n, unit, [&](int i) { return w.items[i].unit; }); unit < end; ++which) {
+        const Item it = w.items[which];
+        double norm = 0.0;
+        for (int i = threadIdx.x; i < it.chunks; i += kThreads) norm += w.partial[it.chunk + i];
+        __syncthreads();
+        norm = sqrt(sum_of_all(norm, scratch));
+        // (a norm that is not finite makes everything of the matrix NaN)
+        const double scale = !(norm < INFINITY) ? NAN : norm > 0.0 ? kScaleX / fmax(norm, static_cast<double>(eps)) : 0.0;
+        const float tiny = scale > 1e36 ? 0x1p100f : 1.0f, rest = static_cast<float>(scale / tiny);     // (its reciprocal is beyond fp32)
+        const int panels = (it.cols + kPanel - 1) / kPanel;
+        for (const int last = min(end, it.unit + it.units); unit < last; ++unit) {
+            const int panel = (unit - it.unit) % panels;
+            for_unit<TYPE>(it, mo, unit - it.unit, false, [&](int row, int c, const float (&v)[4]) {
+                float x[4];
+                uint32_t hi[2], lo[2];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = v[k] * tiny * rest;
+                for (int k = 0; k < 4; ++k) x[k] = v[k] * tiny * rest;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            hi[k] = pack_half(x[2 * k], x[2 * k + 1]);
-            const float2 h = unpack_half(hi[k]);
-            lo[k] = pack_half((x[2 * k] - h.x) * kScaleLow, (x[2 * k + 1] - h.y) * kScaleLow);
+                for (int k = 0; k < 2; ++k) {
+                    hi[k] = pack_half(x[2 * k], x[2 * k + 1]);
+                    const float2 h = unpack_half(hi[k]);
+                    lo[k] = pack_half((x[2 * k] - h.x) * kScaleLow, (x[2 * k + 1] - h.y) * kScaleLow);
+                }
+                const int64_t at = (static_cast<int64_t>(panel) * it.x_pitch + row) * kPanel + c;
+                *reinterpret_cast<uint2 *>(w.panels + static_cast<int64_t>(it.x[0]) * kPanel + at) = make_uint2(hi[0], hi[1]);
+                *reinterpret_cast<uint2 *>(w.panels + static_cast<int64_t>(it.low) * kPanel + at) = make_uint2(lo[0], lo[1]);
+            });
         }
-        const int64_t at = (static_cast<int64_t>(panel) * it.x_pitch + row) * kPanel + c;
-        *reinterpret_cast<uint2 *>(w.panels + static_cast<int64_t>(it.x[0]) * kPanel + at) = make_uint2(hi[0], hi[1]);
-        *reinterpret_cast<uint2 *>(w.panels + static_cast<int64_t>(it.low) * kPanel + at) = make_uint2(lo[0], lo[1]);
-    });
+    }
 }
 
 // ---- the products on the tensor cores --------------------------------------------------
@@ -1112,12 +1155,17 @@ cudaError_t launch_orthogonalize(const OrthArgs &a, cudaStream_t stream)
     const Momentum mo{a.m != nullptr, a.nesterov, a.momentum};
     const bool f32 = a.type == NOVAK_TYPE_F32;
     Layout again;
-    HostItems items{};
+    HostItems<kMostItems> items{};
     int first = 0, count = 0;
     const auto send = [&] {
-        const int64_t chunks = again.chunks - items.item[0].chunk;
-        const cudaError_t e = launch(f32 ? novak_orthogonalize_norm_kernel<0> : novak_orthogonalize_norm_kernel<1>, dim3(static_cast<unsigned>(chunks)),
-                                     kThreads, 0, stream, items, first, count, w, p.control, mo);
+        const dim3 chunks(static_cast<unsigned>(again.chunks - items.item[0].chunk));
+        const auto with = [&](auto few, auto kernel) {
+            std::copy_n(items.item, count, few.item);
+            return launch(kernel, chunks, kThreads, 0, stream, few, first, count, w, p.control, mo);
+        };
+        const cudaError_t e = count <= 8    ? with(HostItems<8>{}, f32 ? novak_orthogonalize_norm_kernel<0, 8> : novak_orthogonalize_norm_kernel<1, 8>)
+                              : count <= 40 ? with(HostItems<40>{}, f32 ? novak_orthogonalize_norm_kernel<0, 40> : novak_orthogonalize_norm_kernel<1, 40>)
+                                            : with(HostItems<kMostItems>{}, f32 ? novak_orthogonalize_norm_kernel<0, kMostItems> : novak_orthogonalize_norm_kernel<1, kMostItems>);
         first += count;
         count = 0;
         return e;
@@ -1138,12 +1186,12 @@ cudaError_t launch_orthogonalize(const OrthArgs &a, cudaStream_t stream)
             first_of[what] += it.tiles[what];
         }
         items.item[count++] = it;
-        if (count == HostItems::kMost) e = send();
+        if (count == kMostItems) e = send();
     }
     if (e == cudaSuccess && count > 0) e = send();
     if (e == cudaSuccess)
-        e = launch(f32 ? novak_orthogonalize_start_kernel<0> : novak_orthogonalize_start_kernel<1>, dim3(static_cast<unsigned>(l.units)), kThreads, 0,
-                   stream, w, n, mo, static_cast<float>(a.eps));
+        e = launch(f32 ? novak_orthogonalize_start_kernel<0> : novak_orthogonalize_start_kernel<1>, 
+                   dim3(static_cast<unsigned>(std::min<int64_t>(l.units, 148 * 4))), kThreads, 0, stream, w, n, l.units, mo, static_cast<float>(a.eps));
     if (e != cudaSuccess) return e;
 
     for (int k = 0; k < a.steps; ++k)

@@ -941,6 +941,8 @@ novak_orthogonalize_products_kernel(const __grid_constant__ ProductArgs a, const
             }
             if (!ok) {
                 if (lane == 0) gave_up(a);
+                taking.untold = true;           // (parts may be on their way to memory)
+                taking.told = 0;
                 break;
             }
             tcgen05_before_sync();

@@ -8,12 +8,19 @@ group), ``p.grad`` supplies the gradients, and a closure passed to ``step``
 is evaluated at Eq. 10's look-ahead point while the group is in its first
 N_taylor steps (Section 5.8: save, extrapolate, evaluate; the step then reads the
 saved parameters, which is the restore).  No arithmetic of the method happens here.
+
+``Muon`` beside it is for the weight matrices of a language model: momentum whose
+step is orthogonalised by Newton-Schulz products, one call of the library per parameter
+group.  Embeddings, norms and biases are NOVAK's.
 """
 from __future__ import annotations
+
+import math
 
 import torch
 
 from . import binding as B
+from . import ops
 
 _GROUP_KEYS = ("lr", "betas", "eps", "weight_decay", "nesterov", "lookahead_k", "lookahead_alpha",
                "nesterov_beta", "lookahead_mode", "rectified", "clip_threshold", "centralize",
@@ -132,3 +139,53 @@ class Novak(torch.optim.Optimizer):
             self._engines[gi] = None
             if sd is not None:
                 self._engine(gi).load_state_dict(sd)
+
+
+class Muon(torch.optim.Optimizer):
+    """Momentum with orthogonalised steps (``ops.orthogonal_step``) over fp32 CUDA matrices:
+    m <- momentum m + g, theta <- (1 - lr weight_decay) theta - lr scale X, where X is
+    g + momentum m (``nesterov``) or m brought close to orthogonal by the Newton-Schulz steps of
+    ``coefficients``.  ``scale``: "spectral", sqrt(max(1, rows / columns)), or "rms",
+    0.2 sqrt(max(rows, columns)), which makes a step as large as Adam's.
+
+    Parameters are contiguous and of two dimensions or more; one of more is a batch of matrices
+    (its last two dimensions each).  Parameters without a gradient are left alone.  Gradients of
+    one group are of one dtype (float32 or bfloat16)."""
+
+    def __init__(self, params, lr=2e-2, momentum=0.95, weight_decay=0.0, *, nesterov=True, scale="spectral",
+                 coefficients=ops.NEWTON_SCHULZ, eps=1e-7):
+        if scale not in ("spectral", "rms"):
+            raise ValueError(f"scale must be 'spectral' or 'rms', got {scale!r}")
+        super().__init__(params, dict(lr=lr, momentum=momentum, weight_decay=weight_decay, nesterov=nesterov, scale=scale,
+                                      coefficients=tuple(tuple(c) for c in coefficients), eps=eps))
+
+    def add_param_group(self, param_group):
+        super().add_param_group(param_group)
+        for p in self.param_groups[-1]["params"]:
+            if p.dim() < 2 or p.dtype != torch.float32 or not p.is_contiguous():
+                self.param_groups.pop()
+                raise ValueError("Muon takes contiguous float32 parameters of two dimensions or more")
+
+    @torch.no_grad()
+    def step(self, closure=None):
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        for group in self.param_groups:
+            params = [p for p in group["params"] if p.grad is not None]
+            if not params:
+                continue
+            for p in params:
+                if "momentum" not in self.state[p]:
+                    self.state[p]["momentum"] = torch.zeros_like(p)
+            steps = [group["lr"] * _scale(group["scale"], *p.shape[-2:]) for p in params]
+            ops.orthogonal_step(params, [p.grad if p.grad.is_contiguous() else p.grad.contiguous() for p in params],
+                                [self.state[p]["momentum"] for p in params], steps, momentum=group["momentum"],
+                                nesterov=group["nesterov"], decay=1.0 - group["lr"] * group["weight_decay"],
+                                coefficients=group["coefficients"], eps=group["eps"])
+        return loss
+
+
+def _scale(kind: str, rows: int, cols: int) -> float:
+    return math.sqrt(max(1.0, rows / max(cols, 1))) if kind == "spectral" else 0.2 * math.sqrt(max(rows, cols))

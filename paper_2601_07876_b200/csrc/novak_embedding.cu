@@ -15,6 +15,7 @@
 // zeros where there are no tokens, the sum of up to 16.  The order of all tokens is cut into pieces of 16
 // besides, and those of longer rows have a CTA each; the last one of a row's pieces to be done adds
 // their sums up in order.  So no word is too frequent.
+// Of few tokens there is one kernel: every CTA looks through the ids for those of its own rows.
 // (Zeros and sums in the first kernel, once it knows its rows: 58 to 77 us for 16384 tokens of 50000 x 768,
 // since its shared memory leaves room for too few warps to hide what loads wait for.)
 #include <algorithm>
@@ -81,6 +82,9 @@ constexpr int kCluster = 8;                             // CTAs that look throug
 constexpr int kList = 4096, kBitWords = 4 * kOwnThreads;        // tokens that a CTA keeps in shared memory; words of its bit map
 constexpr int kPiece = 16;                              // tokens in a piece; rows of more go by pieces
 constexpr int kSlice = 1024, kSumThreads = 256, kSumWarps = kSumThreads / 32;   // columns of a piece's CTA
+// Tokens that one kernel alone does: 197 of 1003 x 768 fp32 3.9 us, 6.8 where some words are frequent, 10.4 where all
+// are the same; two kernels with 513 7.8, 15.9, 20.3.  With 512 it would be 4.2, 12.4, and 29.7 (one CTA's sums).
+constexpr int kFew = 256;
 constexpr int kMostRows = 16;                           // rows of a group of lanes in the second kernel
 
 struct Place {              // of a token in the order of all; row < 0: its row is not summed by pieces
@@ -94,6 +98,7 @@ struct GradArgs : EmbedGradArgs {
     int each;               // rows of a group of them, a power of two, up to kMostRows and `lanes`
     int slices, group;      // of kSlice columns; threads per token there
     int64_t pieces;         // CTAs of the second kernel that sum them
+    bool few;               // and there is no first one
     int *list;              // tokens, for CTAs that have more than kList
     Place *order;
     int2 *rows;             // of the table: how many tokens a row has, and where they are in that order; a single one itself
@@ -103,7 +108,7 @@ struct GradArgs : EmbedGradArgs {
 };
 
 // Sums over the CTA in the order of threads: those before this one, and all.
-__device__ __forceinline__ int scan(int x, int *scratch, int &all)
+template <int THREADS> __device__ __forceinline__ int scan(int x, int *scratch, int &all)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int s = x;
@@ -118,7 +123,7 @@ __device__ __forceinline__ int scan(int x, int *scratch, int &all)
     int before = 0;
     all = 0;
 #pragma unroll
-    for (int w = 0; w < kOwnThreads / 32; ++w) {
+    for (int w = 0; w < THREADS / 32; ++w) {
         const int y = scratch[w];
         if (w < warp) before += y;
         all += y;
@@ -258,7 +263,7 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kOwnThreads, 
         int sum = 0, all;
         if (first < rows)
             for (int i = first; i < min(first + kEach, rows); ++i) sum += sh.counts[i];
-        int at = scan(sum, sh.scratch, all);
+        int at = scan<kOwnThreads>(sum, sh.scratch, all);
         if (first < rows)
             for (int i = first; i < min(first + kEach, rows); ++i) {
                 const int count = sh.counts[i];
@@ -322,7 +327,7 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kOwnThreads, 
             constexpr int kEach = kBitWords / kOwnThreads;
             int bits = 0, all;
             for (int i = 0; i < kEach; ++i) bits += __popc(sh.bits[threadIdx.x * kEach + i]);
-            int at = done + scan(bits, sh.scratch, all);
+            int at = done + scan<kOwnThreads>(bits, sh.scratch, all);
             done += all;
             for (int i = 0; i < kEach; ++i)
                 for (uint32_t m = sh.bits[threadIdx.x * kEach + i]; m; m &= m - 1, ++at) {
@@ -464,34 +469,18 @@ template <int TYPE, int GRAD, bool ALIGNED> __device__ __forceinline__ void sum_
     }
 }
 
-template <int TYPE, int GRAD, bool ALIGNED>
-__global__ void __launch_bounds__(kSumThreads, ALIGNED ? 4 : 3) novak_embedding_grad_kernel(GradArgs a)
+// A group of lanes' rows from row0 on, eight columns a lane: zeros, and sums of up to kPiece tokens.  A lane knows
+// of a row what `mine` says (see GradArgs::rows).
+template <int TYPE, int GRAD, bool ALIGNED, typename Token>
+__device__ __forceinline__ void write_rows(const GradArgs &a, int2 mine, int lanes, int64_t row0, int64_t col, const Token &token)
 {
     using G = typename Elem<GRAD>::T;
     using T = typename Elem<TYPE>::T;
-    start();
-    // Pieces first, since they take long, but by turns with the others: they wait more than they move.
-    const int64_t pieces = a.pieces * a.slices, rest = gridDim.x - pieces, both = 2 * min(pieces, rest), b = blockIdx.x;
-    const bool is_piece = b < both ? b % 2 == 0 : pieces > rest;
-    const int64_t index = b < both ? b / 2 : b - both / 2;
-    if (is_piece) {
-        const int piece = static_cast<int>(index / a.slices);
-        sum_piece<TYPE, GRAD, ALIGNED>(a, piece, static_cast<int>(index - static_cast<int64_t>(piece) * a.slices));
-        return;
-    }
-    const int lanes = ALIGNED ? a.lanes : 32, lane = threadIdx.x % lanes;
-    const int64_t item = index * kSumWarps + threadIdx.x / 32;
-    const int64_t block = item <= INT_MAX && a.steps <= INT_MAX ? static_cast<unsigned>(item) / static_cast<unsigned>(a.steps) : item / a.steps;
-    const int64_t col = ((item - block * a.steps) * lanes + lane) * 8;
+    const int lane = threadIdx.x % lanes, shift = threadIdx.x % 32 / lanes * lanes;
     const int n = static_cast<int>(max(min(a.cols - col, static_cast<int64_t>(8)), static_cast<int64_t>(0)));
-    const int64_t row0 = (block * (32 / lanes) + threadIdx.x % 32 / lanes) * a.each;
     const void *begin = a.dout.ptr, *end = end_of(static_cast<const T *>(a.dout.ptr), a.dout.stride, a.tokens, a.cols);
     const void *out_begin = a.dtable.ptr, *out_end = end_of(static_cast<const G *>(a.dtable.ptr), a.dtable.stride, a.vocab, a.cols);
-    // a lane knows of a row; rows beyond the table are nobody's
-    int2 mine = make_int2(0, INT_MAX);
-    if (lane < a.each && row0 + lane < a.vocab) mine = a.rows[row0 + lane];
-    const unsigned group = lanes == 32 ? ~0u : ((1u << lanes) - 1) << (threadIdx.x % 32 / lanes * lanes);
-    const int shift = threadIdx.x % 32 / lanes * lanes;
+    const unsigned group = lanes == 32 ? ~0u : ((1u << lanes) - 1) << shift;
     G *p = static_cast<G *>(a.dtable.ptr) + row0 * a.dtable.stride + col;
     unsigned none = (__ballot_sync(0xffffffffu, mine.y == 0 && lane < a.each) & group) >> shift;
     unsigned one = (__ballot_sync(0xffffffffu, mine.y == 1) & group) >> shift;
@@ -536,8 +525,143 @@ __global__ void __launch_bounds__(kSumThreads, ALIGNED ? 4 : 3) novak_embedding_
         const int first = __shfl_sync(0xffffffffu, mine.x, i, lanes), count = __shfl_sync(0xffffffffu, mine.y, i, lanes);
         if (some == 0 || (ALIGNED && n == 0)) continue;
         F2 sum[4];
-        sum_tokens<TYPE, ALIGNED>(a, [&](int k) { return a.order[first + k].token; }, count, col, n, begin, end, sum);
+        sum_tokens<TYPE, ALIGNED>(a, [&](int k) { return token(first + k); }, count, col, n, begin, end, sum);
         put_sum<GRAD, ALIGNED>(a, p + i * a.dtable.stride, n, sum, out_begin, out_end);
+    }
+}
+
+template <int TYPE, int GRAD, bool ALIGNED>
+__global__ void __launch_bounds__(kSumThreads, ALIGNED ? 4 : 3) novak_embedding_grad_kernel(GradArgs a)
+{
+    start();
+    // Pieces first, since they take long, but by turns with the others: they wait more than they move.
+    const int64_t pieces = a.pieces * a.slices, rest = gridDim.x - pieces, both = 2 * min(pieces, rest), b = blockIdx.x;
+    const bool is_piece = b < both ? b % 2 == 0 : pieces > rest;
+    const int64_t index = b < both ? b / 2 : b - both / 2;
+    if (is_piece) {
+        const int piece = static_cast<int>(index / a.slices);
+        sum_piece<TYPE, GRAD, ALIGNED>(a, piece, static_cast<int>(index - static_cast<int64_t>(piece) * a.slices));
+        return;
+    }
+    const int lanes = ALIGNED ? a.lanes : 32, lane = threadIdx.x % lanes;
+    const int64_t item = index * kSumWarps + threadIdx.x / 32;
+    const int64_t block = item <= INT_MAX && a.steps <= INT_MAX ? static_cast<unsigned>(item) / static_cast<unsigned>(a.steps) : item / a.steps;
+    const int64_t col = ((item - block * a.steps) * lanes + lane) * 8;
+    const int64_t row0 = (block * (32 / lanes) + threadIdx.x % 32 / lanes) * a.each;
+    // rows beyond the table are nobody's
+    int2 mine = make_int2(0, INT_MAX);
+    if (lane < a.each && row0 + lane < a.vocab) mine = a.rows[row0 + lane];
+    write_rows<TYPE, GRAD, ALIGNED>(a, mine, lanes, row0, col, [&](int k) { return a.order[k].token; });
+}
+
+// Few tokens: one kernel, each of whose CTAs looks through all ids for those of its rows, kSumWarps times a warp's.
+template <int TYPE, int GRAD, bool ALIGNED>
+__global__ void __launch_bounds__(kSumThreads, ALIGNED ? 4 : 3) novak_embedding_few_grad_kernel(GradArgs a)
+{
+    using G = typename Elem<GRAD>::T;
+    using T = typename Elem<TYPE>::T;
+    __shared__ int found[kFew], order[kFew], scratch[kSumWarps];
+    __shared__ __align__(16) uint16_t found_row[kFew + 8];
+    __shared__ uint16_t many[kFew / kPiece];
+    __shared__ int2 rows[kSumThreads];
+    __shared__ int n_many;
+    __shared__ __align__(16) float part[kSumThreads * 8];
+    const int lanes = ALIGNED ? a.lanes : 32, lane = threadIdx.x % lanes, group = threadIdx.x / lanes;
+    const int64_t block = blockIdx.x / a.steps, col = ((blockIdx.x - block * a.steps) * lanes + lane) * 8;
+    const int height = kSumThreads / lanes * a.each;        // (at most kSumThreads)
+    const int64_t row0 = block * height;
+    if (threadIdx.x == 0) n_many = 0;
+    start();
+
+    // the tokens whose rows are here, in order
+    constexpr int kEach = kFew / kSumThreads;
+    int64_t id[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int t = threadIdx.x * kEach + i;
+        id[i] = t < a.tokens ? id_at(a.ids, a.id_type, t) : -1;
+    }
+    const int64_t here = min(static_cast<int64_t>(height), a.vocab - row0);
+    int count = 0, n;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        id[i] = id[i] >= row0 && id[i] - row0 < here ? id[i] - row0 : -1;
+        count += id[i] >= 0;
+    }
+    int at = scan<kSumThreads>(count, scratch, n);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+        if (id[i] >= 0) {
+            found[at] = threadIdx.x * kEach + i;
+            found_row[at++] = static_cast<uint16_t>(id[i]);
+        }
+    if (threadIdx.x < 8) found_row[n + threadIdx.x] = 0xffff;
+    rows[threadIdx.x] = make_int2(0, 0);
+    __syncthreads();
+    // each token: how many of its row there are, and how many of them before it
+    int before[kEach];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const int i = k * kSumThreads + threadIdx.x;
+        if (i >= n) continue;
+        const int row = found_row[i];
+        int of_row = 0, place = 0;
+        for (int j = 0; j < n; j += 8) {
+            const uint4 w = *reinterpret_cast<const uint4 *>(found_row + j);
+            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int m = 0; m < 8; ++m) {
+                const bool same = static_cast<int>(u[m / 2] >> m % 2 * 16 & 0xffffu) == row;
+                of_row += same;
+                place += same && j + m < i;
+            }
+        }
+        before[k] = place;
+        if (place == 0) rows[row].y = of_row;
+    }
+    __syncthreads();
+    count = rows[threadIdx.x].y;
+    int all;
+    at = scan<kSumThreads>(count, scratch, all);
+    if (count > kPiece) many[atomicAdd(&n_many, 1)] = static_cast<uint16_t>(threadIdx.x);
+    rows[threadIdx.x].x = at;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const int i = k * kSumThreads + threadIdx.x;
+        if (i < n) order[rows[found_row[i]].x + before[k]] = found[i];
+    }
+    __syncthreads();
+    if (count == 1) rows[threadIdx.x].x = order[at];
+    __syncthreads();
+    int2 mine = make_int2(0, INT_MAX);
+    if (lane < a.each && group * a.each + lane < here) mine = rows[group * a.each + lane];
+    write_rows<TYPE, GRAD, ALIGNED>(a, mine, lanes, row0 + group * a.each, col, [&](int k) { return order[k]; });
+
+    // rows of more: every group of lanes its share of the tokens, then the groups in order
+    const int n_columns = static_cast<int>(max(min(a.cols - col, static_cast<int64_t>(8)), static_cast<int64_t>(0)));
+    const int groups = kSumThreads / lanes;
+    for (int m = 0; m < n_many; ++m) {
+        const int row = many[m], share = (rows[row].y + groups - 1) / groups, first = min(group * share, rows[row].y);
+        F2 sum[4];
+        const int *tokens = order + rows[row].x + first;
+        sum_tokens<TYPE, ALIGNED>(a, [&](int k) { return tokens[k]; }, min(share, rows[row].y - first), col, n_columns, a.dout.ptr,
+                                  end_of(static_cast<const T *>(a.dout.ptr), a.dout.stride, a.tokens, a.cols), sum);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<float2 *>(part + threadIdx.x * 8 + 2 * i) = make_float2(sum[i].lo(), sum[i].hi());
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] = F2(0.0f);
+            for (int k = 0; k < groups; ++k) {
+                const float *p = part + (k * lanes + lane) * 8;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[i] = sum[i] + F2(p[2 * i], p[2 * i + 1]);
+            }
+            G *p = static_cast<G *>(a.dtable.ptr) + (row0 + row) * a.dtable.stride + col;
+            put_sum<GRAD, ALIGNED>(a, p, n_columns, sum, a.dtable.ptr, end_of(static_cast<const G *>(a.dtable.ptr), a.dtable.stride, a.vocab, a.cols));
+        }
     }
 }
 
@@ -576,6 +700,10 @@ GradLayout layout_of(int64_t tokens, int64_t vocab, int64_t cols)
 template <int TYPE, int GRAD, bool ALIGNED> cudaError_t launch_grad(const GradArgs &g, cudaStream_t stream)
 {
     const int lanes = ALIGNED ? g.lanes : 32, rows = g.each * (32 / lanes);
+    if (g.few) {
+        const int64_t blocks = (g.vocab + rows * kSumWarps - 1) / (rows * kSumWarps);
+        return launch(novak_embedding_few_grad_kernel<TYPE, GRAD, ALIGNED>, dim3(static_cast<unsigned>(blocks * g.steps)), kSumThreads, 0, stream, g);
+    }
     const int64_t items = (g.vocab + rows - 1) / rows * g.steps, ctas = g.pieces * g.slices + (items + kSumWarps - 1) / kSumWarps;
     return launch(novak_embedding_grad_kernel<TYPE, GRAD, ALIGNED>, dim3(static_cast<unsigned>(ctas)), kSumThreads, 0, stream, g);
 }
@@ -607,8 +735,8 @@ cudaError_t launch_embedding_grad(const EmbedGradArgs &a, cudaStream_t stream)
 {
     const GradLayout l = layout_of(a.tokens, a.vocab, a.cols);
     uint8_t *base = static_cast<uint8_t *>(a.work);
-    GradArgs g{a, 8, 0, 0, 0, 1, l.slices, 0, l.pieces, reinterpret_cast<int *>(base + l.list), reinterpret_cast<Place *>(base + l.order),
-               reinterpret_cast<int2 *>(base + l.rows), reinterpret_cast<int *>(base + l.counts), reinterpret_cast<int *>(base + l.valid),
+    GradArgs g{a, 8, 0, 0, 0, 1, l.slices, 0, l.pieces, a.tokens <= kFew, reinterpret_cast<int *>(base + l.list),
+               reinterpret_cast<Place *>(base + l.order), reinterpret_cast<int2 *>(base + l.rows), reinterpret_cast<int *>(base + l.counts), reinterpret_cast<int *>(base + l.valid),
                reinterpret_cast<float *>(base + l.partial)};
     // Neighbouring rows that are short together go to one CTA, as long as there are blocks for all CTAs.
     while ((a.cols << g.fold) < 256 && (a.vocab >> (g.fold + g.shift)) >= 2) ++g.fold;
@@ -616,7 +744,7 @@ cudaError_t launch_embedding_grad(const EmbedGradArgs &a, cudaStream_t stream)
     const int64_t ctas = std::min<int64_t>(int64_t(1) << g.shift, (a.vocab + (int64_t(1) << g.fold) - 1) >> g.fold);
     static std::atomic<uint64_t> asked{0};
     cudaError_t e = ask_shared_memory(novak_embedding_order_kernel, sizeof(OwnShared), asked);
-    if (e == cudaSuccess)
+    if (e == cudaSuccess && !g.few)
         e = launch(novak_embedding_order_kernel, dim3(static_cast<unsigned>((ctas + kCluster - 1) / kCluster * kCluster)), kOwnThreads, sizeof(OwnShared), stream, g);
     if (e != cudaSuccess) return e;
 

@@ -864,13 +864,14 @@ int novak_orthogonal_step(float *const *d_theta, const void *const *d_g, int gra
                           const double *coefficients, int steps, double eps, void *d_work,
                           size_t work_bytes, void *stream);
 
-/* The kernel of the two calls above has warps that wait for one another's copies,
- * products and tiles.  Each wait is bounded (two seconds); where one runs out, which
- * is a fault of this library or of the device, every output of the call (X, or theta)
- * is filled with NaNs, and the count of novak_ops_gave_up goes up.  Test hook for
- * that: novak_orthogonalize with a limit of wait_ns on each wait (0: the usual one)
- * and with the end of tile number `withheld` never announced (of tiles counted from 0
- * in the order in which they are begun; -1: none). */
+/* Matrices beyond 64 rows and columns (small ones are worked on by themselves) go to a
+ * kernel whose warps wait for one another's copies, products and tiles.  Each wait is
+ * bounded (two seconds); where one runs out, which is a fault of this library or of the
+ * device, every output of that kernel (X, or theta) is filled with NaNs, and the count of
+ * novak_ops_gave_up goes up.  Test hook for that: novak_orthogonalize with a limit of
+ * wait_ns on each wait (0: the usual one) and with the end of tile number `withheld` never
+ * announced (of tiles counted from 0 in the order in which they are begun, small matrices
+ * among them; -1: none, and small ones by themselves). */
 int novak_selftest_orthogonalize_wait(const void *const *d_g, const int64_t *g_stride, int type,
                                       void *const *d_out, const int64_t *out_stride,
                                       const int64_t *rows, const int64_t *cols, int n,

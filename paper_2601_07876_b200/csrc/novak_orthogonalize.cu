@@ -125,6 +125,12 @@ __device__ __forceinline__ uint32_t pack_half(float a, float b)
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 __device__ __forceinline__ float2 unpack_half(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
+__device__ __forceinline__ F2 halves(uint32_t w)
+{
+    const float2 p = unpack_half(w);
+    return F2(p.x, p.y);
+}
+__device__ __forceinline__ uint32_t pack_half(F2 x) { return pack_half(x.lo(), x.hi()); }
 
 // Of n items the last one whose first(item) is not above `at`, by the whole warp.
 template <typename First> __device__ __forceinline__ int item_of(int n, int at, const First &first)
@@ -284,6 +290,15 @@ __global__ void __launch_bounds__(kThreads) novak_orthogonalize_norm_kernel(cons
     if (threadIdx.x == 0) w.partial[chunk] = sum;
 }
 
+// What G is multiplied by for X in units of 2^-12, in two factors: its norm's reciprocal may be beyond fp32.  (A norm that is
+// not finite makes everything of the matrix NaN.)
+__device__ __forceinline__ void scale_of(double squares, float eps, float &tiny, float &rest)
+{
+    const double norm = sqrt(squares), scale = !(norm < INFINITY) ? NAN : norm > 0.0 ? kScaleX / fmax(norm, static_cast<double>(eps)) : 0.0;
+    tiny = scale > 1e36 ? 0x1p100f : 1.0f;
+    rest = static_cast<float>(scale / tiny);
+}
+
 // X's two parts in units of 2^-12.
 template <int TYPE>
 __global__ void __launch_bounds__(kThreads) novak_orthogonalize_start_kernel(Work w, int n, int64_t units, Momentum mo, float eps)
@@ -299,10 +314,8 @@ __global__ void __launch_bounds__(kThreads) novak_orthogonalize_start_kernel(Wor
         double norm = 0.0;
         for (int i = threadIdx.x; i < it.chunks; i += kThreads) norm += w.partial[it.chunk + i];
         __syncthreads();
-        norm = sqrt(sum_of_all(norm, scratch));
-        // (a norm that is not finite makes everything of the matrix NaN)
-        const double scale = !(norm < INFINITY) ? NAN : norm > 0.0 ? kScaleX / fmax(norm, static_cast<double>(eps)) : 0.0;
-        const float tiny = scale > 1e36 ? 0x1p100f : 1.0f, rest = static_cast<float>(scale / tiny);     // (its reciprocal is beyond fp32)
+        float tiny, rest;
+        scale_of(sum_of_all(norm, scratch), eps, tiny, rest);
         const int panels = (it.cols + kPanel - 1) / kPanel;
         for (const int last = min(end, it.unit + it.units); unit < last; ++unit) {
             const int panel = (unit - it.unit) % panels;
@@ -323,6 +336,429 @@ __global__ void __launch_bounds__(kThreads) novak_orthogonalize_start_kernel(Wor
             });
         }
     }
+}
+
+// ---- small matrices ------------------------------------------------------------------
+// Of up to 64 rows (or columns), or 128 and no more than 512 of the others: one launch, in which a matrix stays in
+// the shared memory of one CTA, or of a cluster of eight, each of which has an eighth of the longer dimension.  The
+// fifteen products that depend on one another take the kernel below 7 us each, most of it the way through memory; here
+// there are two barriers of the cluster a step (64 x 64: 19 us, by the kernel below 90; 33 x 770: 26 and 120; 128 x 256: 56
+// and 106; 200 of 64 x 768: 427 and 469.  Longer ones of 128 are quicker alone too, 128 x 1024: 76 and 127, but 64 of them
+// take 383 and 241, and what a matrix comes to is not to depend on its company).  The products, 128 x 128 at
+// the most, are ordinary matrix instructions on what lies there: tensor memory would add its copies to that chain.
+// A CTA sums its part of X X^T; each adds up an eighth of all parts and hands that to everybody; B and B X
+// everybody forms alone.  Numbers are as above, and the last step takes X's second part along.
+constexpr int kSmallSide = 128, kSmallThreads = 512, kSmallCluster = 8, kAlone = 128;
+constexpr int kSmallMost = 232448 - 1024;   // shared memory
+
+struct SmallItem {
+    const void *g;
+    void *out;
+    float *m;
+    int64_t g_stride, out_stride;
+    int rows, cols;
+    float step;
+};
+template <int N> struct SmallItems {
+    SmallItem item[N];
+};
+struct SmallArgs {
+    float coefficients[kMostSteps][3];
+    int steps, theta;
+    float decay, eps;
+    Momentum mo;
+};
+
+// Shared memory of a CTA with `width` columns (of X, or of its transpose where it is tall).
+struct SmallLayout {
+    int side, blocks, width;        // padded to 16 (from 64 on 32); of 16 x 16, on and above the diagonal; padded to 16
+    int pitch, x_pitch;             // in elements: an odd number of 16 bytes
+    int sum, a, hi, lo, diag, bytes;        // part at 0
+    __host__ __device__ SmallLayout(int s, int w)
+    {
+        side = pad_to(s, s <= 64 ? 16 : 32);
+        blocks = side / 16 * (side / 16 + 1) / 2;
+        width = pad_to(w, 16);
+        pitch = side + 8;
+        x_pitch = width + 8;
+        const int square = side * pitch * 2, part = blocks * 1024;
+        sum = part;                             // (later B's place)
+        a = sum + (part > square ? part : square);
+        hi = a + square;
+        lo = hi + side * x_pitch * 2;
+        diag = lo + side * x_pitch * 2;
+        bytes = diag + 2 * side * 4;
+    }
+};
+
+__device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void load_matrices_across(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+// d (16 x 8) += a (16 x 16) b (16 x 8)
+__device__ __forceinline__ void multiply(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float4 load_four_at(uint32_t addr)
+{
+    float4 x;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(addr) : "memory");
+    return x;
+}
+__device__ __forceinline__ void store_four_at(uint32_t addr, float4 x)
+{
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(x.x), "f"(x.y), "f"(x.z), "f"(x.w) : "memory");
+}
+__device__ __forceinline__ void store_double_at(uint32_t addr, double x)
+{
+    asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(addr), "d"(x) : "memory");
+}
+
+// The CTA's elements of G, several per thread on their way at a time: f(row of X, column of the slice, row, column, element).
+// X is G, or its transpose where that is tall.
+template <int TYPE, typename F>
+__device__ __forceinline__ void for_slice(const SmallItem &it, const Momentum &mo, int first, int width, bool advance, const F &f)
+{
+    using T = typename Elem<TYPE>::T;
+    constexpr int kAhead = 8;
+    const bool tall = it.rows > it.cols;
+    const unsigned side = min(it.rows, it.cols), inner = tall ? side : width, total = side * width;
+    const unsigned inverse = inner > 1 ? 0xffffffffu / inner + 1 : 0;       // (total x inner is below 2^32)
+    const T *g = static_cast<const T *>(it.g);
+    for (unsigned e0 = threadIdx.x; e0 < total; e0 += kAhead * kSmallThreads) {
+        T raw[kAhead];
+        float m[kAhead];
+        int64_t row[kAhead];
+        unsigned at[kAhead], in[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const unsigned e = e0 + k * kSmallThreads, outer = inner > 1 ? __umulhi(e, inverse) : e;
+            in[k] = e - outer * inner;
+            at[k] = outer;
+            const int64_t r = row[k] = tall ? first + static_cast<int>(outer) : static_cast<int>(outer), c = tall ? in[k] : first + in[k];
+            raw[k] = T(0.0f);
+            m[k] = 0.0f;
+            if (e < total) {
+                raw[k] = g[r * it.g_stride + c];
+                if (mo.on) m[k] = it.m[r * it.cols + c];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (e0 + k * kSmallThreads >= total) continue;
+            const int64_t c = tall ? in[k] : first + in[k];
+            float v = to_float(raw[k]);
+            if (mo.on) {
+                if (advance) it.m[row[k] * it.cols + c] = m[k] = fmaf(mo.momentum, m[k], v);
+                v = mo.nesterov ? fmaf(mo.momentum, m[k], v) : m[k];
+            }
+            f(tall ? in[k] : at[k], tall ? at[k] : in[k], row[k], c, v);
+        }
+    }
+}
+
+template <int TYPE, int N, int C>
+__global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kSmallThreads, 1)
+novak_orthogonalize_small_kernel(const __grid_constant__ SmallItems<N> from, const __grid_constant__ SmallArgs args)
+{
+    extern __shared__ __align__(16) uint8_t raw_shared[];
+    __shared__ double scratch[kSmallThreads / 32], norms[C];
+    constexpr int kWarps = kSmallThreads / 32;
+    const SmallItem &it = from.item[blockIdx.x / C];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, rank = C > 1 ? static_cast<int>(cluster_rank()) : 0;
+    const int s = min(it.rows, it.cols), l = max(it.rows, it.cols);
+    const SmallLayout at(s, (l + C - 1) / C);
+    const int first = rank * at.width, width = max(min(l - first, at.width), 0), ks = at.side / 16;
+    float *const part = reinterpret_cast<float *>(raw_shared), *const sum = reinterpret_cast<float *>(raw_shared + (C > 1 ? at.sum : 0));
+    __half *const gram = reinterpret_cast<__half *>(raw_shared + at.a), *const poly = reinterpret_cast<__half *>(raw_shared + at.sum);
+    __half *const hi = reinterpret_cast<__half *>(raw_shared + at.hi), *const lo = reinterpret_cast<__half *>(raw_shared + at.lo);
+    float *const diag_a = reinterpret_cast<float *>(raw_shared + at.diag), *const diag_b = diag_a + at.side;
+    const uint32_t gram0 = smem_addr(gram), poly0 = smem_addr(poly), hi0 = smem_addr(hi);
+    const auto everybody = [] {
+        if constexpr (C > 1) cluster_sync();
+        else __syncthreads();
+    };
+    // hi and lo lie one behind the other
+    for (int i = threadIdx.x; i < 2 * at.side * at.x_pitch * 2 / 16; i += kSmallThreads) reinterpret_cast<uint4 *>(hi)[i] = make_uint4(0, 0, 0, 0);
+    everybody();
+    start();
+
+    // ---- |G|, in 64 bits (a square in fp32 would be lost below 1e-19), and X
+    double squares = 0.0;
+    for_slice<TYPE>(it, args.mo, first, width, true, [&](int, int, int64_t, int64_t, float v) { squares = fma(static_cast<double>(v), static_cast<double>(v), squares); });
+    for (int d = 16; d > 0; d >>= 1) squares += __shfl_xor_sync(0xffffffffu, squares, d);
+    if (lane == 0) scratch[warp] = squares;
+    __syncthreads();
+    if (threadIdx.x < C) {
+        squares = 0.0;
+        for (int i = 0; i < kWarps; ++i) squares += scratch[i];
+        if constexpr (C > 1) store_double_at(at_rank(smem_addr(&norms[rank]), threadIdx.x), squares);
+        else norms[0] = squares;
+    }
+    everybody();
+    double norm = 0.0;
+    for (int i = 0; i < C; ++i) norm += norms[i];
+    float tiny, rest;
+    scale_of(norm, args.eps, tiny, rest);
+    for_slice<TYPE>(it, args.mo, first, width, false, [&](int i, int j, int64_t, int64_t, float v) {
+        const float x = v * tiny * rest;
+        const __half h = __float2half_rn(x);
+        hi[i * at.x_pitch + j] = h;
+        lo[i * at.x_pitch + j] = __float2half_rn((x - __half2float(h)) * kScaleLow);
+    });
+    __syncthreads();
+
+    // where a lane's row of a 16 x 16 block begins, for one whose rows are the operand's, and for one whose columns are
+    const int row_a = lane % 16, col_a = lane / 16 * 8, row_b = lane / 16 * 8 + lane % 8, col_b = lane / 8 % 2 * 8;
+    const auto block_of = [&](int b, int &bi, int &bj) {
+        bi = 0;
+        for (; b >= ks - bi; ++bi) b -= ks - bi;
+        bj = bi + b;
+    };
+    // the products of rows of a matrix with rows (16 x 16 of them)
+    const auto rows_by_rows = [&](uint32_t from, int pitch, int bi, int bj, int steps, float (&d)[2][4]) {
+        const uint32_t a0 = from + ((bi * 16 + row_a) * pitch + col_a) * 2, b0 = from + ((bj * 16 + row_b) * pitch + col_b) * 2;
+        const auto some = [&](auto count, int k) {
+            constexpr int kCount = decltype(count)::value;
+            uint32_t x[kCount][4], y[kCount][4];
+#pragma unroll
+            for (int i = 0; i < kCount; ++i) {
+                load_matrices(x[i], a0 + (k + i) * 32);
+                load_matrices(y[i], b0 + (k + i) * 32);
+            }
+#pragma unroll
+            for (int i = 0; i < kCount; ++i) {
+                multiply(d[0], x[i], y[i][0], y[i][1]);
+                multiply(d[1], x[i], y[i][2], y[i][3]);
+            }
+        };
+        int k = 0;
+        for (; k + 4 <= steps; k += 4) some(std::integral_constant<int, 4>(), k);
+        for (; k < steps; ++k) some(std::integral_constant<int, 1>(), k);
+    };
+    for (int step = 0; step < args.steps; ++step) {
+        const float ca = args.coefficients[step][0], cb = args.coefficients[step][1], cc = args.coefficients[step][2];
+        const bool full = step + 2 >= args.steps;
+        // this CTA's part of X X^T
+        for (int b = warp; b < at.blocks; b += kWarps) {
+            int bi, bj;
+            block_of(b, bi, bj);
+            float d[2][4] = {};
+            rows_by_rows(hi0, at.x_pitch, bi, bj, at.width / 16, d);
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    *reinterpret_cast<float2 *>(part + b * 256 + (lane / 4 + 8 * h) * 16 + n * 8 + lane % 4 * 2) = make_float2(d[n][2 * h], d[n][2 * h + 1]);
+        }
+        everybody();
+        if constexpr (C > 1) {
+            const int all = at.blocks * 64, each = (all + C - 1) / C;
+            for (int i = rank * each + threadIdx.x; i < min((rank + 1) * each, all); i += kSmallThreads) {
+                const uint32_t mine = smem_addr(part) + i * 16, there = smem_addr(sum) + i * 16;
+                float4 x[C];
+#pragma unroll
+                for (int r = 0; r < C; ++r) x[r] = load_four_at(at_rank(mine, r));
+#pragma unroll
+                for (int r = 1; r < C; ++r) x[0] = make_float4(x[0].x + x[r].x, x[0].y + x[r].y, x[0].z + x[r].z, x[0].w + x[r].w);
+#pragma unroll
+                for (int r = 0; r < C; ++r) store_four_at(at_rank(there, r), x[0]);
+            }
+            cluster_sync();
+        }
+        for (int b = warp; b < at.blocks; b += kWarps) {
+            int bi, bj;
+            block_of(b, bi, bj);
+            float there[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) there[k] = sum[b * 256 + k * 32 + lane];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int i = bi * 16 + 2 * k + lane / 16, j = bj * 16 + lane % 16;
+                const float x = there[k] * (1.0f / (kScaleX * kScaleX));
+                const __half h = i == j ? __half(0.0f) : __float2half_rn(x * kScaleA);
+                if (i == j) diag_a[i] = x;
+                gram[i * at.pitch + j] = h;
+                if (bi != bj) gram[j * at.pitch + i] = h;
+            }
+        }
+        __syncthreads();
+        // B = b A + c A^2
+        for (int b = warp; b < at.blocks; b += kWarps) {
+            int bi, bj;
+            block_of(b, bi, bj);
+            float d[2][4] = {};
+            rows_by_rows(gram0, at.pitch, bi, bj, ks, d);
+            constexpr float kSquare = 1.0f / (kScaleA * kScaleA);
+            // two neighbouring columns at a time
+            float2 of_a[2][2], di;
+            float dj[2][2];
+            di = make_float2(diag_a[bi * 16 + lane / 4], diag_a[bi * 16 + lane / 4 + 8]);
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const int j = bj * 16 + n * 8 + lane % 4 * 2;
+                dj[n][0] = diag_a[j];
+                dj[n][1] = diag_a[j + 1];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) of_a[n][h] = unpack_half(*reinterpret_cast<const uint32_t *>(gram + (bi * 16 + lane / 4 + 8 * h) * at.pitch + j));
+            }
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int i = bi * 16 + lane / 4 + 8 * h, j = bj * 16 + n * 8 + lane % 4 * 2;
+                    const float mine = h ? di.y : di.x;
+                    float v[2];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        v[k] = fmaf(d[n][2 * h + k], kScaleB * cc * kSquare,
+                                    fmaf(cc, mine + dj[n][k], cb) * (kScaleB / kScaleA) * (k ? of_a[n][h].y : of_a[n][h].x));
+                        if (i == j + k) {
+                            diag_b[i] = fmaf(cc, fmaf(d[n][2 * h + k], kSquare, mine * mine), cb * mine);
+                            v[k] = 0.0f;
+                        }
+                    }
+                    const uint32_t w = pack_half(v[0], v[1]);
+                    *reinterpret_cast<uint32_t *>(poly + i * at.pitch + j) = w;
+                    if (bi != bj) {
+                        poly[j * at.pitch + i] = __ushort_as_half(static_cast<uint16_t>(w));
+                        poly[(j + 1) * at.pitch + i] = __ushort_as_half(static_cast<uint16_t>(w >> 16));
+                    }
+                }
+        }
+        __syncthreads();
+        // X <- a X + B X, 16 columns by one warp, or where there are few by several, each some of the rows: all of them have
+        // the columns in registers before the first one writes
+        const auto update = [&](auto rows) {
+            constexpr int kRows = decltype(rows)::value;            // times 16
+            const int columns = at.width / 16, helpers = max(min(kWarps / columns, kRows), 1), together = kWarps / helpers;
+            for (int c0 = 0; c0 < columns; c0 += together) {
+                const int c = c0 + warp / helpers;
+                const bool mine = warp / helpers < together && c < columns;
+                uint32_t x[kRows][4];
+                const uint32_t x0 = hi0 + ((lane / 8 % 2 * 8 + lane % 8) * at.x_pitch + c * 16 + lane / 16 * 8) * 2;
+#pragma unroll
+                for (int k = 0; k < kRows; ++k)
+                    if (mine) load_matrices_across(x[k], x0 + k * 32 * at.x_pitch);
+                if (helpers > 1) __syncthreads();
+                else __syncwarp();
+                for (int m = warp % helpers; mine && m < kRows; m += helpers) {
+                    float d[2][4] = {};
+                    const uint32_t a0 = poly0 + ((m * 16 + row_a) * at.pitch + col_a) * 2;
+                    uint32_t *p[2][2], *q[2][2], of_hi[2][2], of_lo[2][2];
+                    float db[2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int i = m * 16 + lane / 4 + 8 * h;
+                        db[h] = diag_b[i];
+#pragma unroll
+                        for (int n = 0; n < 2; ++n) {
+                            const int e = i * at.x_pitch + c * 16 + n * 8 + lane % 4 * 2;
+                            p[n][h] = reinterpret_cast<uint32_t *>(hi + e);
+                            q[n][h] = reinterpret_cast<uint32_t *>(lo + e);
+                            of_hi[n][h] = *p[n][h];
+                            of_lo[n][h] = *q[n][h];
+                        }
+                    }
+                    uint32_t y[kRows][4];
+#pragma unroll
+                    for (int k = 0; k < kRows; ++k) load_matrices(y[k], a0 + k * 32);
+#pragma unroll
+                    for (int k = 0; k < kRows; ++k) {
+                        multiply(d[0], y[k], x[k][0], x[k][1]);
+                        multiply(d[1], y[k], x[k][2], x[k][3]);
+                    }
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const F2 first_part = halves(of_hi[n][h]), both = fma2(halves(of_lo[n][h]), F2(1.0f / kScaleLow), first_part);
+                            const F2 v = fma2(F2(d[n][2 * h], d[n][2 * h + 1]), F2(1.0f / kScaleB), fma2(F2(db[h]), full ? both : first_part, both * F2(ca)));
+                            const uint32_t w = pack_half(v);
+                            *p[n][h] = w;
+                            *q[n][h] = pack_half(fma2(halves(w), F2(-1.0f), v) * F2(kScaleLow));
+                        }
+                }
+            }
+        };
+        switch (ks) {
+        case 1: update(std::integral_constant<int, 1>()); break;
+        case 2: update(std::integral_constant<int, 2>()); break;
+        case 3: update(std::integral_constant<int, 3>()); break;
+        case 4: update(std::integral_constant<int, 4>()); break;
+        case 6: update(std::integral_constant<int, 6>()); break;
+        default: update(std::integral_constant<int, 8>()); break;
+        }
+        __syncthreads();
+    }
+
+    // ---- the result
+    const bool tall = it.rows > it.cols;
+    const unsigned inner = tall ? s : width, total = static_cast<unsigned>(s) * width;
+    const unsigned inverse = inner > 1 ? 0xffffffffu / inner + 1 : 0;
+#pragma unroll 4
+    for (unsigned e = threadIdx.x; e < total; e += kSmallThreads) {
+        const unsigned outer = inner > 1 ? __umulhi(e, inverse) : e, in = e - outer * inner, i = tall ? in : outer, j = tall ? outer : in;
+        const int64_t row = tall ? first + j : i, col = tall ? i : first + j;
+        const float x = fmaf(__half2float(lo[i * at.x_pitch + j]), 1.0f / kScaleLow, __half2float(hi[i * at.x_pitch + j])) * (1.0f / kScaleX);
+        if (args.theta) {
+            float *p = static_cast<float *>(it.out) + row * it.out_stride + col;
+            *p = fmaf(-it.step, x, args.decay * *p);
+        } else {
+            static_cast<__nv_bfloat16 *>(it.out)[row * it.out_stride + col] = __float2bfloat16_rn(x);
+        }
+    }
+}
+
+// CTAs of a matrix; 0: it is not small.
+int small_ctas(int64_t rows, int64_t cols)
+{
+    const int64_t s = std::min(rows, cols), l = std::max(rows, cols);
+    if (s > kSmallSide || (s > 64 && l > 512)) return 0;
+    const auto fits = [&](int ctas) { return SmallLayout(static_cast<int>(s), static_cast<int>((l + ctas - 1) / ctas)).bytes <= kSmallMost; };
+    // (64 x 128 alone 24 us; with eight CTAs each has a sixteenth of the work and two barriers a step: 256 columns 24 us)
+    return l <= kAlone && fits(1) ? 1 : fits(kSmallCluster) ? kSmallCluster : 0;
+}
+
+template <int TYPE, int N, int C>
+cudaError_t send_small(const SmallItem *items, int count, const SmallArgs &args, int bytes, cudaStream_t stream)
+{
+    static std::atomic<uint64_t> asked{0};
+    const cudaError_t e = ask_shared_memory(novak_orthogonalize_small_kernel<TYPE, N, C>, kSmallMost, asked);
+    if (e != cudaSuccess) return e;
+    SmallItems<N> from{};
+    std::copy_n(items, count, from.item);
+    return launch(novak_orthogonalize_small_kernel<TYPE, N, C>, dim3(static_cast<unsigned>(count * C)), kSmallThreads, bytes, stream, from, args);
+}
+
+// All small ones of a call.
+template <int TYPE, int C> cudaError_t launch_small(const OrthArgs &a, const SmallArgs &args, cudaStream_t stream)
+{
+    SmallItem items[kMostItems];
+    int count = 0, bytes = 0;
+    const auto send = [&] {
+        const cudaError_t e = count <= 8 ? send_small<TYPE, 8, C>(items, count, args, bytes, stream) : send_small<TYPE, kMostItems, C>(items, count, args, bytes, stream);
+        count = bytes = 0;
+        return e;
+    };
+    for (int i = 0; i < a.n; ++i) {
+        if (a.rows[i] == 0 || a.cols[i] == 0 || small_ctas(a.rows[i], a.cols[i]) != C) continue;
+        const int s = static_cast<int>(std::min(a.rows[i], a.cols[i])), l = static_cast<int>(std::max(a.rows[i], a.cols[i]));
+        bytes = std::max(bytes, SmallLayout(s, (l + C - 1) / C).bytes);
+        items[count++] = SmallItem{a.g[i], a.out ? a.out[i] : a.theta[i], a.m ? a.m[i] : nullptr, a.g_stride ? a.g_stride[i] : a.cols[i],
+                                   a.out ? a.out_stride[i] : a.cols[i], static_cast<int>(a.rows[i]), static_cast<int>(a.cols[i]),
+                                   a.step ? static_cast<float>(a.step[i]) : 0.0f};
+        if (count < kMostItems) continue;
+        const cudaError_t e = send();
+        if (e != cudaSuccess) return e;
+    }
+    return count > 0 ? send() : cudaSuccess;
 }
 
 // ---- the products on the tensor cores --------------------------------------------------
@@ -651,13 +1087,6 @@ __device__ __forceinline__ void step_theta(const Item &it, float decay, uint32_t
     }
     __syncwarp();
 }
-
-__device__ __forceinline__ F2 halves(uint32_t w)
-{
-    const float2 p = unpack_half(w);
-    return F2(p.x, p.y);
-}
-__device__ __forceinline__ uint32_t pack_half(F2 x) { return pack_half(x.lo(), x.hi()); }
 
 // A warp that takes tiles out: its place in shared memory and the barrier of what comes there.
 struct Taking {
@@ -1127,12 +1556,29 @@ cudaError_t orthogonalize_gave_up(unsigned *count, cudaStream_t stream)
 
 cudaError_t launch_orthogonalize(const OrthArgs &a, cudaStream_t stream)
 {
+    const Momentum mo{a.m != nullptr, a.nesterov, a.momentum};
+    const bool f32 = a.type == NOVAK_TYPE_F32, all = a.withheld >= 0;
+    SmallArgs small{};
+    for (int k = 0; k < a.steps; ++k)
+        for (int i = 0; i < 3; ++i) small.coefficients[k][i] = a.coefficients[k][i];
+    small.steps = a.steps;
+    small.theta = a.out == nullptr;
+    small.decay = a.decay;
+    small.eps = static_cast<float>(a.eps);
+    small.mo = mo;
+    cudaError_t e = cudaSuccess;
+    if (!all) e = f32 ? launch_small<0, 1>(a, small, stream) : launch_small<1, 1>(a, small, stream);
+    if (!all && e == cudaSuccess) e = f32 ? launch_small<0, kSmallCluster>(a, small, stream) : launch_small<1, kSmallCluster>(a, small, stream);
+    if (e != cudaSuccess) return e;
+    // the others (in a test of the waits, which small ones do without: all)
+    const auto here = [&](int i) { return a.rows[i] > 0 && a.cols[i] > 0 && (all || small_ctas(a.rows[i], a.cols[i]) == 0); };
+
     Layout l;
     Item it{};
     int n = 0, first_of[3] = {};
     int64_t tiles[3][2] = {};           // of a step, by product: of 256 columns, and of 128
     for (int i = 0; i < a.n; ++i)
-        if (a.rows[i] > 0 && a.cols[i] > 0) {
+        if (here(i)) {
             place(l, a.rows[i], a.cols[i], it);
             for (int what = 0; what < 3; ++what)
                 for (int narrow = 0; narrow < 2; ++narrow) tiles[what][narrow] += tiles_of(it, what, narrow ? 128 : 256);
@@ -1156,8 +1602,6 @@ cudaError_t launch_orthogonalize(const OrthArgs &a, cudaStream_t stream)
         p.first[what + 1] = p.first[what] + static_cast<int>(tiles[what][narrow]);
         most = std::max(most, tiles[what][narrow]);
     }
-    const Momentum mo{a.m != nullptr, a.nesterov, a.momentum};
-    const bool f32 = a.type == NOVAK_TYPE_F32;
     Layout again;
     HostItems<kMostItems> items{};
     int first = 0, count = 0;
@@ -1174,9 +1618,8 @@ cudaError_t launch_orthogonalize(const OrthArgs &a, cudaStream_t stream)
         count = 0;
         return e;
     };
-    cudaError_t e = cudaSuccess;
     for (int i = 0; i < a.n && e == cudaSuccess; ++i) {
-        if (a.rows[i] == 0 || a.cols[i] == 0) continue;
+        if (!here(i)) continue;
         place(again, a.rows[i], a.cols[i], it);
         it.g = a.g[i];
         it.out = a.out ? a.out[i] : a.theta[i];

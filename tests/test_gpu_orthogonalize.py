@@ -144,6 +144,40 @@ def test_more_matrices_than_go_with_one_launch(ops):
         assert torch.equal(ops.orthogonalize(ms[i]), got[i])
 
 
+# one CTA and eight, the longest that stay in shared memory and the first that do not, shares that are empty or a part
+SMALL = [(64, 128), (128, 64), (64, 129), (17, 1000), (1000, 17), (64, 6000), (6000, 48), (1, 28000), (30000, 2), (65, 66), (97, 512), (512, 128),
+         (128, 128), (128, 513), (600, 65), (8, 130), (50, 200)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", SMALL)
+def test_small_ones(ops, rows, cols, dtype):
+    g = spectrum(rows, cols, "low rank", rows + cols, dtype)
+    check(ops.orthogonalize(g), g)
+
+
+@pytest.mark.parametrize("rows,cols", [(60, 500), (500, 60), (100, 100), (33, 12), (300, 400)])
+def test_small_steps_are_the_large_ones_step(ops, rows, cols):
+    """theta by the step, m, and X, of one gradient in rows that are apart."""
+    torch.manual_seed(3)
+    g, theta, m = (torch.randn(rows, cols, device="cuda") for _ in range(3))
+    want_m = 0.9 * m.double() + g.double()
+    u = (g.double() + 0.9 * want_m).cpu()
+    before = theta.double().cpu()
+    ops.orthogonal_step([theta], [g], [m], [0.5], momentum=0.9, decay=0.75)
+    R.assert_within(m, want_m.cpu(), 2 * R.U * (want_m.abs().cpu() + 1), "m")
+    x = S.orthogonalized(u)
+    off = float((theta.cpu().double() - (0.75 * before - 0.5 * x)).norm())
+    assert off <= 0.5 * S.orthogonal_tolerance(rows, cols) * float(x.norm()) + 4 * R.U * float(before.norm())
+
+
+def test_more_large_matrices_than_go_with_one_launch(ops):
+    ms = [spectrum(130 + i % 3, 140, "gauss", i) for i in range(230)]
+    got = ops.orthogonalize(ms)
+    for i in (0, 7, 8, 199, 200, 229):
+        assert torch.equal(ops.orthogonalize(ms[i]), got[i])
+
+
 def test_batches_strides_and_nothing(ops):
     base = spectrum(6 * 40, 70, "gauss", 1).view(6, 40, 70)
     batch = base[1::2, 3:37, 5:60]                      # three matrices, rows and matrices apart, bases unaligned

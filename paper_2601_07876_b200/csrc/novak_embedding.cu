@@ -1,8 +1,8 @@
 // Token embedding, out[t] = scale table[ids[t]], and its gradient, the sum of dout's rows
 // over the tokens of an id.
 //
-// Looking up is reading and writing rows; what bounds it is HBM, and for few tokens latency, so
-// that long rows are cut among warps.
+// Looking up is reading and writing rows; what bounds it is HBM (16384 of 50000 x 768 fp32 to bf16: 8.7 us,
+// 7.8 at the copy rate), and for few tokens latency, so that long rows are cut among warps.
 //
 // The gradient of a whole table is mostly zeros to be written; the rest is to bring each id's
 // tokens together in an order that goes by their places alone.  Two kernels.
@@ -14,7 +14,8 @@
 // The second one is one pass over dout and one over the table.  Warps have a few rows of 256 columns:
 // zeros where there are no tokens, the sum of up to 16.  The order of all tokens is cut into pieces of 16
 // besides, and those of longer rows have a CTA each; the last one of a row's pieces to be done adds
-// their sums up in order.  So no word is too frequent.
+// their sums up in order.  So no word is too frequent.  (16384 tokens, some words frequent, 50000 x 768 bf16 to fp32:
+// 58 us, 13 of them the first kernel's; 27.7 at the copy rate.)
 // Of few tokens there is one kernel: every CTA looks through the ids for those of its own rows.
 // (Zeros and sums in the first kernel, once it knows its rows: 58 to 77 us for 16384 tokens of 50000 x 768,
 // since its shared memory leaves room for too few warps to hide what loads wait for.)

@@ -5,7 +5,9 @@
 // What is normalised is h as it is stored, so that the backward pass, which may form xhat from
 // it, sees what the forward pass saw.  Rows are spread as the layer norm's are: read once,
 // held in registers, the next one on its way; one sum over the row's threads where the layer
-// norm has two.
+// norm has two.  Bound by HBM where there are rows enough: 12608 x 768 bf16 with a residual, the 8-bit
+// form left and unpacked, 21.4 us (18.0 at the copy rate); back from that form with a stream's gradient 19.6
+// (10.5: few rows per warp, and a second kernel of 5 us for dw's sums); back from h, 4099 x 4096 fp32, 53.5 (41.6).
 #include <algorithm>
 
 #include "novak_norm.cuh"

@@ -855,7 +855,7 @@ int novak_orthogonalize(const void *const *d_g, const int64_t *g_stride, int typ
  *     m <- momentum m + g,  G = g + momentum m (nesterov not 0) or m,
  *     theta <- decay theta - step[i] X,
  * X that of novak_orthogonalize for G (not rounded to bf16).  theta and m: dense fp32,
- * g: dense, of grad_type.  step: HOST array (learning rate times the matrix's scale);
+ * g: dense, of grad_type; no theta or m may overlap another or a g.  step: HOST array (learning rate times the matrix's scale);
  * momentum in [0, 1), decay and step finite.  The other arguments and d_work as in
  * novak_orthogonalize. */
 int novak_orthogonal_step(float *const *d_theta, const void *const *d_g, int grad_type,

@@ -7,6 +7,9 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <memory>
+#include <new>
+#include <utility>
 
 #include "novak_ops.h"
 
@@ -466,6 +469,27 @@ int novak_orthogonal_step(float *const *d_theta, const void *const *d_g, int gra
         CHECK(check_mat("theta", mat(d_theta[i], cols[i]), NOVAK_TYPE_F32, rows[i], cols[i]));
         CHECK(check_mat("m", mat(d_m[i], cols[i]), NOVAK_TYPE_F32, rows[i], cols[i]));
         CHECK(check_mat("g", mat(d_g[i], cols[i]), grad_type, rows[i], cols[i]));
+    }
+    // what is written belongs to one matrix alone
+    using Range = std::pair<uintptr_t, uintptr_t>;
+    const std::unique_ptr<Range[]> written(new (std::nothrow) Range[2 * static_cast<size_t>(n) + 1]);
+    if (!written) return refuse("no memory on the host");
+    Range *end = written.get();
+    const auto range = [&](const void *p, int i, size_t size) {
+        const uintptr_t first = reinterpret_cast<uintptr_t>(p);
+        return Range(first, first + static_cast<size_t>(rows[i]) * static_cast<size_t>(cols[i]) * size);
+    };
+    for (int i = 0; i < n; ++i)
+        if (rows[i] > 0 && cols[i] > 0)
+            for (const float *p : {d_theta[i], d_m[i]}) *end++ = range(p, i, sizeof(float));
+    std::sort(written.get(), end);
+    for (const Range *r = written.get() + 1; r < end; ++r)
+        if (r->first < r[-1].second) return refuse("theta and m overlap one another");
+    for (int i = 0; i < n; ++i) {
+        if (rows[i] == 0 || cols[i] == 0) continue;
+        const Range g = range(d_g[i], i, grad_type == NOVAK_TYPE_F32 ? 4 : 2);
+        const Range *behind = std::lower_bound(written.get(), end, Range(g.second, 0));     // the first that begins behind g
+        if (behind != written.get() && behind[-1].second > g.first) return refuse("g overlaps theta or m");
     }
     OrthArgs a{d_g, nullptr, grad_type, nullptr, nullptr, rows, cols, n, {}, 0, eps, d_theta, d_m,
                static_cast<float>(momentum), nesterov != 0, step, static_cast<float>(decay), d_work};

@@ -108,6 +108,21 @@ def test_nothing_to_do_needs_no_buffers(lib):
                 bytes=0) == OK
 
 
+@pytest.mark.parametrize("theta,g,m,refused", [
+    ((0, 1000), (2000, 3000), (4000, 5000), None), ((0, 1000), (2000, 2000), (4000, 5000), None),
+    ((0, 144), (2000, 3000), (288, 5000), None), ((0, 1000), (856, 1144), (4000, 5000), None),
+    ((0, 0), (2000, 3000), (4000, 5000), "theta and m"), ((0, 1000), (2000, 3000), (4000, 4000), "theta and m"),
+    ((0, 1000), (2000, 3000), (4000, 1000), "theta and m"), ((0, 140), (2000, 3000), (4000, 5000), "theta and m"),
+    ((0, 1000), (1000, 3000), (4000, 5000), "g overlaps"), ((0, 1000), (2000, 5000), (4000, 5000), "g overlaps"),
+    ((0, 1000), (860, 3000), (4000, 5000), "g overlaps"), ((0, 1000), (2000, 5140), (4000, 5000), "g overlaps")])
+def test_a_step_has_its_matrices_for_itself(lib, theta, g, m, refused):
+    """Two of 4 x 9, 144 bytes each."""
+    at = [pointers(*(P + x for x in p)) for p in (theta, g, m)]
+    assert call(lib, "novak_orthogonal_step", theta=at[0], g=at[1], m=at[2], rows=sizes(4, 4), cols=sizes(9, 9), n=2,
+                step=doubles(1.0, 1.0), bytes=0) == EINVAL
+    assert (refused or "work") in lib.novak_ops_error().decode()
+
+
 def test_no_workspace_is_asked_for_what_will_be_refused(lib):
     ask = lib.novak_orthogonalize_bytes
     assert ask(sizes(4), sizes(9), 1) > 0 and ask(sizes(4), sizes((1 << 16) + 1), 1) == 0 and ask(sizes(-4), sizes(9), 1) == 0

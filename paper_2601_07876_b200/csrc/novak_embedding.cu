@@ -86,6 +86,7 @@ constexpr int kSlice = 1024, kSumThreads = 256, kSumWarps = kSumThreads / 32;   
 // Tokens that one kernel alone does: 197 of 1003 x 768 fp32 3.9 us, 6.8 where some words are frequent, 10.4 where all
 // are the same; two kernels with 513 7.8, 15.9, 20.3.  With 512 it would be 4.2, 12.4, and 29.7 (one CTA's sums).
 constexpr int kFew = 256;
+__host__ __device__ constexpr int64_t padded(int64_t cols) { return (cols + 3) / 4 * 4; }      // a piece's sums, in 16 bytes
 constexpr int kMostRows = 16;                           // rows of a group of lanes in the second kernel
 
 struct Place {              // of a token in the order of all; row < 0: its row is not summed by pieces
@@ -105,7 +106,7 @@ struct GradArgs : EmbedGradArgs {
     int2 *rows;             // of the table: how many tokens a row has, and where they are in that order; a single one itself
     int *counts;            // [piece][slice]: sums that are done, where a row begins in that piece
     int *valid;             // tokens in all
-    float *partial;         // [piece][2][cols]: of a row that began before, of one that begins here
+    float *partial;         // [piece][2][cols, padded]: of a row that began before, of one that begins here
 };
 
 // Sums over the CTA in the order of threads: those before this one, and all.
@@ -439,7 +440,7 @@ template <int TYPE, int GRAD, bool ALIGNED> __device__ __forceinline__ void sum_
             float x = 0.0f;
             for (int i = 0; i < subs; ++i) x += part[i * group * 8 + c];
             const int64_t out = static_cast<int64_t>(slice) * kSlice + c;
-            if (out < a.cols) a.partial[(2 * static_cast<int64_t>(piece) + kind) * a.cols + out] = x;
+            if (out < a.cols) a.partial[(2 * static_cast<int64_t>(piece) + kind) * padded(a.cols) + out] = x;
         }
         // the last of the row's pieces to be done adds all of them up
         const int head = seg.start / kPiece, pieces = (seg.start + seg.count - 1) / kPiece - head + 1;
@@ -449,14 +450,28 @@ template <int TYPE, int GRAD, bool ALIGNED> __device__ __forceinline__ void sum_
         __syncthreads();
         if (!last) continue;
         __threadfence();
-        for (int c = threadIdx.x; c < group * 8; c += kSumThreads) {
-            const int64_t out = static_cast<int64_t>(slice) * kSlice + c;
-            if (out >= a.cols) continue;
-            const float *p = a.partial + (2 * static_cast<int64_t>(head) + 1) * a.cols + out;
-            float x = __ldcg(p);
-#pragma unroll 16
-            for (int i = 1; i < pieces; ++i) x += __ldcg(p + (2 * static_cast<int64_t>(i) - 1) * a.cols);    // (of a row that began before)
-            part[c] = x;
+        // four columns a thread, a share of the pieces each, then the shares in order (16384 tokens of one row of 768: 181 us;
+        // a column a thread and all of the pieces, 241; some words frequent: 46 and 51)
+        const int quads = group * 2, shares = kSumThreads / quads, mine = threadIdx.x / quads, quad = threadIdx.x % quads;
+        const int each = (pieces + shares - 1) / shares, end_at = min((mine + 1) * each, pieces);
+        const int64_t out = static_cast<int64_t>(slice) * kSlice + quad * 4;
+        float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (out < a.cols) {
+            const float *p = a.partial + 2 * static_cast<int64_t>(head) * padded(a.cols) + out;
+#pragma unroll 8
+            for (int i = mine * each; i < end_at; ++i) {        // (behind the first one: of a row that began before)
+                const float4 y = __ldcg(reinterpret_cast<const float4 *>(p + (i == 0 ? 1 : 2 * static_cast<int64_t>(i)) * padded(a.cols)));
+                x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+            }
+        }
+        *reinterpret_cast<float4 *>(part + threadIdx.x * 4) = x;
+        __syncthreads();
+        if (mine == 0) {
+            for (int i = 1; i < shares; ++i) {
+                const float4 y = *reinterpret_cast<const float4 *>(part + (i * quads + quad) * 4);
+                x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+            }
+            *reinterpret_cast<float4 *>(part + quad * 4) = x;
         }
         __syncthreads();
         if (static_cast<int>(threadIdx.x) < group) {
@@ -694,7 +709,7 @@ GradLayout layout_of(int64_t tokens, int64_t vocab, int64_t cols)
     l.counts = l.rows + round_up(vocab * sizeof(int2));
     l.valid = l.counts + round_up(l.pieces * l.slices * sizeof(int));
     l.partial = l.valid + round_up(sizeof(int));
-    l.bytes = l.partial + round_up(2 * l.pieces * cols * sizeof(float));
+    l.bytes = l.partial + round_up(2 * l.pieces * padded(cols) * sizeof(float));
     return l;
 }
 

@@ -2,7 +2,8 @@
 //     X = G / max(|G|, eps), then for each triple (a, b, c): A = X X^T,
 //     X <- a X + (b A + c A^2) X  (X^T X and products from the right where X is tall).
 //
-// Numbers.  The products' operands are fp16 with 11 bits, scaled by powers of two (X by 2^12, A
+// Numbers.  Where matrices are small every operand is two fp16 parts and every product three (see there); what
+// follows is of the larger ones.  The products' operands are fp16 with 11 bits, scaled by powers of two (X by 2^12, A
 // by 2^11, B = b A + c A^2 by 2^12: the spectra that the caller's polynomials allow keep them
 // below 2^16, and what falls out at the other end is 2^-24 of the scale); sums are fp32.  A step
 // multiplies small singular values by a = 3.4 and large ones by about 1, so that what X is
@@ -342,12 +343,15 @@ __global__ void __launch_bounds__(kThreads) novak_orthogonalize_start_kernel(Wor
 // Of up to 64 rows (or columns), or 128 and no more than 512 of the others: one launch, in which a matrix stays in
 // the shared memory of one CTA, or of a cluster of eight, each of which has an eighth of the longer dimension.  The
 // fifteen products that depend on one another take the kernel below 7 us each, most of it the way through memory; here
-// there are two barriers of the cluster a step (64 x 64: 19 us, by the kernel below 90; 33 x 770: 26 and 120; 128 x 256: 56
-// and 106; 200 of 64 x 768: 427 and 469.  Longer ones of 128 are quicker alone too, 128 x 1024: 76 and 127, but 64 of them
-// take 383 and 241, and what a matrix comes to is not to depend on its company).  The products, 128 x 128 at
-// the most, are ordinary matrix instructions on what lies there: tensor memory would add its copies to that chain.
+// there are two barriers of the cluster a step (64 x 64: 26 us, by the kernel below 90; 33 x 770: 33 and 120; 128 x 256: 76
+// and 106).  The products, 128 x 128 at the most, are ordinary matrix instructions on what lies there: tensor memory would
+// add its copies to that chain.
+// With so few elements there are few roundings to average: with operands of 11 bits the result of a 2 x 2 matrix would
+// be up to 1e-2 off.  So X, A and B are two fp16 parts each, first and second, and products are three: first by first, and first
+// by second both ways, in sums of their own.  That is what fp32 arithmetic would give (3e-6 on most spectra, 6e-5
+// where G is of rank one), and takes 30 % longer (33 x 770: 25 us; 128 x 256, whose registers do not suffice, 55).
 // A CTA sums its part of X X^T; each adds up an eighth of all parts and hands that to everybody; B and B X
-// everybody forms alone.  Numbers are as above, and the last step takes X's second part along.
+// everybody forms alone.  Else numbers are as above.
 constexpr int kSmallSide = 128, kSmallThreads = 512, kSmallCluster = 8, kAlone = 128;
 constexpr int kSmallMost = 232448 - 1024;   // shared memory
 
@@ -373,7 +377,7 @@ struct SmallArgs {
 struct SmallLayout {
     int side, blocks, width;        // padded to 16 (from 64 on 32); of 16 x 16, on and above the diagonal; padded to 16
     int pitch, x_pitch;             // in elements: an odd number of 16 bytes
-    int sum, a, hi, lo, diag, bytes;        // part at 0
+    int sum, a, a_low, hi, lo, diag, bytes; // part at 0, later B's second part
     __host__ __device__ SmallLayout(int s, int w)
     {
         side = pad_to(s, s <= 64 ? 16 : 32);
@@ -382,9 +386,10 @@ struct SmallLayout {
         pitch = side + 8;
         x_pitch = width + 8;
         const int square = side * pitch * 2, part = blocks * 1024;
-        sum = part;                             // (later B's place)
-        a = sum + (part > square ? part : square);
-        hi = a + square;
+        sum = part;                             // (later B's first part; 16 x 16 in fp32 take more than rows of as many in fp16)
+        a = sum + part;
+        a_low = a + square;
+        hi = a_low + square;
         lo = hi + side * x_pitch * 2;
         diag = lo + side * x_pitch * 2;
         bytes = diag + 2 * side * 4;
@@ -476,10 +481,12 @@ novak_orthogonalize_small_kernel(const __grid_constant__ SmallItems<N> from, con
     const SmallLayout at(s, (l + C - 1) / C);
     const int first = rank * at.width, width = max(min(l - first, at.width), 0), ks = at.side / 16;
     float *const part = reinterpret_cast<float *>(raw_shared), *const sum = reinterpret_cast<float *>(raw_shared + (C > 1 ? at.sum : 0));
-    __half *const gram = reinterpret_cast<__half *>(raw_shared + at.a), *const poly = reinterpret_cast<__half *>(raw_shared + at.sum);
+    __half *const gram = reinterpret_cast<__half *>(raw_shared + at.a), *const gram_low = reinterpret_cast<__half *>(raw_shared + at.a_low);
+    __half *const poly = reinterpret_cast<__half *>(raw_shared + at.sum), *const poly_low = reinterpret_cast<__half *>(raw_shared);
     __half *const hi = reinterpret_cast<__half *>(raw_shared + at.hi), *const lo = reinterpret_cast<__half *>(raw_shared + at.lo);
     float *const diag_a = reinterpret_cast<float *>(raw_shared + at.diag), *const diag_b = diag_a + at.side;
-    const uint32_t gram0 = smem_addr(gram), poly0 = smem_addr(poly), hi0 = smem_addr(hi);
+    const uint32_t gram0 = smem_addr(gram), poly0 = smem_addr(poly), hi0 = smem_addr(hi), gram_low0 = smem_addr(gram_low),
+                   poly_low0 = smem_addr(poly_low), lo0 = smem_addr(lo);
     const auto everybody = [] {
         if constexpr (C > 1) cluster_sync();
         else __syncthreads();
@@ -521,36 +528,45 @@ novak_orthogonalize_small_kernel(const __grid_constant__ SmallItems<N> from, con
         for (; b >= ks - bi; ++bi) b -= ks - bi;
         bj = bi + b;
     };
-    // the products of rows of a matrix with rows (16 x 16 of them)
-    const auto rows_by_rows = [&](uint32_t from, int pitch, int bi, int bj, int steps, float (&d)[2][4]) {
-        const uint32_t a0 = from + ((bi * 16 + row_a) * pitch + col_a) * 2, b0 = from + ((bj * 16 + row_b) * pitch + col_b) * 2;
+    // the products of rows of a matrix with rows (16 x 16 of them), `low` where its second part is
+    const auto rows_by_rows = [&](uint32_t from, uint32_t low, int pitch, int bi, int bj, int steps, float (&d)[2][4]) {
+        const uint32_t a0 = ((bi * 16 + row_a) * pitch + col_a) * 2, b0 = ((bj * 16 + row_b) * pitch + col_b) * 2;
+        float e[2][4] = {};
         const auto some = [&](auto count, int k) {
             constexpr int kCount = decltype(count)::value;
-            uint32_t x[kCount][4], y[kCount][4];
+            uint32_t x[kCount][4], y[kCount][4], x_low[kCount][4], y_low[kCount][4];
 #pragma unroll
             for (int i = 0; i < kCount; ++i) {
-                load_matrices(x[i], a0 + (k + i) * 32);
-                load_matrices(y[i], b0 + (k + i) * 32);
+                load_matrices(x[i], from + a0 + (k + i) * 32);
+                load_matrices(y[i], from + b0 + (k + i) * 32);
+                load_matrices(x_low[i], low + a0 + (k + i) * 32);
+                load_matrices(y_low[i], low + b0 + (k + i) * 32);
             }
 #pragma unroll
-            for (int i = 0; i < kCount; ++i) {
-                multiply(d[0], x[i], y[i][0], y[i][1]);
-                multiply(d[1], x[i], y[i][2], y[i][3]);
-            }
+            for (int i = 0; i < kCount; ++i)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    multiply(d[n], x[i], y[i][2 * n], y[i][2 * n + 1]);
+                    multiply(e[n], x[i], y_low[i][2 * n], y_low[i][2 * n + 1]);
+                    multiply(e[n], x_low[i], y[i][2 * n], y[i][2 * n + 1]);
+                }
         };
         int k = 0;
-        for (; k + 4 <= steps; k += 4) some(std::integral_constant<int, 4>(), k);
-        for (; k < steps; ++k) some(std::integral_constant<int, 1>(), k);
+        for (; k + 2 <= steps; k += 2) some(std::integral_constant<int, 2>(), k);
+        if (k < steps) some(std::integral_constant<int, 1>(), k);
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) d[n][i] = fmaf(e[n][i], 1.0f / kScaleLow, d[n][i]);
     };
     for (int step = 0; step < args.steps; ++step) {
         const float ca = args.coefficients[step][0], cb = args.coefficients[step][1], cc = args.coefficients[step][2];
-        const bool full = step + 2 >= args.steps;
         // this CTA's part of X X^T
         for (int b = warp; b < at.blocks; b += kWarps) {
             int bi, bj;
             block_of(b, bi, bj);
             float d[2][4] = {};
-            rows_by_rows(hi0, at.x_pitch, bi, bj, at.width / 16, d);
+            rows_by_rows(hi0, lo0, at.x_pitch, bi, bj, at.width / 16, d);
 #pragma unroll
             for (int n = 0; n < 2; ++n)
 #pragma unroll
@@ -582,10 +598,15 @@ novak_orthogonalize_small_kernel(const __grid_constant__ SmallItems<N> from, con
             for (int k = 0; k < 8; ++k) {
                 const int i = bi * 16 + 2 * k + lane / 16, j = bj * 16 + lane % 16;
                 const float x = there[k] * (1.0f / (kScaleX * kScaleX));
-                const __half h = i == j ? __half(0.0f) : __float2half_rn(x * kScaleA);
+                const float y = i == j ? 0.0f : x * kScaleA;
+                const __half h = __float2half_rn(y), low = __float2half_rn((y - __half2float(h)) * kScaleLow);
                 if (i == j) diag_a[i] = x;
                 gram[i * at.pitch + j] = h;
-                if (bi != bj) gram[j * at.pitch + i] = h;
+                gram_low[i * at.pitch + j] = low;
+                if (bi != bj) {
+                    gram[j * at.pitch + i] = h;
+                    gram_low[j * at.pitch + i] = low;
+                }
             }
         }
         __syncthreads();
@@ -594,7 +615,7 @@ novak_orthogonalize_small_kernel(const __grid_constant__ SmallItems<N> from, con
             int bi, bj;
             block_of(b, bi, bj);
             float d[2][4] = {};
-            rows_by_rows(gram0, at.pitch, bi, bj, ks, d);
+            rows_by_rows(gram0, gram_low0, at.pitch, bi, bj, ks, d);
             constexpr float kSquare = 1.0f / (kScaleA * kScaleA);
             // two neighbouring columns at a time
             float2 of_a[2][2], di;
@@ -606,7 +627,11 @@ novak_orthogonalize_small_kernel(const __grid_constant__ SmallItems<N> from, con
                 dj[n][0] = diag_a[j];
                 dj[n][1] = diag_a[j + 1];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) of_a[n][h] = unpack_half(*reinterpret_cast<const uint32_t *>(gram + (bi * 16 + lane / 4 + 8 * h) * at.pitch + j));
+                for (int h = 0; h < 2; ++h) {
+                    const int e = (bi * 16 + lane / 4 + 8 * h) * at.pitch + j;
+                    const float2 x = unpack_half(*reinterpret_cast<const uint32_t *>(gram + e)), low = unpack_half(*reinterpret_cast<const uint32_t *>(gram_low + e));
+                    of_a[n][h] = make_float2(fmaf(low.x, 1.0f / kScaleLow, x.x), fmaf(low.y, 1.0f / kScaleLow, x.y));
+                }
             }
 #pragma unroll
             for (int n = 0; n < 2; ++n)
@@ -625,65 +650,105 @@ novak_orthogonalize_small_kernel(const __grid_constant__ SmallItems<N> from, con
                         }
                     }
                     const uint32_t w = pack_half(v[0], v[1]);
-                    *reinterpret_cast<uint32_t *>(poly + i * at.pitch + j) = w;
-                    if (bi != bj) {
-                        poly[j * at.pitch + i] = __ushort_as_half(static_cast<uint16_t>(w));
-                        poly[(j + 1) * at.pitch + i] = __ushort_as_half(static_cast<uint16_t>(w >> 16));
-                    }
+                    const float2 first_part = unpack_half(w);
+                    const uint32_t low = pack_half((v[0] - first_part.x) * kScaleLow, (v[1] - first_part.y) * kScaleLow);
+                    const auto put = [&](__half *to, uint32_t x) {
+                        *reinterpret_cast<uint32_t *>(to + i * at.pitch + j) = x;
+                        if (bi != bj) {
+                            to[j * at.pitch + i] = __ushort_as_half(static_cast<uint16_t>(x));
+                            to[(j + 1) * at.pitch + i] = __ushort_as_half(static_cast<uint16_t>(x >> 16));
+                        }
+                    };
+                    put(poly, w);
+                    put(poly_low, low);
                 }
         }
         __syncthreads();
-        // X <- a X + B X, 16 columns by one warp, or where there are few by several, each some of the rows: all of them have
-        // the columns in registers before the first one writes
+        // X <- a X + B X, 16 columns by one warp, or where there are few by several, each some of the rows: nobody writes before
+        // all of them have the columns in registers, or (more than 64 rows, for which these do not suffice) their results
         const auto update = [&](auto rows) {
             constexpr int kRows = decltype(rows)::value;            // times 16
+            constexpr int kHeld = kRows <= 4 ? kRows : 0, kResults = kRows <= 4 ? 1 : C > 1 ? 2 : 4;
             const int columns = at.width / 16, helpers = max(min(kWarps / columns, kRows), 1), together = kWarps / helpers;
             for (int c0 = 0; c0 < columns; c0 += together) {
                 const int c = c0 + warp / helpers;
                 const bool mine = warp / helpers < together && c < columns;
-                uint32_t x[kRows][4];
-                const uint32_t x0 = hi0 + ((lane / 8 % 2 * 8 + lane % 8) * at.x_pitch + c * 16 + lane / 16 * 8) * 2;
+                uint32_t x[kHeld + 1][4], x_low[kHeld + 1][4], w[kResults][2][2], w_low[kResults][2][2];
+                const uint32_t x0 = ((lane / 8 % 2 * 8 + lane % 8) * at.x_pitch + c * 16 + lane / 16 * 8) * 2;
+                const auto load = [&](int k, int to) {
+                    load_matrices_across(x[to], hi0 + x0 + k * 32 * at.x_pitch);
+                    load_matrices_across(x_low[to], lo0 + x0 + k * 32 * at.x_pitch);
+                };
+                const auto everything_is_read = [&] {
+                    if (helpers > 1) __syncthreads();
+                    else __syncwarp();
+                };
+                const auto place_of = [&](int m, int n, int h) { return (m * 16 + lane / 4 + 8 * h) * at.x_pitch + c * 16 + lane % 4 * 2 + 8 * n; };
+                const auto multiply_rows = [&](int m, uint32_t (&w)[2][2], uint32_t (&w_low)[2][2]) {
+                    float d[2][4] = {}, e[2][4] = {};
+                    const uint32_t a0 = ((m * 16 + row_a) * at.pitch + col_a) * 2;
+                    constexpr int kAhead = kHeld > 0 ? 2 : 1;
 #pragma unroll
-                for (int k = 0; k < kRows; ++k)
-                    if (mine) load_matrices_across(x[k], x0 + k * 32 * at.x_pitch);
-                if (helpers > 1) __syncthreads();
-                else __syncwarp();
-                for (int m = warp % helpers; mine && m < kRows; m += helpers) {
-                    float d[2][4] = {};
-                    const uint32_t a0 = poly0 + ((m * 16 + row_a) * at.pitch + col_a) * 2;
-                    uint32_t *p[2][2], *q[2][2], of_hi[2][2], of_lo[2][2];
-                    float db[2];
+                    for (int k0 = 0; k0 < kRows; k0 += kAhead) {
+                        uint32_t y[kAhead][4], y_low[kAhead][4];
+#pragma unroll
+                        for (int k = k0; k < k0 + kAhead && k < kRows; ++k) {
+                            load_matrices(y[k - k0], poly0 + a0 + k * 32);
+                            load_matrices(y_low[k - k0], poly_low0 + a0 + k * 32);
+                        }
+                        if (kHeld == 0) load(k0, 0);
+#pragma unroll
+                        for (int k = k0; k < k0 + kAhead && k < kRows; ++k)
+#pragma unroll
+                            for (int n = 0; n < 2; ++n) {
+                                const uint32_t (&of_x)[4] = x[kHeld > 0 ? k : 0], (&of_x_low)[4] = x_low[kHeld > 0 ? k : 0];
+                                multiply(d[n], y[k - k0], of_x[2 * n], of_x[2 * n + 1]);
+                                multiply(e[n], y[k - k0], of_x_low[2 * n], of_x_low[2 * n + 1]);
+                                multiply(e[n], y_low[k - k0], of_x[2 * n], of_x[2 * n + 1]);
+                            }
+                    }
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const int i = m * 16 + lane / 4 + 8 * h;
-                        db[h] = diag_b[i];
+                        const float db = diag_b[m * 16 + lane / 4 + 8 * h];
 #pragma unroll
                         for (int n = 0; n < 2; ++n) {
-                            const int e = i * at.x_pitch + c * 16 + n * 8 + lane % 4 * 2;
-                            p[n][h] = reinterpret_cast<uint32_t *>(hi + e);
-                            q[n][h] = reinterpret_cast<uint32_t *>(lo + e);
-                            of_hi[n][h] = *p[n][h];
-                            of_lo[n][h] = *q[n][h];
+                            const uint32_t of_hi = *reinterpret_cast<const uint32_t *>(hi + place_of(m, n, h)),
+                                           of_lo = *reinterpret_cast<const uint32_t *>(lo + place_of(m, n, h));
+                            const F2 both = fma2(halves(of_lo), F2(1.0f / kScaleLow), halves(of_hi));
+                            const F2 sum = fma2(F2(e[n][2 * h], e[n][2 * h + 1]), F2(1.0f / kScaleLow), F2(d[n][2 * h], d[n][2 * h + 1]));
+                            const F2 v = fma2(sum, F2(1.0f / kScaleB), fma2(F2(db), both, both * F2(ca)));
+                            w[n][h] = pack_half(v);
+                            w_low[n][h] = pack_half(fma2(halves(w[n][h]), F2(-1.0f), v) * F2(kScaleLow));
                         }
                     }
-                    uint32_t y[kRows][4];
-#pragma unroll
-                    for (int k = 0; k < kRows; ++k) load_matrices(y[k], a0 + k * 32);
-#pragma unroll
-                    for (int k = 0; k < kRows; ++k) {
-                        multiply(d[0], y[k], x[k][0], x[k][1]);
-                        multiply(d[1], y[k], x[k][2], x[k][3]);
-                    }
+                };
+                const auto put = [&](int m, const uint32_t (&w)[2][2], const uint32_t (&w_low)[2][2]) {
 #pragma unroll
                     for (int n = 0; n < 2; ++n)
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            const F2 first_part = halves(of_hi[n][h]), both = fma2(halves(of_lo[n][h]), F2(1.0f / kScaleLow), first_part);
-                            const F2 v = fma2(F2(d[n][2 * h], d[n][2 * h + 1]), F2(1.0f / kScaleB), fma2(F2(db[h]), full ? both : first_part, both * F2(ca)));
-                            const uint32_t w = pack_half(v);
-                            *p[n][h] = w;
-                            *q[n][h] = pack_half(fma2(halves(w), F2(-1.0f), v) * F2(kScaleLow));
+                            *reinterpret_cast<uint32_t *>(hi + place_of(m, n, h)) = w[n][h];
+                            *reinterpret_cast<uint32_t *>(lo + place_of(m, n, h)) = w_low[n][h];
                         }
+                };
+                if constexpr (kHeld > 0) {
+#pragma unroll
+                    for (int k = 0; k < kRows; ++k)
+                        if (mine) load(k, k);
+                    everything_is_read();
+                    for (int m = warp % helpers; mine && m < kRows; m += helpers) {
+                        multiply_rows(m, w[0], w_low[0]);
+                        put(m, w[0], w_low[0]);
+                    }
+                } else {
+                    // (64 columns: four helpers at least; one CTA alone 128: two)
+#pragma unroll
+                    for (int i = 0; i < kResults; ++i)
+                        if (mine && warp % helpers + i * helpers < kRows) multiply_rows(warp % helpers + i * helpers, w[i], w_low[i]);
+                    everything_is_read();
+#pragma unroll
+                    for (int i = 0; i < kResults; ++i)
+                        if (mine && warp % helpers + i * helpers < kRows) put(warp % helpers + i * helpers, w[i], w_low[i]);
                 }
             }
         };

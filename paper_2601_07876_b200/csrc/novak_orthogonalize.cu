@@ -17,8 +17,9 @@
 //     B X = B' X + diag(B) X.
 // diag(B) multiplies X's first part like B' does, so that the rounding that B's few large
 // directions leave out stays outside; in the last two steps, after which nothing makes it
-// large any more, both parts.  The last step does without the second part.  All spectra tried then
-// end within 1.3e-3 of the exact result (without it in the last two, 2.3e-3; three, 1e-2).
+// large any more, both parts.  The result is then off by 1e-4 (low rank) to 9e-4 (all singular values alike) of its norm
+// for dense gradients (the last step without the second part: 1.1e-3 for rank one, before 3e-4, and 2 % less time), and by
+// up to 1e-2 where a few elements carry the gradient, whose roundings do not average out.
 //
 // Memory.  Every matrix is kept as panels of 64 columns: the rows of a panel, 128 bytes each,
 // lie one behind the other, rows padded to 128 and columns to 64 with zeros.
@@ -1183,10 +1184,9 @@ struct Taking {
             stores_read();
             if (tile.what > 0) {
                 const int y = c / kPanel * tile.pitch + row0;
-                const bool low = tile.what == 2 && tile.step + 1 < a.steps;
-                mbar_expect(bar, low ? 2 * kPartBytes : kPartBytes);
+                mbar_expect(bar, tile.what == 1 ? kPartBytes : 2 * kPartBytes);
                 load_part(place, map, c % kPanel, tile.in + y, bar);
-                if (low) load_part(place + kPartBytes, map, c % kPanel, tile.low + y, bar);
+                if (tile.what == 2) load_part(place + kPartBytes, map, c % kPanel, tile.low + y, bar);
             }
         }
         __syncwarp();
@@ -1301,20 +1301,20 @@ struct Taking {
                             low[8 * k + i] = pack_half(fma2(halves(h[8 * k + i]), F2(-1.0f), v) * F2(kScaleLow));
                         }
                     }
-                    // (the last step does not ask for the second part)
-                    const bool again = tile.step + 2 < a.steps;
                     put_row(place, lane, h);
-                    if (again) put_row(place + kPartBytes, lane, low);
+                    put_row(place + kPartBytes, lane, low);
                     fence_async_shared();
                     __syncwarp();
                     if (lane == 0) {
                         const int y = c0 / kPanel * tile.pitch + row0;
                         store_part(map, c0 % kPanel, tile.out + y, place);
-                        if (again) store_part(map, c0 % kPanel, tile.low + y, place + kPartBytes);
+                        store_part(map, c0 % kPanel, tile.low + y, place + kPartBytes);
                         stores_commit();
                     }
                 } else {
+                    uint32_t low[16];
                     get_row(place, lane, h);
+                    get_row(place + kPartBytes, lane, low);
                     float v[32];
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
@@ -1322,7 +1322,7 @@ struct Taking {
                         tmem_load16(src + 32 * part + 16 * k, raw);
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
-                            (next_x(tile, 16 * k + 2 * i, F2(raw[2 * i], raw[2 * i + 1]), h[8 * k + i], 0u, d_row, ca, full) * F2(1.0f / kScaleX))
+                            (next_x(tile, 16 * k + 2 * i, F2(raw[2 * i], raw[2 * i + 1]), h[8 * k + i], low[8 * k + i], d_row, ca, full) * F2(1.0f / kScaleX))
                                 .get(v[16 * k + 2 * i], v[16 * k + 2 * i + 1]);
                     }
                     __syncwarp();

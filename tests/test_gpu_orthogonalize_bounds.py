@@ -1,5 +1,7 @@
 """How far orthogonalised updates are from the definition in 64 bits: what include/novak.h promises of them, over many
 matrices of every size and of unlike kinds."""
+import math
+
 import pytest
 import torch
 
@@ -57,3 +59,28 @@ def test_small_matrices_are_as_good_as_fp32(ops, rows, cols, count):
         for a, x in zip(g, unrounded(ops, g)):
             want = S.orthogonalized(a)
             assert far(x, want) <= (TWO_PARTS if kind in ("rank one", "low rank") else TWO_PARTS_DENSE), kind
+
+
+# Larger ones: operands of 11 bits.  The plain sum of what roundings can do (orthogonal_tolerance), 11 u a step with u = 2^-12,
+# holds whatever G is; twice their mean square where so many elements carry G that means hold.
+ANY = 5 * 11 * 2.0 ** -12
+
+
+@pytest.mark.parametrize("rows,cols,count", [(65, 600, 8), (129, 129, 20), (200, 300, 20), (300, 200, 20), (256, 300, 20), (700, 257, 5), (768, 768, 3)])
+def test_larger_matrices(ops, rows, cols, count):
+    unlike = [spectrum(rows, cols, "unlike features", 77 + i).abs().pow(3.0) for i in range(count)]      # of a few rows and columns
+    for kind, g in [*kinds(rows, cols, count), ("very unlike features", unlike)]:
+        for a, x in zip(g, unrounded(ops, g)):
+            means = kind not in ("few", "very unlike features")
+            assert far(x, S.orthogonalized(a)) <= (S.orthogonal_tolerance(rows, cols) if means else ANY), kind
+
+
+@pytest.mark.parametrize("rows,cols", [(200, 300), (300, 200), (768, 768)])
+def test_a_gradient_of_low_rank_keeps_its_second_part_to_the_end(ops, rows, cols):
+    """Without it the last step would add 3.4445 u, a times the first part's rounding, in the directions in which B has
+    nothing.  With it there are the products' roundings, 5.6 u / sqrt(3) in the mean of a step where singular values
+    end, which is the last step's alone here; a tenth is allowed on top."""
+    for kind in ("low rank", "rank one"):
+        g = [spectrum(rows, cols, kind, 5 + i) for i in range(4)]
+        for a, x in zip(g, unrounded(ops, g)):
+            assert far(x, S.orthogonalized(a)) <= 1.1 * 5.6 * 2.0 ** -12 / math.sqrt(3), kind

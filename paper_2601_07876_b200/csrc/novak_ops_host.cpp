@@ -147,7 +147,8 @@ int check_scale(double scale)
 }
 
 // How large |x (a + b x^2 + c x^4)| and |b t + c t^2|, t = x^2, get on [0, r]: at the ends, or
-// where the derivatives a + 3 b t + 5 c t^2 and b + 2 c t are zero.
+// where the derivatives a + 3 b t + 5 c t^2 and b + 2 c t are zero.  (Roots from the sum that does not cancel, so that they
+// hold for any ratio of the coefficients, and of coefficients scaled to 1, so that no square overflows.)
 void reach(const double *abc, double r, double &value, double &product)
 {
     const double a = abc[0], b = abc[1], c = abc[2], top = r * r;
@@ -158,16 +159,14 @@ void reach(const double *abc, double r, double &value, double &product)
     };
     value = product = 0.0;
     at(top);
-    if (c != 0.0) {
-        at(-b / (2.0 * c));
-        const double d = 9.0 * b * b - 20.0 * a * c;
-        if (d >= 0.0) {
-            at((-3.0 * b + std::sqrt(d)) / (10.0 * c));
-            at((-3.0 * b - std::sqrt(d)) / (10.0 * c));
-        }
-    } else if (b != 0.0) {
-        at(-a / (3.0 * b));
-    }
+    if (c != 0.0) at(-b / (2.0 * c));
+    const double most = std::max({std::fabs(a), std::fabs(b), std::fabs(c)});
+    if (most == 0.0) return;
+    const double a1 = a / most, b1 = b / most, c1 = c / most, d = 9.0 * b1 * b1 - 20.0 * a1 * c1;
+    if (d < 0.0) return;
+    const double q = -(3.0 * b1 + std::copysign(std::sqrt(d), b1)) / 2.0;
+    if (c1 != 0.0) at(q / (5.0 * c1));
+    if (q != 0.0) at(a1 / q);
 }
 
 // Everything about the matrices but where they lie.

@@ -175,6 +175,13 @@ template <class F, class... A> void enqueue(F f, const char *where, const Tensor
 }
 #define ENQUEUE(f, on, ...) enqueue(api.f, #f, on, __VA_ARGS__)
 
+// A caller's tensor that has been written to: autograd refuses to go back through what was computed from it before, as
+// it does after torch's own operations in place.
+void changed(const Tensor &t)
+{
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 PyObject *wrap(const Tensor &t) { return THPVariable_Wrap(t); }
 PyObject *none_or(const Tensor &t)
 {
@@ -512,6 +519,7 @@ PyObject *embedding_grad(PyObject *const *args)
     const Tensor work = at::empty({static_cast<int64_t>(need)}, dout.options().dtype(at::kByte));
     ENQUEUE(novak_embedding_grad, dout, dout.data_ptr(), r.stride, type, ids.data_ptr(), id_type, scale, out.data_ptr(),
             o.stride, type_of(out, "out"), static_cast<int>(add), work.data_ptr(), need, tokens, vocab, r.cols);
+    if (add) changed(out);
     return wrap(out);
 }
 
@@ -639,6 +647,10 @@ PyObject *orthogonal_step(PyObject *const *args)
                 reinterpret_cast<float *const *>(m.ptr.data()), theta.rows.data(), theta.cols.data(), n, momentum,
                 static_cast<int>(truth(args[4])), step.data(), decay, abc.data(), static_cast<int>(abc.size() / 3), eps,
                 work.data_ptr(), need);
+        for (int64_t i = 0; i < count; ++i) {
+            changed(params.at(i, "a parameter"));
+            changed(momenta.at(i, "a momentum"));
+        }
     }
     Py_RETURN_NONE;
 }

@@ -241,7 +241,8 @@ def orthogonal_step(params, grads, momenta, steps, momentum: float = 0.95, neste
                     coefficients=NEWTON_SCHULZ, eps: float = 1e-7):
     """In place, for each matrix: m <- momentum m + g, G = g + momentum m (``nesterov``) or m,
     theta <- decay theta - step X, X the orthogonalised G.  ``params`` and ``momenta`` are
-    contiguous float32 tensors, none of them twice, ``grads`` of one dtype, ``steps`` one number each."""
+    contiguous float32 tensors, none of them twice, ``grads`` of one dtype, ``steps`` one number each.
+    To autograd they have changed: it refuses to go back through what was computed from them before."""
     _calls.orthogonal_step(params, grads, momenta, momentum, nesterov, steps, decay, _flat(coefficients), eps)
 
 

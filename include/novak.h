@@ -848,8 +848,9 @@ int novak_embedding_grad(const void *d_dout, int64_t dout_stride, int type, cons
  * d_g, g_stride, d_out, out_stride, rows, cols, coefficients: HOST arrays, read before
  * the call returns.  Matrices without rows or columns are passed over.  Up to 2^16
  * rows and columns and 2^14 matrices.  d_work: novak_orthogonalize_bytes(rows, cols, n)
- * bytes, 256-byte aligned (0 where that is too much); its contents need not be
- * anything and are nothing afterwards.  out may not overlap any G. */
+ * bytes, 256-byte aligned (0 where that is too much; small matrices need next to
+ * nothing); its contents need not be anything and are nothing afterwards.  out may not
+ * overlap any G. */
 size_t novak_orthogonalize_bytes(const int64_t *rows, const int64_t *cols, int n);
 int novak_orthogonalize(const void *const *d_g, const int64_t *g_stride, int type, void *const *d_out,
                         const int64_t *out_stride, const int64_t *rows, const int64_t *cols, int n,
@@ -876,7 +877,7 @@ int novak_orthogonal_step(float *const *d_theta, const void *const *d_g, int gra
  * novak_ops_gave_up goes up.  Test hook for that: novak_orthogonalize with a limit of
  * wait_ns on each wait (0: the usual one) and with the end of tile number `withheld` never
  * announced (of tiles counted from 0 in the order in which they are begun, small matrices
- * among them; -1: none, and small ones by themselves). */
+ * among them, in a workspace of the call's own; -1: none, and small ones by themselves). */
 int novak_selftest_orthogonalize_wait(const void *const *d_g, const int64_t *g_stride, int type,
                                       void *const *d_out, const int64_t *out_stride,
                                       const int64_t *rows, const int64_t *cols, int n,

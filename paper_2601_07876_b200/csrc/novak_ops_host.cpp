@@ -449,7 +449,16 @@ int novak_selftest_orthogonalize_wait(const void *const *d_g, const int64_t *g_s
 {
     OrthArgs a{d_g, g_stride, type, d_out, out_stride, rows, cols, n, {}, 0, eps, nullptr, nullptr, 0.0f, false, nullptr,
                0.0f, d_work, withheld, wait_ns};
-    return orthogonalize(a, coefficients, steps, work_bytes, stream, "novak_selftest_orthogonalize_wait");
+    const char *where = "novak_selftest_orthogonalize_wait";
+    if (withheld < 0) return orthogonalize(a, coefficients, steps, work_bytes, stream, where);
+    // small matrices take the large ones' way, for which the caller's workspace has no place
+    CHECK(check_orthogonalize(rows, cols, n, coefficients, steps, eps));
+    const size_t need = orthogonalize_bytes(rows, cols, n, true);
+    if (need == 0) return orthogonalize(a, coefficients, steps, work_bytes, stream, where);
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    CHECK(finish(cudaMallocAsync(&a.work, need, s), where));
+    const int rc = orthogonalize(a, coefficients, steps, need, stream, where), freed = finish(cudaFreeAsync(a.work, s), where);
+    return rc != NOVAK_OK ? rc : freed;
 }
 
 int novak_orthogonal_step(float *const *d_theta, const void *const *d_g, int grad_type, float *const *d_m,

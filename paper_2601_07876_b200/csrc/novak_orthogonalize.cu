@@ -74,6 +74,7 @@ struct Layout {
     size_t diags, items, partial, done, control, bytes;
 };
 
+constexpr size_t kLeastBytes = 4096;        // of matrices that need no workspace: a caller's buffer is never empty, and is checked like any other
 constexpr size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
 __host__ __device__ constexpr int pad_to(int64_t n, int to) { return static_cast<int>((n + to - 1) / to * to); }
 
@@ -1598,19 +1599,24 @@ int tiles_of(const Item &it, int what, int columns)
 
 }  // namespace
 
-size_t orthogonalize_bytes(const int64_t *rows, const int64_t *cols, int n)
+// Matrices that have a place in the workspace: not those that stay in shared memory (in a test of the waits, which those
+// do without: all).
+static bool placed(int64_t rows, int64_t cols, bool all) { return rows > 0 && cols > 0 && (all || small_ctas(rows, cols) == 0); }
+
+size_t orthogonalize_bytes(const int64_t *rows, const int64_t *cols, int n, bool all)
 {
     Layout l;
     Item it{};
     int count = 0;
-    for (int i = 0; i < n; ++i)
-        if (rows[i] > 0 && cols[i] > 0) {
-            if (!place(l, rows[i], cols[i], it)) return 0;
-            ++count;
-        }
-    if (count == 0) return 0;
+    bool any = false;
+    for (int i = 0; i < n; ++i) {
+        any |= rows[i] > 0 && cols[i] > 0;
+        if (!placed(rows[i], cols[i], all)) continue;
+        if (!place(l, rows[i], cols[i], it)) return 0;
+        ++count;
+    }
     finish_layout(l, count);
-    return l.bytes;
+    return count > 0 ? l.bytes : any ? kLeastBytes : 0;
 }
 
 cudaError_t orthogonalize_gave_up(unsigned *count, cudaStream_t stream)
@@ -1635,8 +1641,8 @@ cudaError_t launch_orthogonalize(const OrthArgs &a, cudaStream_t stream)
     if (!all) e = f32 ? launch_small<0, 1>(a, small, stream) : launch_small<1, 1>(a, small, stream);
     if (!all && e == cudaSuccess) e = f32 ? launch_small<0, kSmallCluster>(a, small, stream) : launch_small<1, kSmallCluster>(a, small, stream);
     if (e != cudaSuccess) return e;
-    // the others (in a test of the waits, which small ones do without: all)
-    const auto here = [&](int i) { return a.rows[i] > 0 && a.cols[i] > 0 && (all || small_ctas(a.rows[i], a.cols[i]) == 0); };
+    // the others
+    const auto here = [&](int i) { return placed(a.rows[i], a.cols[i], all); };
 
     Layout l;
     Item it{};

@@ -1,0 +1,25 @@
+"""What the orthogonalised updates ask for as a workspace."""
+import pytest
+
+from paper_2601_07876_b200 import binding as B
+from test_stream_ops_cpu import sizes
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return B.load_library()
+
+
+def ask(lib, *shapes):
+    return lib.novak_orthogonalize_bytes(sizes(*(r for r, _ in shapes)), sizes(*(c for _, c in shapes)), len(shapes))
+
+
+@pytest.mark.parametrize("shape", [(1, 1), (64, 64), (17, 1000), (1000, 17), (1, 28000), (128, 512), (64, 4096)])
+def test_matrices_that_stay_in_shared_memory_need_next_to_nothing(lib, shape):
+    assert 0 < ask(lib, shape) <= 4096 and ask(lib, *[shape] * 5000) == ask(lib, shape)
+    large = [(300, 300), (2048, 100)]
+    assert ask(lib, *large, *[shape] * 100) == ask(lib, *[shape] * 100, *large) == ask(lib, *large) > 4 * 300 * 300
+
+
+def test_nothing_needs_nothing(lib):
+    assert ask(lib) == 0 and ask(lib, (0, 5), (5, 0)) == 0 and ask(lib, (0, 5), (5, 4)) > 0

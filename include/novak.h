@@ -849,8 +849,9 @@ int novak_embedding_grad(const void *d_dout, int64_t dout_stride, int type, cons
  * the call returns.  Matrices without rows or columns are passed over.  Up to 2^16
  * rows and columns and 2^14 matrices.  d_work: novak_orthogonalize_bytes(rows, cols, n)
  * bytes, 256-byte aligned (0 where that is too much; small matrices need next to
- * nothing); its contents need not be anything and are nothing afterwards.  out may not
- * overlap any G. */
+ * nothing, many larger ones go through 1 GiB in groups, and one that is too large for that has
+ * what it needs, 10 bytes an element if square); its contents need not be anything and
+ * are nothing afterwards.  out may not overlap any G. */
 size_t novak_orthogonalize_bytes(const int64_t *rows, const int64_t *cols, int n);
 int novak_orthogonalize(const void *const *d_g, const int64_t *g_stride, int type, void *const *d_out,
                         const int64_t *out_stride, const int64_t *rows, const int64_t *cols, int n,
@@ -873,7 +874,8 @@ int novak_orthogonal_step(float *const *d_theta, const void *const *d_g, int gra
 /* Matrices beyond 64 rows and columns (small ones are worked on by themselves) go to a
  * kernel whose warps wait for one another's copies, products and tiles.  Each wait is
  * bounded (two seconds); where one runs out, which is a fault of this library or of the
- * device, every output of that kernel (X, or theta) is filled with NaNs, and the count of
+ * device, every output of that kernel (X, or theta; of many matrices each group has a kernel
+ * of its own) is filled with NaNs, and the count of
  * novak_ops_gave_up goes up.  Test hook for that: novak_orthogonalize with a limit of
  * wait_ns on each wait (0: the usual one) and with the end of tile number `withheld` never
  * announced (of tiles counted from 0 in the order in which they are begun, small matrices

@@ -110,7 +110,7 @@ bool place(Layout &l, int64_t rows, int64_t cols, Item &it)
     return true;
 }
 
-bool finish_layout(Layout &l, int n)
+void finish_layout(Layout &l, int n)
 {
     l.diags = static_cast<size_t>(l.panel_rows) * 128;
     l.items = l.diags + round_up(l.diag_floats * sizeof(float));
@@ -118,7 +118,6 @@ bool finish_layout(Layout &l, int n)
     l.done = l.partial + round_up(l.chunks * sizeof(double));
     l.control = l.done + round_up(n * sizeof(unsigned));
     l.bytes = l.control + round_up(sizeof(Control));
-    return true;
 }
 
 // ---- device: what the kernels share -------------------------------------------------
@@ -1603,20 +1602,44 @@ int tiles_of(const Item &it, int what, int columns)
 // do without: all).
 static bool placed(int64_t rows, int64_t cols, bool all) { return rows > 0 && cols > 0 && (all || small_ctas(rows, cols) == 0); }
 
-size_t orthogonalize_bytes(const int64_t *rows, const int64_t *cols, int n, bool all)
+// The matrices of a call in groups that use one workspace after another: f(first one, first one behind, bytes).  A group is as many
+// as fit kGroupBytes, or one that does not: a step of all of a model's matrices takes no more memory than that.
+// What a matrix comes to does not depend on its group.  (Groups' ends cost the last tiles of 15 products each, about 1 %: 24 of
+// 4096 x 4096 in groups of six 31 ms.)  false: more than can be addressed.
+constexpr size_t kGroupBytes = size_t(1) << 30;
+template <typename F> bool for_groups(const int64_t *rows, const int64_t *cols, int n, bool all, const F &f)
 {
-    Layout l;
+    Layout total, l;
     Item it{};
-    int count = 0;
-    bool any = false;
+    int first = 0, count = 0;
     for (int i = 0; i < n; ++i) {
-        any |= rows[i] > 0 && cols[i] > 0;
         if (!placed(rows[i], cols[i], all)) continue;
-        if (!place(l, rows[i], cols[i], it)) return 0;
+        if (!place(total, rows[i], cols[i], it)) return false;
+        Layout longer = l;
+        place(longer, rows[i], cols[i], it);
+        finish_layout(longer, count + 1);
+        if (count > 0 && longer.bytes > kGroupBytes) {
+            f(first, i, l.bytes);
+            longer = Layout();
+            place(longer, rows[i], cols[i], it);
+            finish_layout(longer, 1);
+            first = i;
+            count = 0;
+        }
+        l = longer;
         ++count;
     }
-    finish_layout(l, count);
-    return count > 0 ? l.bytes : any ? kLeastBytes : 0;
+    if (count > 0) f(first, n, l.bytes);
+    return true;
+}
+
+size_t orthogonalize_bytes(const int64_t *rows, const int64_t *cols, int n, bool all)
+{
+    size_t most = 0;
+    if (!for_groups(rows, cols, n, all, [&](int, int, size_t bytes) { most = std::max(most, bytes); })) return 0;
+    for (int i = 0; i < n && most == 0; ++i)
+        if (rows[i] > 0 && cols[i] > 0) most = kLeastBytes;
+    return most;
 }
 
 cudaError_t orthogonalize_gave_up(unsigned *count, cudaStream_t stream)
@@ -1624,6 +1647,9 @@ cudaError_t orthogonalize_gave_up(unsigned *count, cudaStream_t stream)
     cudaError_t e = cudaMemcpyFromSymbolAsync(count, g_orthogonalize_gave_up, sizeof *count, 0, cudaMemcpyDeviceToHost, stream);
     return e == cudaSuccess ? cudaStreamSynchronize(stream) : e;
 }
+
+// Matrices [begin, end) of a call by the tensor cores; `withheld`: of the group's tiles, whose number becomes `tiles_of_it`.
+static cudaError_t launch_group(const OrthArgs &a, int begin, int end, int64_t withheld, int64_t &tiles_of_it, cudaStream_t stream);
 
 cudaError_t launch_orthogonalize(const OrthArgs &a, cudaStream_t stream)
 {
@@ -1640,22 +1666,32 @@ cudaError_t launch_orthogonalize(const OrthArgs &a, cudaStream_t stream)
     cudaError_t e = cudaSuccess;
     if (!all) e = f32 ? launch_small<0, 1>(a, small, stream) : launch_small<1, 1>(a, small, stream);
     if (!all && e == cudaSuccess) e = f32 ? launch_small<0, kSmallCluster>(a, small, stream) : launch_small<1, kSmallCluster>(a, small, stream);
-    if (e != cudaSuccess) return e;
-    // the others
-    const auto here = [&](int i) { return placed(a.rows[i], a.cols[i], all); };
+    int64_t withheld = a.withheld;
+    for_groups(a.rows, a.cols, a.n, all, [&](int begin, int end, size_t) {
+        int64_t tiles = 0;
+        if (e == cudaSuccess) e = launch_group(a, begin, end, withheld, tiles, stream);
+        withheld = withheld >= tiles ? withheld - tiles : -1;
+    });
+    return e;
+}
 
+static cudaError_t launch_group(const OrthArgs &a, int begin, int end, int64_t withheld, int64_t &tiles_of_it, cudaStream_t stream)
+{
+    const Momentum mo{a.m != nullptr, a.nesterov, a.momentum};
+    const bool f32 = a.type == NOVAK_TYPE_F32, all = a.withheld >= 0;
+    const auto here = [&](int i) { return placed(a.rows[i], a.cols[i], all); };
+    cudaError_t e = cudaSuccess;
     Layout l;
     Item it{};
     int n = 0, first_of[3] = {};
     int64_t tiles[3][2] = {};           // of a step, by product: of 256 columns, and of 128
-    for (int i = 0; i < a.n; ++i)
+    for (int i = begin; i < end; ++i)
         if (here(i)) {
             place(l, a.rows[i], a.cols[i], it);
             for (int what = 0; what < 3; ++what)
                 for (int narrow = 0; narrow < 2; ++narrow) tiles[what][narrow] += tiles_of(it, what, narrow ? 128 : 256);
             ++n;
         }
-    if (n == 0) return cudaSuccess;
     finish_layout(l, n);
     uint8_t *base = static_cast<uint8_t *>(a.work);
     const Work w{reinterpret_cast<__half *>(base), reinterpret_cast<float *>(base + l.diags), reinterpret_cast<Item *>(base + l.items),
@@ -1673,6 +1709,7 @@ cudaError_t launch_orthogonalize(const OrthArgs &a, cudaStream_t stream)
         p.first[what + 1] = p.first[what] + static_cast<int>(tiles[what][narrow]);
         most = std::max(most, tiles[what][narrow]);
     }
+    tiles_of_it = static_cast<int64_t>(p.first[3]) * a.steps;
     Layout again;
     HostItems<kMostItems> items{};
     int first = 0, count = 0;
@@ -1689,7 +1726,7 @@ cudaError_t launch_orthogonalize(const OrthArgs &a, cudaStream_t stream)
         count = 0;
         return e;
     };
-    for (int i = 0; i < a.n && e == cudaSuccess; ++i) {
+    for (int i = begin; i < end && e == cudaSuccess; ++i) {
         if (!here(i)) continue;
         place(again, a.rows[i], a.cols[i], it);
         it.g = a.g[i];
@@ -1716,7 +1753,7 @@ cudaError_t launch_orthogonalize(const OrthArgs &a, cudaStream_t stream)
         for (int i = 0; i < 3; ++i) p.coefficients[k][i] = a.coefficients[k][i];
     p.decay = a.decay;
     p.theta = a.out == nullptr;
-    p.withheld = a.withheld;
+    p.withheld = withheld;
     p.wait_ns = a.wait_ns ? a.wait_ns : kWaitNs;
     // the panels as rows of 128 bytes, one behind the other
     const EncodeTiled encode = tensor_map_encoder();

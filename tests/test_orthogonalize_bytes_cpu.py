@@ -23,3 +23,13 @@ def test_matrices_that_stay_in_shared_memory_need_next_to_nothing(lib, shape):
 
 def test_nothing_needs_nothing(lib):
     assert ask(lib) == 0 and ask(lib, (0, 5), (5, 0)) == 0 and ask(lib, (0, 5), (5, 4)) > 0
+
+
+def test_many_matrices_go_through_one_workspace_in_groups(lib):
+    one = ask(lib, (4096, 4096))
+    assert 10 * 4096 ** 2 <= one < 10.2 * 4096 ** 2
+    for n in (7, 24, 400):                              # 6.7e9 elements
+        assert 5 * one < ask(lib, *[(4096, 4096)] * n) <= 1 << 30
+    assert ask(lib, *[(4096, 4096)] * 3) > 2.9 * one
+    huge = ask(lib, (65536, 16384))                     # too large for a group of the usual size: one of its own
+    assert ask(lib, *[(4096, 4096)] * 30, (65536, 16384), *[(4096, 4096)] * 30) == huge > 1 << 30

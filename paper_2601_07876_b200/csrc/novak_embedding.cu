@@ -81,6 +81,7 @@ __global__ void __launch_bounds__(kLookThreads) novak_embedding_kernel(LookArgs 
 constexpr int kOwnThreads = 512, kOwnRows = 4096;       // rows of the table per CTA at most
 constexpr int kCluster = 8;                             // CTAs that look through the ids together (each all of them: 33 MB out of L2, 8 us)
 constexpr int kList = 4096, kBitWords = 4 * kOwnThreads;        // tokens that a CTA keeps in shared memory; words of its bit map
+constexpr int kBits = 32 * kBitWords;                   // tokens in all that it has a bit for
 constexpr int kPiece = 16;                              // tokens in a piece; rows of more go by pieces
 constexpr int kSlice = 1024, kSumThreads = 256, kSumWarps = kSumThreads / 32;   // columns of a piece's CTA
 // Tokens that one kernel alone does: 197 of 1003 x 768 fp32 3.9 us, 6.8 where some words are frequent, 10.4 where all
@@ -101,7 +102,7 @@ struct GradArgs : EmbedGradArgs {
     int slices, group;      // of kSlice columns; threads per token there
     int64_t pieces;         // CTAs of the second kernel that sum them
     bool few;               // and there is no first one
-    int *list;              // tokens, for CTAs that have more than kList
+    void *list;             // for CTAs that have more than kList tokens: tokens; or of more than kBits in all int2, rows of the CTA and tokens
     Place *order;
     int2 *rows;             // of the table: how many tokens a row has, and where they are in that order; a single one itself
     int *counts;            // [piece][slice]: sums that are done, where a row begins in that piece
@@ -158,11 +159,16 @@ __device__ __forceinline__ uint32_t atomic_add_at(uint32_t addr, uint32_t x)
 __device__ __forceinline__ void store_at(uint32_t addr, int x) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(x) : "memory"); }
 __device__ __forceinline__ void store_at(uint32_t addr, uint16_t x) { asm volatile("st.shared::cluster.u16 [%0], %1;" ::"r"(addr), "h"(x) : "memory"); }
 
+constexpr int kFetched = 8;                             // ids of a thread on their way, where a CTA looks through all of them
+static_assert(kOwnRows <= kList, "a place for each row");
+
+// (98604 bytes.  1 KB more, and two CTAs no longer fit the split of an SM's memory that the second kernel takes as well:
+// setting it anew costs 2 us a call.)
 struct OwnShared {
     int counts[kOwnRows], starts[kOwnRows];
-    int found[kList], list[kList];              // tokens as they were found, row by row
+    int found[kList], list[kList];              // tokens as they were found (or, of more, where each row's next one goes); row by row
     uint16_t found_row[kList];
-    uint32_t bits[kBitWords];
+    __align__(16) uint32_t bits[kBitWords];
     uint16_t few[kOwnRows], many[kOwnRows];     // rows of 1 to 16 tokens, and of more
     int passed[kCluster];                       // tokens that this CTA found, by whose they are
     int before[kCluster], valid[kCluster];      // of each CTA's share of the ids: those of CTAs before this one; all
@@ -170,16 +176,185 @@ struct OwnShared {
     int n, n_few, n_many;
 };
 
+// How ids are dealt out, as a CTA sees it: blocks of 2^fold rows: own, own + 2^shift, ...; some of the last one's may be
+// beyond the table.
+struct Dealt {
+    const int64_t own, low;
+    const int fold, above, inside, rows;
+    __device__ __forceinline__ explicit Dealt(const GradArgs &a)
+        : own(blockIdx.x), low((int64_t(1) << a.shift) - 1), fold(a.fold), above(a.fold + a.shift), inside((1 << a.fold) - 1),
+          rows(static_cast<int>(max((((a.vocab + inside) >> fold) - own + low) >> a.shift, static_cast<int64_t>(0)) << fold))
+    {
+    }
+    __device__ __forceinline__ int row_of(int64_t id) const { return static_cast<int>(id >> above << fold | (id & inside)); }
+    __device__ __forceinline__ int64_t id_of(int row) const { return static_cast<int64_t>(row >> fold) << above | own << fold | (row & inside); }
+    __device__ __forceinline__ uint32_t owner(uint32_t id) const { return id >> fold & static_cast<uint32_t>(low); }
+};
+
+// The ids from t0 on, N a thread (what is none: the largest number).
+template <int N> __device__ __forceinline__ void fetch_ids(const GradArgs &a, int64_t t0, uint32_t (&id)[N])
+{
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const int64_t t = t0 + k * kOwnThreads + threadIdx.x, x = t < a.tokens ? id_at(a.ids, a.id_type, t) : -1;
+        id[k] = x >= 0 && x < a.vocab ? static_cast<uint32_t>(x) : ~0u;
+    }
+}
+
+// Places for a warp's tokens among those of the CTAs `whose` they are: kList for who has none.
+__device__ __forceinline__ uint32_t places(bool ours, uint32_t whose, OwnShared &sh)
+{
+    const unsigned all = __ballot_sync(0xffffffffu, ours);
+    if (__popc(all) <= 4) {
+        if (!ours) return kList;
+        atomicAdd(&sh.passed[whose], 1);
+        return atomic_add_at(at_rank(smem_addr(&sh.n), whose), 1);
+    }
+    // some word is frequent: one addition for all of a CTA's
+    const int lane = threadIdx.x & 31;
+    uint32_t at = kList;
+    for (unsigned left = all; left;) {
+        const int leader = __ffs(static_cast<int>(left)) - 1;
+        const uint32_t of = __shfl_sync(0xffffffffu, whose, leader);
+        const unsigned same = __ballot_sync(0xffffffffu, ours && whose == of);
+        left &= ~same;
+        uint32_t base = 0;
+        if (lane == leader) {
+            atomicAdd(&sh.passed[of], __popc(same));
+            base = atomic_add_at(at_rank(smem_addr(&sh.n), of), __popc(same));
+        }
+        base = __shfl_sync(0xffffffffu, base, leader);
+        if (same >> lane & 1) at = base + __popc(same & ((1u << lane) - 1));
+    }
+    return at;
+}
+
+// All ids, for this CTA's tokens in order, whatever their number, and how many each of its rows has.
+__device__ __forceinline__ void list_in_order(const GradArgs &a, const Dealt &deal, OwnShared &sh, int2 *list)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    constexpr int kSums = kFetched * kOwnThreads / 32, kEach = kSums / 32;
+    static_assert(kEach == 4 && 2 * kSums <= kBitWords, "an int4; two of them in the map's place");
+    int *const found_now = reinterpret_cast<int *>(sh.bits);       // tokens of 32 ids each
+    uint32_t id[kFetched], next[kFetched];
+    fetch_ids(a, 0, id);
+    int done = 0, turn = 0;
+    for (int64_t t0 = 0; t0 < a.tokens; t0 += kFetched * kOwnThreads, turn ^= 1) {
+        fetch_ids(a, t0 + kFetched * kOwnThreads, next);
+        unsigned mine[kFetched];
+#pragma unroll
+        for (int k = 0; k < kFetched; ++k) {
+            mine[k] = __ballot_sync(0xffffffffu, id[k] != ~0u && deal.owner(id[k]) == deal.own);
+            if (lane == 0) found_now[turn * kSums + k * (kOwnThreads / 32) + warp] = __popc(mine[k]);
+        }
+        __syncthreads();            // (two of them by turns: one barrier is enough)
+        // where each 32 ids' tokens go: four sums of them a lane
+        const int4 sums = *reinterpret_cast<const int4 *>(found_now + turn * kSums + lane * kEach);
+        const int sum = sums.x + sums.y + sums.z + sums.w;
+        int to_here = sum;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, to_here, d);
+            if (lane >= d) to_here += y;
+        }
+#pragma unroll
+        for (int k = 0; k < kFetched; ++k) {
+            if (mine[k] != 0) {             // (most often none is, and all of this is the cost of a pass over all ids)
+                const int which = k * (kOwnThreads / 32) + warp, i = which % kEach;
+                const int in_lane = (i > 0 ? sums.x : 0) + (i > 1 ? sums.y : 0) + (i > 2 ? sums.z : 0);
+                const int at = __shfl_sync(0xffffffffu, to_here - sum + in_lane, which / kEach), row = deal.row_of(id[k]);
+                const bool it = mine[k] >> lane & 1;
+                if (it) list[done + at + __popc(mine[k] & ((1u << lane) - 1))] = make_int2(row, static_cast<int>(t0 + k * kOwnThreads + threadIdx.x));
+                count_rows(it, row, sh.counts);
+            }
+            id[k] = next[k];
+        }
+        done += __shfl_sync(0xffffffffu, to_here, 31);
+    }
+}
+
+// The order of a list that is in order: each warp has some of the rows, and goes through all of the list.
+__device__ __forceinline__ void order_list(const GradArgs &a, const Dealt &deal, OwnShared &sh, const int2 *list, int before, int n)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    constexpr int kWarps = kOwnThreads / 32;
+    for (int i = threadIdx.x; i < deal.rows; i += kOwnThreads) sh.found[i] = sh.starts[i];
+    __syncthreads();
+    const auto put = [&](int row, int token, int place, int count, int start, unsigned same) {
+        const int id = static_cast<int>(deal.id_of(row)), at = before + place + __popc(same & ((1u << lane) - 1));
+        if (count == 1) a.rows[id] = make_int2(token, 1);
+        a.order[at] = count > kPiece ? Place{id, before + start, count, token} : Place{-1, 0, 0, token};
+    };
+    // (a word may be on most of them: the place of one row's next token is at hand, the others' are in shared memory)
+    int held = -1, held_place = 0, held_count = 0, held_start = 0;
+    for (int i0 = 0; i0 < n; i0 += 32 * kFetched) {
+        int2 x[kFetched];           // (no row's number is negative)
+#pragma unroll
+        for (int k = 0; k < kFetched; ++k) x[k] = i0 + k * 32 + lane < n ? list[i0 + k * 32 + lane] : make_int2(-1, 0);
+#pragma unroll
+        for (int k = 0; k < kFetched; ++k) {
+            const int row = x[k].x;
+            const bool mine = row >= 0 && row % kWarps == warp;
+            const unsigned of_held = __ballot_sync(0xffffffffu, mine && row == held);
+            if (mine && row == held) put(row, x[k].y, held_place, held_count, held_start, of_held);
+            held_place += __popc(of_held);
+            // the others, row by row
+            for (unsigned left = __ballot_sync(0xffffffffu, mine) & ~of_held; left;) {
+                const int of = __shfl_sync(0xffffffffu, row, __ffs(static_cast<int>(left)) - 1);
+                const unsigned same = __ballot_sync(0xffffffffu, row == of);
+                left &= ~same;
+                const int place = sh.found[of], next = place + __popc(same), count = sh.counts[of], start = sh.starts[of];
+                if (row == of) put(row, x[k].y, place, count, start, same);
+                __syncwarp();
+                const bool hold = __popc(same) > __popc(of_held);
+                if (lane == 0) {
+                    sh.found[of] = next;
+                    if (hold && held >= 0) sh.found[held] = held_place;
+                }
+                __syncwarp();
+                if (hold) {
+                    held = of;
+                    held_place = next;
+                    held_count = count;
+                    held_start = start;
+                }
+            }
+        }
+    }
+    for (int k = 0; k < sh.n_many; ++k)
+        for (int i = threadIdx.x; i < a.slices; i += kOwnThreads) a.counts[static_cast<int64_t>((before + sh.starts[sh.many[k]]) / kPiece) * a.slices + i] = 0;
+}
+
+// The rows of many tokens by comparing each with all of its row, a warp 32 of them at a time.
+__device__ __forceinline__ void order_by_comparing(const GradArgs &a, const Dealt &deal, const OwnShared &sh, int before)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int unit = 0;
+    for (int k = 0; k < sh.n_many; ++k) {
+        const int row = sh.many[k], count = sh.counts[row], first = sh.starts[row] - count;
+        for (int i = 0; i < count; i += 32, ++unit) {
+            if (unit % (kOwnThreads / 32) != warp) continue;
+            const int x = i + lane < count ? sh.list[first + i + lane] : INT_MAX;
+            int place = 0;
+#pragma unroll 8
+            for (int j = 0; j < count; ++j) place += sh.list[first + j] < x;
+            if (i + lane < count) a.order[before + first + place] = Place{static_cast<int>(deal.id_of(row)), before + first, count, x};
+        }
+        for (int i = threadIdx.x; i < a.slices; i += kOwnThreads) a.counts[static_cast<int64_t>((before + first) / kPiece) * a.slices + i] = 0;
+    }
+}
+
+// LONG: of more tokens in all than the map has bits for.  A map a row for each 65536 of them would cost their number times
+// the rows' (1048576 tokens of 50000 words alike, 16 columns: 4.7 ms, this way 1.3; 4194304 of one word 114 and 24).
+template <bool LONG>
 __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kOwnThreads, 2) novak_embedding_order_kernel(GradArgs a)
 {
     extern __shared__ uint8_t raw_shared[];
     OwnShared &sh = *reinterpret_cast<OwnShared *>(raw_shared);
-    const int64_t own = blockIdx.x, low = (int64_t(1) << a.shift) - 1;
-    const int fold = a.fold, above = fold + a.shift, inside = (1 << fold) - 1;
-    // blocks of 2^fold rows: own, own + 2^shift, ...; some of the last one's may be beyond the table
-    const int rows = static_cast<int>(max((((a.vocab + inside) >> fold) - own + low) >> a.shift, static_cast<int64_t>(0)) << fold);
-    const auto row_of = [&](int64_t id) { return static_cast<int>(id >> above << fold | (id & inside)); };
-    const auto id_of = [&](int row) { return static_cast<int64_t>(row >> fold) << above | own << fold | (row & inside); };
+    const Dealt deal(a);
+    const int64_t own = deal.own;
+    const int rows = deal.rows;
+    const auto id_of = [&](int row) { return deal.id_of(row); };
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     for (int i = threadIdx.x; i < rows; i += kOwnThreads) sh.counts[i] = 0;
     if (threadIdx.x < kCluster) sh.passed[threadIdx.x] = 0;
@@ -188,33 +363,33 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kOwnThreads, 
     start();
 
     // ---- this CTA's share of the ids: whose they are, and how many belong to CTAs before this cluster
-    constexpr int kAhead = 4, kAgain = 8;
-    const auto fetch = [&](int64_t t0, auto &id) {          // (what is none: the largest number)
-#pragma unroll
-        for (int k = 0; k < static_cast<int>(sizeof id / sizeof id[0]); ++k) {
-            const int64_t t = t0 + k * kOwnThreads + threadIdx.x, x = t < a.tokens ? id_at(a.ids, a.id_type, t) : -1;
-            id[k] = x >= 0 && x < a.vocab ? static_cast<uint32_t>(x) : ~0u;
-        }
-    };
-    const auto owner = [&](uint32_t id) { return id >> fold & static_cast<uint32_t>(low); };
+    constexpr int kAhead = 4;
     const uint32_t rank = cluster_rank(), cluster0 = static_cast<uint32_t>(own) - rank;
     {
         int before = 0, valid = 0;
         for (int64_t t0 = rank * kAhead * kOwnThreads; t0 < a.tokens; t0 += kCluster * kAhead * kOwnThreads) {
             uint32_t id[kAhead];
-            fetch(t0, id);
+            fetch_ids(a, t0, id);
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) {
-                const uint32_t whose = owner(id[k]) - cluster0;
-                if (id[k] == ~0u) continue;
-                ++valid;
-                before += owner(id[k]) < cluster0;
-                if (whose >= kCluster) continue;
-                atomicAdd(&sh.passed[whose], 1);
-                const uint32_t at = atomic_add_at(at_rank(smem_addr(&sh.n), whose), 1);
+                const uint32_t whose = deal.owner(id[k]) - cluster0;
+                uint32_t at;
+                if constexpr (LONG) {
+                    const bool there = id[k] != ~0u, ours = there && whose < kCluster;
+                    valid += there;
+                    before += there && deal.owner(id[k]) < cluster0;
+                    at = places(ours, whose, sh);
+                } else {
+                    if (id[k] == ~0u) continue;
+                    ++valid;
+                    before += deal.owner(id[k]) < cluster0;
+                    if (whose >= kCluster) continue;
+                    atomicAdd(&sh.passed[whose], 1);
+                    at = atomic_add_at(at_rank(smem_addr(&sh.n), whose), 1);
+                }
                 if (at < kList) {
                     store_at(at_rank(smem_addr(&sh.found[at]), whose), static_cast<int>(t0 + k * kOwnThreads + threadIdx.x));
-                    store_at(at_rank(smem_addr(&sh.found_row[at]), whose), static_cast<uint16_t>(row_of(id[k])));
+                    store_at(at_rank(smem_addr(&sh.found_row[at]), whose), static_cast<uint16_t>(deal.row_of(id[k])));
                 }
             }
         }
@@ -245,15 +420,16 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kOwnThreads, 
         *a.valid = valid;
     }
     const int n = sh.n;
-    int *list = n <= kList ? sh.list : a.list + before;
     if (n <= kList) {
         for (int i = warp * 32; i < n; i += kOwnThreads) count_rows(i + lane < n, i + lane < n ? sh.found_row[i + lane] : 0, sh.counts);
+    } else if constexpr (LONG) {
+        list_in_order(a, deal, sh, static_cast<int2 *>(a.list) + before);
     } else {
-        for (int64_t t0 = 0; t0 < a.tokens; t0 += kAgain * kOwnThreads) {
-            uint32_t id[kAgain];
-            fetch(t0, id);
+        for (int64_t t0 = 0; t0 < a.tokens; t0 += kFetched * kOwnThreads) {
+            uint32_t id[kFetched];
+            fetch_ids(a, t0, id);
 #pragma unroll
-            for (int k = 0; k < kAgain; ++k) count_rows(id[k] != ~0u && owner(id[k]) == own, row_of(id[k]), sh.counts);
+            for (int k = 0; k < kFetched; ++k) count_rows(id[k] != ~0u && deal.owner(id[k]) == own, deal.row_of(id[k]), sh.counts);
         }
     }
     __syncthreads();
@@ -281,29 +457,32 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kOwnThreads, 
     __syncthreads();
 
     // ---- the tokens, row by row: put there in any order (starts go up to the ends) ...
-    const auto put = [&](bool mine, int row, int t) {
-        if (__any_sync(0xffffffffu, mine)) {
-            const int place = count_rows(mine, row, sh.starts);
-            if (mine) list[place] = t;
-        }
-    };
+    int *const list = LONG || n <= kList ? sh.list : static_cast<int *>(a.list) + before;
     if (n <= kList) {
         for (int i = warp * 32; i < n; i += kOwnThreads) {
             const bool in = i + lane < n;
-            put(in, in ? sh.found_row[i + lane] : 0, in ? sh.found[i + lane] : 0);
+            const int place = count_rows(in, in ? sh.found_row[i + lane] : 0, sh.starts);
+            if (in) list[place] = sh.found[i + lane];
         }
+    } else if constexpr (LONG) {
+        order_list(a, deal, sh, static_cast<const int2 *>(a.list) + before, before, n);
+        return;
     } else {
-        for (int64_t t0 = 0; t0 < a.tokens; t0 += kAgain * kOwnThreads) {
-            uint32_t id[kAgain];
-            fetch(t0, id);
+        for (int64_t t0 = 0; t0 < a.tokens; t0 += kFetched * kOwnThreads) {
+            uint32_t id[kFetched];
+            fetch_ids(a, t0, id);
 #pragma unroll
-            for (int k = 0; k < kAgain; ++k)
-                put(id[k] != ~0u && owner(id[k]) == own, row_of(id[k]), static_cast<int>(t0 + k * kOwnThreads + threadIdx.x));
+            for (int k = 0; k < kFetched; ++k) {
+                const bool mine = id[k] != ~0u && deal.owner(id[k]) == own;
+                if (!__any_sync(0xffffffffu, mine)) continue;
+                const int place = count_rows(mine, deal.row_of(id[k]), sh.starts);
+                if (mine) list[place] = static_cast<int>(t0 + k * kOwnThreads + threadIdx.x);
+            }
         }
     }
     __syncthreads();
 
-    // ---- ... and then in order.  Of few tokens a lane has one each: its place is the number of tokens before it.
+    // ... and then in order.  Of few tokens a lane has one each: its place is the number of tokens before it.
     const int n_few = sh.n_few;
     for (int i = warp; i < n_few; i += kOwnThreads / 32) {
         const int row = sh.few[i], count = sh.counts[row], first = sh.starts[row] - count;
@@ -313,31 +492,31 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kOwnThreads, 
         for (int j = 0; j < count; ++j) place += __shfl_sync(0xffffffffu, x, j) < x;
         if (lane < count) a.order[before + first + place] = Place{-1, 0, 0, x};
     }
-    // Many: the tokens as bits of a map, 65536 of them at a time.
-    for (int k = 0; k < sh.n_many; ++k) {
-        const int row = sh.many[k], count = sh.counts[row], first = sh.starts[row] - count;
-        int done = 0;
-        for (int64_t t0 = 0; t0 < a.tokens && done < count; t0 += 32 * kBitWords) {
+    if constexpr (LONG) {
+        order_by_comparing(a, deal, sh, before);
+    } else {
+        // Many: the tokens as bits of a map.
+        for (int k = 0; k < sh.n_many; ++k) {
+            const int row = sh.many[k], count = sh.counts[row], first = sh.starts[row] - count;
             __syncthreads();
             for (int i = threadIdx.x; i < kBitWords; i += kOwnThreads) sh.bits[i] = 0;
             __syncthreads();
             for (int i = threadIdx.x; i < count; i += kOwnThreads) {
-                const int64_t t = list[first + i] - t0;
-                if (t >= 0 && t < 32 * kBitWords) atomicOr(&sh.bits[t >> 5], 1u << (t & 31));
+                const int t = list[first + i];
+                atomicOr(&sh.bits[t >> 5], 1u << (t & 31));
             }
             __syncthreads();
             constexpr int kEach = kBitWords / kOwnThreads;
             int bits = 0, all;
             for (int i = 0; i < kEach; ++i) bits += __popc(sh.bits[threadIdx.x * kEach + i]);
-            int at = done + scan<kOwnThreads>(bits, sh.scratch, all);
-            done += all;
+            int at = scan<kOwnThreads>(bits, sh.scratch, all);
             for (int i = 0; i < kEach; ++i)
                 for (uint32_t m = sh.bits[threadIdx.x * kEach + i]; m; m &= m - 1, ++at) {
-                    const int t = static_cast<int>(t0) + (threadIdx.x * kEach + i) * 32 + __ffs(static_cast<int>(m)) - 1;
+                    const int t = (threadIdx.x * kEach + i) * 32 + __ffs(static_cast<int>(m)) - 1;
                     a.order[before + first + at] = Place{static_cast<int>(id_of(row)), before + first, count, t};
                 }
+            for (int i = threadIdx.x; i < a.slices; i += kOwnThreads) a.counts[static_cast<int64_t>((before + first) / kPiece) * a.slices + i] = 0;
         }
-        for (int i = threadIdx.x; i < a.slices; i += kOwnThreads) a.counts[static_cast<int64_t>((before + first) / kPiece) * a.slices + i] = 0;
     }
 }
 
@@ -704,7 +883,7 @@ GradLayout layout_of(int64_t tokens, int64_t vocab, int64_t cols)
     l.pieces = tokens > kPiece ? (tokens + kPiece - 1) / kPiece : 0;        // (fewer tokens are no long row's)
     l.slices = static_cast<int>((cols + kSlice - 1) / kSlice);
     l.list = 0;
-    l.order = l.list + round_up((tokens > kList ? tokens : 0) * sizeof(int));
+    l.order = l.list + round_up((tokens > kBits ? tokens * sizeof(int2) : tokens > kList ? tokens * sizeof(int) : 0));
     l.rows = l.order + round_up(tokens * sizeof(Place));
     l.counts = l.rows + round_up(vocab * sizeof(int2));
     l.valid = l.counts + round_up(l.pieces * l.slices * sizeof(int));
@@ -751,17 +930,18 @@ cudaError_t launch_embedding_grad(const EmbedGradArgs &a, cudaStream_t stream)
 {
     const GradLayout l = layout_of(a.tokens, a.vocab, a.cols);
     uint8_t *base = static_cast<uint8_t *>(a.work);
-    GradArgs g{a, 8, 0, 0, 0, 1, l.slices, 0, l.pieces, a.tokens <= kFew, reinterpret_cast<int *>(base + l.list),
+    GradArgs g{a, 8, 0, 0, 0, 1, l.slices, 0, l.pieces, a.tokens <= kFew, base + l.list,
                reinterpret_cast<Place *>(base + l.order), reinterpret_cast<int2 *>(base + l.rows), reinterpret_cast<int *>(base + l.counts), reinterpret_cast<int *>(base + l.valid),
                reinterpret_cast<float *>(base + l.partial)};
     // Neighbouring rows that are short together go to one CTA, as long as there are blocks for all CTAs.
     while ((a.cols << g.fold) < 256 && (a.vocab >> (g.fold + g.shift)) >= 2) ++g.fold;
     while (((((a.vocab + (1 << g.fold) - 1) >> g.fold) + (int64_t(1) << g.shift) - 1) >> g.shift << g.fold) > kOwnRows) ++g.shift;
     const int64_t ctas = std::min<int64_t>(int64_t(1) << g.shift, (a.vocab + (int64_t(1) << g.fold) - 1) >> g.fold);
-    static std::atomic<uint64_t> asked{0};
-    cudaError_t e = ask_shared_memory(novak_embedding_order_kernel, sizeof(OwnShared), asked);
+    static std::atomic<uint64_t> asked[2] = {};
+    const auto kernel = a.tokens > kBits ? novak_embedding_order_kernel<true> : novak_embedding_order_kernel<false>;
+    cudaError_t e = ask_shared_memory(kernel, sizeof(OwnShared), asked[a.tokens > kBits]);
     if (e == cudaSuccess && !g.few)
-        e = launch(novak_embedding_order_kernel, dim3(static_cast<unsigned>((ctas + kCluster - 1) / kCluster * kCluster)), kOwnThreads, sizeof(OwnShared), stream, g);
+        e = launch(kernel, dim3(static_cast<unsigned>((ctas + kCluster - 1) / kCluster * kCluster)), kOwnThreads, sizeof(OwnShared), stream, g);
     if (e != cudaSuccess) return e;
 
     const bool aligned = (a.tokens == 0 || wide(a.dout, a.type, a.tokens)) && wide(a.dtable, a.grad_type, a.vocab) && a.cols % 8 == 0;

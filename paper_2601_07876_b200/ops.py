@@ -282,8 +282,9 @@ def linear_weight_grad(dy, kept: Act8, affine=None, bias: bool = True, dtype=tor
 
 
 def wait_failures() -> int:
-    """How many bounded waits inside the weight gradient's kernel ran out on the current
-    device since the library was loaded (0, or something is broken; see include/novak.h).
+    """How many bounded waits inside the kernels of the weight gradient and of the orthogonalised
+    updates ran out on the current device since the library was loaded (0, or something is
+    broken; see include/novak.h).
     Synchronises torch's current stream."""
     lib, count = B.load_library(), B.c_uint32()
     status = lib.novak_ops_gave_up(B.byref(count), torch.cuda.current_stream().cuda_stream)

@@ -871,6 +871,23 @@ int novak_orthogonal_step(float *const *d_theta, const void *const *d_g, int gra
                           const double *coefficients, int steps, double eps, void *d_work,
                           size_t work_bytes, void *stream);
 
+/* The same three with operands of two fp16 parts for the larger matrices too, as the small ones
+ * have them always: three products for each, two to three times as long (4096 x 4096: 3.5 ms,
+ * 1.2 otherwise), and 6 bytes an element more of workspace if square.  What is left are the tensor
+ * cores' sums: X is 3e-6 (256 x 300) to 3e-5 (4096 x 4096) of its norm off for a dense G, 2e-6
+ * where a few elements carry G, and where all of G is in one direction 2e-4 to 2e-3 (the
+ * same in fp32 throughout: 1e-4 to 5e-4). */
+size_t novak_orthogonalize_fine_bytes(const int64_t *rows, const int64_t *cols, int n);
+int novak_orthogonalize_fine(const void *const *d_g, const int64_t *g_stride, int type,
+                             void *const *d_out, const int64_t *out_stride, const int64_t *rows,
+                             const int64_t *cols, int n, const double *coefficients, int steps,
+                             double eps, void *d_work, size_t work_bytes, void *stream);
+int novak_orthogonal_step_fine(float *const *d_theta, const void *const *d_g, int grad_type,
+                               float *const *d_m, const int64_t *rows, const int64_t *cols, int n,
+                               double momentum, int nesterov, const double *step, double decay,
+                               const double *coefficients, int steps, double eps, void *d_work,
+                               size_t work_bytes, void *stream);
+
 /* Matrices beyond 64 rows and columns (small ones are worked on by themselves) go to a
  * kernel whose warps wait for one another's copies, products and tiles.  Each wait is
  * bounded (two seconds); where one runs out, which is a fault of this library or of the

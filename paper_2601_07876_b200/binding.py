@@ -180,6 +180,11 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
                                         c_size_t, vp]),
         "novak_orthogonal_step": (c_int, [vp, vp, c_int, vp, vp, vp, c_int, c_double, c_int, vp, c_double,
                                           vp, c_int, c_double, vp, c_size_t, vp]),
+        "novak_orthogonalize_fine_bytes": (c_size_t, [vp, vp, c_int]),
+        "novak_orthogonalize_fine": (c_int, [vp, vp, c_int, vp, vp, vp, vp, c_int, vp, c_int, c_double, vp,
+                                        c_size_t, vp]),
+        "novak_orthogonal_step_fine": (c_int, [vp, vp, c_int, vp, vp, vp, c_int, c_double, c_int, vp, c_double,
+                                          vp, c_int, c_double, vp, c_size_t, vp]),
         "novak_selftest_orthogonalize_wait": (c_int, [vp, vp, c_int, vp, vp, vp, vp, c_int, vp, c_int,
                                                       c_double, vp, c_size_t, c_int64, c_uint64, vp]),
         "novak_ops_gave_up": (c_int, [POINTER(c_uint32), vp]),

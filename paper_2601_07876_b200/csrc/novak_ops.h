@@ -143,12 +143,13 @@ struct OrthArgs {               // arrays of n on the host
     const double *step;
     float decay;
     void *work;
+    bool fine = false;          // operands of two parts in the large ones' products too
     int64_t withheld = -1;      // a tile whose end is not announced (a test of the waits' limit)
     uint64_t wait_ns = 0;       // a wait's limit; 0: the usual one
 };
 // 0: the matrices are too large or too many to be addressed.  `all`: where a.withheld >= 0, with which small matrices
 // need a place too.
-size_t orthogonalize_bytes(const int64_t *rows, const int64_t *cols, int n, bool all = false);
+size_t orthogonalize_bytes(const int64_t *rows, const int64_t *cols, int n, bool fine, bool all = false);
 cudaError_t orthogonalize_gave_up(unsigned *count, cudaStream_t stream);
 cudaError_t launch_orthogonalize(const OrthArgs &a, cudaStream_t stream);
 

@@ -194,7 +194,7 @@ int check_orthogonalize(const int64_t *rows, const int64_t *cols, int n, const d
 
 int check_orthogonalize_work(const OrthArgs &a, size_t work_bytes)
 {
-    const size_t need = orthogonalize_bytes(a.rows, a.cols, a.n);
+    const size_t need = orthogonalize_bytes(a.rows, a.cols, a.n, a.fine);
     bool any = false;
     for (int i = 0; i < a.n; ++i) any |= a.rows[i] > 0 && a.cols[i] > 0;
     if (any && need == 0) return refuse("the matrices are more than can be addressed in one call");
@@ -219,6 +219,57 @@ int orthogonalize(OrthArgs &a, const double *coefficients, int steps, size_t wor
         CHECK(check_mat("g", mat(a.g[i], a.g_stride[i]), a.type, a.rows[i], a.cols[i]));
         CHECK(check_mat("out", mat(a.out[i], a.out_stride[i]), NOVAK_TYPE_BF16, a.rows[i], a.cols[i]));
     }
+    set_coefficients(a, coefficients, steps);
+    CHECK(check_orthogonalize_work(a, work_bytes));
+    return finish(launch_orthogonalize(a, static_cast<cudaStream_t>(stream)), where);
+}
+
+size_t workspace(const int64_t *rows, const int64_t *cols, int n, bool fine)
+{
+    const double one[3] = {1.0, 0.0, 0.0};
+    return check_orthogonalize(rows, cols, n, one, 1, 0.0) == NOVAK_OK ? orthogonalize_bytes(rows, cols, n, fine) : 0;
+}
+
+int orthogonal_step(float *const *d_theta, const void *const *d_g, int grad_type, float *const *d_m, const int64_t *rows,
+                    const int64_t *cols, int n, double momentum, int nesterov, const double *step, double decay,
+                    const double *coefficients, int steps, double eps, void *d_work, size_t work_bytes, bool fine, void *stream,
+                    const char *where)
+{
+    if (!is_type(grad_type)) return refuse("bad type");
+    CHECK(check_orthogonalize(rows, cols, n, coefficients, steps, eps));
+    if (!(momentum >= 0.0 && momentum < 1.0)) return refuse("momentum must be in [0, 1)");
+    if (!std::isfinite(decay)) return refuse("decay must be finite");
+    if (n > 0 && (!d_theta || !d_g || !d_m || !step)) return refuse("an array is NULL");
+    for (int i = 0; i < n; ++i) {
+        if (!std::isfinite(step[i])) return refuse("step must be finite");
+        if (cols[i] == 0) continue;
+        CHECK(check_mat("theta", mat(d_theta[i], cols[i]), NOVAK_TYPE_F32, rows[i], cols[i]));
+        CHECK(check_mat("m", mat(d_m[i], cols[i]), NOVAK_TYPE_F32, rows[i], cols[i]));
+        CHECK(check_mat("g", mat(d_g[i], cols[i]), grad_type, rows[i], cols[i]));
+    }
+    // what is written belongs to one matrix alone
+    using Range = std::pair<uintptr_t, uintptr_t>;
+    const std::unique_ptr<Range[]> written(new (std::nothrow) Range[2 * static_cast<size_t>(n) + 1]);
+    if (!written) return refuse("no memory on the host");
+    Range *end = written.get();
+    const auto range = [&](const void *p, int i, size_t size) {
+        const uintptr_t first = reinterpret_cast<uintptr_t>(p);
+        return Range(first, first + static_cast<size_t>(rows[i]) * static_cast<size_t>(cols[i]) * size);
+    };
+    for (int i = 0; i < n; ++i)
+        if (rows[i] > 0 && cols[i] > 0)
+            for (const float *p : {d_theta[i], d_m[i]}) *end++ = range(p, i, sizeof(float));
+    std::sort(written.get(), end);
+    for (const Range *r = written.get() + 1; r < end; ++r)
+        if (r->first < r[-1].second) return refuse("theta and m overlap one another");
+    for (int i = 0; i < n; ++i) {
+        if (rows[i] == 0 || cols[i] == 0) continue;
+        const Range g = range(d_g[i], i, grad_type == NOVAK_TYPE_F32 ? 4 : 2);
+        const Range *behind = std::lower_bound(written.get(), end, Range(g.second, 0));     // the first that begins behind g
+        if (behind != written.get() && behind[-1].second > g.first) return refuse("g overlaps theta or m");
+    }
+    OrthArgs a{d_g, nullptr, grad_type, nullptr, nullptr, rows, cols, n, {}, 0, eps, d_theta, d_m,
+               static_cast<float>(momentum), nesterov != 0, step, static_cast<float>(decay), d_work, fine};
     set_coefficients(a, coefficients, steps);
     CHECK(check_orthogonalize_work(a, work_bytes));
     return finish(launch_orthogonalize(a, static_cast<cudaStream_t>(stream)), where);
@@ -427,11 +478,9 @@ int novak_embedding_grad(const void *d_dout, int64_t dout_stride, int type, cons
     return finish(launch_embedding_grad(a, static_cast<cudaStream_t>(stream)), "novak_embedding_grad");
 }
 
-size_t novak_orthogonalize_bytes(const int64_t *rows, const int64_t *cols, int n)
-{
-    const double one[3] = {1.0, 0.0, 0.0};
-    return check_orthogonalize(rows, cols, n, one, 1, 0.0) == NOVAK_OK ? orthogonalize_bytes(rows, cols, n) : 0;
-}
+size_t novak_orthogonalize_bytes(const int64_t *rows, const int64_t *cols, int n) { return workspace(rows, cols, n, false); }
+
+size_t novak_orthogonalize_fine_bytes(const int64_t *rows, const int64_t *cols, int n) { return workspace(rows, cols, n, true); }
 
 int novak_orthogonalize(const void *const *d_g, const int64_t *g_stride, int type, void *const *d_out,
                         const int64_t *out_stride, const int64_t *rows, const int64_t *cols, int n,
@@ -442,18 +491,27 @@ int novak_orthogonalize(const void *const *d_g, const int64_t *g_stride, int typ
     return orthogonalize(a, coefficients, steps, work_bytes, stream, "novak_orthogonalize");
 }
 
+int novak_orthogonalize_fine(const void *const *d_g, const int64_t *g_stride, int type, void *const *d_out,
+                             const int64_t *out_stride, const int64_t *rows, const int64_t *cols, int n,
+                             const double *coefficients, int steps, double eps, void *d_work, size_t work_bytes, void *stream)
+{
+    OrthArgs a{d_g, g_stride, type, d_out, out_stride, rows, cols, n, {}, 0, eps, nullptr, nullptr, 0.0f, false, nullptr,
+               0.0f, d_work, true};
+    return orthogonalize(a, coefficients, steps, work_bytes, stream, "novak_orthogonalize_fine");
+}
+
 int novak_selftest_orthogonalize_wait(const void *const *d_g, const int64_t *g_stride, int type, void *const *d_out,
                                       const int64_t *out_stride, const int64_t *rows, const int64_t *cols, int n,
                                       const double *coefficients, int steps, double eps, void *d_work,
                                       size_t work_bytes, int64_t withheld, uint64_t wait_ns, void *stream)
 {
     OrthArgs a{d_g, g_stride, type, d_out, out_stride, rows, cols, n, {}, 0, eps, nullptr, nullptr, 0.0f, false, nullptr,
-               0.0f, d_work, withheld, wait_ns};
+               0.0f, d_work, false, withheld, wait_ns};
     const char *where = "novak_selftest_orthogonalize_wait";
     if (withheld < 0) return orthogonalize(a, coefficients, steps, work_bytes, stream, where);
     // small matrices take the large ones' way, for which the caller's workspace has no place
     CHECK(check_orthogonalize(rows, cols, n, coefficients, steps, eps));
-    const size_t need = orthogonalize_bytes(rows, cols, n, true);
+    const size_t need = orthogonalize_bytes(rows, cols, n, false, true);
     if (need == 0) return orthogonalize(a, coefficients, steps, work_bytes, stream, where);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     CHECK(finish(cudaMallocAsync(&a.work, need, s), where));
@@ -466,44 +524,17 @@ int novak_orthogonal_step(float *const *d_theta, const void *const *d_g, int gra
                           const double *step, double decay, const double *coefficients, int steps, double eps,
                           void *d_work, size_t work_bytes, void *stream)
 {
-    if (!is_type(grad_type)) return refuse("bad type");
-    CHECK(check_orthogonalize(rows, cols, n, coefficients, steps, eps));
-    if (!(momentum >= 0.0 && momentum < 1.0)) return refuse("momentum must be in [0, 1)");
-    if (!std::isfinite(decay)) return refuse("decay must be finite");
-    if (n > 0 && (!d_theta || !d_g || !d_m || !step)) return refuse("an array is NULL");
-    for (int i = 0; i < n; ++i) {
-        if (!std::isfinite(step[i])) return refuse("step must be finite");
-        if (cols[i] == 0) continue;
-        CHECK(check_mat("theta", mat(d_theta[i], cols[i]), NOVAK_TYPE_F32, rows[i], cols[i]));
-        CHECK(check_mat("m", mat(d_m[i], cols[i]), NOVAK_TYPE_F32, rows[i], cols[i]));
-        CHECK(check_mat("g", mat(d_g[i], cols[i]), grad_type, rows[i], cols[i]));
-    }
-    // what is written belongs to one matrix alone
-    using Range = std::pair<uintptr_t, uintptr_t>;
-    const std::unique_ptr<Range[]> written(new (std::nothrow) Range[2 * static_cast<size_t>(n) + 1]);
-    if (!written) return refuse("no memory on the host");
-    Range *end = written.get();
-    const auto range = [&](const void *p, int i, size_t size) {
-        const uintptr_t first = reinterpret_cast<uintptr_t>(p);
-        return Range(first, first + static_cast<size_t>(rows[i]) * static_cast<size_t>(cols[i]) * size);
-    };
-    for (int i = 0; i < n; ++i)
-        if (rows[i] > 0 && cols[i] > 0)
-            for (const float *p : {d_theta[i], d_m[i]}) *end++ = range(p, i, sizeof(float));
-    std::sort(written.get(), end);
-    for (const Range *r = written.get() + 1; r < end; ++r)
-        if (r->first < r[-1].second) return refuse("theta and m overlap one another");
-    for (int i = 0; i < n; ++i) {
-        if (rows[i] == 0 || cols[i] == 0) continue;
-        const Range g = range(d_g[i], i, grad_type == NOVAK_TYPE_F32 ? 4 : 2);
-        const Range *behind = std::lower_bound(written.get(), end, Range(g.second, 0));     // the first that begins behind g
-        if (behind != written.get() && behind[-1].second > g.first) return refuse("g overlaps theta or m");
-    }
-    OrthArgs a{d_g, nullptr, grad_type, nullptr, nullptr, rows, cols, n, {}, 0, eps, d_theta, d_m,
-               static_cast<float>(momentum), nesterov != 0, step, static_cast<float>(decay), d_work};
-    set_coefficients(a, coefficients, steps);
-    CHECK(check_orthogonalize_work(a, work_bytes));
-    return finish(launch_orthogonalize(a, static_cast<cudaStream_t>(stream)), "novak_orthogonal_step");
+    return orthogonal_step(d_theta, d_g, grad_type, d_m, rows, cols, n, momentum, nesterov, step, decay, coefficients, steps, eps,
+                           d_work, work_bytes, false, stream, "novak_orthogonal_step");
+}
+
+int novak_orthogonal_step_fine(float *const *d_theta, const void *const *d_g, int grad_type, float *const *d_m,
+                               const int64_t *rows, const int64_t *cols, int n, double momentum, int nesterov,
+                               const double *step, double decay, const double *coefficients, int steps, double eps,
+                               void *d_work, size_t work_bytes, void *stream)
+{
+    return orthogonal_step(d_theta, d_g, grad_type, d_m, rows, cols, n, momentum, nesterov, step, decay, coefficients, steps, eps,
+                           d_work, work_bytes, true, stream, "novak_orthogonal_step_fine");
 }
 
 int novak_activation(const void *d_u, int64_t u_stride, void *d_a, int64_t a_stride, int type, int kind,

@@ -20,6 +20,10 @@
 // large any more, both parts.  The result is then off by 1e-4 (low rank) to 9e-4 (all singular values alike) of its norm
 // for dense gradients (the last step without the second part: 1.1e-3 for rank one, before 3e-4, and 2 % less time), and by
 // up to 1e-2 where a few elements carry the gradient, whose roundings do not average out.
+// Whoever asks for it (`fine`) has operands of two parts here too, X, A and B, and three times the products, one behind
+// the other into the same sums: first by first parts, first by second, second by first.  Second parts are not scaled then;
+// they end at 2^-24 of the first ones' unit, 2^-36 of |X|.  (4096 x 4096 1.2 and 3.5 ms, 12 of 2304 x 768 and 768 x 768 0.64 and
+// 1.2; 5e-4 and 3e-5 off.  What is left are the tensor cores' sums, which cut off what fp32 would round.)
 //
 // Memory.  Every matrix is kept as panels of 64 columns: the rows of a panel, 128 bytes each,
 // lie one behind the other, rows padded to 128 and columns to 64 with zeros.
@@ -48,7 +52,8 @@ struct Item {
     float *m;
     int64_t g_stride, out_stride;
     int rows, cols, tall, side; // side: of A and B
-    int x[2], low, gram, poly;  // X's first part (taken in turns), second part, A, B
+    int x[2], low[2], gram, poly;       // X's first part (taken in turns), second part (one place unless fine), A, B
+    int gram_low, poly_low;     // fine: their second parts
     int x_pitch, s_pitch;       // rows of a panel
     int diag;                   // floats from the diagonals' start: A's, then B's (s_pitch each)
     int unit, units;            // of 128 rows of a panel: first one, how many
@@ -79,7 +84,7 @@ constexpr size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
 __host__ __device__ constexpr int pad_to(int64_t n, int to) { return static_cast<int>((n + to - 1) / to * to); }
 
 // Places of one more matrix behind those that are there.
-bool place(Layout &l, int64_t rows, int64_t cols, Item &it)
+bool place(Layout &l, int64_t rows, int64_t cols, bool fine, Item &it)
 {
     it.rows = static_cast<int>(rows);
     it.cols = static_cast<int>(cols);
@@ -88,16 +93,21 @@ bool place(Layout &l, int64_t rows, int64_t cols, Item &it)
     it.x_pitch = pad_to(rows, kBlock);
     it.s_pitch = pad_to(it.side, kBlock);
     const int64_t x = (cols + kPanel - 1) / kPanel * it.x_pitch, s = static_cast<int64_t>((it.side + kPanel - 1) / kPanel) * it.s_pitch;
-    if (l.panel_rows + 3 * x + 2 * s > INT_MAX - (1 << 24)) return false;       // (boxes beyond the last panel have places too)
+    if (l.panel_rows + (fine ? 4 : 3) * x + (fine ? 4 : 2) * s > INT_MAX - (1 << 24)) return false;     // (boxes beyond the last panel have places too)
     int64_t at = l.panel_rows;
-    for (int *p : {&it.x[0], &it.x[1], &it.low}) {
-        *p = static_cast<int>(at);
-        at += x;
-    }
-    for (int *p : {&it.gram, &it.poly}) {
-        *p = static_cast<int>(at);
-        at += s;
-    }
+    const auto next = [&](int64_t size, bool own = true) {
+        const int p = static_cast<int>(at);
+        if (own) at += size;
+        return p;
+    };
+    it.x[0] = next(x);
+    it.x[1] = next(x);
+    it.low[0] = next(x, fine);
+    it.low[1] = next(x);
+    it.gram = next(s);
+    it.poly = next(s);
+    it.gram_low = next(s, fine);
+    it.poly_low = next(s, fine);
     l.panel_rows = at;
     it.diag = static_cast<int>(l.diag_floats);
     l.diag_floats += 2 * it.s_pitch;
@@ -303,7 +313,7 @@ __device__ __forceinline__ void scale_of(double squares, float eps, float &tiny,
 
 // X's two parts in units of 2^-12.
 template <int TYPE>
-__global__ void __launch_bounds__(kThreads) novak_orthogonalize_start_kernel(Work w, int n, int64_t units, Momentum mo, float eps)
+__global__ void __launch_bounds__(kThreads) novak_orthogonalize_start_kernel(Work w, int n, int64_t units, Momentum mo, float eps, float low_scale)
 {
     __shared__ double scratch[kThreads / 32];
     start();
@@ -330,11 +340,11 @@ __global__ void __launch_bounds__(kThreads) novak_orthogonalize_start_kernel(Wor
                 for (int k = 0; k < 2; ++k) {
                     hi[k] = pack_half(x[2 * k], x[2 * k + 1]);
                     const float2 h = unpack_half(hi[k]);
-                    lo[k] = pack_half((x[2 * k] - h.x) * kScaleLow, (x[2 * k + 1] - h.y) * kScaleLow);
+                    lo[k] = pack_half((x[2 * k] - h.x) * low_scale, (x[2 * k + 1] - h.y) * low_scale);
                 }
                 const int64_t at = (static_cast<int64_t>(panel) * it.x_pitch + row) * kPanel + c;
                 *reinterpret_cast<uint2 *>(w.panels + static_cast<int64_t>(it.x[0]) * kPanel + at) = make_uint2(hi[0], hi[1]);
-                *reinterpret_cast<uint2 *>(w.panels + static_cast<int64_t>(it.low) * kPanel + at) = make_uint2(lo[0], lo[1]);
+                *reinterpret_cast<uint2 *>(w.panels + static_cast<int64_t>(it.low[0]) * kPanel + at) = make_uint2(lo[0], lo[1]);
             });
         }
     }
@@ -858,17 +868,18 @@ struct Tile {
     int what;               // 0: A; 1: B; 2: X; -1: no more
     int which, step, columns;
     int row, col;           // of the tile
-    int steps;              // of 64 products
+    int steps;              // of 64 products (fine: three times as many)
     int a, a_step, a_half;  // rows of 128 bytes: the first box of a CTA's 128 rows, the next 64 products, its second box
     int b, b_step, b_half;
     int a_rank, b_rank;     // what the second CTA of the pair adds to a and b
+    int a_low, b_low;       // fine: from the operands' first parts to their second ones
     uint32_t descriptor;    // of the instruction
     unsigned need;          // parts of this matrix that have to be stored before
     int announced;          // 0: a test's tile whose end nobody is told
     // of what takes it out, in rows of 128 bytes as above:
     int height, width;      // rows and columns that are stored
     int pitch;              // rows of a panel
-    int in, low, out;       // what the tile needs beside its products, X's second part, where it goes
+    int in, low, out, out_low;      // what the tile needs beside its products and its second part, where it goes and where that does
     int diag;               // floats to the diagonal that is needed, or that A's and B's own diagonals are put to
     int tall;
 };
@@ -980,7 +991,7 @@ __device__ constexpr uint32_t fp16_descriptor(int columns, bool a_across, bool b
 }
 
 // Tile number t, by the whole warp.
-__device__ __forceinline__ Tile tile_at(const ProductArgs &a, int64_t t)
+template <bool FINE> __device__ __forceinline__ Tile tile_at(const ProductArgs &a, int64_t t)
 {
     Tile r{};
     const int per_step = a.first[3];
@@ -1051,8 +1062,14 @@ __device__ __forceinline__ Tile tile_at(const ProductArgs &a, int64_t t)
     r.width = r.what == 2 ? it.cols : it.side;
     r.pitch = r.height;
     r.in = r.what == 2 ? it.x[turn] : it.gram;
-    r.low = it.low;
+    r.low = r.what == 2 ? it.low[turn] : it.gram_low;
     r.out = r.what == 0 ? it.gram : r.what == 1 ? it.poly : it.x[1 - turn];
+    r.out_low = r.what == 0 ? it.gram_low : r.what == 1 ? it.poly_low : it.low[1 - turn];
+    if constexpr (FINE) {
+        const int of_x = it.low[turn] - it.x[turn], of_poly = it.poly_low - it.poly;
+        r.a_low = r.what == 0 ? of_x : r.what == 1 ? it.gram_low - it.gram : it.tall ? of_x : of_poly;
+        r.b_low = r.what < 2 ? r.a_low : it.tall ? of_poly : of_x;
+    }
     r.diag = it.diag + (r.what == 2 ? it.s_pitch : 0);
     r.tall = it.tall;
     return r;
@@ -1155,7 +1172,8 @@ __device__ __forceinline__ void step_theta(const Item &it, float decay, uint32_t
 }
 
 // A warp that takes tiles out: its place in shared memory and the barrier of what comes there.
-struct Taking {
+template <bool FINE> struct Taking {
+    static constexpr float kLow = FINE ? 1.0f : kScaleLow;
     const ProductArgs &a;
     const CUtensorMap *map;
     uint32_t place, bar;
@@ -1184,9 +1202,10 @@ struct Taking {
             stores_read();
             if (tile.what > 0) {
                 const int y = c / kPanel * tile.pitch + row0;
-                mbar_expect(bar, tile.what == 1 ? kPartBytes : 2 * kPartBytes);
+                const bool low = FINE || tile.what == 2;
+                mbar_expect(bar, low ? 2 * kPartBytes : kPartBytes);
                 load_part(place, map, c % kPanel, tile.in + y, bar);
-                if (tile.what == 2) load_part(place + kPartBytes, map, c % kPanel, tile.low + y, bar);
+                if (low) load_part(place + kPartBytes, map, c % kPanel, tile.low + y, bar);
             }
         }
         __syncwarp();
@@ -1206,14 +1225,20 @@ struct Taking {
     }
     // The diagonal's elements of columns i and i + 1 of a part.
     __device__ __forceinline__ F2 columns(int i) const { return F2(__shfl_sync(0xffffffffu, column, i), __shfl_sync(0xffffffffu, column, i + 1)); }
-    // Sixteen columns of A or B, from the sums in tensor memory (and of what A has there).
+    // Two elements as they are kept: first part, and second.
+    __device__ __forceinline__ void keep(F2 v, uint32_t &h, uint32_t &low) const
+    {
+        h = pack_half(v);
+        if constexpr (FINE) low = pack_half(fma2(halves(h), F2(-1.0f), v));
+    }
+    // Sixteen columns of A or B, from the sums in tensor memory (and of what A has there: h, and fine low).
     __device__ __forceinline__ void square16(const Tile &tile, int row, bool diagonal, float d_row, const float (&raw)[16],
-                                             uint32_t *h, int first) const
+                                             uint32_t *h, uint32_t *low, int first) const
     {
         const int on = (threadIdx.x & 31) - first;              // this row's diagonal element
         if (tile.what == 0) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) h[i] = pack_half(F2(raw[2 * i], raw[2 * i + 1]) * F2(kScaleA / (kScaleX * kScaleX)));
+            for (int i = 0; i < 8; ++i) keep(F2(raw[2 * i], raw[2 * i + 1]) * F2(kScaleA / (kScaleX * kScaleX)), h[i], low[i]);
             if (diagonal && on >= 0 && on < 16) {
                 float mine = 0.0f;
 #pragma unroll
@@ -1236,14 +1261,17 @@ struct Taking {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const F2 d = columns(first + 2 * i);
-                h[i] = pack_half(fma2(F2(raw[2 * i], raw[2 * i + 1]), rest, fma2(d, cd, bd) * halves(h[i])));
+                F2 of_a = halves(h[i]);
+                if constexpr (FINE) of_a = of_a + halves(low[i]);
+                keep(fma2(F2(raw[2 * i], raw[2 * i + 1]), rest, fma2(d, cd, bd) * of_a), h[i], low[i]);
             }
         }
         if (diagonal) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if (2 * i == on) h[i] &= 0xffff0000u;
-                if (2 * i + 1 == on) h[i] &= 0xffffu;
+                const uint32_t mask = 2 * i == on ? 0xffff0000u : 2 * i + 1 == on ? 0xffffu : ~0u;
+                h[i] &= mask;
+                if constexpr (FINE) low[i] &= mask;
             }
         }
     }
@@ -1267,24 +1295,44 @@ struct Taking {
                 __syncwarp();
                 uint32_t h[16];
                 if (tile.what < 2) {
-                    if (tile.what == 1) get_row(place, lane, h);
+                    uint32_t low[16];
+                    if (tile.what == 1) {
+                        get_row(place, lane, h);
+                        if constexpr (FINE) get_row(place + kPartBytes, lane, low);
+                    }
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         float raw[16];
                         tmem_load16(src + 32 * part + 16 * k, raw);
                         // (a warp's 32 x 32 are on the diagonal as a whole, or off)
-                        square16(tile, row, c0 == row0, d_row, raw, h + 8 * k, 16 * k);
+                        square16(tile, row, c0 == row0, d_row, raw, h + 8 * k, low + 8 * k, 16 * k);
                     }
                     // above the diagonal's blocks: the transposed part too
                     const bool mirror = c0 / kBlock > row0 / kBlock;
+                    const int y = c0 / kPanel * tile.pitch + row0, y_across = row0 / kPanel * tile.pitch + c0;
                     put_row(place, lane, h);
-                    if (mirror) put_across(place + kPartBytes, h);
+                    if constexpr (FINE) put_row(place + kPartBytes, lane, low);
+                    else if (mirror) put_across(place + kPartBytes, h);
                     fence_async_shared();
                     __syncwarp();
                     if (lane == 0) {
-                        store_part(map, c0 % kPanel, tile.out + c0 / kPanel * tile.pitch + row0, place);
-                        if (mirror) store_part(map, row0 % kPanel, tile.out + row0 / kPanel * tile.pitch + c0, place + kPartBytes);
+                        store_part(map, c0 % kPanel, tile.out + y, place);
+                        if constexpr (FINE) store_part(map, c0 % kPanel, tile.out_low + y, place + kPartBytes);
+                        else if (mirror) store_part(map, row0 % kPanel, tile.out + y_across, place + kPartBytes);
                         stores_commit();
+                    }
+                    if (FINE && mirror) {               // (both places once more)
+                        if (lane == 0) stores_read();
+                        __syncwarp();
+                        put_across(place, h);
+                        put_across(place + kPartBytes, low);
+                        fence_async_shared();
+                        __syncwarp();
+                        if (lane == 0) {
+                            store_part(map, row0 % kPanel, tile.out + y_across, place);
+                            store_part(map, row0 % kPanel, tile.out_low + y_across, place + kPartBytes);
+                            stores_commit();
+                        }
                     }
                 } else if (!last) {
                     uint32_t low[16];
@@ -1298,7 +1346,7 @@ struct Taking {
                         for (int i = 0; i < 8; ++i) {
                             const F2 v = next_x(tile, 16 * k + 2 * i, F2(raw[2 * i], raw[2 * i + 1]), h[8 * k + i], low[8 * k + i], d_row, ca, full);
                             h[8 * k + i] = pack_half(v);
-                            low[8 * k + i] = pack_half(fma2(halves(h[8 * k + i]), F2(-1.0f), v) * F2(kScaleLow));
+                            low[8 * k + i] = pack_half(fma2(halves(h[8 * k + i]), F2(-1.0f), v) * F2(kLow));
                         }
                     }
                     put_row(place, lane, h);
@@ -1308,7 +1356,7 @@ struct Taking {
                     if (lane == 0) {
                         const int y = c0 / kPanel * tile.pitch + row0;
                         store_part(map, c0 % kPanel, tile.out + y, place);
-                        store_part(map, c0 % kPanel, tile.low + y, place + kPartBytes);
+                        store_part(map, c0 % kPanel, tile.out_low + y, place + kPartBytes);
                         stores_commit();
                     }
                 } else {
@@ -1341,13 +1389,14 @@ struct Taking {
     // Two elements of the next X: a x + d x + (the product's sum), x by its two parts.
     __device__ __forceinline__ F2 next_x(const Tile &tile, int i, F2 sum, uint32_t hi, uint32_t low, float d_row, float ca, bool full) const
     {
-        const F2 p = halves(hi), x = fma2(halves(low), F2(1.0f / kScaleLow), p);
+        const F2 p = halves(hi), x = fma2(halves(low), F2(1.0f / kLow), p);
         F2 d(d_row);
         if (tile.tall) d = columns(i);
-        return fma2(sum, F2(1.0f / kScaleB), fma2(d, full ? x : p, x * F2(ca)));
+        return fma2(sum, F2(1.0f / kScaleB), fma2(d, FINE || full ? x : p, x * F2(ca)));
     }
 };
 
+template <bool FINE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
 novak_orthogonalize_products_kernel(const __grid_constant__ ProductArgs a, const __grid_constant__ CUtensorMap map,
                                     const __grid_constant__ CUtensorMap part_map)
@@ -1407,7 +1456,7 @@ novak_orthogonalize_products_kernel(const __grid_constant__ ProductArgs a, const
     };
     if (warp < kOutWarps) {
         const int group = warp / 4, quarter = warp % 4;
-        Taking taking{a, &part_map, places + warp * kPlaceBytes, smem_addr(&sh.part_full[warp]), 0, false, 0, 0, false, 0, 0, 0, 0.0f, 0.0f};
+        Taking<FINE> taking{a, &part_map, places + warp * kPlaceBytes, smem_addr(&sh.part_full[warp]), 0, false, 0, 0, false, 0, 0, 0, 0.0f, 0.0f};
         for (uint32_t count = 0;; ++count) {
             const uint32_t buf = count & 1, ready = smem_addr(&sh.ready[ring.slot]);
             // (nobody waits longer than need be for what is stored)
@@ -1463,9 +1512,18 @@ novak_orthogonalize_products_kernel(const __grid_constant__ ProductArgs a, const
                 // (what other SMs have stored is there for tensor copies, this warp's and those of the warps that wait for `ready`)
                 asm volatile("fence.proxy.async;" ::: "memory");
                 if (ok) mbar_arrive(ready);
-                const int boxes = tile.columns / 128;
+                const int boxes = tile.columns / 128, all = (FINE ? 3 : 1) * tile.steps;
                 int ya = tile.a + static_cast<int>(rank) * tile.a_rank, yb = tile.b + static_cast<int>(rank) * tile.b_rank;
-                for (int i = 0; ok && i < tile.steps; ++i, ya += tile.a_step, yb += tile.b_step) {
+                for (int i = 0; ok && i < all; ++i, ya += tile.a_step, yb += tile.b_step) {
+                    // fine: first parts, then the first by the second, then the second by the first
+                    if (FINE && i == tile.steps) {
+                        ya -= tile.steps * tile.a_step;
+                        yb += tile.b_low - tile.steps * tile.b_step;
+                    }
+                    if (FINE && i == 2 * tile.steps) {
+                        ya += tile.a_low - tile.steps * tile.a_step;
+                        yb -= tile.b_low + tile.steps * tile.b_step;
+                    }
                     ok = mbar_wait(smem_addr(&sh.empty[at.slot]), at.phase ^ 1, a.wait_ns);
                     if (!ok) break;
                     const uint32_t bar = full0 + at.slot * 8, dst = stages + at.slot * kStageBytes;
@@ -1476,7 +1534,7 @@ novak_orthogonalize_products_kernel(const __grid_constant__ ProductArgs a, const
                     if (boxes == 2) load_box(dst + 3 * kBoxBytes, &map, yb + tile.b_half, bar);
                     at.advance();
                     ++issued;
-                    if (rank == 0 && i == max(tile.steps - 12, 0)) mbar_arrive(smem_addr(&sh.want));
+                    if (rank == 0 && i == max(all - 12, 0)) mbar_arrive(smem_addr(&sh.want));
                 }
                 if (!ok) gave_up(a);
             }
@@ -1503,7 +1561,8 @@ novak_orthogonalize_products_kernel(const __grid_constant__ ProductArgs a, const
             const uint64_t a0 = operand_desc(stages, kBoxBytes, 1024), b0 = operand_desc(stages + 2 * kBoxBytes, kBoxBytes, 1024);
             ok = mbar_wait_warp(smem_addr(&sh.out_empty[buf]), ((count >> 1) & 1) ^ 1, a.wait_ns);
             tcgen05_after_sync();
-            for (int i = 0; ok && i < tile.steps; ++i) {
+            const int all = (FINE ? 3 : 1) * tile.steps;
+            for (int i = 0; ok && i < all; ++i) {
                 ok = mbar_wait_warp(smem_addr(&sh.full[at.slot]), at.phase, a.wait_ns);
                 if (!ok) break;
                 tcgen05_after_sync();
@@ -1512,7 +1571,7 @@ novak_orthogonalize_products_kernel(const __grid_constant__ ProductArgs a, const
 #pragma unroll
                     for (int k = 0; k < 4; ++k) mma_pair_bf16(d, a_at + k * a_next, b_at + k * b_next, tile.descriptor, i > 0 || k > 0);
                     mma_commit_pair(smem_addr(&sh.empty[at.slot]));
-                    if (i == tile.steps - 1) mma_commit_pair(smem_addr(&sh.out_full[buf]));
+                    if (i == all - 1) mma_commit_pair(smem_addr(&sh.out_full[buf]));
                 }
                 __syncwarp();
                 at.advance();
@@ -1538,7 +1597,7 @@ novak_orthogonalize_products_kernel(const __grid_constant__ ProductArgs a, const
             t = __shfl_sync(0xffffffffu, t, 0);
             more = t < all;
             Tile tile{};
-            if (more) tile = tile_at(a, t);
+            if (more) tile = tile_at<FINE>(a, t);
             else tile.what = -1;
             if (!mbar_wait_warp(smem_addr(&sh.tile_empty[ring.slot]), ring.phase ^ 1, a.wait_ns)) {
                 ok = false;
@@ -1607,21 +1666,21 @@ static bool placed(int64_t rows, int64_t cols, bool all) { return rows > 0 && co
 // What a matrix comes to does not depend on its group.  (Groups' ends cost the last tiles of 15 products each, about 1 %: 24 of
 // 4096 x 4096 in groups of six 31 ms.)  false: more than can be addressed.
 constexpr size_t kGroupBytes = size_t(1) << 30;
-template <typename F> bool for_groups(const int64_t *rows, const int64_t *cols, int n, bool all, const F &f)
+template <typename F> bool for_groups(const int64_t *rows, const int64_t *cols, int n, bool fine, bool all, const F &f)
 {
     Layout total, l;
     Item it{};
     int first = 0, count = 0;
     for (int i = 0; i < n; ++i) {
         if (!placed(rows[i], cols[i], all)) continue;
-        if (!place(total, rows[i], cols[i], it)) return false;
+        if (!place(total, rows[i], cols[i], fine, it)) return false;
         Layout longer = l;
-        place(longer, rows[i], cols[i], it);
+        place(longer, rows[i], cols[i], fine, it);
         finish_layout(longer, count + 1);
         if (count > 0 && longer.bytes > kGroupBytes) {
             f(first, i, l.bytes);
             longer = Layout();
-            place(longer, rows[i], cols[i], it);
+            place(longer, rows[i], cols[i], fine, it);
             finish_layout(longer, 1);
             first = i;
             count = 0;
@@ -1633,10 +1692,10 @@ template <typename F> bool for_groups(const int64_t *rows, const int64_t *cols, 
     return true;
 }
 
-size_t orthogonalize_bytes(const int64_t *rows, const int64_t *cols, int n, bool all)
+size_t orthogonalize_bytes(const int64_t *rows, const int64_t *cols, int n, bool fine, bool all)
 {
     size_t most = 0;
-    if (!for_groups(rows, cols, n, all, [&](int, int, size_t bytes) { most = std::max(most, bytes); })) return 0;
+    if (!for_groups(rows, cols, n, fine, all, [&](int, int, size_t bytes) { most = std::max(most, bytes); })) return 0;
     for (int i = 0; i < n && most == 0; ++i)
         if (rows[i] > 0 && cols[i] > 0) most = kLeastBytes;
     return most;
@@ -1667,7 +1726,7 @@ cudaError_t launch_orthogonalize(const OrthArgs &a, cudaStream_t stream)
     if (!all) e = f32 ? launch_small<0, 1>(a, small, stream) : launch_small<1, 1>(a, small, stream);
     if (!all && e == cudaSuccess) e = f32 ? launch_small<0, kSmallCluster>(a, small, stream) : launch_small<1, kSmallCluster>(a, small, stream);
     int64_t withheld = a.withheld;
-    for_groups(a.rows, a.cols, a.n, all, [&](int begin, int end, size_t) {
+    for_groups(a.rows, a.cols, a.n, a.fine, all, [&](int begin, int end, size_t) {
         int64_t tiles = 0;
         if (e == cudaSuccess) e = launch_group(a, begin, end, withheld, tiles, stream);
         withheld = withheld >= tiles ? withheld - tiles : -1;
@@ -1687,7 +1746,7 @@ static cudaError_t launch_group(const OrthArgs &a, int begin, int end, int64_t w
     int64_t tiles[3][2] = {};           // of a step, by product: of 256 columns, and of 128
     for (int i = begin; i < end; ++i)
         if (here(i)) {
-            place(l, a.rows[i], a.cols[i], it);
+            place(l, a.rows[i], a.cols[i], a.fine, it);
             for (int what = 0; what < 3; ++what)
                 for (int narrow = 0; narrow < 2; ++narrow) tiles[what][narrow] += tiles_of(it, what, narrow ? 128 : 256);
             ++n;
@@ -1728,7 +1787,7 @@ static cudaError_t launch_group(const OrthArgs &a, int begin, int end, int64_t w
     };
     for (int i = begin; i < end && e == cudaSuccess; ++i) {
         if (!here(i)) continue;
-        place(again, a.rows[i], a.cols[i], it);
+        place(again, a.rows[i], a.cols[i], a.fine, it);
         it.g = a.g[i];
         it.out = a.out ? a.out[i] : a.theta[i];
         it.m = a.m ? a.m[i] : nullptr;
@@ -1746,7 +1805,7 @@ static cudaError_t launch_group(const OrthArgs &a, int begin, int end, int64_t w
     if (e == cudaSuccess && count > 0) e = send();
     if (e == cudaSuccess)
         e = launch(f32 ? novak_orthogonalize_start_kernel<0> : novak_orthogonalize_start_kernel<1>, 
-                   dim3(static_cast<unsigned>(std::min<int64_t>(l.units, 148 * 4))), kThreads, 0, stream, w, n, l.units, mo, static_cast<float>(a.eps));
+                   dim3(static_cast<unsigned>(std::min<int64_t>(l.units, 148 * 4))), kThreads, 0, stream, w, n, l.units, mo, static_cast<float>(a.eps), a.fine ? 1.0f : kScaleLow);
     if (e != cudaSuccess) return e;
 
     for (int k = 0; k < a.steps; ++k)
@@ -1769,10 +1828,11 @@ static cudaError_t launch_group(const OrthArgs &a, int begin, int end, int64_t w
     if (encode(&part_map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, dims, strides, part_box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return cudaErrorInvalidValue;
-    static std::atomic<uint64_t> asked{0};
-    e = ask_shared_memory(novak_orthogonalize_products_kernel, kSmemBytes, asked);
+    static std::atomic<uint64_t> asked[2] = {};
+    const auto kernel = a.fine ? novak_orthogonalize_products_kernel<true> : novak_orthogonalize_products_kernel<false>;
+    e = ask_shared_memory(kernel, kSmemBytes, asked[a.fine]);
     if (e != cudaSuccess) return e;
-    return launch(novak_orthogonalize_products_kernel, dim3(static_cast<unsigned>(2 * std::min<int64_t>(kPairs, most))), kTcThreads, kSmemBytes,
+    return launch(kernel, dim3(static_cast<unsigned>(2 * std::min<int64_t>(kPairs, most))), kTcThreads, kSmemBytes,
                   stream, p, map, part_map);
 }
 

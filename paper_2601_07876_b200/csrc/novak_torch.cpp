@@ -149,7 +149,8 @@ Tensor new_like(const Tensor &t) { return at::empty(t.sizes(), t.options()); }
     X(novak_layer_norm_backward) X(novak_activation) X(novak_activation_backward) X(novak_linear_weight_grad_bytes)    \
     X(novak_linear_weight_grad) X(novak_rms_norm) X(novak_rms_norm_backward_bytes) X(novak_rms_norm_backward)          \
     X(novak_embedding) X(novak_embedding_grad_bytes) X(novak_embedding_grad) X(novak_orthogonalize_bytes)              \
-    X(novak_orthogonalize) X(novak_orthogonal_step) X(novak_ops_error)
+    X(novak_orthogonalize) X(novak_orthogonal_step) X(novak_orthogonalize_fine_bytes) X(novak_orthogonalize_fine)      \
+    X(novak_orthogonal_step_fine) X(novak_ops_error)
 struct Api {
 #define X(f) decltype(&::f) f = nullptr;
     NOVAK_ENTRIES(X)
@@ -575,7 +576,7 @@ struct Matrices {
     }
 };
 
-// orthogonalize(list, coefficients, eps) -> list
+// orthogonalize(list, coefficients, eps, fine) -> list
 PyObject *orthogonalize(PyObject *const *args)
 {
     const Tensors list(args[0], "a list of tensors is needed");
@@ -599,15 +600,17 @@ PyObject *orthogonalize(PyObject *const *args)
     const int n = g.count();
     if (n > 0) {
         const Tensor &on = list.at(0, "a matrix");
-        const size_t need = api.novak_orthogonalize_bytes(g.rows.data(), g.cols.data(), n);
+        const bool fine = truth(args[3]);
+        const size_t need = (fine ? api.novak_orthogonalize_fine_bytes : api.novak_orthogonalize_bytes)(g.rows.data(), g.cols.data(), n);
         const Tensor work = at::empty({static_cast<int64_t>(need)}, on.options().dtype(at::kByte));
-        ENQUEUE(novak_orthogonalize, on, g.ptr.data(), g.stride.data(), type, out.ptr.data(), out.stride.data(), g.rows.data(),
-                g.cols.data(), n, abc.data(), static_cast<int>(abc.size() / 3), eps, work.data_ptr(), need);
+        enqueue(fine ? api.novak_orthogonalize_fine : api.novak_orthogonalize, fine ? "novak_orthogonalize_fine" : "novak_orthogonalize", on,
+                g.ptr.data(), g.stride.data(), type, out.ptr.data(), out.stride.data(), g.rows.data(), g.cols.data(), n, abc.data(),
+                static_cast<int>(abc.size() / 3), eps, work.data_ptr(), need);
     }
     return result.release();
 }
 
-// orthogonal_step(parameters, gradients, momenta, momentum, nesterov, steps, decay, coefficients, eps)
+// orthogonal_step(parameters, gradients, momenta, momentum, nesterov, steps, decay, coefficients, eps, fine)
 PyObject *orthogonal_step(PyObject *const *args)
 {
     const Tensors params(args[0], "a list of parameters is needed"), grads(args[1], "a list of gradients is needed"),
@@ -641,9 +644,11 @@ PyObject *orthogonal_step(PyObject *const *args)
     const int n = theta.count();
     if (n > 0) {
         const Tensor &on = params.at(0, "a parameter");
-        const size_t need = api.novak_orthogonalize_bytes(theta.rows.data(), theta.cols.data(), n);
+        const bool fine = truth(args[9]);
+        const size_t need = (fine ? api.novak_orthogonalize_fine_bytes : api.novak_orthogonalize_bytes)(theta.rows.data(), theta.cols.data(), n);
         const Tensor work = at::empty({static_cast<int64_t>(need)}, on.options().dtype(at::kByte));
-        ENQUEUE(novak_orthogonal_step, on, reinterpret_cast<float *const *>(theta.ptr.data()), g.ptr.data(), type,
+        enqueue(fine ? api.novak_orthogonal_step_fine : api.novak_orthogonal_step,
+                fine ? "novak_orthogonal_step_fine" : "novak_orthogonal_step", on, reinterpret_cast<float *const *>(theta.ptr.data()), g.ptr.data(), type,
                 reinterpret_cast<float *const *>(m.ptr.data()), theta.rows.data(), theta.cols.data(), n, momentum,
                 static_cast<int>(truth(args[4])), step.data(), decay, abc.data(), static_cast<int>(abc.size() / 3), eps,
                 work.data_ptr(), need);
@@ -675,7 +680,7 @@ template <PyObject *(*F)(PyObject *const *), int N> PyMethodDef def(const char *
 }
 
 PyMethodDef methods[] = {
-    def<bind, 20>("bind"),
+    def<bind, 23>("bind"),
     def<pack, 1>("pack"),
     def<unpack, 2>("unpack"),
     def<layer_norm, 5>("layer_norm"),
@@ -687,8 +692,8 @@ PyMethodDef methods[] = {
     def<rms_norm_backward, 7>("rms_norm_backward"),
     def<embedding, 4>("embedding"),
     def<embedding_grad, 6>("embedding_grad"),
-    def<orthogonalize, 3>("orthogonalize"),
-    def<orthogonal_step, 9>("orthogonal_step"),
+    def<orthogonalize, 4>("orthogonalize"),
+    def<orthogonal_step, 10>("orthogonal_step"),
     {nullptr, nullptr, 0, nullptr},
 };
 

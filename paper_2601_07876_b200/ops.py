@@ -28,7 +28,7 @@ _ENTRIES = ("novak_act8_pack", "novak_act8_unpack", "novak_layer_norm", "novak_l
             "novak_linear_weight_grad_bytes", "novak_linear_weight_grad", "novak_rms_norm",
             "novak_rms_norm_backward_bytes", "novak_rms_norm_backward", "novak_embedding", "novak_embedding_grad_bytes",
             "novak_embedding_grad", "novak_orthogonalize_bytes", "novak_orthogonalize", "novak_orthogonal_step",
-            "novak_ops_error")
+            "novak_orthogonalize_fine_bytes", "novak_orthogonalize_fine", "novak_orthogonal_step_fine", "novak_ops_error")
 
 # The triples (a, b, c) of five Newton-Schulz steps that bring singular values above 1e-3 of the
 # largest to between 0.7 and 1.2 (those of the Muon optimiser).
@@ -226,24 +226,27 @@ def _flat(coefficients):
     return flat
 
 
-def orthogonalize(matrices, coefficients=NEWTON_SCHULZ, eps: float = 1e-7):
+def orthogonalize(matrices, coefficients=NEWTON_SCHULZ, eps: float = 1e-7, fine: bool = False):
     """Matrices brought close to orthogonal (their singular values close to 1) by Newton-Schulz
     products, as new bfloat16 tensors: X = G / max(|G|, eps), then X <- a X + (b A + c A^2) X
     with A = X X^T for each (a, b, c) of ``coefficients``.  ``matrices`` is a tensor or a list of
     tensors of one dtype (float32 or bfloat16), which are worked on together; one of more than two
-    dimensions is a batch of matrices.  See include/novak.h for what is held in how many bits."""
+    dimensions is a batch of matrices.  Matrices that are not small (include/novak.h) go through products of
+    fp16 operands, 1e-4 to 1e-3 off for dense matrices and up to 1e-2 where a few elements carry all; with
+    ``fine`` operands are of two parts, as the small ones' always are, which makes that 3e-6 to 3e-5, and takes
+    two to three times as long."""
     if isinstance(matrices, torch.Tensor):
-        return _calls.orthogonalize((matrices,), _flat(coefficients), eps)[0]
-    return _calls.orthogonalize(matrices, _flat(coefficients), eps)
+        return _calls.orthogonalize((matrices,), _flat(coefficients), eps, fine)[0]
+    return _calls.orthogonalize(matrices, _flat(coefficients), eps, fine)
 
 
 def orthogonal_step(params, grads, momenta, steps, momentum: float = 0.95, nesterov: bool = True, decay: float = 1.0,
-                    coefficients=NEWTON_SCHULZ, eps: float = 1e-7):
+                    coefficients=NEWTON_SCHULZ, eps: float = 1e-7, fine: bool = False):
     """In place, for each matrix: m <- momentum m + g, G = g + momentum m (``nesterov``) or m,
-    theta <- decay theta - step X, X the orthogonalised G.  ``params`` and ``momenta`` are
+    theta <- decay theta - step X, X the orthogonalised G (``fine``: see ``orthogonalize``).  ``params`` and ``momenta`` are
     contiguous float32 tensors, none of them twice, ``grads`` of one dtype, ``steps`` one number each.
     To autograd they have changed: it refuses to go back through what was computed from them before."""
-    _calls.orthogonal_step(params, grads, momenta, momentum, nesterov, steps, decay, _flat(coefficients), eps)
+    _calls.orthogonal_step(params, grads, momenta, momentum, nesterov, steps, decay, _flat(coefficients), eps, fine)
 
 
 def _kind(kind) -> int:

@@ -150,14 +150,15 @@ class Muon(torch.optim.Optimizer):
 
     Parameters are contiguous and of two dimensions or more; one of more is a batch of matrices
     (its last two dimensions each).  Parameters without a gradient are left alone.  Gradients of
-    one group are of one dtype (float32 or bfloat16)."""
+    one group are of one dtype (float32 or bfloat16).  ``fine``: operands of two fp16 parts,
+    two to three times as long (``ops.orthogonalize``)."""
 
     def __init__(self, params, lr=2e-2, momentum=0.95, weight_decay=0.0, *, nesterov=True, scale="spectral",
-                 coefficients=ops.NEWTON_SCHULZ, eps=1e-7):
+                 coefficients=ops.NEWTON_SCHULZ, eps=1e-7, fine=False):
         if scale not in ("spectral", "rms"):
             raise ValueError(f"scale must be 'spectral' or 'rms', got {scale!r}")
         super().__init__(params, dict(lr=lr, momentum=momentum, weight_decay=weight_decay, nesterov=nesterov, scale=scale,
-                                      coefficients=tuple(tuple(c) for c in coefficients), eps=eps))
+                                      coefficients=tuple(tuple(c) for c in coefficients), eps=eps, fine=fine))
 
     def add_param_group(self, param_group):
         super().add_param_group(param_group)
@@ -183,7 +184,7 @@ class Muon(torch.optim.Optimizer):
             ops.orthogonal_step(params, [p.grad if p.grad.is_contiguous() else p.grad.contiguous() for p in params],
                                 [self.state[p]["momentum"] for p in params], steps, momentum=group["momentum"],
                                 nesterov=group["nesterov"], decay=1.0 - group["lr"] * group["weight_decay"],
-                                coefficients=group["coefficients"], eps=group["eps"])
+                                coefficients=group["coefficients"], eps=group["eps"], fine=group.get("fine", False))
         return loss
 
 

@@ -33,3 +33,11 @@ def test_many_matrices_go_through_one_workspace_in_groups(lib):
     assert ask(lib, *[(4096, 4096)] * 3) > 2.9 * one
     huge = ask(lib, (65536, 16384))                     # too large for a group of the usual size: one of its own
     assert ask(lib, *[(4096, 4096)] * 30, (65536, 16384), *[(4096, 4096)] * 30) == huge > 1 << 30
+
+
+def test_operands_of_two_parts_take_more(lib):
+    def fine(*shapes):
+        return lib.novak_orthogonalize_fine_bytes(sizes(*(r for r, _ in shapes)), sizes(*(c for _, c in shapes)), len(shapes))
+    assert 16 * 4096 ** 2 <= fine((4096, 4096)) < 16.2 * 4096 ** 2
+    assert fine((64, 64)) == ask(lib, (64, 64)) and fine() == 0 and fine(*[(4096, 4096)] * 24) <= 1 << 30
+    assert fine((65536 + 1, 4)) == 0

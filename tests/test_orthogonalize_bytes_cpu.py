@@ -2,7 +2,7 @@
 import pytest
 
 from paper_2601_07876_b200 import binding as B
-from test_stream_ops_cpu import sizes
+from test_stream_ops_cpu import MUON, P, doubles, pointers, sizes
 
 
 @pytest.fixture(scope="module")
@@ -41,3 +41,14 @@ def test_operands_of_two_parts_take_more(lib):
     assert 16 * 4096 ** 2 <= fine((4096, 4096)) < 16.2 * 4096 ** 2
     assert fine((64, 64)) == ask(lib, (64, 64)) and fine() == 0 and fine(*[(4096, 4096)] * 24) <= 1 << 30
     assert fine((65536 + 1, 4)) == 0
+
+
+@pytest.mark.parametrize("change", [dict(work=None), dict(bytes=1000), dict(type=2), dict(n=-1), dict(steps=0), dict(eps=-1.0)])
+def test_refusals_with_operands_of_two_parts(lib, change):
+    base = dict(g=pointers(P, P), gs=sizes(9, 9), type=0, out=pointers(P, P), os=sizes(9, 9), rows=sizes(4, 5), cols=sizes(9, 9), n=2,
+                abc=doubles(*MUON), steps=1, eps=1e-7, work=P, bytes=1 << 40, stream=None)
+    assert lib.novak_orthogonalize_fine(*{**base, **change}.values()) == B.NOVAK_EINVAL and lib.novak_ops_error()
+    change = {k: v for k, v in change.items() if k != "n"} or dict(n=-1)
+    base = dict(theta=pointers(P), g=pointers(P), type=0, m=pointers(P), rows=sizes(4), cols=sizes(9), n=1, momentum=0.9, nesterov=1,
+                step=doubles(0.1), decay=1.0, abc=doubles(*MUON), steps=1, eps=1e-7, work=P, bytes=1 << 40, stream=None)
+    assert lib.novak_orthogonal_step_fine(*{**base, **change}.values()) == B.NOVAK_EINVAL       # (theta and m are one, too)

@@ -812,7 +812,7 @@ int novak_embedding(const void *d_ids, int id_type, const void *d_table, int64_t
  * that no id names being zeros; with `add` not 0 that sum is added to what dtable
  * holds (in fp32, rounded once), and rows that no id names stay as they are.  dout
  * of `type`, dtable of grad_type.  Tokens of one id are summed in fp32 in an order that
- * goes by their places alone.  d_work: novak_embedding_grad_bytes(tokens, vocab,
+ * goes by their places alone.  dtable may not overlap dout.  d_work: novak_embedding_grad_bytes(tokens, vocab,
  * cols) bytes, 256-byte aligned; its contents need not be anything and are nothing
  * afterwards. */
 size_t novak_embedding_grad_bytes(int64_t tokens, int64_t vocab, int64_t cols);
